@@ -288,6 +288,125 @@ detox_status detox_aggregate(const detox_pipeline_desc* desc, const float* X, in
                              size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * The worker's side (Algorithm 1 lets a worker compute its gradient by any program; the paper fixes none): operators of
+ * a pre-norm gated feed-forward sublayer,
+ *     s = x + residual,   y = rmsnorm(s),   h = act(y Wg^T) * (y Wu^T),
+ * with their backward passes and with the 8-bit form in which activations are kept between the two.  The vote compares
+ * gradients bit for bit, so all of them add in a fixed order (no floating-point atomics): the same inputs give the same
+ * bits in every call on every GPU of the kind.
+ *
+ *   - Matrices are row-major with a row stride in ELEMENTS (>= columns); a row is a token.  Sums, norms and products are
+ *     accumulated in fp32, and every output is rounded once.
+ *   - 16-byte aligned bases and strides take the vectorised paths (for the products: TMA); any other layout gives the same results
+ *     more slowly (for the products through aligned copies in the workspace).
+ *   - Zero rows are accepted: nothing is written but the weight gradients, which are zero.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum {
+    DETOX_DTYPE_FLOAT = 0,
+    DETOX_DTYPE_HALF = 1,
+    DETOX_DTYPE_BFLOAT = 2
+} detox_dtype;
+
+typedef enum {
+    DETOX_ACT_SILU = 0,         /* g / (1 + exp(-g)) */
+    DETOX_ACT_GELU = 1,         /* g (1 + erf(g / sqrt 2)) / 2 */
+    DETOX_ACT_RELU = 2          /* max(g, 0); derivative 0 at 0 */
+} detox_act;
+
+/* ---------------------------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits.  Every block of DETOX_KEEP_BLOCK columns of a row (the last may be shorter) shares a
+ * power-of-two scale 2^e, e the smallest integer with amax <= 448 * 2^e (amax over the block's finite entries, e >= -126);
+ * an entry v is kept as the e4m3 number nearest to v * 2^-e (ties to even).  Inf and NaN are kept as NaN.  The scales
+ * being powers of two, taking a value out again is exact in fp32, and in bf16 and fp16 for values that they hold.
+ *
+ *   X  dev, rows x ld     dtype FLOAT, HALF or BFLOAT
+ *   Q  dev, rows x ldq    out: e4m3 numbers, one byte each
+ *   E  dev, rows x lde    out: biased exponents e + 127 (the E8M0 format), ceil(cols / DETOX_KEEP_BLOCK) a row
+ * detox_checkpoint_unpack is the way back: X[r][c] = Q[r][c] * 2^e, rounded to dtype (fp16: clamped to +-65504).
+ * ------------------------------------------------------------------------------------------- */
+#define DETOX_KEEP_BLOCK 128
+detox_status detox_checkpoint_pack(int dtype, const void* X, int64_t ld, int64_t rows, int64_t cols, uint8_t* Q, int64_t ldq,
+                                   uint8_t* E, int64_t lde, void* stream);
+detox_status detox_checkpoint_unpack(int dtype, const uint8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t rows,
+                                     int64_t cols, void* X, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Root-mean-square norm with the residual's addition:
+ *     s = x + residual,   rstd = 1 / sqrt(mean(s^2) + eps),   y = s * rstd * w      (the norm is of s before its rounding)
+ *
+ *   X, R   dev, rows x ldx / ldr    input, residual (NULL: none); same dtype as w and the outputs
+ *   w      dev, cols                weight
+ *   S      dev, rows x lds          out: the sum; NULL when not wanted.  May be X or R itself (same base and stride)
+ *   Y      dev, rows x ldy          out: the normed rows; may be NULL
+ *   Q, E   dev                      out: the normed rows in the 8-bit form above (taken from fp32); both may be NULL
+ *   rstd   dev, rows (fp32)         out: for the backward pass; may be NULL
+ * At least one of S, Y, Q, rstd is given.  eps >= 0.  No workspace.
+ * ------------------------------------------------------------------------------------------- */
+detox_status detox_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w, int64_t rows,
+                           int64_t cols, float eps, void* S, int64_t lds, void* Y, int64_t ldy, uint8_t* Q, int64_t ldq,
+                           uint8_t* E, int64_t lde, float* rstd, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Its backward pass.  With hat = S * rstd:
+ *     dx = dS + rstd * (w dY - hat * mean(w dY hat))      (also the gradient of the residual)
+ *     dw = sum over the rows of dY * hat
+ *   dY   dev, rows x lddy       gradient of the normed rows
+ *   dS   dev, rows x ldds       gradient that reaches the sum by its other uses (NULL: none)
+ *   S    dev, rows x lds        the forward pass's sum (its x when there was no residual); rstd as it left it
+ *   dX   dev, rows x lddx       out; may be dY or dS itself (same base and stride).  NULL: only dw
+ *   dw   dev, cols (fp32)       out.  NULL: only dX
+ *   ws   detox_rmsnorm_backward_workspace_bytes(rows, cols) bytes
+ * ------------------------------------------------------------------------------------------- */
+size_t detox_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+detox_status detox_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, const void* dS, int64_t ldds, const void* S,
+                                    int64_t lds, const void* w, const float* rstd, int64_t rows, int64_t cols, void* dX,
+                                    int64_t lddx, float* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Gated pair of projections: h = act(g) * u with g = x Wg^T, u = x Wu^T in one kernel (g and u stay fp32 and are never
+ * stored in full), and its backward pass
+ *     dg = dh * u * act'(g),   du = dh * act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
+ * dg and du are rounded to dtype, the type the tensor cores multiply; every sum over them is fp32.
+ *
+ * The input is X, or its 8-bit form XQ, XE (X = NULL).  With the kept buffers (all four or none) detox_gated leaves g and
+ * u there in the 8-bit form, and detox_gated_backward reads them; without them it computes g and u again from the input.
+ *
+ *   H    dev, tokens x ldh      out
+ *   dH   dev, tokens x lddh     gradient of h
+ *   dX   dev, tokens x lddx     out; may be NULL
+ *   dWg, dWu  dev, hidden x lddw   out, dtype `dw_dtype`: the descriptor's, or DETOX_DTYPE_FLOAT (then they can be
+ *                               pieces of a row of the matrix that the vote reads); both may be NULL
+ *   ws   detox_gated_workspace_bytes(desc) / detox_gated_backward_workspace_bytes(desc) bytes; its first int32 is the
+ *        device status word (see "Errors" above)
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t dtype;               /* detox_dtype: HALF or BFLOAT */
+    int32_t act;                 /* detox_act */
+    int64_t tokens, in_dim, hidden;
+    const void* X;               /* dev, tokens x ldx; or NULL */
+    int64_t ldx;
+    const uint8_t* XQ;           /* dev, tokens x ldxq: used when X is NULL */
+    int64_t ldxq;
+    const uint8_t* XE;           /* dev, tokens x ldxe */
+    int64_t ldxe;
+    const void* Wg;              /* dev, hidden x ldwg */
+    int64_t ldwg;
+    const void* Wu;              /* dev, hidden x ldwu */
+    int64_t ldwu;
+    uint8_t* GQ;                 /* kept g: dev, tokens x ldq; or NULL */
+    uint8_t* GE;                 /*         dev, tokens x lde */
+    uint8_t* UQ;                 /* kept u, same strides */
+    uint8_t* UE;
+    int64_t ldq, lde;
+} detox_gated_desc;
+
+size_t detox_gated_workspace_bytes(const detox_gated_desc* desc);
+detox_status detox_gated(const detox_gated_desc* desc, void* H, int64_t ldh, void* ws, size_t ws_bytes, void* stream);
+size_t detox_gated_backward_workspace_bytes(const detox_gated_desc* desc);
+detox_status detox_gated_backward(const detox_gated_desc* desc, const void* dH, int64_t lddh, void* dX, int64_t lddx,
+                                  void* dWg, void* dWu, int64_t lddw, int dw_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Self-test of the bounded device-side waits (no counterpart in the paper; a diagnostic).  Launches one
  * warp that waits, with the same wait routine the distance kernels use, on a barrier that nothing will
  * ever complete, for at most `limit_cycles` SM clocks (1 .. 2e9).  The wait must give up by itself: after

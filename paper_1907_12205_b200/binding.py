@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -27,6 +27,9 @@ EXPORTS = (
     "agg_bulyan_workspace_bytes", "agg_bulyan", "detox_aggregate_workspace_bytes", "detox_aggregate",
     "detox_selftest_bounded_wait", "agg_pairwise_sqdist_workspace_bytes", "agg_pairwise_sqdist",
     "detox_kernel_launch_count", "detox_vote_hier_mean_many", "detox_tc_split_mode", "detox_tc_repeated_passes",
+    "detox_checkpoint_pack", "detox_checkpoint_unpack", "detox_rmsnorm", "detox_rmsnorm_backward_workspace_bytes",
+    "detox_rmsnorm_backward", "detox_gated_workspace_bytes", "detox_gated", "detox_gated_backward_workspace_bytes",
+    "detox_gated_backward",
 )
 
 
@@ -44,6 +47,18 @@ class PipelineDesc(ctypes.Structure):
         ("set_offsets", ctypes.POINTER(ctypes.c_int32)), ("set_members", ctypes.POINTER(ctypes.c_int32)),
         ("a1", ctypes.c_int32), ("f", ctypes.c_int32), ("m_sel", ctypes.c_int32),
         ("gm_iters", ctypes.c_int32), ("gm_eps", ctypes.c_float),
+    ]
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+        ("tokens", ctypes.c_int64), ("in_dim", ctypes.c_int64), ("hidden", ctypes.c_int64),
+        ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+        ("XQ", ctypes.c_void_p), ("ldxq", ctypes.c_int64), ("XE", ctypes.c_void_p), ("ldxe", ctypes.c_int64),
+        ("Wg", ctypes.c_void_p), ("ldwg", ctypes.c_int64), ("Wu", ctypes.c_void_p), ("ldwu", ctypes.c_int64),
+        ("GQ", ctypes.c_void_p), ("GE", ctypes.c_void_p), ("UQ", ctypes.c_void_p), ("UE", ctypes.c_void_p),
+        ("ldq", ctypes.c_int64), ("lde", ctypes.c_int64),
     ]
 
 
@@ -95,6 +110,20 @@ def load() -> ctypes.CDLL:
     lib.detox_tc_repeated_passes.argtypes = []
     lib.detox_kernel_launch_count.restype = ctypes.c_ulonglong
     lib.detox_kernel_launch_count.argtypes = []
+    lib.detox_checkpoint_pack.argtypes = [_int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
+    lib.detox_checkpoint_unpack.argtypes = [_int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp]
+    lib.detox_rmsnorm.argtypes = [_int, _vp, _i64, _vp, _i64, _vp, _i64, _i64, ctypes.c_float, _vp, _i64, _vp, _i64, _vp,
+                                  _i64, _vp, _i64, _vp, _vp]
+    lib.detox_rmsnorm_backward_workspace_bytes.restype = _sz
+    lib.detox_rmsnorm_backward_workspace_bytes.argtypes = [_i64, _i64]
+    lib.detox_rmsnorm_backward.argtypes = [_int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _vp,
+                                           _sz, _vp]
+    for name in ("detox_gated", "detox_gated_backward"):
+        fn = getattr(lib, name + "_workspace_bytes")
+        fn.restype = _sz
+        fn.argtypes = [ctypes.POINTER(GatedDesc)]
+    lib.detox_gated.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _sz, _vp]
+    lib.detox_gated_backward.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _i64, _vp, _vp, _i64, _int, _vp, _sz, _vp]
     _lib = lib
     return lib
 
@@ -454,3 +483,240 @@ def detox_aggregate(pipe: Pipeline, X, out: Optional[torch.Tensor] = None, winne
     _check(lib.detox_aggregate(ctypes.byref(pipe.desc), xp, ld, out.data_ptr(), winner.data_ptr(), _ptr(sel),
                                _ptr(sel_workers), wp, wb, _stream(stream)), "detox_aggregate")
     return dict(out=out, winner=winner, sel=sel, sel_workers=sel_workers)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# The worker's side: norm, 8-bit checkpoints, gated projections.
+
+DTYPE_FLOAT, DTYPE_HALF, DTYPE_BFLOAT = range(3)
+ACT_SILU, ACT_GELU, ACT_RELU = range(3)
+KEEP_BLOCK = 128
+_DTYPE = {torch.float32: DTYPE_FLOAT, torch.float16: DTYPE_HALF, torch.bfloat16: DTYPE_BFLOAT}
+
+
+class RmsNorm(NamedTuple):
+    """What detox_rmsnorm leaves; None where it was not asked for."""
+    sum: Optional[torch.Tensor]
+    y: Optional[torch.Tensor]
+    q: Optional[torch.Tensor]
+    e: Optional[torch.Tensor]
+    rstd: torch.Tensor
+
+
+class Kept(NamedTuple):
+    """g and u of a gated pair of projections in the 8-bit form (values, scales)."""
+    gq: torch.Tensor
+    ge: torch.Tensor
+    uq: torch.Tensor
+    ue: torch.Tensor
+
+
+def _rows(t: torch.Tensor, what: str, dtype=None, shape=None):
+    """(pointer, row stride) of a matrix with contiguous rows, after checking its type and shape."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+        raise TypeError(f"{what}: expected a 2-D CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {(rows, cols)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), ld
+
+
+def _dtype_code(dtype, what: str) -> int:
+    if dtype not in _DTYPE:
+        raise TypeError(f"{what}: expected float32, float16 or bfloat16, got {dtype}")
+    return _DTYPE[dtype]
+
+
+def _blocks(cols: int) -> int:
+    return -(-cols // KEEP_BLOCK)
+
+
+def _kept_pair(q, e, what: str, shape=None):
+    qp, ldq = _rows(q, what, torch.float8_e4m3fn, shape)
+    ep, lde = _rows(e, what + " scales", torch.float8_e8m0fnu, (q.shape[0], _blocks(q.shape[1])))
+    return qp, ldq, ep, lde
+
+
+def _new_kept(rows: int, cols: int, device):
+    # (rows a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses)
+    q = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    return q, torch.empty((rows, _blocks(cols)), dtype=torch.float8_e8m0fnu, device=device)
+
+
+def _new_rows(rows: int, cols: int, dtype, device):
+    # (rows a multiple of 16 bytes apart)
+    n = 16 // dtype.itemsize
+    return torch.empty((rows, -(-cols // n) * n), dtype=dtype, device=device)[:, :cols]
+
+
+def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
+    """Rows in the 8-bit form: (q, e), float8_e4m3fn values and float8_e8m0fnu scales, one for each block of KEEP_BLOCK
+    columns of a row.  out: such a pair to write into."""
+    xp, ld = _rows(x, "x")
+    code = _dtype_code(x.dtype, "x")
+    rows, cols = x.shape
+    q, e = _new_kept(rows, cols, x.device) if out is None else out
+    qp, ldq, ep, lde = _kept_pair(q, e, "out", (rows, cols))
+    _check(load().detox_checkpoint_pack(code, xp, ld, rows, cols, qp, ldq, ep, lde, _stream(stream)), "detox_checkpoint_pack")
+    return q, e
+
+
+def detox_checkpoint_unpack(q: torch.Tensor, e: torch.Tensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                            stream=None) -> torch.Tensor:
+    """The way back from detox_checkpoint_pack: rows of `dtype`."""
+    qp, ldq, ep, lde = _kept_pair(q, e, "q")
+    rows, cols = q.shape
+    if out is None:
+        out = _new_rows(rows, cols, dtype, q.device)
+    code = _dtype_code(out.dtype, "out")
+    xp, ld = _rows(out, "out", None, (rows, cols))
+    _check(load().detox_checkpoint_unpack(code, qp, ldq, ep, lde, rows, cols, xp, ld, _stream(stream)), "detox_checkpoint_unpack")
+    return out
+
+
+def detox_rmsnorm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  want_y: bool = True, want_q: bool = False, sum_out: Optional[torch.Tensor] = None, stream=None) -> RmsNorm:
+    """s = x + residual, y = s / rms(s) * w.  want_q: y also (want_y=False: only) in the 8-bit form.  The sum comes back
+    when there is a residual, in sum_out when given (which may be x or residual itself)."""
+    xp, ldx = _rows(x, "x")
+    code = _dtype_code(x.dtype, "x")
+    shape = rows, cols = tuple(x.shape)
+    if not (w.is_cuda and w.dtype == x.dtype and w.shape == (cols,) and w.is_contiguous()):
+        raise TypeError("w: expected a contiguous vector of x's type with an entry for each column")
+    rp = sp = yp = qp = ep = None
+    ldr = lds = ldy = ldq = lde = 0
+    s = y = q = e = None
+    if residual is not None:
+        rp, ldr = _rows(residual, "residual", x.dtype, shape)
+        s = _new_rows(rows, cols, x.dtype, x.device) if sum_out is None else sum_out
+        sp, lds = _rows(s, "sum_out", x.dtype, shape)
+    elif sum_out is not None:
+        raise ValueError("sum_out: there is no residual to add")
+    if want_y:
+        y = _new_rows(rows, cols, x.dtype, x.device)
+        yp, ldy = y.data_ptr(), max(y.stride(0), cols)
+    if want_q:
+        q, e = _new_kept(rows, cols, x.device)
+        qp, ldq, ep, lde = q.data_ptr(), max(q.stride(0), cols), e.data_ptr(), max(e.stride(0), 1)
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(load().detox_rmsnorm(code, xp, ldx, rp, ldr, w.data_ptr(), rows, cols, eps, sp, lds, yp, ldy, qp, ldq, ep, lde,
+                                rstd.data_ptr(), _stream(stream)), "detox_rmsnorm")
+    return RmsNorm(s, y, q, e, rstd)
+
+
+def detox_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().detox_rmsnorm_backward_workspace_bytes(rows, cols))
+
+
+def detox_rmsnorm_backward(dy: torch.Tensor, s: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor,
+                           ds: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                           dw: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of detox_rmsnorm: (dx, dw).  s: the sum of the forward pass (its x when there was no residual); ds: the
+    gradient that reaches the sum by its other uses.  dx is also the residual's gradient; dw is fp32."""
+    lib = load()
+    code = _dtype_code(s.dtype, "s")
+    sp, lds = _rows(s, "s")
+    shape = rows, cols = tuple(s.shape)
+    dyp, lddy = _rows(dy, "dy", s.dtype, shape)
+    dsp, ldds = (None, 0) if ds is None else _rows(ds, "ds", s.dtype, shape)
+    if not (w.is_cuda and w.dtype == s.dtype and w.shape == (cols,) and w.is_contiguous()):
+        raise TypeError("w: expected a contiguous vector of s's type with an entry for each column")
+    if not (rstd.is_cuda and rstd.dtype == torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous()):
+        raise TypeError("rstd: expected a contiguous float32 vector with an entry for each row")
+    if dx is None:
+        dx = _new_rows(rows, cols, s.dtype, s.device)
+    dxp, lddx = _rows(dx, "dx", s.dtype, shape)
+    if dw is None:
+        dw = torch.empty(cols, dtype=torch.float32, device=s.device)
+    elif not (dw.is_cuda and dw.dtype == torch.float32 and dw.shape == (cols,) and dw.is_contiguous()):
+        raise TypeError("dw: expected a contiguous float32 vector with an entry for each column")
+    ws, wp, wb = _ws(lib.detox_rmsnorm_backward_workspace_bytes(rows, cols), ws, s.device)
+    _check(lib.detox_rmsnorm_backward(code, dyp, lddy, dsp, ldds, sp, lds, w.data_ptr(), rstd.data_ptr(), rows, cols, dxp, lddx,
+                                      dw.data_ptr(), wp, wb, _stream(stream)), "detox_rmsnorm_backward")
+    return dx, dw
+
+
+def _gated_desc(x, wg, wu, act: int, kept: Optional[Kept]):
+    """The descriptor; x is a matrix or its 8-bit form (q, e).  Returns (desc, dtype, tokens, in_dim, hidden, device)."""
+    d = GatedDesc()
+    d.Wg, d.ldwg = _rows(wg, "wg")
+    d.Wu, d.ldwu = _rows(wu, "wu", wg.dtype, tuple(wg.shape))
+    hidden, in_dim = wg.shape
+    d.dtype, d.act = _dtype_code(wg.dtype, "wg"), int(act)
+    if isinstance(x, torch.Tensor):
+        d.X, d.ldx = _rows(x, "x", wg.dtype)
+        tokens, cols = x.shape
+    else:
+        q, e = x
+        d.XQ, d.ldxq, d.XE, d.ldxe = _kept_pair(q, e, "x")
+        tokens, cols = q.shape
+    if cols != in_dim:
+        raise ValueError(f"x has {cols} columns, the weights {in_dim}")
+    d.tokens, d.in_dim, d.hidden = tokens, in_dim, hidden
+    if kept is not None:
+        d.GQ, d.ldq, d.GE, d.lde = _kept_pair(kept.gq, kept.ge, "kept g", (tokens, hidden))
+        d.UQ, ldq, d.UE, lde = _kept_pair(kept.uq, kept.ue, "kept u", (tokens, hidden))
+        if (ldq, lde) != (d.ldq, d.lde):
+            raise ValueError("kept g and u must have the same strides")
+    return d, tokens, in_dim, hidden
+
+
+def detox_gated_workspace_bytes(x, wg, wu, act: int = ACT_SILU, kept: Optional[Kept] = None) -> int:
+    return int(load().detox_gated_workspace_bytes(ctypes.byref(_gated_desc(x, wg, wu, act, kept)[0])))
+
+
+def detox_gated(x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU, keep: bool = False,
+                h: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """h = act(x wg^T) * (x wu^T).  x: a matrix, or its 8-bit form as a pair (q, e).  keep=True returns (h, Kept): g and u
+    in the 8-bit form for the backward pass."""
+    lib = load()
+    kept = None
+    if keep:
+        tokens = (x if isinstance(x, torch.Tensor) else x[0]).shape[0]
+        kept = Kept(*_new_kept(tokens, wg.shape[0], wg.device), *_new_kept(tokens, wg.shape[0], wg.device))
+    d, tokens, _, hidden = _gated_desc(x, wg, wu, act, kept)
+    if h is None:
+        h = _new_rows(tokens, hidden, wg.dtype, wg.device)
+    hp, ldh = _rows(h, "h", wg.dtype, (tokens, hidden))
+    ref = ctypes.byref(d)
+    ws, wp, wb = _ws(lib.detox_gated_workspace_bytes(ref), ws, wg.device)
+    _check(lib.detox_gated(ref, hp, ldh, wp, wb, _stream(stream)), "detox_gated")
+    return (h, kept) if keep else h
+
+
+def detox_gated_backward_workspace_bytes(x, wg, wu, act: int = ACT_SILU, kept: Optional[Kept] = None) -> int:
+    return int(load().detox_gated_backward_workspace_bytes(ctypes.byref(_gated_desc(x, wg, wu, act, kept)[0])))
+
+
+def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU,
+                         kept: Optional[Kept] = None, dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
+                         dwu: Optional[torch.Tensor] = None, dw_dtype=None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of detox_gated: (dx, dwg, dwu).  kept: what the forward pass kept; without it g and u are computed again.
+    x as in detox_gated.  The weight gradients have the weights' type, or float32 with dw_dtype (or buffers of it, such as
+    pieces of a gradient's row)."""
+    lib = load()
+    d, tokens, in_dim, hidden = _gated_desc(x, wg, wu, act, kept)
+    dhp, lddh = _rows(dh, "dh", wg.dtype, (tokens, hidden))
+    if dx is None:
+        dx = _new_rows(tokens, in_dim, wg.dtype, wg.device)
+    dxp, lddx = _rows(dx, "dx", wg.dtype, (tokens, in_dim))
+    if (dwg is None) != (dwu is None):
+        raise ValueError("give both weight gradients or none")
+    if dwg is None:
+        dwg, dwu = (_new_rows(hidden, in_dim, dw_dtype or wg.dtype, wg.device) for _ in range(2))
+    gp, lddw = _rows(dwg, "dwg", dw_dtype, (hidden, in_dim))
+    up, ldu = _rows(dwu, "dwu", dwg.dtype, (hidden, in_dim))
+    if ldu != lddw:
+        raise ValueError("dwg and dwu must have the same stride")
+    ref = ctypes.byref(d)
+    ws, wp, wb = _ws(lib.detox_gated_backward_workspace_bytes(ref), ws, wg.device)
+    _check(lib.detox_gated_backward(ref, dhp, lddh, dxp, lddx, gp, up, lddw, _dtype_code(dwg.dtype, "dwg"), wp, wb,
+                                    _stream(stream)), "detox_gated_backward")
+    return dx, dwg, dwu

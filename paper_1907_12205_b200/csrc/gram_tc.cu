@@ -896,6 +896,19 @@ detox_status make_xmap(void* map, const float* X, int64_t ld, int m, int64_t d, 
     return r == CUDA_SUCCESS ? DETOX_OK : DETOX_ERR_CUDA;
 }
 
+detox_status make_map_16bit(void* map, bool bf16, const void* X, int64_t ld, int64_t rows, int64_t cols, int box_rows) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return DETOX_ERR_CUDA;
+    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t gstride[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    const cuuint32_t estride[2] = {1, 1};
+    CUresult r = enc(static_cast<CUtensorMap*>(map), bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                     2, const_cast<void*>(X), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DETOX_OK : DETOX_ERR_CUDA;
+}
+
 namespace {
 
 template <int J>

@@ -38,5 +38,7 @@ detox_status launch_gram_f16_vote(const float* X, int64_t ld, int n, int64_t d, 
 // The driver's tensor-map encoder for X as a 2-D fp32 tensor (d columns innermost, m rows, row pitch ld), zero fill
 // outside; swizzle128 = false: rows of a box land one after another.
 detox_status make_xmap(void* map, const float* X, int64_t ld, int m, int64_t d, int box_cols, int box_rows, bool swizzle128);
+// The same for a matrix of 16-bit entries (half or bfloat16): boxes of 64 columns, 128-byte swizzle.
+detox_status make_map_16bit(void* map, bool bf16, const void* X, int64_t ld, int64_t rows, int64_t cols, int box_rows);
 
 }  // namespace detox

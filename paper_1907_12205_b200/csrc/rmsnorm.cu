@@ -1,0 +1,380 @@
+// Root-mean-square norm with the residual's addition, and its backward pass.
+//
+// Forward:   s = x + r;  rstd = 1 / sqrt(mean(s^2) + eps);  y = s rstd w, as it is and / or in the 8-bit form.
+// Backward:  with hat = s rstd:  dx = dS + rstd (w dy - hat mean(w dy hat));  dw = sum over rows of dy hat.
+//
+// Both are bound by HBM, so a row is read once and stays in registers: TPR threads hold it, EPT entries each, in 16-byte
+// pieces dealt round the threads (piece t, t + TPR, ...).  With the 8-bit output a block of 128 columns then lies in 16
+// neighbouring lanes (fp32: 32), which agree on its largest entry by shuffles.  Up to 1024 columns a warp takes a row
+// and no barrier is needed; above that a CTA does.
+//
+// dw adds in a fixed order: a CTA takes every gridDim-th row and adds in registers, leaves one row of partial sums, and a
+// second kernel adds those column by column.
+#include "worker.cuh"
+
+namespace detox {
+
+namespace {
+
+// entries [c, c + N) of a row, zero beyond `cols`
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_piece(const T* row, int64_t c, int64_t cols, float (&f)[Piece<T>::N]) {
+    constexpr int N = Piece<T>::N;
+    if (VEC && c + N <= cols) {
+        Piece<T>::split(ld_stream_u4(row + c), f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_piece(T* row, int64_t c, int64_t cols, const float (&f)[Piece<T>::N]) {
+    constexpr int N = Piece<T>::N;
+    if (VEC && c + N <= cols) {
+        st_stream_u4(row + c, Piece<T>::join(f));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Sum over the TPR threads of a row (the same value in all of them; fixed order).  TPR > 32: the whole CTA; `turn`
+// alternates between two halves of `sm`, so that one barrier a sum is enough.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* sm, int turn) {
+    v = warp_sum(v);
+    if constexpr (TPR > 32) {
+        constexpr int W = TPR / 32;
+        float* at = sm + (turn & 1) * W;
+        if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v += at[i];
+    }
+    return v;
+}
+
+
+template <int TPR> constexpr int kBlockOf = TPR < 256 ? 256 : TPR;   // threads of a CTA
+
+struct NormOut {
+    void* S; int64_t lds;
+    void* Y; int64_t ldy;
+    uint8_t* Q; int64_t ldq;
+    uint8_t* E; int64_t lde;
+    float* rstd;
+};
+
+// X, R and S may be the same buffer: a row is in registers before any of it is written.
+template <typename T, int TPR, int EPT, bool VEC>
+__global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr,
+                                                                       const T* __restrict__ w, int64_t rows, int64_t cols,
+                                                                       float eps, NormOut o) {
+    constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
+    __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (TPR == 32 && row >= rows) return;   // (TPR > 32: a CTA per row, all of them there)
+
+    float v[P][N];
+    const T* x = X + row * ldx;
+#pragma unroll
+    for (int i = 0; i < P; ++i) load_piece<T, VEC>(x, (int64_t)(t + i * TPR) * N, cols, v[i]);
+    if (R) {
+        const T* r = R + row * ldr;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float f[N];
+            load_piece<T, VEC>(r, (int64_t)(t + i * TPR) * N, cols, f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i][j] += f[j];
+        }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum = fmaf(v[i][j], v[i][j], sum);
+    sum = row_sum<TPR>(sum, sm, 0);
+    const float rstd = rsqrtf(sum / (float)cols + eps);
+    if (o.rstd && t == 0) o.rstd[row] = rstd;
+    if (o.S) {
+        T* s = static_cast<T*>(o.S) + row * o.lds;
+#pragma unroll
+        for (int i = 0; i < P; ++i) store_piece<T, VEC>(s, (int64_t)(t + i * TPR) * N, cols, v[i]);
+    }
+    if (!o.Y && !o.Q) return;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int64_t c = (int64_t)(t + i * TPR) * N;
+        float f[N];
+        if (VEC && c + N <= cols) {
+            Piece<T>::split(__ldg(reinterpret_cast<const uint4*>(w + c)), f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(w[c + j]) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i][j] = c + j < cols ? v[i][j] * rstd * f[j] : 0.f;
+        if (o.Y) store_piece<T, VEC>(static_cast<T*>(o.Y) + row * o.ldy, c, cols, v[i]);
+        if (o.Q) {
+            constexpr int kLanes = kKeepBlock / N;   // 16, or 32 in fp32: the lanes of a block lie side by side
+            float amax = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) amax = fmaxf(amax, finite_abs(v[i][j]));
+#pragma unroll
+            for (int s = kLanes / 2; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+            const uint32_t e = keep_exponent(amax);
+            const float inv = keep_inverse(e);
+            uint32_t q[N / 4];
+#pragma unroll
+            for (int j = 0; j < N / 4; ++j)
+                q[j] = keep4(v[i][4 * j] * inv, v[i][4 * j + 1] * inv, v[i][4 * j + 2] * inv, v[i][4 * j + 3] * inv);
+            uint8_t* to = o.Q + row * o.ldq + c;
+            if (VEC && c + N <= cols) {
+                if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(q[0], q[1]));
+                else __stcs(reinterpret_cast<unsigned int*>(to), q[0]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (c + j < cols) to[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+            }
+            if (c < cols && t % kLanes == 0) o.E[row * o.lde + c / kKeepBlock] = (uint8_t)e;
+        }
+    }
+}
+
+constexpr int kMaxParts = kSMs * 4;   // CTAs of the backward pass, each leaving one row of partial sums of dw
+
+template <typename T, int TPR, int EPT, bool VEC>
+__global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_backward_kernel(
+    const T* dY, int64_t lddy, const T* dS, int64_t ldds, const T* __restrict__ S, int64_t lds, const T* __restrict__ w,
+    const float* __restrict__ rstd_of, int64_t rows, int64_t cols, T* dX, int64_t lddx, float* __restrict__ parts) {
+    constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
+    __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
+    const int t = threadIdx.x % TPR;
+    const float inv_cols = 1.f / (float)cols;
+    float acc[P][N];
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < rows; row += (int64_t)gridDim.x * RPB, ++turn) {
+        const float rstd = rstd_of[row];
+        float dyw[P][N], hat[P][N];
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * N;
+            load_piece<T, VEC>(dY + row * lddy, c, cols, dyw[i]);
+            load_piece<T, VEC>(S + row * lds, c, cols, hat[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * N;
+            float f[N];
+            if (VEC && c + N <= cols) {
+                Piece<T>::split(__ldg(reinterpret_cast<const uint4*>(w + c)), f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(w[c + j]) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                hat[i][j] *= rstd;
+                acc[i][j] = fmaf(dyw[i][j], hat[i][j], acc[i][j]);
+                dyw[i][j] *= f[j];
+                dot = fmaf(dyw[i][j], hat[i][j], dot);
+            }
+        }
+        if (!dX) continue;
+        dot = row_sum<TPR>(dot, sm, turn) * inv_cols;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * N;
+            float f[N];
+            if (dS) {
+                load_piece<T, VEC>(dS + row * ldds, c, cols, f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = fmaf(rstd, fmaf(-hat[i][j], dot, dyw[i][j]), f[j]);
+            store_piece<T, VEC>(dX + row * lddx, c, cols, f);
+        }
+    }
+    if (!parts) return;
+    float* part = parts + (int64_t)blockIdx.x * cols;
+    if constexpr (RPB == 1) {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int64_t c = (int64_t)(t + i * TPR) * N + j;
+                if (c < cols) part[c] = acc[i][j];
+            }
+    } else {
+        // the CTA's warps one after another
+        __shared__ float all[TPR * EPT];
+        for (int k = 0; k < RPB; ++k) {
+            if (threadIdx.x / TPR == k) {
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const int c = (t + i * TPR) * N + j;
+                        all[c] = k == 0 ? acc[i][j] : all[c] + acc[i][j];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < cols; c += kBlockOf<TPR>) part[c] = all[c];
+    }
+}
+
+// dw[c] = sum over the partial rows: 32 columns a CTA, 32 threads a column, each over every 32nd row
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ parts, int nparts, int64_t cols,
+                                                          float* __restrict__ dw) {
+    __shared__ float sm[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + x;
+    float sum = 0.f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int r = y; r < nparts; r += 32) sum += parts[(int64_t)r * cols + c];
+    }
+    sm[y][x] = sum;
+    __syncthreads();
+    sum = warp_sum(sm[x][y]);
+    if (x == 0 && (int64_t)blockIdx.x * 32 + y < cols) dw[(int64_t)blockIdx.x * 32 + y] = sum;
+}
+
+struct Backward {
+    const void* dY; int64_t lddy;
+    const void* dS; int64_t ldds;
+    const void* S; int64_t lds;
+    const void* w;
+    const float* rstd;
+    int64_t rows, cols;
+    void* dX; int64_t lddx;
+    float* parts;
+};
+
+// calls f<TPR, EPT>() with the smallest pair that holds a row
+template <typename F>
+detox_status by_width(int64_t cols, F f) {
+    if (cols <= 32 * 8) return f.template operator()<32, 8>();
+    if (cols <= 32 * 16) return f.template operator()<32, 16>();
+    if (cols <= 32 * 32) return f.template operator()<32, 32>();
+    if (cols <= 256 * 8) return f.template operator()<256, 8>();
+    if (cols <= 256 * 16) return f.template operator()<256, 16>();
+    if (cols <= 256 * 32) return f.template operator()<256, 32>();
+    return f.template operator()<1024, 32>();
+}
+int rows_per_cta(int64_t cols) { return cols <= 1024 ? 8 : 1; }
+
+template <typename T, bool VEC>
+struct Fwd {
+    const void* X; int64_t ldx;
+    const void* R; int64_t ldr;
+    const void* w;
+    int64_t rows, cols;
+    float eps;
+    NormOut o;
+    cudaStream_t s;
+    template <int TPR, int EPT>
+    detox_status operator()() const {
+        constexpr int RPB = kBlockOf<TPR> / TPR;
+        rmsnorm_kernel<T, TPR, EPT, VEC><<<(unsigned)ceil_div(rows, (int64_t)RPB), kBlockOf<TPR>, 0, s>>>(
+            static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows, cols, eps, o);
+        return launch_status();
+    }
+};
+
+template <typename T, bool VEC>
+struct Bwd {
+    Backward b;
+    int nparts;
+    cudaStream_t s;
+    template <int TPR, int EPT>
+    detox_status operator()() const {
+        rmsnorm_backward_kernel<T, TPR, EPT, VEC><<<(unsigned)nparts, kBlockOf<TPR>, 0, s>>>(
+            static_cast<const T*>(b.dY), b.lddy, static_cast<const T*>(b.dS), b.ldds, static_cast<const T*>(b.S), b.lds,
+            static_cast<const T*>(b.w), b.rstd, b.rows, b.cols, static_cast<T*>(b.dX), b.lddx, b.parts);
+        return launch_status();
+    }
+};
+
+// 16-byte pieces can be used: base and stride of every matrix that is there
+template <typename T>
+bool pieces(const void* p, int64_t ld) {
+    return p == nullptr || (aligned16(p) && ld % Piece<T>::N == 0);
+}
+
+template <typename T>
+detox_status forward(const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w, int64_t rows, int64_t cols,
+                     float eps, const NormOut& o, cudaStream_t s) {
+    const bool vec = pieces<T>(X, ldx) && pieces<T>(R, ldr) && aligned16(w) && pieces<T>(o.S, o.lds) && pieces<T>(o.Y, o.ldy) &&
+                     (o.Q == nullptr || (aligned16(o.Q) && o.ldq % 8 == 0));
+    if (vec) return by_width(cols, Fwd<T, true>{X, ldx, R, ldr, w, rows, cols, eps, o, s});
+    return by_width(cols, Fwd<T, false>{X, ldx, R, ldr, w, rows, cols, eps, o, s});
+}
+
+template <typename T>
+detox_status backward(const Backward& b, int nparts, cudaStream_t s) {
+    const bool vec = pieces<T>(b.dY, b.lddy) && pieces<T>(b.dS, b.ldds) && pieces<T>(b.S, b.lds) && aligned16(b.w) &&
+                     pieces<T>(b.dX, b.lddx);
+    if (vec) return by_width(b.cols, Bwd<T, true>{b, nparts, s});
+    return by_width(b.cols, Bwd<T, false>{b, nparts, s});
+}
+
+int parts_of(int64_t rows, int64_t cols) {
+    const int64_t need = ceil_div(rows, (int64_t)rows_per_cta(cols));
+    return (int)(need < kMaxParts ? need : kMaxParts);
+}
+
+}  // namespace
+
+detox_status launch_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w,
+                            int64_t rows, int64_t cols, float eps, void* S, int64_t lds, void* Y, int64_t ldy,
+                            uint8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, float* rstd, cudaStream_t s) {
+    if (rows == 0) return DETOX_OK;
+    const NormOut o{S, lds, Y, ldy, Q, ldq, E, lde, rstd};
+    if (dtype == DETOX_DTYPE_FLOAT) return forward<float>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
+    if (dtype == DETOX_DTYPE_HALF) return forward<__half>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
+    return forward<__nv_bfloat16>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
+}
+
+size_t rmsnorm_backward_ws_bytes(int64_t rows, int64_t cols) {
+    return align_up((size_t)(rows > 0 ? parts_of(rows, cols) : 1) * (size_t)cols * sizeof(float));
+}
+
+detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, const void* dS, int64_t ldds, const void* S,
+                                     int64_t lds, const void* w, const float* rstd, int64_t rows, int64_t cols, void* dX,
+                                     int64_t lddx, float* dw, void* ws, cudaStream_t s) {
+    if (rows == 0) {
+        if (dw && cudaMemsetAsync(dw, 0, (size_t)cols * sizeof(float), s) != cudaSuccess) return DETOX_ERR_CUDA;
+        return DETOX_OK;
+    }
+    const int nparts = parts_of(rows, cols);
+    float* parts = dw ? static_cast<float*>(ws) : nullptr;
+    const Backward b{dY, lddy, dS, ldds, S, lds, w, rstd, rows, cols, dX, lddx, parts};
+    detox_status st;
+    if (dtype == DETOX_DTYPE_FLOAT) st = backward<float>(b, nparts, s);
+    else if (dtype == DETOX_DTYPE_HALF) st = backward<__half>(b, nparts, s);
+    else st = backward<__nv_bfloat16>(b, nparts, s);
+    if (st != DETOX_OK || !dw) return st;
+    rmsnorm_dw_kernel<<<(unsigned)ceil_div(cols, (int64_t)32), 1024, 0, s>>>(parts, nparts, cols, dw);
+    return launch_status();
+}
+
+}  // namespace detox
