@@ -10,10 +10,16 @@
 // The reduction runs along the rows of memory in the first two (K-major operands); dgrad's weights and both operands of wgrad
 // lie the other way round and are read as MN-major tiles: nothing is transposed in memory.
 //
-// CTA: one warp issues the TMA copies of 64-wide slices of both operands into a ring of stages, one thread issues
-// the MMAs, four warps drain the accumulator.  Two accumulators of 128 x 256 fill the tensor memory, so a tile is drained
-// while the next one is multiplied.  The grid is persistent.  Ragged edges: TMA fills with zeros outside a matrix and
-// the epilogue masks its stores.
+// A CTA: one warp issues the TMA copies of 64-wide slices of both operands into a ring of stages, one thread issues
+// the MMAs, four warps drain the accumulator.  Two accumulators share the tensor memory, so a tile is drained while the
+// next one is multiplied.  Ragged edges: TMA fills with zeros outside a matrix and the epilogue masks its stores.
+// Three shapes of the work (gemm_shape chooses):
+//   pair     two CTAs of a cluster multiply one 256 x 256 tile (cta_group::2): each holds 128 rows of either operand, so
+//            a byte of shared memory feeds twice the MMA work that a CTA on its own gets out of it; persistent grid
+//   single   one CTA, 128 x 256 or 128 x 128; persistent grid
+//   split    few tiles: the CTAs of a cluster take a share of one tile's reduction each, leave fp32 sums in shared memory
+//            and then finish a share of its rows each, adding the others' sums over distributed shared memory in
+//            the order of their ranks
 #include <cuda.h>
 
 #include <type_traits>
@@ -29,26 +35,40 @@ namespace {
 enum Form { kForward = 0, kRecompute = 1, kDgrad = 2, kWgrad = 3 };
 
 constexpr int kSlice = 64;                       // entries of the reduction per stage: one 128-byte swizzled row
-constexpr int kTileM = 128, kTileN = 256;
 constexpr uint32_t kChunkBytes = 64 * 128;       // 64 rows of 128 bytes
-constexpr uint32_t kABytes = kTileM * 128, kBBytes = kTileN * 128, kStageBytes = kABytes + kBBytes;
-constexpr int kStages = 4;
 constexpr int kEpiWarps = 4, kThreads = 32 * (2 + kEpiWarps);
-constexpr int kTmemCols = 2 * kTileN;
+constexpr int kMaxSplit = 8;                     // CTAs of a portable cluster
+constexpr int kMaxStages = 6;
+
+// CG: CTAs that multiply one tile together.  BN: columns of the tile (forward, recompute: half of g, half of u).
+template <int CG, int BN>
+struct Tile {
+    static constexpr int M = 128 * CG, N = BN;
+    static constexpr int rows_b = BN / CG;                                    // rows of B that a CTA holds
+    static constexpr uint32_t a_bytes = 128 * 128, b_bytes = rows_b * 128, stage_bytes = a_bytes + b_bytes;
+    static constexpr int stages = stage_bytes > 32768 ? 4 : 6;
+    static constexpr int tmem_cols = 2 * BN;
+    static constexpr int pitch = BN + 4;                                      // floats between rows of a split's sums
+};
 
 struct GemmSmem {
-    uint64_t full[kStages];        // a stage's copies have landed
-    uint64_t empty[kStages];       // the MMAs that read it are done
+    uint64_t full[kMaxStages];     // a stage's copies have landed (pair: both CTAs', counted at the first one)
+    uint64_t empty[kMaxStages];    // the MMAs that read it are done
     uint64_t accum_full[2];        // an accumulator is complete
-    uint64_t accum_empty[2];       // ... and drained
+    uint64_t accum_empty[2];       // ... and drained (pair: by both CTAs, counted at the first one)
     uint32_t tmem_base;
     int abort_flag;
 };
-constexpr size_t kSmemBytes = kStages * (size_t)kStageBytes + sizeof(GemmSmem) + 1024;
+template <int CG, int BN>
+constexpr size_t kSmemBytes = Tile<CG, BN>::stages * (size_t)Tile<CG, BN>::stage_bytes + sizeof(GemmSmem) + 1024;
+static_assert(128 * Tile<1, 256>::pitch * 4 <= Tile<1, 256>::stages * Tile<1, 256>::stage_bytes, "a split's sums fit the stages");
+static_assert(128 * Tile<1, 128>::pitch * 4 <= Tile<1, 128>::stages * Tile<1, 128>::stage_bytes, "a split's sums fit the stages");
 
 struct GemmArgs {
     int mt, nt;                    // output tiles (wgrad: mt counts those of dWg and of dWu)
     int kb0, kb1;                  // slices of the first and of the second product that are added up
+    int split;                     // CTAs that share a tile's reduction
+    bool n_first;                  // neighbouring tiles lie along a row of the output (else along a column)
     int act;
     int64_t rows, cols;            // of the output (forward, recompute: of h)
     void* out0; void* out1;        // forward: h, -; recompute: dg, du; dgrad: dx, -; wgrad: dWg, dWu
@@ -71,6 +91,82 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
     desc |= (uint64_t)1 << 46;
     desc |= (uint64_t)2 << 61;                              // 128-byte swizzle
     return desc;
+}
+
+// ---- the forms of the tcgen05 / cluster instructions that a pair of CTAs needs -------------------
+template <int CG>
+__device__ __forceinline__ void tmem_alloc_cg(uint32_t* slot, uint32_t ncols) {
+    if constexpr (CG == 1) {
+        tmem_alloc(slot, ncols);
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void tmem_dealloc_cg(uint32_t taddr, uint32_t ncols) {
+    if constexpr (CG == 1) tmem_dealloc(taddr, ncols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma_f16_cg(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 1) {
+        mma_f16(tmem_d, adesc, bdesc, idesc, accumulate);
+    } else {
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+            : "memory");
+    }
+}
+// arrive on `bar` (pair: on the barrier at this place in both CTAs) once the MMAs issued so far have finished
+template <int CG>
+__device__ __forceinline__ void mma_commit_cg(uint64_t* bar) {
+    if constexpr (CG == 1) mma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+// the address, in the cluster's shared memory, of what lies at `addr` in the CTA of rank `rank`
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// 2-D TMA load into this CTA, completion counted on `bar`: a barrier of this CTA, or (pair) of the first CTA
+template <int CG>
+__device__ __forceinline__ void tma_load_cg(uint8_t* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+            ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+            ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
 }
 
 __device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&f)[32]) {
@@ -193,18 +289,41 @@ __device__ __forceinline__ void keep32(uint8_t* row, int64_t c, int64_t cols, bo
     }
 }
 
+// E consecutive entries of an output row (E = 2 or 4), as the lanes of a warp store a split's finished row
+template <typename OT, int E>
+__device__ __forceinline__ void store_few(OT* row, int64_t c, int64_t cols, bool vec, const float (&f)[E]) {
+    if (vec && c + E <= cols) {
+        if constexpr (sizeof(OT) == 2) {
+            if constexpr (E == 4) *reinterpret_cast<uint2*>(row + c) = make_uint2(pack2<OT>(f[0], f[1]), pack2<OT>(f[2], f[3]));
+            else *reinterpret_cast<uint32_t*>(row + c) = pack2<OT>(f[0], f[1]);
+        } else {
+            if constexpr (E == 4) *reinterpret_cast<float4*>(row + c) = make_float4(f[0], f[1], f[2], f[3]);
+            else *reinterpret_cast<float2*>(row + c) = make_float2(f[0], f[1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (c + i < cols) row[c + i] = from_f32<OT>(f[i]);
+    }
+}
+
 // Maps: forward, recompute: a0 = x, b0 = Wg, b1 = Wu; dgrad: a0 = dg, a1 = du, b0 = Wg, b1 = Wu; wgrad: a0 = dg,
 // a1 = du, b0 = x.
-template <typename T, typename OT, int FORM>
+template <typename T, typename OT, int FORM, int CG, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
 gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
                   const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1,
                   const __grid_constant__ GemmArgs p, int* __restrict__ status) {
+    using TL = Tile<CG, BN>;
+    constexpr int kStages = TL::stages;
+    constexpr bool kGated = FORM == kForward || FORM == kRecompute;
+    constexpr int kHalf = BN / 2;                    // columns of g (and of u) in a tile
     extern __shared__ uint8_t smem_raw[];
     uint8_t* stages = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzled tiles need 1024-byte alignment
-    GemmSmem* sm = reinterpret_cast<GemmSmem*>(stages + (size_t)kStages * kStageBytes);
+    GemmSmem* sm = reinterpret_cast<GemmSmem*>(stages + (size_t)kStages * TL::stage_bytes);
     volatile int* abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 || p.split > 1 ? cluster_rank() : 0u;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -213,98 +332,124 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sm->accum_full[b], 1);
-            mbar_init(&sm->accum_empty[b], kEpiWarps);
+            mbar_init(&sm->accum_empty[b], kEpiWarps * CG);
         }
         sm->abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == 0) tmem_alloc(&sm->tmem_base, kTmemCols);
+    if (warp == 0) tmem_alloc_cg<CG>(&sm->tmem_base, TL::tmem_cols);
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_sync();           // the other CTA's barriers are there before anything arrives on them
     tc_fence_after();
     const uint32_t tmem = sm->tmem_base;
 
-    const int nkb = p.kb0 + p.kb1;
+    // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
+    const int unit_ctas = CG == 2 ? 2 : p.split;
+    const int64_t unit = blockIdx.x / unit_ctas, units = gridDim.x / unit_ctas;
     const int64_t tiles = (int64_t)p.mt * p.nt;
+    const int nkb = p.kb0 + p.kb1;
+    // this CTA's slices of the reduction
+    const int kb_begin = CG == 2 ? 0 : (int)((int64_t)nkb * rank / p.split);
+    const int kb_end = CG == 2 ? nkb : (int)((int64_t)nkb * (rank + 1) / p.split);
+    auto place = [&](int64_t tile, int& m, int& n) {
+        if (p.n_first) { n = (int)(tile % p.nt); m = (int)(tile / p.nt); }
+        else { m = (int)(tile % p.mt); n = (int)(tile / p.mt); }
+    };
 
     if (warp == 0) {
         if (lane == 0) {
             // ------------------------------------------------ copies
+            const int cta_m = CG == 2 ? (int)rank * 128 : 0;          // first row of this CTA's part of A in the tile
             int s = 0;
             uint32_t ph = 0;
             int64_t issued = 0;
             bool ok = true;
-            for (int64_t tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
-                const int m = (int)(tile % p.mt), n = (int)(tile / p.mt);
-                for (int kb = 0; kb < nkb; ++kb) {
+            for (int64_t tile = unit; ok && tile < tiles; tile += units) {
+                int m, n;
+                place(tile, m, n);
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, status)) { ok = false; break; }
-                    uint8_t* a = stages + (size_t)s * kStageBytes;
-                    uint8_t* b = a + kABytes;
-                    uint64_t* bar = &sm->full[s];
-                    mbar_expect_tx(bar, kStageBytes);
-                    if constexpr (FORM == kForward || FORM == kRecompute) {
-                        tma_load_2d(a, &a0, kb * kSlice, m * kTileM, bar);
-                        tma_load_2d(b, &b0, kb * kSlice, n * 128, bar);
-                        tma_load_2d(b + 128 * 128, &b1, kb * kSlice, n * 128, bar);
-                    } else if constexpr (FORM == kDgrad) {
-                        const bool second = kb >= p.kb0;
-                        const int k = (second ? kb - p.kb0 : kb) * kSlice;
-                        tma_load_2d(a, second ? &a1 : &a0, k, m * kTileM, bar);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            tma_load_2d(b + c * kChunkBytes, second ? &b1 : &b0, n * kTileN + c * 64, k, bar);
+                    uint8_t* a = stages + (size_t)s * TL::stage_bytes;
+                    uint8_t* b = a + TL::a_bytes;
+                    uint32_t bar = smem_u32(&sm->full[s]);
+                    if constexpr (CG == 2) {
+                        if (rank == 0) mbar_expect_tx(&sm->full[s], 2 * TL::stage_bytes);
+                        bar = cluster_addr(bar, 0);
                     } else {
-                        const int half = p.mt / 2;
-                        const bool second = m >= half;
-                        const int row = (second ? m - half : m) * kTileM;
+                        mbar_expect_tx(&sm->full[s], TL::stage_bytes);
+                    }
+                    if constexpr (kGated) {
+                        tma_load_cg<CG>(a, &a0, kb * kSlice, m * TL::M + cta_m, bar);
+                        if constexpr (CG == 2) {                       // the first CTA brings Wg, the second Wu
+                            tma_load_cg<CG>(b, rank == 0 ? &b0 : &b1, kb * kSlice, n * kHalf, bar);
+                        } else {
+                            tma_load_cg<CG>(b, &b0, kb * kSlice, n * kHalf, bar);
+                            tma_load_cg<CG>(b + kHalf * 128, &b1, kb * kSlice, n * kHalf, bar);
+                        }
+                    } else {
+                        const int col = n * BN + (CG == 2 ? (int)rank * TL::rows_b : 0);
+                        if constexpr (FORM == kDgrad) {
+                            const bool second = kb >= p.kb0;
+                            const int k = (second ? kb - p.kb0 : kb) * kSlice;
+                            tma_load_cg<CG>(a, second ? &a1 : &a0, k, m * TL::M + cta_m, bar);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c)
-                            tma_load_2d(a + c * kChunkBytes, second ? &a1 : &a0, row + c * 64, kb * kSlice, bar);
+                            for (int c = 0; c < TL::rows_b / 64; ++c)
+                                tma_load_cg<CG>(b + c * kChunkBytes, second ? &b1 : &b0, col + c * 64, k, bar);
+                        } else {
+                            const int half = p.mt / 2;
+                            const bool second = m >= half;
+                            const int row = (second ? m - half : m) * TL::M + cta_m;
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            tma_load_2d(b + c * kChunkBytes, &b0, n * kTileN + c * 64, kb * kSlice, bar);
+                            for (int c = 0; c < 2; ++c)
+                                tma_load_cg<CG>(a + c * kChunkBytes, second ? &a1 : &a0, row + c * 64, kb * kSlice, bar);
+#pragma unroll
+                            for (int c = 0; c < TL::rows_b / 64; ++c)
+                                tma_load_cg<CG>(b + c * kChunkBytes, &b0, col + c * 64, kb * kSlice, bar);
+                        }
                     }
                     ++issued;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
             if (*abort_flag) {
-                // give the copies still in flight a bounded time to land before the CTA goes away
+                // give the copies still in flight a bounded time to land before the CTA goes away (a pair's are counted
+                // at the first CTA, whichever CTA they belong to)
                 for (int64_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-                    for (uint32_t spin = 0; spin < (1u << 16) && !mbar_test(&sm->full[i % kStages], (uint32_t)(i / kStages) & 1u); ++spin)
+                    for (uint32_t spin = 0; spin < (1u << 14) && (rank != 0 || !mbar_test(&sm->full[i % kStages], (uint32_t)(i / kStages) & 1u)); ++spin)
                         __nanosleep(64);
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && (CG == 1 || rank == 0)) {
             // ------------------------------------------------ MMAs
             constexpr bool kAmn = FORM == kWgrad, kBmn = FORM == kDgrad || FORM == kWgrad;
             constexpr uint32_t fmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;   // A and B: fp16 or bf16
             constexpr uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((kAmn ? 1u : 0u) << 15) | ((kBmn ? 1u : 0u) << 16) |
-                                       ((uint32_t)(kTileN >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+                                       ((uint32_t)(TL::N >> 3) << 17) | ((uint32_t)(TL::M >> 4) << 24);
             // 16 steps of the reduction: 32 bytes along a K-major row, 16 rows of an MN-major chunk
             constexpr uint64_t kAstep = kAmn ? 16 * 128 / 16 : 2, kBstep = kBmn ? 16 * 128 / 16 : 2;
             int s = 0, buf = 0;
             uint32_t ph = 0, aph = 0;
             bool ok = true;
-            for (int64_t tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+            for (int64_t tile = unit; ok && tile < tiles; tile += units) {
                 if (!mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status)) break;
                 tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)(buf * kTileN);
-                for (int kb = 0; kb < nkb; ++kb) {
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!mbar_wait(&sm->full[s], ph, abort_flag, status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t addr = smem_u32(stages + (size_t)s * kStageBytes);
+                    const uint32_t addr = smem_u32(stages + (size_t)s * TL::stage_bytes);
                     const uint64_t ad = kAmn ? smem_desc_mn(addr) : smem_desc(addr);
-                    const uint64_t bd = kBmn ? smem_desc_mn(addr + kABytes) : smem_desc(addr + kABytes);
+                    const uint64_t bd = kBmn ? smem_desc_mn(addr + TL::a_bytes) : smem_desc(addr + TL::a_bytes);
 #pragma unroll
                     for (int kk = 0; kk < kSlice / 16; ++kk)
-                        mma_f16(d, ad + kk * kAstep, bd + kk * kBstep, idesc, (kb | kk) != 0 ? 1u : 0u);
-                    mma_commit(&sm->empty[s]);
+                        mma_f16_cg<CG>(d, ad + kk * kAstep, bd + kk * kBstep, idesc, kb != kb_begin || kk != 0 ? 1u : 0u);
+                    mma_commit_cg<CG>(&sm->empty[s]);
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
-                if (ok) mma_commit(&sm->accum_full[buf]);
+                if (ok) mma_commit_cg<CG>(&sm->accum_full[buf]);
                 if (++buf == 2) { buf = 0; aph ^= 1u; }
             }
         }
@@ -314,21 +459,36 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         const int part = warp & 3;   // the 32 accumulator lanes that this warp may read
         int buf = 0;
         uint32_t ph = 0;
-        for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-            int m = (int)(tile % p.mt);
-            const int n = (int)(tile / p.mt);
+        for (int64_t tile = unit; tile < tiles; tile += units) {
+            int m, n;
+            place(tile, m, n);
             if (!__all_sync(0xffffffffu, mbar_wait(&sm->accum_full[buf], ph, abort_flag, status))) break;
             tc_fence_after();
-            const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(buf * kTileN);
-            if constexpr (FORM == kForward || FORM == kRecompute) {
-                const int64_t row = (int64_t)m * kTileM + part * 32 + lane, c0 = (int64_t)n * 128;
+            const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(buf * BN);
+            const int in_tile = (CG == 2 ? (int)rank * 128 : 0) + part * 32 + lane;
+            if (CG == 1 && p.split > 1) {
+                // (the one tile of this cluster, all its MMAs done: the stages are free to take the sums)
+                const int m_out = FORM == kWgrad && m >= p.mt / 2 ? m - p.mt / 2 : m;
+                float* row = reinterpret_cast<float*>(stages) + (size_t)in_tile * TL::pitch;
+#pragma unroll 1
+                for (int c = 0; c < BN; c += 32) {
+                    float f[32];
+                    tmem_load32(at + c, f);
+                    if ((int64_t)m_out * TL::M + in_tile < p.rows) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            *reinterpret_cast<float4*>(row + c + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+                    }
+                }
+            } else if constexpr (kGated) {
+                const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * kHalf;
                 const bool live = row < p.rows;
                 float gmax = 0.f, umax = 0.f;
 #pragma unroll 1
-                for (int c = 0; c < 128; c += 32) {
+                for (int c = 0; c < kHalf; c += 32) {
                     float g[32], u[32];
                     tmem_load32(at + c, g);
-                    tmem_load32(at + 128 + c, u);
+                    tmem_load32(at + kHalf + c, u);
                     if constexpr (FORM == kForward) {
                         if (p.gq) {
 #pragma unroll
@@ -347,15 +507,15 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                         store32(static_cast<T*>(p.out1) + row * p.ldo, c0 + c, p.cols, true, u);
                     }
                 }
-                if (FORM == kForward && p.gq) {
+                if (FORM == kForward && BN == 256 && p.gq) {
                     const uint32_t ge = keep_exponent(gmax), ue = keep_exponent(umax);
                     const float ginv = keep_inverse(ge), uinv = keep_inverse(ue);
 #pragma unroll 1
-                    for (int c = 0; c < 128; c += 32) {
+                    for (int c = 0; c < kHalf; c += 32) {
                         float f[32];
                         tmem_load32(at + c, f);
                         if (live) keep32(p.gq + row * p.ldq, c0 + c, p.cols, p.q_vec, ginv, f);
-                        tmem_load32(at + 128 + c, f);
+                        tmem_load32(at + kHalf + c, f);
                         if (live) keep32(p.uq + row * p.ldq, c0 + c, p.cols, p.q_vec, uinv, f);
                     }
                     if (live) {
@@ -366,9 +526,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             } else {
                 void* out = p.out0;
                 if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
-                const int64_t row = (int64_t)m * kTileM + part * 32 + lane, c0 = (int64_t)n * kTileN;
+                const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * BN;
 #pragma unroll 1
-                for (int c = 0; c < kTileN; c += 32) {
+                for (int c = 0; c < BN; c += 32) {
                     float f[32];
                     tmem_load32(at + c, f);
                     if (row < p.rows) store32(static_cast<OT*>(out) + row * p.ldo, c0 + c, p.cols, p.out_vec, f);
@@ -376,14 +536,117 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm->accum_empty[buf]);
+            if (lane == 0) {
+                if constexpr (CG == 2) mbar_arrive_cluster(cluster_addr(smem_u32(&sm->accum_empty[buf]), 0));
+                else mbar_arrive(&sm->accum_empty[buf]);
+            }
             if (++buf == 2) { buf = 0; ph ^= 1u; }
         }
         __syncwarp();
     }
+
+    if constexpr (CG == 1) {
+        if (p.split > 1) {
+            // ------------------------------------------------ the cluster's sums are added and the tile is finished
+            __syncthreads();
+            cluster_sync();
+            int m, n;
+            place(unit, m, n);
+            void* out = p.out0;
+            if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
+            const int64_t row0 = (int64_t)m * TL::M;
+            const int live = (int)(p.rows - row0 < TL::M ? p.rows - row0 : TL::M);
+            const int share = (live + p.split - 1) / p.split;
+            const int last = (int)(rank + 1) * share < live ? (int)(rank + 1) * share : live;
+            constexpr int E = BN / 64;                   // a lane's columns: E of the tile's first half, E of the second
+            uint32_t from[kMaxSplit];
+#pragma unroll
+            for (int k = 0; k < kMaxSplit; ++k) from[k] = cluster_addr(smem_u32(stages), k < p.split ? k : 0);
+            for (int r = (int)rank * share + warp; r < last; r += kThreads / 32) {
+                const uint32_t off = ((uint32_t)r * TL::pitch + (uint32_t)lane * E) * 4u;
+                float a[E], b[E], va[kMaxSplit][E], vb[kMaxSplit][E];
+#pragma unroll
+                for (int k = 0; k < kMaxSplit; ++k) {
+                    if (k < p.split) {
+                        if constexpr (E == 4) {
+                            const float4 x = ld_cluster_f4(from[k] + off), y = ld_cluster_f4(from[k] + off + kHalf * 4);
+                            va[k][0] = x.x; va[k][1] = x.y; va[k][2] = x.z; va[k][3] = x.w;
+                            vb[k][0] = y.x; vb[k][1] = y.y; vb[k][2] = y.z; vb[k][3] = y.w;
+                        } else {
+                            const float2 x = ld_cluster_f2(from[k] + off), y = ld_cluster_f2(from[k] + off + kHalf * 4);
+                            va[k][0] = x.x; va[k][1] = x.y;
+                            vb[k][0] = y.x; vb[k][1] = y.y;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) { a[i] = va[0][i]; b[i] = vb[0][i]; }
+#pragma unroll
+                for (int k = 1; k < kMaxSplit; ++k) {
+                    if (k < p.split) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) { a[i] += va[k][i]; b[i] += vb[k][i]; }
+                    }
+                }
+                const int64_t row = row0 + r;
+                if constexpr (kGated) {
+                    const int64_t c = (int64_t)n * kHalf + lane * E;
+                    if constexpr (FORM == kForward) {
+                        if (BN == 256 && p.gq) {
+                            float gmax = 0.f, umax = 0.f;
+#pragma unroll
+                            for (int i = 0; i < E; ++i) {
+                                gmax = fmaxf(gmax, finite_abs(a[i]));
+                                umax = fmaxf(umax, finite_abs(b[i]));
+                            }
+#pragma unroll
+                            for (int o = 16; o > 0; o >>= 1) {
+                                gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
+                                umax = fmaxf(umax, __shfl_xor_sync(0xffffffffu, umax, o));
+                            }
+                            const uint32_t ge = keep_exponent(gmax), ue = keep_exponent(umax);
+                            const float gi = keep_inverse(ge), ui = keep_inverse(ue);
+                            const uint32_t gq = keep4(a[0] * gi, a[1] * gi, a[E - 2] * gi, a[E - 1] * gi);
+                            const uint32_t uq = keep4(b[0] * ui, b[1] * ui, b[E - 2] * ui, b[E - 1] * ui);
+                            if (p.q_vec && c + E <= p.cols) {
+                                *reinterpret_cast<uint32_t*>(p.gq + row * p.ldq + c) = gq;
+                                *reinterpret_cast<uint32_t*>(p.uq + row * p.ldq + c) = uq;
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < E; ++i)
+                                    if (c + i < p.cols) {
+                                        p.gq[row * p.ldq + c + i] = (uint8_t)(gq >> (8 * i));
+                                        p.uq[row * p.ldq + c + i] = (uint8_t)(uq >> (8 * i));
+                                    }
+                            }
+                            if (lane == 0) {
+                                p.ge[row * p.lde + n] = (uint8_t)ge;
+                                p.ue[row * p.lde + n] = (uint8_t)ue;
+                            }
+                        }
+                        by_act(p.act, HOf<E>{a, b});
+                        store_few<T, E>(static_cast<T*>(out) + row * p.ldo, c, p.cols, p.out_vec, b);
+                    } else {
+                        float dh[E];
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            dh[i] = c + i < p.cols ? to_f32(static_cast<const T*>(p.dh)[row * p.lddh + c + i]) : 0.f;
+                        by_act(p.act, DguOf<E>{a, b, dh});
+                        store_few<T, E>(static_cast<T*>(p.out0) + row * p.ldo, c, p.cols, true, a);
+                        store_few<T, E>(static_cast<T*>(p.out1) + row * p.ldo, c, p.cols, true, b);
+                    }
+                } else {
+                    const int64_t c = (int64_t)n * BN + lane * E;
+                    store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c, p.cols, p.out_vec, a);
+                    store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c + kHalf, p.cols, p.out_vec, b);
+                }
+            }
+        }
+    }
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) tmem_dealloc(tmem, kTmemCols);
+    if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
+    if (warp == 0) tmem_dealloc_cg<CG>(tmem, TL::tmem_cols);
 }
 
 // ---- dg and du from the kept g and u ------------------------------------------------------------
@@ -535,27 +798,77 @@ detox_status weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char
     return DETOX_OK;
 }
 
-// One product: maps, grid, launch.  Each map's matrix is rows x cols with boxes of `box` rows.
+// Which shape a product of `rows` x `cols` (of the accumulator: forward and recompute have 2 x hidden columns) with nkb
+// slices takes.
+struct Shape {
+    int cg, bn, split;
+};
+Shape gemm_shape(int64_t rows, int64_t cols, int nkb, bool keeps) {
+    (void)keeps;
+    const int64_t tiles = ceil_div(rows, (int64_t)128) * ceil_div(cols, (int64_t)256);
+    if (tiles >= kSMs) return Shape{2, 256, 1};
+    int split = (int)(kSMs / tiles);
+    if (split > kMaxSplit) split = kMaxSplit;
+    if (split > nkb) split = nkb;
+    return Shape{1, 256, split};
+}
+
+// One product: maps, grid, launch.  The matrices of the maps are rows x cols.
 struct MapOf {
     Mat m;
     int64_t rows, cols;
-    int box;
 };
-template <typename T, typename OT, int FORM>
-detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, int* status,
-                         cudaStream_t s) {
+template <typename T, typename OT, int FORM, int CG, int BN>
+detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, GemmArgs args, int split, int* status,
+                          cudaStream_t s) {
+    using TL = Tile<CG, BN>;
+    constexpr bool kGated = FORM == kForward || FORM == kRecompute;
+    // boxes of 64 columns: 128 rows of A and as many of the weights as a tile has columns of g, or 64 steps of the reduction
+    const int box_a = FORM == kWgrad ? 64 : 128, box_b = kGated ? BN / 2 : 64;
     CUtensorMap maps[4];
     const MapOf* of[4] = {&a0, &a1, &b0, &b1};
     for (int i = 0; i < 4; ++i) {
         const detox_status st = make_map_16bit(&maps[i], std::is_same<T, __nv_bfloat16>::value, of[i]->m.p, of[i]->m.ld, of[i]->rows,
-                                               of[i]->cols, of[i]->box);
+                                               of[i]->cols, i < 2 ? box_a : box_b);
         if (st != DETOX_OK) return st;
     }
-    auto* k = gated_gemm_kernel<T, OT, FORM>;
-    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes) != cudaSuccess) return DETOX_ERR_CUDA;
+    args.mt = (int)ceil_div(args.rows, (int64_t)TL::M) * (FORM == kWgrad ? 2 : 1);
+    args.nt = (int)ceil_div(args.cols, (int64_t)(kGated ? BN / 2 : BN));
+    args.split = split;
+    // The operand whose strips the neighbouring tiles share is read once; the other one is read again for every strip, and should
+    // be the smaller one, which stays in L2.
+    args.n_first = args.rows * (FORM == kWgrad ? 2 : 1) > args.cols * (kGated ? 2 : 1);
+    auto* k = gated_gemm_kernel<T, OT, FORM, CG, BN>;
+    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes<CG, BN>) != cudaSuccess) return DETOX_ERR_CUDA;
     const int64_t tiles = (int64_t)args.mt * args.nt;
-    k<<<(unsigned)(tiles < kSMs ? tiles : kSMs), kThreads, kSmemBytes, s>>>(maps[0], maps[1], maps[2], maps[3], args, status);
+    const int unit = CG == 2 ? 2 : split;
+    // a split's cluster finishes one tile; the others' grids are persistent
+    const int64_t units = split > 1 || tiles < kSMs / unit ? tiles : kSMs / unit;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * unit));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes<CG, BN>;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)unit;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, k, maps[0], maps[1], maps[2], maps[3], args, status) != cudaSuccess) {
+        launch_status();
+        return DETOX_ERR_CUDA;
+    }
     return launch_status();
+}
+template <typename T, typename OT, int FORM>
+detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, int* status,
+                         cudaStream_t s) {
+    const Shape sh = gemm_shape(args.rows * (FORM == kWgrad ? 2 : 1), args.cols * (FORM == kForward || FORM == kRecompute ? 2 : 1),
+                                args.kb0 + args.kb1, args.gq != nullptr);
+    if (sh.cg == 2) return launch_shape<T, OT, FORM, 2, 256>(a0, a1, b0, b1, args, 1, status, s);
+    if (sh.bn == 256) return launch_shape<T, OT, FORM, 1, 256>(a0, a1, b0, b1, args, sh.split, status, s);
+    return launch_shape<T, OT, FORM, 1, 128>(a0, a1, b0, b1, args, sh.split, status, s);
 }
 
 template <typename T>
@@ -568,8 +881,6 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
     if (st == DETOX_OK) st = weight_matrices(g, q, ws, &wg, &wu, s);
     if (st != DETOX_OK) return st;
     GemmArgs a{};
-    a.mt = (int)ceil_div(g.tokens, (int64_t)kTileM);
-    a.nt = (int)ceil_div(g.hidden, (int64_t)128);
     a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
     a.act = g.act;
     a.rows = g.tokens;
@@ -580,7 +891,7 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
     a.gq = g.GQ; a.ge = g.GE; a.uq = g.UQ; a.ue = g.UE;
     a.ldq = g.ldq; a.lde = g.lde;
     a.q_vec = aligned16(g.GQ) && aligned16(g.UQ) && g.ldq % 16 == 0;
-    const MapOf mx{x, g.tokens, g.in_dim, 128}, mg{wg, g.hidden, g.in_dim, 128}, mu{wu, g.hidden, g.in_dim, 128};
+    const MapOf mx{x, g.tokens, g.in_dim}, mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
     return launch_gemm<T, T, kForward>(mx, mx, mg, mu, a, status, s);
 }
 
@@ -588,8 +899,6 @@ template <typename T, typename OT>
 detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Mat& du, const Mat& x, void* dWg, void* dWu,
                               int64_t lddw, int* status, cudaStream_t s) {
     GemmArgs a{};
-    a.mt = 2 * (int)ceil_div(g.hidden, (int64_t)kTileM);
-    a.nt = (int)ceil_div(g.in_dim, (int64_t)kTileN);
     a.kb0 = (int)ceil_div(g.tokens, (int64_t)kSlice);
     a.rows = g.hidden;
     a.cols = g.in_dim;
@@ -597,7 +906,7 @@ detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Ma
     a.out1 = dWu;
     a.ldo = lddw;
     a.out_vec = aligned16(dWg) && aligned16(dWu) && lddw % Piece<OT>::N == 0;
-    const MapOf mg{dg, g.tokens, g.hidden, 64}, mu{du, g.tokens, g.hidden, 64}, mx{x, g.tokens, g.in_dim, 64};
+    const MapOf mg{dg, g.tokens, g.hidden}, mu{du, g.tokens, g.hidden}, mx{x, g.tokens, g.in_dim};
     return launch_gemm<T, OT, kWgrad>(mg, mu, mx, mx, a, status, s);
 }
 
@@ -623,8 +932,6 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         st = launch_status();
     } else {
         GemmArgs a{};
-        a.mt = (int)ceil_div(g.tokens, (int64_t)kTileM);
-        a.nt = (int)ceil_div(g.hidden, (int64_t)128);
         a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
         a.act = g.act;
         a.rows = g.tokens;
@@ -635,22 +942,20 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         a.dh = dH;
         a.lddh = lddh;
         a.dh_vec = tma_ok(dH, lddh);
-        const MapOf mx{x, g.tokens, g.in_dim, 128}, mg{wg, g.hidden, g.in_dim, 128}, mu{wu, g.hidden, g.in_dim, 128};
+        const MapOf mx{x, g.tokens, g.in_dim}, mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
         st = launch_gemm<T, T, kRecompute>(mx, mx, mg, mu, a, status, s);
     }
     if (st != DETOX_OK) return st;
     if (dX) {
         GemmArgs a{};
-        a.mt = (int)ceil_div(g.tokens, (int64_t)kTileM);
-        a.nt = (int)ceil_div(g.in_dim, (int64_t)kTileN);
         a.kb0 = a.kb1 = (int)ceil_div(g.hidden, (int64_t)kSlice);
         a.rows = g.tokens;
         a.cols = g.in_dim;
         a.out0 = dX;
         a.ldo = lddx;
         a.out_vec = tma_ok(dX, lddx);
-        const MapOf mdg{dg, g.tokens, g.hidden, 128}, mdu{du, g.tokens, g.hidden, 128};
-        const MapOf mg{wg, g.hidden, g.in_dim, 64}, mu{wu, g.hidden, g.in_dim, 64};
+        const MapOf mdg{dg, g.tokens, g.hidden}, mdu{du, g.tokens, g.hidden};
+        const MapOf mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
         st = launch_gemm<T, T, kDgrad>(mdg, mdu, mg, mu, a, status, s);
         if (st != DETOX_OK) return st;
     }

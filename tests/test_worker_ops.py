@@ -300,7 +300,9 @@ def taken(q, e):
 
 
 GATED_SHAPES = [(1, 1, 1), (1, 64, 128), (1, 2048, 300), (2, 8, 130), (5, 100, 77), (48, 256, 512), (127, 72, 129), (128, 64, 128),
-                (129, 65, 257), (130, 1000, 33), (300, 513, 391), (1000, 128, 640), (257, 2056, 1031)]
+                (129, 65, 257), (130, 1000, 33), (300, 513, 391), (1000, 128, 640), (257, 2056, 1031),
+                # enough tiles for pairs of CTAs: in the forward pass, for dx, for the weight gradients
+                (2100, 72, 1301), (2049, 2401, 41), (33, 2399, 1301)]
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
