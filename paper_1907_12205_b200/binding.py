@@ -151,8 +151,8 @@ def _host_i32(a: Sequence[int]) -> np.ndarray:
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:   # the current stream's handle, without a Stream object around it (3.2 -> 0.3 us a call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -520,11 +520,13 @@ def _rows(t: torch.Tensor, what: str, dtype=None, shape=None):
     rows, cols = t.shape
     if shape is not None and (rows, cols) != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {(rows, cols)}")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{what}: rows must be contiguous")
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
     if ld < cols:
-        raise ValueError(f"{what}: rows overlap")
+        if rows > 1:
+            raise ValueError(f"{what}: rows overlap")
+        ld = cols
     return t.data_ptr(), ld
 
 
@@ -544,16 +546,16 @@ def _kept_pair(q, e, what: str, shape=None):
     return qp, ldq, ep, lde
 
 
-def _new_kept(rows: int, cols: int, device):
-    # (rows a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses)
-    q = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
-    return q, torch.empty((rows, _blocks(cols)), dtype=torch.float8_e8m0fnu, device=device)
-
-
-def _new_rows(rows: int, cols: int, dtype, device):
-    # (rows a multiple of 16 bytes apart)
+def _new_rows(rows: int, cols: int, dtype, like: torch.Tensor):
+    """A matrix whose rows lie a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses."""
     n = 16 // dtype.itemsize
-    return torch.empty((rows, -(-cols // n) * n), dtype=dtype, device=device)[:, :cols]
+    if cols % n == 0:
+        return like.new_empty((rows, cols), dtype=dtype)
+    return like.new_empty((rows, -(-cols // n) * n), dtype=dtype)[:, :cols]
+
+
+def _new_kept(rows: int, cols: int, like: torch.Tensor):
+    return _new_rows(rows, cols, torch.float8_e4m3fn, like), like.new_empty((rows, _blocks(cols)), dtype=torch.float8_e8m0fnu)
 
 
 def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
@@ -562,7 +564,7 @@ def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
     xp, ld = _rows(x, "x")
     code = _dtype_code(x.dtype, "x")
     rows, cols = x.shape
-    q, e = _new_kept(rows, cols, x.device) if out is None else out
+    q, e = _new_kept(rows, cols, x) if out is None else out
     qp, ldq, ep, lde = _kept_pair(q, e, "out", (rows, cols))
     _check(load().detox_checkpoint_pack(code, xp, ld, rows, cols, qp, ldq, ep, lde, _stream(stream)), "detox_checkpoint_pack")
     return q, e
@@ -574,7 +576,7 @@ def detox_checkpoint_unpack(q: torch.Tensor, e: torch.Tensor, dtype=torch.bfloat
     qp, ldq, ep, lde = _kept_pair(q, e, "q")
     rows, cols = q.shape
     if out is None:
-        out = _new_rows(rows, cols, dtype, q.device)
+        out = _new_rows(rows, cols, dtype, q)
     code = _dtype_code(out.dtype, "out")
     xp, ld = _rows(out, "out", None, (rows, cols))
     _check(load().detox_checkpoint_unpack(code, qp, ldq, ep, lde, rows, cols, xp, ld, _stream(stream)), "detox_checkpoint_unpack")
@@ -595,17 +597,17 @@ def detox_rmsnorm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Ten
     s = y = q = e = None
     if residual is not None:
         rp, ldr = _rows(residual, "residual", x.dtype, shape)
-        s = _new_rows(rows, cols, x.dtype, x.device) if sum_out is None else sum_out
+        s = _new_rows(rows, cols, x.dtype, x) if sum_out is None else sum_out
         sp, lds = _rows(s, "sum_out", x.dtype, shape)
     elif sum_out is not None:
         raise ValueError("sum_out: there is no residual to add")
     if want_y:
-        y = _new_rows(rows, cols, x.dtype, x.device)
+        y = _new_rows(rows, cols, x.dtype, x)
         yp, ldy = y.data_ptr(), max(y.stride(0), cols)
     if want_q:
-        q, e = _new_kept(rows, cols, x.device)
+        q, e = _new_kept(rows, cols, x)
         qp, ldq, ep, lde = q.data_ptr(), max(q.stride(0), cols), e.data_ptr(), max(e.stride(0), 1)
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    rstd = x.new_empty(rows, dtype=torch.float32)
     _check(load().detox_rmsnorm(code, xp, ldx, rp, ldr, w.data_ptr(), rows, cols, eps, sp, lds, yp, ldy, qp, ldq, ep, lde,
                                 rstd.data_ptr(), _stream(stream)), "detox_rmsnorm")
     return RmsNorm(s, y, q, e, rstd)
@@ -631,10 +633,10 @@ def detox_rmsnorm_backward(dy: torch.Tensor, s: torch.Tensor, w: torch.Tensor, r
     if not (rstd.is_cuda and rstd.dtype == torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous()):
         raise TypeError("rstd: expected a contiguous float32 vector with an entry for each row")
     if dx is None:
-        dx = _new_rows(rows, cols, s.dtype, s.device)
+        dx = _new_rows(rows, cols, s.dtype, s)
     dxp, lddx = _rows(dx, "dx", s.dtype, shape)
     if dw is None:
-        dw = torch.empty(cols, dtype=torch.float32, device=s.device)
+        dw = s.new_empty(cols, dtype=torch.float32)
     elif not (dw.is_cuda and dw.dtype == torch.float32 and dw.shape == (cols,) and dw.is_contiguous()):
         raise TypeError("dw: expected a contiguous float32 vector with an entry for each column")
     ws, wp, wb = _ws(lib.detox_rmsnorm_backward_workspace_bytes(rows, cols), ws, s.device)
@@ -680,10 +682,10 @@ def detox_gated(x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU, keep
     kept = None
     if keep:
         tokens = (x if isinstance(x, torch.Tensor) else x[0]).shape[0]
-        kept = Kept(*_new_kept(tokens, wg.shape[0], wg.device), *_new_kept(tokens, wg.shape[0], wg.device))
+        kept = Kept(*_new_kept(tokens, wg.shape[0], wg), *_new_kept(tokens, wg.shape[0], wg))
     d, tokens, _, hidden = _gated_desc(x, wg, wu, act, kept)
     if h is None:
-        h = _new_rows(tokens, hidden, wg.dtype, wg.device)
+        h = _new_rows(tokens, hidden, wg.dtype, wg)
     hp, ldh = _rows(h, "h", wg.dtype, (tokens, hidden))
     ref = ctypes.byref(d)
     ws, wp, wb = _ws(lib.detox_gated_workspace_bytes(ref), ws, wg.device)
@@ -705,12 +707,12 @@ def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor
     d, tokens, in_dim, hidden = _gated_desc(x, wg, wu, act, kept)
     dhp, lddh = _rows(dh, "dh", wg.dtype, (tokens, hidden))
     if dx is None:
-        dx = _new_rows(tokens, in_dim, wg.dtype, wg.device)
+        dx = _new_rows(tokens, in_dim, wg.dtype, wg)
     dxp, lddx = _rows(dx, "dx", wg.dtype, (tokens, in_dim))
     if (dwg is None) != (dwu is None):
         raise ValueError("give both weight gradients or none")
     if dwg is None:
-        dwg, dwu = (_new_rows(hidden, in_dim, dw_dtype or wg.dtype, wg.device) for _ in range(2))
+        dwg, dwu = (_new_rows(hidden, in_dim, dw_dtype or wg.dtype, wg) for _ in range(2))
     gp, lddw = _rows(dwg, "dwg", dw_dtype, (hidden, in_dim))
     up, ldu = _rows(dwu, "dwu", dwg.dtype, (hidden, in_dim))
     if ldu != lddw:

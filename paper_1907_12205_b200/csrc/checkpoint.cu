@@ -31,6 +31,8 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ X,
                                                         int nblk, uint8_t* __restrict__ Q, int64_t ldq,
                                                         uint8_t* __restrict__ E, int64_t lde) {
     constexpr int N = Piece<T>::N;
+    pdl_trigger();
+    pdl_wait();
     const int64_t groups = (int64_t)gridDim.x * (kThreads / kLanes);
     const int part = threadIdx.x % kLanes;
     const int64_t drow = groups / nblk;
@@ -82,6 +84,8 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const uint8_t* __restr
                                                           const uint8_t* __restrict__ E, int64_t lde, int64_t rows,
                                                           int64_t cols, int nblk, T* __restrict__ X, int64_t ld) {
     constexpr int N = Piece<T>::N;
+    pdl_trigger();
+    pdl_wait();
     const int64_t groups = (int64_t)gridDim.x * (kThreads / kLanes);
     const int part = threadIdx.x % kLanes;
     const int64_t drow = groups / nblk;
@@ -139,8 +143,7 @@ detox_status pack(const void* X, int64_t ld, int64_t rows, int64_t cols, uint8_t
     const int nblk = (int)ceil_div(cols, (int64_t)kKeepBlock);
     const bool vec = aligned16(X) && ld % Piece<T>::N == 0 && aligned16(Q) && ldq % 16 == 0;
     auto* k = vec ? pack_kernel<T, true> : pack_kernel<T, false>;
-    k<<<grid_for(rows, nblk), kThreads, 0, s>>>(static_cast<const T*>(X), ld, rows, cols, nblk, Q, ldq, E, lde);
-    return launch_status();
+    return launch_chained(k, grid_for(rows, nblk), kThreads, 0, 1, s, static_cast<const T*>(X), ld, rows, cols, nblk, Q, ldq, E, lde);
 }
 template <typename T>
 detox_status unpack(const uint8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t rows, int64_t cols, void* X,
@@ -148,8 +151,7 @@ detox_status unpack(const uint8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde
     const int nblk = (int)ceil_div(cols, (int64_t)kKeepBlock);
     const bool vec = aligned16(X) && ld % Piece<T>::N == 0 && aligned16(Q) && ldq % 16 == 0;
     auto* k = vec ? unpack_kernel<T, true> : unpack_kernel<T, false>;
-    k<<<grid_for(rows, nblk), kThreads, 0, s>>>(Q, ldq, E, lde, rows, cols, nblk, static_cast<T*>(X), ld);
-    return launch_status();
+    return launch_chained(k, grid_for(rows, nblk), kThreads, 0, 1, s, Q, ldq, E, lde, rows, cols, nblk, static_cast<T*>(X), ld);
 }
 
 }  // namespace

@@ -68,6 +68,7 @@ struct GemmArgs {
     int mt, nt;                    // output tiles (wgrad: mt counts those of dWg and of dWu)
     int kb0, kb1;                  // slices of the first and of the second product that are added up
     int split;                     // CTAs that share a tile's reduction
+    bool clear_status;             // first kernel of the call that may set the status word
     bool n_first;                  // neighbouring tiles lie along a row of the output (else along a column)
     int act;
     int64_t rows, cols;            // of the output (forward, recompute: of h)
@@ -337,12 +338,21 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         sm->abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == 0) tmem_alloc_cg<CG>(&sm->tmem_base, TL::tmem_cols);
+    if (warp == 1) tmem_alloc_cg<CG>(&sm->tmem_base, TL::tmem_cols);
     tc_fence_before();
-    __syncthreads();
-    if constexpr (CG == 2) cluster_sync();           // the other CTA's barriers are there before anything arrives on them
+    if constexpr (CG == 2) {
+        __syncthreads();
+        cluster_sync();                              // the other CTA's barriers are there before anything arrives on them
+    } else {
+        // the copies need only the barriers, which their own warp has set up: they start without waiting for the others
+        __syncwarp();
+        if (warp == 0) asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
+        else asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+    }
     tc_fence_after();
-    const uint32_t tmem = sm->tmem_base;
+    pdl_trigger();
+    pdl_wait();
+    if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it about a second later)
 
     // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
     const int unit_ctas = CG == 2 ? 2 : p.split;
@@ -430,6 +440,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                                        ((uint32_t)(TL::N >> 3) << 17) | ((uint32_t)(TL::M >> 4) << 24);
             // 16 steps of the reduction: 32 bytes along a K-major row, 16 rows of an MN-major chunk
             constexpr uint64_t kAstep = kAmn ? 16 * 128 / 16 : 2, kBstep = kBmn ? 16 * 128 / 16 : 2;
+            const uint32_t tmem = sm->tmem_base;
             int s = 0, buf = 0;
             uint32_t ph = 0, aph = 0;
             bool ok = true;
@@ -456,6 +467,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         __syncwarp();
     } else {
         // ---------------------------------------------------- epilogue: a thread has one row of the tile
+        const uint32_t tmem = sm->tmem_base;
         const int part = warp & 3;   // the 32 accumulator lanes that this warp may read
         int buf = 0;
         uint32_t ph = 0;
@@ -470,11 +482,13 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 // (the one tile of this cluster, all its MMAs done: the stages are free to take the sums)
                 const int m_out = FORM == kWgrad && m >= p.mt / 2 ? m - p.mt / 2 : m;
                 float* row = reinterpret_cast<float*>(stages) + (size_t)in_tile * TL::pitch;
+                const bool live = (int64_t)m_out * TL::M + in_tile < p.rows;
+                const int c_end = __any_sync(0xffffffffu, live) ? BN : 0;
 #pragma unroll 1
-                for (int c = 0; c < BN; c += 32) {
+                for (int c = 0; c < c_end; c += 32) {
                     float f[32];
                     tmem_load32(at + c, f);
-                    if ((int64_t)m_out * TL::M + in_tile < p.rows) {
+                    if (live) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             *reinterpret_cast<float4*>(row + c + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
@@ -646,89 +660,110 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
-    if (warp == 0) tmem_dealloc_cg<CG>(tmem, TL::tmem_cols);
+    if (warp == 1) tmem_dealloc_cg<CG>(sm->tmem_base, TL::tmem_cols);
 }
 
-// ---- dg and du from the kept g and u ------------------------------------------------------------
-// One pass: dh, both 8-bit matrices with their scales in, dg and du out.  A thread has 8 columns of a row.
-template <typename T>
-__global__ void __launch_bounds__(256) dgu_kernel(const T* __restrict__ dH, int64_t lddh, bool dh_vec,
-                                                  const uint8_t* __restrict__ GQ, const uint8_t* __restrict__ GE,
-                                                  const uint8_t* __restrict__ UQ, const uint8_t* __restrict__ UE, int64_t ldq,
-                                                  int64_t lde, bool q_vec, int act, int64_t rows, int64_t cols,
-                                                  T* __restrict__ dG, T* __restrict__ dU, int64_t ldo) {
-    const int64_t per_row = (cols + 7) / 8;
-    const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-    int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    int64_t row = item / per_row, k = item % per_row;
-    const int64_t drow = stride / per_row, dk = stride % per_row;
-    while (row < rows) {
-        const int64_t c = k * 8;
-        const bool full = c + 8 <= cols;
-        float dh[8], g[8], u[8];
-        if (full && dh_vec) {
-            Piece<T>::split(ld_stream_u4(dH + row * lddh + c), dh);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dh[i] = c + i < cols ? to_f32(dH[row * lddh + c + i]) : 0.f;
-        }
-        uint2 gq = make_uint2(0u, 0u), uq = make_uint2(0u, 0u);
-        if (full && q_vec) {
-            gq = __ldcs(reinterpret_cast<const uint2*>(GQ + row * ldq + c));
-            uq = __ldcs(reinterpret_cast<const uint2*>(UQ + row * ldq + c));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (c + i < cols) {
-                    const uint32_t a = (uint32_t)GQ[row * ldq + c + i] << (8 * (i % 4)), b = (uint32_t)UQ[row * ldq + c + i] << (8 * (i % 4));
-                    if (i < 4) { gq.x |= a; uq.x |= b; } else { gq.y |= a; uq.y |= b; }
-                }
-            }
-        }
-        const float gs = keep_scale_of_byte(GE[row * lde + c / kKeepBlock]), us = keep_scale_of_byte(UE[row * lde + c / kKeepBlock]);
-        float f[4];
-        taken4(gq.x, f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = f[i] * gs;
-        taken4(gq.y, f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[4 + i] = f[i] * gs;
-        taken4(uq.x, f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = f[i] * us;
-        taken4(uq.y, f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[4 + i] = f[i] * us;
-        by_act(act, DguOf<8>{g, u, dh});
-        // (the workspace rows are padded to whole pieces)
-        *reinterpret_cast<uint4*>(dG + row * ldo + c) = Piece<T>::join(g);
-        *reinterpret_cast<uint4*>(dU + row * ldo + c) = Piece<T>::join(u);
+// ---- what the backward pass lays out before its products -----------------------------------------
+// dg and du from the kept g and u, in one pass: dh and both 8-bit matrices with their scales in, dg and du out; and,
+// when the input comes in 8 bits, its entries for the weight gradients.  A thread has 8 columns of a row at a time.
+struct PrepareArgs {
+    const void* dh; int64_t lddh; bool dh_vec;
+    const uint8_t *gq, *ge, *uq, *ue;
+    int64_t ldq, lde;
+    bool q_vec;
+    int act;
+    int64_t rows, cols;
+    void *dg, *du;
+    int64_t ldo;
+    const uint8_t *xq, *xe;        // null: nothing to lay out
+    int64_t ldxq, ldxe;
+    bool xq_vec;
+    int64_t x_cols;
+    void* x; int64_t ldx;
+};
+
+// The pieces of 8 columns of a matrix, dealt to the threads of the grid; the row is carried along, not divided out.
+struct Pieces {
+    int64_t row, k, drow, dk, per_row;
+    __device__ __forceinline__ explicit Pieces(int64_t cols) : per_row((cols + 7) / 8) {
+        const int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, stride = (int64_t)gridDim.x * blockDim.x;
+        row = item / per_row;
+        k = item % per_row;
+        drow = stride / per_row;
+        dk = stride % per_row;
+    }
+    __device__ __forceinline__ void next() {
         row += drow;
         k += dk;
         if (k >= per_row) { k -= per_row; ++row; }
+    }
+};
+// 8 bytes of a row of 8-bit entries, zeros beyond its end
+__device__ __forceinline__ uint2 load8(const uint8_t* row, int64_t c, int64_t cols, bool vec) {
+    if (vec && c + 8 <= cols) return __ldcs(reinterpret_cast<const uint2*>(row + c));
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) w[i / 4] |= (uint32_t)row[c + i] << (8 * (i % 4));
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void taken8(uint2 q, uint8_t e, float (&f)[8]) {
+    const float scale = keep_scale_of_byte(e);
+    float lo[4], hi[4];
+    taken4(q.x, lo);
+    taken4(q.y, hi);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] = lo[i] * scale; f[4 + i] = hi[i] * scale; }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) gated_prepare_kernel(const __grid_constant__ PrepareArgs p) {
+    pdl_trigger();
+    pdl_wait();
+    for (Pieces it(p.cols); it.row < p.rows; it.next()) {
+        const int64_t c = it.k * 8;
+        const T* dh_row = static_cast<const T*>(p.dh) + it.row * p.lddh;
+        float dh[8], g[8], u[8];
+        if (p.dh_vec && c + 8 <= p.cols) {
+            Piece<T>::split(ld_stream_u4(dh_row + c), dh);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dh[i] = c + i < p.cols ? to_f32(dh_row[c + i]) : 0.f;
+        }
+        const int64_t at = it.row * p.ldq, block = it.row * p.lde + c / kKeepBlock;
+        taken8(load8(p.gq + at, c, p.cols, p.q_vec), p.ge[block], g);
+        taken8(load8(p.uq + at, c, p.cols, p.q_vec), p.ue[block], u);
+        by_act(p.act, DguOf<8>{g, u, dh});
+        // (the workspace rows are padded to whole pieces)
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.dg) + it.row * p.ldo + c) = Piece<T>::join(g);
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.du) + it.row * p.ldo + c) = Piece<T>::join(u);
+    }
+    if (!p.xq) return;
+    for (Pieces it(p.x_cols); it.row < p.rows; it.next()) {
+        const int64_t c = it.k * 8;
+        float x[8];
+        taken8(load8(p.xq + it.row * p.ldxq, c, p.x_cols, p.xq_vec), p.xe[it.row * p.ldxe + c / kKeepBlock], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = taken_clamp<T>(x[i]);
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.x) + it.row * p.ldx + c) = Piece<T>::join(x);
     }
 }
 
 // A matrix that TMA cannot address, copied to 16-byte aligned rows.
 __global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restrict__ X, int64_t ld, int64_t rows,
                                                          int64_t cols, uint16_t* __restrict__ Y, int64_t ldy) {
-    const int64_t per_row = (cols + 7) / 8;
-    const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-    int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    int64_t row = item / per_row, k = item % per_row;
-    const int64_t drow = stride / per_row, dk = stride % per_row;
-    while (row < rows) {
-        const int64_t c = k * 8;
+    pdl_trigger();
+    pdl_wait();
+    for (Pieces it(cols); it.row < rows; it.next()) {
+        const int64_t c = it.k * 8;
+        const uint16_t* x = X + it.row * ld;
         uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = c + 2 * i < cols ? X[row * ld + c + 2 * i] : 0u, hi = c + 2 * i + 1 < cols ? X[row * ld + c + 2 * i + 1] : 0u;
+            const uint32_t lo = c + 2 * i < cols ? x[c + 2 * i] : 0u, hi = c + 2 * i + 1 < cols ? x[c + 2 * i + 1] : 0u;
             v[i] = lo | (hi << 16);
         }
-        *reinterpret_cast<uint4*>(Y + row * ldy + c) = make_uint4(v[0], v[1], v[2], v[3]);
-        row += drow;
-        k += dk;
-        if (k >= per_row) { k -= per_row; ++row; }
+        *reinterpret_cast<uint4*>(Y + it.row * ldy + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
 
@@ -772,10 +807,9 @@ unsigned items_grid(int64_t items) {
 }
 
 detox_status aligned_copy(const void* X, int64_t ld, int64_t rows, int64_t cols, void* to, Mat* out, cudaStream_t s) {
-    align_rows_kernel<<<items_grid(rows * ceil_div(cols, (int64_t)8)), 256, 0, s>>>(
-        static_cast<const uint16_t*>(X), ld, rows, cols, static_cast<uint16_t*>(to), padded(cols));
     *out = Mat{to, padded(cols)};
-    return launch_status();
+    return launch_chained(align_rows_kernel, items_grid(rows * ceil_div(cols, (int64_t)8)), 256, 0, 1, s,
+                          static_cast<const uint16_t*>(X), ld, rows, cols, static_cast<uint16_t*>(to), padded(cols));
 }
 
 detox_status input_matrix(const detox_gated_desc& g, const GatedPlan& q, char* ws, Mat* out, cudaStream_t s) {
@@ -798,19 +832,37 @@ detox_status weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char
     return DETOX_OK;
 }
 
-// Which shape a product of `rows` x `cols` (of the accumulator: forward and recompute have 2 x hidden columns) with nkb
-// slices takes.
+// Which shape a product takes: rows x cols is the accumulator (forward and recompute have 2 x hidden columns), nkb the slices of
+// its reduction.  The least of an estimate, in units of 10 ns, that was fitted to measurements of every shape:
+//   a slice        pair 28: the MMAs' own rate.  128 x 256 on one CTA 42, 128 x 128 27: a CTA takes in about 64 bytes a clock,
+//                  and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.  With one row of tiles every
+//                  byte of the weights comes from HBM for a single use, and the narrow tile is no faster (42).
+//   a tile         150 (drain of the last accumulator), 500 with a split (the cluster meets twice, sums move)
+//   a launch       500
+// The number of clusters that fit at once is that of a B200 (2 dies, GPCs of 14 to 20 SMs); it is a constant, so that
+// every GPU takes the same shape and gives the same bits.
 struct Shape {
     int cg, bn, split;
 };
 Shape gemm_shape(int64_t rows, int64_t cols, int nkb, bool keeps) {
-    (void)keeps;
-    const int64_t tiles = ceil_div(rows, (int64_t)128) * ceil_div(cols, (int64_t)256);
-    if (tiles >= kSMs) return Shape{2, 256, 1};
-    int split = (int)(kSMs / tiles);
-    if (split > kMaxSplit) split = kMaxSplit;
-    if (split > nkb) split = nkb;
-    return Shape{1, 256, split};
+    static const int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
+    Shape best{2, 256, 1};
+    int64_t least = INT64_MAX;
+    auto consider = [&](int cg, int bn, int split, int64_t slice) {
+        const int64_t tiles = ceil_div(rows, (int64_t)(128 * cg)) * ceil_div(cols, (int64_t)bn);
+        const int64_t waves = ceil_div(tiles, (int64_t)kClusters[cg * split]);
+        const int64_t time = waves * (ceil_div((int64_t)nkb, (int64_t)split) * slice + (split > 1 ? 500 : 150)) + 500;
+        if (time < least) {
+            least = time;
+            best = Shape{cg, bn, split};
+        }
+    };
+    consider(2, 256, 1, 28);
+    for (int split = 1; split <= kMaxSplit && split <= nkb; ++split) {
+        consider(1, 256, split, 42);
+        if (!keeps) consider(1, 128, split, rows <= 128 ? 42 : 27);   // (the 8-bit form needs a block of 128 columns in a tile)
+    }
+    return best;
 }
 
 // One product: maps, grid, launch.  The matrices of the maps are rows x cols.
@@ -825,9 +877,10 @@ detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, con
     constexpr bool kGated = FORM == kForward || FORM == kRecompute;
     // boxes of 64 columns: 128 rows of A and as many of the weights as a tile has columns of g, or 64 steps of the reduction
     const int box_a = FORM == kWgrad ? 64 : 128, box_b = kGated ? BN / 2 : 64;
-    CUtensorMap maps[4];
+    CUtensorMap maps[4] = {};
     const MapOf* of[4] = {&a0, &a1, &b0, &b1};
     for (int i = 0; i < 4; ++i) {
+        if ((kGated && i == 1) || (FORM == kWgrad && i == 3)) continue;   // not read
         const detox_status st = make_map_16bit(&maps[i], std::is_same<T, __nv_bfloat16>::value, of[i]->m.p, of[i]->m.ld, of[i]->rows,
                                                of[i]->cols, i < 2 ? box_a : box_b);
         if (st != DETOX_OK) return st;
@@ -844,22 +897,8 @@ detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, con
     const int unit = CG == 2 ? 2 : split;
     // a split's cluster finishes one tile; the others' grids are persistent
     const int64_t units = split > 1 || tiles < kSMs / unit ? tiles : kSMs / unit;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * unit));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes<CG, BN>;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)unit;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, k, maps[0], maps[1], maps[2], maps[3], args, status) != cudaSuccess) {
-        launch_status();
-        return DETOX_ERR_CUDA;
-    }
-    return launch_status();
+    return launch_chained(k, (unsigned)(units * unit), kThreads, kSmemBytes<CG, BN>, (unsigned)unit, s, maps[0], maps[1], maps[2],
+                          maps[3], args, status);
 }
 template <typename T, typename OT, int FORM>
 detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, int* status,
@@ -875,12 +914,12 @@ template <typename T>
 detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, cudaStream_t s) {
     const GatedPlan q = gated_plan(g, false);
     int* status = reinterpret_cast<int*>(ws);
-    if (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess) return DETOX_ERR_CUDA;
     Mat x, wg, wu;
     detox_status st = input_matrix(g, q, ws, &x, s);
     if (st == DETOX_OK) st = weight_matrices(g, q, ws, &wg, &wu, s);
     if (st != DETOX_OK) return st;
     GemmArgs a{};
+    a.clear_status = true;
     a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
     a.act = g.act;
     a.rows = g.tokens;
@@ -897,8 +936,9 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
 
 template <typename T, typename OT>
 detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Mat& du, const Mat& x, void* dWg, void* dWu,
-                              int64_t lddw, int* status, cudaStream_t s) {
+                              int64_t lddw, bool clear_status, int* status, cudaStream_t s) {
     GemmArgs a{};
+    a.clear_status = clear_status;
     a.kb0 = (int)ceil_div(g.tokens, (int64_t)kSlice);
     a.rows = g.hidden;
     a.cols = g.in_dim;
@@ -915,23 +955,35 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
                       int64_t lddw, int dw_dtype, char* ws, cudaStream_t s) {
     const GatedPlan q = gated_plan(g, true);
     int* status = reinterpret_cast<int*>(ws);
-    if (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess) return DETOX_ERR_CUDA;
     const bool kept = g.GQ != nullptr;
     const int64_t ldf = padded(g.hidden);
     const Mat dg{ws + q.dg, ldf}, du{ws + q.du, ldf};
     Mat x{nullptr, 0}, wg{nullptr, 0}, wu{nullptr, 0};
     detox_status st = DETOX_OK;
-    if (dWg || !kept) st = input_matrix(g, q, ws, &x, s);
+    const bool with_x = kept && !g.X && dWg;         // an 8-bit input, laid out in the pass that makes dg and du
+    if (with_x) x = Mat{ws + q.x, padded(g.in_dim)};
+    else if (dWg || !kept) st = input_matrix(g, q, ws, &x, s);
     if (st == DETOX_OK && (dX || !kept)) st = weight_matrices(g, q, ws, &wg, &wu, s);
     if (st != DETOX_OK) return st;
     if (kept) {
-        const bool q_vec = aligned_to(g.GQ, 8) && aligned_to(g.UQ, 8) && g.ldq % 8 == 0;
-        dgu_kernel<T><<<items_grid(g.tokens * ceil_div(g.hidden, (int64_t)8)), 256, 0, s>>>(
-            static_cast<const T*>(dH), lddh, tma_ok(dH, lddh), g.GQ, g.GE, g.UQ, g.UE, g.ldq, g.lde, q_vec, g.act, g.tokens,
-            g.hidden, static_cast<T*>(const_cast<void*>(dg.p)), static_cast<T*>(const_cast<void*>(du.p)), ldf);
-        st = launch_status();
+        PrepareArgs a{};
+        a.dh = dH; a.lddh = lddh; a.dh_vec = tma_ok(dH, lddh);
+        a.gq = g.GQ; a.ge = g.GE; a.uq = g.UQ; a.ue = g.UE;
+        a.ldq = g.ldq; a.lde = g.lde;
+        a.q_vec = aligned_to(g.GQ, 8) && aligned_to(g.UQ, 8) && g.ldq % 8 == 0;
+        a.act = g.act;
+        a.rows = g.tokens; a.cols = g.hidden;
+        a.dg = const_cast<void*>(dg.p); a.du = const_cast<void*>(du.p); a.ldo = ldf;
+        if (with_x) {
+            a.xq = g.XQ; a.xe = g.XE; a.ldxq = g.ldxq; a.ldxe = g.ldxe;
+            a.xq_vec = aligned_to(g.XQ, 8) && g.ldxq % 8 == 0;
+            a.x_cols = g.in_dim;
+            a.x = const_cast<void*>(x.p); a.ldx = x.ld;
+        }
+        st = launch_chained(gated_prepare_kernel<T>, items_grid(g.tokens * ceil_div(g.hidden, (int64_t)8)), 256, 0, 1, s, a);
     } else {
         GemmArgs a{};
+        a.clear_status = true;
         a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
         a.act = g.act;
         a.rows = g.tokens;
@@ -948,6 +1000,7 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
     if (st != DETOX_OK) return st;
     if (dX) {
         GemmArgs a{};
+        a.clear_status = kept;
         a.kb0 = a.kb1 = (int)ceil_div(g.hidden, (int64_t)kSlice);
         a.rows = g.tokens;
         a.cols = g.in_dim;
@@ -960,8 +1013,8 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         if (st != DETOX_OK) return st;
     }
     if (!dWg) return DETOX_OK;
-    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, status, s);
-    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, status, s);
+    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, status, s);
+    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, status, s);
 }
 
 }  // namespace

@@ -79,6 +79,8 @@ __global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_kernel(const T* X, int6
                                                                        float eps, NormOut o) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
+    pdl_trigger();
+    pdl_wait();
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     if (TPR == 32 && row >= rows) return;   // (TPR > 32: a CTA per row, all of them there)
@@ -159,6 +161,8 @@ __global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_backward_kernel(
     const float* __restrict__ rstd_of, int64_t rows, int64_t cols, T* dX, int64_t lddx, float* __restrict__ parts) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
+    pdl_trigger();
+    pdl_wait();
     const int t = threadIdx.x % TPR;
     const float inv_cols = 1.f / (float)cols;
     float acc[P][N];
@@ -245,6 +249,8 @@ __global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_backward_kernel(
 __global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ parts, int nparts, int64_t cols,
                                                           float* __restrict__ dw) {
     __shared__ float sm[32][33];
+    pdl_trigger();
+    pdl_wait();
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + x;
     float sum = 0.f;
@@ -294,9 +300,9 @@ struct Fwd {
     template <int TPR, int EPT>
     detox_status operator()() const {
         constexpr int RPB = kBlockOf<TPR> / TPR;
-        rmsnorm_kernel<T, TPR, EPT, VEC><<<(unsigned)ceil_div(rows, (int64_t)RPB), kBlockOf<TPR>, 0, s>>>(
-            static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows, cols, eps, o);
-        return launch_status();
+        return launch_chained(rmsnorm_kernel<T, TPR, EPT, VEC>, (unsigned)ceil_div(rows, (int64_t)RPB), kBlockOf<TPR>, 0, 1, s,
+                              static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows, cols,
+                              eps, o);
     }
 };
 
@@ -307,10 +313,9 @@ struct Bwd {
     cudaStream_t s;
     template <int TPR, int EPT>
     detox_status operator()() const {
-        rmsnorm_backward_kernel<T, TPR, EPT, VEC><<<(unsigned)nparts, kBlockOf<TPR>, 0, s>>>(
-            static_cast<const T*>(b.dY), b.lddy, static_cast<const T*>(b.dS), b.ldds, static_cast<const T*>(b.S), b.lds,
-            static_cast<const T*>(b.w), b.rstd, b.rows, b.cols, static_cast<T*>(b.dX), b.lddx, b.parts);
-        return launch_status();
+        return launch_chained(rmsnorm_backward_kernel<T, TPR, EPT, VEC>, (unsigned)nparts, kBlockOf<TPR>, 0, 1, s,
+                              static_cast<const T*>(b.dY), b.lddy, static_cast<const T*>(b.dS), b.ldds, static_cast<const T*>(b.S),
+                              b.lds, static_cast<const T*>(b.w), b.rstd, b.rows, b.cols, static_cast<T*>(b.dX), b.lddx, b.parts);
     }
 };
 
@@ -373,8 +378,7 @@ detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, co
     else if (dtype == DETOX_DTYPE_HALF) st = backward<__half>(b, nparts, s);
     else st = backward<__nv_bfloat16>(b, nparts, s);
     if (st != DETOX_OK || !dw) return st;
-    rmsnorm_dw_kernel<<<(unsigned)ceil_div(cols, (int64_t)32), 1024, 0, s>>>(parts, nparts, cols, dw);
-    return launch_status();
+    return launch_chained(rmsnorm_dw_kernel, (unsigned)ceil_div(cols, (int64_t)32), 1024, 0, 1, s, parts, nparts, cols, dw);
 }
 
 }  // namespace detox

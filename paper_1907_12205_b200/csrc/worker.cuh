@@ -108,6 +108,33 @@ template <> __device__ __forceinline__ float taken_clamp<__half>(float v) {
     return v > 65504.f ? 65504.f : (v < -65504.f ? -65504.f : v);
 }
 
+// ---- launches that overlap the end of the kernel before them -------------------------------------
+// A step is a chain of short kernels, so each is launched while the one before it drains: its setup (barriers, tensor
+// memory) runs early, and pdl_wait holds it until everything before it in the stream has finished and is visible.
+// pdl_trigger lets the next one in as soon as all of this kernel's CTAs have started.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+detox_status launch_chained(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t s,
+                            const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
+    return launch_status() == DETOX_OK && ok ? DETOX_OK : DETOX_ERR_CUDA;
+}
+
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // ---- launchers (each enqueues on `s`; none synchronises) ---------------------------------------
