@@ -504,23 +504,41 @@ class RmsNorm(NamedTuple):
 
 
 class Kept(NamedTuple):
-    """g and u of a gated pair of projections in the 8-bit form (values, scales)."""
-    gq: torch.Tensor
-    ge: torch.Tensor
-    uq: torch.Tensor
-    ue: torch.Tensor
+    """g and u of a gated pair of projections in the 8-bit form: values [2, tokens, hidden], scales [2, tokens, blocks]."""
+    q: torch.Tensor
+    e: torch.Tensor
+
+    @property
+    def gq(self):
+        return self.q[0]
+
+    @property
+    def ge(self):
+        return self.e[0]
+
+    @property
+    def uq(self):
+        return self.q[1]
+
+    @property
+    def ue(self):
+        return self.e[1]
 
 
 def _rows(t: torch.Tensor, what: str, dtype=None, shape=None):
     """(pointer, row stride) of a matrix with contiguous rows, after checking its type and shape."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+    try:
+        rows, cols = t.shape
+        ld, step = t.stride()
+        here = t.is_cuda
+    except (AttributeError, ValueError, TypeError):
+        here = False
+    if not here:
         raise TypeError(f"{what}: expected a 2-D CUDA tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
-    rows, cols = t.shape
     if shape is not None and (rows, cols) != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {(rows, cols)}")
-    ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: rows must be contiguous")
     if ld < cols:
@@ -531,9 +549,16 @@ def _rows(t: torch.Tensor, what: str, dtype=None, shape=None):
 
 
 def _dtype_code(dtype, what: str) -> int:
-    if dtype not in _DTYPE:
+    code = _DTYPE.get(dtype)
+    if code is None:
         raise TypeError(f"{what}: expected float32, float16 or bfloat16, got {dtype}")
-    return _DTYPE[dtype]
+    return code
+
+
+def _vector(t: torch.Tensor, what: str, dtype, n: int) -> int:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()):
+        raise TypeError(f"{what}: expected a contiguous CUDA vector of {n} entries of {dtype}")
+    return t.data_ptr()
 
 
 def _blocks(cols: int) -> int:
@@ -542,20 +567,30 @@ def _blocks(cols: int) -> int:
 
 def _kept_pair(q, e, what: str, shape=None):
     qp, ldq = _rows(q, what, torch.float8_e4m3fn, shape)
-    ep, lde = _rows(e, what + " scales", torch.float8_e8m0fnu, (q.shape[0], _blocks(q.shape[1])))
+    rows, cols = q.shape
+    ep, lde = _rows(e, what + " scales", torch.float8_e8m0fnu, (rows, _blocks(cols)))
     return qp, ldq, ep, lde
 
 
 def _new_rows(rows: int, cols: int, dtype, like: torch.Tensor):
-    """A matrix whose rows lie a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses."""
+    """(matrix, pointer, stride): rows a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses."""
     n = 16 // dtype.itemsize
-    if cols % n == 0:
-        return like.new_empty((rows, cols), dtype=dtype)
-    return like.new_empty((rows, -(-cols // n) * n), dtype=dtype)[:, :cols]
+    ld = -(-cols // n) * n
+    t = like.new_empty((rows, ld), dtype=dtype)
+    return (t if ld == cols else t[:, :cols]), t.data_ptr(), ld
 
 
 def _new_kept(rows: int, cols: int, like: torch.Tensor):
-    return _new_rows(rows, cols, torch.float8_e4m3fn, like), like.new_empty((rows, _blocks(cols)), dtype=torch.float8_e8m0fnu)
+    q, qp, ldq = _new_rows(rows, cols, torch.float8_e4m3fn, like)
+    lde = _blocks(cols)
+    e = like.new_empty((rows, lde), dtype=torch.float8_e8m0fnu)
+    return q, e, (qp, ldq, e.data_ptr(), lde)
+
+
+def _workspace(nbytes: int, ws: Optional[torch.Tensor], like: torch.Tensor):
+    if ws is None:
+        ws = like.new_empty((max(int(nbytes), 256),), dtype=torch.uint8)
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
@@ -564,8 +599,11 @@ def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
     xp, ld = _rows(x, "x")
     code = _dtype_code(x.dtype, "x")
     rows, cols = x.shape
-    q, e = _new_kept(rows, cols, x) if out is None else out
-    qp, ldq, ep, lde = _kept_pair(q, e, "out", (rows, cols))
+    if out is None:
+        q, e, (qp, ldq, ep, lde) = _new_kept(rows, cols, x)
+    else:
+        q, e = out
+        qp, ldq, ep, lde = _kept_pair(q, e, "out", (rows, cols))
     _check(load().detox_checkpoint_pack(code, xp, ld, rows, cols, qp, ldq, ep, lde, _stream(stream)), "detox_checkpoint_pack")
     return q, e
 
@@ -575,10 +613,11 @@ def detox_checkpoint_unpack(q: torch.Tensor, e: torch.Tensor, dtype=torch.bfloat
     """The way back from detox_checkpoint_pack: rows of `dtype`."""
     qp, ldq, ep, lde = _kept_pair(q, e, "q")
     rows, cols = q.shape
+    code = _dtype_code(dtype if out is None else out.dtype, "out")
     if out is None:
-        out = _new_rows(rows, cols, dtype, q)
-    code = _dtype_code(out.dtype, "out")
-    xp, ld = _rows(out, "out", None, (rows, cols))
+        out, xp, ld = _new_rows(rows, cols, dtype, q)
+    else:
+        xp, ld = _rows(out, "out", None, (rows, cols))
     _check(load().detox_checkpoint_unpack(code, qp, ldq, ep, lde, rows, cols, xp, ld, _stream(stream)), "detox_checkpoint_unpack")
     return out
 
@@ -588,27 +627,27 @@ def detox_rmsnorm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Ten
     """s = x + residual, y = s / rms(s) * w.  want_q: y also (want_y=False: only) in the 8-bit form.  The sum comes back
     when there is a residual, in sum_out when given (which may be x or residual itself)."""
     xp, ldx = _rows(x, "x")
-    code = _dtype_code(x.dtype, "x")
+    dtype = x.dtype
+    code = _dtype_code(dtype, "x")
     shape = rows, cols = tuple(x.shape)
-    if not (w.is_cuda and w.dtype == x.dtype and w.shape == (cols,) and w.is_contiguous()):
-        raise TypeError("w: expected a contiguous vector of x's type with an entry for each column")
-    rp = sp = yp = qp = ep = None
+    wp = _vector(w, "w", dtype, cols)
+    rp = sp = yp = qp = ep = s = y = q = e = None
     ldr = lds = ldy = ldq = lde = 0
-    s = y = q = e = None
     if residual is not None:
-        rp, ldr = _rows(residual, "residual", x.dtype, shape)
-        s = _new_rows(rows, cols, x.dtype, x) if sum_out is None else sum_out
-        sp, lds = _rows(s, "sum_out", x.dtype, shape)
+        rp, ldr = _rows(residual, "residual", dtype, shape)
+        if sum_out is None:
+            s, sp, lds = _new_rows(rows, cols, dtype, x)
+        else:
+            s = sum_out
+            sp, lds = _rows(s, "sum_out", dtype, shape)
     elif sum_out is not None:
         raise ValueError("sum_out: there is no residual to add")
     if want_y:
-        y = _new_rows(rows, cols, x.dtype, x)
-        yp, ldy = y.data_ptr(), max(y.stride(0), cols)
+        y, yp, ldy = _new_rows(rows, cols, dtype, x)
     if want_q:
-        q, e = _new_kept(rows, cols, x)
-        qp, ldq, ep, lde = q.data_ptr(), max(q.stride(0), cols), e.data_ptr(), max(e.stride(0), 1)
-    rstd = x.new_empty(rows, dtype=torch.float32)
-    _check(load().detox_rmsnorm(code, xp, ldx, rp, ldr, w.data_ptr(), rows, cols, eps, sp, lds, yp, ldy, qp, ldq, ep, lde,
+        q, e, (qp, ldq, ep, lde) = _new_kept(rows, cols, x)
+    rstd = x.new_empty((rows,), dtype=torch.float32)
+    _check(load().detox_rmsnorm(code, xp, ldx, rp, ldr, wp, rows, cols, eps, sp, lds, yp, ldy, qp, ldq, ep, lde,
                                 rstd.data_ptr(), _stream(stream)), "detox_rmsnorm")
     return RmsNorm(s, y, q, e, rstd)
 
@@ -623,50 +662,56 @@ def detox_rmsnorm_backward(dy: torch.Tensor, s: torch.Tensor, w: torch.Tensor, r
     """Gradients of detox_rmsnorm: (dx, dw).  s: the sum of the forward pass (its x when there was no residual); ds: the
     gradient that reaches the sum by its other uses.  dx is also the residual's gradient; dw is fp32."""
     lib = load()
-    code = _dtype_code(s.dtype, "s")
     sp, lds = _rows(s, "s")
+    dtype = s.dtype
+    code = _dtype_code(dtype, "s")
     shape = rows, cols = tuple(s.shape)
-    dyp, lddy = _rows(dy, "dy", s.dtype, shape)
-    dsp, ldds = (None, 0) if ds is None else _rows(ds, "ds", s.dtype, shape)
-    if not (w.is_cuda and w.dtype == s.dtype and w.shape == (cols,) and w.is_contiguous()):
-        raise TypeError("w: expected a contiguous vector of s's type with an entry for each column")
-    if not (rstd.is_cuda and rstd.dtype == torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous()):
-        raise TypeError("rstd: expected a contiguous float32 vector with an entry for each row")
+    dyp, lddy = _rows(dy, "dy", dtype, shape)
+    dsp, ldds = (None, 0) if ds is None else _rows(ds, "ds", dtype, shape)
+    wp, rp = _vector(w, "w", dtype, cols), _vector(rstd, "rstd", torch.float32, rows)
     if dx is None:
-        dx = _new_rows(rows, cols, s.dtype, s)
-    dxp, lddx = _rows(dx, "dx", s.dtype, shape)
+        dx, dxp, lddx = _new_rows(rows, cols, dtype, s)
+    else:
+        dxp, lddx = _rows(dx, "dx", dtype, shape)
     if dw is None:
-        dw = s.new_empty(cols, dtype=torch.float32)
-    elif not (dw.is_cuda and dw.dtype == torch.float32 and dw.shape == (cols,) and dw.is_contiguous()):
-        raise TypeError("dw: expected a contiguous float32 vector with an entry for each column")
-    ws, wp, wb = _ws(lib.detox_rmsnorm_backward_workspace_bytes(rows, cols), ws, s.device)
-    _check(lib.detox_rmsnorm_backward(code, dyp, lddy, dsp, ldds, sp, lds, w.data_ptr(), rstd.data_ptr(), rows, cols, dxp, lddx,
-                                      dw.data_ptr(), wp, wb, _stream(stream)), "detox_rmsnorm_backward")
+        dw = s.new_empty((cols,), dtype=torch.float32)
+    dwp = _vector(dw, "dw", torch.float32, cols)
+    ws, wsp, wb = _workspace(lib.detox_rmsnorm_backward_workspace_bytes(rows, cols), ws, s)
+    _check(lib.detox_rmsnorm_backward(code, dyp, lddy, dsp, ldds, sp, lds, wp, rp, rows, cols, dxp, lddx, dwp, wsp, wb,
+                                      _stream(stream)), "detox_rmsnorm_backward")
     return dx, dw
 
 
 def _gated_desc(x, wg, wu, act: int, kept: Optional[Kept]):
-    """The descriptor; x is a matrix or its 8-bit form (q, e).  Returns (desc, dtype, tokens, in_dim, hidden, device)."""
-    d = GatedDesc()
-    d.Wg, d.ldwg = _rows(wg, "wg")
-    d.Wu, d.ldwu = _rows(wu, "wu", wg.dtype, tuple(wg.shape))
-    hidden, in_dim = wg.shape
-    d.dtype, d.act = _dtype_code(wg.dtype, "wg"), int(act)
+    """(descriptor, tokens, in_dim, hidden); x is a matrix or its 8-bit form (q, e)."""
+    dtype = wg.dtype
+    wgp, ldwg = _rows(wg, "wg")
+    shape = hidden, in_dim = tuple(wg.shape)
+    wup, ldwu = _rows(wu, "wu", dtype, shape)
+    xp = xq = xe = kg = ke = ku = kf = None
+    ldx = ldxq = ldxe = ldq = lde = 0
     if isinstance(x, torch.Tensor):
-        d.X, d.ldx = _rows(x, "x", wg.dtype)
+        xp, ldx = _rows(x, "x", dtype)
         tokens, cols = x.shape
     else:
         q, e = x
-        d.XQ, d.ldxq, d.XE, d.ldxe = _kept_pair(q, e, "x")
+        xq, ldxq, xe, ldxe = _kept_pair(q, e, "x")
         tokens, cols = q.shape
     if cols != in_dim:
         raise ValueError(f"x has {cols} columns, the weights {in_dim}")
-    d.tokens, d.in_dim, d.hidden = tokens, in_dim, hidden
     if kept is not None:
-        d.GQ, d.ldq, d.GE, d.lde = _kept_pair(kept.gq, kept.ge, "kept g", (tokens, hidden))
-        d.UQ, ldq, d.UE, lde = _kept_pair(kept.uq, kept.ue, "kept u", (tokens, hidden))
-        if (ldq, lde) != (d.ldq, d.lde):
-            raise ValueError("kept g and u must have the same strides")
+        q, e = kept
+        if not (q.is_cuda and e.is_cuda and q.dtype == torch.float8_e4m3fn and e.dtype == torch.float8_e8m0fnu):
+            raise TypeError("kept: expected float8_e4m3fn values and float8_e8m0fnu scales on the GPU")
+        if q.shape != (2, tokens, hidden) or e.shape != (2, tokens, _blocks(hidden)):
+            raise ValueError(f"kept: expected values [2, {tokens}, {hidden}] and their scales")
+        (half_q, ldq, step_q), (half_e, lde, step_e) = q.stride(), e.stride()
+        if (step_q != 1 and hidden > 1) or (step_e != 1 and e.shape[2] > 1):
+            raise ValueError("kept: rows must be contiguous")
+        kg, ke = q.data_ptr(), e.data_ptr()
+        ku, kf = kg + half_q, ke + half_e
+    d = GatedDesc(_dtype_code(dtype, "wg"), int(act), tokens, in_dim, hidden, xp, ldx, xq, ldxq, xe, ldxe, wgp, ldwg, wup, ldwu,
+                  kg, ke, ku, kf, ldq, lde)
     return d, tokens, in_dim, hidden
 
 
@@ -679,16 +724,20 @@ def detox_gated(x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU, keep
     """h = act(x wg^T) * (x wu^T).  x: a matrix, or its 8-bit form as a pair (q, e).  keep=True returns (h, Kept): g and u
     in the 8-bit form for the backward pass."""
     lib = load()
-    kept = None
+    d, tokens, _, hidden = _gated_desc(x, wg, wu, act, None)
     if keep:
-        tokens = (x if isinstance(x, torch.Tensor) else x[0]).shape[0]
-        kept = Kept(*_new_kept(tokens, wg.shape[0], wg), *_new_kept(tokens, wg.shape[0], wg))
-    d, tokens, _, hidden = _gated_desc(x, wg, wu, act, kept)
+        d.ldq, d.lde = ldq, lde = -(-hidden // 16) * 16, _blocks(hidden)
+        q = wg.new_empty((2, tokens, ldq), dtype=torch.float8_e4m3fn)
+        e = wg.new_empty((2, tokens, lde), dtype=torch.float8_e8m0fnu)
+        d.GQ, d.GE = qp, ep = q.data_ptr(), e.data_ptr()
+        d.UQ, d.UE = qp + tokens * ldq, ep + tokens * lde
+        kept = Kept(q if ldq == hidden else q[:, :, :hidden], e)
     if h is None:
-        h = _new_rows(tokens, hidden, wg.dtype, wg)
-    hp, ldh = _rows(h, "h", wg.dtype, (tokens, hidden))
+        h, hp, ldh = _new_rows(tokens, hidden, wg.dtype, wg)
+    else:
+        hp, ldh = _rows(h, "h", wg.dtype, (tokens, hidden))
     ref = ctypes.byref(d)
-    ws, wp, wb = _ws(lib.detox_gated_workspace_bytes(ref), ws, wg.device)
+    ws, wp, wb = _workspace(lib.detox_gated_workspace_bytes(ref), ws, wg)
     _check(lib.detox_gated(ref, hp, ldh, wp, wb, _stream(stream)), "detox_gated")
     return (h, kept) if keep else h
 
@@ -705,20 +754,24 @@ def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor
     pieces of a gradient's row)."""
     lib = load()
     d, tokens, in_dim, hidden = _gated_desc(x, wg, wu, act, kept)
-    dhp, lddh = _rows(dh, "dh", wg.dtype, (tokens, hidden))
+    dtype, shape = wg.dtype, (hidden, in_dim)
+    dhp, lddh = _rows(dh, "dh", dtype, (tokens, hidden))
     if dx is None:
-        dx = _new_rows(tokens, in_dim, wg.dtype, wg)
-    dxp, lddx = _rows(dx, "dx", wg.dtype, (tokens, in_dim))
+        dx, dxp, lddx = _new_rows(tokens, in_dim, dtype, wg)
+    else:
+        dxp, lddx = _rows(dx, "dx", dtype, (tokens, in_dim))
     if (dwg is None) != (dwu is None):
         raise ValueError("give both weight gradients or none")
     if dwg is None:
-        dwg, dwu = (_new_rows(hidden, in_dim, dw_dtype or wg.dtype, wg) for _ in range(2))
-    gp, lddw = _rows(dwg, "dwg", dw_dtype, (hidden, in_dim))
-    up, ldu = _rows(dwu, "dwu", dwg.dtype, (hidden, in_dim))
-    if ldu != lddw:
-        raise ValueError("dwg and dwu must have the same stride")
+        dwg, gp, lddw = _new_rows(hidden, in_dim, dw_dtype or dtype, wg)
+        dwu, up, _ = _new_rows(hidden, in_dim, dw_dtype or dtype, wg)
+    else:
+        gp, lddw = _rows(dwg, "dwg", dw_dtype, shape)
+        up, ldu = _rows(dwu, "dwu", dwg.dtype, shape)
+        if ldu != lddw:
+            raise ValueError("dwg and dwu must have the same stride")
     ref = ctypes.byref(d)
-    ws, wp, wb = _ws(lib.detox_gated_backward_workspace_bytes(ref), ws, wg.device)
+    ws, wp, wb = _workspace(lib.detox_gated_backward_workspace_bytes(ref), ws, wg)
     _check(lib.detox_gated_backward(ref, dhp, lddh, dxp, lddx, gp, up, lddw, _dtype_code(dwg.dtype, "dwg"), wp, wb,
                                     _stream(stream)), "detox_gated_backward")
     return dx, dwg, dwu

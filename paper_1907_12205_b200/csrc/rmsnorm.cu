@@ -6,7 +6,8 @@
 // Both are bound by HBM, so a row is read once and stays in registers: TPR threads hold it, EPT entries each, in 16-byte
 // pieces dealt round the threads (piece t, t + TPR, ...).  With the 8-bit output a block of 128 columns then lies in 16
 // neighbouring lanes (fp32: 32), which agree on its largest entry by shuffles.  Up to 1024 columns a warp takes a row
-// and no barrier is needed; above that a CTA does.
+// and no barrier is needed; above that a CTA does.  The grid is persistent: the next row's pieces are asked for before the
+// present row's sum is formed, so that memory stays busy through the reductions.
 //
 // dw adds in a fixed order: a CTA takes every gridDim-th row and adds in registers, leaves one row of partial sums, and a
 // second kernel adds those column by column.
@@ -16,19 +17,18 @@ namespace detox {
 
 namespace {
 
-// entries [c, c + N) of a row, zero beyond `cols`
+// entries [c, c + N) of a row as they lie in memory, zeros beyond `cols`
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_piece(const T* row, int64_t c, int64_t cols, float (&f)[Piece<T>::N]) {
+__device__ __forceinline__ uint4 load_piece(const T* row, int c, int cols) {
     constexpr int N = Piece<T>::N;
-    if (VEC && c + N <= cols) {
-        Piece<T>::split(ld_stream_u4(row + c), f);
-    } else {
+    if (VEC && c + N <= cols) return ld_stream_u4(row + c);
+    float f[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
-    }
+    for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
+    return Piece<T>::join(f);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T* row, int64_t c, int64_t cols, const float (&f)[Piece<T>::N]) {
+__device__ __forceinline__ void store_piece(T* row, int c, int cols, const float (&f)[Piece<T>::N]) {
     constexpr int N = Piece<T>::N;
     if (VEC && c + N <= cols) {
         st_stream_u4(row + c, Piece<T>::join(f));
@@ -37,6 +37,12 @@ __device__ __forceinline__ void store_piece(T* row, int64_t c, int64_t cols, con
         for (int j = 0; j < N; ++j)
             if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
     }
+}
+// the weight's pieces, which a thread keeps for all its rows
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 load_weight(const T* w, int c, int cols) {
+    if (VEC && c + Piece<T>::N <= cols) return __ldg(reinterpret_cast<const uint4*>(w + c));
+    return load_piece<T, false>(w, c, cols);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -63,6 +69,12 @@ __device__ __forceinline__ float row_sum(float v, float* sm, int turn) {
 
 
 template <int TPR> constexpr int kBlockOf = TPR < 256 ? 256 : TPR;   // threads of a CTA
+// Persistent CTAs on an SM: as many as their registers allow when the next row waits in registers too.
+template <int TPR, int EPT> constexpr int kForwardCtas = TPR == 1024 ? 1 : (EPT == 32 ? 2 : 4);
+template <int TPR, int EPT> constexpr int kBackwardCtas = TPR == 1024 ? 1 : (EPT == 32 ? 1 : (EPT == 16 ? 2 : 4));
+
+// Whether the next row is fetched early and the weight stays in registers: CTAs of 1024 threads have no registers for that.
+template <int TPR> constexpr bool kAhead = TPR < 1024;
 
 struct NormOut {
     void* S; int64_t lds;
@@ -74,157 +86,177 @@ struct NormOut {
 
 // X, R and S may be the same buffer: a row is in registers before any of it is written.
 template <typename T, int TPR, int EPT, bool VEC>
-__global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr,
-                                                                       const T* __restrict__ w, int64_t rows, int64_t cols,
-                                                                       float eps, NormOut o) {
+__global__ void __launch_bounds__(kBlockOf<TPR>, (kForwardCtas<TPR, EPT>))
+rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __restrict__ w, int64_t rows, int cols, float eps,
+               NormOut o) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
     pdl_trigger();
     pdl_wait();
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (TPR == 32 && row >= rows) return;   // (TPR > 32: a CTA per row, all of them there)
-
-    float v[P][N];
-    const T* x = X + row * ldx;
-#pragma unroll
-    for (int i = 0; i < P; ++i) load_piece<T, VEC>(x, (int64_t)(t + i * TPR) * N, cols, v[i]);
-    if (R) {
-        const T* r = R + row * ldr;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= rows) return;                   // (TPR = 32: whole warps; else never: a CTA has at least one row)
+    uint4 weight[P], x[P], r[P];
+    auto fetch = [&](int64_t at) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            float f[N];
-            load_piece<T, VEC>(r, (int64_t)(t + i * TPR) * N, cols, f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[i][j] += f[j];
+            const int c = (t + i * TPR) * N;
+            x[i] = load_piece<T, VEC>(X + at * ldx, c, cols);
+            if (R) r[i] = load_piece<T, VEC>(R + at * ldr, c, cols);
         }
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) sum = fmaf(v[i][j], v[i][j], sum);
-    sum = row_sum<TPR>(sum, sm, 0);
-    const float rstd = rsqrtf(sum / (float)cols + eps);
-    if (o.rstd && t == 0) o.rstd[row] = rstd;
-    if (o.S) {
-        T* s = static_cast<T*>(o.S) + row * o.lds;
-#pragma unroll
-        for (int i = 0; i < P; ++i) store_piece<T, VEC>(s, (int64_t)(t + i * TPR) * N, cols, v[i]);
-    }
-    if (!o.Y && !o.Q) return;
+    };
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int64_t c = (int64_t)(t + i * TPR) * N;
-        float f[N];
-        if (VEC && c + N <= cols) {
-            Piece<T>::split(__ldg(reinterpret_cast<const uint4*>(w + c)), f);
-        } else {
+        if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
+        r[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    fetch(row);
+    for (int turn = 0;; ++turn) {
+        if (!kAhead<TPR> && turn > 0) fetch(row);
+        float v[P][N];
+        float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(w[c + j]) : 0.f;
-        }
+        for (int i = 0; i < P; ++i) {
+            Piece<T>::split(x[i], v[i]);
+            if (R) {
+                float f[N];
+                Piece<T>::split(r[i], f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[i][j] = c + j < cols ? v[i][j] * rstd * f[j] : 0.f;
-        if (o.Y) store_piece<T, VEC>(static_cast<T*>(o.Y) + row * o.ldy, c, cols, v[i]);
-        if (o.Q) {
-            constexpr int kLanes = kKeepBlock / N;   // 16, or 32 in fp32: the lanes of a block lie side by side
-            float amax = 0.f;
-#pragma unroll
-            for (int j = 0; j < N; ++j) amax = fmaxf(amax, finite_abs(v[i][j]));
-#pragma unroll
-            for (int s = kLanes / 2; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
-            const uint32_t e = keep_exponent(amax);
-            const float inv = keep_inverse(e);
-            uint32_t q[N / 4];
-#pragma unroll
-            for (int j = 0; j < N / 4; ++j)
-                q[j] = keep4(v[i][4 * j] * inv, v[i][4 * j + 1] * inv, v[i][4 * j + 2] * inv, v[i][4 * j + 3] * inv);
-            uint8_t* to = o.Q + row * o.ldq + c;
-            if (VEC && c + N <= cols) {
-                if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(q[0], q[1]));
-                else __stcs(reinterpret_cast<unsigned int*>(to), q[0]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (c + j < cols) to[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+                for (int j = 0; j < N; ++j) v[i][j] += f[j];
             }
-            if (c < cols && t % kLanes == 0) o.E[row * o.lde + c / kKeepBlock] = (uint8_t)e;
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum = fmaf(v[i][j], v[i][j], sum);
         }
+        const int64_t next = row + stride;
+        if (kAhead<TPR> && next < rows) fetch(next);
+        sum = row_sum<TPR>(sum, sm, turn);
+        const float rstd = rsqrtf(sum / (float)cols + eps);
+        if (o.rstd && t == 0) o.rstd[row] = rstd;
+        if (o.S) {
+            T* s = static_cast<T*>(o.S) + row * o.lds;
+#pragma unroll
+            for (int i = 0; i < P; ++i) store_piece<T, VEC>(s, (t + i * TPR) * N, cols, v[i]);
+        }
+        if (o.Y || o.Q) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int c = (t + i * TPR) * N;
+                float f[N];
+                Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, c, cols), f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[i][j] = c + j < cols ? v[i][j] * rstd * f[j] : 0.f;
+                if (o.Y) store_piece<T, VEC>(static_cast<T*>(o.Y) + row * o.ldy, c, cols, v[i]);
+                if (o.Q) {
+                    constexpr int kLanes = kKeepBlock / N;   // 16, or 32 in fp32: the lanes of a block lie side by side
+                    float amax = 0.f;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) amax = fmaxf(amax, finite_abs(v[i][j]));
+#pragma unroll
+                    for (int s = kLanes / 2; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+                    const uint32_t e = keep_exponent(amax);
+                    const float inv = keep_inverse(e);
+                    uint32_t q[N / 4];
+#pragma unroll
+                    for (int j = 0; j < N / 4; ++j)
+                        q[j] = keep4(v[i][4 * j] * inv, v[i][4 * j + 1] * inv, v[i][4 * j + 2] * inv, v[i][4 * j + 3] * inv);
+                    uint8_t* to = o.Q + row * o.ldq + c;
+                    if (VEC && c + N <= cols) {
+                        if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(q[0], q[1]));
+                        else __stcs(reinterpret_cast<unsigned int*>(to), q[0]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            if (c + j < cols) to[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+                    }
+                    if (c < cols && t % kLanes == 0) o.E[row * o.lde + c / kKeepBlock] = (uint8_t)e;
+                }
+            }
+        }
+        if (next >= rows) break;
+        row = next;
     }
 }
 
-constexpr int kMaxParts = kSMs * 4;   // CTAs of the backward pass, each leaving one row of partial sums of dw
-
 template <typename T, int TPR, int EPT, bool VEC>
-__global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_backward_kernel(
+__global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsnorm_backward_kernel(
     const T* dY, int64_t lddy, const T* dS, int64_t ldds, const T* __restrict__ S, int64_t lds, const T* __restrict__ w,
-    const float* __restrict__ rstd_of, int64_t rows, int64_t cols, T* dX, int64_t lddx, float* __restrict__ parts) {
+    const float* __restrict__ rstd_of, int64_t rows, int cols, T* dX, int64_t lddx, float* __restrict__ parts,
+    int64_t ldp) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
     pdl_trigger();
     pdl_wait();
     const int t = threadIdx.x % TPR;
     const float inv_cols = 1.f / (float)cols;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     float acc[P][N];
+    uint4 weight[P], dy[P], s[P], ds[P];
+    float rstd = 0.f;
+    auto fetch = [&](int64_t at) {
+        rstd = rstd_of[at];
 #pragma unroll
-    for (int i = 0; i < P; ++i)
+        for (int i = 0; i < P; ++i) {
+            const int c = (t + i * TPR) * N;
+            dy[i] = load_piece<T, VEC>(dY + at * lddy, c, cols);
+            s[i] = load_piece<T, VEC>(S + at * lds, c, cols);
+            if (dS) ds[i] = load_piece<T, VEC>(dS + at * ldds, c, cols);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
+        ds[i] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < rows; row += (int64_t)gridDim.x * RPB, ++turn) {
-        const float rstd = rstd_of[row];
+    }
+    if (kAhead<TPR> && row < rows) fetch(row);
+    for (int turn = 0; row < rows; ++turn) {
+        if (!kAhead<TPR>) fetch(row);
         float dyw[P][N], hat[P][N];
+        const float scale = rstd;
+        uint4 extra[P];
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * N;
-            load_piece<T, VEC>(dY + row * lddy, c, cols, dyw[i]);
-            load_piece<T, VEC>(S + row * lds, c, cols, hat[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * N;
+            extra[i] = ds[i];
             float f[N];
-            if (VEC && c + N <= cols) {
-                Piece<T>::split(__ldg(reinterpret_cast<const uint4*>(w + c)), f);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(w[c + j]) : 0.f;
-            }
+            Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, (t + i * TPR) * N, cols), f);
+            Piece<T>::split(dy[i], dyw[i]);
+            Piece<T>::split(s[i], hat[i]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                hat[i][j] *= rstd;
+                hat[i][j] *= scale;
                 acc[i][j] = fmaf(dyw[i][j], hat[i][j], acc[i][j]);
                 dyw[i][j] *= f[j];
                 dot = fmaf(dyw[i][j], hat[i][j], dot);
             }
         }
-        if (!dX) continue;
-        dot = row_sum<TPR>(dot, sm, turn) * inv_cols;
+        const int64_t next = row + stride;
+        if (kAhead<TPR> && next < rows) fetch(next);
+        if (dX) {
+            dot = row_sum<TPR>(dot, sm, turn) * inv_cols;
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * N;
-            float f[N];
-            if (dS) {
-                load_piece<T, VEC>(dS + row * ldds, c, cols, f);
-            } else {
+            for (int i = 0; i < P; ++i) {
+                float out[N];
+                Piece<T>::split(extra[i], out);
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = 0.f;
+                for (int j = 0; j < N; ++j) out[j] = fmaf(scale, fmaf(-hat[i][j], dot, dyw[i][j]), out[j]);
+                store_piece<T, VEC>(dX + row * lddx, (t + i * TPR) * N, cols, out);
             }
-#pragma unroll
-            for (int j = 0; j < N; ++j) f[j] = fmaf(rstd, fmaf(-hat[i][j], dot, dyw[i][j]), f[j]);
-            store_piece<T, VEC>(dX + row * lddx, c, cols, f);
         }
+        row = next;
     }
     if (!parts) return;
-    float* part = parts + (int64_t)blockIdx.x * cols;
+    float* part = parts + (int64_t)blockIdx.x * ldp;
     if constexpr (RPB == 1) {
 #pragma unroll
         for (int i = 0; i < P; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int64_t c = (int64_t)(t + i * TPR) * N + j;
-                if (c < cols) part[c] = acc[i][j];
+            for (int j = 0; j < N; j += 4) {
+                const int c = (t + i * TPR) * N + j;
+                if (c < ldp) *reinterpret_cast<float4*>(part + c) = make_float4(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]);
             }
     } else {
         // the CTA's warps one after another
@@ -245,24 +277,35 @@ __global__ void __launch_bounds__(kBlockOf<TPR>) rmsnorm_backward_kernel(
     }
 }
 
-// dw[c] = sum over the partial rows: 32 columns a CTA, 32 threads a column, each over every 32nd row
-__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ parts, int nparts, int64_t cols,
-                                                          float* __restrict__ dw) {
-    __shared__ float sm[32][33];
+// dw[c] = sum over the partial rows: a CTA has 32 columns, a thread 4 of them and every 128th row
+constexpr int kDwThreads = 1024, kDwCols = 32;
+__global__ void __launch_bounds__(kDwThreads) rmsnorm_dw_kernel(const float* __restrict__ parts, int nparts, int64_t ldp,
+                                                                int cols, float* __restrict__ dw) {
+    constexpr int kQuads = kDwCols / 4, kGroups = kDwThreads / kQuads;
+    __shared__ float sm[kGroups][kDwCols + 1];
     pdl_trigger();
     pdl_wait();
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + x;
-    float sum = 0.f;
-    if (c < cols) {
-#pragma unroll 8
-        for (int r = y; r < nparts; r += 32) sum += parts[(int64_t)r * cols + c];
+    const int x = threadIdx.x % kQuads, y = threadIdx.x / kQuads;
+    const float* from = parts + (int64_t)blockIdx.x * kDwCols + 4 * x;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 5
+    for (int r = y; r < nparts; r += kGroups) {
+        const float4 v = *reinterpret_cast<const float4*>(from + (int64_t)r * ldp);
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }
-    sm[y][x] = sum;
+    sm[y][4 * x] = sum.x; sm[y][4 * x + 1] = sum.y; sm[y][4 * x + 2] = sum.z; sm[y][4 * x + 3] = sum.w;
     __syncthreads();
-    sum = warp_sum(sm[x][y]);
-    if (x == 0 && (int64_t)blockIdx.x * 32 + y < cols) dw[(int64_t)blockIdx.x * 32 + y] = sum;
+    // a warp for each column
+    const int c = threadIdx.x / 32, lane = threadIdx.x % 32;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGroups / 32; ++k) v += sm[lane + 32 * k][c];
+    v = warp_sum(v);
+    const int64_t col = (int64_t)blockIdx.x * kDwCols + c;
+    if (lane == 0 && col < cols) dw[col] = v;
 }
+static_assert(kDwThreads / 32 == kDwCols, "a warp for each column");
+int64_t parts_pitch(int64_t cols) { return (cols + kDwCols - 1) / kDwCols * kDwCols; }
 
 struct Backward {
     const void* dY; int64_t lddy;
@@ -284,9 +327,25 @@ detox_status by_width(int64_t cols, F f) {
     if (cols <= 256 * 8) return f.template operator()<256, 8>();
     if (cols <= 256 * 16) return f.template operator()<256, 16>();
     if (cols <= 256 * 32) return f.template operator()<256, 32>();
+    if (cols <= 1024 * 16) return f.template operator()<1024, 16>();
     return f.template operator()<1024, 32>();
 }
-int rows_per_cta(int64_t cols) { return cols <= 1024 ? 8 : 1; }
+// CTAs of the backward pass, each leaving one row of partial sums of dw
+struct CountParts {
+    int64_t rows;
+    int* out;
+    template <int TPR, int EPT>
+    detox_status operator()() const {
+        const int64_t need = ceil_div(rows, (int64_t)(kBlockOf<TPR> / TPR)), most = (int64_t)kSMs * kBackwardCtas<TPR, EPT>;
+        *out = (int)(need < most ? need : most);
+        return DETOX_OK;
+    }
+};
+int parts_of(int64_t rows, int64_t cols) {
+    int n = 0;
+    by_width(cols, CountParts{rows, &n});
+    return n;
+}
 
 template <typename T, bool VEC>
 struct Fwd {
@@ -300,9 +359,10 @@ struct Fwd {
     template <int TPR, int EPT>
     detox_status operator()() const {
         constexpr int RPB = kBlockOf<TPR> / TPR;
-        return launch_chained(rmsnorm_kernel<T, TPR, EPT, VEC>, (unsigned)ceil_div(rows, (int64_t)RPB), kBlockOf<TPR>, 0, 1, s,
-                              static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows, cols,
-                              eps, o);
+        const int64_t need = ceil_div(rows, (int64_t)RPB), most = (int64_t)kSMs * kForwardCtas<TPR, EPT>;
+        return launch_chained(rmsnorm_kernel<T, TPR, EPT, VEC>, (unsigned)(need < most ? need : most), kBlockOf<TPR>, 0, 1, s,
+                              static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows,
+                              (int)cols, eps, o);
     }
 };
 
@@ -315,7 +375,8 @@ struct Bwd {
     detox_status operator()() const {
         return launch_chained(rmsnorm_backward_kernel<T, TPR, EPT, VEC>, (unsigned)nparts, kBlockOf<TPR>, 0, 1, s,
                               static_cast<const T*>(b.dY), b.lddy, static_cast<const T*>(b.dS), b.ldds, static_cast<const T*>(b.S),
-                              b.lds, static_cast<const T*>(b.w), b.rstd, b.rows, b.cols, static_cast<T*>(b.dX), b.lddx, b.parts);
+                              b.lds, static_cast<const T*>(b.w), b.rstd, b.rows, (int)b.cols, static_cast<T*>(b.dX), b.lddx, b.parts,
+                              parts_pitch(b.cols));
     }
 };
 
@@ -342,11 +403,6 @@ detox_status backward(const Backward& b, int nparts, cudaStream_t s) {
     return by_width(b.cols, Bwd<T, false>{b, nparts, s});
 }
 
-int parts_of(int64_t rows, int64_t cols) {
-    const int64_t need = ceil_div(rows, (int64_t)rows_per_cta(cols));
-    return (int)(need < kMaxParts ? need : kMaxParts);
-}
-
 }  // namespace
 
 detox_status launch_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w,
@@ -360,7 +416,7 @@ detox_status launch_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R
 }
 
 size_t rmsnorm_backward_ws_bytes(int64_t rows, int64_t cols) {
-    return align_up((size_t)(rows > 0 ? parts_of(rows, cols) : 1) * (size_t)cols * sizeof(float));
+    return align_up((size_t)(rows > 0 ? parts_of(rows, cols) : 1) * (size_t)parts_pitch(cols) * sizeof(float));
 }
 
 detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, const void* dS, int64_t ldds, const void* S,
@@ -378,7 +434,8 @@ detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, co
     else if (dtype == DETOX_DTYPE_HALF) st = backward<__half>(b, nparts, s);
     else st = backward<__nv_bfloat16>(b, nparts, s);
     if (st != DETOX_OK || !dw) return st;
-    return launch_chained(rmsnorm_dw_kernel, (unsigned)ceil_div(cols, (int64_t)32), 1024, 0, 1, s, parts, nparts, cols, dw);
+    return launch_chained(rmsnorm_dw_kernel, (unsigned)ceil_div(cols, (int64_t)kDwCols), kDwThreads, 0, 1, s, parts, nparts,
+                          parts_pitch(cols), (int)cols, dw);
 }
 
 }  // namespace detox
