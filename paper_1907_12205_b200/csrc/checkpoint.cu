@@ -43,30 +43,22 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ X,
         const int64_t c0 = (int64_t)w.blk * kKeepBlock + part * kPer;
         const bool full = VEC && live && c0 + kPer <= cols;
         const T* x = X + w.row * ld + c0;
-        float v[kPer];
+        uint64_t v[kPer / 2];
         if (full) {
 #pragma unroll
             for (int i = 0; i < kPer / N; ++i) {
-                float f[N];
+                uint64_t f[N / 2];
                 Piece<T>::split(ld_stream_u4(x + i * N), f);
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i * N + j] = f[j];
+                for (int j = 0; j < N / 2; ++j) v[i * (N / 2) + j] = f[j];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) v[i] = live && c0 + i < cols ? to_f32(x[i]) : 0.f;
+            for (int i = 0; i < kPer / 2; ++i)
+                v[i] = pair_of(live && c0 + 2 * i < cols ? to_f32(x[2 * i]) : 0.f, live && c0 + 2 * i + 1 < cols ? to_f32(x[2 * i + 1]) : 0.f);
         }
-        float amax = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) amax = fmaxf(amax, finite_abs(v[i]));
-#pragma unroll
-        for (int o = kLanes / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const uint32_t e = keep_exponent(amax);
-        const float inv = keep_inverse(e);
         uint32_t q[kPer / 4];
-#pragma unroll
-        for (int i = 0; i < kPer / 4; ++i)
-            q[i] = keep4(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+        const uint32_t e = keep_pairs<kPer / 2, kLanes>(v, q);
         uint8_t* to = Q + w.row * ldq + c0;
         if (full) {
             st_stream_u4(to, make_uint4(q[0], q[1], q[2], q[3]));

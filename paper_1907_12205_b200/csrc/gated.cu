@@ -276,8 +276,12 @@ __device__ __forceinline__ void load32(const T* row, int64_t c, int64_t cols, bo
     }
 }
 // 32 entries of the 8-bit form
-__device__ __forceinline__ void keep32(uint8_t* row, int64_t c, int64_t cols, bool vec, float inv, const float (&f)[32]) {
+__device__ __forceinline__ void keep32(uint8_t* row, int64_t c, int64_t cols, bool vec, bool odd, float inv, float (&f)[32]) {
     uint32_t q[8];
+    if (odd) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) f[i] = inf_to_nan(f[i]);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = keep4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
     if (vec && c + 32 <= cols) {
@@ -507,8 +511,8 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                         if (p.gq) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
-                                gmax = fmaxf(gmax, finite_abs(g[i]));
-                                umax = fmaxf(umax, finite_abs(u[i]));
+                                gmax = fmaxf(gmax, fabsf(g[i]));
+                                umax = fmaxf(umax, fabsf(u[i]));
                             }
                         }
                         by_act(p.act, HOf<32>{g, u});
@@ -522,15 +526,27 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     }
                 }
                 if (FORM == kForward && BN == 256 && p.gq) {
+                    const bool odd = __any_sync(0xffffffffu, is_inf(gmax) || is_inf(umax));   // an Inf somewhere: see keep_pairs
+                    if (odd) {
+                        gmax = umax = 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < kHalf; c += 32) {
+                            float f[32];
+                            tmem_load32(at + c, f);
+                            for (int i = 0; i < 32; ++i) gmax = fmaxf(gmax, fabsf(inf_to_nan(f[i])));
+                            tmem_load32(at + kHalf + c, f);
+                            for (int i = 0; i < 32; ++i) umax = fmaxf(umax, fabsf(inf_to_nan(f[i])));
+                        }
+                    }
                     const uint32_t ge = keep_exponent(gmax), ue = keep_exponent(umax);
                     const float ginv = keep_inverse(ge), uinv = keep_inverse(ue);
 #pragma unroll 1
                     for (int c = 0; c < kHalf; c += 32) {
                         float f[32];
                         tmem_load32(at + c, f);
-                        if (live) keep32(p.gq + row * p.ldq, c0 + c, p.cols, p.q_vec, ginv, f);
+                        if (live) keep32(p.gq + row * p.ldq, c0 + c, p.cols, p.q_vec, odd, ginv, f);
                         tmem_load32(at + kHalf + c, f);
-                        if (live) keep32(p.uq + row * p.ldq, c0 + c, p.cols, p.q_vec, uinv, f);
+                        if (live) keep32(p.uq + row * p.ldq, c0 + c, p.cols, p.q_vec, odd, uinv, f);
                     }
                     if (live) {
                         p.ge[row * p.lde + n] = (uint8_t)ge;
@@ -607,21 +623,11 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     const int64_t c = (int64_t)n * kHalf + lane * E;
                     if constexpr (FORM == kForward) {
                         if (BN == 256 && p.gq) {
-                            float gmax = 0.f, umax = 0.f;
-#pragma unroll
-                            for (int i = 0; i < E; ++i) {
-                                gmax = fmaxf(gmax, finite_abs(a[i]));
-                                umax = fmaxf(umax, finite_abs(b[i]));
-                            }
-#pragma unroll
-                            for (int o = 16; o > 0; o >>= 1) {
-                                gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
-                                umax = fmaxf(umax, __shfl_xor_sync(0xffffffffu, umax, o));
-                            }
-                            const uint32_t ge = keep_exponent(gmax), ue = keep_exponent(umax);
-                            const float gi = keep_inverse(ge), ui = keep_inverse(ue);
-                            const uint32_t gq = keep4(a[0] * gi, a[1] * gi, a[E - 2] * gi, a[E - 1] * gi);
-                            const uint32_t uq = keep4(b[0] * ui, b[1] * ui, b[E - 2] * ui, b[E - 1] * ui);
+                            uint64_t ga[2] = {pair_of(a[0], a[1]), pair_of(a[E - 2], a[E - 1])};
+                            uint64_t ub[2] = {pair_of(b[0], b[1]), pair_of(b[E - 2], b[E - 1])};
+                            uint32_t gk[1], uk[1];
+                            const uint32_t ge = keep_pairs<2, 32>(ga, gk), ue = keep_pairs<2, 32>(ub, uk);
+                            const uint32_t gq = gk[0], uq = uk[0];
                             if (p.q_vec && c + E <= p.cols) {
                                 *reinterpret_cast<uint32_t*>(p.gq + row * p.ldq + c) = gq;
                                 *reinterpret_cast<uint32_t*>(p.uq + row * p.ldq + c) = uq;

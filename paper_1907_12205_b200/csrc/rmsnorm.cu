@@ -28,14 +28,14 @@ __device__ __forceinline__ uint4 load_piece(const T* row, int c, int cols) {
     return Piece<T>::join(f);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T* row, int c, int cols, const float (&f)[Piece<T>::N]) {
+__device__ __forceinline__ void store_piece(T* row, int c, int cols, const uint64_t (&p)[Piece<T>::N / 2]) {
     constexpr int N = Piece<T>::N;
     if (VEC && c + N <= cols) {
-        st_stream_u4(row + c, Piece<T>::join(f));
+        st_stream_u4(row + c, Piece<T>::join(p));
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
+            if (c + j < cols) row[c + j] = from_f32<T>(j & 1 ? pair_hi(p[j / 2]) : pair_lo(p[j / 2]));
     }
 }
 // the weight's pieces, which a thread keeps for all its rows
@@ -67,7 +67,6 @@ __device__ __forceinline__ float row_sum(float v, float* sm, int turn) {
     return v;
 }
 
-
 template <int TPR> constexpr int kBlockOf = TPR < 256 ? 256 : TPR;   // threads of a CTA
 // Persistent CTAs on an SM: as many as their registers allow when the next row waits in registers too.
 template <int TPR, int EPT> constexpr int kForwardCtas = TPR == 1024 ? 1 : (EPT == 32 ? 2 : 4);
@@ -98,40 +97,42 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     if (row >= rows) return;                   // (TPR = 32: whole warps; else never: a CTA has at least one row)
     uint4 weight[P], x[P], r[P];
-    auto fetch = [&](int64_t at) {
+    const T *from_x = X + row * ldx, *from_r = R ? R + row * ldr : nullptr;
+    auto fetch = [&] {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int c = (t + i * TPR) * N;
-            x[i] = load_piece<T, VEC>(X + at * ldx, c, cols);
-            if (R) r[i] = load_piece<T, VEC>(R + at * ldr, c, cols);
+            x[i] = load_piece<T, VEC>(from_x, c, cols);
+            if (from_r) r[i] = load_piece<T, VEC>(from_r, c, cols);
         }
+        from_x += stride * ldx;
+        if (from_r) from_r += stride * ldr;
     };
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
+    for (int i = 0; i < P; ++i)
         if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
-        r[i] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    fetch(row);
+    if (kAhead<TPR>) fetch();
     for (int turn = 0;; ++turn) {
-        if (!kAhead<TPR> && turn > 0) fetch(row);
-        float v[P][N];
-        float sum = 0.f;
+        if (!kAhead<TPR>) fetch();
+        uint64_t v[P][N / 2];
+        uint64_t sum2 = 0ull;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             Piece<T>::split(x[i], v[i]);
-            if (R) {
-                float f[N];
+            if (from_r) {
+                uint64_t f[N / 2];
                 Piece<T>::split(r[i], f);
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] += f[j];
+                for (int j = 0; j < N / 2; ++j) v[i][j] = add2(v[i][j], f[j]);
             }
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum = fmaf(v[i][j], v[i][j], sum);
+            for (int j = 0; j < N / 2; ++j) sum2 = fma2(v[i][j], v[i][j], sum2);
         }
         const int64_t next = row + stride;
-        if (kAhead<TPR> && next < rows) fetch(next);
-        sum = row_sum<TPR>(sum, sm, turn);
+        if (kAhead<TPR> && next < rows) fetch();
+        const float sum = row_sum<TPR>(pair_lo(sum2) + pair_hi(sum2), sm, turn);
         const float rstd = rsqrtf(sum / (float)cols + eps);
+        const uint64_t rstd2 = pair_of(rstd, rstd);
         if (o.rstd && t == 0) o.rstd[row] = rstd;
         if (o.S) {
             T* s = static_cast<T*>(o.S) + row * o.lds;
@@ -141,25 +142,17 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
         if (o.Y || o.Q) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
+                // (beyond the row's end: zeros, or NaN from 0 * Inf, which a block's largest entry passes over)
                 const int c = (t + i * TPR) * N;
-                float f[N];
+                uint64_t f[N / 2];
                 Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, c, cols), f);
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] = c + j < cols ? v[i][j] * rstd * f[j] : 0.f;
+                for (int j = 0; j < N / 2; ++j) v[i][j] = mul2(mul2(v[i][j], rstd2), f[j]);
                 if (o.Y) store_piece<T, VEC>(static_cast<T*>(o.Y) + row * o.ldy, c, cols, v[i]);
                 if (o.Q) {
                     constexpr int kLanes = kKeepBlock / N;   // 16, or 32 in fp32: the lanes of a block lie side by side
-                    float amax = 0.f;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) amax = fmaxf(amax, finite_abs(v[i][j]));
-#pragma unroll
-                    for (int s = kLanes / 2; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
-                    const uint32_t e = keep_exponent(amax);
-                    const float inv = keep_inverse(e);
                     uint32_t q[N / 4];
-#pragma unroll
-                    for (int j = 0; j < N / 4; ++j)
-                        q[j] = keep4(v[i][4 * j] * inv, v[i][4 * j + 1] * inv, v[i][4 * j + 2] * inv, v[i][4 * j + 3] * inv);
+                    const uint32_t e = keep_pairs<N / 2, kLanes>(v[i], q);
                     uint8_t* to = o.Q + row * o.ldq + c;
                     if (VEC && c + N <= cols) {
                         if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(q[0], q[1]));
@@ -191,58 +184,65 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
     const float inv_cols = 1.f / (float)cols;
     const int64_t stride = (int64_t)gridDim.x * RPB;
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    float acc[P][N];
+    uint64_t acc[P][N / 2];
     uint4 weight[P], dy[P], s[P], ds[P];
     float rstd = 0.f;
-    auto fetch = [&](int64_t at) {
-        rstd = rstd_of[at];
+    const T *from_dy = dY + row * lddy, *from_s = S + row * lds, *from_ds = dS ? dS + row * ldds : nullptr;
+    const float* from_rstd = rstd_of + row;
+    auto fetch = [&] {
+        rstd = *from_rstd;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int c = (t + i * TPR) * N;
-            dy[i] = load_piece<T, VEC>(dY + at * lddy, c, cols);
-            s[i] = load_piece<T, VEC>(S + at * lds, c, cols);
-            if (dS) ds[i] = load_piece<T, VEC>(dS + at * ldds, c, cols);
+            dy[i] = load_piece<T, VEC>(from_dy, c, cols);
+            s[i] = load_piece<T, VEC>(from_s, c, cols);
+            if (from_ds) ds[i] = load_piece<T, VEC>(from_ds, c, cols);
         }
+        from_rstd += stride;
+        from_dy += stride * lddy;
+        from_s += stride * lds;
+        if (from_ds) from_ds += stride * ldds;
     };
 #pragma unroll
     for (int i = 0; i < P; ++i) {
         if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
         ds[i] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
+        for (int j = 0; j < N / 2; ++j) acc[i][j] = 0ull;
     }
-    if (kAhead<TPR> && row < rows) fetch(row);
+    if (kAhead<TPR> && row < rows) fetch();
     for (int turn = 0; row < rows; ++turn) {
-        if (!kAhead<TPR>) fetch(row);
-        float dyw[P][N], hat[P][N];
-        const float scale = rstd;
+        if (!kAhead<TPR>) fetch();
+        uint64_t dyw[P][N / 2], hat[P][N / 2];
+        const uint64_t scale2 = pair_of(rstd, rstd);
         uint4 extra[P];
-        float dot = 0.f;
+        uint64_t dot2 = 0ull;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             extra[i] = ds[i];
-            float f[N];
+            uint64_t f[N / 2];
             Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, (t + i * TPR) * N, cols), f);
             Piece<T>::split(dy[i], dyw[i]);
             Piece<T>::split(s[i], hat[i]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                hat[i][j] *= scale;
-                acc[i][j] = fmaf(dyw[i][j], hat[i][j], acc[i][j]);
-                dyw[i][j] *= f[j];
-                dot = fmaf(dyw[i][j], hat[i][j], dot);
+            for (int j = 0; j < N / 2; ++j) {
+                hat[i][j] = mul2(hat[i][j], scale2);
+                acc[i][j] = fma2(dyw[i][j], hat[i][j], acc[i][j]);
+                dyw[i][j] = mul2(dyw[i][j], f[j]);
+                dot2 = fma2(dyw[i][j], hat[i][j], dot2);
             }
         }
         const int64_t next = row + stride;
-        if (kAhead<TPR> && next < rows) fetch(next);
+        if (kAhead<TPR> && next < rows) fetch();
         if (dX) {
-            dot = row_sum<TPR>(dot, sm, turn) * inv_cols;
+            const float dot = row_sum<TPR>(pair_lo(dot2) + pair_hi(dot2), sm, turn) * -inv_cols;
+            const uint64_t ndot2 = pair_of(dot, dot);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                float out[N];
+                uint64_t out[N / 2];
                 Piece<T>::split(extra[i], out);
 #pragma unroll
-                for (int j = 0; j < N; ++j) out[j] = fmaf(scale, fmaf(-hat[i][j], dot, dyw[i][j]), out[j]);
+                for (int j = 0; j < N / 2; ++j) out[j] = fma2(scale2, fma2(hat[i][j], ndot2, dyw[i][j]), out[j]);
                 store_piece<T, VEC>(dX + row * lddx, (t + i * TPR) * N, cols, out);
             }
         }
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
 #pragma unroll
             for (int j = 0; j < N; j += 4) {
                 const int c = (t + i * TPR) * N + j;
-                if (c < ldp) *reinterpret_cast<float4*>(part + c) = make_float4(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]);
+                if (c < ldp) *reinterpret_cast<ulonglong2*>(part + c) = make_ulonglong2(acc[i][j / 2], acc[i][j / 2 + 1]);
             }
     } else {
         // the CTA's warps one after another
@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
                         const int c = (t + i * TPR) * N + j;
-                        all[c] = k == 0 ? acc[i][j] : all[c] + acc[i][j];
+                        const float a = j & 1 ? pair_hi(acc[i][j / 2]) : pair_lo(acc[i][j / 2]);
+                        all[c] = k == 0 ? a : all[c] + a;
                     }
             }
             __syncthreads();

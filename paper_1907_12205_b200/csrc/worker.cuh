@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace detox {
 
@@ -38,6 +39,13 @@ template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v)
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
 }
 
+// packed pairs of fp32
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    return ((uint64_t)__float_as_uint(hi) << 32) | __float_as_uint(lo);
+}
+__device__ __forceinline__ float pair_lo(uint64_t p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float pair_hi(uint64_t p) { return __uint_as_float((uint32_t)(p >> 32)); }
+
 // the 16 / sizeof(T) entries of a 16-byte piece
 template <typename T>
 struct Piece {
@@ -55,6 +63,32 @@ struct Piece {
             }
         }
     }
+    // the same as packed pairs of fp32, which the two-lane instructions work on
+    static __device__ __forceinline__ void split(uint4 v, uint64_t (&p)[N / 2]) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                p[i] = ((uint64_t)w[2 * i + 1] << 32) | w[2 * i];
+            } else {
+                const float2 f = unpack2<T>(w[i]);
+                p[i] = pair_of(f.x, f.y);
+            }
+        }
+    }
+    static __device__ __forceinline__ uint4 join(const uint64_t (&p)[N / 2]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[2 * i] = (uint32_t)p[i];
+                w[2 * i + 1] = (uint32_t)(p[i] >> 32);
+            } else {
+                w[i] = pack2<T>(pair_lo(p[i]), pair_hi(p[i]));
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
     static __device__ __forceinline__ uint4 join(const float (&f)[N]) {
         uint32_t w[4];
 #pragma unroll
@@ -67,11 +101,6 @@ struct Piece {
 };
 
 // ---- the 8-bit form ---------------------------------------------------------------------------
-// |v| where v is finite, else 0: what a block's largest entry is taken over
-__device__ __forceinline__ float finite_abs(float v) {
-    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-    return b < 0x7f800000u ? __uint_as_float(b) : 0.f;
-}
 // Biased exponent (e + 127) of the scale: the smallest e with amax <= 448 * 2^e = 1.75 * 2^(e+8), at least -126.
 // Adding 0x1fffff carries into the exponent exactly when the mantissa is above 1.75.
 __device__ __forceinline__ uint32_t keep_exponent(float amax) {
@@ -85,14 +114,43 @@ __device__ __forceinline__ float keep_inverse(uint32_t e) { return __uint_as_flo
 __device__ __forceinline__ float keep_scale_of_byte(uint32_t e) {
     return __uint_as_float(e == 0u ? 0x00400000u : (e == 255u ? 0x7fc00000u : e << 23));
 }
-// Four values, already divided by the scale, to four e4m3 bytes (a first).  The conversion saturates, and scaled
-// finite values are at most 448, so only an Inf could come out as a number: v + 0 v turns it into NaN beforehand.
+// A block's largest entry is taken as max |v|, which passes over NaN.  Only when that comes out as Inf is it taken again
+// after the Infs have been turned into NaN (v + 0 v), which is also how they are kept.
+__device__ __forceinline__ bool is_inf(float amax) { return amax > 3.402823466e38f; }
+__device__ __forceinline__ float inf_to_nan(float v) { return fmaf(v, 0.f, v); }
+// Four values, already divided by the scale (so at most 448, or NaN), to four e4m3 bytes (a first).
 __device__ __forceinline__ uint32_t keep4(float a, float b, float c, float d) {
     uint16_t lo, hi;
-    a = fmaf(a, 0.f, a); b = fmaf(b, 0.f, b); c = fmaf(c, 0.f, c); d = fmaf(d, 0.f, d);
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
     return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+// The 8-bit form of 2 * PAIRS entries of a block that lies in LANES neighbouring lanes of a warp (whole warps call this).
+// Returns the biased exponent; v is used up.
+template <int PAIRS, int LANES>
+__device__ __forceinline__ uint32_t keep_pairs(uint64_t (&v)[PAIRS], uint32_t (&q)[PAIRS / 2]) {
+    auto largest = [&] {
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) amax = fmaxf(amax, fmaxf(fabsf(pair_lo(v[i])), fabsf(pair_hi(v[i]))));
+#pragma unroll
+        for (int s = LANES / 2; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+        return amax;
+    };
+    float amax = largest();
+    if (__any_sync(0xffffffffu, is_inf(amax))) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[i] = pair_of(inf_to_nan(pair_lo(v[i])), inf_to_nan(pair_hi(v[i])));
+        amax = largest();
+    }
+    const uint32_t e = keep_exponent(amax);
+    const float inv = keep_inverse(e);
+    const uint64_t inv2 = pair_of(inv, inv);
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) v[i] = mul2(v[i], inv2);
+#pragma unroll
+    for (int i = 0; i < PAIRS / 2; ++i) q[i] = keep4(pair_lo(v[2 * i]), pair_hi(v[2 * i]), pair_lo(v[2 * i + 1]), pair_hi(v[2 * i + 1]));
+    return e;
 }
 // ... and back (not yet multiplied by the scale)
 __device__ __forceinline__ void taken4(uint32_t q, float (&f)[4]) {
