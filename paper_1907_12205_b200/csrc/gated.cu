@@ -11,7 +11,7 @@
 // lie the other way round and are read as MN-major tiles: nothing is transposed in memory.
 //
 // A CTA: one warp issues the TMA copies of 64-wide slices of both operands into a ring of stages, one thread issues
-// the MMAs, four warps drain the accumulator.  Two accumulators share the tensor memory, so a tile is drained while the
+// the MMAs, eight warps drain the accumulator (two to each quarter of its rows).  Two accumulators share the tensor memory, so a tile is drained while the
 // next one is multiplied.  Ragged edges: TMA fills with zeros outside a matrix and the epilogue masks its stores.
 // Three shapes of the work (gemm_shape chooses):
 //   pair     two CTAs of a cluster multiply one 256 x 256 tile (cta_group::2): each holds 128 rows of either operand, so
@@ -36,7 +36,7 @@ enum Form { kForward = 0, kRecompute = 1, kDgrad = 2, kWgrad = 3 };
 
 constexpr int kSlice = 64;                       // entries of the reduction per stage: one 128-byte swizzled row
 constexpr uint32_t kChunkBytes = 64 * 128;       // 64 rows of 128 bytes
-constexpr int kEpiWarps = 4, kThreads = 32 * (2 + kEpiWarps);
+constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
 constexpr int kMaxSplit = 8;                     // CTAs of a portable cluster
 constexpr int kMaxStages = 6;
 
@@ -78,9 +78,8 @@ struct GemmArgs {
     uint8_t *gq, *ge, *uq, *ue;    // forward: the kept g and u, or null
     int64_t ldq, lde;
     bool q_vec;
-    const void* dh;                // recompute
+    const void* dh;                // recompute (16-byte aligned rows)
     int64_t lddh;
-    bool dh_vec;
 };
 
 // Shared-memory descriptor of an MN-major operand: chunks of 64 entries (128 swizzled bytes) by 64 steps of the
@@ -170,21 +169,37 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
     return v;
 }
 
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&f)[32]) {
-    uint32_t v[32];
+// 32 columns of this thread's accumulator row, or two times 32.  Load and wait are one statement, so that nothing that uses
+// the values can be moved between them.
+__device__ __forceinline__ void tmem_load32(uint32_t at, float (&f)[32]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
-          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-        : "r"(taddr)
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]), "=f"(f[8]),
+          "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]), "=f"(f[16]),
+          "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]), "=f"(f[22]), "=f"(f[23]), "=f"(f[24]),
+          "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31])
+        : "r"(at)
         : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+}
+__device__ __forceinline__ void tmem_load32(uint32_t at_f, uint32_t at_g, float (&f)[32], float (&g)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, "
+        "%46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]), "=f"(f[8]),
+          "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]), "=f"(f[16]),
+          "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]), "=f"(f[22]), "=f"(f[23]), "=f"(f[24]),
+          "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31]),
+          "=f"(g[0]), "=f"(g[1]), "=f"(g[2]), "=f"(g[3]), "=f"(g[4]), "=f"(g[5]), "=f"(g[6]), "=f"(g[7]), "=f"(g[8]),
+            "=f"(g[9]), "=f"(g[10]), "=f"(g[11]), "=f"(g[12]), "=f"(g[13]), "=f"(g[14]), "=f"(g[15]), "=f"(g[16]),
+            "=f"(g[17]), "=f"(g[18]), "=f"(g[19]), "=f"(g[20]), "=f"(g[21]), "=f"(g[22]), "=f"(g[23]), "=f"(g[24]),
+            "=f"(g[25]), "=f"(g[26]), "=f"(g[27]), "=f"(g[28]), "=f"(g[29]), "=f"(g[30]), "=f"(g[31])
+        : "r"(at_f), "r"(at_g)
+        : "memory");
 }
 
 // ---- activations: a = act(g), da = act'(g) -----------------------------------------------------
@@ -207,6 +222,22 @@ __device__ __forceinline__ void act_both(float g, float& a, float& da) {
     } else {
         a = fmaxf(g, 0.f);
         da = g > 0.f ? 1.f : 0.f;
+    }
+}
+// The same for two entries at a time.
+template <int ACT>
+__device__ __forceinline__ void act_both(uint64_t g, uint64_t& a, uint64_t& da) {
+    if constexpr (ACT == DETOX_ACT_SILU) {
+        const uint64_t one = pair_of(1.f, 1.f);
+        const uint64_t s = pair_of(__fdividef(1.f, 1.f + __expf(-pair_lo(g))), __fdividef(1.f, 1.f + __expf(-pair_hi(g))));
+        a = mul2(g, s);
+        da = fma2(a, sub2(one, s), s);
+    } else {
+        float al, ah, dl, dh;
+        act_both<ACT>(pair_lo(g), al, dl);
+        act_both<ACT>(pair_hi(g), ah, dh);
+        a = pair_of(al, ah);
+        da = pair_of(dl, dh);
     }
 }
 // calls f<ACT>()
@@ -237,6 +268,22 @@ struct DguOf {   // (g, u, dh) -> (dg, du, -)
             act_both<ACT>(g[i], a, da);
             g[i] = dh[i] * u[i] * da;
             u[i] = dh[i] * a;
+        }
+    }
+};
+
+template <int NP>
+struct DguPairsOf {   // the same on pairs
+    uint64_t (&g)[NP];
+    uint64_t (&u)[NP];
+    const uint64_t (&dh)[NP];
+    template <int ACT> __device__ __forceinline__ void operator()() {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            uint64_t a, da;
+            act_both<ACT>(g[i], a, da);
+            g[i] = mul2(mul2(dh[i], u[i]), da);
+            u[i] = mul2(dh[i], a);
         }
     }
 };
@@ -472,7 +519,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     } else {
         // ---------------------------------------------------- epilogue: a thread has one row of the tile
         const uint32_t tmem = sm->tmem_base;
-        const int part = warp & 3;   // the 32 accumulator lanes that this warp may read
+        const int part = warp & 3, half = (warp - 2) >> 2;   // the 32 accumulator lanes that this warp may read; its columns
         int buf = 0;
         uint32_t ph = 0;
         for (int64_t tile = unit; tile < tiles; tile += units) {
@@ -487,9 +534,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 const int m_out = FORM == kWgrad && m >= p.mt / 2 ? m - p.mt / 2 : m;
                 float* row = reinterpret_cast<float*>(stages) + (size_t)in_tile * TL::pitch;
                 const bool live = (int64_t)m_out * TL::M + in_tile < p.rows;
-                const int c_end = __any_sync(0xffffffffu, live) ? BN : 0;
+                const int c_end = __any_sync(0xffffffffu, live) ? (half + 1) * kHalf : 0;
 #pragma unroll 1
-                for (int c = 0; c < c_end; c += 32) {
+                for (int c = half * kHalf; c < c_end; c += 32) {
                     float f[32];
                     tmem_load32(at + c, f);
                     if (live) {
@@ -501,64 +548,60 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             } else if constexpr (kGated) {
                 const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * kHalf;
                 const bool live = row < p.rows;
-                float gmax = 0.f, umax = 0.f;
+                const int c_begin = half * (kHalf / 2), c_end = c_begin + kHalf / 2;     // this warp's columns of h
 #pragma unroll 1
-                for (int c = 0; c < kHalf; c += 32) {
+                for (int c = c_begin; c < c_end; c += 32) {
                     float g[32], u[32];
-                    tmem_load32(at + c, g);
-                    tmem_load32(at + kHalf + c, u);
+                    tmem_load32(at + c, at + kHalf + c, g, u);
                     if constexpr (FORM == kForward) {
-                        if (p.gq) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                gmax = fmaxf(gmax, fabsf(g[i]));
-                                umax = fmaxf(umax, fabsf(u[i]));
-                            }
-                        }
                         by_act(p.act, HOf<32>{g, u});
                         if (live) store32(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, p.out_vec, u);
                     } else if (live) {
                         float dh[32];
-                        load32(static_cast<const T*>(p.dh) + row * p.lddh, c0 + c, p.cols, p.dh_vec, dh);
+                        load32(static_cast<const T*>(p.dh) + row * p.lddh, c0 + c, p.cols, true, dh);
                         by_act(p.act, DguOf<32>{g, u, dh});
                         store32(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, true, g);
                         store32(static_cast<T*>(p.out1) + row * p.ldo, c0 + c, p.cols, true, u);
                     }
                 }
                 if (FORM == kForward && BN == 256 && p.gq) {
-                    const bool odd = __any_sync(0xffffffffu, is_inf(gmax) || is_inf(umax));   // an Inf somewhere: see keep_pairs
-                    if (odd) {
-                        gmax = umax = 0.f;
-#pragma unroll 1
-                        for (int c = 0; c < kHalf; c += 32) {
-                            float f[32];
-                            tmem_load32(at + c, f);
-                            for (int i = 0; i < 32; ++i) gmax = fmaxf(gmax, fabsf(inf_to_nan(f[i])));
-                            tmem_load32(at + kHalf + c, f);
-                            for (int i = 0; i < 32; ++i) umax = fmaxf(umax, fabsf(inf_to_nan(f[i])));
-                        }
-                    }
-                    const uint32_t ge = keep_exponent(gmax), ue = keep_exponent(umax);
-                    const float ginv = keep_inverse(ge), uinv = keep_inverse(ue);
+                    // half of the warps keep g, the others u: a thread finds the largest of its 128 entries, then converts them
+                    const uint32_t from = at + half * kHalf;
+                    float amax = 0.f;
 #pragma unroll 1
                     for (int c = 0; c < kHalf; c += 32) {
                         float f[32];
-                        tmem_load32(at + c, f);
-                        if (live) keep32(p.gq + row * p.ldq, c0 + c, p.cols, p.q_vec, odd, ginv, f);
-                        tmem_load32(at + kHalf + c, f);
-                        if (live) keep32(p.uq + row * p.ldq, c0 + c, p.cols, p.q_vec, odd, uinv, f);
+                        tmem_load32(from + c, f);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(f[i]));
                     }
-                    if (live) {
-                        p.ge[row * p.lde + n] = (uint8_t)ge;
-                        p.ue[row * p.lde + n] = (uint8_t)ue;
+                    const bool odd = __any_sync(0xffffffffu, is_inf(amax));   // an Inf somewhere: see keep_pairs
+                    if (odd) {
+                        amax = 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < kHalf; c += 32) {
+                            float f[32];
+                            tmem_load32(from + c, f);
+                            for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(inf_to_nan(f[i])));
+                        }
                     }
+                    const uint32_t e = keep_exponent(amax);
+                    const float inv = keep_inverse(e);
+                    uint8_t* to = (half ? p.uq : p.gq) + row * p.ldq;
+#pragma unroll 1
+                    for (int c = 0; c < kHalf; c += 32) {
+                        float f[32];
+                        tmem_load32(from + c, f);
+                        if (live) keep32(to, c0 + c, p.cols, p.q_vec, odd, inv, f);
+                    }
+                    if (live) (half ? p.ue : p.ge)[row * p.lde + n] = (uint8_t)e;
                 }
             } else {
                 void* out = p.out0;
                 if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
                 const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * BN;
 #pragma unroll 1
-                for (int c = 0; c < BN; c += 32) {
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
                     float f[32];
                     tmem_load32(at + c, f);
                     if (row < p.rows) store32(static_cast<OT*>(out) + row * p.ldo, c0 + c, p.cols, p.out_vec, f);
@@ -671,7 +714,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
 
 // ---- what the backward pass lays out before its products -----------------------------------------
 // dg and du from the kept g and u, in one pass: dh and both 8-bit matrices with their scales in, dg and du out; and,
-// when the input comes in 8 bits, its entries for the weight gradients.  A thread has 8 columns of a row at a time.
+// when the input comes in 8 bits, its entries for the weight gradients.
 struct PrepareArgs {
     const void* dh; int64_t lddh; bool dh_vec;
     const uint8_t *gq, *ge, *uq, *ue;
@@ -688,10 +731,11 @@ struct PrepareArgs {
     void* x; int64_t ldx;
 };
 
-// The pieces of 8 columns of a matrix, dealt to the threads of the grid; the row is carried along, not divided out.
+// The pieces of `W` columns of a matrix, dealt to the threads of the grid; the row is carried along, not divided out.
+template <int W>
 struct Pieces {
     int64_t row, k, drow, dk, per_row;
-    __device__ __forceinline__ explicit Pieces(int64_t cols) : per_row((cols + 7) / 8) {
+    __device__ __forceinline__ explicit Pieces(int64_t cols) : per_row((cols + W - 1) / W) {
         const int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, stride = (int64_t)gridDim.x * blockDim.x;
         row = item / per_row;
         k = item % per_row;
@@ -704,72 +748,100 @@ struct Pieces {
         if (k >= per_row) { k -= per_row; ++row; }
     }
 };
-// 8 bytes of a row of 8-bit entries, zeros beyond its end
-__device__ __forceinline__ uint2 load8(const uint8_t* row, int64_t c, int64_t cols, bool vec) {
-    if (vec && c + 8 <= cols) return __ldcs(reinterpret_cast<const uint2*>(row + c));
-    uint32_t w[2] = {0u, 0u};
+constexpr int kWide = 16;   // columns of a thread: 16 bytes of the 8-bit form
+// 16 bytes of a row of 8-bit entries, zeros beyond its end
+__device__ __forceinline__ uint4 load_kept(const uint8_t* row, int64_t c, int64_t cols, bool vec) {
+    if (vec && c + kWide <= cols) return ld_stream_u4(row + c);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kWide; ++i)
         if (c + i < cols) w[i / 4] |= (uint32_t)row[c + i] << (8 * (i % 4));
-    return make_uint2(w[0], w[1]);
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void taken8(uint2 q, uint8_t e, float (&f)[8]) {
+__device__ __forceinline__ void taken_pairs(uint4 q, uint8_t e, uint64_t (&p)[kWide / 2]) {
     const float scale = keep_scale_of_byte(e);
-    float lo[4], hi[4];
-    taken4(q.x, lo);
-    taken4(q.y, hi);
+    const uint64_t scale2 = pair_of(scale, scale);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { f[i] = lo[i] * scale; f[4 + i] = hi[i] * scale; }
+    for (int i = 0; i < 4; ++i) {
+        float f[4];
+        taken4(w[i], f);
+        p[2 * i] = mul2(pair_of(f[0], f[1]), scale2);
+        p[2 * i + 1] = mul2(pair_of(f[2], f[3]), scale2);
+    }
+}
+// two 16-byte pieces of a workspace row (padded to whole pieces)
+template <typename T>
+__device__ __forceinline__ void store_wide(T* to, const uint64_t (&p)[kWide / 2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint64_t half[4] = {p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]};
+        *reinterpret_cast<uint4*>(to + 8 * k) = Piece<T>::join(half);
+    }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) gated_prepare_kernel(const __grid_constant__ PrepareArgs p) {
     pdl_trigger();
     pdl_wait();
-    for (Pieces it(p.cols); it.row < p.rows; it.next()) {
-        const int64_t c = it.k * 8;
+    for (Pieces<kWide> it(p.cols); it.row < p.rows; it.next()) {
+        const int64_t c = it.k * kWide;
         const T* dh_row = static_cast<const T*>(p.dh) + it.row * p.lddh;
-        float dh[8], g[8], u[8];
-        if (p.dh_vec && c + 8 <= p.cols) {
-            Piece<T>::split(ld_stream_u4(dh_row + c), dh);
+        const int64_t at = it.row * p.ldq, block = it.row * p.lde + c / kKeepBlock;
+        uint64_t dh[8], g[8], u[8];
+        const uint4 gq = load_kept(p.gq + at, c, p.cols, p.q_vec), uq = load_kept(p.uq + at, c, p.cols, p.q_vec);
+        const uint8_t ge = p.ge[block], ue = p.ue[block];
+        if (p.dh_vec && c + kWide <= p.cols) {
+            uint64_t lo[4], hi[4];
+            Piece<T>::split(ld_stream_u4(dh_row + c), lo);
+            Piece<T>::split(ld_stream_u4(dh_row + c + 8), hi);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { dh[i] = lo[i]; dh[4 + i] = hi[i]; }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dh[i] = c + i < p.cols ? to_f32(dh_row[c + i]) : 0.f;
+            for (int i = 0; i < 8; ++i)
+                dh[i] = pair_of(c + 2 * i < p.cols ? to_f32(dh_row[c + 2 * i]) : 0.f, c + 2 * i + 1 < p.cols ? to_f32(dh_row[c + 2 * i + 1]) : 0.f);
         }
-        const int64_t at = it.row * p.ldq, block = it.row * p.lde + c / kKeepBlock;
-        taken8(load8(p.gq + at, c, p.cols, p.q_vec), p.ge[block], g);
-        taken8(load8(p.uq + at, c, p.cols, p.q_vec), p.ue[block], u);
-        by_act(p.act, DguOf<8>{g, u, dh});
-        // (the workspace rows are padded to whole pieces)
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.dg) + it.row * p.ldo + c) = Piece<T>::join(g);
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.du) + it.row * p.ldo + c) = Piece<T>::join(u);
+        taken_pairs(gq, ge, g);
+        taken_pairs(uq, ue, u);
+        by_act(p.act, DguPairsOf<8>{g, u, dh});
+        store_wide(static_cast<T*>(p.dg) + it.row * p.ldo + c, g);
+        store_wide(static_cast<T*>(p.du) + it.row * p.ldo + c, u);
     }
     if (!p.xq) return;
-    for (Pieces it(p.x_cols); it.row < p.rows; it.next()) {
-        const int64_t c = it.k * 8;
-        float x[8];
-        taken8(load8(p.xq + it.row * p.ldxq, c, p.x_cols, p.xq_vec), p.xe[it.row * p.ldxe + c / kKeepBlock], x);
+    for (Pieces<kWide> it(p.x_cols); it.row < p.rows; it.next()) {
+        const int64_t c = it.k * kWide;
+        uint64_t x[8];
+        taken_pairs(load_kept(p.xq + it.row * p.ldxq, c, p.x_cols, p.xq_vec), p.xe[it.row * p.ldxe + c / kKeepBlock], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = taken_clamp<T>(x[i]);
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.x) + it.row * p.ldx + c) = Piece<T>::join(x);
+        for (int i = 0; i < 8; ++i) x[i] = pair_of(taken_clamp<T>(pair_lo(x[i])), taken_clamp<T>(pair_hi(x[i])));
+        store_wide(static_cast<T*>(p.x) + it.row * p.ldx + c, x);
     }
 }
 
-// A matrix that TMA cannot address, copied to 16-byte aligned rows.
-__global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t* __restrict__ X, int64_t ld, int64_t rows,
-                                                         int64_t cols, uint16_t* __restrict__ Y, int64_t ldy) {
+// Matrices whose rows are not 16-byte aligned, copied to rows that are (blockIdx.y says which).
+constexpr int kMaxCopies = 4;
+struct CopyArgs {
+    const uint16_t* from[kMaxCopies];
+    int64_t ld[kMaxCopies], rows[kMaxCopies], cols[kMaxCopies];
+    uint16_t* to[kMaxCopies];
+    int64_t ld_to[kMaxCopies];
+};
+__global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ CopyArgs p) {
     pdl_trigger();
     pdl_wait();
-    for (Pieces it(cols); it.row < rows; it.next()) {
+    const int which = blockIdx.y;
+    const int64_t cols = p.cols[which];
+    for (Pieces<8> it(cols); it.row < p.rows[which]; it.next()) {
         const int64_t c = it.k * 8;
-        const uint16_t* x = X + it.row * ld;
+        const uint16_t* x = p.from[which] + it.row * p.ld[which];
         uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t lo = c + 2 * i < cols ? x[c + 2 * i] : 0u, hi = c + 2 * i + 1 < cols ? x[c + 2 * i + 1] : 0u;
             v[i] = lo | (hi << 16);
         }
-        *reinterpret_cast<uint4*>(Y + it.row * ldy + c) = make_uint4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<uint4*>(p.to[which] + it.row * p.ld_to[which] + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
 
@@ -782,10 +854,10 @@ struct Mat {
 bool tma_ok(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
 int64_t padded(int64_t cols) { return (cols + 63) / 64 * 64; }
 
-// The workspace: status word | aligned copies where TMA needs them (x also when it comes in 8 bits) | dg | du
+// The workspace: status word | aligned copies where a kernel needs them (x also when it comes in 8 bits) | dg | du
 struct GatedPlan {
     bool copy_x, copy_wg, copy_wu;
-    size_t x, wg, wu, dg, du, total;
+    size_t x, wg, wu, dh, dg, du, total;
 };
 GatedPlan gated_plan(const detox_gated_desc& g, bool backward) {
     GatedPlan q;
@@ -801,6 +873,7 @@ GatedPlan gated_plan(const detox_gated_desc& g, bool backward) {
     q.x = take(q.copy_x, g.tokens, g.in_dim);
     q.wg = take(q.copy_wg, g.hidden, g.in_dim);
     q.wu = take(q.copy_wu, g.hidden, g.in_dim);
+    q.dh = take(backward && !g.GQ, g.tokens, g.hidden);
     q.dg = take(backward, g.tokens, g.hidden);
     q.du = take(backward, g.tokens, g.hidden);
     q.total = off;
@@ -812,30 +885,42 @@ unsigned items_grid(int64_t items) {
     return (unsigned)(need < most ? need : most);
 }
 
-detox_status aligned_copy(const void* X, int64_t ld, int64_t rows, int64_t cols, void* to, Mat* out, cudaStream_t s) {
-    *out = Mat{to, padded(cols)};
-    return launch_chained(align_rows_kernel, items_grid(rows * ceil_div(cols, (int64_t)8)), 256, 0, 1, s,
-                          static_cast<const uint16_t*>(X), ld, rows, cols, static_cast<uint16_t*>(to), padded(cols));
-}
-
-detox_status input_matrix(const detox_gated_desc& g, const GatedPlan& q, char* ws, Mat* out, cudaStream_t s) {
-    if (!q.copy_x) {
-        *out = Mat{g.X, g.ldx};
+// The copies of a call, in one launch.
+struct Copies {
+    CopyArgs args{};
+    int n = 0;
+    int64_t items = 0;
+    // `m` as it is, or where its copy will be
+    Mat add(bool copy, const Mat& m, int64_t rows, int64_t cols, void* to) {
+        if (!copy) return m;
+        args.from[n] = static_cast<const uint16_t*>(m.p);
+        args.ld[n] = m.ld;
+        args.rows[n] = rows;
+        args.cols[n] = cols;
+        args.to[n] = static_cast<uint16_t*>(to);
+        args.ld_to[n] = padded(cols);
+        const int64_t k = rows * ceil_div(cols, (int64_t)8);
+        items = k > items ? k : items;
+        ++n;
+        return Mat{to, padded(cols)};
+    }
+    detox_status launch(cudaStream_t s) const {
+        if (n == 0) return DETOX_OK;
+        return launch_chained(align_rows_kernel, dim3(items_grid(items), (unsigned)n), 256, 0, 1, s, args);
+    }
+};
+// x where the products can read it; an 8-bit x is laid out by a kernel of its own
+detox_status input_matrix(const detox_gated_desc& g, const GatedPlan& q, char* ws, Copies* copies, Mat* out, cudaStream_t s) {
+    if (g.X) {
+        *out = copies->add(q.copy_x, Mat{g.X, g.ldx}, g.tokens, g.in_dim, ws + q.x);
         return DETOX_OK;
     }
-    if (g.X) return aligned_copy(g.X, g.ldx, g.tokens, g.in_dim, ws + q.x, out, s);
     *out = Mat{ws + q.x, padded(g.in_dim)};
     return launch_checkpoint_unpack(g.dtype, g.XQ, g.ldxq, g.XE, g.ldxe, g.tokens, g.in_dim, ws + q.x, padded(g.in_dim), s);
 }
-detox_status weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Mat* wg, Mat* wu, cudaStream_t s) {
-    *wg = Mat{g.Wg, g.ldwg};
-    *wu = Mat{g.Wu, g.ldwu};
-    if (q.copy_wg) {
-        const detox_status st = aligned_copy(g.Wg, g.ldwg, g.hidden, g.in_dim, ws + q.wg, wg, s);
-        if (st != DETOX_OK) return st;
-    }
-    if (q.copy_wu) return aligned_copy(g.Wu, g.ldwu, g.hidden, g.in_dim, ws + q.wu, wu, s);
-    return DETOX_OK;
+void weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Copies* copies, Mat* wg, Mat* wu) {
+    *wg = copies->add(q.copy_wg, Mat{g.Wg, g.ldwg}, g.hidden, g.in_dim, ws + q.wg);
+    *wu = copies->add(q.copy_wu, Mat{g.Wu, g.ldwu}, g.hidden, g.in_dim, ws + q.wu);
 }
 
 // Which shape a product takes: rows x cols is the accumulator (forward and recompute have 2 x hidden columns), nkb the slices of
@@ -921,8 +1006,10 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
     const GatedPlan q = gated_plan(g, false);
     int* status = reinterpret_cast<int*>(ws);
     Mat x, wg, wu;
-    detox_status st = input_matrix(g, q, ws, &x, s);
-    if (st == DETOX_OK) st = weight_matrices(g, q, ws, &wg, &wu, s);
+    Copies copies;
+    detox_status st = input_matrix(g, q, ws, &copies, &x, s);
+    weight_matrices(g, q, ws, &copies, &wg, &wu);
+    if (st == DETOX_OK) st = copies.launch(s);
     if (st != DETOX_OK) return st;
     GemmArgs a{};
     a.clear_status = true;
@@ -966,27 +1053,30 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
     const Mat dg{ws + q.dg, ldf}, du{ws + q.du, ldf};
     Mat x{nullptr, 0}, wg{nullptr, 0}, wu{nullptr, 0};
     detox_status st = DETOX_OK;
+    Copies copies;
     const bool with_x = kept && !g.X && dWg;         // an 8-bit input, laid out in the pass that makes dg and du
     if (with_x) x = Mat{ws + q.x, padded(g.in_dim)};
-    else if (dWg || !kept) st = input_matrix(g, q, ws, &x, s);
-    if (st == DETOX_OK && (dX || !kept)) st = weight_matrices(g, q, ws, &wg, &wu, s);
+    else if (dWg || !kept) st = input_matrix(g, q, ws, &copies, &x, s);
+    if (dX || !kept) weight_matrices(g, q, ws, &copies, &wg, &wu);
+    const Mat dh = copies.add(!kept && !tma_ok(dH, lddh), Mat{dH, lddh}, g.tokens, g.hidden, ws + q.dh);
+    if (st == DETOX_OK) st = copies.launch(s);
     if (st != DETOX_OK) return st;
     if (kept) {
         PrepareArgs a{};
         a.dh = dH; a.lddh = lddh; a.dh_vec = tma_ok(dH, lddh);
         a.gq = g.GQ; a.ge = g.GE; a.uq = g.UQ; a.ue = g.UE;
         a.ldq = g.ldq; a.lde = g.lde;
-        a.q_vec = aligned_to(g.GQ, 8) && aligned_to(g.UQ, 8) && g.ldq % 8 == 0;
+        a.q_vec = aligned16(g.GQ) && aligned16(g.UQ) && g.ldq % 16 == 0;
         a.act = g.act;
         a.rows = g.tokens; a.cols = g.hidden;
         a.dg = const_cast<void*>(dg.p); a.du = const_cast<void*>(du.p); a.ldo = ldf;
         if (with_x) {
             a.xq = g.XQ; a.xe = g.XE; a.ldxq = g.ldxq; a.ldxe = g.ldxe;
-            a.xq_vec = aligned_to(g.XQ, 8) && g.ldxq % 8 == 0;
+            a.xq_vec = aligned16(g.XQ) && g.ldxq % 16 == 0;
             a.x_cols = g.in_dim;
             a.x = const_cast<void*>(x.p); a.ldx = x.ld;
         }
-        st = launch_chained(gated_prepare_kernel<T>, items_grid(g.tokens * ceil_div(g.hidden, (int64_t)8)), 256, 0, 1, s, a);
+        st = launch_chained(gated_prepare_kernel<T>, items_grid(g.tokens * ceil_div(g.hidden, (int64_t)kWide)), 256, 0, 1, s, a);
     } else {
         GemmArgs a{};
         a.clear_status = true;
@@ -997,9 +1087,8 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         a.out0 = const_cast<void*>(dg.p);
         a.out1 = const_cast<void*>(du.p);
         a.ldo = ldf;
-        a.dh = dH;
-        a.lddh = lddh;
-        a.dh_vec = tma_ok(dH, lddh);
+        a.dh = dh.p;
+        a.lddh = dh.ld;
         const MapOf mx{x, g.tokens, g.in_dim}, mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
         st = launch_gemm<T, T, kRecompute>(mx, mx, mg, mu, a, status, s);
     }
