@@ -169,35 +169,28 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
     return v;
 }
 
-// 32 columns of this thread's accumulator row, or two times 32.  Load and wait are one statement, so that nothing that uses
-// the values can be moved between them.
-__device__ __forceinline__ void tmem_load32(uint32_t at, float (&f)[32]) {
+// kChunk columns of this thread's accumulator row, or two times as many.  Load and wait are one statement, so that nothing that
+// uses the values can be moved between them.  Sixteen columns at a time: a CTA with one tile runs its epilogue once, and the
+// longer a body is unrolled, the more of it goes into fetching instructions (a tile of 128 x 256: 2.6 us with 32, 2.1 with 16).
+constexpr int kChunk = 16;
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&f)[kChunk]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]), "=f"(f[8]),
-          "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]), "=f"(f[16]),
-          "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]), "=f"(f[22]), "=f"(f[23]), "=f"(f[24]),
-          "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31])
+        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]),
+          "=f"(f[8]), "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15])
         : "r"(at)
         : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at_f, uint32_t at_g, float (&f)[32], float (&g)[32]) {
+__device__ __forceinline__ void tmem_load(uint32_t at_f, uint32_t at_g, float (&f)[kChunk], float (&g)[kChunk]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, "
-        "%46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]), "=f"(f[8]),
-          "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]), "=f"(f[16]),
-          "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]), "=f"(f[22]), "=f"(f[23]), "=f"(f[24]),
-          "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31]),
-          "=f"(g[0]), "=f"(g[1]), "=f"(g[2]), "=f"(g[3]), "=f"(g[4]), "=f"(g[5]), "=f"(g[6]), "=f"(g[7]), "=f"(g[8]),
-            "=f"(g[9]), "=f"(g[10]), "=f"(g[11]), "=f"(g[12]), "=f"(g[13]), "=f"(g[14]), "=f"(g[15]), "=f"(g[16]),
-            "=f"(g[17]), "=f"(g[18]), "=f"(g[19]), "=f"(g[20]), "=f"(g[21]), "=f"(g[22]), "=f"(g[23]), "=f"(g[24]),
-            "=f"(g[25]), "=f"(g[26]), "=f"(g[27]), "=f"(g[28]), "=f"(g[29]), "=f"(g[30]), "=f"(g[31])
+        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]),
+          "=f"(f[8]), "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]),
+          "=f"(g[0]), "=f"(g[1]), "=f"(g[2]), "=f"(g[3]), "=f"(g[4]), "=f"(g[5]), "=f"(g[6]), "=f"(g[7]),
+          "=f"(g[8]), "=f"(g[9]), "=f"(g[10]), "=f"(g[11]), "=f"(g[12]), "=f"(g[13]), "=f"(g[14]), "=f"(g[15])
         : "r"(at_f), "r"(at_g)
         : "memory");
 }
@@ -288,13 +281,13 @@ struct DguPairsOf {   // the same on pairs
     }
 };
 
-// ---- 32 consecutive entries of an output row ----------------------------------------------------
+// ---- kChunk consecutive entries of an output row -------------------------------------------------
 template <typename OT>
-__device__ __forceinline__ void store32(OT* row, int64_t c, int64_t cols, bool vec, const float (&f)[32]) {
+__device__ __forceinline__ void store_chunk(OT* row, int64_t c, int64_t cols, bool vec, const float (&f)[kChunk]) {
     constexpr int N = Piece<OT>::N;
-    if (vec && c + 32 <= cols) {
+    if (vec && c + kChunk <= cols) {
 #pragma unroll
-        for (int i = 0; i < 32 / N; ++i) {
+        for (int i = 0; i < kChunk / N; ++i) {
             float p[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) p[j] = f[i * N + j];
@@ -302,16 +295,16 @@ __device__ __forceinline__ void store32(OT* row, int64_t c, int64_t cols, bool v
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
+        for (int i = 0; i < kChunk; ++i)
             if (c + i < cols) row[c + i] = from_f32<OT>(f[i]);
     }
 }
 template <typename T>
-__device__ __forceinline__ void load32(const T* row, int64_t c, int64_t cols, bool vec, float (&f)[32]) {
+__device__ __forceinline__ void load_chunk(const T* row, int64_t c, int64_t cols, float (&f)[kChunk]) {
     constexpr int N = Piece<T>::N;
-    if (vec && c + 32 <= cols) {
+    if (c + kChunk <= cols) {
 #pragma unroll
-        for (int i = 0; i < 32 / N; ++i) {
+        for (int i = 0; i < kChunk / N; ++i) {
             float p[N];
             Piece<T>::split(*reinterpret_cast<const uint4*>(row + c + i * N), p);
 #pragma unroll
@@ -319,24 +312,23 @@ __device__ __forceinline__ void load32(const T* row, int64_t c, int64_t cols, bo
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.f;
+        for (int i = 0; i < kChunk; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.f;
     }
 }
-// 32 entries of the 8-bit form
-__device__ __forceinline__ void keep32(uint8_t* row, int64_t c, int64_t cols, bool vec, bool odd, float inv, float (&f)[32]) {
-    uint32_t q[8];
+// ... in the 8-bit form
+__device__ __forceinline__ void keep_chunk(uint8_t* row, int64_t c, int64_t cols, bool vec, bool odd, float inv, float (&f)[kChunk]) {
+    uint32_t q[4];
     if (odd) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = inf_to_nan(f[i]);
+        for (int i = 0; i < kChunk; ++i) f[i] = inf_to_nan(f[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = keep4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
-    if (vec && c + 32 <= cols) {
+    for (int i = 0; i < 4; ++i) q[i] = keep4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
+    if (vec && c + kChunk <= cols) {
         *reinterpret_cast<uint4*>(row + c) = make_uint4(q[0], q[1], q[2], q[3]);
-        *reinterpret_cast<uint4*>(row + c + 16) = make_uint4(q[4], q[5], q[6], q[7]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
+        for (int i = 0; i < kChunk; ++i)
             if (c + i < cols) row[c + i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
     }
 }
@@ -356,6 +348,97 @@ __device__ __forceinline__ void store_few(OT* row, int64_t c, int64_t cols, bool
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (c + i < cols) row[c + i] = from_f32<OT>(f[i]);
+    }
+}
+
+// The end of a split: the CTA of rank `rank` finishes its share of the tile's rows.  A warp takes B of them at a time, a lane
+// E columns of the tile's first half and E of the second; the S sums of an entry lie in the S CTAs' shared memory and are all
+// asked for before the first is used (one round trip over the cluster's network), then added in the order of the ranks.
+template <typename T, typename OT, int FORM, int BN, int S>
+__device__ __forceinline__ void finish_split(const GemmArgs& p, int m, int n, uint32_t rank, uint32_t sums, int warp, int lane) {
+    using TL = Tile<1, BN>;
+    constexpr bool kGated = FORM == kForward || FORM == kRecompute;
+    constexpr int kHalf = BN / 2, E = BN / 64, B = S <= 2 ? 4 : 2;
+    void* out = p.out0;
+    if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
+    const int64_t row0 = (int64_t)m * TL::M;
+    const int live = (int)(p.rows - row0 < TL::M ? p.rows - row0 : TL::M);
+    const int share = (live + S - 1) / S;
+    const int last = (int)(rank + 1) * share < live ? (int)(rank + 1) * share : live;
+    uint32_t from[S];
+#pragma unroll
+    for (int k = 0; k < S; ++k) from[k] = cluster_addr(sums, k) + (uint32_t)lane * (E * 4);
+    for (int r0 = (int)rank * share + warp * B; r0 < last; r0 += kThreads / 32 * B) {
+        float va[B][S][E], vb[B][S][E];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const uint32_t off = (uint32_t)(r0 + i < last ? r0 + i : r0) * (TL::pitch * 4);
+#pragma unroll
+            for (int k = 0; k < S; ++k) {
+                if constexpr (E == 4) {
+                    const float4 x = ld_cluster_f4(from[k] + off), y = ld_cluster_f4(from[k] + off + kHalf * 4);
+                    va[i][k][0] = x.x; va[i][k][1] = x.y; va[i][k][2] = x.z; va[i][k][3] = x.w;
+                    vb[i][k][0] = y.x; vb[i][k][1] = y.y; vb[i][k][2] = y.z; vb[i][k][3] = y.w;
+                } else {
+                    const float2 x = ld_cluster_f2(from[k] + off), y = ld_cluster_f2(from[k] + off + kHalf * 4);
+                    va[i][k][0] = x.x; va[i][k][1] = x.y;
+                    vb[i][k][0] = y.x; vb[i][k][1] = y.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (r0 + i >= last) break;
+            float a[E], b[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                a[j] = va[i][0][j];
+                b[j] = vb[i][0][j];
+#pragma unroll
+                for (int k = 1; k < S; ++k) { a[j] += va[i][k][j]; b[j] += vb[i][k][j]; }
+            }
+            const int64_t row = row0 + r0 + i;
+            if constexpr (kGated) {
+                const int64_t c = (int64_t)n * kHalf + lane * E;
+                if constexpr (FORM == kForward) {
+                    if (BN == 256 && p.gq) {
+                        uint64_t ga[2] = {pair_of(a[0], a[1]), pair_of(a[E - 2], a[E - 1])};
+                        uint64_t ub[2] = {pair_of(b[0], b[1]), pair_of(b[E - 2], b[E - 1])};
+                        uint32_t gq[1], uq[1];
+                        const uint32_t ge = keep_pairs<2, 32>(ga, gq), ue = keep_pairs<2, 32>(ub, uq);
+                        if (p.q_vec && c + E <= p.cols) {
+                            *reinterpret_cast<uint32_t*>(p.gq + row * p.ldq + c) = gq[0];
+                            *reinterpret_cast<uint32_t*>(p.uq + row * p.ldq + c) = uq[0];
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < E; ++j)
+                                if (c + j < p.cols) {
+                                    p.gq[row * p.ldq + c + j] = (uint8_t)(gq[0] >> (8 * j));
+                                    p.uq[row * p.ldq + c + j] = (uint8_t)(uq[0] >> (8 * j));
+                                }
+                        }
+                        if (lane == 0) {
+                            p.ge[row * p.lde + n] = (uint8_t)ge;
+                            p.ue[row * p.lde + n] = (uint8_t)ue;
+                        }
+                    }
+                    by_act(p.act, HOf<E>{a, b});
+                    store_few<T, E>(static_cast<T*>(out) + row * p.ldo, c, p.cols, p.out_vec, b);
+                } else {
+                    float dh[E];
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        dh[j] = c + j < p.cols ? to_f32(static_cast<const T*>(p.dh)[row * p.lddh + c + j]) : 0.f;
+                    by_act(p.act, DguOf<E>{a, b, dh});
+                    store_few<T, E>(static_cast<T*>(p.out0) + row * p.ldo, c, p.cols, true, a);
+                    store_few<T, E>(static_cast<T*>(p.out1) + row * p.ldo, c, p.cols, true, b);
+                }
+            } else {
+                const int64_t c = (int64_t)n * BN + lane * E;
+                store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c, p.cols, p.out_vec, a);
+                store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c + kHalf, p.cols, p.out_vec, b);
+            }
+        }
     }
 }
 
@@ -536,12 +619,12 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 const bool live = (int64_t)m_out * TL::M + in_tile < p.rows;
                 const int c_end = __any_sync(0xffffffffu, live) ? (half + 1) * kHalf : 0;
 #pragma unroll 1
-                for (int c = half * kHalf; c < c_end; c += 32) {
-                    float f[32];
-                    tmem_load32(at + c, f);
+                for (int c = half * kHalf; c < c_end; c += kChunk) {
+                    float f[kChunk];
+                    tmem_load(at + c, f);
                     if (live) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
+                        for (int i = 0; i < kChunk / 4; ++i)
                             *reinterpret_cast<float4*>(row + c + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
                     }
                 }
@@ -550,18 +633,18 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 const bool live = row < p.rows;
                 const int c_begin = half * (kHalf / 2), c_end = c_begin + kHalf / 2;     // this warp's columns of h
 #pragma unroll 1
-                for (int c = c_begin; c < c_end; c += 32) {
-                    float g[32], u[32];
-                    tmem_load32(at + c, at + kHalf + c, g, u);
+                for (int c = c_begin; c < c_end; c += kChunk) {
+                    float g[kChunk], u[kChunk];
+                    tmem_load(at + c, at + kHalf + c, g, u);
                     if constexpr (FORM == kForward) {
-                        by_act(p.act, HOf<32>{g, u});
-                        if (live) store32(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, p.out_vec, u);
+                        by_act(p.act, HOf<kChunk>{g, u});
+                        if (live) store_chunk(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, p.out_vec, u);
                     } else if (live) {
-                        float dh[32];
-                        load32(static_cast<const T*>(p.dh) + row * p.lddh, c0 + c, p.cols, true, dh);
-                        by_act(p.act, DguOf<32>{g, u, dh});
-                        store32(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, true, g);
-                        store32(static_cast<T*>(p.out1) + row * p.ldo, c0 + c, p.cols, true, u);
+                        float dh[kChunk];
+                        load_chunk(static_cast<const T*>(p.dh) + row * p.lddh, c0 + c, p.cols, dh);
+                        by_act(p.act, DguOf<kChunk>{g, u, dh});
+                        store_chunk(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, true, g);
+                        store_chunk(static_cast<T*>(p.out1) + row * p.ldo, c0 + c, p.cols, true, u);
                     }
                 }
                 if (FORM == kForward && BN == 256 && p.gq) {
@@ -569,30 +652,30 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     const uint32_t from = at + half * kHalf;
                     float amax = 0.f;
 #pragma unroll 1
-                    for (int c = 0; c < kHalf; c += 32) {
-                        float f[32];
-                        tmem_load32(from + c, f);
+                    for (int c = 0; c < kHalf; c += kChunk) {
+                        float f[kChunk];
+                        tmem_load(from + c, f);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(f[i]));
+                        for (int i = 0; i < kChunk; ++i) amax = fmaxf(amax, fabsf(f[i]));
                     }
                     const bool odd = __any_sync(0xffffffffu, is_inf(amax));   // an Inf somewhere: see keep_pairs
                     if (odd) {
                         amax = 0.f;
 #pragma unroll 1
-                        for (int c = 0; c < kHalf; c += 32) {
-                            float f[32];
-                            tmem_load32(from + c, f);
-                            for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(inf_to_nan(f[i])));
+                        for (int c = 0; c < kHalf; c += kChunk) {
+                            float f[kChunk];
+                            tmem_load(from + c, f);
+                            for (int i = 0; i < kChunk; ++i) amax = fmaxf(amax, fabsf(inf_to_nan(f[i])));
                         }
                     }
                     const uint32_t e = keep_exponent(amax);
                     const float inv = keep_inverse(e);
                     uint8_t* to = (half ? p.uq : p.gq) + row * p.ldq;
 #pragma unroll 1
-                    for (int c = 0; c < kHalf; c += 32) {
-                        float f[32];
-                        tmem_load32(from + c, f);
-                        if (live) keep32(to, c0 + c, p.cols, p.q_vec, odd, inv, f);
+                    for (int c = 0; c < kHalf; c += kChunk) {
+                        float f[kChunk];
+                        tmem_load(from + c, f);
+                        if (live) keep_chunk(to, c0 + c, p.cols, p.q_vec, odd, inv, f);
                     }
                     if (live) (half ? p.ue : p.ge)[row * p.lde + n] = (uint8_t)e;
                 }
@@ -601,10 +684,10 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
                 const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * BN;
 #pragma unroll 1
-                for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
-                    float f[32];
-                    tmem_load32(at + c, f);
-                    if (row < p.rows) store32(static_cast<OT*>(out) + row * p.ldo, c0 + c, p.cols, p.out_vec, f);
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c += kChunk) {
+                    float f[kChunk];
+                    tmem_load(at + c, f);
+                    if (row < p.rows) store_chunk(static_cast<OT*>(out) + row * p.ldo, c0 + c, p.cols, p.out_vec, f);
                 }
             }
             tc_fence_before();
@@ -625,85 +708,12 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             cluster_sync();
             int m, n;
             place(unit, m, n);
-            void* out = p.out0;
-            if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
-            const int64_t row0 = (int64_t)m * TL::M;
-            const int live = (int)(p.rows - row0 < TL::M ? p.rows - row0 : TL::M);
-            const int share = (live + p.split - 1) / p.split;
-            const int last = (int)(rank + 1) * share < live ? (int)(rank + 1) * share : live;
-            constexpr int E = BN / 64;                   // a lane's columns: E of the tile's first half, E of the second
-            uint32_t from[kMaxSplit];
-#pragma unroll
-            for (int k = 0; k < kMaxSplit; ++k) from[k] = cluster_addr(smem_u32(stages), k < p.split ? k : 0);
-            for (int r = (int)rank * share + warp; r < last; r += kThreads / 32) {
-                const uint32_t off = ((uint32_t)r * TL::pitch + (uint32_t)lane * E) * 4u;
-                float a[E], b[E], va[kMaxSplit][E], vb[kMaxSplit][E];
-#pragma unroll
-                for (int k = 0; k < kMaxSplit; ++k) {
-                    if (k < p.split) {
-                        if constexpr (E == 4) {
-                            const float4 x = ld_cluster_f4(from[k] + off), y = ld_cluster_f4(from[k] + off + kHalf * 4);
-                            va[k][0] = x.x; va[k][1] = x.y; va[k][2] = x.z; va[k][3] = x.w;
-                            vb[k][0] = y.x; vb[k][1] = y.y; vb[k][2] = y.z; vb[k][3] = y.w;
-                        } else {
-                            const float2 x = ld_cluster_f2(from[k] + off), y = ld_cluster_f2(from[k] + off + kHalf * 4);
-                            va[k][0] = x.x; va[k][1] = x.y;
-                            vb[k][0] = y.x; vb[k][1] = y.y;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) { a[i] = va[0][i]; b[i] = vb[0][i]; }
-#pragma unroll
-                for (int k = 1; k < kMaxSplit; ++k) {
-                    if (k < p.split) {
-#pragma unroll
-                        for (int i = 0; i < E; ++i) { a[i] += va[k][i]; b[i] += vb[k][i]; }
-                    }
-                }
-                const int64_t row = row0 + r;
-                if constexpr (kGated) {
-                    const int64_t c = (int64_t)n * kHalf + lane * E;
-                    if constexpr (FORM == kForward) {
-                        if (BN == 256 && p.gq) {
-                            uint64_t ga[2] = {pair_of(a[0], a[1]), pair_of(a[E - 2], a[E - 1])};
-                            uint64_t ub[2] = {pair_of(b[0], b[1]), pair_of(b[E - 2], b[E - 1])};
-                            uint32_t gk[1], uk[1];
-                            const uint32_t ge = keep_pairs<2, 32>(ga, gk), ue = keep_pairs<2, 32>(ub, uk);
-                            const uint32_t gq = gk[0], uq = uk[0];
-                            if (p.q_vec && c + E <= p.cols) {
-                                *reinterpret_cast<uint32_t*>(p.gq + row * p.ldq + c) = gq;
-                                *reinterpret_cast<uint32_t*>(p.uq + row * p.ldq + c) = uq;
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < E; ++i)
-                                    if (c + i < p.cols) {
-                                        p.gq[row * p.ldq + c + i] = (uint8_t)(gq >> (8 * i));
-                                        p.uq[row * p.ldq + c + i] = (uint8_t)(uq >> (8 * i));
-                                    }
-                            }
-                            if (lane == 0) {
-                                p.ge[row * p.lde + n] = (uint8_t)ge;
-                                p.ue[row * p.lde + n] = (uint8_t)ue;
-                            }
-                        }
-                        by_act(p.act, HOf<E>{a, b});
-                        store_few<T, E>(static_cast<T*>(out) + row * p.ldo, c, p.cols, p.out_vec, b);
-                    } else {
-                        float dh[E];
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            dh[i] = c + i < p.cols ? to_f32(static_cast<const T*>(p.dh)[row * p.lddh + c + i]) : 0.f;
-                        by_act(p.act, DguOf<E>{a, b, dh});
-                        store_few<T, E>(static_cast<T*>(p.out0) + row * p.ldo, c, p.cols, true, a);
-                        store_few<T, E>(static_cast<T*>(p.out1) + row * p.ldo, c, p.cols, true, b);
-                    }
-                } else {
-                    const int64_t c = (int64_t)n * BN + lane * E;
-                    store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c, p.cols, p.out_vec, a);
-                    store_few<OT, E>(static_cast<OT*>(out) + row * p.ldo, c + kHalf, p.cols, p.out_vec, b);
-                }
-            }
+            const uint32_t sums = smem_u32(stages);
+            if (p.split == 2) finish_split<T, OT, FORM, BN, 2>(p, m, n, rank, sums, warp, lane);
+            else if (p.split == 3) finish_split<T, OT, FORM, BN, 3>(p, m, n, rank, sums, warp, lane);
+            else if (p.split == 4) finish_split<T, OT, FORM, BN, 4>(p, m, n, rank, sums, warp, lane);
+            else if (p.split == 6) finish_split<T, OT, FORM, BN, 6>(p, m, n, rank, sums, warp, lane);
+            else finish_split<T, OT, FORM, BN, 8>(p, m, n, rank, sums, warp, lane);
         }
     }
     tc_fence_before();
@@ -927,9 +937,9 @@ void weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Co
 // its reduction.  The least of an estimate, in units of 10 ns, that was fitted to measurements of every shape:
 //   a slice        pair 28: the MMAs' own rate.  128 x 256 on one CTA 42, 128 x 128 27: a CTA takes in about 64 bytes a clock,
 //                  and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.  With one row of tiles every
-//                  byte of the weights comes from HBM for a single use, and the narrow tile is no faster (42).
-//   a tile         150 (drain of the last accumulator), 500 with a split (the cluster meets twice, sums move)
-//   a launch       500
+//                  byte of the weights comes from HBM for a single use, and no shape is faster than another (42).
+//   a tile         150 (drain of the last accumulator), or with a split of S 350 + 25 S (the cluster meets, sums move)
+//   a launch       400
 // The number of clusters that fit at once is that of a B200 (2 dies, GPCs of 14 to 20 SMs); it is a constant, so that
 // every GPU takes the same shape and gives the same bits.
 struct Shape {
@@ -942,16 +952,18 @@ Shape gemm_shape(int64_t rows, int64_t cols, int nkb, bool keeps) {
     auto consider = [&](int cg, int bn, int split, int64_t slice) {
         const int64_t tiles = ceil_div(rows, (int64_t)(128 * cg)) * ceil_div(cols, (int64_t)bn);
         const int64_t waves = ceil_div(tiles, (int64_t)kClusters[cg * split]);
-        const int64_t time = waves * (ceil_div((int64_t)nkb, (int64_t)split) * slice + (split > 1 ? 500 : 150)) + 500;
+        const int64_t time = waves * (ceil_div((int64_t)nkb, (int64_t)split) * slice + (split > 1 ? 350 + 25 * split : 150)) + 400;
         if (time < least) {
             least = time;
             best = Shape{cg, bn, split};
         }
     };
-    consider(2, 256, 1, 28);
-    for (int split = 1; split <= kMaxSplit && split <= nkb; ++split) {
+    const bool one_row = rows <= 128;
+    consider(2, 256, 1, one_row ? 42 : 28);
+    for (int split : {1, 2, 3, 4, 6, 8}) {   // (clusters of 5 and 7 leave more SMs idle than their neighbours)
+        if (split > nkb) break;
         consider(1, 256, split, 42);
-        if (!keeps) consider(1, 128, split, rows <= 128 ? 42 : 27);   // (the 8-bit form needs a block of 128 columns in a tile)
+        if (!keeps) consider(1, 128, split, one_row ? 42 : 27);   // (the 8-bit form needs a block of 128 columns in a tile)
     }
     return best;
 }
