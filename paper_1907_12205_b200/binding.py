@@ -1,4 +1,4 @@
-"""ctypes binding of libdetox.so: argument marshalling only.
+"""Binding of libdetox.so (ctypes; for the worker-side operators a compiled module): argument marshalling only.
 
 Every function has the name and the meaning of the C entry point in include/detox.h.  Tensors are
 torch CUDA tensors used as device memory; matrices may be column-sliced views (the row stride is
@@ -525,131 +525,43 @@ class Kept(NamedTuple):
         return self.e[1]
 
 
-def _rows(t: torch.Tensor, what: str, dtype=None, shape=None):
-    """(pointer, row stride) of a matrix with contiguous rows, after checking its type and shape."""
-    try:
-        rows, cols = t.shape
-        ld, step = t.stride()
-        here = t.is_cuda
-    except (AttributeError, ValueError, TypeError):
-        here = False
-    if not here:
-        raise TypeError(f"{what}: expected a 2-D CUDA tensor")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
-    if shape is not None and (rows, cols) != shape:
-        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {(rows, cols)}")
-    if step != 1 and cols > 1:
-        raise ValueError(f"{what}: rows must be contiguous")
-    if ld < cols:
-        if rows > 1:
-            raise ValueError(f"{what}: rows overlap")
-        ld = cols
-    return t.data_ptr(), ld
+_worker_module = None
 
 
-def _dtype_code(dtype, what: str) -> int:
-    code = _DTYPE.get(dtype)
-    if code is None:
-        raise TypeError(f"{what}: expected float32, float16 or bfloat16, got {dtype}")
-    return code
+def _worker():
+    """The compiled module that checks tensors, makes outputs and calls the library for the functions below (a call's
+    marshalling in Python took 10 to 40 us, more than the small kernels).  Raises if it is not built."""
+    global _worker_module
+    if _worker_module is None:
+        load()
+        from . import _worker as module
+        module.set_error(DetoxError)
+        _worker_module = module
+    return _worker_module
 
 
-def _vector(t: torch.Tensor, what: str, dtype, n: int) -> int:
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()):
-        raise TypeError(f"{what}: expected a contiguous CUDA vector of {n} entries of {dtype}")
-    return t.data_ptr()
-
-
-def _blocks(cols: int) -> int:
-    return -(-cols // KEEP_BLOCK)
-
-
-def _kept_pair(q, e, what: str, shape=None):
-    qp, ldq = _rows(q, what, torch.float8_e4m3fn, shape)
-    rows, cols = q.shape
-    ep, lde = _rows(e, what + " scales", torch.float8_e8m0fnu, (rows, _blocks(cols)))
-    return qp, ldq, ep, lde
-
-
-def _new_rows(rows: int, cols: int, dtype, like: torch.Tensor):
-    """(matrix, pointer, stride): rows a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses."""
-    n = 16 // dtype.itemsize
-    ld = -(-cols // n) * n
-    t = like.new_empty((rows, ld), dtype=dtype)
-    return (t if ld == cols else t[:, :cols]), t.data_ptr(), ld
-
-
-def _new_kept(rows: int, cols: int, like: torch.Tensor):
-    q, qp, ldq = _new_rows(rows, cols, torch.float8_e4m3fn, like)
-    lde = _blocks(cols)
-    e = like.new_empty((rows, lde), dtype=torch.float8_e8m0fnu)
-    return q, e, (qp, ldq, e.data_ptr(), lde)
-
-
-def _workspace(nbytes: int, ws: Optional[torch.Tensor], like: torch.Tensor):
-    if ws is None:
-        ws = like.new_empty((max(int(nbytes), 256),), dtype=torch.uint8)
-    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+def _handle(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def detox_checkpoint_pack(x: torch.Tensor, out=None, stream=None):
     """Rows in the 8-bit form: (q, e), float8_e4m3fn values and float8_e8m0fnu scales, one for each block of KEEP_BLOCK
     columns of a row.  out: such a pair to write into."""
-    xp, ld = _rows(x, "x")
-    code = _dtype_code(x.dtype, "x")
-    rows, cols = x.shape
-    if out is None:
-        q, e, (qp, ldq, ep, lde) = _new_kept(rows, cols, x)
-    else:
-        q, e = out
-        qp, ldq, ep, lde = _kept_pair(q, e, "out", (rows, cols))
-    _check(load().detox_checkpoint_pack(code, xp, ld, rows, cols, qp, ldq, ep, lde, _stream(stream)), "detox_checkpoint_pack")
-    return q, e
+    q, e = (None, None) if out is None else out
+    return (_worker_module or _worker()).checkpoint_pack(x, q, e, _handle(stream))
 
 
 def detox_checkpoint_unpack(q: torch.Tensor, e: torch.Tensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
                             stream=None) -> torch.Tensor:
     """The way back from detox_checkpoint_pack: rows of `dtype`."""
-    qp, ldq, ep, lde = _kept_pair(q, e, "q")
-    rows, cols = q.shape
-    code = _dtype_code(dtype if out is None else out.dtype, "out")
-    if out is None:
-        out, xp, ld = _new_rows(rows, cols, dtype, q)
-    else:
-        xp, ld = _rows(out, "out", None, (rows, cols))
-    _check(load().detox_checkpoint_unpack(code, qp, ldq, ep, lde, rows, cols, xp, ld, _stream(stream)), "detox_checkpoint_unpack")
-    return out
+    return (_worker_module or _worker()).checkpoint_unpack(q, e, _dtype_code(dtype), out, _handle(stream))
 
 
 def detox_rmsnorm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                   want_y: bool = True, want_q: bool = False, sum_out: Optional[torch.Tensor] = None, stream=None) -> RmsNorm:
     """s = x + residual, y = s / rms(s) * w.  want_q: y also (want_y=False: only) in the 8-bit form.  The sum comes back
     when there is a residual, in sum_out when given (which may be x or residual itself)."""
-    xp, ldx = _rows(x, "x")
-    dtype = x.dtype
-    code = _dtype_code(dtype, "x")
-    shape = rows, cols = tuple(x.shape)
-    wp = _vector(w, "w", dtype, cols)
-    rp = sp = yp = qp = ep = s = y = q = e = None
-    ldr = lds = ldy = ldq = lde = 0
-    if residual is not None:
-        rp, ldr = _rows(residual, "residual", dtype, shape)
-        if sum_out is None:
-            s, sp, lds = _new_rows(rows, cols, dtype, x)
-        else:
-            s = sum_out
-            sp, lds = _rows(s, "sum_out", dtype, shape)
-    elif sum_out is not None:
-        raise ValueError("sum_out: there is no residual to add")
-    if want_y:
-        y, yp, ldy = _new_rows(rows, cols, dtype, x)
-    if want_q:
-        q, e, (qp, ldq, ep, lde) = _new_kept(rows, cols, x)
-    rstd = x.new_empty((rows,), dtype=torch.float32)
-    _check(load().detox_rmsnorm(code, xp, ldx, rp, ldr, wp, rows, cols, eps, sp, lds, yp, ldy, qp, ldq, ep, lde,
-                                rstd.data_ptr(), _stream(stream)), "detox_rmsnorm")
-    return RmsNorm(s, y, q, e, rstd)
+    return RmsNorm._make((_worker_module or _worker()).rmsnorm(x, w, residual, eps, want_y, want_q, sum_out, _handle(stream)))
 
 
 def detox_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
@@ -661,89 +573,33 @@ def detox_rmsnorm_backward(dy: torch.Tensor, s: torch.Tensor, w: torch.Tensor, r
                            dw: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Gradients of detox_rmsnorm: (dx, dw).  s: the sum of the forward pass (its x when there was no residual); ds: the
     gradient that reaches the sum by its other uses.  dx is also the residual's gradient; dw is fp32."""
-    lib = load()
-    sp, lds = _rows(s, "s")
-    dtype = s.dtype
-    code = _dtype_code(dtype, "s")
-    shape = rows, cols = tuple(s.shape)
-    dyp, lddy = _rows(dy, "dy", dtype, shape)
-    dsp, ldds = (None, 0) if ds is None else _rows(ds, "ds", dtype, shape)
-    wp, rp = _vector(w, "w", dtype, cols), _vector(rstd, "rstd", torch.float32, rows)
-    if dx is None:
-        dx, dxp, lddx = _new_rows(rows, cols, dtype, s)
-    else:
-        dxp, lddx = _rows(dx, "dx", dtype, shape)
-    if dw is None:
-        dw = s.new_empty((cols,), dtype=torch.float32)
-    dwp = _vector(dw, "dw", torch.float32, cols)
-    ws, wsp, wb = _workspace(lib.detox_rmsnorm_backward_workspace_bytes(rows, cols), ws, s)
-    _check(lib.detox_rmsnorm_backward(code, dyp, lddy, dsp, ldds, sp, lds, wp, rp, rows, cols, dxp, lddx, dwp, wsp, wb,
-                                      _stream(stream)), "detox_rmsnorm_backward")
-    return dx, dw
+    return (_worker_module or _worker()).rmsnorm_backward(dy, s, w, rstd, ds, dx, dw, ws, _handle(stream))
 
 
-def _gated_desc(x, wg, wu, act: int, kept: Optional[Kept]):
-    """(descriptor, tokens, in_dim, hidden); x is a matrix or its 8-bit form (q, e)."""
-    dtype = wg.dtype
-    wgp, ldwg = _rows(wg, "wg")
-    shape = hidden, in_dim = tuple(wg.shape)
-    wup, ldwu = _rows(wu, "wu", dtype, shape)
-    xp = xq = xe = kg = ke = ku = kf = None
-    ldx = ldxq = ldxe = ldq = lde = 0
-    if isinstance(x, torch.Tensor):
-        xp, ldx = _rows(x, "x", dtype)
-        tokens, cols = x.shape
-    else:
-        q, e = x
-        xq, ldxq, xe, ldxe = _kept_pair(q, e, "x")
-        tokens, cols = q.shape
-    if cols != in_dim:
-        raise ValueError(f"x has {cols} columns, the weights {in_dim}")
-    if kept is not None:
-        q, e = kept
-        if not (q.is_cuda and e.is_cuda and q.dtype == torch.float8_e4m3fn and e.dtype == torch.float8_e8m0fnu):
-            raise TypeError("kept: expected float8_e4m3fn values and float8_e8m0fnu scales on the GPU")
-        if q.shape != (2, tokens, hidden) or e.shape != (2, tokens, _blocks(hidden)):
-            raise ValueError(f"kept: expected values [2, {tokens}, {hidden}] and their scales")
-        (half_q, ldq, step_q), (half_e, lde, step_e) = q.stride(), e.stride()
-        if (step_q != 1 and hidden > 1) or (step_e != 1 and e.shape[2] > 1):
-            raise ValueError("kept: rows must be contiguous")
-        kg, ke = q.data_ptr(), e.data_ptr()
-        ku, kf = kg + half_q, ke + half_e
-    d = GatedDesc(_dtype_code(dtype, "wg"), int(act), tokens, in_dim, hidden, xp, ldx, xq, ldxq, xe, ldxe, wgp, ldwg, wup, ldwu,
-                  kg, ke, ku, kf, ldq, lde)
-    return d, tokens, in_dim, hidden
+def _gated_inputs(x, kept: Optional[Kept]):
+    """x (a matrix, or its 8-bit form as a pair) and kept, as the module takes them."""
+    x, xe = (x, None) if isinstance(x, torch.Tensor) else x
+    q, e = (None, None) if kept is None else kept
+    return x, xe, q, e
 
 
 def detox_gated_workspace_bytes(x, wg, wu, act: int = ACT_SILU, kept: Optional[Kept] = None) -> int:
-    return int(load().detox_gated_workspace_bytes(ctypes.byref(_gated_desc(x, wg, wu, act, kept)[0])))
+    x, xe, q, e = _gated_inputs(x, kept)
+    return _worker().gated_workspace_bytes(x, xe, wg, wu, act, q, e, False)
 
 
 def detox_gated(x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU, keep: bool = False,
                 h: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """h = act(x wg^T) * (x wu^T).  x: a matrix, or its 8-bit form as a pair (q, e).  keep=True returns (h, Kept): g and u
     in the 8-bit form for the backward pass."""
-    lib = load()
-    d, tokens, _, hidden = _gated_desc(x, wg, wu, act, None)
-    if keep:
-        d.ldq, d.lde = ldq, lde = -(-hidden // 16) * 16, _blocks(hidden)
-        q = wg.new_empty((2, tokens, ldq), dtype=torch.float8_e4m3fn)
-        e = wg.new_empty((2, tokens, lde), dtype=torch.float8_e8m0fnu)
-        d.GQ, d.GE = qp, ep = q.data_ptr(), e.data_ptr()
-        d.UQ, d.UE = qp + tokens * ldq, ep + tokens * lde
-        kept = Kept(q if ldq == hidden else q[:, :, :hidden], e)
-    if h is None:
-        h, hp, ldh = _new_rows(tokens, hidden, wg.dtype, wg)
-    else:
-        hp, ldh = _rows(h, "h", wg.dtype, (tokens, hidden))
-    ref = ctypes.byref(d)
-    ws, wp, wb = _workspace(lib.detox_gated_workspace_bytes(ref), ws, wg)
-    _check(lib.detox_gated(ref, hp, ldh, wp, wb, _stream(stream)), "detox_gated")
-    return (h, kept) if keep else h
+    x, xe = (x, None) if isinstance(x, torch.Tensor) else x
+    h, q, e = (_worker_module or _worker()).gated(x, xe, wg, wu, act, None, None, keep, h, ws, _handle(stream))
+    return (h, Kept(q, e)) if keep else h
 
 
 def detox_gated_backward_workspace_bytes(x, wg, wu, act: int = ACT_SILU, kept: Optional[Kept] = None) -> int:
-    return int(load().detox_gated_backward_workspace_bytes(ctypes.byref(_gated_desc(x, wg, wu, act, kept)[0])))
+    x, xe, q, e = _gated_inputs(x, kept)
+    return _worker().gated_workspace_bytes(x, xe, wg, wu, act, q, e, True)
 
 
 def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU,
@@ -752,26 +608,12 @@ def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor
     """Gradients of detox_gated: (dx, dwg, dwu).  kept: what the forward pass kept; without it g and u are computed again.
     x as in detox_gated.  The weight gradients have the weights' type, or float32 with dw_dtype (or buffers of it, such as
     pieces of a gradient's row)."""
-    lib = load()
-    d, tokens, in_dim, hidden = _gated_desc(x, wg, wu, act, kept)
-    dtype, shape = wg.dtype, (hidden, in_dim)
-    dhp, lddh = _rows(dh, "dh", dtype, (tokens, hidden))
-    if dx is None:
-        dx, dxp, lddx = _new_rows(tokens, in_dim, dtype, wg)
-    else:
-        dxp, lddx = _rows(dx, "dx", dtype, (tokens, in_dim))
-    if (dwg is None) != (dwu is None):
-        raise ValueError("give both weight gradients or none")
-    if dwg is None:
-        dwg, gp, lddw = _new_rows(hidden, in_dim, dw_dtype or dtype, wg)
-        dwu, up, _ = _new_rows(hidden, in_dim, dw_dtype or dtype, wg)
-    else:
-        gp, lddw = _rows(dwg, "dwg", dw_dtype, shape)
-        up, ldu = _rows(dwu, "dwu", dwg.dtype, shape)
-        if ldu != lddw:
-            raise ValueError("dwg and dwu must have the same stride")
-    ref = ctypes.byref(d)
-    ws, wp, wb = _workspace(lib.detox_gated_backward_workspace_bytes(ref), ws, wg)
-    _check(lib.detox_gated_backward(ref, dhp, lddh, dxp, lddx, gp, up, lddw, _dtype_code(dwg.dtype, "dwg"), wp, wb,
-                                    _stream(stream)), "detox_gated_backward")
-    return dx, dwg, dwu
+    x, xe, q, e = _gated_inputs(x, kept)
+    return (_worker_module or _worker()).gated_backward(x, xe, wg, wu, act, q, e, dh, dx, dwg, dwu,
+                                                        -1 if dw_dtype is None else _dtype_code(dw_dtype), ws, _handle(stream))
+
+
+def _dtype_code(dtype) -> int:
+    if dtype not in _DTYPE:
+        raise TypeError(f"expected float32, float16 or bfloat16, got {dtype}")
+    return _DTYPE[dtype]

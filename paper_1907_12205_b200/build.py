@@ -1,4 +1,5 @@
-"""Builds libdetox.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libdetox.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and the Python module _worker that
+calls it (g++, against the installed torch)."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -11,6 +12,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdetox.so")
+MODULE_SRC = os.path.join(PKG, "csrc_py", "worker_module.cpp")
+MODULE = os.path.join(PKG, "_worker.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -44,6 +47,27 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _build_module(force: bool):
+    """The Python module; it finds libdetox.so beside itself."""
+    newest = max(os.path.getmtime(p) for p in (MODULE_SRC, os.path.join(ROOT, "include", "detox.h")))
+    if not force and os.path.exists(MODULE) and os.path.getmtime(MODULE) >= newest:
+        return
+    import sysconfig
+
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"], MODULE_SRC, "-o", MODULE,
+           "-L", PKG, "-l:libdetox.so", "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+           "-Wl,-rpath,$ORIGIN"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed on {MODULE_SRC}:\n{res.stdout}\n{res.stderr}")
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     if force:
@@ -58,6 +82,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         res = subprocess.run(cmd, capture_output=True, text=True)
         if res.returncode != 0:
             raise RuntimeError(f"link failed:\n{res.stdout}\n{res.stderr}")
+    _build_module(force)
     return LIB
 
 

@@ -69,6 +69,7 @@ struct GemmArgs {
     int kb0, kb1;                  // slices of the first and of the second product that are added up
     int split;                     // CTAs that share a tile's reduction
     bool clear_status;             // first kernel of the call that may set the status word
+    bool beside;                   // runs beside the product before it in the stream, see below
     bool n_first;                  // neighbouring tiles lie along a row of the output (else along a column)
     int act;
     int64_t rows, cols;            // of the output (forward, recompute: of h)
@@ -484,8 +485,11 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         else asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
     }
     tc_fence_after();
+    // The next kernel is let in only after this one's own wait, so by then all that came before this one is finished.  A
+    // product that needs nothing from the one before it (wgrad from dgrad) then need not wait to start, and takes the SMs
+    // that the other leaves idle; it waits at its end instead, so that whatever waits for it waits for both.
+    if (!p.beside) pdl_wait();
     pdl_trigger();
-    pdl_wait();
     if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it about a second later)
 
     // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
@@ -720,6 +724,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     __syncthreads();
     if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
     if (warp == 1) tmem_dealloc_cg<CG>(sm->tmem_base, TL::tmem_cols);
+    if (p.beside) pdl_wait();
 }
 
 // ---- what the backward pass lays out before its products -----------------------------------------
@@ -1041,9 +1046,10 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
 
 template <typename T, typename OT>
 detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Mat& du, const Mat& x, void* dWg, void* dWu,
-                              int64_t lddw, bool clear_status, int* status, cudaStream_t s) {
+                              int64_t lddw, bool clear_status, bool beside, int* status, cudaStream_t s) {
     GemmArgs a{};
     a.clear_status = clear_status;
+    a.beside = beside;
     a.kb0 = (int)ceil_div(g.tokens, (int64_t)kSlice);
     a.rows = g.hidden;
     a.cols = g.in_dim;
@@ -1120,8 +1126,8 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         if (st != DETOX_OK) return st;
     }
     if (!dWg) return DETOX_OK;
-    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, status, s);
-    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, status, s);
+    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, status, s);
+    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, status, s);
 }
 
 }  // namespace
