@@ -503,3 +503,127 @@ def test_status_word_reads_zero():
     dx.detox_gated_backward(dh, x, wg, wu, ws=ws)
     assert dx.read_status(ws) == 0
     dx.check_status(ws)
+
+
+def test_inf_and_nan_in_kept_projections():
+    """Inf and NaN among g and u are kept as NaN, and a block's scale comes from its finite entries: in the epilogue of a tile
+    of its own and in that of a tile whose reduction is split."""
+    gen = generator(41)
+    for tokens, in_dim in ((300, 64), (3, 1024), (2100, 64)):
+        x, wg, wu = ints(gen, -2, 2, tokens, in_dim), ints(gen, -1, 1, 700, in_dim), ints(gen, -1, 1, 700, in_dim)
+        wg[5, :] = math.inf       # g[:, 5] = +-Inf or NaN
+        wu[300, 0] = math.nan
+        dev = [t.to(BF16).to(DEV) for t in (x, wg, wu)]
+        _, kept = dx.detox_gated(*dev, dx.ACT_RELU, keep=True)
+        for w, q, e, bad in ((wg, kept.gq, kept.ge, 5), (wu, kept.uq, kept.ue, 300)):
+            fine = w.clone()
+            fine[bad] = 0.0
+            v = x @ fine.T
+            ref_q, ref_e, _ = kept_by_definition(v.numpy())
+            got = q.float().cpu().numpy()
+            assert np.isnan(got[:, bad]).all()
+            got[:, bad] = ref_q[:, bad] = 0.0
+            assert np.array_equal(got, ref_q) and np.array_equal(e.view(torch.uint8).cpu().numpy(), ref_e)
+
+
+@pytest.mark.parametrize("tokens,in_dim,hidden", [(9, 600, 300), (300, 100, 260), (2050, 64, 1400)])
+def test_kept_buffers_of_any_alignment(tokens, in_dim, hidden):
+    """Kept buffers with odd strides and offsets, which the C interface allows, hold and give back the same."""
+    import ctypes
+    gen = generator(42)
+    x, wg, wu, dh = (randn(gen, *s).to(F16).to(DEV) for s in ((tokens, in_dim), (hidden, in_dim), (hidden, in_dim), (tokens, hidden)))
+    h, kept = dx.detox_gated(x, wg, wu, dx.ACT_GELU, keep=True)
+    nb = -(-hidden // 128)
+    ldq, lde = hidden + 3, nb + 1
+    q = torch.full((2 * tokens * ldq + 8,), 9, dtype=torch.uint8, device=DEV)
+    e = torch.full((2 * tokens * lde + 8,), 9, dtype=torch.uint8, device=DEV)
+    vq = [q[1 + i * tokens * ldq: 1 + (i + 1) * tokens * ldq].view(tokens, ldq) for i in range(2)]
+    ve = [e[i * tokens * lde: (i + 1) * tokens * lde].view(tokens, lde) for i in range(2)]
+    d = dx.GatedDesc(dx.DTYPE_HALF, dx.ACT_GELU, tokens, in_dim, hidden, x.data_ptr(), x.stride(0), None, 0, None, 0, wg.data_ptr(), wg.stride(0),
+                     wu.data_ptr(), wu.stride(0), vq[0].data_ptr(), ve[0].data_ptr(), vq[1].data_ptr(), ve[1].data_ptr(), ldq, lde)
+    lib = dx.load()
+    ws = torch.empty(max(lib.detox_gated_workspace_bytes(ctypes.byref(d)), 256), dtype=torch.uint8, device=DEV)
+    h2 = torch.empty_like(h)
+    assert lib.detox_gated(ctypes.byref(d), h2.data_ptr(), h2.stride(0), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(h2, h)
+    for i, (a, b) in enumerate(((kept.gq, kept.ge), (kept.uq, kept.ue))):
+        assert torch.equal(vq[i][:, :hidden], a.view(torch.uint8)) and torch.equal(ve[i][:, :nb], b.view(torch.uint8))
+        assert bool((vq[i][:, hidden:] == 9).all()) and bool((ve[i][:, nb:] == 9).all())
+    f8, e8 = q[1: 1 + 2 * tokens * ldq].view(torch.float8_e4m3fn).view(2, tokens, ldq), e[: 2 * tokens * lde].view(torch.float8_e8m0fnu).view(2, tokens, lde)
+    odd = dx.Kept(f8[:, :, :hidden], e8[:, :, :nb])
+    for a, b in zip(dx.detox_gated_backward(dh, x, wg, wu, dx.ACT_GELU, kept=kept), dx.detox_gated_backward(dh, x, wg, wu, dx.ACT_GELU, kept=odd)):
+        assert torch.equal(a, b)
+
+
+def test_calls_one_after_another_on_the_same_buffers():
+    """Kernels start while the ones before them finish; calls that reuse outputs and workspace must not meet."""
+    gen = generator(43)
+    shapes = ((260, 512), (1408, 512), (1408, 512), (260, 1408))
+    sets = [[randn(gen, *s).to(BF16).to(DEV) for s in shapes] for _ in range(3)]
+    want = []
+    for x, wg, wu, dh in sets:
+        want.append([t.clone() for t in dx.detox_gated_backward(dh, x, wg, wu)])
+        torch.cuda.synchronize()
+    outs = [torch.empty_like(t) for t in want[0]]
+    ws = torch.empty(dx.detox_gated_backward_workspace_bytes(*sets[0][:3]), dtype=torch.uint8, device=DEV)
+    copies = []
+    for k in range(30):
+        x, wg, wu, dh = sets[k % 3]
+        dx.detox_gated_backward(dh, x, wg, wu, dx=outs[0], dwg=outs[1], dwu=outs[2], ws=ws)
+        if k >= 24:
+            copies.append((k % 3, [t.clone() for t in outs]))
+    # a chain in which each call reads what the one before it wrote
+    y = dx.detox_rmsnorm(sets[0][0], sets[0][1][0].contiguous()).y
+    for _ in range(10):
+        y = dx.detox_rmsnorm(y, sets[0][1][0].contiguous(), residual=sets[0][0]).y
+        q, e = dx.detox_checkpoint_pack(y)
+        y = dx.detox_checkpoint_unpack(q, e, BF16)
+    torch.cuda.synchronize()
+    for which, got in copies:
+        assert all(torch.equal(a, b) for a, b in zip(got, want[which]))
+    z = dx.detox_rmsnorm(sets[0][0], sets[0][1][0].contiguous()).y
+    for _ in range(10):
+        torch.cuda.synchronize()
+        z = dx.detox_rmsnorm(z, sets[0][1][0].contiguous(), residual=sets[0][0]).y
+        torch.cuda.synchronize()
+        q, e = dx.detox_checkpoint_pack(z)
+        torch.cuda.synchronize()
+        z = dx.detox_checkpoint_unpack(q, e, BF16)
+    assert torch.equal(y, z)
+
+
+def test_offsets_that_pass_32_bits():
+    """More than 2^32 entries of h: the first and last tokens are the ones of a small call, and so are their gradients."""
+    tokens, in_dim, hidden = 1_050_000, 64, 4096 + 8
+    g = torch.Generator(device=DEV).manual_seed(7)
+    x = torch.randn((tokens, in_dim), generator=g, device=DEV, dtype=torch.float32).to(BF16)
+    wg, wu = (torch.randn((hidden, in_dim), generator=g, device=DEV).mul_(0.125).to(BF16) for _ in range(2))
+    h = dx.detox_gated(x, wg, wu)
+    ends = torch.cat([torch.arange(300, device=DEV), torch.arange(tokens - 300, tokens, device=DEV)])
+    few = x[ends].contiguous()
+    ref = (torch.nn.functional.silu(few.double() @ wg.double().T) * (few.double() @ wu.double().T))
+    # silu is Lipschitz with 1.1; sums of 64 products of size up to 20
+    assert bool(((h[ends].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-3).all())
+    dh = h
+    gx, a, b = dx.detox_gated_backward(dh, x, wg, wu, dw_dtype=F32)
+    few_gx = dx.detox_gated_backward(dh[ends].contiguous(), few, wg, wu)[0]
+    assert bool(((gx[ends].double() - few_gx.double()).norm(dim=1) <= 2.0 ** -7 * few_gx.double().norm(dim=1)).all())
+    # dWu over all tokens, for the last rows of the weight: du = dh act(g), rounded to bf16
+    last = slice(hidden - 3, hidden)
+    total = torch.zeros((3, in_dim), dtype=torch.float64, device=DEV)
+    size = torch.zeros((3, in_dim), dtype=torch.float64, device=DEV)
+    for k in range(0, tokens, 150_000):
+        xs, ds = x[k: k + 150_000].double(), dh[k: k + 150_000, last].double()
+        du = ds * torch.nn.functional.silu(xs @ wg[last].double().T)
+        total += du.T @ xs
+        size += du.abs().T @ xs.abs()
+    # a rounding of 2^-8 in each du, and an fp32 chain over the tokens
+    assert bool(((b[last].double() - total).abs() <= (2.0 ** -8 + tokens * 2.0 ** -23) * size).all())
+    del h, dh, gx
+
+    rows = 1_100_000
+    x = torch.randn((rows, 4096), generator=g, device=DEV, dtype=F16)
+    w = torch.ones(4096, device=DEV, dtype=F16)
+    got = dx.detox_rmsnorm(x, w, want_y=True)
+    few = dx.detox_rmsnorm(x[-5:].contiguous(), w)
+    assert torch.equal(got.y[-5:], few.y) and torch.equal(got.rstd[-5:], few.rstd)
