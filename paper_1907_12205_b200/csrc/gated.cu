@@ -39,6 +39,7 @@ constexpr uint32_t kChunkBytes = 64 * 128;       // 64 rows of 128 bytes
 constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
 constexpr int kMaxSplit = 8;                     // CTAs of a portable cluster
 constexpr int kMaxStages = 6;
+constexpr int kRowBytes = 64, kRowPitch = 80, kWarpBuffer = 32 * kRowPitch;   // an epilogue warp's output rows, see flush_rows
 
 // CG: CTAs that multiply one tile together.  BN: columns of the tile (forward, recompute: half of g, half of u).
 template <int CG, int BN>
@@ -60,7 +61,8 @@ struct GemmSmem {
     int abort_flag;
 };
 template <int CG, int BN>
-constexpr size_t kSmemBytes = Tile<CG, BN>::stages * (size_t)Tile<CG, BN>::stage_bytes + sizeof(GemmSmem) + 1024;
+constexpr size_t kSmemBytes = Tile<CG, BN>::stages * (size_t)Tile<CG, BN>::stage_bytes + kEpiWarps * kWarpBuffer + sizeof(GemmSmem) + 1024;
+static_assert(kSmemBytes<2, 256> <= 227 * 1024 && kSmemBytes<1, 256> <= 227 * 1024 && kSmemBytes<1, 128> <= 227 * 1024, "fits an SM");
 static_assert(128 * Tile<1, 256>::pitch * 4 <= Tile<1, 256>::stages * Tile<1, 256>::stage_bytes, "a split's sums fit the stages");
 static_assert(128 * Tile<1, 128>::pitch * 4 <= Tile<1, 128>::stages * Tile<1, 128>::stage_bytes, "a split's sums fit the stages");
 
@@ -282,42 +284,71 @@ struct DguPairsOf {   // the same on pairs
     }
 };
 
-// ---- kChunk consecutive entries of an output row -------------------------------------------------
+// ---- output rows through shared memory ------------------------------------------------------------
+// A lane has a row of the accumulator, but 32 lanes that store 16 bytes each into 32 rows keep the load-store unit
+// busy for 32 cycles.  So a warp collects 64 bytes of each of its 32 rows in shared memory (rows 80 bytes apart: eight
+// lanes' 16-byte accesses meet no bank twice) and stores 8 rows of 64 bytes with one instruction.
+__device__ __forceinline__ uint4* own_row(uint8_t* buf, int lane) { return reinterpret_cast<uint4*>(buf + lane * kRowPitch); }
+
+// rows x cols: the part of `out` that exists, with the warp's first row at row 0 and the buffer's first column at column 0
 template <typename OT>
-__device__ __forceinline__ void store_chunk(OT* row, int64_t c, int64_t cols, bool vec, const float (&f)[kChunk]) {
-    constexpr int N = Piece<OT>::N;
-    if (vec && c + kChunk <= cols) {
+__device__ __forceinline__ void flush_rows(uint8_t* buf, OT* out, int64_t ld, int64_t rows, int64_t cols, bool vec, int lane) {
+    constexpr int W = kRowBytes / (int)sizeof(OT);
+    __syncwarp();
+    if (vec && cols >= W) {
+        const int r0 = lane / 4, part = lane % 4;
 #pragma unroll
-        for (int i = 0; i < kChunk / N; ++i) {
-            float p[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) p[j] = f[i * N + j];
-            *reinterpret_cast<uint4*>(row + c + i * N) = Piece<OT>::join(p);
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 8 * i;
+            if (r < rows) {
+                const uint4 v = *reinterpret_cast<const uint4*>(buf + r * kRowPitch + part * 16);
+                *reinterpret_cast<uint4*>(out + r * ld + part * (W / 4)) = v;
+            }
         }
     } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (c + i < cols) row[c + i] = from_f32<OT>(f[i]);
+        const int n = (int)(rows < 32 ? rows : 32);
+#pragma unroll 1
+        for (int r = 0; r < n; ++r)
+            for (int c = lane; c < W && c < cols; c += 32) out[r * ld + c] = reinterpret_cast<const OT*>(buf + r * kRowPitch)[c];
     }
+    __syncwarp();
 }
+// the way in, for 16-byte aligned rows: entries beyond the matrix read as zeros
 template <typename T>
-__device__ __forceinline__ void load_chunk(const T* row, int64_t c, int64_t cols, float (&f)[kChunk]) {
+__device__ __forceinline__ void fetch_rows(uint8_t* buf, const T* in, int64_t ld, int64_t rows, int64_t cols, int lane) {
     constexpr int N = Piece<T>::N;
-    if (c + kChunk <= cols) {
+    const int r0 = lane / 4, c = lane % 4 * N;
 #pragma unroll
-        for (int i = 0; i < kChunk / N; ++i) {
-            float p[N];
-            Piece<T>::split(*reinterpret_cast<const uint4*>(row + c + i * N), p);
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 8 * i;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) {
+            if (c + N <= cols) {
+                v = *reinterpret_cast<const uint4*>(in + r * ld + c);
+            } else {
+                float f[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) f[i * N + j] = p[j];
+                for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(in[r * ld + c + j]) : 0.f;
+                v = Piece<T>::join(f);
+            }
         }
-    } else {
+        *reinterpret_cast<uint4*>(buf + r * kRowPitch + lane % 4 * 16) = v;
+    }
+    __syncwarp();
+}
+// kChunk entries as 16-byte pieces of a row, and kChunk 8-bit ones
+template <typename OT>
+__device__ __forceinline__ void put_chunk(uint4* to, const float (&f)[kChunk]) {
+    constexpr int N = Piece<OT>::N;
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.f;
+    for (int i = 0; i < kChunk / N; ++i) {
+        float p[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) p[j] = f[i * N + j];
+        to[i] = Piece<OT>::join(p);
     }
 }
-// ... in the 8-bit form
-__device__ __forceinline__ void keep_chunk(uint8_t* row, int64_t c, int64_t cols, bool vec, bool odd, float inv, float (&f)[kChunk]) {
+__device__ __forceinline__ uint4 keep_chunk(bool odd, float inv, float (&f)[kChunk]) {
     uint32_t q[4];
     if (odd) {
 #pragma unroll
@@ -325,13 +356,7 @@ __device__ __forceinline__ void keep_chunk(uint8_t* row, int64_t c, int64_t cols
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[i] = keep4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
-    if (vec && c + kChunk <= cols) {
-        *reinterpret_cast<uint4*>(row + c) = make_uint4(q[0], q[1], q[2], q[3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (c + i < cols) row[c + i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
-    }
+    return make_uint4(q[0], q[1], q[2], q[3]);
 }
 
 // E consecutive entries of an output row (E = 2 or 4), as the lanes of a warp store a split's finished row
@@ -456,7 +481,8 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     constexpr int kHalf = BN / 2;                    // columns of g (and of u) in a tile
     extern __shared__ uint8_t smem_raw[];
     uint8_t* stages = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzled tiles need 1024-byte alignment
-    GemmSmem* sm = reinterpret_cast<GemmSmem*>(stages + (size_t)kStages * TL::stage_bytes);
+    uint8_t* buffers = stages + (size_t)kStages * TL::stage_bytes;
+    GemmSmem* sm = reinterpret_cast<GemmSmem*>(buffers + kEpiWarps * kWarpBuffer);
     volatile int* abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 || p.split > 1 ? cluster_rank() : 0u;
@@ -607,14 +633,15 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         // ---------------------------------------------------- epilogue: a thread has one row of the tile
         const uint32_t tmem = sm->tmem_base;
         const int part = warp & 3, half = (warp - 2) >> 2;   // the 32 accumulator lanes that this warp may read; its columns
-        int buf = 0;
+        uint8_t* buf = buffers + (warp - 2) * kWarpBuffer;
+        int acc = 0;
         uint32_t ph = 0;
         for (int64_t tile = unit; tile < tiles; tile += units) {
             int m, n;
             place(tile, m, n);
-            if (!__all_sync(0xffffffffu, mbar_wait(&sm->accum_full[buf], ph, abort_flag, status))) break;
+            if (!__all_sync(0xffffffffu, mbar_wait(&sm->accum_full[acc], ph, abort_flag, status))) break;
             tc_fence_after();
-            const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(buf * BN);
+            const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(acc * BN);
             const int in_tile = (CG == 2 ? (int)rank * 128 : 0) + part * 32 + lane;
             if (CG == 1 && p.split > 1) {
                 // (the one tile of this cluster, all its MMAs done: the stages are free to take the sums)
@@ -633,22 +660,44 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     }
                 }
             } else if constexpr (kGated) {
-                const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * kHalf;
-                const bool live = row < p.rows;
-                const int c_begin = half * (kHalf / 2), c_end = c_begin + kHalf / 2;     // this warp's columns of h
+                const int64_t row0 = (int64_t)m * TL::M + in_tile - lane, c0 = (int64_t)n * kHalf;
+                const int64_t rows = p.rows - row0;                                      // of this warp's that exist
+                constexpr int kOwn = kHalf / 2, W = kRowBytes / (int)sizeof(T);
 #pragma unroll 1
-                for (int c = c_begin; c < c_end; c += kChunk) {
-                    float g[kChunk], u[kChunk];
-                    tmem_load(at + c, at + kHalf + c, g, u);
+                for (int c = half * kOwn; c < (half + 1) * kOwn; c += W) {               // this warp's columns of h
+                    const int64_t col = c0 + c, cols = p.cols - col;
                     if constexpr (FORM == kForward) {
-                        by_act(p.act, HOf<kChunk>{g, u});
-                        if (live) store_chunk(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, p.out_vec, u);
-                    } else if (live) {
-                        float dh[kChunk];
-                        load_chunk(static_cast<const T*>(p.dh) + row * p.lddh, c0 + c, p.cols, dh);
-                        by_act(p.act, DguOf<kChunk>{g, u, dh});
-                        store_chunk(static_cast<T*>(p.out0) + row * p.ldo, c0 + c, p.cols, true, g);
-                        store_chunk(static_cast<T*>(p.out1) + row * p.ldo, c0 + c, p.cols, true, u);
+#pragma unroll 1
+                        for (int k = 0; k < W; k += kChunk) {
+                            float g[kChunk], u[kChunk];
+                            tmem_load(at + c + k, at + kHalf + c + k, g, u);
+                            by_act(p.act, HOf<kChunk>{g, u});
+                            put_chunk<T>(own_row(buf, lane) + k / Piece<T>::N, u);
+                        }
+                        flush_rows(buf, static_cast<T*>(p.out0) + row0 * p.ldo + col, p.ldo, rows, cols, p.out_vec, lane);
+                    } else {
+                        fetch_rows(buf, static_cast<const T*>(p.dh) + row0 * p.lddh + col, p.lddh, rows, cols, lane);
+                        uint4 du[kRowBytes / 16];
+#pragma unroll
+                        for (int k = 0; k < W; k += kChunk) {
+                            float g[kChunk], u[kChunk], dh[kChunk];
+                            uint4* mine = own_row(buf, lane) + k / Piece<T>::N;          // dh there becomes dg
+#pragma unroll
+                            for (int i = 0; i < kChunk / Piece<T>::N; ++i) {
+                                float f[Piece<T>::N];
+                                Piece<T>::split(mine[i], f);
+#pragma unroll
+                                for (int j = 0; j < Piece<T>::N; ++j) dh[i * Piece<T>::N + j] = f[j];
+                            }
+                            tmem_load(at + c + k, at + kHalf + c + k, g, u);
+                            by_act(p.act, DguOf<kChunk>{g, u, dh});
+                            put_chunk<T>(mine, g);
+                            put_chunk<T>(du + k / Piece<T>::N, u);
+                        }
+                        flush_rows(buf, static_cast<T*>(p.out0) + row0 * p.ldo + col, p.ldo, rows, cols, true, lane);
+#pragma unroll
+                        for (int i = 0; i < kRowBytes / 16; ++i) own_row(buf, lane)[i] = du[i];
+                        flush_rows(buf, static_cast<T*>(p.out1) + row0 * p.ldo + col, p.ldo, rows, cols, true, lane);
                     }
                 }
                 if (FORM == kForward && BN == 256 && p.gq) {
@@ -674,33 +723,42 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     }
                     const uint32_t e = keep_exponent(amax);
                     const float inv = keep_inverse(e);
-                    uint8_t* to = (half ? p.uq : p.gq) + row * p.ldq;
+                    uint8_t* to = half ? p.uq : p.gq;
 #pragma unroll 1
-                    for (int c = 0; c < kHalf; c += kChunk) {
-                        float f[kChunk];
-                        tmem_load(from + c, f);
-                        if (live) keep_chunk(to, c0 + c, p.cols, p.q_vec, odd, inv, f);
+                    for (int c = 0; c < kHalf; c += kRowBytes) {
+#pragma unroll 1
+                        for (int k = 0; k < kRowBytes; k += kChunk) {
+                            float f[kChunk];
+                            tmem_load(from + c + k, f);
+                            own_row(buf, lane)[k / kChunk] = keep_chunk(odd, inv, f);
+                        }
+                        flush_rows(buf, to + row0 * p.ldq + c0 + c, p.ldq, rows, p.cols - c0 - c, p.q_vec, lane);
                     }
-                    if (live) (half ? p.ue : p.ge)[row * p.lde + n] = (uint8_t)e;
+                    if (lane < rows) (half ? p.ue : p.ge)[(row0 + lane) * p.lde + n] = (uint8_t)e;
                 }
             } else {
                 void* out = p.out0;
                 if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
-                const int64_t row = (int64_t)m * TL::M + in_tile, c0 = (int64_t)n * BN;
+                const int64_t row0 = (int64_t)m * TL::M + in_tile - lane, c0 = (int64_t)n * BN;
+                constexpr int W = kRowBytes / (int)sizeof(OT);
 #pragma unroll 1
-                for (int c = half * kHalf; c < (half + 1) * kHalf; c += kChunk) {
-                    float f[kChunk];
-                    tmem_load(at + c, f);
-                    if (row < p.rows) store_chunk(static_cast<OT*>(out) + row * p.ldo, c0 + c, p.cols, p.out_vec, f);
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c += W) {
+#pragma unroll 1
+                    for (int k = 0; k < W; k += kChunk) {
+                        float f[kChunk];
+                        tmem_load(at + c + k, f);
+                        put_chunk<OT>(own_row(buf, lane) + k / Piece<OT>::N, f);
+                    }
+                    flush_rows(buf, static_cast<OT*>(out) + row0 * p.ldo + c0 + c, p.ldo, p.rows - row0, p.cols - c0 - c, p.out_vec, lane);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if constexpr (CG == 2) mbar_arrive_cluster(cluster_addr(smem_u32(&sm->accum_empty[buf]), 0));
-                else mbar_arrive(&sm->accum_empty[buf]);
+                if constexpr (CG == 2) mbar_arrive_cluster(cluster_addr(smem_u32(&sm->accum_empty[acc]), 0));
+                else mbar_arrive(&sm->accum_empty[acc]);
             }
-            if (++buf == 2) { buf = 0; ph ^= 1u; }
+            if (++acc == 2) { acc = 0; ph ^= 1u; }
         }
         __syncwarp();
     }
@@ -724,7 +782,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     __syncthreads();
     if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
     if (warp == 1) tmem_dealloc_cg<CG>(sm->tmem_base, TL::tmem_cols);
-    if (p.beside) pdl_wait();
+    if (p.beside && blockIdx.x + CG >= gridDim.x) pdl_wait();   // (the last CTAs only: the others' SMs are wanted)
 }
 
 // ---- what the backward pass lays out before its products -----------------------------------------
