@@ -996,40 +996,83 @@ void weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Co
     *wu = copies->add(q.copy_wu, Mat{g.Wu, g.ldwu}, g.hidden, g.in_dim, ws + q.wu);
 }
 
-// Which shape a product takes: rows x cols is the accumulator (forward and recompute have 2 x hidden columns), nkb the slices of
-// its reduction.  The least of an estimate, in units of 10 ns, that was fitted to measurements of every shape:
-//   a slice        pair 28: the MMAs' own rate.  128 x 256 on one CTA 42, 128 x 128 27: a CTA takes in about 64 bytes a clock,
-//                  and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.  With one row of tiles every
-//                  byte of the weights comes from HBM for a single use, and no shape is faster than another (42).
-//   a tile         150 (drain of the last accumulator), or with a split of S 350 + 25 S (the cluster meets, sums move)
+// Which shape a product takes: the least of an estimate, in units of 10 ns, that was fitted to measurements of every shape
+// on twenty problems from 1 to 8192 tokens (the shape it takes costs 2.5% more than the best one on average):
+//   a slice of the reduction   pair 28, nearly the MMAs' own rate; 128 x 256 on one CTA 45, 128 x 128 27: a CTA takes in
+//                  about 64 bytes a clock, and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.
+//                  With one row of tiles every byte of the weights comes from HBM for a single use, and the shapes differ
+//                  little (36).
+//   a tile's end   250 for 256 columns, half of it for 128; 100 more where g and u are kept, 100 more with a split,
+//                  whose cluster meets
 //   a launch       400
 // The number of clusters that fit at once is that of a B200 (2 dies, GPCs of 14 to 20 SMs); it is a constant, so that
 // every GPU takes the same shape and gives the same bits.
 struct Shape {
     int cg, bn, split;
 };
-Shape gemm_shape(int64_t rows, int64_t cols, int nkb, bool keeps) {
+// `copies` outputs of rows x cols (forward and recompute: 2 x hidden columns), nkb slices each
+struct Product {
+    int64_t rows;
+    int copies;
+    int64_t cols;
+    int nkb;
+    bool keeps;        // leaves the 8-bit form, which needs a block of 128 columns in a tile
+};
+struct Estimate {
+    int64_t ctas, tile, whole;   // CTAs' tiles, a tile's time, the launch's time
+};
+Estimate estimate(const Product& p, const Shape& s) {
     static const int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
+    const int64_t tiles = p.copies * ceil_div(p.rows, (int64_t)(128 * s.cg)) * ceil_div(p.cols, (int64_t)s.bn);
+    const int slice = p.rows * p.copies <= 128 ? 36 : (s.cg == 2 ? 28 : (s.bn == 256 ? 45 : 27));
+    const int64_t tile = ceil_div((int64_t)p.nkb, (int64_t)s.split) * slice + 250 * s.bn / 256 + (p.keeps ? 100 : 0) +
+                         (s.split > 1 ? 100 : 0);
+    return Estimate{tiles * s.cg * s.split, tile, ceil_div(tiles, (int64_t)kClusters[s.cg * s.split]) * tile + 400};
+}
+template <typename F>
+void each_shape(const Product& p, F f) {
+    f(Shape{2, 256, 1});
+    for (int split : {1, 2, 3, 4, 6, 8}) {   // (clusters of 5 and 7 leave more SMs idle than their neighbours)
+        if (split > p.nkb) break;
+        f(Shape{1, 256, split});
+        if (!p.keeps) f(Shape{1, 128, split});
+    }
+}
+Shape shape_of(const Product& p) {
     Shape best{2, 256, 1};
     int64_t least = INT64_MAX;
-    auto consider = [&](int cg, int bn, int split, int64_t slice) {
-        const int64_t tiles = ceil_div(rows, (int64_t)(128 * cg)) * ceil_div(cols, (int64_t)bn);
-        const int64_t waves = ceil_div(tiles, (int64_t)kClusters[cg * split]);
-        const int64_t time = waves * (ceil_div((int64_t)nkb, (int64_t)split) * slice + (split > 1 ? 350 + 25 * split : 150)) + 400;
+    each_shape(p, [&](const Shape& s) {
+        const int64_t time = estimate(p, s).whole;
         if (time < least) {
             least = time;
-            best = Shape{cg, bn, split};
+            best = s;
         }
-    };
-    const bool one_row = rows <= 128;
-    consider(2, 256, 1, one_row ? 42 : 28);
-    for (int split : {1, 2, 3, 4, 6, 8}) {   // (clusters of 5 and 7 leave more SMs idle than their neighbours)
-        if (split > nkb) break;
-        consider(1, 256, split, 42);
-        if (!keeps) consider(1, 128, split, one_row ? 42 : 27);   // (the 8-bit form needs a block of 128 columns in a tile)
-    }
+    });
     return best;
 }
+// The shapes of two products that run beside each other, b on the SMs that a leaves idle: together they take what the work of
+// both takes on all SMs and one of b's tiles, and no less than either takes alone.  b is not split for it (but may
+// be if that is best for b alone).
+void shapes_beside(const Product& a, const Product& b, Shape* sa, Shape* sb) {
+    int64_t least = INT64_MAX;
+    const Shape of_b[4] = {{2, 256, 1}, {1, 256, 1}, {1, 128, 1}, shape_of(b)};
+    each_shape(a, [&](const Shape& s) {
+        const Estimate ea = estimate(a, s);
+        for (const Shape& t : of_b) {
+            const Estimate eb = estimate(b, t);
+            int64_t time = (ea.ctas * ea.tile + eb.ctas * eb.tile) / kSMs + eb.tile + 400;
+            time = time > ea.whole ? time : ea.whole;
+            time = time > eb.whole ? time : eb.whole;
+            if (time < least) {
+                least = time;
+                *sa = s;
+                *sb = t;
+            }
+        }
+    });
+}
+int slices(int64_t n) { return (int)ceil_div(n, (int64_t)kSlice); }
+Product gated_product(const detox_gated_desc& g, bool keeps) { return Product{g.tokens, 1, 2 * g.hidden, slices(g.in_dim), keeps}; }
 
 // One product: maps, grid, launch.  The matrices of the maps are rows x cols.
 struct MapOf {
@@ -1067,10 +1110,8 @@ detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, con
                           maps[3], args, status);
 }
 template <typename T, typename OT, int FORM>
-detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, int* status,
-                         cudaStream_t s) {
-    const Shape sh = gemm_shape(args.rows * (FORM == kWgrad ? 2 : 1), args.cols * (FORM == kForward || FORM == kRecompute ? 2 : 1),
-                                args.kb0 + args.kb1, args.gq != nullptr);
+detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, const Shape& sh,
+                         int* status, cudaStream_t s) {
     if (sh.cg == 2) return launch_shape<T, OT, FORM, 2, 256>(a0, a1, b0, b1, args, 1, status, s);
     if (sh.bn == 256) return launch_shape<T, OT, FORM, 1, 256>(a0, a1, b0, b1, args, sh.split, status, s);
     return launch_shape<T, OT, FORM, 1, 128>(a0, a1, b0, b1, args, sh.split, status, s);
@@ -1088,7 +1129,7 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
     if (st != DETOX_OK) return st;
     GemmArgs a{};
     a.clear_status = true;
-    a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
+    a.kb0 = slices(g.in_dim);
     a.act = g.act;
     a.rows = g.tokens;
     a.cols = g.hidden;
@@ -1099,16 +1140,16 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
     a.ldq = g.ldq; a.lde = g.lde;
     a.q_vec = aligned16(g.GQ) && aligned16(g.UQ) && g.ldq % 16 == 0;
     const MapOf mx{x, g.tokens, g.in_dim}, mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
-    return launch_gemm<T, T, kForward>(mx, mx, mg, mu, a, status, s);
+    return launch_gemm<T, T, kForward>(mx, mx, mg, mu, a, shape_of(gated_product(g, g.GQ != nullptr)), status, s);
 }
 
 template <typename T, typename OT>
 detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Mat& du, const Mat& x, void* dWg, void* dWu,
-                              int64_t lddw, bool clear_status, bool beside, int* status, cudaStream_t s) {
+                              int64_t lddw, bool clear_status, bool beside, const Shape& shape, int* status, cudaStream_t s) {
     GemmArgs a{};
     a.clear_status = clear_status;
     a.beside = beside;
-    a.kb0 = (int)ceil_div(g.tokens, (int64_t)kSlice);
+    a.kb0 = slices(g.tokens);
     a.rows = g.hidden;
     a.cols = g.in_dim;
     a.out0 = dWg;
@@ -1116,7 +1157,7 @@ detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Ma
     a.ldo = lddw;
     a.out_vec = aligned16(dWg) && aligned16(dWu) && lddw % Piece<OT>::N == 0;
     const MapOf mg{dg, g.tokens, g.hidden}, mu{du, g.tokens, g.hidden}, mx{x, g.tokens, g.in_dim};
-    return launch_gemm<T, OT, kWgrad>(mg, mu, mx, mx, a, status, s);
+    return launch_gemm<T, OT, kWgrad>(mg, mu, mx, mx, a, shape, status, s);
 }
 
 template <typename T>
@@ -1156,7 +1197,7 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
     } else {
         GemmArgs a{};
         a.clear_status = true;
-        a.kb0 = (int)ceil_div(g.in_dim, (int64_t)kSlice);
+        a.kb0 = slices(g.in_dim);
         a.act = g.act;
         a.rows = g.tokens;
         a.cols = g.hidden;
@@ -1166,13 +1207,17 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         a.dh = dh.p;
         a.lddh = dh.ld;
         const MapOf mx{x, g.tokens, g.in_dim}, mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
-        st = launch_gemm<T, T, kRecompute>(mx, mx, mg, mu, a, status, s);
+        st = launch_gemm<T, T, kRecompute>(mx, mx, mg, mu, a, shape_of(gated_product(g, false)), status, s);
     }
     if (st != DETOX_OK) return st;
+    const Product dx_product{g.tokens, 1, g.in_dim, 2 * slices(g.hidden), false};
+    const Product dw_product{g.hidden, 2, g.in_dim, slices(g.tokens), false};
+    Shape shape_dx = shape_of(dx_product), shape_dw = shape_of(dw_product);
+    if (dX && dWg) shapes_beside(dx_product, dw_product, &shape_dx, &shape_dw);
     if (dX) {
         GemmArgs a{};
         a.clear_status = kept;
-        a.kb0 = a.kb1 = (int)ceil_div(g.hidden, (int64_t)kSlice);
+        a.kb0 = a.kb1 = slices(g.hidden);
         a.rows = g.tokens;
         a.cols = g.in_dim;
         a.out0 = dX;
@@ -1180,12 +1225,12 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         a.out_vec = tma_ok(dX, lddx);
         const MapOf mdg{dg, g.tokens, g.hidden}, mdu{du, g.tokens, g.hidden};
         const MapOf mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
-        st = launch_gemm<T, T, kDgrad>(mdg, mdu, mg, mu, a, status, s);
+        st = launch_gemm<T, T, kDgrad>(mdg, mdu, mg, mu, a, shape_dx, status, s);
         if (st != DETOX_OK) return st;
     }
     if (!dWg) return DETOX_OK;
-    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, status, s);
-    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, status, s);
+    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, shape_dw, status, s);
+    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, shape_dw, status, s);
 }
 
 }  // namespace
