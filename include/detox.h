@@ -340,8 +340,9 @@ detox_status detox_checkpoint_unpack(int dtype, const uint8_t* Q, int64_t ldq, c
  *   Y      dev, rows x ldy          out: the normed rows; may be NULL
  *   Q, E   dev                      out: the normed rows in the 8-bit form above (taken from fp32); both may be NULL
  *   rstd   dev, rows (fp32)         out: for the backward pass; may be NULL
- * At least one of S, Y, Q, rstd is given.  eps >= 0.  No workspace.
+ * At least one of S, Y, Q, rstd is given.  eps >= 0.  cols <= DETOX_NORM_MAX_COLS (a CTA holds a row).  No workspace.
  * ------------------------------------------------------------------------------------------- */
+#define DETOX_NORM_MAX_COLS 32768
 detox_status detox_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w, int64_t rows,
                            int64_t cols, float eps, void* S, int64_t lds, void* Y, int64_t ldy, uint8_t* Q, int64_t ldq,
                            uint8_t* E, int64_t lde, float* rstd, void* stream);
@@ -367,6 +368,9 @@ detox_status detox_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, con
  * stored in full), and its backward pass
  *     dg = dh * u * act'(g),   du = dh * act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
  * dg and du are rounded to dtype, the type the tensor cores multiply; every sum over them is fp32.
+ *
+ * dtype is HALF or BFLOAT (FLOAT: DETOX_ERR_UNSUPPORTED); tokens, in_dim and hidden are at most 2^30.  The weight gradients do
+ * not wait for dX: both products share the GPU.
  *
  * The input is X, or its 8-bit form XQ, XE (X = NULL).  With the kept buffers (all four or none) detox_gated leaves g and
  * u there in the 8-bit form, and detox_gated_backward reads them; without them it computes g and u again from the input.

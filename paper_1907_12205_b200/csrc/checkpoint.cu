@@ -26,9 +26,9 @@ struct Walk {
     }
 };
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ X, int64_t ld, int64_t rows, int64_t cols,
-                                                        int nblk, uint8_t* __restrict__ Q, int64_t ldq,
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ X, int64_t ld, Span span, int64_t rows, int64_t cols,
+                                                        int nblk, uint8_t* __restrict__ Q, int64_t ldq, bool q_vec,
                                                         uint8_t* __restrict__ E, int64_t lde) {
     constexpr int N = Piece<T>::N;
     pdl_trigger();
@@ -41,26 +41,23 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ X,
     for (; __any_sync(0xffffffffu, w.row < rows); w.step(drow, dblk, nblk)) {
         const bool live = w.row < rows;
         const int64_t c0 = (int64_t)w.blk * kKeepBlock + part * kPer;
-        const bool full = VEC && live && c0 + kPer <= cols;
-        const T* x = X + w.row * ld + c0;
+        const bool full = live && c0 + kPer <= cols;
+        const T* x = X + w.row * ld;
+        uint4 raw[kPer / N];
+#pragma unroll
+        for (int i = 0; i < kPer / N; ++i) raw[i] = load_piece<ANY>(x, c0 + i * N, live ? cols : (int64_t)0, span);
         uint64_t v[kPer / 2];
-        if (full) {
 #pragma unroll
-            for (int i = 0; i < kPer / N; ++i) {
-                uint64_t f[N / 2];
-                Piece<T>::split(ld_stream_u4(x + i * N), f);
+        for (int i = 0; i < kPer / N; ++i) {
+            uint64_t f[N / 2];
+            Piece<T>::split(raw[i], f);
 #pragma unroll
-                for (int j = 0; j < N / 2; ++j) v[i * (N / 2) + j] = f[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer / 2; ++i)
-                v[i] = pair_of(live && c0 + 2 * i < cols ? to_f32(x[2 * i]) : 0.f, live && c0 + 2 * i + 1 < cols ? to_f32(x[2 * i + 1]) : 0.f);
+            for (int j = 0; j < N / 2; ++j) v[i * (N / 2) + j] = f[j];
         }
         uint32_t q[kPer / 4];
         const uint32_t e = keep_pairs<kPer / 2, kLanes>(v, q);
         uint8_t* to = Q + w.row * ldq + c0;
-        if (full) {
+        if (full && (!ANY || q_vec)) {
             st_stream_u4(to, make_uint4(q[0], q[1], q[2], q[3]));
         } else if (live) {
 #pragma unroll
@@ -133,9 +130,10 @@ template <typename T>
 detox_status pack(const void* X, int64_t ld, int64_t rows, int64_t cols, uint8_t* Q, int64_t ldq, uint8_t* E, int64_t lde,
                   cudaStream_t s) {
     const int nblk = (int)ceil_div(cols, (int64_t)kKeepBlock);
-    const bool vec = aligned16(X) && ld % Piece<T>::N == 0 && aligned16(Q) && ldq % 16 == 0;
-    auto* k = vec ? pack_kernel<T, true> : pack_kernel<T, false>;
-    return launch_chained(k, grid_for(rows, nblk), kThreads, 0, 1, s, static_cast<const T*>(X), ld, rows, cols, nblk, Q, ldq, E, lde);
+    const Span span = span_of<T>(X, ld, rows, cols);
+    const bool q_vec = aligned16(Q) && ldq % 16 == 0;
+    return launch_chained(cols % Piece<T>::N == 0 && span.vec && q_vec ? pack_kernel<T, false> : pack_kernel<T, true>, grid_for(rows, nblk), kThreads, 0, 1, s,
+                          static_cast<const T*>(X), ld, span, rows, cols, nblk, Q, ldq, q_vec, E, lde);
 }
 template <typename T>
 detox_status unpack(const uint8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t rows, int64_t cols, void* X,

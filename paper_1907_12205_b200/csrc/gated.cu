@@ -789,7 +789,8 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
 // dg and du from the kept g and u, in one pass: dh and both 8-bit matrices with their scales in, dg and du out; and,
 // when the input comes in 8 bits, its entries for the weight gradients.
 struct PrepareArgs {
-    const void* dh; int64_t lddh; bool dh_vec;
+    const void* dh; int64_t lddh;
+    Span dh_span;
     const uint8_t *gq, *ge, *uq, *ue;
     int64_t ldq, lde;
     bool q_vec;
@@ -864,16 +865,12 @@ __global__ void __launch_bounds__(256) gated_prepare_kernel(const __grid_constan
         uint64_t dh[8], g[8], u[8];
         const uint4 gq = load_kept(p.gq + at, c, p.cols, p.q_vec), uq = load_kept(p.uq + at, c, p.cols, p.q_vec);
         const uint8_t ge = p.ge[block], ue = p.ue[block];
-        if (p.dh_vec && c + kWide <= p.cols) {
-            uint64_t lo[4], hi[4];
-            Piece<T>::split(ld_stream_u4(dh_row + c), lo);
-            Piece<T>::split(ld_stream_u4(dh_row + c + 8), hi);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { dh[i] = lo[i]; dh[4 + i] = hi[i]; }
-        } else {
+        for (int k = 0; k < 2; ++k) {
+            uint64_t f[4];
+            Piece<T>::split(load_piece<true>(dh_row, c + 8 * k, p.cols, p.dh_span), f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                dh[i] = pair_of(c + 2 * i < p.cols ? to_f32(dh_row[c + 2 * i]) : 0.f, c + 2 * i + 1 < p.cols ? to_f32(dh_row[c + 2 * i + 1]) : 0.f);
+            for (int i = 0; i < 4; ++i) dh[4 * k + i] = f[i];
         }
         taken_pairs(gq, ge, g);
         taken_pairs(uq, ue, u);
@@ -895,7 +892,8 @@ __global__ void __launch_bounds__(256) gated_prepare_kernel(const __grid_constan
 // Matrices whose rows are not 16-byte aligned, copied to rows that are (blockIdx.y says which).
 constexpr int kMaxCopies = 4;
 struct CopyArgs {
-    const uint16_t* from[kMaxCopies];
+    const __half* from[kMaxCopies];                // (16-bit entries of either type)
+    Span span[kMaxCopies];
     int64_t ld[kMaxCopies], rows[kMaxCopies], cols[kMaxCopies];
     uint16_t* to[kMaxCopies];
     int64_t ld_to[kMaxCopies];
@@ -907,14 +905,8 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
     const int64_t cols = p.cols[which];
     for (Pieces<8> it(cols); it.row < p.rows[which]; it.next()) {
         const int64_t c = it.k * 8;
-        const uint16_t* x = p.from[which] + it.row * p.ld[which];
-        uint32_t v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = c + 2 * i < cols ? x[c + 2 * i] : 0u, hi = c + 2 * i + 1 < cols ? x[c + 2 * i + 1] : 0u;
-            v[i] = lo | (hi << 16);
-        }
-        *reinterpret_cast<uint4*>(p.to[which] + it.row * p.ld_to[which] + c) = make_uint4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<uint4*>(p.to[which] + it.row * p.ld_to[which] + c) =
+            load_piece<true>(p.from[which] + it.row * p.ld[which], c, cols, p.span[which]);
     }
 }
 
@@ -966,7 +958,8 @@ struct Copies {
     // `m` as it is, or where its copy will be
     Mat add(bool copy, const Mat& m, int64_t rows, int64_t cols, void* to) {
         if (!copy) return m;
-        args.from[n] = static_cast<const uint16_t*>(m.p);
+        args.from[n] = static_cast<const __half*>(m.p);
+        args.span[n] = span_of<__half>(m.p, m.ld, rows, cols);
         args.ld[n] = m.ld;
         args.rows[n] = rows;
         args.cols[n] = cols;
@@ -1180,7 +1173,7 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
     if (st != DETOX_OK) return st;
     if (kept) {
         PrepareArgs a{};
-        a.dh = dH; a.lddh = lddh; a.dh_vec = tma_ok(dH, lddh);
+        a.dh = dH; a.lddh = lddh; a.dh_span = span_of<T>(dH, lddh, g.tokens, g.hidden);
         a.gq = g.GQ; a.ge = g.GE; a.uq = g.UQ; a.ue = g.UE;
         a.ldq = g.ldq; a.lde = g.lde;
         a.q_vec = aligned16(g.GQ) && aligned16(g.UQ) && g.ldq % 16 == 0;

@@ -5,7 +5,7 @@
 //
 // Both are bound by HBM, so a row is read once and stays in registers: TPR threads hold it, EPT entries each, in 16-byte
 // pieces dealt round the threads (piece t, t + TPR, ...).  With the 8-bit output a block of 128 columns then lies in 16
-// neighbouring lanes (fp32: 32), which agree on its largest entry by shuffles.  Up to 1024 columns a warp takes a row
+// neighbouring lanes (fp32: 32), which agree on its largest entry by shuffles.  Up to 512 columns a warp takes a row
 // and no barrier is needed; above that a CTA does.  The grid is persistent: the next row's pieces are asked for before the
 // present row's sum is formed, so that memory stays busy through the reductions.
 //
@@ -16,34 +16,6 @@
 namespace detox {
 
 namespace {
-
-// entries [c, c + N) of a row as they lie in memory, zeros beyond `cols`
-template <typename T, bool VEC>
-__device__ __forceinline__ uint4 load_piece(const T* row, int c, int cols) {
-    constexpr int N = Piece<T>::N;
-    if (VEC && c + N <= cols) return ld_stream_u4(row + c);
-    float f[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
-    return Piece<T>::join(f);
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T* row, int c, int cols, const uint64_t (&p)[Piece<T>::N / 2]) {
-    constexpr int N = Piece<T>::N;
-    if (VEC && c + N <= cols) {
-        st_stream_u4(row + c, Piece<T>::join(p));
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (c + j < cols) row[c + j] = from_f32<T>(j & 1 ? pair_hi(p[j / 2]) : pair_lo(p[j / 2]));
-    }
-}
-// the weight's pieces, which a thread keeps for all its rows
-template <typename T, bool VEC>
-__device__ __forceinline__ uint4 load_weight(const T* w, int c, int cols) {
-    if (VEC && c + Piece<T>::N <= cols) return __ldg(reinterpret_cast<const uint4*>(w + c));
-    return load_piece<T, false>(w, c, cols);
-}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -67,13 +39,12 @@ __device__ __forceinline__ float row_sum(float v, float* sm, int turn) {
     return v;
 }
 
-template <int TPR> constexpr int kBlockOf = TPR < 256 ? 256 : TPR;   // threads of a CTA
-// Persistent CTAs on an SM: as many as their registers allow when the next row waits in registers too.
-template <int TPR, int EPT> constexpr int kForwardCtas = TPR == 1024 ? 1 : (EPT == 32 ? 2 : 4);
-template <int TPR, int EPT> constexpr int kBackwardCtas = TPR == 1024 ? 1 : (EPT == 32 ? 1 : (EPT == 16 ? 2 : 4));
-
-// Whether the next row is fetched early and the weight stays in registers: CTAs of 1024 threads have no registers for that.
-template <int TPR> constexpr bool kAhead = TPR < 1024;
+template <int TPR> constexpr int kBlockOf = TPR < 128 ? 256 : TPR;   // threads of a CTA
+// Persistent CTAs on an SM: as many as the registers of a row's entries allow (64 or 128 a thread), with the next row waiting in
+// registers too.  CTAs of 1024 threads with more than 8 entries each have no registers for that.
+template <int TPR, int EPT> constexpr int kForwardCtas = 1024 / kBlockOf<TPR>;
+template <int TPR, int EPT> constexpr int kBackwardCtas = TPR == 1024 ? 1 : (EPT == 8 ? 1024 : 512) / kBlockOf<TPR>;
+template <int TPR, int EPT> constexpr bool kAhead = TPR < 1024 || EPT == 8;
 
 struct NormOut {
     void* S; int64_t lds;
@@ -81,13 +52,19 @@ struct NormOut {
     uint8_t* Q; int64_t ldq;
     uint8_t* E; int64_t lde;
     float* rstd;
+    bool s_vec, y_vec, q_vec;   // 16-byte (8-bit form: 8-byte) stores
+};
+struct NormIn {
+    const void* X; int64_t ldx;
+    const void* R; int64_t ldr;
+    const void* w;
+    Span x, r, weight;
 };
 
 // X, R and S may be the same buffer: a row is in registers before any of it is written.
-template <typename T, int TPR, int EPT, bool VEC>
+template <typename T, int TPR, int EPT, bool ANY>
 __global__ void __launch_bounds__(kBlockOf<TPR>, (kForwardCtas<TPR, EPT>))
-rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __restrict__ w, int64_t rows, int cols, float eps,
-               NormOut o) {
+rmsnorm_kernel(const __grid_constant__ NormIn in, int64_t rows, int cols, float eps, const __grid_constant__ NormOut o) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
     pdl_trigger();
@@ -95,25 +72,26 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
     const int t = threadIdx.x % TPR;
     const int64_t stride = (int64_t)gridDim.x * RPB;
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (row >= rows) return;                   // (TPR = 32: whole warps; else never: a CTA has at least one row)
+    if (row >= rows) return;                   // (TPR = 32: whole warps; else never: a CTA has a row)
     uint4 weight[P], x[P], r[P];
-    const T *from_x = X + row * ldx, *from_r = R ? R + row * ldr : nullptr;
+    const T *w = static_cast<const T*>(in.w), *from_x = static_cast<const T*>(in.X) + row * in.ldx;
+    const T* from_r = in.R ? static_cast<const T*>(in.R) + row * in.ldr : nullptr;
     auto fetch = [&] {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int c = (t + i * TPR) * N;
-            x[i] = load_piece<T, VEC>(from_x, c, cols);
-            if (from_r) r[i] = load_piece<T, VEC>(from_r, c, cols);
+            x[i] = load_piece<ANY>(from_x, c, cols, in.x);
+            if (from_r) r[i] = load_piece<ANY>(from_r, c, cols, in.r);
         }
-        from_x += stride * ldx;
-        if (from_r) from_r += stride * ldr;
+        from_x += stride * in.ldx;
+        if (from_r) from_r += stride * in.ldr;
     };
 #pragma unroll
     for (int i = 0; i < P; ++i)
-        if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
-    if (kAhead<TPR>) fetch();
+        if ((kAhead<TPR, EPT>)) weight[i] = load_piece<ANY>(w, (t + i * TPR) * N, cols, in.weight);
+    if ((kAhead<TPR, EPT>)) fetch();
     for (int turn = 0;; ++turn) {
-        if (!kAhead<TPR>) fetch();
+        if (!(kAhead<TPR, EPT>)) fetch();
         uint64_t v[P][N / 2];
         uint64_t sum2 = 0ull;
 #pragma unroll
@@ -129,7 +107,7 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
             for (int j = 0; j < N / 2; ++j) sum2 = fma2(v[i][j], v[i][j], sum2);
         }
         const int64_t next = row + stride;
-        if (kAhead<TPR> && next < rows) fetch();
+        if ((kAhead<TPR, EPT>) && next < rows) fetch();
         const float sum = row_sum<TPR>(pair_lo(sum2) + pair_hi(sum2), sm, turn);
         const float rstd = rsqrtf(sum / (float)cols + eps);
         const uint64_t rstd2 = pair_of(rstd, rstd);
@@ -137,7 +115,7 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
         if (o.S) {
             T* s = static_cast<T*>(o.S) + row * o.lds;
 #pragma unroll
-            for (int i = 0; i < P; ++i) store_piece<T, VEC>(s, (t + i * TPR) * N, cols, v[i]);
+            for (int i = 0; i < P; ++i) store_piece(s, (t + i * TPR) * N, cols, !ANY || o.s_vec, v[i]);
         }
         if (o.Y || o.Q) {
 #pragma unroll
@@ -145,16 +123,16 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
                 // (beyond the row's end: zeros, or NaN from 0 * Inf, which a block's largest entry passes over)
                 const int c = (t + i * TPR) * N;
                 uint64_t f[N / 2];
-                Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, c, cols), f);
+                Piece<T>::split((kAhead<TPR, EPT>) ? weight[i] : load_piece<ANY>(w, c, cols, in.weight), f);
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) v[i][j] = mul2(mul2(v[i][j], rstd2), f[j]);
-                if (o.Y) store_piece<T, VEC>(static_cast<T*>(o.Y) + row * o.ldy, c, cols, v[i]);
+                if (o.Y) store_piece(static_cast<T*>(o.Y) + row * o.ldy, c, cols, !ANY || o.y_vec, v[i]);
                 if (o.Q) {
                     constexpr int kLanes = kKeepBlock / N;   // 16, or 32 in fp32: the lanes of a block lie side by side
                     uint32_t q[N / 4];
                     const uint32_t e = keep_pairs<N / 2, kLanes>(v[i], q);
                     uint8_t* to = o.Q + row * o.ldq + c;
-                    if (VEC && c + N <= cols) {
+                    if ((!ANY || o.q_vec) && c + N <= cols) {
                         if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(q[0], q[1]));
                         else __stcs(reinterpret_cast<unsigned int*>(to), q[0]);
                     } else {
@@ -171,10 +149,14 @@ rmsnorm_kernel(const T* X, int64_t ldx, const T* R, int64_t ldr, const T* __rest
     }
 }
 
-template <typename T, int TPR, int EPT, bool VEC>
+struct BackwardSpans {
+    Span dy, ds, s, weight;
+};
+
+template <typename T, int TPR, int EPT, bool ANY>
 __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsnorm_backward_kernel(
     const T* dY, int64_t lddy, const T* dS, int64_t ldds, const T* __restrict__ S, int64_t lds, const T* __restrict__ w,
-    const float* __restrict__ rstd_of, int64_t rows, int cols, T* dX, int64_t lddx, float* __restrict__ parts,
+    const float* __restrict__ rstd_of, const __grid_constant__ BackwardSpans in, int64_t rows, int cols, T* dX, int64_t lddx, bool dx_vec, float* __restrict__ parts,
     int64_t ldp) {
     constexpr int N = Piece<T>::N, P = EPT / N, RPB = kBlockOf<TPR> / TPR;
     __shared__ float sm[TPR > 32 ? 2 * (TPR / 32) : 1];
@@ -190,13 +172,13 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
     const T *from_dy = dY + row * lddy, *from_s = S + row * lds, *from_ds = dS ? dS + row * ldds : nullptr;
     const float* from_rstd = rstd_of + row;
     auto fetch = [&] {
-        rstd = *from_rstd;
+        rstd = load_here(from_rstd);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int c = (t + i * TPR) * N;
-            dy[i] = load_piece<T, VEC>(from_dy, c, cols);
-            s[i] = load_piece<T, VEC>(from_s, c, cols);
-            if (from_ds) ds[i] = load_piece<T, VEC>(from_ds, c, cols);
+            dy[i] = load_piece<ANY>(from_dy, c, cols, in.dy);
+            s[i] = load_piece<ANY>(from_s, c, cols, in.s);
+            if (from_ds) ds[i] = load_piece<ANY>(from_ds, c, cols, in.ds);
         }
         from_rstd += stride;
         from_dy += stride * lddy;
@@ -205,14 +187,14 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
     };
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        if (kAhead<TPR>) weight[i] = load_weight<T, VEC>(w, (t + i * TPR) * N, cols);
+        if ((kAhead<TPR, EPT>)) weight[i] = load_piece<ANY>(w, (t + i * TPR) * N, cols, in.weight);
         ds[i] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) acc[i][j] = 0ull;
     }
-    if (kAhead<TPR> && row < rows) fetch();
+    if ((kAhead<TPR, EPT>) && row < rows) fetch();
     for (int turn = 0; row < rows; ++turn) {
-        if (!kAhead<TPR>) fetch();
+        if (!(kAhead<TPR, EPT>)) fetch();
         uint64_t dyw[P][N / 2], hat[P][N / 2];
         const uint64_t scale2 = pair_of(rstd, rstd);
         uint4 extra[P];
@@ -221,7 +203,7 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
         for (int i = 0; i < P; ++i) {
             extra[i] = ds[i];
             uint64_t f[N / 2];
-            Piece<T>::split(kAhead<TPR> ? weight[i] : load_weight<T, VEC>(w, (t + i * TPR) * N, cols), f);
+            Piece<T>::split((kAhead<TPR, EPT>) ? weight[i] : load_piece<ANY>(w, (t + i * TPR) * N, cols, in.weight), f);
             Piece<T>::split(dy[i], dyw[i]);
             Piece<T>::split(s[i], hat[i]);
 #pragma unroll
@@ -233,7 +215,7 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
             }
         }
         const int64_t next = row + stride;
-        if (kAhead<TPR> && next < rows) fetch();
+        if ((kAhead<TPR, EPT>) && next < rows) fetch();
         if (dX) {
             const float dot = row_sum<TPR>(pair_lo(dot2) + pair_hi(dot2), sm, turn) * -inv_cols;
             const uint64_t ndot2 = pair_of(dot, dot);
@@ -243,7 +225,7 @@ __global__ void __launch_bounds__(kBlockOf<TPR>, (kBackwardCtas<TPR, EPT>)) rmsn
                 Piece<T>::split(extra[i], out);
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) out[j] = fma2(scale2, fma2(hat[i][j], ndot2, dyw[i][j]), out[j]);
-                store_piece<T, VEC>(dX + row * lddx, (t + i * TPR) * N, cols, out);
+                store_piece(dX + row * lddx, (t + i * TPR) * N, cols, !ANY || dx_vec, out);
             }
         }
         row = next;
@@ -308,29 +290,30 @@ __global__ void __launch_bounds__(kDwThreads) rmsnorm_dw_kernel(const float* __r
 static_assert(kDwThreads / 32 == kDwCols, "a warp for each column");
 int64_t parts_pitch(int64_t cols) { return (cols + kDwCols - 1) / kDwCols * kDwCols; }
 
-struct Backward {
-    const void* dY; int64_t lddy;
-    const void* dS; int64_t ldds;
-    const void* S; int64_t lds;
-    const void* w;
-    const float* rstd;
-    int64_t rows, cols;
-    void* dX; int64_t lddx;
-    float* parts;
-};
-
-// calls f<TPR, EPT>() with the smallest pair that holds a row
-template <typename F>
+// Calls f<TPR, EPT>() with the threads and entries for rows of this width: up to 512 columns (fp32: 256) a warp, without
+// barriers; then 8 entries a thread where that is enough, since registers are what limits the rows in flight.
+template <typename T, typename F>
 detox_status by_width(int64_t cols, F f) {
     if (cols <= 32 * 8) return f.template operator()<32, 8>();
-    if (cols <= 32 * 16) return f.template operator()<32, 16>();
-    if (cols <= 32 * 32) return f.template operator()<32, 32>();
+    if (sizeof(T) == 2 && cols <= 32 * 16) return f.template operator()<32, 16>();
+    if (cols <= 128 * 8) return f.template operator()<128, 8>();
     if (cols <= 256 * 8) return f.template operator()<256, 8>();
-    if (cols <= 256 * 16) return f.template operator()<256, 16>();
-    if (cols <= 256 * 32) return f.template operator()<256, 32>();
+    if constexpr (sizeof(T) == 2) {
+        if (cols <= 256 * 16) return f.template operator()<256, 16>();
+        if (cols <= 512 * 16) return f.template operator()<512, 16>();
+    } else {
+        if (cols <= 512 * 8) return f.template operator()<512, 8>();
+        if (cols <= 1024 * 8) return f.template operator()<1024, 8>();
+    }
     if (cols <= 1024 * 16) return f.template operator()<1024, 16>();
     return f.template operator()<1024, 32>();
 }
+// 16-byte pieces can be stored: base and stride
+template <typename T>
+bool pieces(const void* p, int64_t ld) {
+    return aligned16(p) && ld % Piece<T>::N == 0;
+}
+
 // CTAs of the backward pass, each leaving one row of partial sums of dw
 struct CountParts {
     int64_t rows;
@@ -342,17 +325,16 @@ struct CountParts {
         return DETOX_OK;
     }
 };
+template <typename T>
 int parts_of(int64_t rows, int64_t cols) {
     int n = 0;
-    by_width(cols, CountParts{rows, &n});
+    by_width<T>(cols, CountParts{rows, &n});
     return n;
 }
 
-template <typename T, bool VEC>
-struct Fwd {
-    const void* X; int64_t ldx;
-    const void* R; int64_t ldr;
-    const void* w;
+template <typename T, bool ANY>
+struct Forward {
+    NormIn in;
     int64_t rows, cols;
     float eps;
     NormOut o;
@@ -361,47 +343,58 @@ struct Fwd {
     detox_status operator()() const {
         constexpr int RPB = kBlockOf<TPR> / TPR;
         const int64_t need = ceil_div(rows, (int64_t)RPB), most = (int64_t)kSMs * kForwardCtas<TPR, EPT>;
-        return launch_chained(rmsnorm_kernel<T, TPR, EPT, VEC>, (unsigned)(need < most ? need : most), kBlockOf<TPR>, 0, 1, s,
-                              static_cast<const T*>(X), ldx, static_cast<const T*>(R), ldr, static_cast<const T*>(w), rows,
+        return launch_chained(rmsnorm_kernel<T, TPR, EPT, ANY>, (unsigned)(need < most ? need : most), kBlockOf<TPR>, 0, 1, s, in, rows,
                               (int)cols, eps, o);
     }
 };
 
-template <typename T, bool VEC>
-struct Bwd {
-    Backward b;
+struct BackwardIn {
+    const void* dY; int64_t lddy;
+    const void* dS; int64_t ldds;
+    const void* S; int64_t lds;
+    const void* w;
+    const float* rstd;
+    BackwardSpans span;
+};
+template <typename T, bool ANY>
+struct Backward {
+    BackwardIn in;
+    int64_t rows, cols;
+    void* dX; int64_t lddx;
+    float* parts;
     int nparts;
     cudaStream_t s;
     template <int TPR, int EPT>
     detox_status operator()() const {
-        return launch_chained(rmsnorm_backward_kernel<T, TPR, EPT, VEC>, (unsigned)nparts, kBlockOf<TPR>, 0, 1, s,
-                              static_cast<const T*>(b.dY), b.lddy, static_cast<const T*>(b.dS), b.ldds, static_cast<const T*>(b.S),
-                              b.lds, static_cast<const T*>(b.w), b.rstd, b.rows, (int)b.cols, static_cast<T*>(b.dX), b.lddx, b.parts,
-                              parts_pitch(b.cols));
+        return launch_chained(rmsnorm_backward_kernel<T, TPR, EPT, ANY>, (unsigned)nparts, kBlockOf<TPR>, 0, 1, s,
+                              static_cast<const T*>(in.dY), in.lddy, static_cast<const T*>(in.dS), in.ldds, static_cast<const T*>(in.S),
+                              in.lds, static_cast<const T*>(in.w), in.rstd, in.span, rows, (int)cols, static_cast<T*>(dX), lddx, pieces<T>(dX, lddx), parts, parts_pitch(cols));
     }
 };
 
-// 16-byte pieces can be used: base and stride of every matrix that is there
 template <typename T>
-bool pieces(const void* p, int64_t ld) {
-    return p == nullptr || (aligned16(p) && ld % Piece<T>::N == 0);
+detox_status forward(NormIn in, int64_t rows, int64_t cols, float eps, NormOut o, cudaStream_t s) {
+    in.x = span_of<T>(in.X, in.ldx, rows, cols);
+    in.r = span_of<T>(in.R, in.ldr, rows, cols);
+    in.weight = span_of<T>(in.w, 0, 1, cols);
+    o.s_vec = pieces<T>(o.S, o.lds);
+    o.y_vec = pieces<T>(o.Y, o.ldy);
+    o.q_vec = aligned_to(o.Q, 8) && o.ldq % 8 == 0;
+    if (cols % Piece<T>::N == 0 && in.x.vec && (!in.R || in.r.vec) && in.weight.vec && (!o.S || o.s_vec) && (!o.Y || o.y_vec) && (!o.Q || o.q_vec))
+        return by_width<T>(cols, Forward<T, false>{in, rows, cols, eps, o, s});
+    return by_width<T>(cols, Forward<T, true>{in, rows, cols, eps, o, s});
 }
 
 template <typename T>
-detox_status forward(const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w, int64_t rows, int64_t cols,
-                     float eps, const NormOut& o, cudaStream_t s) {
-    const bool vec = pieces<T>(X, ldx) && pieces<T>(R, ldr) && aligned16(w) && pieces<T>(o.S, o.lds) && pieces<T>(o.Y, o.ldy) &&
-                     (o.Q == nullptr || (aligned16(o.Q) && o.ldq % 8 == 0));
-    if (vec) return by_width(cols, Fwd<T, true>{X, ldx, R, ldr, w, rows, cols, eps, o, s});
-    return by_width(cols, Fwd<T, false>{X, ldx, R, ldr, w, rows, cols, eps, o, s});
-}
-
-template <typename T>
-detox_status backward(const Backward& b, int nparts, cudaStream_t s) {
-    const bool vec = pieces<T>(b.dY, b.lddy) && pieces<T>(b.dS, b.ldds) && pieces<T>(b.S, b.lds) && aligned16(b.w) &&
-                     pieces<T>(b.dX, b.lddx);
-    if (vec) return by_width(b.cols, Bwd<T, true>{b, nparts, s});
-    return by_width(b.cols, Bwd<T, false>{b, nparts, s});
+detox_status backward(BackwardIn in, int64_t rows, int64_t cols, void* dX, int64_t lddx, float* parts, cudaStream_t s) {
+    const int nparts = parts_of<T>(rows, cols);
+    in.span.dy = span_of<T>(in.dY, in.lddy, rows, cols);
+    in.span.ds = span_of<T>(in.dS, in.ldds, rows, cols);
+    in.span.s = span_of<T>(in.S, in.lds, rows, cols);
+    in.span.weight = span_of<T>(in.w, 0, 1, cols);
+    if (cols % Piece<T>::N == 0 && in.span.dy.vec && (!in.dS || in.span.ds.vec) && in.span.s.vec && in.span.weight.vec && (!dX || pieces<T>(dX, lddx)))
+        return by_width<T>(cols, Backward<T, false>{in, rows, cols, dX, lddx, parts, nparts, s});
+    return by_width<T>(cols, Backward<T, true>{in, rows, cols, dX, lddx, parts, nparts, s});
 }
 
 }  // namespace
@@ -410,14 +403,17 @@ detox_status launch_rmsnorm(int dtype, const void* X, int64_t ldx, const void* R
                             int64_t rows, int64_t cols, float eps, void* S, int64_t lds, void* Y, int64_t ldy,
                             uint8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, float* rstd, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
-    const NormOut o{S, lds, Y, ldy, Q, ldq, E, lde, rstd};
-    if (dtype == DETOX_DTYPE_FLOAT) return forward<float>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
-    if (dtype == DETOX_DTYPE_HALF) return forward<__half>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
-    return forward<__nv_bfloat16>(X, ldx, R, ldr, w, rows, cols, eps, o, s);
+    const NormIn in{X, ldx, R, ldr, w, {}, {}, {}};
+    const NormOut o{S, lds, Y, ldy, Q, ldq, E, lde, rstd, false, false, false};
+    if (dtype == DETOX_DTYPE_FLOAT) return forward<float>(in, rows, cols, eps, o, s);
+    if (dtype == DETOX_DTYPE_HALF) return forward<__half>(in, rows, cols, eps, o, s);
+    return forward<__nv_bfloat16>(in, rows, cols, eps, o, s);
 }
 
 size_t rmsnorm_backward_ws_bytes(int64_t rows, int64_t cols) {
-    return align_up((size_t)(rows > 0 ? parts_of(rows, cols) : 1) * (size_t)parts_pitch(cols) * sizeof(float));
+    int n = 1;   // (whatever the type)
+    if (rows > 0) n = parts_of<float>(rows, cols) > parts_of<__half>(rows, cols) ? parts_of<float>(rows, cols) : parts_of<__half>(rows, cols);
+    return align_up((size_t)n * (size_t)parts_pitch(cols) * sizeof(float));
 }
 
 detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, const void* dS, int64_t ldds, const void* S,
@@ -427,16 +423,15 @@ detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, co
         if (dw && cudaMemsetAsync(dw, 0, (size_t)cols * sizeof(float), s) != cudaSuccess) return DETOX_ERR_CUDA;
         return DETOX_OK;
     }
-    const int nparts = parts_of(rows, cols);
     float* parts = dw ? static_cast<float*>(ws) : nullptr;
-    const Backward b{dY, lddy, dS, ldds, S, lds, w, rstd, rows, cols, dX, lddx, parts};
+    const BackwardIn in{dY, lddy, dS, ldds, S, lds, w, rstd, {}};
     detox_status st;
-    if (dtype == DETOX_DTYPE_FLOAT) st = backward<float>(b, nparts, s);
-    else if (dtype == DETOX_DTYPE_HALF) st = backward<__half>(b, nparts, s);
-    else st = backward<__nv_bfloat16>(b, nparts, s);
+    if (dtype == DETOX_DTYPE_FLOAT) st = backward<float>(in, rows, cols, dX, lddx, parts, s);
+    else if (dtype == DETOX_DTYPE_HALF) st = backward<__half>(in, rows, cols, dX, lddx, parts, s);
+    else st = backward<__nv_bfloat16>(in, rows, cols, dX, lddx, parts, s);
     if (st != DETOX_OK || !dw) return st;
-    return launch_chained(rmsnorm_dw_kernel, (unsigned)ceil_div(cols, (int64_t)kDwCols), kDwThreads, 0, 1, s, parts, nparts,
-                          parts_pitch(cols), (int)cols, dw);
+    return launch_chained(rmsnorm_dw_kernel, (unsigned)ceil_div(cols, (int64_t)kDwCols), kDwThreads, 0, 1, s, parts,
+                          dtype == DETOX_DTYPE_FLOAT ? parts_of<float>(rows, cols) : parts_of<__half>(rows, cols), parts_pitch(cols), (int)cols, dw);
 }
 
 }  // namespace detox

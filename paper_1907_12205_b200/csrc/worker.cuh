@@ -100,6 +100,90 @@ struct Piece {
     }
 };
 
+// ---- rows of any alignment ----------------------------------------------------------------------
+// A matrix as the kernels that take any alignment read it: `vec` says that its rows are 16-byte aligned; otherwise `lo` and
+// `hi` bound its bytes.
+struct Span {
+    uintptr_t lo, hi;
+    bool vec;
+};
+template <typename T>
+Span span_of(const void* p, int64_t ld, int64_t rows, int64_t cols) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return Span{at, at + ((uintptr_t)(rows - 1) * (uintptr_t)ld + (uintptr_t)cols) * sizeof(T), aligned16(p) && ld % Piece<T>::N == 0};
+}
+// entries [c, c + N) of a row as they lie in memory, bit for bit, zeros beyond `cols`
+template <typename T, typename I>
+__device__ __forceinline__ uint4 gather_piece(const T* row, I c, I cols) {
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(row);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = c + i < cols ? x[c + i] : 0u;
+    } else {
+        const uint16_t* x = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = (c + 2 * i < cols ? (uint32_t)x[c + 2 * i] : 0u) | (c + 2 * i + 1 < cols ? (uint32_t)x[c + 2 * i + 1] << 16 : 0u);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 16 bytes, or zeros.  Volatile: the load is issued where it is written.  The compiler otherwise moves the loads of the next row
+// behind the reduction of the present one, which they are there to overlap (norm's backward pass 28.4 instead of 25.7 us).
+__device__ __forceinline__ uint4 load_here(const void* from, bool want) {
+    uint4 v;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+        "@p ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+        : "l"(from), "r"((uint32_t)want)
+        : "memory");
+    return v;
+}
+__device__ __forceinline__ float load_here(const float* from) {
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(from) : "memory");
+    return v;
+}
+// The same.  ANY = false: the rows are 16-byte aligned and whole pieces long.  ANY = true: see span; where they are not aligned a piece is two aligned loads,
+// shifted together (a norm of 4928 x 1087 bf16 with such rows: 27 us with a load for each entry), and only at the ends of
+// the matrix, where those would reach outside it, a load for each entry.
+template <bool ANY, typename T, typename I>
+__device__ __forceinline__ uint4 load_piece(const T* row, I c, I cols, const Span& span) {
+    if constexpr (!ANY) return load_here(row + c, c < cols);
+    if (c + Piece<T>::N > cols) return gather_piece(row, c, cols);
+    if (span.vec) return ld_stream_u4(row + c);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), a = at & ~(uintptr_t)15;
+    if (a < span.lo || a + 32 > span.hi) return gather_piece(row, c, cols);
+    const uint4 x = *reinterpret_cast<const uint4*>(a), y = *reinterpret_cast<const uint4*>(a + 16);
+    uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    const uint32_t by = (uint32_t)(at & 15);
+    if (by & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (by & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (by & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
+}
+// ... and stored
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, int c, int cols, bool vec, const uint64_t (&p)[Piece<T>::N / 2]) {
+    constexpr int N = Piece<T>::N;
+    if (vec && c + N <= cols) {
+        st_stream_u4(row + c, Piece<T>::join(p));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c + j < cols) row[c + j] = from_f32<T>(j & 1 ? pair_hi(p[j / 2]) : pair_lo(p[j / 2]));
+    }
+}
+
 // ---- the 8-bit form ---------------------------------------------------------------------------
 // Biased exponent (e + 127) of the scale: the smallest e with amax <= 448 * 2^e = 1.75 * 2^(e+8), at least -126.
 // Adding 0x1fffff carries into the exponent exactly when the mantissa is above 1.75.

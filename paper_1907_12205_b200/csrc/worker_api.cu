@@ -7,7 +7,7 @@ using namespace detox;
 namespace {
 
 constexpr int64_t kMaxDim = (int64_t)1 << 30;      // TMA coordinates and tile counts are 32-bit
-constexpr int64_t kMaxNormCols = 32768;            // a CTA of 1024 threads holds a row, 32 entries each
+constexpr int64_t kMaxNormCols = DETOX_NORM_MAX_COLS;   // a CTA of 1024 threads holds a row, 32 entries each
 
 int dtype_size(int dtype) {
     return dtype == DETOX_DTYPE_FLOAT ? 4 : ((dtype == DETOX_DTYPE_HALF || dtype == DETOX_DTYPE_BFLOAT) ? 2 : 0);
