@@ -11,9 +11,10 @@
 // lie the other way round and are read as MN-major tiles: nothing is transposed in memory.
 //
 // A CTA: one warp issues the TMA copies of 64-wide slices of both operands into a ring of stages, one thread issues
-// the MMAs, eight warps drain the accumulator (two to each quarter of its rows).  Two accumulators share the tensor memory, so a tile is drained while the
-// next one is multiplied.  Ragged edges: TMA fills with zeros outside a matrix and the epilogue masks its stores.
-// Three shapes of the work (gemm_shape chooses):
+// the MMAs, eight warps drain the accumulator (two to each quarter of its rows).  Two accumulators share the tensor memory, so
+// a tile is drained while the next one is multiplied.  Ragged edges: TMA fills with zeros outside a matrix and the epilogue
+// masks its stores.
+// Three shapes of the work (shape_of and shapes_beside choose):
 //   pair     two CTAs of a cluster multiply one 256 x 256 tile (cta_group::2): each holds 128 rows of either operand, so
 //            a byte of shared memory feeds twice the MMA work that a CTA on its own gets out of it; persistent grid
 //   single   one CTA, 128 x 256 or 128 x 128; persistent grid
@@ -203,7 +204,7 @@ template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
     if constexpr (ACT == DETOX_ACT_SILU) return __fdividef(g, 1.f + __expf(-g));
     if constexpr (ACT == DETOX_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
-    return fmaxf(g, 0.f);
+    return g < 0.f ? 0.f : g;   // (NaN stays NaN)
 }
 template <int ACT>
 __device__ __forceinline__ void act_both(float g, float& a, float& da) {
@@ -216,7 +217,7 @@ __device__ __forceinline__ void act_both(float g, float& a, float& da) {
         a = g * c;
         da = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), c);
     } else {
-        a = fmaxf(g, 0.f);
+        a = act_of<ACT>(g);
         da = g > 0.f ? 1.f : 0.f;
     }
 }

@@ -627,3 +627,84 @@ def test_offsets_that_pass_32_bits():
     got = dx.detox_rmsnorm(x, w, want_y=True)
     few = dx.detox_rmsnorm(x[-5:].contiguous(), w)
     assert torch.equal(got.y[-5:], few.y) and torch.equal(got.rstd[-5:], few.rstd)
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("tokens", [3, 300])
+def test_nan_reaches_its_own_outputs(act, tokens):
+    """A NaN in a token makes that token's h, dx and all weight gradients NaN, whatever the activation; a NaN in dh does so for its
+    row of the weight gradients and its token's dx."""
+    gen = generator(51)
+    x, wg, wu, dh = (randn(gen, *s).to(BF16).to(DEV) for s in ((tokens, 96), (140, 96), (140, 96), (tokens, 140)))
+    bad = x.clone()
+    bad[1, 7] = math.nan
+    h, kept = dx.detox_gated(bad, wg, wu, ACTS[act], keep=True)
+    assert bool(h[1].isnan().all()) and not bool(h[0].isnan().any())
+    for k in (None, kept):
+        gx, a, b = dx.detox_gated_backward(dh, bad, wg, wu, ACTS[act], kept=k)
+        assert bool(gx[1].isnan().all()) and not bool(gx[0].isnan().any()) and bool(b.isnan().all())
+    hurt = dh.clone()
+    hurt[1, 5] = math.nan
+    gx, a, b = dx.detox_gated_backward(hurt, x, wg, wu, ACTS[act])
+    assert bool(gx[1].isnan().all()) and not bool(gx[0].isnan().any())
+    assert bool(b[5].isnan().all()) and not bool(b[4].isnan().any()) and not bool(b[6].isnan().any())
+
+
+@pytest.mark.parametrize("tokens,in_dim,hidden", [(1, 64, 128), (70, 97, 131), (520, 512, 300), (2100, 64, 1300)])
+def test_workspaces_are_as_large_as_they_say(tokens, in_dim, hidden):
+    """With exactly the bytes the helpers ask for, between guard bands that nothing may touch."""
+    gen = generator(52)
+    x, wg, wu, dh = (randn(gen, *s).to(F16).to(DEV) for s in ((tokens, in_dim), (hidden, in_dim), (hidden, in_dim), (tokens, hidden)))
+
+    def guarded(n):
+        buf = torch.full((n + 8192,), 0xA5, dtype=torch.uint8, device=DEV)
+        return buf, buf[4096: 4096 + n]
+
+    def intact(buf, n):
+        return bool((buf[:4096] == 0xA5).all()) and bool((buf[4096 + n:] == 0xA5).all())
+
+    pair = dx.detox_checkpoint_pack(x)
+    for xin in (x, pair):
+        n = dx.detox_gated_workspace_bytes(xin, wg, wu)
+        buf, ws = guarded(n)
+        h, kept = dx.detox_gated(xin, wg, wu, keep=True, ws=ws)
+        assert intact(buf, n)
+        for k in (None, kept):
+            n = dx.detox_gated_backward_workspace_bytes(xin, wg, wu, kept=k)
+            buf, ws = guarded(n)
+            dx.detox_gated_backward(dh, xin, wg, wu, kept=k, ws=ws)
+            assert intact(buf, n)
+    for dtype in (F16, F32):
+        n = dx.detox_rmsnorm_backward_workspace_bytes(tokens, in_dim)
+        buf, ws = guarded(n)
+        dx.detox_rmsnorm_backward(x.to(dtype), x.to(dtype), wg[0].to(dtype).contiguous(), torch.ones(tokens, device=DEV), ws=ws)
+        assert intact(buf, n)
+    with pytest.raises(dx.DetoxError) as e:
+        dx.detox_gated(x, wg, wu, ws=torch.empty(0, dtype=torch.uint8, device=DEV))
+    assert e.value.code == 3
+
+
+def test_refusals_of_the_binding():
+    x, w = torch.zeros((8, 64), dtype=BF16, device=DEV), torch.zeros((32, 64), dtype=BF16, device=DEV)
+    dh = torch.zeros((8, 32), dtype=BF16, device=DEV)
+    for wrong in (lambda: dx.detox_gated(x.float(), w, w), lambda: dx.detox_gated(x, w, w.half()), lambda: dx.detox_gated(x[0], w, w),
+                  lambda: dx.detox_rmsnorm(x, w), lambda: dx.detox_rmsnorm(x.int(), w[0]), lambda: dx.detox_checkpoint_pack(x.double()),
+                  lambda: dx.detox_checkpoint_unpack(x, x), lambda: dx.detox_gated_backward(dh, x, w, w, dw_dtype=torch.int32),
+                  lambda: dx.detox_rmsnorm_backward(x, x, w[0], torch.zeros(7, device=DEV)), lambda: dx.detox_gated(None, w, w)):
+        with pytest.raises(TypeError):
+            wrong()
+    for wrong in (lambda: dx.detox_gated(x[:, :32], w, w), lambda: dx.detox_gated(x.T, x.T, x.T), lambda: dx.detox_gated(x, w, w[:8]),
+                  lambda: dx.detox_gated_backward(dh[:4], x, w, w), lambda: dx.detox_gated_backward(dh, x, w, w, dwg=torch.zeros_like(w)),
+                  lambda: dx.detox_rmsnorm(x, w[0].contiguous(), residual=x[:4]), lambda: dx.detox_rmsnorm(x, w[0].contiguous(), sum_out=x)):
+        with pytest.raises(ValueError):
+            wrong()
+    with pytest.raises(dx.DetoxError) as e:
+        dx.detox_gated(x.float(), w.float(), w.float())
+    assert e.value.code == 2                       # the tensor cores multiply 16-bit entries
+    with pytest.raises(dx.DetoxError) as e:
+        dx.detox_gated(x, w, w, act=9)
+    assert e.value.code == 1
+    with pytest.raises(dx.DetoxError) as e:
+        wide = torch.zeros((2, 40000), dtype=BF16, device=DEV)
+        dx.detox_rmsnorm(wide, wide[0].contiguous())
+    assert e.value.code == 2
