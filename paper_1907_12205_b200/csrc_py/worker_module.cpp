@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -98,22 +99,26 @@ void* vector_of(const at::Tensor& t, const char* what, at::ScalarType type, int6
     return t.data_ptr();
 }
 
+// A new tensor on `like`'s device, without a way through the dispatcher for each.
+at::Tensor new_tensor(at::IntArrayRef sizes, at::IntArrayRef strides, at::ScalarType type, const at::Tensor& like) {
+    return at::detail::empty_strided_cuda(sizes, strides, type, like.device());
+}
+
 // A new matrix; rows a multiple of 16 bytes apart, so that the kernels can use 16-byte accesses.
 Rows new_rows(int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor& like) {
     const int64_t n = 16 / (int64_t)c10::elementSize(type), ld = (cols + n - 1) / n * n;
-    const auto options = like.options().dtype(type);
-    at::Tensor t = ld == cols ? at::empty({rows, cols}, options) : at::empty_strided({rows, cols}, {ld, 1}, options);
+    at::Tensor t = new_tensor({rows, cols}, {ld, 1}, type, like);
     void* p = t.data_ptr();
     return Rows{std::move(t), p, ld, rows, cols};
 }
-at::Tensor new_vector(int64_t n, at::ScalarType type, const at::Tensor& like) { return at::empty({n}, like.options().dtype(type)); }
+at::Tensor new_vector(int64_t n, at::ScalarType type, const at::Tensor& like) { return new_tensor({n}, {1}, type, like); }
 
 // Values and scales of the 8-bit form.
 struct Pair {
     Rows q, e;
 };
 Pair new_pair(int64_t rows, int64_t cols, const at::Tensor& like) {
-    at::Tensor e = at::empty({rows, blocks(cols)}, like.options().dtype(kScales));
+    at::Tensor e = new_tensor({rows, blocks(cols)}, {blocks(cols), 1}, kScales, like);
     void* p = e.data_ptr();
     return Pair{new_rows(rows, cols, kValues, like), Rows{std::move(e), p, blocks(cols), rows, blocks(cols)}};
 }
@@ -326,8 +331,8 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor q, e;
         if (PyObject_IsTrue(a[7])) {
             const int64_t ld = (d.hidden + 15) / 16 * 16, nb = blocks(d.hidden);
-            q = at::empty_strided({2, d.tokens, d.hidden}, {d.tokens * ld, ld, 1}, g.like.options().dtype(kValues));
-            e = at::empty({2, d.tokens, nb}, g.like.options().dtype(kScales));
+            q = new_tensor({2, d.tokens, d.hidden}, {d.tokens * ld, ld, 1}, kValues, g.like);
+            e = new_tensor({2, d.tokens, nb}, {d.tokens * nb, nb, 1}, kScales, g.like);
             d.GQ = static_cast<uint8_t*>(q.data_ptr());
             d.GE = static_cast<uint8_t*>(e.data_ptr());
             d.UQ = d.GQ + d.tokens * ld;
