@@ -39,6 +39,15 @@ __device__ __forceinline__ float row_sum(float v, float* sm, int turn) {
     return v;
 }
 
+// 1 / sqrt(x) to about half a unit: rsqrtf is off by up to two, which moved a whole row's 8-bit entries over their rounding
+// boundaries more often than the rest of the arithmetic; one Newton step, its residual 1 - x r^2 without a rounding that counts.
+__device__ __forceinline__ float inverse_root(float x) {
+    const float r = rsqrtf(x);
+    if (!(r > 0.f && r < 3.402823466e38f)) return r;
+    const float h = x * r, l = fmaf(x, r, -h);
+    return fmaf(0.5f * r, fmaf(-l, r, fmaf(-h, r, 1.f)), r);
+}
+
 template <int TPR> constexpr int kBlockOf = TPR < 128 ? 256 : TPR;   // threads of a CTA
 // Persistent CTAs on an SM: as many as the registers of a row's entries allow (64 or 128 a thread), with the next row waiting in
 // registers too.  CTAs of 1024 threads with more than 8 entries each have no registers for that.
@@ -109,7 +118,7 @@ rmsnorm_kernel(const __grid_constant__ NormIn in, int64_t rows, int cols, float 
         const int64_t next = row + stride;
         if ((kAhead<TPR, EPT>) && next < rows) fetch();
         const float sum = row_sum<TPR>(pair_lo(sum2) + pair_hi(sum2), sm, turn);
-        const float rstd = rsqrtf(sum / (float)cols + eps);
+        const float rstd = inverse_root(sum / (float)cols + eps);
         const uint64_t rstd2 = pair_of(rstd, rstd);
         if (o.rstd && t == 0) o.rstd[row] = rstd;
         if (o.S) {
