@@ -625,6 +625,12 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
+            // The last MMAs' arrivals have to land before this CTA goes away: they may come from the pair's other CTA, and the next
+            // kernel's barriers lie at the same place.
+            for (int i = 0; ok && i < kStages; ++i) {
+                ok = mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, status);
+                if (++s == kStages) { s = 0; ph ^= 1u; }
+            }
             if (*abort_flag) {
                 // give the copies still in flight a bounded time to land before the CTA goes away (a pair's are counted
                 // at the first CTA, whichever CTA they belong to)
@@ -648,7 +654,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             uint32_t ph = 0, aph = 0;
             bool ok = true;
             for (TileWalk t(p, unit, units); ok && t.more(); t.next()) {
-                if (!mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status)) break;
+                if (!mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
@@ -664,6 +670,11 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
                 if (ok) mma_commit_cg<CG>(&sm->accum_full[buf]);
+                if (++buf == 2) { buf = 0; aph ^= 1u; }
+            }
+            // ... and so do the last accumulators' arrivals, from both CTAs' epilogues
+            for (int i = 0; ok && i < 2; ++i) {
+                ok = mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status);
                 if (++buf == 2) { buf = 0; aph ^= 1u; }
             }
         }
