@@ -1038,7 +1038,7 @@ void weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Co
 }
 
 // Which shape a product takes: the least of an estimate, in units of 10 ns, that was fitted to measurements of every shape
-// on twenty problems from 1 to 8192 tokens (the shape it takes costs 2.5% more than the best one on average):
+// on twenty problems from 1 to 8192 tokens (the shape it takes costs 1.4% more than the best one on average):
 //   a slice of the reduction   pair 28, nearly the MMAs' own rate; 128 x 256 on one CTA 45, 128 x 128 27: a CTA takes in
 //                  about 64 bytes a clock, and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.
 //                  With one row of tiles every byte of the weights comes from HBM for a single use, and the shapes differ
