@@ -677,6 +677,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 ok = mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status);
                 if (++buf == 2) { buf = 0; aph ^= 1u; }
             }
+            // a wait ran out: the MMAs that were issued end within microseconds, and their arrivals must not reach the next kernel
+            if (!ok)
+                for (int i = 0; i < 1024; ++i) __nanosleep(1000);
         }
         __syncwarp();
     } else {
