@@ -201,37 +201,6 @@ __device__ __forceinline__ void tmem_load(uint32_t at_f, uint32_t at_g, float (&
         : "memory");
 }
 
-// A block of the 8-bit form, 128 columns of this thread's row, at once.
-__device__ __forceinline__ void tmem_load_block(uint32_t at, float (&f)[128]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
-        "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, "
-        "%42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, "
-        "%62, %63, %64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, %80, %81, "
-        "%82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, %98, %99, %100, "
-        "%101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, %115, %116, "
-        "%117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%128];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]),
-          "=f"(f[8]), "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15]),
-          "=f"(f[16]), "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]), "=f"(f[22]), "=f"(f[23]),
-          "=f"(f[24]), "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31]),
-          "=f"(f[32]), "=f"(f[33]), "=f"(f[34]), "=f"(f[35]), "=f"(f[36]), "=f"(f[37]), "=f"(f[38]), "=f"(f[39]),
-          "=f"(f[40]), "=f"(f[41]), "=f"(f[42]), "=f"(f[43]), "=f"(f[44]), "=f"(f[45]), "=f"(f[46]), "=f"(f[47]),
-          "=f"(f[48]), "=f"(f[49]), "=f"(f[50]), "=f"(f[51]), "=f"(f[52]), "=f"(f[53]), "=f"(f[54]), "=f"(f[55]),
-          "=f"(f[56]), "=f"(f[57]), "=f"(f[58]), "=f"(f[59]), "=f"(f[60]), "=f"(f[61]), "=f"(f[62]), "=f"(f[63]),
-          "=f"(f[64]), "=f"(f[65]), "=f"(f[66]), "=f"(f[67]), "=f"(f[68]), "=f"(f[69]), "=f"(f[70]), "=f"(f[71]),
-          "=f"(f[72]), "=f"(f[73]), "=f"(f[74]), "=f"(f[75]), "=f"(f[76]), "=f"(f[77]), "=f"(f[78]), "=f"(f[79]),
-          "=f"(f[80]), "=f"(f[81]), "=f"(f[82]), "=f"(f[83]), "=f"(f[84]), "=f"(f[85]), "=f"(f[86]), "=f"(f[87]),
-          "=f"(f[88]), "=f"(f[89]), "=f"(f[90]), "=f"(f[91]), "=f"(f[92]), "=f"(f[93]), "=f"(f[94]), "=f"(f[95]),
-          "=f"(f[96]), "=f"(f[97]), "=f"(f[98]), "=f"(f[99]), "=f"(f[100]), "=f"(f[101]), "=f"(f[102]), "=f"(f[103]),
-          "=f"(f[104]), "=f"(f[105]), "=f"(f[106]), "=f"(f[107]), "=f"(f[108]), "=f"(f[109]), "=f"(f[110]), "=f"(f[111]),
-          "=f"(f[112]), "=f"(f[113]), "=f"(f[114]), "=f"(f[115]), "=f"(f[116]), "=f"(f[117]), "=f"(f[118]), "=f"(f[119]),
-          "=f"(f[120]), "=f"(f[121]), "=f"(f[122]), "=f"(f[123]), "=f"(f[124]), "=f"(f[125]), "=f"(f[126]), "=f"(f[127])
-        : "r"(at)
-        : "memory");
-}
-
 // ---- activations: a = act(g), da = act'(g) -----------------------------------------------------
 template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
@@ -370,7 +339,7 @@ __device__ __forceinline__ void fetch_rows(uint8_t* buf, const T* in, int64_t ld
     }
     __syncwarp();
 }
-// kChunk entries as 16-byte pieces of a row
+// kChunk entries as 16-byte pieces of a row, and kChunk 8-bit ones
 template <typename OT>
 __device__ __forceinline__ void put_chunk(uint4* to, const float (&f)[kChunk]) {
     constexpr int N = Piece<OT>::N;
@@ -382,6 +351,17 @@ __device__ __forceinline__ void put_chunk(uint4* to, const float (&f)[kChunk]) {
         to[i] = Piece<OT>::join(p);
     }
 }
+__device__ __forceinline__ uint4 keep_chunk(bool odd, float inv, float (&f)[kChunk]) {
+    uint32_t q[4];
+    if (odd) {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) f[i] = inf_to_nan(f[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = keep4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
+    return make_uint4(q[0], q[1], q[2], q[3]);
+}
+
 // E consecutive entries of an output row (E = 2 or 4), as the lanes of a warp store a split's finished row
 template <typename OT, int E>
 __device__ __forceinline__ void store_few(OT* row, int64_t c, int64_t cols, bool vec, const float (&f)[E]) {
@@ -755,33 +735,35 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                 }
                 if (FORM == kForward && BN == 256 && p.gq) {
                     // half of the warps keep g, the others u: a thread finds the largest of its 128 entries, then converts them
-                    float f[kKeepBlock];
-                    tmem_load_block(at + half * kHalf, f);
+                    const uint32_t from = at + half * kHalf;
                     float amax = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < kHalf; c += kChunk) {
+                        float f[kChunk];
+                        tmem_load(from + c, f);
 #pragma unroll
-                    for (int i = 0; i < kKeepBlock; ++i) amax = fmaxf(amax, fabsf(f[i]));
-                    if (is_inf(amax)) {   // see keep_pairs
+                        for (int i = 0; i < kChunk; ++i) amax = fmaxf(amax, fabsf(f[i]));
+                    }
+                    const bool odd = __any_sync(0xffffffffu, is_inf(amax));   // an Inf somewhere: see keep_pairs
+                    if (odd) {
                         amax = 0.f;
-#pragma unroll
-                        for (int i = 0; i < kKeepBlock; ++i) {
-                            f[i] = inf_to_nan(f[i]);
-                            amax = fmaxf(amax, fabsf(f[i]));
+#pragma unroll 1
+                        for (int c = 0; c < kHalf; c += kChunk) {
+                            float f[kChunk];
+                            tmem_load(from + c, f);
+                            for (int i = 0; i < kChunk; ++i) amax = fmaxf(amax, fabsf(inf_to_nan(f[i])));
                         }
                     }
                     const uint32_t e = keep_exponent(amax);
                     const float inv = keep_inverse(e);
                     uint8_t* to = half ? p.uq : p.gq;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < kHalf; c += kRowBytes) {
-#pragma unroll
-                        for (int k = 0; k < kRowBytes; k += 16) {
-                            uint32_t q[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int i = c + k + 4 * j;
-                                q[j] = keep4(f[i] * inv, f[i + 1] * inv, f[i + 2] * inv, f[i + 3] * inv);
-                            }
-                            own_row(buf, lane)[k / 16] = make_uint4(q[0], q[1], q[2], q[3]);
+#pragma unroll 1
+                        for (int k = 0; k < kRowBytes; k += kChunk) {
+                            float f[kChunk];
+                            tmem_load(from + c + k, f);
+                            own_row(buf, lane)[k / kChunk] = keep_chunk(odd, inv, f);
                         }
                         flush_rows(buf, to + row0 * p.ldq + c0 + c, p.ldq, rows, p.cols - c0 - c, p.q_vec, lane);
                     }
