@@ -471,28 +471,6 @@ __device__ __forceinline__ void finish_split(const GemmArgs& p, int m, int n, ui
     }
 }
 
-// A unit's tiles: every units-th one, along the axis that neighbours share first.  Stepped, not divided out (each role does it for
-// every tile, and a 64-bit division takes a few hundred cycles).
-struct TileWalk {
-    bool n_first;
-    int fast, slow, fast_end, slow_end, fast_step, slow_step;
-    __device__ __forceinline__ TileWalk(const GemmArgs& p, int unit, int units)
-        : n_first(p.n_first), fast_end(n_first ? p.nt : p.mt), slow_end(n_first ? p.mt : p.nt) {
-        fast = unit % fast_end;
-        slow = unit / fast_end;
-        fast_step = units % fast_end;
-        slow_step = units / fast_end;
-    }
-    __device__ __forceinline__ bool more() const { return slow < slow_end; }
-    __device__ __forceinline__ void next() {
-        fast += fast_step;
-        slow += slow_step;
-        if (fast >= fast_end) { fast -= fast_end; ++slow; }
-    }
-    __device__ __forceinline__ int m() const { return n_first ? slow : fast; }
-    __device__ __forceinline__ int n() const { return n_first ? fast : slow; }
-};
-
 // Maps: forward, recompute: a0 = x, b0 = Wg, b1 = Wu; dgrad: a0 = dg, a1 = du, b0 = Wg, b1 = Wu; wgrad: a0 = dg,
 // a1 = du, b0 = x.
 template <typename T, typename OT, int FORM, int CG, int BN>
@@ -545,11 +523,16 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
 
     // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
     const int unit_ctas = CG == 2 ? 2 : p.split;
-    const int unit = (int)(blockIdx.x / unit_ctas), units = (int)(gridDim.x / unit_ctas);
+    const int64_t unit = blockIdx.x / unit_ctas, units = gridDim.x / unit_ctas;
+    const int64_t tiles = (int64_t)p.mt * p.nt;
     const int nkb = p.kb0 + p.kb1;
     // this CTA's slices of the reduction
     const int kb_begin = CG == 2 ? 0 : (int)((int64_t)nkb * rank / p.split);
     const int kb_end = CG == 2 ? nkb : (int)((int64_t)nkb * (rank + 1) / p.split);
+    auto place = [&](int64_t tile, int& m, int& n) {
+        if (p.n_first) { n = (int)(tile % p.nt); m = (int)(tile / p.nt); }
+        else { m = (int)(tile % p.mt); n = (int)(tile / p.mt); }
+    };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -559,8 +542,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             uint32_t ph = 0;
             int64_t issued = 0;
             bool ok = true;
-            for (TileWalk t(p, unit, units); ok && t.more(); t.next()) {
-                const int m = t.m(), n = t.n();
+            for (int64_t tile = unit; ok && tile < tiles; tile += units) {
+                int m, n;
+                place(tile, m, n);
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, status)) { ok = false; break; }
                     uint8_t* a = stages + (size_t)s * TL::stage_bytes;
@@ -633,7 +617,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             int s = 0, buf = 0;
             uint32_t ph = 0, aph = 0;
             bool ok = true;
-            for (TileWalk t(p, unit, units); ok && t.more(); t.next()) {
+            for (int64_t tile = unit; ok && tile < tiles; tile += units) {
                 if (!mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
@@ -669,9 +653,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         uint8_t* buf = buffers + (warp - 2) * kWarpBuffer;
         int acc = 0;
         uint32_t ph = 0;
-        for (TileWalk t(p, unit, units); t.more(); t.next()) {
-            int m = t.m();
-            const int n = t.n();
+        for (int64_t tile = unit; tile < tiles; tile += units) {
+            int m, n;
+            place(tile, m, n);
             if (!__all_sync(0xffffffffu, mbar_wait(&sm->accum_full[acc], ph, abort_flag, status))) break;
             tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(acc * BN);
@@ -801,8 +785,8 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             // ------------------------------------------------ the cluster's sums are added and the tile is finished
             __syncthreads();
             cluster_sync();
-            const TileWalk t(p, unit, units);
-            const int m = t.m(), n = t.n();
+            int m, n;
+            place(unit, m, n);
             const uint32_t sums = smem_u32(stages);
             if (p.split == 2) finish_split<T, OT, FORM, BN, 2>(p, m, n, rank, sums, warp, lane);
             else if (p.split == 3) finish_split<T, OT, FORM, BN, 3>(p, m, n, rank, sums, warp, lane);
