@@ -147,10 +147,8 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Relaxed: it says that the accumulator has been read, and what was read is in registers.  A release at cluster scope would also
-// wait for the output rows' stores to arrive, about 1 us of a tile.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // 2-D TMA load into this CTA, completion counted on `bar`: a barrier of this CTA, or (pair) of the first CTA
 template <int CG>
