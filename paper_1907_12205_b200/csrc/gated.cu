@@ -14,7 +14,7 @@
 // the MMAs, eight warps drain the accumulator (two to each quarter of its rows).  Two accumulators share the tensor memory, so
 // a tile is drained while the next one is multiplied.  Ragged edges: TMA fills with zeros outside a matrix and the epilogue
 // masks its stores.
-// Three shapes of the work (shape_of and shapes_beside choose):
+// Three shapes of the work (shape_of chooses):
 //   pair     two CTAs of a cluster multiply one 256 x 256 tile (cta_group::2): each holds 128 rows of either operand, so
 //            a byte of shared memory feeds twice the MMA work that a CTA on its own gets out of it; persistent grid
 //   single   one CTA, 128 x 256 or 128 x 128; persistent grid
@@ -72,7 +72,6 @@ struct GemmArgs {
     int kb0, kb1;                  // slices of the first and of the second product that are added up
     int split;                     // CTAs that share a tile's reduction
     bool clear_status;             // first kernel of the call that may set the status word
-    bool beside;                   // runs beside the product before it in the stream, see below
     bool n_first;                  // neighbouring tiles lie along a row of the output (else along a column)
     int act;
     int64_t rows, cols;            // of the output (forward, recompute: of h)
@@ -512,10 +511,8 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         else asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
     }
     tc_fence_after();
-    // The next kernel is let in only after this one's own wait, so by then all that came before this one is finished.  A
-    // product that needs nothing from the one before it (wgrad from dgrad) then need not wait to start, and takes the SMs
-    // that the other leaves idle; it waits at its end instead, so that whatever waits for it waits for both.
-    if (!p.beside) pdl_wait();
+    // The next kernel is let in only after this one's own wait, so by then all that came before this one is finished.
+    pdl_wait();
     pdl_trigger();
     if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it about a second later)
 
@@ -797,7 +794,6 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     __syncthreads();
     if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
     if (warp == 1) tmem_dealloc_cg<CG>(sm->tmem_base, TL::tmem_cols);
-    if (p.beside && blockIdx.x + CG >= gridDim.x) pdl_wait();   // (the last CTAs only: the others' SMs are wanted)
 }
 
 // ---- what the backward pass lays out before its products -----------------------------------------
@@ -1026,16 +1022,13 @@ struct Product {
     int nkb;
     bool keeps;        // leaves the 8-bit form, which needs a block of 128 columns in a tile
 };
-struct Estimate {
-    int64_t ctas, tile, whole;   // CTAs' tiles, a tile's time, the launch's time
-};
-Estimate estimate(const Product& p, const Shape& s) {
+int64_t estimate(const Product& p, const Shape& s) {
     static const int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
     const int64_t tiles = p.copies * ceil_div(p.rows, (int64_t)(128 * s.cg)) * ceil_div(p.cols, (int64_t)s.bn);
     const int slice = p.rows * p.copies <= 128 ? 36 : (s.cg == 2 ? 28 : (s.bn == 256 ? 45 : 27));
     const int64_t tile = ceil_div((int64_t)p.nkb, (int64_t)s.split) * slice + 250 * s.bn / 256 + (p.keeps ? 100 : 0) +
                          (s.split > 1 ? 100 : 0);
-    return Estimate{tiles * s.cg * s.split, tile, ceil_div(tiles, (int64_t)kClusters[s.cg * s.split]) * tile + 400};
+    return ceil_div(tiles, (int64_t)kClusters[s.cg * s.split]) * tile + 400;
 }
 template <typename F>
 void each_shape(const Product& p, F f) {
@@ -1050,34 +1043,13 @@ Shape shape_of(const Product& p) {
     Shape best{2, 256, 1};
     int64_t least = INT64_MAX;
     each_shape(p, [&](const Shape& s) {
-        const int64_t time = estimate(p, s).whole;
+        const int64_t time = estimate(p, s);
         if (time < least) {
             least = time;
             best = s;
         }
     });
     return best;
-}
-// The shapes of two products that run beside each other, b on the SMs that a leaves idle: together they take what the work of
-// both takes on all SMs and one of b's tiles, and no less than either takes alone.  b is not split for it (but may
-// be if that is best for b alone).
-void shapes_beside(const Product& a, const Product& b, Shape* sa, Shape* sb) {
-    int64_t least = INT64_MAX;
-    const Shape of_b[4] = {{2, 256, 1}, {1, 256, 1}, {1, 128, 1}, shape_of(b)};
-    each_shape(a, [&](const Shape& s) {
-        const Estimate ea = estimate(a, s);
-        for (const Shape& t : of_b) {
-            const Estimate eb = estimate(b, t);
-            int64_t time = (ea.ctas * ea.tile + eb.ctas * eb.tile) / kSMs + eb.tile + 400;
-            time = time > ea.whole ? time : ea.whole;
-            time = time > eb.whole ? time : eb.whole;
-            if (time < least) {
-                least = time;
-                *sa = s;
-                *sb = t;
-            }
-        }
-    });
 }
 int slices(int64_t n) { return (int)ceil_div(n, (int64_t)kSlice); }
 Product gated_product(const detox_gated_desc& g, bool keeps) { return Product{g.tokens, 1, 2 * g.hidden, slices(g.in_dim), keeps}; }
@@ -1153,10 +1125,9 @@ detox_status forward(const detox_gated_desc& g, void* H, int64_t ldh, char* ws, 
 
 template <typename T, typename OT>
 detox_status weight_gradients(const detox_gated_desc& g, const Mat& dg, const Mat& du, const Mat& x, void* dWg, void* dWu,
-                              int64_t lddw, bool clear_status, bool beside, const Shape& shape, int* status, cudaStream_t s) {
+                              int64_t lddw, bool clear_status, const Shape& shape, int* status, cudaStream_t s) {
     GemmArgs a{};
     a.clear_status = clear_status;
-    a.beside = beside;
     a.kb0 = slices(g.tokens);
     a.rows = g.hidden;
     a.cols = g.in_dim;
@@ -1220,8 +1191,6 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
     if (st != DETOX_OK) return st;
     const Product dx_product{g.tokens, 1, g.in_dim, 2 * slices(g.hidden), false};
     const Product dw_product{g.hidden, 2, g.in_dim, slices(g.tokens), false};
-    Shape shape_dx = shape_of(dx_product), shape_dw = shape_of(dw_product);
-    if (dX && dWg) shapes_beside(dx_product, dw_product, &shape_dx, &shape_dw);
     if (dX) {
         GemmArgs a{};
         a.clear_status = kept;
@@ -1233,12 +1202,12 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
         a.out_vec = tma_ok(dX, lddx);
         const MapOf mdg{dg, g.tokens, g.hidden}, mdu{du, g.tokens, g.hidden};
         const MapOf mg{wg, g.hidden, g.in_dim}, mu{wu, g.hidden, g.in_dim};
-        st = launch_gemm<T, T, kDgrad>(mdg, mdu, mg, mu, a, shape_dx, status, s);
+        st = launch_gemm<T, T, kDgrad>(mdg, mdu, mg, mu, a, shape_of(dx_product), status, s);
         if (st != DETOX_OK) return st;
     }
     if (!dWg) return DETOX_OK;
-    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, shape_dw, status, s);
-    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, dX != nullptr, shape_dw, status, s);
+    if (dw_dtype == DETOX_DTYPE_FLOAT) return weight_gradients<T, float>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, shape_of(dw_product), status, s);
+    return weight_gradients<T, T>(g, dg, du, x, dWg, dWu, lddw, kept && !dX, shape_of(dw_product), status, s);
 }
 
 }  // namespace
