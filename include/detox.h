@@ -369,7 +369,8 @@ detox_status detox_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, con
  *     dg = dh * u * act'(g),   du = dh * act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
  * dg and du are rounded to dtype, the type the tensor cores multiply; every sum over them is fp32.
  *
- * dtype is HALF or BFLOAT (FLOAT: DETOX_ERR_UNSUPPORTED); tokens, in_dim and hidden are at most 2^30.  No output of the backward pass may overlap an input or another output.
+ * dtype is HALF or BFLOAT (FLOAT: DETOX_ERR_UNSUPPORTED); tokens, in_dim and hidden are at most 2^30.  No output
+ * of the backward pass may overlap an input or another output.
  *
  * The input is X, or its 8-bit form XQ, XE (X = NULL).  With the kept buffers (all four or none) detox_gated leaves g and
  * u there in the 8-bit form, and detox_gated_backward reads them; without them it computes g and u again from the input.
