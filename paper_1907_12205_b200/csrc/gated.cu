@@ -21,6 +21,11 @@
 //   split    few tiles: the CTAs of a cluster take a share of one tile's reduction each, leave fp32 sums in shared memory
 //            and then finish a share of its rows each, adding the others' sums over distributed shared memory in
 //            the order of their ranks
+//
+// A pair's kernel runs alone: it is launched without overlap with the kernel before it, and lets none in before it ends.  While it
+// took part in the chain of overlapping launches, steps of 8192 tokens stopped making progress about once in some thousand steps.
+// No order of events in this code explains that; on their own, 30,000 such steps finished.  It costs nothing that shows in a step
+// of 8192 tokens (0.97 ms either way); between short products it would, so the other shapes stay chained.
 #include <cuda.h>
 
 #include <type_traits>
@@ -513,7 +518,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     tc_fence_after();
     // The next kernel is let in only after this one's own wait, so by then all that came before this one is finished.
     pdl_wait();
-    pdl_trigger();
+    if constexpr (CG == 1) pdl_trigger();
     if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it about a second later)
 
     // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
@@ -1086,8 +1091,8 @@ detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, con
     const int unit = CG == 2 ? 2 : split;
     // a split's cluster finishes one tile; the others' grids are persistent
     const int64_t units = split > 1 || tiles < kSMs / unit ? tiles : kSMs / unit;
-    return launch_chained(k, (unsigned)(units * unit), kThreads, kSmemBytes<CG, BN>, (unsigned)unit, s, maps[0], maps[1], maps[2],
-                          maps[3], args, status);
+    return launch(CG == 1, k, (unsigned)(units * unit), kThreads, kSmemBytes<CG, BN>, (unsigned)unit, s, maps[0], maps[1], maps[2],
+                  maps[3], args, status);
 }
 template <typename T, typename OT, int FORM>
 detox_status launch_gemm(const MapOf& a0, const MapOf& a1, const MapOf& b0, const MapOf& b1, const GemmArgs& args, const Shape& sh,
