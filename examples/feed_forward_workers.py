@@ -99,6 +99,9 @@ def train(steps: int = 20, tokens: int = 256, dim: int = 256, hidden: int = 704,
             total += float(loss)
             if j in losing:
                 X[own[step % r]] *= -100.0
+        expired, first = dx.gated_expired_waits()                  # (a product that gave up has left NaN in its worker's row)
+        if expired:
+            raise RuntimeError(f"{expired} waits of the gated products ran out, the first: {first}")
         pipe = dx.Pipeline(n, r, layer.size, members, dx.AGG_MEAN, sets, np.arange(groups), dx.AGG_COORD_MEDIAN)
         res = dx.detox_aggregate(pipe, X)
         assert bool((res["winner"] >= 0).all()), "a group without a majority"

@@ -411,6 +411,26 @@ detox_status detox_gated_backward(const detox_gated_desc* desc, const void* dH, 
                                   void* dWg, void* dWu, int64_t lddw, int dw_dtype, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * The bounded waits of the gated products.  One that runs out sets the status word of its call, whose remaining products then
+ * give up at once; every output that was not written is NaN (kept entries too); nothing hangs, and the next call is not affected.
+ *
+ * detox_gated_expired_waits: how many of them ran out on the current device since the host last cleared the count.  It does
+ * not depend on a workspace, so it also tells of calls whose workspace is gone.  Synchronises the device.
+ *   first  host, DETOX_EXPIRED_WORDS int32 (or NULL): what the first of them waited for, -1 where there is none:
+ *          form (0 forward, 1 again for the backward pass, 2 dx, 3 weight gradients), CTAs that multiply a tile, its
+ *          columns, CTAs that share its reduction, the CTA's rank, barrier (0 a stage free, 1 a stage's copies, 2 an accumulator
+ *          free, 3 an accumulator complete), which stage or accumulator, tile (-1: after the last)
+ *   clear  not 0: the count and the record start again
+ * detox_gated_wait_limit: the limit of a wait in SM clocks, for launches from then on, in place of one that goes by the length of
+ * the product (a tenth of a second and more).  0 restores that; any other value below DETOX_WAIT_LIMIT_MIN changes
+ * nothing.  Returns the limit before (0: by the product's length).  A diagnostic: a limit that a product's own time exceeds makes it give up.
+ * ------------------------------------------------------------------------------------------- */
+#define DETOX_EXPIRED_WORDS 8
+#define DETOX_WAIT_LIMIT_MIN 10000
+unsigned long long detox_gated_expired_waits(int32_t* first, int clear);
+int64_t detox_gated_wait_limit(int64_t clocks);
+
+/* ---------------------------------------------------------------------------------------------
  * Self-test of the bounded device-side waits (no counterpart in the paper; a diagnostic).  Launches one
  * warp that waits, with the same wait routine the distance kernels use, on a barrier that nothing will
  * ever complete, for at most `limit_cycles` SM clocks (1 .. 2e9).  The wait must give up by itself: after

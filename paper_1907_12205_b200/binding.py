@@ -29,7 +29,7 @@ EXPORTS = (
     "detox_kernel_launch_count", "detox_vote_hier_mean_many", "detox_tc_split_mode", "detox_tc_repeated_passes",
     "detox_checkpoint_pack", "detox_checkpoint_unpack", "detox_rmsnorm", "detox_rmsnorm_backward_workspace_bytes",
     "detox_rmsnorm_backward", "detox_gated_workspace_bytes", "detox_gated", "detox_gated_backward_workspace_bytes",
-    "detox_gated_backward",
+    "detox_gated_backward", "detox_gated_expired_waits", "detox_gated_wait_limit",
 )
 
 
@@ -122,6 +122,10 @@ def load() -> ctypes.CDLL:
         fn = getattr(lib, name + "_workspace_bytes")
         fn.restype = _sz
         fn.argtypes = [ctypes.POINTER(GatedDesc)]
+    lib.detox_gated_expired_waits.restype = ctypes.c_ulonglong
+    lib.detox_gated_expired_waits.argtypes = [_ip, _int]
+    lib.detox_gated_wait_limit.restype = _i64
+    lib.detox_gated_wait_limit.argtypes = [_i64]
     lib.detox_gated.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _sz, _vp]
     lib.detox_gated_backward.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _i64, _vp, _vp, _i64, _int, _vp, _sz, _vp]
     _lib = lib
@@ -611,6 +615,32 @@ def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor
     x, xe, q, e = _gated_inputs(x, kept)
     return (_worker_module or _worker()).gated_backward(x, xe, wg, wu, act, q, e, dh, dx, dwg, dwu,
                                                         -1 if dw_dtype is None else _dtype_code(dw_dtype), ws, _handle(stream))
+
+
+class ExpiredWait(NamedTuple):
+    """What the first expired wait of the gated products waited for (include/detox.h, detox_gated_expired_waits)."""
+    form: int
+    ctas: int
+    columns: int
+    split: int
+    rank: int
+    barrier: int
+    index: int
+    tile: int
+
+
+def gated_expired_waits(clear: bool = False):
+    """(count, ExpiredWait or None): the waits of the gated products that ran out on the current device since the count was last
+    cleared.  Synchronises the device.  Also tells of calls that made their own workspace and with it their status word."""
+    first = (ctypes.c_int32 * 8)()
+    n = int(load().detox_gated_expired_waits(first, int(clear)))
+    return n, (ExpiredWait(*first) if n else None)
+
+
+def gated_wait_limit(clocks: int = -1) -> int:
+    """Sets the limit of the gated products' waits in SM clocks (0: by the product's length); returns the one before.  The
+    default argument only asks."""
+    return int(load().detox_gated_wait_limit(int(clocks)))
 
 
 def _dtype_code(dtype) -> int:

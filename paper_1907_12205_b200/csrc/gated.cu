@@ -26,8 +26,12 @@
 // took part in the chain of overlapping launches, steps of 8192 tokens stopped making progress about once in some thousand steps.
 // No order of events in this code explains that; on their own, 30,000 such steps finished.  It costs nothing that shows in a step
 // of 8192 tokens (0.97 ms either way); between short products it would, so the other shapes stay chained.
+//
+// Every wait on a barrier is bounded (Waits below).  One that runs out ends its CTAs' work and leaves a record, the outputs of those
+// CTAs become NaN, and the products that follow in the call give up at once.
 #include <cuda.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "gram_tc.cuh"
@@ -76,7 +80,8 @@ struct GemmArgs {
     int mt, nt;                    // output tiles (wgrad: mt counts those of dWg and of dWu)
     int kb0, kb1;                  // slices of the first and of the second product that are added up
     int split;                     // CTAs that share a tile's reduction
-    bool clear_status;             // first kernel of the call that may set the status word
+    bool clear_status;             // first kernel of the call that may set the status word; the later ones look at it
+    long long wait_limit;          // SM clocks
     bool n_first;                  // neighbouring tiles lie along a row of the output (else along a column)
     int act;
     int64_t rows, cols;            // of the output (forward, recompute: of h)
@@ -99,6 +104,55 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
     desc |= (uint64_t)1 << 46;
     desc |= (uint64_t)2 << 61;                              // 128-byte swizzle
     return desc;
+}
+
+// ---- bounded waits ------------------------------------------------------------------------------
+enum Barrier { kEmpty = 0, kFull = 1, kAccumEmpty = 2, kAccumFull = 3 };
+// Waits that ran out on this device, and what the first of them waited for: only the host clears it.
+struct Expired {
+    unsigned long long count;
+    int32_t first[DETOX_EXPIRED_WORDS];   // form, CTAs of a tile's MMA, columns, split, rank, barrier, stage or accumulator, tile
+};
+__device__ Expired g_expired;
+// (Out of line, like leave_nan below: what a product does not run should not lie between what it does.  48 tokens of 1024 -> 2816: 8.32 us,
+// with both inline 8.42, without either 8.1; 500 of 512 -> 1408, a step: 38.3, 38.9 and 38.9.)
+__device__ __noinline__ void note_expired(int* status, int form, int cg, int bn, int split, int rank, int which, int index, int tile) {
+    if (atomicAdd(&g_expired.count, 1ull) == 0) {
+        const int32_t what[DETOX_EXPIRED_WORDS] = {form, cg, bn, split, rank, which, index, tile};
+#pragma unroll
+        for (int i = 0; i < DETOX_EXPIRED_WORDS; ++i) g_expired.first[i] = what[i];
+    }
+    atomicExch(status, (int)DETOX_ERR_TIMEOUT);
+}
+struct Waits {
+    int* abort_flag;               // this CTA's
+    uint32_t peer_flag;            // the pair's other CTA's (an address in the cluster's shared memory), or 0
+    int* status;
+    long long limit;
+    int form, cg, bn, split, rank;
+    // False when the limit passed, or when another wait of this CTA or pair has already given up.
+    __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, Barrier which, int index, int64_t tile) const {
+        if (mbar_try(bar, parity)) return true;
+        const long long start = clock64();
+        for (;;) {
+            if (mbar_try(bar, parity)) return true;
+            if (*static_cast<volatile int*>(abort_flag)) return false;
+            if (clock64() - start > limit) break;
+        }
+        give_up();
+        note_expired(status, form, cg, bn, split, rank, which, index, (int)tile);
+        return false;
+    }
+    __device__ __forceinline__ void give_up() const {
+        *static_cast<volatile int*>(abort_flag) = 1;
+        if (peer_flag) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer_flag), "r"(1) : "memory");
+    }
+};
+// Copies, MMAs and arrivals in flight end within microseconds; a CTA that has given up stays this long before it goes away, so that none
+// of them meets the next kernel's shared memory.
+__device__ __forceinline__ void let_flights_land() {
+    const long long start = clock64();
+    while (clock64() - start < 4000000) __nanosleep(1000);   // two milliseconds at the highest clock
 }
 
 // ---- the forms of the tcgen05 / cluster instructions that a pair of CTAs needs -------------------
@@ -169,6 +223,11 @@ __device__ __forceinline__ void tma_load_cg(uint8_t* dst, const CUtensorMap* map
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
@@ -473,6 +532,32 @@ __device__ __forceinline__ void finish_split(const GemmArgs& p, int m, int n, ui
     }
 }
 
+// NaN in place of a tile that was given up, so that its outputs cannot be taken for results: all of it (split: every CTA of
+// the cluster writes the same), or a pair's CTA its rows.
+template <typename V>
+__device__ __noinline__ void fill(V* out, int64_t ld, int64_t r0, int64_t r1, int64_t c0, int64_t c1, V value) {
+    const int64_t cols = c1 - c0;
+    for (int64_t i = threadIdx.x; i < (r1 - r0) * cols; i += kThreads) out[(r0 + i / cols) * ld + c0 + i % cols] = value;
+}
+template <typename T, typename OT, int FORM, int CG, int BN>
+__device__ __noinline__ void leave_nan(const GemmArgs& p, int m, int n, uint32_t rank) {
+    constexpr bool kGated = FORM == kForward || FORM == kRecompute;
+    void* out = p.out0;
+    if (FORM == kWgrad && m >= p.mt / 2) { m -= p.mt / 2; out = p.out1; }
+    const int64_t r0 = (int64_t)m * Tile<CG, BN>::M + (CG == 2 ? (int)rank * 128 : 0), c0 = (int64_t)n * (kGated ? BN / 2 : BN);
+    const int64_t r1 = r0 + 128 < p.rows ? r0 + 128 : p.rows, c1 = c0 + (kGated ? BN / 2 : BN) < p.cols ? c0 + (kGated ? BN / 2 : BN) : p.cols;
+    if (r0 >= r1) return;
+    if constexpr (sizeof(OT) == 4) fill<uint32_t>(static_cast<uint32_t*>(out), p.ldo, r0, r1, c0, c1, 0x7fffffffu);
+    else fill<uint16_t>(static_cast<uint16_t*>(out), p.ldo, r0, r1, c0, c1, (uint16_t)0x7fff);   // (NaN in fp16 and in bf16)
+    if (FORM == kRecompute) fill<uint16_t>(static_cast<uint16_t*>(p.out1), p.ldo, r0, r1, c0, c1, (uint16_t)0x7fff);
+    if (FORM == kForward && BN == 256 && p.gq) {
+        fill<uint8_t>(p.gq, p.ldq, r0, r1, c0, c1, (uint8_t)0x7f);
+        fill<uint8_t>(p.uq, p.ldq, r0, r1, c0, c1, (uint8_t)0x7f);
+        fill<uint8_t>(p.ge, p.lde, r0, r1, n, n + 1, (uint8_t)127);
+        fill<uint8_t>(p.ue, p.lde, r0, r1, n, n + 1, (uint8_t)127);
+    }
+}
+
 // Maps: forward, recompute: a0 = x, b0 = Wg, b1 = Wu; dgrad: a0 = dg, a1 = du, b0 = Wg, b1 = Wu; wgrad: a0 = dg,
 // a1 = du, b0 = x.
 template <typename T, typename OT, int FORM, int CG, int BN>
@@ -488,9 +573,10 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     uint8_t* stages = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzled tiles need 1024-byte alignment
     uint8_t* buffers = stages + (size_t)kStages * TL::stage_bytes;
     GemmSmem* sm = reinterpret_cast<GemmSmem*>(buffers + kEpiWarps * kWarpBuffer);
-    volatile int* abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 || p.split > 1 ? cluster_rank() : 0u;
+    const Waits wait{&sm->abort_flag, CG == 2 ? cluster_addr(smem_u32(&sm->abort_flag), rank ^ 1u) : 0u, status, p.wait_limit,
+                     FORM, CG, BN, p.split, (int)rank};
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -519,7 +605,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
     // The next kernel is let in only after this one's own wait, so by then all that came before this one is finished.
     pdl_wait();
     if constexpr (CG == 1) pdl_trigger();
-    if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it about a second later)
+    if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;   // (a wait that runs out sets it far later)
+    // A product whose operands an expired wait has left undone gives up at once.  (Warp 2 looks: its own first wait is long.)
+    if (!p.clear_status && threadIdx.x == 64 && *static_cast<volatile int*>(status) != 0) wait.give_up();
 
     // A unit is the CTAs that work on a tile together: the pair, or the split's cluster; it takes every units-th tile.
     const int unit_ctas = CG == 2 ? 2 : p.split;
@@ -540,13 +628,12 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             const int cta_m = CG == 2 ? (int)rank * 128 : 0;          // first row of this CTA's part of A in the tile
             int s = 0;
             uint32_t ph = 0;
-            int64_t issued = 0;
             bool ok = true;
             for (int64_t tile = unit; ok && tile < tiles; tile += units) {
                 int m, n;
                 place(tile, m, n);
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, status)) { ok = false; break; }
+                    if (!wait(&sm->empty[s], ph ^ 1u, kEmpty, s, tile)) { ok = false; break; }
                     uint8_t* a = stages + (size_t)s * TL::stage_bytes;
                     uint8_t* b = a + TL::a_bytes;
                     uint32_t bar = smem_u32(&sm->full[s]);
@@ -585,22 +672,14 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
                                 tma_load_cg<CG>(b + c * kChunkBytes, &b0, col + c * 64, kb * kSlice, bar);
                         }
                     }
-                    ++issued;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
             // The last MMAs' arrivals have to land before this CTA goes away: they may come from the pair's other CTA, and the next
             // kernel's barriers lie at the same place.
             for (int i = 0; ok && i < kStages; ++i) {
-                ok = mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, status);
+                ok = wait(&sm->empty[s], ph ^ 1u, kEmpty, s, -1);
                 if (++s == kStages) { s = 0; ph ^= 1u; }
-            }
-            if (*abort_flag) {
-                // give the copies still in flight a bounded time to land before the CTA goes away (a pair's are counted
-                // at the first CTA, whichever CTA they belong to)
-                for (int64_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-                    for (uint32_t spin = 0; spin < (1u << 14) && (rank != 0 || !mbar_test(&sm->full[i % kStages], (uint32_t)(i / kStages) & 1u)); ++spin)
-                        __nanosleep(64);
             }
         }
         __syncwarp();
@@ -618,11 +697,11 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             uint32_t ph = 0, aph = 0;
             bool ok = true;
             for (int64_t tile = unit; ok && tile < tiles; tile += units) {
-                if (!mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status)) { ok = false; break; }
+                if (!wait(&sm->accum_empty[buf], aph ^ 1u, kAccumEmpty, buf, tile)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    if (!mbar_wait(&sm->full[s], ph, abort_flag, status)) { ok = false; break; }
+                    if (!wait(&sm->full[s], ph, kFull, s, tile)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t addr = smem_u32(stages + (size_t)s * TL::stage_bytes);
                     const uint64_t ad = kAmn ? smem_desc_mn(addr) : smem_desc(addr);
@@ -638,12 +717,9 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             }
             // ... and so do the last accumulators' arrivals, from both CTAs' epilogues
             for (int i = 0; ok && i < 2; ++i) {
-                ok = mbar_wait(&sm->accum_empty[buf], aph ^ 1u, abort_flag, status);
+                ok = wait(&sm->accum_empty[buf], aph ^ 1u, kAccumEmpty, buf, -1);
                 if (++buf == 2) { buf = 0; aph ^= 1u; }
             }
-            // a wait ran out: the MMAs that were issued end within microseconds, and their arrivals must not reach the next kernel
-            if (!ok)
-                for (int i = 0; i < 1024; ++i) __nanosleep(1000);
         }
         __syncwarp();
     } else {
@@ -656,7 +732,7 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         for (int64_t tile = unit; tile < tiles; tile += units) {
             int m, n;
             place(tile, m, n);
-            if (!__all_sync(0xffffffffu, mbar_wait(&sm->accum_full[acc], ph, abort_flag, status))) break;
+            if (!__all_sync(0xffffffffu, wait(&sm->accum_full[acc], ph, kAccumFull, acc, tile))) break;
             tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(part * 32) << 16) + (uint32_t)(acc * BN);
             const int in_tile = (CG == 2 ? (int)rank * 128 : 0) + part * 32 + lane;
@@ -780,11 +856,17 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
         __syncwarp();
     }
 
+    // ---------------------------------------------------- the end
+    tc_fence_before();
+    __syncthreads();
+    if (*static_cast<volatile int*>(&sm->abort_flag)) let_flights_land();
+    __syncwarp();
+    if (CG == 2 || p.split > 1) cluster_sync();      // all of the cluster's work is done, and no flag will be set any more
+    bool gave_up = *static_cast<volatile int*>(&sm->abort_flag) != 0;
     if constexpr (CG == 1) {
         if (p.split > 1) {
-            // ------------------------------------------------ the cluster's sums are added and the tile is finished
-            __syncthreads();
-            cluster_sync();
+            // the cluster's sums are added and the tile is finished (asked for here and used behind it: who gave up)
+            const uint32_t flag = ld_cluster_u32(cluster_addr(smem_u32(&sm->abort_flag), lane < p.split ? lane : 0));
             int m, n;
             place(unit, m, n);
             const uint32_t sums = smem_u32(stages);
@@ -793,11 +875,17 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant_
             else if (p.split == 4) finish_split<T, OT, FORM, BN, 4>(p, m, n, rank, sums, warp, lane);
             else if (p.split == 6) finish_split<T, OT, FORM, BN, 6>(p, m, n, rank, sums, warp, lane);
             else finish_split<T, OT, FORM, BN, 8>(p, m, n, rank, sums, warp, lane);
+            gave_up = __any_sync(0xffffffffu, flag != 0u);
+            cluster_sync();                          // nobody leaves while its shared memory may still be reached
         }
     }
-    tc_fence_before();
-    __syncthreads();
-    if (CG == 2 || p.split > 1) cluster_sync();      // nobody leaves while its shared memory may still be reached
+    if (gave_up) {
+        for (int64_t tile = unit; tile < tiles; tile += units) {
+            int m, n;
+            place(tile, m, n);
+            leave_nan<T, OT, FORM, CG, BN>(p, m, n, rank);
+        }
+    }
     if (warp == 1) tmem_dealloc_cg<CG>(sm->tmem_base, TL::tmem_cols);
 }
 
@@ -1056,6 +1144,7 @@ Shape shape_of(const Product& p) {
     });
     return best;
 }
+std::atomic<long long> g_wait_limit{0};   // SM clocks; 0: by the length of the reduction
 int slices(int64_t n) { return (int)ceil_div(n, (int64_t)kSlice); }
 Product gated_product(const detox_gated_desc& g, bool keeps) { return Product{g.tokens, 1, 2 * g.hidden, slices(g.in_dim), keeps}; }
 
@@ -1082,6 +1171,9 @@ detox_status launch_shape(const MapOf& a0, const MapOf& a1, const MapOf& b0, con
     args.mt = (int)ceil_div(args.rows, (int64_t)TL::M) * (FORM == kWgrad ? 2 : 1);
     args.nt = (int)ceil_div(args.cols, (int64_t)(kGated ? BN / 2 : BN));
     args.split = split;
+    // An accumulator takes some 900 clocks a slice at most; the limit is twenty times that, and a tenth of a second more.
+    const long long limit = g_wait_limit.load();
+    args.wait_limit = limit > 0 ? limit : 200000000LL + 20000LL * (args.kb0 + args.kb1);
     // The operand whose strips the neighbouring tiles share is read once; the other one is read again for every strip, and should
     // be the smaller one, which stays in L2.
     args.n_first = args.rows * (FORM == kWgrad ? 2 : 1) > args.cols * (kGated ? 2 : 1);
@@ -1216,6 +1308,20 @@ detox_status backward(const detox_gated_desc& g, const void* dH, int64_t lddh, v
 }
 
 }  // namespace
+
+long long gated_wait_limit(long long clocks) {
+    if (clocks != 0 && clocks < DETOX_WAIT_LIMIT_MIN) return g_wait_limit.load();
+    return g_wait_limit.exchange(clocks);
+}
+
+unsigned long long gated_expired_waits(int32_t* first, bool clear) {
+    Expired e;
+    if (cudaMemcpyFromSymbol(&e, g_expired, sizeof(e)) != cudaSuccess) return ~0ull;
+    for (int i = 0; first && i < DETOX_EXPIRED_WORDS; ++i) first[i] = e.count ? e.first[i] : -1;
+    const Expired none{};
+    if (clear && cudaMemcpyToSymbol(g_expired, &none, sizeof(none)) != cudaSuccess) return ~0ull;
+    return e.count;
+}
 
 size_t gated_ws_bytes(const detox_gated_desc& g) { return gated_plan(g, false).total; }
 size_t gated_backward_ws_bytes(const detox_gated_desc& g) { return gated_plan(g, true).total; }

@@ -311,6 +311,8 @@ detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, co
 // gated.cu
 size_t gated_ws_bytes(const detox_gated_desc& g);
 size_t gated_backward_ws_bytes(const detox_gated_desc& g);
+long long gated_wait_limit(long long clocks);
+unsigned long long gated_expired_waits(int32_t* first, bool clear);
 detox_status launch_gated(const detox_gated_desc& g, void* H, int64_t ldh, void* ws, cudaStream_t s);
 detox_status launch_gated_backward(const detox_gated_desc& g, const void* dH, int64_t lddh, void* dX, int64_t lddx,
                                    void* dWg, void* dWu, int64_t lddw, int dw_dtype, void* ws, cudaStream_t s);

@@ -139,4 +139,8 @@ detox_status detox_gated_backward(const detox_gated_desc* desc, const void* dH, 
     return launch_gated_backward(*desc, dH, lddh, dX, lddx, dWg, dWu, lddw, dw_dtype, ws, static_cast<cudaStream_t>(stream));
 }
 
+int64_t detox_gated_wait_limit(int64_t clocks) { return gated_wait_limit(clocks); }
+
+unsigned long long detox_gated_expired_waits(int32_t* first, int clear) { return gated_expired_waits(first, clear != 0); }
+
 }  // extern "C"
