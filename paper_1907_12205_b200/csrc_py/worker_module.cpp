@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -129,12 +130,23 @@ Pair pair_of(const at::Tensor& q, const at::Tensor& e, const char* what, const c
 }
 uint8_t* bytes(const Rows& r) { return static_cast<uint8_t*>(r.p); }
 
-void* stream_of(PyObject* o) {
-    if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
-    void* s = PyLong_AsVoidPtr(o);
-    if (PyErr_Occurred()) throw Raised{};
-    return s;
-}
+// The stream of a call: the caller's, or the current one.  While this lives it is the current stream, so that the outputs and the
+// workspace are made for it: a workspace that came from another stream's pool could be handed out again there, at the call's
+// return, while this stream's kernels still use it, and an output might still be in use there.
+struct OnStream {
+    cudaStream_t s;
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    OnStream(PyObject* given, const at::Tensor& like) {
+        const c10::DeviceIndex device = like.device().index();
+        s = c10::cuda::getCurrentCUDAStream(device).stream();
+        if (given == Py_None) return;
+        void* const handle = PyLong_AsVoidPtr(given);
+        if (PyErr_Occurred()) throw Raised{};
+        if (static_cast<cudaStream_t>(handle) == s) return;
+        s = static_cast<cudaStream_t>(handle);
+        guard.reset_stream(c10::cuda::getStreamFromExternal(s, device));
+    }
+};
 int64_t integer(PyObject* o) {
     const int64_t v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) throw Raised{};
@@ -184,6 +196,7 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("checkpoint_pack", n, 4, [&] {
         const Rows x = rows_of(tensor(a[0], "x"), "x");
         const int code = code_of(x.t.scalar_type(), "x");
+        const OnStream on(a[3], x.t);
         Pair to;
         if (const at::Tensor* q = optional_tensor(a[1], "out")) {
             to = pair_of(*q, tensor(a[2], "out scales"), "out", "out scales");
@@ -191,7 +204,7 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
         } else {
             to = new_pair(x.rows, x.cols, x.t);
         }
-        check(detox_checkpoint_pack(code, x.p, x.ld, x.rows, x.cols, bytes(to.q), to.q.ld, bytes(to.e), to.e.ld, stream_of(a[3])),
+        check(detox_checkpoint_pack(code, x.p, x.ld, x.rows, x.cols, bytes(to.q), to.q.ld, bytes(to.e), to.e.ld, on.s),
               "detox_checkpoint_pack");
         return wrap_all(to.q.t, to.e.t);
     });
@@ -201,11 +214,12 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* checkpoint_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("checkpoint_unpack", n, 5, [&] {
         const Pair from = pair_of(tensor(a[0], "q"), tensor(a[1], "e"), "q", "e");
+        const OnStream on(a[4], from.q.t);
         Rows x;
         if (const at::Tensor* t = optional_tensor(a[3], "out")) x = rows_of(*t, "out", t->scalar_type(), from.q.rows, from.q.cols);
         else x = new_rows(from.q.rows, from.q.cols, type_of((int)integer(a[2])), from.q.t);
         check(detox_checkpoint_unpack(code_of(x.t.scalar_type(), "out"), bytes(from.q), from.q.ld, bytes(from.e), from.e.ld, x.rows,
-                                      x.cols, x.p, x.ld, stream_of(a[4])),
+                                      x.cols, x.p, x.ld, on.s),
               "detox_checkpoint_unpack");
         return wrap(x.t);
     });
@@ -220,6 +234,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* w = vector_of(tensor(a[1], "w"), "w", type, x.cols);
         const double eps = PyFloat_AsDouble(a[3]);
         if (PyErr_Occurred()) throw Raised{};
+        const OnStream on(a[7], x.t);
         Rows r, s, y;
         Pair q;
         if (const at::Tensor* t = optional_tensor(a[2], "residual")) {
@@ -233,7 +248,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (PyObject_IsTrue(a[5])) q = new_pair(x.rows, x.cols, x.t);
         const at::Tensor rstd = new_vector(x.rows, at::kFloat, x.t);
         check(detox_rmsnorm(code, x.p, x.ld, r.p, r.ld, w, x.rows, x.cols, (float)eps, s.p, s.ld, y.p, y.ld, bytes(q.q), q.q.ld,
-                            bytes(q.e), q.e.ld, static_cast<float*>(rstd.data_ptr()), stream_of(a[7])),
+                            bytes(q.e), q.e.ld, static_cast<float*>(rstd.data_ptr()), on.s),
               "detox_rmsnorm");
         return wrap_all(s.t, y.t, q.q.t, q.e.t, rstd);
     });
@@ -248,6 +263,7 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Rows dy = rows_of(tensor(a[0], "dy"), "dy", type, s.rows, s.cols);
         void* w = vector_of(tensor(a[2], "w"), "w", type, s.cols);
         void* rstd = vector_of(tensor(a[3], "rstd"), "rstd", at::kFloat, s.rows);
+        const OnStream on(a[8], s.t);
         Rows ds, dx;
         if (const at::Tensor* t = optional_tensor(a[4], "ds")) ds = rows_of(*t, "ds", type, s.rows, s.cols);
         if (const at::Tensor* t = optional_tensor(a[5], "dx")) dx = rows_of(*t, "dx", type, s.rows, s.cols);
@@ -257,7 +273,7 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* dwp = vector_of(dw, "dw", at::kFloat, s.cols);
         const Workspace ws = workspace(a[7], detox_rmsnorm_backward_workspace_bytes(s.rows, s.cols), s.t);
         check(detox_rmsnorm_backward(code, dy.p, dy.ld, ds.p, ds.ld, s.p, s.ld, w, static_cast<const float*>(rstd), s.rows, s.cols, dx.p,
-                                     dx.ld, static_cast<float*>(dwp), ws.p, ws.bytes, stream_of(a[8])),
+                                     dx.ld, static_cast<float*>(dwp), ws.p, ws.bytes, on.s),
               "detox_rmsnorm_backward");
         return wrap_all(dx.t, dw);
     });
@@ -328,6 +344,7 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("gated", n, 11, [&] {
         Gated g = gated_desc(a);
         detox_gated_desc& d = g.d;
+        const OnStream on(a[10], g.like);
         at::Tensor q, e;
         if (PyObject_IsTrue(a[7])) {
             const int64_t ld = (d.hidden + 15) / 16 * 16, nb = blocks(d.hidden);
@@ -344,7 +361,7 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (const at::Tensor* t = optional_tensor(a[8], "h")) h = rows_of(*t, "h", g.type, d.tokens, d.hidden);
         else h = new_rows(d.tokens, d.hidden, g.type, g.like);
         const Workspace ws = workspace(a[9], detox_gated_workspace_bytes(&d), g.like);
-        check(detox_gated(&d, h.p, h.ld, ws.p, ws.bytes, stream_of(a[10])), "detox_gated");
+        check(detox_gated(&d, h.p, h.ld, ws.p, ws.bytes, on.s), "detox_gated");
         return wrap_all(h.t, q, e);
     });
 }
@@ -355,6 +372,7 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Gated g = gated_desc(a);
         const detox_gated_desc& d = g.d;
         const Rows dh = rows_of(tensor(a[7], "dh"), "dh", g.type, d.tokens, d.hidden);
+        const OnStream on(a[13], g.like);
         Rows dx, dwg, dwu;
         if (const at::Tensor* t = optional_tensor(a[8], "dx")) dx = rows_of(*t, "dx", g.type, d.tokens, d.in_dim);
         else dx = new_rows(d.tokens, d.in_dim, g.type, g.like);
@@ -372,7 +390,7 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const Workspace ws = workspace(a[12], detox_gated_backward_workspace_bytes(&d), g.like);
         check(detox_gated_backward(&d, dh.p, dh.ld, dx.p, dx.ld, dwg.p, dwu.p, dwg.ld, code_of(dwg.t.scalar_type(), "dwg"), ws.p, ws.bytes,
-                                   stream_of(a[13])),
+                                   on.s),
               "detox_gated_backward");
         return wrap_all(dx.t, dwg.t, dwu.t);
     });
