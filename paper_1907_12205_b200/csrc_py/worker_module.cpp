@@ -66,6 +66,16 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
     return *t;
 }
 
+// The device of the present call, -1 until its first tensor has been looked at: all tensors of a call lie on one device, which is
+// where it is launched, whatever the current device is.
+thread_local c10::DeviceIndex g_device = -1;
+void on_device(const at::Tensor& t, const char* what) {
+    if (!t.is_cuda()) raise(PyExc_TypeError, "%s: expected a CUDA tensor", what);
+    const c10::DeviceIndex d = t.device().index();
+    if (g_device < 0) g_device = d;
+    if (d != g_device) raise(PyExc_ValueError, "%s: on cuda:%d, the tensors before it on cuda:%d", what, (int)d, (int)g_device);
+}
+
 // A matrix with contiguous rows.
 struct Rows {
     at::Tensor t;
@@ -74,6 +84,7 @@ struct Rows {
 };
 Rows rows_of(const at::Tensor& t, const char* what) {
     if (!t.is_cuda() || t.dim() != 2) raise(PyExc_TypeError, "%s: expected a 2-D CUDA tensor", what);
+    on_device(t, what);
     Rows r{t, t.data_ptr(), t.stride(0), t.size(0), t.size(1)};
     if (t.stride(1) != 1 && r.cols > 1) raise(PyExc_ValueError, "%s: rows must be contiguous", what);
     if (r.ld < r.cols) {
@@ -97,6 +108,7 @@ Rows rows_of(const at::Tensor& t, const char* what, at::ScalarType type, int64_t
 void* vector_of(const at::Tensor& t, const char* what, at::ScalarType type, int64_t n) {
     if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 1 || t.size(0) != n || !t.is_contiguous())
         raise(PyExc_TypeError, "%s: expected a contiguous CUDA vector of %lld entries of %s", what, (long long)n, c10::toString(type));
+    on_device(t, what);
     return t.data_ptr();
 }
 
@@ -131,14 +143,16 @@ Pair pair_of(const at::Tensor& q, const at::Tensor& e, const char* what, const c
 uint8_t* bytes(const Rows& r) { return static_cast<uint8_t*>(r.p); }
 
 // The stream of a call: the caller's, or the current one.  While this lives it is the current stream, so that the outputs and the
-// workspace are made for it: a workspace that came from another stream's pool could be handed out again there, at the call's
+// workspace are made for it (and the tensors' device the current one): a workspace that came from another stream's pool could be handed out again there, at the call's
 // return, while this stream's kernels still use it, and an output might still be in use there.
 struct OnStream {
     cudaStream_t s;
     c10::cuda::OptionalCUDAStreamGuard guard;
     OnStream(PyObject* given, const at::Tensor& like) {
         const c10::DeviceIndex device = like.device().index();
-        s = c10::cuda::getCurrentCUDAStream(device).stream();
+        const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device);
+        s = current.stream();
+        if (device != c10::cuda::current_device()) guard.reset_stream(current);
         if (given == Py_None) return;
         void* const handle = PyLong_AsVoidPtr(given);
         if (PyErr_Occurred()) throw Raised{};
@@ -160,7 +174,11 @@ struct Workspace {
     size_t bytes;
 };
 Workspace workspace(PyObject* given, size_t need, const at::Tensor& like) {
-    if (const at::Tensor* t = optional_tensor(given, "ws")) return Workspace{*t, t->data_ptr(), (size_t)t->nbytes()};
+    if (const at::Tensor* t = optional_tensor(given, "ws")) {
+        on_device(*t, "ws");
+        if (!t->is_contiguous()) raise(PyExc_ValueError, "ws: expected a contiguous tensor");
+        return Workspace{*t, t->data_ptr(), (size_t)t->nbytes()};
+    }
     at::Tensor t = new_vector((int64_t)(need < 256 ? 256 : need), at::kByte, like);
     return Workspace{t, t.data_ptr(), (size_t)t.nbytes()};
 }
@@ -182,6 +200,7 @@ PyObject* wrap_all(const T&... t) {
 template <typename F>
 PyObject* guarded(const char* name, Py_ssize_t n, Py_ssize_t want, F body) {
     HANDLE_TH_ERRORS
+    g_device = -1;
     if (n != want) return PyErr_Format(PyExc_TypeError, "%s: %zd arguments, got %zd", name, want, n);
     try {
         return body();
@@ -314,7 +333,9 @@ Gated gated_desc(PyObject* const* a) {
     if (cols != d.in_dim) raise(PyExc_ValueError, "x has %lld columns, the weights %lld", (long long)cols, (long long)d.in_dim);
     if (const at::Tensor* q = optional_tensor(a[5], "kept")) {
         const at::Tensor& e = tensor(a[6], "kept scales");
-        if (!q->is_cuda() || !e.is_cuda() || q->scalar_type() != kValues || e.scalar_type() != kScales)
+        on_device(*q, "kept");
+        on_device(e, "kept scales");
+        if (q->scalar_type() != kValues || e.scalar_type() != kScales)
             raise(PyExc_TypeError, "kept: expected float8_e4m3fn values and float8_e8m0fnu scales on the GPU");
         const int64_t nb = blocks(d.hidden);
         if (q->dim() != 3 || q->size(0) != 2 || q->size(1) != d.tokens || q->size(2) != d.hidden || e.dim() != 3 || e.size(0) != 2 ||
