@@ -8,6 +8,8 @@ is no CPU path: if the library is not built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 from typing import NamedTuple, Optional, Sequence
 
@@ -160,6 +162,28 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_object(stream):
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+
+
+def _made_for_stream(fn):
+    """With a stream given, it is the current one during the call, so that outputs and workspace are made for it: blocks of
+    another stream's pool may still be in use there, or (the workspace, at the call's return) be used there again."""
+    at = list(inspect.signature(fn).parameters).index("stream")
+
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return fn(*args, **kw)
+        with torch.cuda.stream(_stream_object(stream)):
+            return fn(*args, **kw)
+
+    return call
+
+
 def _ws(nbytes: int, ws: Optional[torch.Tensor], device):
     if ws is None:
         ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
@@ -179,6 +203,7 @@ def check_status(ws: torch.Tensor, what: str = "device status", stream=None):
     _check(read_status(ws, stream), what)
 
 
+@_made_for_stream
 def detox_selftest_bounded_wait(limit_cycles: int = 100_000, status: Optional[torch.Tensor] = None, stream=None):
     """Runs the library's bounded wait on a barrier that nothing completes; returns the int32 status tensor, which
     reads 5 (DETOX_ERR_TIMEOUT) once the stream has been synchronised."""
@@ -197,6 +222,7 @@ def detox_vote_workspace_bytes(n: int, r: int) -> int:
     return int(load().detox_vote_workspace_bytes(n, r))
 
 
+@_made_for_stream
 def detox_vote(X, r: int, members, Z: Optional[torch.Tensor] = None, winner: Optional[torch.Tensor] = None,
                want_Z: bool = True, ws: Optional[torch.Tensor] = None, stream=None):
     """Majority vote per node group.  Returns (Z or None, winner)."""
@@ -232,6 +258,7 @@ def detox_vote_noalloc(X, r: int, members, Z: torch.Tensor, winner: torch.Tensor
     return Z, winner
 
 
+@_made_for_stream
 def detox_hier_mean(Z, set_offsets, set_members, M: Optional[torch.Tensor] = None, stream=None):
     lib = load()
     zp, ldz, G, d = _mat(Z)
@@ -246,6 +273,7 @@ def detox_hier_mean(Z, set_offsets, set_members, M: Optional[torch.Tensor] = Non
     return M
 
 
+@_made_for_stream
 def detox_vote_hier_mean(X, r: int, members, set_offsets, set_members, M: Optional[torch.Tensor] = None,
                          winner: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Vote and mean over each vote set in one pass.  Returns (M [S, d], winner [G])."""
@@ -266,6 +294,7 @@ def detox_vote_hier_mean(X, r: int, members, set_offsets, set_members, M: Option
     return M, winner
 
 
+@_made_for_stream
 def detox_vote_hier_mean_many(X, r: int, members_dev: torch.Tensor, set_offsets=None, M: Optional[torch.Tensor] = None,
                               winner: Optional[torch.Tensor] = None, stream=None):
     """Vote and set means for very many nodes with short vectors.  members_dev: int32 CUDA tensor [n];
@@ -294,6 +323,7 @@ def agg_coord_median_workspace_bytes(m: int, d: int) -> int:
     return int(load().agg_coord_median_workspace_bytes(m, d))
 
 
+@_made_for_stream
 def agg_coord_median(X, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     lib = load()
     xp, ld, m, d = _mat(X)
@@ -304,6 +334,7 @@ def agg_coord_median(X, out: Optional[torch.Tensor] = None, ws: Optional[torch.T
     return out
 
 
+@_made_for_stream
 def agg_trimmed_mean(X, trim: int, out: Optional[torch.Tensor] = None, stream=None):
     """Coordinate-wise mean after dropping the `trim` smallest and `trim` largest values."""
     lib = load()
@@ -314,6 +345,7 @@ def agg_trimmed_mean(X, trim: int, out: Optional[torch.Tensor] = None, stream=No
     return out
 
 
+@_made_for_stream
 def agg_sign_majority(X, out: Optional[torch.Tensor] = None, stream=None):
     """Coordinate-wise sign(sum of signs): -1, 0 or +1 per coordinate."""
     lib = load()
@@ -324,6 +356,7 @@ def agg_sign_majority(X, out: Optional[torch.Tensor] = None, stream=None):
     return out
 
 
+@_made_for_stream
 def agg_geometric_median(X, iters: int = 32, eps: float = 1e-12, out: Optional[torch.Tensor] = None,
                          ws: Optional[torch.Tensor] = None, stream=None):
     """Geometric median of at most 32 rows by `iters` Weiszfeld iterations started at the mean."""
@@ -360,6 +393,7 @@ def agg_pairwise_sqdist_workspace_bytes(m: int, d: int) -> int:
     return int(load().agg_pairwise_sqdist_workspace_bytes(m, d))
 
 
+@_made_for_stream
 def agg_pairwise_sqdist(X, D: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Squared distances between the rows: D [m, m] float64, symmetric, zero diagonal."""
     lib = load()
@@ -375,6 +409,7 @@ def agg_multikrum_workspace_bytes(m: int, d: int) -> int:
     return int(load().agg_multikrum_workspace_bytes(m, d))
 
 
+@_made_for_stream
 def agg_multikrum(X, f: int, m_sel: int, out: Optional[torch.Tensor] = None, sel: Optional[torch.Tensor] = None,
                   scores: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Returns (out [d] float32, sel [m_sel] int32 ascending, scores [m] float64)."""
@@ -396,6 +431,7 @@ def agg_bulyan_workspace_bytes(m: int, d: int) -> int:
     return int(load().agg_bulyan_workspace_bytes(m, d))
 
 
+@_made_for_stream
 def agg_bulyan(X, f: int, out: Optional[torch.Tensor] = None, sel: Optional[torch.Tensor] = None,
                ws: Optional[torch.Tensor] = None, stream=None):
     """Returns (out [d] float32, sel [m - 2f] int32 in selection order)."""
@@ -458,6 +494,7 @@ def detox_aggregate_workspace_bytes(pipe: Pipeline) -> int:
     return pipe.workspace_bytes()
 
 
+@_made_for_stream
 def detox_aggregate(pipe: Pipeline, X, out: Optional[torch.Tensor] = None, winner: Optional[torch.Tensor] = None,
                     sel: Optional[torch.Tensor] = None, sel_workers: Optional[torch.Tensor] = None,
                     ws: Optional[torch.Tensor] = None, stream=None):
