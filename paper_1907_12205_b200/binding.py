@@ -187,6 +187,10 @@ def _made_for_stream(fn):
 def _ws(nbytes: int, ws: Optional[torch.Tensor], device):
     if ws is None:
         ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+    elif ws.device != device:
+        raise TypeError(f"ws: expected a tensor on {device}, got one on {ws.device}")
+    elif not ws.is_contiguous():
+        raise ValueError("ws: expected a contiguous tensor")
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 

@@ -81,3 +81,15 @@ def test_the_functions_keep_their_signatures():
     import inspect
     assert list(inspect.signature(binding.detox_vote).parameters) == ["X", "r", "members", "Z", "winner", "want_Z", "ws", "stream"]
     assert binding.detox_vote.__doc__.startswith("Majority vote")
+
+
+def test_a_workspace_elsewhere_or_smaller_than_it_looks_is_refused():
+    host, meta = torch.device("cpu"), torch.device("meta")
+    t = torch.empty(512, dtype=torch.uint8)
+    assert binding._ws(300, t, host)[1:] == (t.data_ptr(), 512)
+    for where in (torch.device(DEV), meta):
+        with pytest.raises(TypeError, match="ws"):
+            binding._ws(300, t, where)
+    for wrong in (t[:1].expand(512), t[::2]):
+        with pytest.raises(ValueError, match="ws"):
+            binding._ws(300, wrong, host)
