@@ -263,10 +263,31 @@ __device__ __forceinline__ void tmem_load(uint32_t at_f, uint32_t at_g, float (&
 }
 
 // ---- activations: a = act(g), da = act'(g) -----------------------------------------------------
+// gelu: the normal distribution function and e = exp(-g^2 / 2).  For negative g it is small, and (1 + erf) / 2 would lose its bits
+// there, 0.1% at -4 and all of them below -5.5.  With x = |g| and t = 1 / (1 + 0.3 x), the distribution function at -x is e R(x), and
+// R(x) / t a polynomial in t: fitted to the least largest relative error over 0 <= x <= 14, 1.5e-7; with the arithmetic's own
+// error 3e-6 of its size down to g = -8.  (erfcf is as good and made a step of 500 tokens 2.4 us of 38.6 slower.)
+__device__ __forceinline__ float normal_cdf(float g, float& e) {
+    const float x = fabsf(g), t = __fdividef(1.f, fmaf(0.3f, x, 1.f));
+    e = __expf(-0.5f * x * x);
+    float q = 0.035674829f;
+    q = fmaf(q, t, -0.157203287f);
+    q = fmaf(q, t, 0.206353813f);
+    q = fmaf(q, t, -0.0536838956f);
+    q = fmaf(q, t, 0.12856175f);
+    q = fmaf(q, t, 0.099913463f);
+    q = fmaf(q, t, 0.120753959f);
+    q = fmaf(q, t, 0.119629301f);
+    const float tail = e * (t * q);
+    return g < 0.f ? tail : 1.f - tail;
+}
 template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
     if constexpr (ACT == DETOX_ACT_SILU) return __fdividef(g, 1.f + __expf(-g));
-    if constexpr (ACT == DETOX_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+    if constexpr (ACT == DETOX_ACT_GELU) {
+        float e;
+        return g * normal_cdf(g, e);
+    }
     return g < 0.f ? 0.f : g;   // (NaN stays NaN)
 }
 template <int ACT>
@@ -276,9 +297,10 @@ __device__ __forceinline__ void act_both(float g, float& a, float& da) {
         a = g * s;
         da = fmaf(a, 1.f - s, s);
     } else if constexpr (ACT == DETOX_ACT_GELU) {
-        const float c = fmaf(0.5f, erff(g * 0.70710678f), 0.5f);
+        float e;
+        const float c = normal_cdf(g, e);
         a = g * c;
-        da = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), c);
+        da = fmaf(g * 0.39894228f, e, c);
     } else {
         a = act_of<ACT>(g);
         da = g > 0.f ? 1.f : 0.f;
