@@ -367,10 +367,13 @@ detox_status detox_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, con
  * Gated pair of projections: h = act(g) * u with g = x Wg^T, u = x Wu^T in one kernel (g and u stay fp32 and are never
  * stored in full), and its backward pass
  *     dg = dh * u * act'(g),   du = dh * act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,   dWu = du^T x.
- * dg and du are rounded to dtype, the type the tensor cores multiply; every sum over them is fp32.
+ * dg and du are rounded to dtype, the type the tensor cores multiply; every sum over them is fp32.  Beside the rounding that is
+ * a matter of range in HALF: an entry of dg or du above 65504 becomes Inf, and the row of dX and the rows of dWg and dWu that it enters
+ * Inf or NaN, even where their sums would be in range; one below 2^-25 becomes 0, and below 2^-14 it has fewer bits.  Scale the
+ * loss (dH) by a power of two so that they lie between; BFLOAT has the range of fp32.
  *
  * dtype is HALF or BFLOAT (FLOAT: DETOX_ERR_UNSUPPORTED); tokens, in_dim and hidden are at most 2^30.  No output
- * of the backward pass may overlap an input or another output.
+ * of either pass may overlap an input or another output.
  *
  * The input is X, or its 8-bit form XQ, XE (X = NULL).  With the kept buffers (all four or none) detox_gated leaves g and
  * u there in the 8-bit form, and detox_gated_backward reads them; without them it computes g and u again from the input.

@@ -653,7 +653,7 @@ def detox_gated_backward(dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor
                          dwu: Optional[torch.Tensor] = None, dw_dtype=None, ws: Optional[torch.Tensor] = None, stream=None):
     """Gradients of detox_gated: (dx, dwg, dwu).  kept: what the forward pass kept; without it g and u are computed again.
     x as in detox_gated.  The weight gradients have the weights' type, or float32 with dw_dtype (or buffers of it, such as
-    pieces of a gradient's row)."""
+    pieces of a gradient's row).  In float16 the gradients of g and u have to stay below 65504 and well above 2^-25: scale dh."""
     x, xe, q, e = _gated_inputs(x, kept)
     return (_worker_module or _worker()).gated_backward(x, xe, wg, wu, act, q, e, dh, dx, dwg, dwu,
                                                         -1 if dw_dtype is None else _dtype_code(dw_dtype), ws, _handle(stream))
