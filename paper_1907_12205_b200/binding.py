@@ -532,7 +532,8 @@ def detox_aggregate(pipe: Pipeline, X, out: Optional[torch.Tensor] = None, winne
 
 # ------------------------------------------------------------------------------------------------------------------
 # The worker's side: norm, 8-bit checkpoints, gated projections.  With `stream` a call makes its outputs and its workspace for
-# that stream, as it would under torch.cuda.stream(stream).
+# that stream, as it would under torch.cuda.stream(stream).  No graph is recorded: tensors that require grad are refused outside
+# torch.no_grad().
 
 DTYPE_FLOAT, DTYPE_HALF, DTYPE_BFLOAT = range(3)
 ACT_SILU, ACT_GELU, ACT_RELU = range(3)

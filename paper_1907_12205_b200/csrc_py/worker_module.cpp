@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -54,11 +55,15 @@ at::ScalarType type_of(int code) {
     return code == DETOX_DTYPE_FLOAT ? at::kFloat : code == DETOX_DTYPE_HALF ? at::kHalf : at::kBFloat16;
 }
 
-// None or a tensor
+// None or a tensor.  The operators record no graph (their backward passes are functions of their own), so an input that asks for one is
+// refused rather than cut off in silence.
 const at::Tensor* optional_tensor(PyObject* o, const char* what) {
     if (o == Py_None) return nullptr;
     if (!THPVariable_Check(o)) raise(PyExc_TypeError, "%s: expected a tensor", what);
-    return &THPVariable_Unpack(o);
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        raise(PyExc_RuntimeError, "%s requires grad, but no graph is recorded here: call under torch.no_grad(), or pass a detached tensor", what);
+    return &t;
 }
 const at::Tensor& tensor(PyObject* o, const char* what) {
     const at::Tensor* t = optional_tensor(o, what);
