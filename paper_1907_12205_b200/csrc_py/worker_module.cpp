@@ -171,6 +171,16 @@ int64_t integer(PyObject* o) {
     if (v == -1 && PyErr_Occurred()) throw Raised{};
     return v;
 }
+// one of an enumeration's codes (what does not fit its type is none of them)
+int32_t code(PyObject* o) {
+    const int64_t v = integer(o);
+    return v < INT32_MIN || v > INT32_MAX ? -1 : (int32_t)v;
+}
+bool truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
 
 // The caller's workspace, or a new one.
 struct Workspace {
@@ -268,8 +278,8 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         } else if (a[6] != Py_None) {
             raise(PyExc_ValueError, "sum_out: there is no residual to add");
         }
-        if (PyObject_IsTrue(a[4])) y = new_rows(x.rows, x.cols, type, x.t);
-        if (PyObject_IsTrue(a[5])) q = new_pair(x.rows, x.cols, x.t);
+        if (truth(a[4])) y = new_rows(x.rows, x.cols, type, x.t);
+        if (truth(a[5])) q = new_pair(x.rows, x.cols, x.t);
         const at::Tensor rstd = new_vector(x.rows, at::kFloat, x.t);
         check(detox_rmsnorm(code, x.p, x.ld, r.p, r.ld, w, x.rows, x.cols, (float)eps, s.p, s.ld, y.p, y.ld, bytes(q.q), q.q.ld,
                             bytes(q.e), q.e.ld, static_cast<float*>(rstd.data_ptr()), on.s),
@@ -317,7 +327,7 @@ Gated gated_desc(PyObject* const* a) {
     const Rows wu = rows_of(tensor(a[3], "wu"), "wu", g.type, wg.rows, wg.cols);
     detox_gated_desc& d = g.d;
     d.dtype = code_of(g.type, "wg");
-    d.act = (int32_t)integer(a[4]);
+    d.act = code(a[4]);
     d.hidden = wg.rows;
     d.in_dim = wg.cols;
     d.Wg = wg.p; d.ldwg = wg.ld;
@@ -361,7 +371,7 @@ Gated gated_desc(PyObject* const* a) {
 PyObject* gated_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("gated_workspace_bytes", n, 8, [&] {
         const Gated g = gated_desc(a);
-        return PyLong_FromSize_t(PyObject_IsTrue(a[7]) ? detox_gated_backward_workspace_bytes(&g.d) : detox_gated_workspace_bytes(&g.d));
+        return PyLong_FromSize_t(truth(a[7]) ? detox_gated_backward_workspace_bytes(&g.d) : detox_gated_workspace_bytes(&g.d));
     });
 }
 
@@ -372,7 +382,7 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
         detox_gated_desc& d = g.d;
         const OnStream on(a[10], g.like);
         at::Tensor q, e;
-        if (PyObject_IsTrue(a[7])) {
+        if (truth(a[7])) {
             const int64_t ld = (d.hidden + 15) / 16 * 16, nb = blocks(d.hidden);
             q = new_tensor({2, d.tokens, d.hidden}, {d.tokens * ld, ld, 1}, kValues, g.like);
             e = new_tensor({2, d.tokens, nb}, {d.tokens * nb, nb, 1}, kScales, g.like);
