@@ -21,7 +21,7 @@ def inputs(tokens, in_dim, hidden, dtype=BF16, seed=0):
 @pytest.fixture
 def short_limit():
     """Ten thousand clocks, some six microseconds.  (A wait looks at the clock only after the hardware has suspended it for a while, so the
-    accumulators of the products here take 30 us and more.)"""
+    accumulators of the products here take 45 us and more.)"""
     assert dx.gated_expired_waits(clear=True)[0] == 0
     yield lambda: dx.gated_wait_limit(10_000)
     torch.cuda.synchronize()
@@ -30,8 +30,8 @@ def short_limit():
 
 
 # what the shape rule takes for them: CTAs that multiply a tile, its columns, CTAs that share its reduction
-FORWARD = [((3, 65536, 300), False, (1, 128, 8)), ((3, 65536, 300), True, (1, 256, 8)), ((1280, 8192, 1800), False, (1, 128, 1)),
-           ((1152, 8192, 1024), True, (1, 256, 2)), ((2048, 4096, 4096), False, (2, 256, 1)), ((2048, 4096, 4096), True, (2, 256, 1))]
+FORWARD = [((3, 65536, 300), False, (1, 128, 8)), ((3, 65536, 300), True, (1, 256, 8)), ((1280, 16384, 1800), False, (1, 128, 1)),
+           ((1152, 16384, 1024), True, (1, 256, 2)), ((2048, 16384, 4096), False, (2, 256, 1)), ((2048, 16384, 4096), True, (2, 256, 1))]
 
 
 @pytest.mark.gpu
@@ -64,7 +64,7 @@ def test_a_forward_wait_that_runs_out_is_reported_and_the_next_call_is_right(sho
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("sizes", [(2048, 4096, 4096), (1000, 8192, 4800), (64, 8192, 20000)])
+@pytest.mark.parametrize("sizes", [(2048, 16384, 8192), (1000, 16384, 9600), (64, 32768, 9000)])
 @pytest.mark.parametrize("kept", [False, True])
 def test_a_backward_wait_that_runs_out_ends_the_call(short_limit, sizes, kept):
     x, wg, wu, dh = inputs(*sizes)
@@ -87,7 +87,7 @@ def test_a_backward_wait_that_runs_out_ends_the_call(short_limit, sizes, kept):
 @pytest.mark.gpu
 def test_an_expired_wait_is_known_without_a_workspace(short_limit):
     """Calls that make their own workspace take its status word with them; the count stays, over later calls too."""
-    x, wg, wu, _ = inputs(2048, 4096, 4096)
+    x, wg, wu, _ = inputs(2048, 16384, 4096)
     short_limit()
     dx.detox_gated(x, wg, wu)
     dx.gated_wait_limit(0)
