@@ -24,8 +24,8 @@
 //
 // A pair's kernel runs alone: it is launched without overlap with the kernel before it, and lets none in before it ends.  While it
 // took part in the chain of overlapping launches, steps of 8192 tokens stopped making progress about once in some thousand steps.
-// No order of events in this code explains that; on their own, 30,000 such steps finished.  It costs nothing that shows in a step
-// of 8192 tokens (0.97 ms either way); between short products it would, so the other shapes stay chained.
+// No order of events in this code explains that; on their own, 80,000 such steps finished.  It costs nothing that shows in a step
+// of 8192 tokens (0.97 ms either way) and 4 us in a backward pass of 1001 (70.9 -> 74.4, two pairs), so the other shapes stay chained.
 //
 // Every wait on a barrier is bounded (Waits below).  One that runs out ends its CTAs' work and leaves a record, the outputs of those
 // CTAs become NaN, and the products that follow in the call give up at once.
@@ -1115,8 +1115,9 @@ void weight_matrices(const detox_gated_desc& g, const GatedPlan& q, char* ws, Co
     *wu = copies->add(q.copy_wu, Mat{g.Wu, g.ldwu}, g.hidden, g.in_dim, ws + q.wu);
 }
 
-// Which shape a product takes: the least of an estimate, in units of 10 ns, that was fitted to measurements of every shape
-// on twenty problems from 1 to 8192 tokens (the shape it takes costs 1.4% more than the best one on average):
+// Which shape a product takes: the least of an estimate, in units of 10 ns, that was fitted to measurements of every shape on
+// twenty problems from 1 to 8192 tokens, while pairs too were launched overlapping the kernel before.  (On the present code the shape it
+// takes costs 3.3% more than the best one on average, 20% at worst, over the four products of eighteen of them.)
 //   a slice of the reduction   pair 28, nearly the MMAs' own rate; 128 x 256 on one CTA 45, 128 x 128 27: a CTA takes in
 //                  about 64 bytes a clock, and these need 48 and 32 KB a slice for 1/2 and 1/4 of a pair tile's work.
 //                  With one row of tiles every byte of the weights comes from HBM for a single use, and the shapes differ
