@@ -22,8 +22,9 @@
  *   - Errors: argument problems are reported before anything is launched; a failed launch returns
  *     DETOX_ERR_CUDA.  Nothing aborts or throws.  Multi-Krum and Bulyan run kernels that wait on
  *     asynchronous copies (9 to 16 long rows) or on the tensor cores (17 to 256 rows); every such
- *     device-side wait is bounded.  Device status word: the first int32 of the workspace passed to
- *     agg_multikrum, agg_bulyan or detox_aggregate.  The call clears it; should a wait run out in any
+ *     device-side wait is bounded, and so are those of the gated products.  Device status word: the first int32
+ *     of the workspace passed to agg_multikrum, agg_bulyan, agg_pairwise_sqdist, detox_aggregate, detox_gated or
+ *     detox_gated_backward.  The call clears it; should a wait run out in any
  *     stage of the call it reads DETOX_ERR_TIMEOUT once the stream has been synchronised (0 otherwise),
  *     the outputs are then not valid (the index outputs still hold in-range indices), and nothing
  *     hangs or faults.
@@ -416,6 +417,10 @@ detox_status detox_gated_backward(const detox_gated_desc* desc, const void* dH, 
 /* ---------------------------------------------------------------------------------------------
  * The bounded waits of the gated products.  One that runs out sets the status word of its call, whose remaining products then
  * give up at once; every output that was not written is NaN (kept entries too); nothing hangs, and the next call is not affected.
+ *
+ * Large products, which pairs of CTAs multiply, are launched without overlap with the stream's other kernels.  While they
+ * overlapped, full batches stopped making progress about once in some thousand steps; that it was the overlap is what long
+ * series of steps since then say, not a proof.
  *
  * detox_gated_expired_waits: how many of them ran out on the current device since the host last cleared the count.  It does
  * not depend on a workspace, so it also tells of calls whose workspace is gone.  Synchronises the device.
