@@ -439,6 +439,163 @@ unsigned long long detox_gated_expired_waits(int32_t* first, int clear);
 int64_t detox_gated_wait_limit(int64_t clocks);
 
 /* ---------------------------------------------------------------------------------------------
+ * Token embedding, with the worker's side: rows of a table, scaled,
+ *     Y[t] = scale * W[tokens[t]]
+ * and the table's gradient
+ *     dW[v] = (dW[v] +) scale * sum of dY[t] over the rows t with tokens[t] = v,
+ * added in fp32 in an order that depends on the sizes and the tokens alone.  A negative token is padding: its row is zero and it has no
+ * gradient.  A token >= vocab has a row of NaN, and no gradient either.
+ *
+ *   W       dev, vocab x ldw        dtype FLOAT, HALF or BFLOAT
+ *   tokens  dev, rows               int32 or int64, see `index`
+ *   Y       dev, rows x ldy         out, dtype
+ *   dY      dev, rows x lddy        dtype
+ *   dW      dev, vocab x lddw       out, dtype `dw_dtype`: dtype, or DETOX_DTYPE_FLOAT (then it can be a piece of a row of the matrix that the
+ *                                   vote reads).  accumulate = 0: every row is written, those of tokens that do not occur with zeros.  Else the sums
+ *                                   are added to what dW holds (fp32 sum, rounded once), and rows of tokens that do not occur are left alone
+ *   ws      detox_embedding_backward_workspace_bytes(rows, vocab, cols) bytes
+ * No output may overlap an input.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum {
+    DETOX_INDEX_INT32 = 0,
+    DETOX_INDEX_INT64 = 1
+} detox_index;
+
+detox_status detox_embedding(int dtype, const void* W, int64_t ldw, int64_t vocab, int64_t cols, int index, const void* tokens,
+                             int64_t rows, float scale, void* Y, int64_t ldy, void* stream);
+size_t detox_embedding_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t cols);
+detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, int index, const void* tokens, int64_t rows, int64_t vocab,
+                                      int64_t cols, float scale, void* dW, int64_t lddw, int dw_dtype, int accumulate, void* ws,
+                                      size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Losses over logits.  Z has a row of vocab logits for each token position, y the token chosen there; with temperature 1 / scale (scale > 0)
+ *     lse[t] = log sum_j exp(scale Z[t][j]),     logp[t] = scale Z[t][y[t]] - lse[t]
+ * Every dtype is computed in fp32 and rounded once.
+ *   - y[t] < 0: the row has no chosen token.  It is not read; its logp and lse are 0, it takes no part in a loss, and its gradient is zero.
+ *     y[t] >= vocab: logp is NaN (and with it the loss and the row's gradient).
+ *   - Logits of -Inf (masked entries) have probability and gradient 0.  A row of nothing but -Inf: lse and logp are -Inf, its gradient zero.
+ *   - vocab <= DETOX_LOGITS_MAX_COLS (a cluster of CTAs holds a row).
+ *   - dZ may be Z itself (same base and stride).
+ *
+ *   Z, dZ    dev, rows x ldz / lddz    dtype FLOAT, HALF or BFLOAT
+ *   y        dev, rows                 int32 or int64 (`index`)
+ *   logp, lse, dlogp                   dev, rows, fp32
+ * detox_token_logp_backward: dZ[t][j] = scale dlogp[t] (1[j = y[t]] - exp(scale Z[t][j] - lse[t])), lse as detox_token_logp left it.  A row whose
+ * dlogp is 0 is not read, and its gradient is zero.
+ * ------------------------------------------------------------------------------------------- */
+#define DETOX_LOGITS_MAX_COLS 262144
+detox_status detox_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
+                              float* logp, float* lse, void* stream);
+detox_status detox_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
+                                       float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Clipped policy loss with a KL term, and the gradient of the logits in the same pass over them.  With the ratio r = exp(logp - old[t]),
+ *     pg[t] = -min(r A[t], min(max(r, 1 - clip_low), 1 + clip_high) A[t])
+ *     kl[t] = exp(ref[t] - logp) - (ref[t] - logp) - 1                  (0 without ref)
+ *     loss  = sum over t of w[t] (pg[t] + kl_coef kl[t])                (without w: w[t] = 1 / rows)
+ *   old, A   dev, rows (fp32)    log-probability under the policy that chose the tokens, and advantage
+ *   ref      dev, rows (fp32)    log-probability under the reference policy; may be NULL
+ *   w        dev, rows (fp32)    weights, such as mask / number of tokens; may be NULL.  A row of weight 0 counts like one without a chosen token
+ *                                (logp 0), whatever its logits, old, A and ref hold
+ *   stats    dev, 4 (fp32)       out: loss, sum w pg, sum w kl, sum of w over the clipped tokens (r A > clipped r A); added in a fixed order
+ *   logp     dev, rows (fp32)    out; may be NULL
+ *   dZ       dev, rows x lddz    out: grad_scale * d loss / d Z; NULL: not wanted
+ *   ws       detox_policy_loss_workspace_bytes(rows) bytes
+ * clip_low in [0, 1], clip_high >= 0.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t dtype, index;        /* detox_dtype of the logits, detox_index of y */
+    int64_t rows, vocab;
+    const void* Z;               /* dev, rows x ldz */
+    int64_t ldz;
+    const void* y;               /* dev, rows */
+    const float* old_logp;       /* dev, rows */
+    const float* advantage;      /* dev, rows */
+    const float* ref_logp;       /* dev, rows; or NULL */
+    const float* weight;         /* dev, rows; or NULL */
+    float clip_low, clip_high, kl_coef, scale, grad_scale;
+} detox_policy_desc;
+
+size_t detox_policy_loss_workspace_bytes(int64_t rows);
+detox_status detox_policy_loss(const detox_policy_desc* desc, float* stats, float* logp, void* dZ, int64_t lddz, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Preference loss of paired log ratios.  The rows are packed sequences: rows offsets[i] .. offsets[i + 1] - 1 are sequence i, and sequences 2p and
+ * 2p + 1 are the preferred and the other answer of pair p.  S_i = sum of logp over sequence i (rows without a chosen token, such as a prompt's, add 0):
+ *     margin[p] = beta ((S_2p - ref_2p) - (S_2p+1 - ref_2p+1))
+ *     loss      = mean over p of -(1 - smoothing) log sigmoid(margin[p]) - smoothing log sigmoid(-margin[p])
+ *   offsets  dev, 2 pairs + 1 (int32)   ascending, 0 .. rows (others are clamped; the results are then of no use).  Rows of no sequence have zero gradients
+ *   ref      dev, 2 pairs (fp32)        the sums under the reference policy
+ *   loss     dev, 1 (fp32)              out (0 pairs: 0)
+ *   margin   dev, pairs (fp32)          out
+ *   sums     dev, 2 pairs (fp32)        out: S
+ *   dZ       dev, rows x lddz           out: grad_scale * d loss / d Z; NULL: not wanted
+ *   ws       detox_preference_loss_workspace_bytes(rows, pairs) bytes
+ * smoothing in [0, 1].  The sums over tokens are formed in 64 bits.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t dtype, index;
+    int64_t rows, vocab, pairs;
+    const void* Z;               /* dev, rows x ldz */
+    int64_t ldz;
+    const void* y;               /* dev, rows */
+    const int32_t* offsets;      /* dev, 2 pairs + 1 */
+    const float* ref;            /* dev, 2 pairs */
+    float beta, smoothing, scale, grad_scale;
+} detox_preference_desc;
+
+size_t detox_preference_loss_workspace_bytes(int64_t rows, int64_t pairs);
+detox_status detox_preference_loss(const detox_preference_desc* desc, float* loss, float* margin, float* sums, void* dZ, int64_t lddz,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * One AdamW step over many tensors: what the server does with the aggregated gradient (whose pieces the tensors' gradients can be).
+ *     m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2                      (g: the gradient times grad_scale)
+ *     p <- p - lr (weight_decay p + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps))
+ * in fp32; with a master copy p is read from it and written to it unrounded, and P gets it rounded to its type.
+ *
+ * States in 32 bits: M and V hold m and v.  States in 8 bits: they hold m and sqrt(v) in the 8-bit form of the checkpoints above, taken over the
+ * tensor's n entries as one row, except that an entry is rounded up or down at random, so that its mean is right (to the nearest,
+ * sqrt(v) would not move at all: beta2 changes it by far less than the form's step).  A root that is not 0 is never kept as 0.  The step itself uses m and v
+ * before they are rounded.  The random bits are a function of seed, step, the tensor's key and the entry alone, so every copy of a server gets the same states:
+ *     mix(x): x ^= x >> 16;  x *= 0x85ebca6b;  x ^= x >> 13;  x *= 0xc2b2ae35;  x ^= x >> 16          (32 bits)
+ *     h = mix(mix(mix(seed + 0x9e3779b9 step) + key) ^ entry),  m takes h & 0xffff, sqrt(v) h >> 16
+ * and an entry between two neighbours is rounded away from zero when its distance from the lower one, in steps, plus those bits / 2^16 reaches 1.
+ *
+ * tensors: host, `count` of them; read before the call returns.  No two buffers of a call may overlap, but P may be the master itself (FLOAT; give
+ * it as P alone).  Entries are contiguous; any alignment to the entry's size works, 16 bytes (8 for 16-bit entries, 4 for 8-bit ones) is faster.
+ * A tensor without entries is passed over.  No workspace.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    void* P;                     /* dev, n: the weights */
+    const void* G;               /* dev, n: the gradient */
+    float* master;               /* dev, n: fp32 copy of the weights; or NULL */
+    void* M;                     /* dev, n: fp32, or e4m3 */
+    uint8_t* ME;                 /* dev, ceil(n / DETOX_KEEP_BLOCK): scales; 32 bits: not used */
+    void* V;
+    uint8_t* VE;
+    int64_t n;
+    int32_t p_dtype, g_dtype;    /* detox_dtype */
+    float weight_decay;
+    uint32_t key;
+} detox_adamw_tensor;
+
+typedef struct {
+    int32_t bits;                /* of the states: 32 or 8 */
+    uint32_t seed;               /* 8 bits only */
+    double lr, beta1, beta2, eps;
+    float grad_scale;
+    int64_t step;                /* >= 1: the number of this step */
+    const float* lr_dev;         /* dev, 1: read instead of lr when the step runs (a captured one reads it at each replay); or NULL */
+    const int64_t* step_dev;     /* dev, 1: likewise for step (taken as 1 when it is less); or NULL */
+} detox_adamw_desc;
+
+detox_status detox_adamw(const detox_adamw_desc* desc, const detox_adamw_tensor* tensors, int64_t count, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Self-test of the bounded device-side waits (no counterpart in the paper; a diagnostic).  Launches one
  * warp that waits, with the same wait routine the distance kernels use, on a barrier that nothing will
  * ever complete, for at most `limit_cycles` SM clocks (1 .. 2e9).  The wait must give up by itself: after
