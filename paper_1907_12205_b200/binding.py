@@ -32,6 +32,9 @@ EXPORTS = (
     "detox_checkpoint_pack", "detox_checkpoint_unpack", "detox_rmsnorm", "detox_rmsnorm_backward_workspace_bytes",
     "detox_rmsnorm_backward", "detox_gated_workspace_bytes", "detox_gated", "detox_gated_backward_workspace_bytes",
     "detox_gated_backward", "detox_gated_expired_waits", "detox_gated_wait_limit",
+    "detox_embedding", "detox_embedding_backward_workspace_bytes", "detox_embedding_backward", "detox_token_logp",
+    "detox_token_logp_backward", "detox_policy_loss_workspace_bytes", "detox_policy_loss",
+    "detox_preference_loss_workspace_bytes", "detox_preference_loss", "detox_adamw",
 )
 
 
@@ -61,6 +64,41 @@ class GatedDesc(ctypes.Structure):
         ("Wg", ctypes.c_void_p), ("ldwg", ctypes.c_int64), ("Wu", ctypes.c_void_p), ("ldwu", ctypes.c_int64),
         ("GQ", ctypes.c_void_p), ("GE", ctypes.c_void_p), ("UQ", ctypes.c_void_p), ("UE", ctypes.c_void_p),
         ("ldq", ctypes.c_int64), ("lde", ctypes.c_int64),
+    ]
+
+
+class PolicyDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("index", ctypes.c_int32), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+        ("Z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("y", ctypes.c_void_p), ("old_logp", ctypes.c_void_p),
+        ("advantage", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+        ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float), ("scale", ctypes.c_float),
+        ("grad_scale", ctypes.c_float),
+    ]
+
+
+class PreferenceDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("index", ctypes.c_int32), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+        ("pairs", ctypes.c_int64), ("Z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("y", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p), ("ref", ctypes.c_void_p), ("beta", ctypes.c_float), ("smoothing", ctypes.c_float),
+        ("scale", ctypes.c_float), ("grad_scale", ctypes.c_float),
+    ]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [
+        ("P", ctypes.c_void_p), ("G", ctypes.c_void_p), ("master", ctypes.c_void_p), ("M", ctypes.c_void_p), ("ME", ctypes.c_void_p),
+        ("V", ctypes.c_void_p), ("VE", ctypes.c_void_p), ("n", ctypes.c_int64), ("p_dtype", ctypes.c_int32),
+        ("g_dtype", ctypes.c_int32), ("weight_decay", ctypes.c_float), ("key", ctypes.c_uint32),
+    ]
+
+
+class AdamWDesc(ctypes.Structure):
+    _fields_ = [
+        ("bits", ctypes.c_int32), ("seed", ctypes.c_uint32), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("grad_scale", ctypes.c_float), ("step", ctypes.c_int64),
+        ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p),
     ]
 
 
@@ -130,6 +168,20 @@ def load() -> ctypes.CDLL:
     lib.detox_gated_wait_limit.argtypes = [_i64]
     lib.detox_gated.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _sz, _vp]
     lib.detox_gated_backward.argtypes = [ctypes.POINTER(GatedDesc), _vp, _i64, _vp, _i64, _vp, _vp, _i64, _int, _vp, _sz, _vp]
+    _f = ctypes.c_float
+    lib.detox_embedding.argtypes = [_int, _vp, _i64, _i64, _i64, _int, _vp, _i64, _f, _vp, _i64, _vp]
+    lib.detox_embedding_backward_workspace_bytes.restype = _sz
+    lib.detox_embedding_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
+    lib.detox_embedding_backward.argtypes = [_int, _vp, _i64, _int, _vp, _i64, _i64, _i64, _f, _vp, _i64, _int, _int, _vp, _sz, _vp]
+    lib.detox_token_logp.argtypes = [_int, _vp, _i64, _i64, _i64, _int, _vp, _f, _vp, _vp, _vp]
+    lib.detox_token_logp_backward.argtypes = [_int, _vp, _i64, _i64, _i64, _int, _vp, _f, _vp, _vp, _vp, _i64, _vp]
+    lib.detox_policy_loss_workspace_bytes.restype = _sz
+    lib.detox_policy_loss_workspace_bytes.argtypes = [_i64]
+    lib.detox_policy_loss.argtypes = [ctypes.POINTER(PolicyDesc), _vp, _vp, _vp, _i64, _vp, _sz, _vp]
+    lib.detox_preference_loss_workspace_bytes.restype = _sz
+    lib.detox_preference_loss_workspace_bytes.argtypes = [_i64, _i64]
+    lib.detox_preference_loss.argtypes = [ctypes.POINTER(PreferenceDesc), _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]
+    lib.detox_adamw.argtypes = [ctypes.POINTER(AdamWDesc), ctypes.POINTER(AdamWTensor), _i64, _vp]
     _lib = lib
     return lib
 
@@ -684,6 +736,136 @@ def gated_wait_limit(clocks: int = -1) -> int:
     """Sets the limit of the gated products' waits in SM clocks (0: by the product's length); returns the one before.  The
     default argument only asks."""
     return int(load().detox_gated_wait_limit(int(clocks)))
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Around the sublayer: the token embedding, the losses over logits, and the optimizer's step on the server.
+
+LOGITS_MAX_COLS = 262144
+
+
+def detox_embedding(tokens: torch.Tensor, w: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Rows of the table w [vocab, cols], scaled: [tokens, cols].  tokens: a vector of int32 or int64; a negative one is padding (a
+    row of zeros), one beyond the vocabulary gives a row of NaN."""
+    return (_worker_module or _worker()).embedding(tokens, w, scale, out, _handle(stream))
+
+
+def detox_embedding_backward_workspace_bytes(rows: int, vocab: int, cols: int) -> int:
+    return int(load().detox_embedding_backward_workspace_bytes(rows, vocab, cols))
+
+
+def detox_embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0, dw: Optional[torch.Tensor] = None,
+                             dw_dtype=None, accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the table, [vocab, cols], the rows of equal tokens added in a fixed order.  It has dy's type, or float32 with dw_dtype (or
+    a dw of it, such as a piece of a gradient's row).  accumulate: add to dw, as for a table that is the output head too; rows of tokens
+    that do not occur are left alone."""
+    return (_worker_module or _worker()).embedding_backward(dy, tokens, vocab, scale, dw, -1 if dw_dtype is None else _dtype_code(dw_dtype),
+                                                            accumulate, ws, _handle(stream))
+
+
+class TokenLogp(NamedTuple):
+    """Log-probabilities of the chosen tokens, and the rows' log-sum-exp for the backward pass."""
+    logp: torch.Tensor
+    lse: torch.Tensor
+
+
+def detox_token_logp(z: torch.Tensor, y: torch.Tensor, scale: float = 1.0, stream=None) -> TokenLogp:
+    """logp[t] = log softmax(scale z[t])[y[t]] for logits z [tokens, vocab].  y < 0: no token was chosen there; the row is not read and
+    both results are 0."""
+    return TokenLogp._make((_worker_module or _worker()).token_logp(z, y, scale, _handle(stream)))
+
+
+def detox_token_logp_backward(dlogp: torch.Tensor, z: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, scale: float = 1.0,
+                              dz: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the logits for a gradient of detox_token_logp's logp.  dz may be z itself."""
+    return (_worker_module or _worker()).token_logp_backward(dlogp, z, y, lse, scale, dz, _handle(stream))
+
+
+class PolicyLoss(NamedTuple):
+    """What detox_policy_loss leaves.  stats: loss, and the weighted sums of the policy's term, of the KL term and of the clipped tokens; dz is
+    None where no gradient was wanted."""
+    stats: torch.Tensor
+    logp: torch.Tensor
+    dz: Optional[torch.Tensor]
+
+    @property
+    def loss(self):
+        return self.stats[0]
+
+    @property
+    def pg(self):
+        return self.stats[1]
+
+    @property
+    def kl(self):
+        return self.stats[2]
+
+    @property
+    def clipped(self):
+        return self.stats[3]
+
+
+def detox_policy_loss_workspace_bytes(rows: int) -> int:
+    return int(load().detox_policy_loss_workspace_bytes(rows))
+
+
+def detox_policy_loss(z: torch.Tensor, y: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor,
+                      ref_logp: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                      clip_high: float = 0.2, kl_coef: float = 0.0, scale: float = 1.0, want_grad: bool = True, grad_scale: float = 1.0,
+                      dz: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> PolicyLoss:
+    """The clipped policy loss sum of weight (pg + kl_coef kl) over the tokens, and with want_grad grad_scale times its gradient by the logits, from
+    one pass over them.  weight: such as mask / number of tokens (default 1 / rows); rows of weight 0 or without a chosen token (y < 0)
+    are not read and have zero gradients.  dz may be z itself."""
+    return PolicyLoss._make((_worker_module or _worker()).policy_loss(z, y, old_logp, advantage, ref_logp, weight, clip_low, clip_high,
+                                                                      kl_coef, scale, want_grad, grad_scale, dz, ws, _handle(stream)))
+
+
+class PreferenceLoss(NamedTuple):
+    """What detox_preference_loss leaves: loss [1], margin [pairs], sums of logp [2 pairs], and the logits' gradient (or None)."""
+    loss: torch.Tensor
+    margin: torch.Tensor
+    sums: torch.Tensor
+    dz: Optional[torch.Tensor]
+
+
+def detox_preference_loss_workspace_bytes(rows: int, pairs: int) -> int:
+    return int(load().detox_preference_loss_workspace_bytes(rows, pairs))
+
+
+def detox_preference_loss(z: torch.Tensor, y: torch.Tensor, offsets: torch.Tensor, ref: torch.Tensor, beta: float = 0.1,
+                          smoothing: float = 0.0, scale: float = 1.0, want_grad: bool = True, grad_scale: float = 1.0,
+                          dz: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> PreferenceLoss:
+    """Mean loss of pairs of packed sequences, preferred and other in turn: offsets [2 pairs + 1] int32 bounds their rows, ref [2 pairs] holds
+    their sums of logp under the reference policy.  Rows with y < 0 (prompts) and rows of no sequence count nothing.  dz may be z itself."""
+    return PreferenceLoss._make((_worker_module or _worker()).preference_loss(z, y, offsets, ref, beta, smoothing, scale, want_grad,
+                                                                              grad_scale, dz, ws, _handle(stream)))
+
+
+def detox_adamw_state(params: Sequence[torch.Tensor], bits: int = 32):
+    """New states for detox_adamw, all zeros: (m, v), lists of float32 tensors, or with bits=8 of pairs (values, scales)."""
+    if bits not in (8, 32):
+        raise ValueError(f"bits: expected 8 or 32, got {bits}")
+
+    def state(p):
+        if bits == 32:
+            return torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+        q = torch.zeros(p.numel(), dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+        e = torch.ones(-(-p.numel() // KEEP_BLOCK), dtype=torch.uint8, device=p.device).view(torch.float8_e8m0fnu)   # 2^-126, a zero block's
+        return q, e
+
+    return [state(p) for p in params], [state(p) for p in params]
+
+
+def detox_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence, v: Sequence, step, lr, beta1: float = 0.9,
+                beta2: float = 0.999, eps: float = 1e-8, weight_decay=0.0, masters: Optional[Sequence] = None, grad_scale: float = 1.0,
+                seed: int = 0, stream=None) -> None:
+    """One AdamW step over all tensors, in place.  step counts from 1; step and lr may be CUDA tensors of one int64 and one float32, which the
+    step reads when it runs (so a captured one can be replayed).  m, v: as detox_adamw_state makes them; in 8 bits v holds the root, and both
+    are rounded at random with bits that follow from seed, step, a tensor's place in the list and the entry.  weight_decay: a number, or one
+    for each tensor.  masters: float32 copies of the params (or None for some), which then are what is stepped."""
+    (_worker_module or _worker()).adamw(params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, masters, grad_scale, seed,
+                                        _handle(stream))
 
 
 def _dtype_code(dtype) -> int:

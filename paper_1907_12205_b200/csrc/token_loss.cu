@@ -1,0 +1,583 @@
+// Losses over logits: log-probabilities of chosen tokens, the clipped policy loss with a KL term, the preference loss of paired log ratios.
+//
+// Per row, with x = scale z log2(e):  lse = ln sum 2^x,  logp = (x_y - log2 sum) ln 2,  d loss / d z_j = c (1[j = y] - 2^x_j / sum).
+// All of it is bound by HBM: the logits are the largest matrix of a training step, and the least is to read them once and write their
+// gradient once.
+//
+//   rows_kernel      a cluster of 1 to 8 CTAs holds a row in registers: entries come in 16-byte pieces, each thread takes 2^(x - its own largest x), the
+//                    pairs (largest, sum) of all warps meet once a row (through distributed shared memory where there are several CTAs), and the policy
+//                    loss's gradient is the kept powers times one number a thread.  So the logits are read once, one power is taken of each entry (the
+//                    special-function unit would be the bound with two), and a row has one barrier.  The next row's pieces are asked for before the
+//                    present row's sums meet.
+//   backward_kernel  the gradient where lse is known: entry by entry.  The preference loss needs all of a pair's rows before any gradient, so it takes this
+//                    second pass; it goes through the rows backwards, since the last ones that were read still lie in L2.
+//   pairs_kernel     sums over sequences, margins and the rows' gradients, a CTA a pair.
+//   total_kernel     sums of the CTAs' parts, in order.
+#include "worker.cuh"
+
+namespace detox {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
+
+// ---- clusters -------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// two floats to the same place in another CTA's shared memory
+__device__ __forceinline__ void store_at(const float2* here, uint32_t rank, float2 v) {
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(here), there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// (largest x, sum of 2^(x - largest)) of two sets; the empty set is (-Inf, 0)
+__device__ __forceinline__ float2 joined(float2 a, float2 b) {
+    const float m = a.x > b.x ? a.x : b.x;   // (NaN sums stay NaN whatever m is)
+    const float m0 = m == minus_inf() ? 0.f : m;
+    return make_float2(m, a.y * exp2_fast(a.x - m0) + b.y * exp2_fast(b.x - m0));
+}
+
+// ---- what a row has beside its logits --------------------------------------------------------------
+enum Mode { kLogp, kPolicy };
+
+struct RowsArgs {
+    const void* Z;
+    int64_t ldz;
+    Span span;
+    int64_t rows;
+    int vocab, chunk;              // columns of a row, and of a CTA's part of it
+    int cluster;
+    const void* y;
+    bool wide;                     // y in 64 bits
+    float k2;                      // scale log2(e)
+    float* logp;
+    float* lse;
+    float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
+    // the policy loss
+    const float *old_logp, *advantage, *ref_logp, *weight;
+    float low, high, kl_coef, even_weight, grad_scale;   // grad_scale: times scale
+    void* dZ;
+    int64_t lddz;
+    bool dz_vec;
+    double* parts;                 // 4 for each cluster
+};
+
+__device__ __forceinline__ int64_t chosen(const void* y, bool wide, int64_t row) {
+    return wide ? static_cast<const int64_t*>(y)[row] : (int64_t)static_cast<const int32_t*>(y)[row];
+}
+
+// The largest entry of pieces, two at a time where they are 16 bits wide (NaN is passed over).
+template <typename T> struct Largest;
+template <> struct Largest<float> {
+    float m;
+    __device__ __forceinline__ Largest() : m(minus_inf()) {}
+    __device__ __forceinline__ void take(uint4 v) {
+        m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    __device__ __forceinline__ float value() const { return m; }
+    static constexpr uint32_t kNone = 0xff800000u;             // -Inf
+};
+template <> struct Largest<__half> {
+    uint32_t m = 0xfc00fc00u;
+    __device__ __forceinline__ void take(uint4 v) { two(v.x); two(v.y); two(v.z); two(v.w); }
+    __device__ __forceinline__ void two(uint32_t w) {
+        const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&m), *reinterpret_cast<const __half2*>(&w));
+        m = *reinterpret_cast<const uint32_t*>(&r);
+    }
+    __device__ __forceinline__ float value() const { const float2 f = unpack2<__half>(m); return fmaxf(f.x, f.y); }
+    static constexpr uint32_t kNone = 0xfc00fc00u;
+};
+template <> struct Largest<__nv_bfloat16> {
+    uint32_t m = 0xff80ff80u;
+    __device__ __forceinline__ void take(uint4 v) { two(v.x); two(v.y); two(v.z); two(v.w); }
+    __device__ __forceinline__ void two(uint32_t w) {
+        const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&w));
+        m = *reinterpret_cast<const uint32_t*>(&r);
+    }
+    __device__ __forceinline__ float value() const { const float2 f = unpack2<__nv_bfloat16>(m); return fmaxf(f.x, f.y); }
+    static constexpr uint32_t kNone = 0xff80ff80u;
+};
+// a piece of which only the first `n` entries are in the row: -Inf for the others
+template <typename T>
+__device__ __forceinline__ uint4 only_first(uint4 v, int n) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            if (i >= n) w[i] = Largest<T>::kNone;
+        } else {
+            if (2 * i >= n) w[i] = Largest<T>::kNone;
+            else if (2 * i + 1 >= n) w[i] = (w[i] & 0xffffu) | (Largest<T>::kNone & 0xffff0000u);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Registers: a thread holds P pieces of the next row (not AHEAD: of this one, and is done with them when it has the powers) and, for the gradient,
+// this row's powers in fp32.  16 pieces of fp32 leave no room for both.
+template <typename T, int P> constexpr bool kAhead = P * Piece<T>::N + 4 * P <= 96;
+template <typename T, int P, Mode MODE>
+constexpr int kRegisters = (MODE == kPolicy ? P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) : 4 * P) + 32;
+template <typename T, int THREADS, int P, Mode MODE>
+constexpr int kCtas = 65536 / (THREADS * kRegisters<T, P, MODE>) < 2048 / THREADS ? 65536 / (THREADS * kRegisters<T, P, MODE>) : 2048 / THREADS;
+
+template <typename T, int THREADS, int P, Mode MODE, bool ANY>
+__global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P, MODE>)) rows_kernel(const __grid_constant__ RowsArgs g) {
+    constexpr int N = Piece<T>::N, WARPS = THREADS / 32;
+    constexpr bool AHEAD = kAhead<T, P>;
+    __shared__ float2 met[2][kMaxCluster * WARPS];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int cluster = g.cluster;
+    const uint32_t rank = cluster > 1 ? cluster_rank() : 0u;
+    const int64_t stride = gridDim.x / cluster;
+    const int begin = (int)rank * g.chunk;                    // this CTA's columns of a row
+    const int cols = g.vocab - begin < g.chunk ? g.vocab - begin : g.chunk;
+    if (cluster == 1) pdl_trigger();
+    pdl_wait();
+    int64_t row = blockIdx.x / cluster;
+    const T* Z = static_cast<const T*>(g.Z);
+    uint4 raw[P];
+    // a row's chosen token, -1 where the row does not count, and its weight
+    auto look = [&](int64_t r, int64_t& token, float& weight) {
+        token = -1;
+        weight = 0.f;
+        if (r >= g.rows) return;
+        token = chosen(g.y, g.wide, r);
+        weight = MODE == kLogp ? 1.f : (g.weight ? g.weight[r] : g.even_weight);
+        if (weight == 0.f) token = -1;
+    };
+    auto fetch = [&](int64_t r, bool want) {
+        const T* from = Z + r * g.ldz + begin;
+#pragma unroll
+        for (int i = 0; i < P; ++i) raw[i] = load_piece<ANY>(from, (int)(threadIdx.x + i * THREADS) * N, want ? cols : 0, g.span);
+    };
+    int64_t y, next_y;
+    float w, next_w;
+    look(row, y, w);
+    look(row + stride, next_y, next_w);
+    if (AHEAD) fetch(row, y >= 0);
+    double sum_loss = 0., sum_pg = 0., sum_kl = 0., sum_clip = 0.;
+    int turn = 0;
+    for (; row < g.rows; row += stride) {
+        const int64_t next = row + stride;
+        const bool live = y >= 0;                              // (the same in all CTAs of the cluster)
+        if (!AHEAD) fetch(row, live);
+        float zy = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
+        if (live) {
+            zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
+            if (MODE == kPolicy) {
+                old = g.old_logp[row];
+                adv = g.advantage[row];
+                if (g.ref_logp) ref = g.ref_logp[row];
+            }
+        }
+        float top = minus_inf(), sum = 0.f;
+        float e[MODE == kPolicy ? P * N : 1];
+        if (live) {
+            Largest<T> most;
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int c = (int)(threadIdx.x + i * THREADS) * N;
+                if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
+                most.take(raw[i]);
+            }
+            top = most.value() * g.k2;
+            const float base = top == minus_inf() ? 0.f : top;
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float f[N];
+                Piece<T>::split(raw[i], f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    f[j] = exp2_fast(fmaf(f[j], g.k2, -base));
+                    sum += f[j];
+                    if constexpr (MODE == kPolicy) e[i * N + j] = f[j];
+                }
+            }
+        }
+        if (AHEAD) fetch(next, next_y >= 0);
+        float logp = 0.f, lse = 0.f, factor = 0.f, coef = 0.f;
+        if (live) {
+            float2 all = make_float2(top, sum);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                all = joined(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, o), __shfl_xor_sync(0xffffffffu, all.y, o)));
+            // (slots are written again two live rows on, and every thread has passed the barrier between)
+            float2* slots = met[turn & 1];
+            ++turn;
+            if (cluster == 1) {
+                if (lane == 0) slots[warp] = all;
+                __syncthreads();
+            } else {
+                if (lane < cluster) store_at(&slots[(int)rank * WARPS + warp], (uint32_t)lane, all);
+                cluster_meet();
+            }
+            all = make_float2(minus_inf(), 0.f);
+            for (int i = lane; i < cluster * WARPS; i += 32) all = joined(all, slots[i]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                all = joined(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, o), __shfl_xor_sync(0xffffffffu, all.y, o)));
+            const float lg = log2f(all.y);
+            const bool empty = all.x == minus_inf() && all.y == 0.f;   // nothing but -Inf
+            logp = empty ? (y < g.vocab ? minus_inf() : zy) : (fmaf(zy, g.k2, -all.x) - lg) * kLn2;
+            lse = empty ? minus_inf() : (all.x + lg) * kLn2;
+            if (MODE == kPolicy) {
+                const float r = expf(logp - old);
+                const float free = r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
+                const bool clipped = free > held;
+                const float pg = -(clipped ? held : free);
+                float kl = 0.f, slope = clipped ? 0.f : -free;
+                if (g.ref_logp) {
+                    const float d = ref - logp, x = expm1f(d);
+                    kl = x - d;
+                    slope = fmaf(-g.kl_coef, x, slope);
+                }
+                if (rank == 0 && threadIdx.x == 0) {
+                    sum_loss += (double)w * ((double)pg + (double)g.kl_coef * (double)kl);
+                    sum_pg += (double)w * (double)pg;
+                    sum_kl += (double)w * (double)kl;
+                    if (clipped) sum_clip += (double)w;
+                }
+                coef = empty ? 0.f : g.grad_scale * w * slope;
+                factor = empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
+            }
+        }
+        if (rank == 0 && threadIdx.x == 0) {
+            if (g.logp) g.logp[row] = logp;
+            if (MODE == kLogp && g.lse) g.lse[row] = lse;
+            if (MODE == kLogp && g.zeros) g.zeros[row] = 0.f;
+        }
+        if constexpr (MODE == kPolicy) {
+            if (g.dZ) {
+                T* to = static_cast<T*>(g.dZ) + row * g.lddz + begin;
+                const int at = (int)(y - begin);               // the chosen entry, if it is one of this CTA's
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const int c = (int)(threadIdx.x + i * THREADS) * N;
+                    if (c >= cols) continue;
+                    uint64_t out[N / 2];
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j)
+                        out[j] = live ? mul2(pair_of(e[i * N + 2 * j], e[i * N + 2 * j + 1]), pair_of(factor, factor)) : 0ull;
+                    if (live && at >= c && at < c + N) {
+#pragma unroll
+                        for (int j = 0; j < N / 2; ++j)
+                            out[j] = pair_of(pair_lo(out[j]) + (at == c + 2 * j ? coef : 0.f), pair_hi(out[j]) + (at == c + 2 * j + 1 ? coef : 0.f));
+                    }
+                    store_piece(to, c, cols, !ANY || g.dz_vec, out);
+                }
+            }
+        }
+        y = next_y;
+        w = next_w;
+        look(next + stride, next_y, next_w);
+    }
+    if (MODE == kPolicy && rank == 0 && threadIdx.x == 0) {
+        double* to = g.parts + 4 * (blockIdx.x / cluster);
+        to[0] = sum_loss; to[1] = sum_pg; to[2] = sum_kl; to[3] = sum_clip;
+    }
+    if (cluster > 1) cluster_meet();   // no CTA leaves while another may still write to its shared memory
+}
+
+// out[i] = factor * sum over k of parts[k][i], i < WIDTH; one warp, fixed order
+template <int WIDTH>
+__global__ void total_kernel(const double* __restrict__ parts, int64_t count, double factor, float* __restrict__ out) {
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x;
+    double sum[WIDTH] = {};
+    for (int64_t k = lane; k < count; k += 32)
+#pragma unroll
+        for (int i = 0; i < WIDTH; ++i) sum[i] += parts[k * WIDTH + i];
+#pragma unroll
+    for (int i = 0; i < WIDTH; ++i) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        if (lane == 0) out[i] = (float)(factor * sum[i]);
+    }
+}
+
+// ---- the gradient from lse -------------------------------------------------------------------------
+constexpr int kBackThreads = 256, kBackPieces = 4;
+
+struct BackArgs {
+    const void* Z;
+    int64_t ldz;
+    Span span;
+    int64_t rows;
+    int vocab, slices;
+    const void* y;
+    bool wide;
+    float k2, scale;               // scale: of the logits and of the gradient
+    const float *lse, *dlogp;
+    void* dZ;
+    int64_t lddz;
+    bool dz_vec;
+};
+
+// a warp for each slice of 32 * kBackPieces pieces, from the last one back
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_constant__ BackArgs g) {
+    constexpr int N = Piece<T>::N, kSlice = 32 * kBackPieces * N;
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x % 32;
+    const int64_t items = g.rows * g.slices, stride = (int64_t)gridDim.x * (kBackThreads / 32);
+    for (int64_t k = (int64_t)blockIdx.x * (kBackThreads / 32) + threadIdx.x / 32; k < items; k += stride) {
+        const int64_t item = items - 1 - k, row = item / g.slices;
+        const int c0 = (int)(item - row * g.slices) * kSlice + lane * N;
+        const int64_t y = chosen(g.y, g.wide, row);
+        const float d = g.dlogp[row];
+        const float lse = g.lse[row];
+        const bool live = y >= 0 && d != 0.f && lse != minus_inf();
+        const T* from = static_cast<const T*>(g.Z) + row * g.ldz;
+        uint4 raw[kBackPieces];
+#pragma unroll
+        for (int i = 0; i < kBackPieces; ++i) raw[i] = load_piece<ANY>(from, c0 + i * 32 * N, live ? g.vocab : 0, g.span);
+        const float coef = y < g.vocab ? d * g.scale : __int_as_float(0x7fc00000);
+        const float base = -lse * kLog2e;
+        T* to = static_cast<T*>(g.dZ) + row * g.lddz;
+#pragma unroll
+        for (int i = 0; i < kBackPieces; ++i) {
+            const int c = c0 + i * 32 * N;
+            if (c >= g.vocab) continue;
+            float f[N];
+            Piece<T>::split(raw[i], f);
+            uint64_t out[N / 2];
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = live ? coef * ((y == c + j ? 1.f : 0.f) - exp2_fast(fmaf(f[j], g.k2, base))) : 0.f;
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) out[j] = pair_of(f[2 * j], f[2 * j + 1]);
+            store_piece(to, c, g.vocab, !ANY || g.dz_vec, out);
+        }
+    }
+}
+
+// ---- pairs of sequences ----------------------------------------------------------------------------
+constexpr int kPairThreads = 256;
+
+__global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __restrict__ logp, int64_t rows, const int32_t* __restrict__ offsets,
+                                                             const float* __restrict__ ref, int64_t pairs, float beta, float smoothing,
+                                                             float grad, float* __restrict__ margin, float* __restrict__ sums,
+                                                             float* __restrict__ dlogp, double* __restrict__ parts) {
+    __shared__ double sm[2][kPairThreads / 32];
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
+        int64_t at[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int64_t least = i ? at[i - 1] : 0, o = offsets[2 * p + i];
+            at[i] = o < least ? least : (o > rows ? rows : o);
+        }
+        double s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            double x = 0.;
+            for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kPairThreads) x += (double)logp[t];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            if (lane == 0) sm[i][warp] = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = 0.;
+#pragma unroll
+            for (int k = 0; k < kPairThreads / 32; ++k) s[i] += sm[i][k];
+        }
+        const double h = (double)beta * ((s[0] - (double)ref[2 * p]) - (s[1] - (double)ref[2 * p + 1]));
+        const float x = (float)h;
+        // -log sigmoid(x) = max(-x, 0) + log(1 + e^-|x|), and the sigmoids, from one exponential
+        const float u = expf(-fabsf(x)), l = log1pf(u), up = 1.f / (1.f + u), down = u / (1.f + u);
+        const float plus = x >= 0.f ? up : (x < 0.f ? down : x), minus = x >= 0.f ? down : (x < 0.f ? up : x);   // sigmoid(x), sigmoid(-x)
+        if (threadIdx.x == 0) {
+            const float rise = x < 0.f ? -x : 0.f, fall = x > 0.f ? x : 0.f;
+            parts[p] = (double)((1.f - smoothing) * (rise + l) + smoothing * (fall + l));
+            margin[p] = x;
+            sums[2 * p] = (float)s[0];
+            sums[2 * p + 1] = (float)s[1];
+        }
+        if (dlogp) {
+            const float d = grad * (smoothing * plus - (1.f - smoothing) * minus);
+            for (int64_t t = at[0] + threadIdx.x; t < at[1]; t += kPairThreads) dlogp[t] = d;
+            for (int64_t t = at[1] + threadIdx.x; t < at[2]; t += kPairThreads) dlogp[t] = -d;
+        }
+        __syncthreads();
+    }
+}
+
+// ---- shapes ----------------------------------------------------------------------------------------
+// How many CTAs share a row: as many as its entries need registers of; then, while rows are so few that SMs are left over, more, down to
+// kLeastChunk entries each.
+constexpr int kLeastChunk = 2048;
+struct Shape {
+    int cluster, chunk;
+};
+template <typename T>
+Shape shape_of(int64_t rows, int64_t vocab) {
+    constexpr int N = Piece<T>::N;
+    int64_t cluster = ceil_div(vocab, (int64_t)512 * 8 * N);   // eight pieces a thread, the next row's beside them
+    if (cluster > kMaxCluster) cluster = kMaxCluster;          // (fp32: sixteen)
+    while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= kSMs && vocab >= cluster * 2 * kLeastChunk) cluster *= 2;
+    const int64_t chunk = ceil_div(ceil_div(vocab, cluster), (int64_t)N) * N;
+    return Shape{(int)ceil_div(vocab, chunk), (int)chunk};
+}
+// Calls f<THREADS, P>() with the smallest CTA that has room for `chunk` entries.
+template <typename T, typename F>
+detox_status by_chunk(int chunk, F f) {
+    constexpr int N = Piece<T>::N;
+    if (chunk <= 128 * 1 * N) return f.template operator()<128, 1>();
+    if (chunk <= 128 * 4 * N) return f.template operator()<128, 4>();
+    if (chunk <= 256 * 4 * N) return f.template operator()<256, 4>();
+    if (chunk <= 256 * 8 * N) return f.template operator()<256, 8>();
+    if (chunk <= 512 * 8 * N) return f.template operator()<512, 8>();
+    if constexpr (N == 4) {
+        if (chunk <= 512 * 16 * N) return f.template operator()<512, 16>();
+    }
+    return DETOX_ERR_UNSUPPORTED;
+}
+
+template <typename T, Mode MODE, bool ANY>
+struct Rows {
+    const RowsArgs& g;
+    int64_t* clusters;
+    cudaStream_t s;
+    template <int THREADS, int P>
+    detox_status operator()() const {
+        const int64_t most = (int64_t)kSMs * kCtas<T, THREADS, P, MODE> / g.cluster;
+        *clusters = g.rows < most ? g.rows : most;
+        // Clusters that fill the SMs' registers do not overlap with the stream's other kernels, as the gated products' pairs do not.
+        return launch(g.cluster == 1, rows_kernel<T, THREADS, P, MODE, ANY>, (unsigned)(*clusters * g.cluster), THREADS, 0, (unsigned)g.cluster, s, g);
+    }
+};
+template <typename T>
+bool pieces(const void* p, int64_t ld) {
+    return aligned16(p) && ld % Piece<T>::N == 0;
+}
+// clusters: how many parts the policy loss has
+template <typename T, Mode MODE>
+detox_status rows_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
+    const Shape shape = shape_of<T>(g.rows, g.vocab);
+    g.cluster = shape.cluster;
+    g.chunk = shape.chunk;
+    g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
+    g.dz_vec = pieces<T>(g.dZ, g.lddz);
+    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec)) return by_chunk<T>(g.chunk, Rows<T, MODE, false>{g, clusters, s});
+    return by_chunk<T>(g.chunk, Rows<T, MODE, true>{g, clusters, s});
+}
+template <Mode MODE>
+detox_status rows_of(int dtype, const RowsArgs& g, int64_t* clusters, cudaStream_t s) {
+    if (dtype == DETOX_DTYPE_FLOAT) return rows_of<float, MODE>(g, clusters, s);
+    if (dtype == DETOX_DTYPE_HALF) return rows_of<__half, MODE>(g, clusters, s);
+    return rows_of<__nv_bfloat16, MODE>(g, clusters, s);
+}
+
+template <typename T>
+detox_status backward_of(BackArgs g, cudaStream_t s) {
+    g.slices = (int)ceil_div((int64_t)g.vocab, (int64_t)32 * kBackPieces * Piece<T>::N);
+    g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
+    g.dz_vec = pieces<T>(g.dZ, g.lddz);
+    const bool any = !(g.vocab % Piece<T>::N == 0 && g.span.vec && g.dz_vec);
+    const int64_t need = ceil_div(g.rows * g.slices, (int64_t)(kBackThreads / 32)), most = (int64_t)kSMs * 16;
+    return launch_chained(any ? backward_kernel<T, true> : backward_kernel<T, false>, (unsigned)(need < most ? need : most), kBackThreads, 0, 1, s, g);
+}
+
+}  // namespace
+
+detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
+                               float* logp, float* lse, float* zeros, cudaStream_t s) {
+    if (rows == 0) return DETOX_OK;
+    RowsArgs g = {};
+    g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
+    g.y = y; g.wide = index == DETOX_INDEX_INT64;
+    g.k2 = scale * kLog2e;
+    g.logp = logp; g.lse = lse; g.zeros = zeros;
+    int64_t clusters;
+    return rows_of<kLogp>(dtype, g, &clusters, s);
+}
+
+detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
+                                        float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s) {
+    if (rows == 0) return DETOX_OK;
+    BackArgs g = {};
+    g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
+    g.y = y; g.wide = index == DETOX_INDEX_INT64;
+    g.k2 = scale * kLog2e;
+    g.scale = scale;
+    g.lse = lse; g.dlogp = dlogp;
+    g.dZ = dZ; g.lddz = lddz;
+    if (dtype == DETOX_DTYPE_FLOAT) return backward_of<float>(g, s);
+    if (dtype == DETOX_DTYPE_HALF) return backward_of<__half>(g, s);
+    return backward_of<__nv_bfloat16>(g, s);
+}
+
+size_t policy_loss_ws_bytes(int64_t rows) {
+    const int64_t most = (int64_t)kSMs * 16;   // CTAs of 128 threads on an SM
+    return align_up((size_t)(rows < most ? rows : most) * 4 * sizeof(double));
+}
+
+detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float* logp, void* dZ, int64_t lddz, void* ws, cudaStream_t s) {
+    int64_t clusters = 0;
+    double* parts = static_cast<double*>(ws);
+    if (d.rows > 0) {
+        RowsArgs g = {};
+        g.Z = d.Z; g.ldz = d.ldz; g.rows = d.rows; g.vocab = (int)d.vocab;
+        g.y = d.y; g.wide = d.index == DETOX_INDEX_INT64;
+        g.k2 = d.scale * kLog2e;
+        g.logp = logp;
+        g.old_logp = d.old_logp; g.advantage = d.advantage; g.ref_logp = d.ref_logp; g.weight = d.weight;
+        g.low = 1.f - d.clip_low; g.high = 1.f + d.clip_high;
+        g.kl_coef = d.kl_coef;
+        g.even_weight = (float)(1.0 / (double)d.rows);
+        g.grad_scale = d.grad_scale * d.scale;
+        g.dZ = dZ; g.lddz = lddz;
+        g.parts = parts;
+        const detox_status st = rows_of<kPolicy>(d.dtype, g, &clusters, s);
+        if (st != DETOX_OK) return st;
+    }
+    return launch_chained(total_kernel<4>, 1, 32, 0, 1, s, parts, clusters, 1.0, stats);
+}
+
+// lse, logp and its gradient for each row, then a part of the loss for each pair
+size_t preference_loss_ws_bytes(int64_t rows, int64_t pairs) {
+    return 3 * align_up((size_t)rows * sizeof(float)) + align_up((size_t)pairs * sizeof(double));
+}
+
+detox_status launch_preference_loss(const detox_preference_desc& d, float* loss, float* margin, float* sums, void* dZ, int64_t lddz, void* ws,
+                                    cudaStream_t s) {
+    const size_t vector = align_up((size_t)d.rows * sizeof(float));
+    char* at = static_cast<char*>(ws);
+    float *logp = reinterpret_cast<float*>(at), *lse = reinterpret_cast<float*>(at + vector), *dlogp = reinterpret_cast<float*>(at + 2 * vector);
+    double* parts = reinterpret_cast<double*>(at + 3 * vector);
+    detox_status st = launch_token_logp(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, logp, lse, dZ ? dlogp : nullptr, s);
+    if (st != DETOX_OK) return st;
+    if (d.pairs > 0) {
+        const int64_t most = (int64_t)kSMs * 8;
+        const float grad = (float)((double)d.grad_scale * (double)d.beta / (double)d.pairs);
+        st = launch_chained(pairs_kernel, (unsigned)(d.pairs < most ? d.pairs : most), kPairThreads, 0, 1, s, logp, d.rows, d.offsets, d.ref,
+                            d.pairs, d.beta, d.smoothing, grad, margin, sums, dZ && d.rows ? dlogp : nullptr, parts);
+        if (st != DETOX_OK) return st;
+    }
+    st = launch_chained(total_kernel<1>, 1, 32, 0, 1, s, parts, d.pairs, d.pairs > 0 ? 1.0 / (double)d.pairs : 0.0, loss);
+    if (st != DETOX_OK || !dZ) return st;
+    return launch_token_logp_backward(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, lse, dlogp, dZ, lddz, s);
+}
+
+}  // namespace detox

@@ -1,4 +1,4 @@
-// Shared by the worker-side operators (rmsnorm.cu, checkpoint.cu, gated.cu): element types, the 8-bit form of kept
+// Shared by the worker-side operators and the optimizer (rmsnorm.cu, checkpoint.cu, gated.cu, embedding.cu, token_loss.cu, adamw.cu): element types, the 8-bit form of kept
 // activations, and the launcher declarations (internal).
 #pragma once
 
@@ -307,6 +307,28 @@ size_t rmsnorm_backward_ws_bytes(int64_t rows, int64_t cols);
 detox_status launch_rmsnorm_backward(int dtype, const void* dY, int64_t lddy, const void* dS, int64_t ldds, const void* S,
                                      int64_t lds, const void* w, const float* rstd, int64_t rows, int64_t cols, void* dX,
                                      int64_t lddx, float* dw, void* ws, cudaStream_t s);
+
+// embedding.cu
+detox_status launch_embedding(int dtype, const void* W, int64_t ldw, int64_t vocab, int64_t cols, int index, const void* tokens,
+                              int64_t rows, float scale, void* Y, int64_t ldy, cudaStream_t s);
+size_t embedding_backward_ws_bytes(int64_t rows, int64_t vocab, int64_t cols);
+detox_status launch_embedding_backward(int dtype, const void* dY, int64_t lddy, int index, const void* tokens, int64_t rows, int64_t vocab,
+                                       int64_t cols, float scale, void* dW, int64_t lddw, int dw_dtype, bool add, void* ws, cudaStream_t s);
+
+// token_loss.cu
+// zeros: a vector of `rows` entries that is cleared on the way; or NULL
+detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
+                               float* logp, float* lse, float* zeros, cudaStream_t s);
+detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
+                                        float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s);
+size_t policy_loss_ws_bytes(int64_t rows);
+detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float* logp, void* dZ, int64_t lddz, void* ws, cudaStream_t s);
+size_t preference_loss_ws_bytes(int64_t rows, int64_t pairs);
+detox_status launch_preference_loss(const detox_preference_desc& d, float* loss, float* margin, float* sums, void* dZ, int64_t lddz, void* ws,
+                                    cudaStream_t s);
+
+// adamw.cu
+detox_status launch_adamw(const detox_adamw_desc& d, const detox_adamw_tensor* tensors, int64_t count, cudaStream_t s);
 
 // gated.cu
 size_t gated_ws_bytes(const detox_gated_desc& g);

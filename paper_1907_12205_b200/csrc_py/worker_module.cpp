@@ -1,10 +1,12 @@
-// Python entry of the worker-side operators: checks the tensors, makes the outputs that the caller did not pass, and calls
+// Python entry of the worker-side operators and the optimizer's step: checks the tensors, makes the outputs that the caller did not pass, and calls
 // the C functions of include/detox.h.
 //
 // A worker's small steps are bound by what a call costs on the host, and most of that is not the launch (2.3 us): from
 // Python, each output tensor took 2 us and each tensor's checks 0.6.  Here they take a fraction of that: a norm of one row with
 // all its outputs 20.8 -> 8.8 us, a step of 500 tokens 63 -> 39 us, and with outputs made past the dispatcher 7.7 and 38 today.
 #include <Python.h>
+
+#include <vector>
 
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
@@ -432,6 +434,282 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- embedding, losses over logits, the optimizer's step ----
+
+double number(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised{};
+    return v;
+}
+float* floats(const at::Tensor& t, const char* what, int64_t n) { return static_cast<float*>(vector_of(t, what, at::kFloat, n)); }
+float* optional_floats(PyObject* o, const char* what, int64_t n) {
+    const at::Tensor* t = optional_tensor(o, what);
+    return t ? floats(*t, what, n) : nullptr;
+}
+
+// Token numbers: a contiguous vector of int32 or int64.
+struct Index {
+    const void* p;
+    int code;
+    int64_t n;
+};
+Index index_of(const at::Tensor& t, const char* what) {
+    const at::ScalarType type = t.scalar_type();
+    if (!t.is_cuda() || (type != at::kInt && type != at::kLong) || t.dim() != 1 || !t.is_contiguous())
+        raise(PyExc_TypeError, "%s: expected a contiguous CUDA vector of int32 or int64", what);
+    on_device(t, what);
+    return Index{t.data_ptr(), type == at::kInt ? DETOX_INDEX_INT32 : DETOX_INDEX_INT64, t.size(0)};
+}
+Index index_of(const at::Tensor& t, const char* what, int64_t n) {
+    const Index i = index_of(t, what);
+    if (i.n != n) raise(PyExc_ValueError, "%s: expected %lld entries, got %lld", what, (long long)n, (long long)i.n);
+    return i;
+}
+
+// (tokens, w, scale, out, stream)
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("embedding", n, 5, [&] {
+        const Rows w = rows_of(tensor(a[1], "w"), "w");
+        const at::ScalarType type = w.t.scalar_type();
+        const int code = code_of(type, "w");
+        const Index tokens = index_of(tensor(a[0], "tokens"), "tokens");
+        const float scale = (float)number(a[2]);
+        const OnStream on(a[4], w.t);
+        Rows y;
+        if (const at::Tensor* t = optional_tensor(a[3], "out")) y = rows_of(*t, "out", type, tokens.n, w.cols);
+        else y = new_rows(tokens.n, w.cols, type, w.t);
+        check(detox_embedding(code, w.p, w.ld, w.rows, w.cols, tokens.code, tokens.p, tokens.n, scale, y.p, y.ld, on.s), "detox_embedding");
+        return wrap(y.t);
+    });
+}
+
+// (dy, tokens, vocab, scale, dw, dw dtype code or -1, accumulate, ws, stream)
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("embedding_backward", n, 9, [&] {
+        const Rows dy = rows_of(tensor(a[0], "dy"), "dy");
+        const at::ScalarType type = dy.t.scalar_type();
+        const int code = code_of(type, "dy");
+        const Index tokens = index_of(tensor(a[1], "tokens"), "tokens", dy.rows);
+        const int64_t vocab = integer(a[2]), want = integer(a[5]);
+        if (vocab < 1) raise(PyExc_ValueError, "vocab: expected a positive number, got %lld", (long long)vocab);
+        const float scale = (float)number(a[3]);
+        const bool add = truth(a[6]);
+        const OnStream on(a[8], dy.t);
+        Rows dw;
+        if (const at::Tensor* t = optional_tensor(a[4], "dw")) {
+            dw = rows_of(*t, "dw", want >= 0 ? type_of((int)want) : t->scalar_type(), vocab, dy.cols);
+        } else {
+            if (add) raise(PyExc_ValueError, "accumulate: there is no dw to add to");
+            dw = new_rows(vocab, dy.cols, want >= 0 ? type_of((int)want) : type, dy.t);
+        }
+        const Workspace ws = workspace(a[7], detox_embedding_backward_workspace_bytes(dy.rows, vocab, dy.cols), dy.t);
+        check(detox_embedding_backward(code, dy.p, dy.ld, tokens.code, tokens.p, dy.rows, vocab, dy.cols, scale, dw.p, dw.ld,
+                                       code_of(dw.t.scalar_type(), "dw"), add, ws.p, ws.bytes, on.s),
+              "detox_embedding_backward");
+        return wrap(dw.t);
+    });
+}
+
+// Logits and the tokens chosen there.
+struct Logits {
+    Rows z;
+    Index y;
+    int code;
+    float scale;
+};
+Logits logits_of(PyObject* z, PyObject* y, PyObject* scale) {
+    Logits l;
+    l.z = rows_of(tensor(z, "z"), "z");
+    l.code = code_of(l.z.t.scalar_type(), "z");
+    l.y = index_of(tensor(y, "y"), "y", l.z.rows);
+    l.scale = (float)number(scale);
+    return l;
+}
+// the gradient of logits: the caller's, or a new one where it is wanted
+Rows dz_of(PyObject* given, bool want, const Logits& l) {
+    if (const at::Tensor* t = optional_tensor(given, "dz")) return rows_of(*t, "dz", l.z.t.scalar_type(), l.z.rows, l.z.cols);
+    return want ? new_rows(l.z.rows, l.z.cols, l.z.t.scalar_type(), l.z.t) : Rows{};
+}
+
+// (z, y, scale, stream) -> (logp, lse)
+PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("token_logp", n, 4, [&] {
+        const Logits l = logits_of(a[0], a[1], a[2]);
+        const OnStream on(a[3], l.z.t);
+        const at::Tensor logp = new_vector(l.z.rows, at::kFloat, l.z.t), lse = new_vector(l.z.rows, at::kFloat, l.z.t);
+        check(detox_token_logp(l.code, l.z.p, l.z.ld, l.z.rows, l.z.cols, l.y.code, l.y.p, l.scale, static_cast<float*>(logp.data_ptr()),
+                               static_cast<float*>(lse.data_ptr()), on.s),
+              "detox_token_logp");
+        return wrap_all(logp, lse);
+    });
+}
+
+// (dlogp, z, y, lse, scale, dz, stream)
+PyObject* token_logp_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("token_logp_backward", n, 7, [&] {
+        const Logits l = logits_of(a[1], a[2], a[4]);
+        const float *dlogp = floats(tensor(a[0], "dlogp"), "dlogp", l.z.rows), *lse = floats(tensor(a[3], "lse"), "lse", l.z.rows);
+        const OnStream on(a[6], l.z.t);
+        const Rows dz = dz_of(a[5], true, l);
+        check(detox_token_logp_backward(l.code, l.z.p, l.z.ld, l.z.rows, l.z.cols, l.y.code, l.y.p, l.scale, lse, dlogp, dz.p, dz.ld, on.s),
+              "detox_token_logp_backward");
+        return wrap(dz.t);
+    });
+}
+
+// (z, y, old, advantage, ref, weight, clip_low, clip_high, kl_coef, scale, want_grad, grad_scale, dz, ws, stream) -> (stats, logp, dz)
+PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("policy_loss", n, 15, [&] {
+        const Logits l = logits_of(a[0], a[1], a[9]);
+        detox_policy_desc d{};
+        d.dtype = l.code; d.index = l.y.code;
+        d.rows = l.z.rows; d.vocab = l.z.cols;
+        d.Z = l.z.p; d.ldz = l.z.ld;
+        d.y = l.y.p;
+        d.old_logp = floats(tensor(a[2], "old_logp"), "old_logp", d.rows);
+        d.advantage = floats(tensor(a[3], "advantage"), "advantage", d.rows);
+        d.ref_logp = optional_floats(a[4], "ref_logp", d.rows);
+        d.weight = optional_floats(a[5], "weight", d.rows);
+        d.clip_low = (float)number(a[6]); d.clip_high = (float)number(a[7]); d.kl_coef = (float)number(a[8]);
+        d.scale = l.scale; d.grad_scale = (float)number(a[11]);
+        const bool want = truth(a[10]);
+        if (!want && a[12] != Py_None) raise(PyExc_ValueError, "dz: no gradient is wanted");
+        const OnStream on(a[14], l.z.t);
+        const at::Tensor stats = new_vector(4, at::kFloat, l.z.t), logp = new_vector(d.rows, at::kFloat, l.z.t);
+        const Rows dz = dz_of(a[12], want, l);
+        const Workspace ws = workspace(a[13], detox_policy_loss_workspace_bytes(d.rows), l.z.t);
+        check(detox_policy_loss(&d, static_cast<float*>(stats.data_ptr()), static_cast<float*>(logp.data_ptr()), dz.p, dz.ld, ws.p, ws.bytes, on.s),
+              "detox_policy_loss");
+        return wrap_all(stats, logp, dz.t);
+    });
+}
+
+// (z, y, offsets, ref, beta, smoothing, scale, want_grad, grad_scale, dz, ws, stream) -> (loss, margin, sums, dz)
+PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("preference_loss", n, 12, [&] {
+        const Logits l = logits_of(a[0], a[1], a[6]);
+        detox_preference_desc d{};
+        d.dtype = l.code; d.index = l.y.code;
+        d.rows = l.z.rows; d.vocab = l.z.cols;
+        d.Z = l.z.p; d.ldz = l.z.ld;
+        d.y = l.y.p;
+        const at::Tensor &offsets = tensor(a[2], "offsets"), &ref = tensor(a[3], "ref");
+        if (ref.dim() != 1 || ref.size(0) % 2) raise(PyExc_ValueError, "ref: expected a vector with two entries for each pair");
+        d.pairs = ref.size(0) / 2;
+        d.ref = floats(ref, "ref", 2 * d.pairs);
+        d.offsets = static_cast<const int32_t*>(vector_of(offsets, "offsets", at::kInt, 2 * d.pairs + 1));
+        d.beta = (float)number(a[4]); d.smoothing = (float)number(a[5]);
+        d.scale = l.scale; d.grad_scale = (float)number(a[8]);
+        const bool want = truth(a[7]);
+        if (!want && a[9] != Py_None) raise(PyExc_ValueError, "dz: no gradient is wanted");
+        const OnStream on(a[11], l.z.t);
+        const at::Tensor loss = new_vector(1, at::kFloat, l.z.t), margin = new_vector(d.pairs, at::kFloat, l.z.t),
+                         sums = new_vector(2 * d.pairs, at::kFloat, l.z.t);
+        const Rows dz = dz_of(a[9], want, l);
+        const Workspace ws = workspace(a[10], detox_preference_loss_workspace_bytes(d.rows, d.pairs), l.z.t);
+        check(detox_preference_loss(&d, static_cast<float*>(loss.data_ptr()), static_cast<float*>(margin.data_ptr()),
+                                    static_cast<float*>(sums.data_ptr()), dz.p, dz.ld, ws.p, ws.bytes, on.s),
+              "detox_preference_loss");
+        return wrap_all(loss, margin, sums, dz.t);
+    });
+}
+
+// A sequence of `n` objects (any number with n < 0).
+struct Items {
+    PyObject* fast;
+    Items(PyObject* o, const char* what, Py_ssize_t n) : fast(PySequence_Fast(o, what)) {
+        if (!fast) throw Raised{};
+        if (n >= 0 && size() != n) {
+            const Py_ssize_t got = size();
+            Py_DECREF(fast);
+            raise(PyExc_ValueError, "%s: expected %zd of them, got %zd", what, n, got);
+        }
+    }
+    ~Items() { Py_DECREF(fast); }
+    Items(const Items&) = delete;
+    Items& operator=(const Items&) = delete;
+    Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
+    PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
+};
+// A tensor as the vector of its entries.
+void* entries_of(const at::Tensor& t, const char* what, int64_t n) {
+    if (!t.is_contiguous()) raise(PyExc_ValueError, "%s: expected contiguous tensors", what);
+    on_device(t, what);
+    if (t.numel() != n) raise(PyExc_ValueError, "%s: expected a tensor of %lld entries, got one of %lld", what, (long long)n, (long long)t.numel());
+    return t.data_ptr();
+}
+void* entries_of(PyObject* o, const char* what, int64_t n, at::ScalarType type) {
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != type) raise(PyExc_TypeError, "%s: expected %s, got %s", what, c10::toString(type), c10::toString(t.scalar_type()));
+    return entries_of(t, what, n);
+}
+// one entry of `type` on the GPU, or a number on the host
+const void* scalar_of(PyObject* o, const char* what, at::ScalarType type) {
+    if (!THPVariable_Check(o)) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    if (!t.is_cuda() || t.scalar_type() != type || t.numel() != 1) raise(PyExc_TypeError, "%s: expected a number, or a CUDA tensor of one %s", what, c10::toString(type));
+    on_device(t, what);
+    return t.data_ptr();
+}
+
+// (params, grads, m, v, step, lr, beta1, beta2, eps, weight decays, masters, grad_scale, seed, stream)
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("adamw", n, 14, [&]() -> PyObject* {
+        const Items params(a[0], "params", -1), grads(a[1], "grads", params.size()), ms(a[2], "m", params.size()), vs(a[3], "v", params.size());
+        const bool many_decays = !PyFloat_Check(a[9]) && !PyLong_Check(a[9]);
+        const Items decays(many_decays ? a[9] : a[0], "weight_decay", params.size());
+        const Items masters(a[10] == Py_None ? a[0] : a[10], "masters", params.size());
+        const double decay = many_decays ? 0.0 : number(a[9]);
+        std::vector<detox_adamw_tensor> of((size_t)params.size());
+        detox_adamw_desc d{};
+        d.bits = 32;
+        at::Tensor like;
+        for (Py_ssize_t i = 0; i < params.size(); ++i) {
+            detox_adamw_tensor& t = of[(size_t)i];
+            const at::Tensor &p = tensor(params[i], "params"), &g = tensor(grads[i], "grads");
+            if (!p.is_cuda() || !g.is_cuda()) raise(PyExc_TypeError, "params, grads: expected CUDA tensors");
+            t.n = p.numel();
+            t.p_dtype = code_of(p.scalar_type(), "params");
+            t.g_dtype = code_of(g.scalar_type(), "grads");
+            t.P = entries_of(p, "params", t.n);
+            t.G = entries_of(g, "grads", t.n);
+            if (a[10] != Py_None && masters[i] != Py_None) t.master = static_cast<float*>(entries_of(masters[i], "masters", t.n, at::kFloat));
+            const bool eight = PyTuple_Check(ms[i]) || PyList_Check(ms[i]);
+            if (i == 0) d.bits = eight ? 8 : 32;
+            if (eight != (d.bits == 8)) raise(PyExc_TypeError, "m, v: states of all tensors in 32 bits or all in 8");
+            if (eight) {
+                const Items m(ms[i], "a state in 8 bits: values and scales", 2), v(vs[i], "a state in 8 bits: values and scales", 2);
+                t.M = entries_of(m[0], "m", t.n, kValues);
+                t.ME = static_cast<uint8_t*>(entries_of(m[1], "m scales", blocks(t.n), kScales));
+                t.V = entries_of(v[0], "v", t.n, kValues);
+                t.VE = static_cast<uint8_t*>(entries_of(v[1], "v scales", blocks(t.n), kScales));
+            } else {
+                t.M = entries_of(ms[i], "m", t.n, at::kFloat);
+                t.V = entries_of(vs[i], "v", t.n, at::kFloat);
+            }
+            t.weight_decay = (float)(many_decays ? number(decays[i]) : decay);
+            t.key = (uint32_t)i;
+            if (!like.defined()) like = p;
+        }
+        d.step_dev = static_cast<const int64_t*>(scalar_of(a[4], "step", at::kLong));
+        if (!d.step_dev) d.step = integer(a[4]);
+        d.lr_dev = static_cast<const float*>(scalar_of(a[5], "lr", at::kFloat));
+        if (!d.lr_dev) d.lr = number(a[5]);
+        d.beta1 = number(a[6]); d.beta2 = number(a[7]); d.eps = number(a[8]);
+        d.grad_scale = (float)number(a[11]);
+        const int64_t seed = integer(a[12]);
+        if (seed < 0 || seed > (int64_t)UINT32_MAX) raise(PyExc_ValueError, "seed: expected 0 to 2^32 - 1");
+        d.seed = (uint32_t)seed;
+        if (!like.defined()) {
+            check(detox_adamw(&d, nullptr, 0, nullptr), "detox_adamw");
+            Py_RETURN_NONE;
+        }
+        const OnStream on(a[13], like);
+        check(detox_adamw(&d, of.data(), (int64_t)of.size(), on.s), "detox_adamw");
+        Py_RETURN_NONE;
+    });
+}
+
 PyObject* set_error(PyObject*, PyObject* type) {
     Py_INCREF(type);
     Py_XDECREF(g_error);
@@ -443,7 +721,8 @@ PyObject* set_error(PyObject*, PyObject* type) {
     { #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {
     DETOX_METHOD(checkpoint_pack), DETOX_METHOD(checkpoint_unpack), DETOX_METHOD(rmsnorm), DETOX_METHOD(rmsnorm_backward),
-    DETOX_METHOD(gated_workspace_bytes), DETOX_METHOD(gated), DETOX_METHOD(gated_backward),
+    DETOX_METHOD(gated_workspace_bytes), DETOX_METHOD(gated), DETOX_METHOD(gated_backward), DETOX_METHOD(embedding), DETOX_METHOD(embedding_backward), DETOX_METHOD(token_logp),
+    DETOX_METHOD(token_logp_backward), DETOX_METHOD(policy_loss), DETOX_METHOD(preference_loss), DETOX_METHOD(adamw),
     {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_worker", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
