@@ -4,8 +4,7 @@
 //
 // Bound by HBM: every buffer is read once and written once (fp32 weights and states: 28 bytes an entry; bf16 weights, fp32 masters and
 // gradients, 8-bit states: 18).  The tensors' pointers travel as kernel parameters, so a step is one launch for each few hundred of them,
-// with nothing to copy and nothing to set up, and a captured one keeps them.  A warp takes 4 blocks of 128 entries at a time, 4 entries a lane and
-// block, so that a block's scale is one warp-wide reduction and every access of a warp is contiguous: 16 bytes a lane in fp32, and where a buffer is not aligned for
+// with nothing to copy and nothing to set up, and a captured one keeps them; tensors of different types take a launch for each kind.  A CTA takes a few thousand entries at a time, a warp 128 of them, 4 a lane, so that a block's scale is one warp-wide reduction and every access of a warp is contiguous: 16 bytes a lane in fp32, and where a buffer is not aligned for
 // that, single entries dealt round the lanes.
 //
 // 8 bits: m and sqrt(v) as e4m3 numbers with a power-of-two scale for each block.  Of v the root is kept, since its range is half as
@@ -20,8 +19,11 @@ namespace detox {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlocks = 4;                       // blocks of 128 entries that a warp has in flight
-constexpr int kUnit = kBlocks * kKeepBlock;
+// Blocks of 128 entries that a warp has in flight, and CTAs of an SM: what 64 Ki registers allow
+template <bool EIGHT> constexpr int kBlocks = EIGHT ? 2 : 2;
+template <bool EIGHT> constexpr int kCtas = EIGHT ? 4 : 4;
+template <bool EIGHT> constexpr int kUnit = kBlocks<EIGHT> * kKeepBlock * (kThreads / 32);   // entries that a CTA takes at a time
+constexpr int kKinds = 3 * 3 * 2;                // types of weights and gradients, with a master copy or without
 
 struct Tensor {
     void* P;
@@ -34,7 +36,7 @@ struct Tensor {
     int64_t n;
     float weight_decay;
     uint32_t key;
-    uint8_t p_dtype, g_dtype, vec;               // vec: every buffer is aligned for a lane's 4 entries
+    bool vec;                                    // every buffer is aligned for a lane's 4 entries
 };
 struct Numbers {
     float lr, beta1, beta2, rest1, rest2, eps, grad_scale;   // rest: 1 - beta
@@ -63,109 +65,225 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// 4 entries of a lane: contiguous ones (vec), or lane, lane + 32, ... of the block, where there are so many
-template <typename T>
-__device__ __forceinline__ void load4(const T* from, bool vec, int lane, int64_t left, float (&f)[4]) {
-    if (vec) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 x = ld_stream_f4(reinterpret_cast<const float*>(from) + 4 * lane);
-            f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
-        } else {
-            const uint2 x = __ldcs(reinterpret_cast<const uint2*>(from + 4 * lane));
-            const float2 a = unpack2<T>(x.x), b = unpack2<T>(x.y);
-            f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
-        }
-    } else {
+// The root and the inverse to a unit or so, an instruction each (sqrtf and a division cost some eight an entry).  Numbers below 2^-126 count as 0: as v they
+// are squares that fp32 has lost most bits of already.
+__device__ __forceinline__ float root_of(float x) {
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float inverse_of(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 4 entries of a lane: contiguous ones (VEC), or lane, lane + 32, ... of the block, where there are so many
+template <bool VEC, typename T>
+__device__ __forceinline__ void load4(const T* from, int lane, int left, float (&f)[4]) {
+    if constexpr (!VEC) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = 32 * j + lane < left ? to_f32(from[32 * j + lane]) : 0.f;
+    } else if constexpr (sizeof(T) == 4) {
+        const float4 x = ld_stream_f4(reinterpret_cast<const float*>(from) + 4 * lane);
+        f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+    } else {
+        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(from + 4 * lane));
+        const float2 a = unpack2<T>(x.x), b = unpack2<T>(x.y);
+        f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
     }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T* to, bool vec, int lane, int64_t left, const float (&f)[4]) {
-    if (vec) {
-        if constexpr (sizeof(T) == 4) st_stream_f4(reinterpret_cast<float*>(to) + 4 * lane, make_float4(f[0], f[1], f[2], f[3]));
-        else __stcs(reinterpret_cast<uint2*>(to + 4 * lane), make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])));
-    } else {
+template <bool VEC, typename T>
+__device__ __forceinline__ void store4(T* to, int lane, int left, const float (&f)[4]) {
+    if constexpr (!VEC) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (32 * j + lane < left) to[32 * j + lane] = from_f32<T>(f[j]);
+    } else if constexpr (sizeof(T) == 4) {
+        st_stream_f4(reinterpret_cast<float*>(to) + 4 * lane, make_float4(f[0], f[1], f[2], f[3]));
+    } else {
+        __stcs(reinterpret_cast<uint2*>(to + 4 * lane), make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])));
     }
-}
-__device__ __forceinline__ void load4(const void* from, int dtype, int64_t at, bool vec, int lane, int64_t left, float (&f)[4]) {
-    if (dtype == DETOX_DTYPE_FLOAT) load4(static_cast<const float*>(from) + at, vec, lane, left, f);
-    else if (dtype == DETOX_DTYPE_HALF) load4(static_cast<const __half*>(from) + at, vec, lane, left, f);
-    else load4(static_cast<const __nv_bfloat16*>(from) + at, vec, lane, left, f);
-}
-__device__ __forceinline__ void store4(void* to, int dtype, int64_t at, bool vec, int lane, int64_t left, const float (&f)[4]) {
-    if (dtype == DETOX_DTYPE_FLOAT) store4(static_cast<float*>(to) + at, vec, lane, left, f);
-    else if (dtype == DETOX_DTYPE_HALF) store4(static_cast<__half*>(to) + at, vec, lane, left, f);
-    else store4(static_cast<__nv_bfloat16*>(to) + at, vec, lane, left, f);
 }
 // 4 bytes of a lane, as one word
-__device__ __forceinline__ uint32_t load_bytes(const uint8_t* from, bool vec, int lane, int64_t left) {
-    if (vec) return __ldcs(reinterpret_cast<const unsigned int*>(from) + lane);
+template <bool VEC>
+__device__ __forceinline__ uint32_t load_bytes(const uint8_t* from, int lane, int left) {
     uint32_t q = 0u;
+    if constexpr (VEC) {
+        q = __ldcs(reinterpret_cast<const unsigned int*>(from) + lane);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (32 * j + lane < left) q |= (uint32_t)from[32 * j + lane] << (8 * j);
+        for (int j = 0; j < 4; ++j)
+            if (32 * j + lane < left) q |= (uint32_t)from[32 * j + lane] << (8 * j);
+    }
     return q;
 }
-__device__ __forceinline__ void store_bytes(uint8_t* to, bool vec, int lane, int64_t left, uint32_t q) {
-    if (vec) {
+template <bool VEC>
+__device__ __forceinline__ void store_bytes(uint8_t* to, int lane, int left, uint32_t q) {
+    if constexpr (VEC) {
         __stcs(reinterpret_cast<unsigned int*>(to) + lane, q);
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (32 * j + lane < left) to[32 * j + lane] = (uint8_t)(q >> (8 * j));
+        for (int j = 0; j < 4; ++j)
+            if (32 * j + lane < left) to[32 * j + lane] = (uint8_t)(q >> (8 * j));
+    }
 }
 
 // The 8-bit form of a block, 4 entries a lane, rounded at random with `bits` (16 of them an entry).  POSITIVE: entries > 0 stay so.
 // Inf and NaN become NaN and do not count for the scale.
+//
+// e4m3 keeps 3 of the 23 bits behind an fp32 number's first one, so the random bits are added to the number's own above the 4th lowest, and
+// the lowest 20 cut off.  Below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5: such an entry is lifted by 2^-6 for it.  Blocks
+// without such entries (most: they are 2^-15 of the block's largest) and with finite ones only need none of that.
 template <bool POSITIVE>
 __device__ __forceinline__ uint32_t keep_at_random(const float (&x)[4], const uint32_t (&bits)[4], uint32_t* q) {
-    uint32_t top = 0u;
+    uint32_t a[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t a = __float_as_uint(x[j]) & 0x7fffffffu;
-        if (a < 0x7f800000u && a > top) top = a;
+    for (int j = 0; j < 4; ++j) a[j] = POSITIVE ? __float_as_uint(x[j]) : __float_as_uint(x[j]) & 0x7fffffffu;   // (a root of NaN has no sign)
+    uint32_t top = __reduce_max_sync(0xffffffffu, max(max(a[0], a[1]), max(a[2], a[3])));
+    const bool finite = top < 0x7f800000u;
+    if (!finite) {
+        top = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (a[j] < 0x7f800000u) top = max(top, a[j]);
+        top = __reduce_max_sync(0xffffffffu, top);
     }
-    const uint32_t e = keep_exponent(__uint_as_float(__reduce_max_sync(0xffffffffu, top)));
+    const uint32_t e = keep_exponent(__uint_as_float(top));
     const float inverse = keep_inverse(e);
+    const uint32_t least = __reduce_min_sync(0xffffffffu, min(min(a[0], a[1]), min(a[2], a[3])));
     float r[4];
+    if (finite && __uint_as_float(least) * inverse >= 0.015625f) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float a = fabsf(x[j]) * inverse;           // at most 448: e4m3 keeps 3 of fp32's 23 bits behind the first
-        const float lift = a < 0.015625f ? 0.015625f : 0.f;   // below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5
-        const uint32_t b = (__float_as_uint(a + lift) + (bits[j] << 4)) & 0xfff00000u;
-        float k = __uint_as_float(b) - lift;
-        if (POSITIVE && a > 0.f && k == 0.f) k = 0.001953125f;
-        r[j] = a <= 448.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);
+        for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(x[j] * inverse) + (bits[j] << 4)) & 0xfff00000u);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float v = fabsf(x[j]) * inverse;
+            const float lift = v < 0.015625f ? 0.015625f : 0.f;
+            float k = __uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift;
+            if (POSITIVE && v > 0.f && k == 0.f) k = 0.001953125f;
+            r[j] = v <= 448.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);
+        }
     }
     *q = keep4(r[0], r[1], r[2], r[3]);
     return e;
 }
 
-template <bool EIGHT, int CAP>
-__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Numbers number) {
+struct Now {
+    float lr, c1, root_c2;
+    uint32_t seed;                               // of the tensor's random bits
+};
+
+// A unit of tensor t from entry `at` on.  PT, GT: of the weights and the gradient
+template <bool EIGHT, bool VEC, typename PT, typename GT, bool MASTER>
+__device__ __forceinline__ void step_unit(const Tensor& t, int64_t at, const Numbers& number, const Now& now) {
+    constexpr int B = kBlocks<EIGHT>, kStep = kKeepBlock * (kThreads / 32);
+    const int lane = threadIdx.x % 32, first = threadIdx.x / 32 * kKeepBlock;   // this warp's blocks start at at + first + b kStep
+    const GT* G = static_cast<const GT*>(t.G) + at;
+    PT* P = static_cast<PT*>(t.P) + at;
+    float* master = t.master + at;
+    const int rest = t.n - at < kUnit<EIGHT> ? (int)(t.n - at) : kUnit<EIGHT>;
+    float g[B][4], p[B][4];
+    float m32[EIGHT ? 1 : B][4], v32[EIGHT ? 1 : B][4];
+    uint32_t mq[B], vq[B];
+    float ms[B], vs[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const int i = first + b * kStep;
+        const int left = rest - i;
+        if (!VEC && left <= 0) continue;
+        load4<VEC>(G + i, lane, left, g[b]);
+        if constexpr (MASTER) load4<VEC>(master + i, lane, left, p[b]);
+        else load4<VEC>(P + i, lane, left, p[b]);
+        if constexpr (EIGHT) {
+            mq[b] = load_bytes<VEC>(static_cast<const uint8_t*>(t.M) + at + i, lane, left);
+            vq[b] = load_bytes<VEC>(static_cast<const uint8_t*>(t.V) + at + i, lane, left);
+            ms[b] = keep_scale_of_byte(t.ME[(at + i) / kKeepBlock]);
+            vs[b] = keep_scale_of_byte(t.VE[(at + i) / kKeepBlock]);
+        } else {
+            load4<VEC>(static_cast<const float*>(t.M) + at + i, lane, left, m32[b]);
+            load4<VEC>(static_cast<const float*>(t.V) + at + i, lane, left, v32[b]);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const int i = first + b * kStep;
+        const int left = rest - i;
+        if (!VEC && left <= 0) continue;
+        float m[4], v[4], root[4];
+        if constexpr (EIGHT) {
+            taken4(mq[b], m);
+            taken4(vq[b], v);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (EIGHT) {
+                m[j] *= ms[b];
+                v[j] *= vs[b];
+                v[j] *= v[j];
+            } else {
+                m[j] = m32[b][j];
+                v[j] = v32[b][j];
+            }
+            const float x = g[b][j] * number.grad_scale;
+            m[j] = fmaf(number.beta1, m[j], number.rest1 * x);
+            v[j] = fmaf(number.beta2, v[j], number.rest2 * (x * x));
+            root[j] = root_of(v[j]);
+            const float direction = m[j] * now.c1 * inverse_of(fmaf(root[j], now.root_c2, number.eps));
+            p[b][j] = fmaf(-now.lr, fmaf(t.weight_decay, p[b][j], direction), p[b][j]);
+        }
+        if constexpr (MASTER) store4<VEC>(master + i, lane, left, p[b]);
+        store4<VEC>(P + i, lane, left, p[b]);
+        if constexpr (EIGHT) {
+            uint32_t rm[4], rv[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t h = mix(now.seed ^ ((uint32_t)at + (uint32_t)(i + (VEC ? 4 * lane + j : 32 * j + lane))));
+                rm[j] = h & 0xffffu;
+                rv[j] = h >> 16;
+            }
+            uint32_t q;
+            const uint32_t me = keep_at_random<false>(m, rm, &q);
+            store_bytes<VEC>(static_cast<uint8_t*>(t.M) + at + i, lane, left, q);
+            const uint32_t ve = keep_at_random<true>(root, rv, &q);
+            store_bytes<VEC>(static_cast<uint8_t*>(t.V) + at + i, lane, left, q);
+            if (lane == 0) {
+                t.ME[(at + i) / kKeepBlock] = (uint8_t)me;
+                t.VE[(at + i) / kKeepBlock] = (uint8_t)ve;
+            }
+        } else {
+            store4<VEC>(static_cast<float*>(t.M) + at + i, lane, left, m);
+            store4<VEC>(static_cast<float*>(t.V) + at + i, lane, left, v);
+        }
+    }
+}
+
+// Tensors of any alignment, and the ends of all: a function of its own, since beside the other's its registers do not fit (5 to 80 words spilled)
+template <bool EIGHT, typename PT, typename GT, bool MASTER>
+__device__ __noinline__ void step_any(const Tensor& t, int64_t at, const Numbers& number, Now now) {
+    step_unit<EIGHT, false, PT, GT, MASTER>(t, at, number, now);
+}
+
+template <bool EIGHT, typename PT, typename GT, bool MASTER, int CAP>
+__global__ void __launch_bounds__(kThreads, kCtas<EIGHT>) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Numbers number) {
     pdl_trigger();
     pdl_wait();
-    const int lane = threadIdx.x % 32;
-    float lr = number.lr, c1 = number.c1, root_c2 = number.root_c2;
+    Now now{number.lr, number.c1, number.root_c2, 0u};
     uint32_t step = number.step;
-    if (number.lr_dev) lr = *number.lr_dev;
+    if (number.lr_dev) now.lr = *number.lr_dev;
     if (number.step_dev) {
         const int64_t t = *number.step_dev;
         step = (uint32_t)t;
         const float count = t < 1 ? 1.f : (float)t;
         // 1 - b^t = -(e^(t log b) - 1), without the difference's loss of bits (b = 0: log b = -Inf)
-        c1 = 1.f / -expm1f(count * number.log_beta1);
-        root_c2 = sqrtf(1.f / -expm1f(count * number.log_beta2));
+        now.c1 = 1.f / -expm1f(count * number.log_beta1);
+        now.root_c2 = sqrtf(1.f / -expm1f(count * number.log_beta2));
     }
     const uint32_t start = EIGHT ? mix(number.seed + 0x9e3779b9u * step) : 0u;
-    const int64_t units = table.end[table.count - 1], stride = (int64_t)gridDim.x * (kThreads / 32);
+    const int64_t units = table.end[table.count - 1];
     int which = 0;
-    for (int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; unit < units; unit += stride) {
+    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
         if (unit >= table.end[which]) {
             // the first tensor that ends behind this unit
             int lo = which + 1, hi = table.count - 1;
@@ -177,109 +295,74 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
             which = lo;
         }
         const Tensor& t = table.of[which];
-        const int64_t at = (unit - (which ? table.end[which - 1] : 0)) * kUnit;
-        float g[kBlocks][4], p[kBlocks][4], m[kBlocks][4], v[kBlocks][4];
-        uint32_t mq[kBlocks], vq[kBlocks];
-        float ms[kBlocks], vs[kBlocks];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int64_t i = at + b * kKeepBlock, left = t.n - i;
-            if (left <= 0) continue;
-            const bool vec = t.vec && left >= kKeepBlock;
-            load4(t.G, t.g_dtype, i, vec, lane, left, g[b]);
-            if (t.master) load4(t.master + i, vec, lane, left, p[b]);
-            else load4(t.P, t.p_dtype, i, vec, lane, left, p[b]);
-            if constexpr (EIGHT) {
-                mq[b] = load_bytes(static_cast<const uint8_t*>(t.M) + i, vec, lane, left);
-                vq[b] = load_bytes(static_cast<const uint8_t*>(t.V) + i, vec, lane, left);
-                ms[b] = keep_scale_of_byte(t.ME[i / kKeepBlock]);
-                vs[b] = keep_scale_of_byte(t.VE[i / kKeepBlock]);
-            } else {
-                load4(static_cast<const float*>(t.M) + i, vec, lane, left, m[b]);
-                load4(static_cast<const float*>(t.V) + i, vec, lane, left, v[b]);
-            }
-        }
-        const uint32_t seed = EIGHT ? mix(start + t.key) : 0u;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int64_t i = at + b * kKeepBlock, left = t.n - i;
-            if (left <= 0) continue;
-            const bool vec = t.vec && left >= kKeepBlock;
-            if constexpr (EIGHT) {
-                taken4(mq[b], m[b]);
-                taken4(vq[b], v[b]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    m[b][j] *= ms[b];
-                    const float root = v[b][j] * vs[b];
-                    v[b][j] = root * root;
-                }
-            }
-            float root[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = g[b][j] * number.grad_scale;
-                m[b][j] = fmaf(number.beta1, m[b][j], number.rest1 * x);
-                v[b][j] = fmaf(number.beta2, v[b][j], number.rest2 * (x * x));
-                root[j] = sqrtf(v[b][j]);
-                const float direction = __fdividef(m[b][j] * c1, fmaf(root[j], root_c2, number.eps));
-                p[b][j] = fmaf(-lr, fmaf(t.weight_decay, p[b][j], direction), p[b][j]);
-            }
-            if (t.master) store4(t.master + i, vec, lane, left, p[b]);
-            store4(t.P, t.p_dtype, i, vec, lane, left, p[b]);
-            if constexpr (EIGHT) {
-                uint32_t rm[4], rv[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t h = mix(seed ^ (uint32_t)(i + (vec ? 4 * lane + j : 32 * j + lane)));
-                    rm[j] = h & 0xffffu;
-                    rv[j] = h >> 16;
-                }
-                uint32_t q;
-                const uint32_t me = keep_at_random<false>(m[b], rm, &q);
-                store_bytes(static_cast<uint8_t*>(t.M) + i, vec, lane, left, q);
-                const uint32_t ve = keep_at_random<true>(root, rv, &q);
-                store_bytes(static_cast<uint8_t*>(t.V) + i, vec, lane, left, q);
-                if (lane == 0) {
-                    t.ME[i / kKeepBlock] = (uint8_t)me;
-                    t.VE[i / kKeepBlock] = (uint8_t)ve;
-                }
-            } else {
-                store4(static_cast<float*>(t.M) + i, vec, lane, left, m[b]);
-                store4(static_cast<float*>(t.V) + i, vec, lane, left, v[b]);
-            }
-        }
+        const int64_t at = (unit - (which ? table.end[which - 1] : 0)) * kUnit<EIGHT>;
+        if (EIGHT) now.seed = mix(start + t.key);
+        if (t.vec && t.n - at >= kUnit<EIGHT>) step_unit<EIGHT, true, PT, GT, MASTER>(t, at, number, now);
+        else step_any<EIGHT, PT, GT, MASTER>(t, at, number, now);
     }
 }
 
 bool aligned_for(const void* p, int size) { return aligned_to(p, (size_t)size * 4); }
 
-template <bool EIGHT, int CAP>
-detox_status step_of(const Numbers& number, const detox_adamw_tensor* from, const detox_adamw_tensor* end, const detox_adamw_tensor** next,
-                     cudaStream_t s) {
-    static thread_local Table<CAP> table;
-    int64_t units = 0;
-    int n = 0;
-    for (; from != end && n < CAP; ++from) {
-        if (from->n == 0) continue;
-        const int ps = from->p_dtype == DETOX_DTYPE_FLOAT ? 4 : 2, gs = from->g_dtype == DETOX_DTYPE_FLOAT ? 4 : 2, ss = EIGHT ? 1 : 4;
-        Tensor& t = table.of[n];
-        t.P = from->P; t.G = from->G; t.master = from->master;
-        t.M = from->M; t.ME = from->ME; t.V = from->V; t.VE = from->VE;
-        t.n = from->n;
-        t.weight_decay = from->weight_decay;
-        t.key = from->key;
-        t.p_dtype = (uint8_t)from->p_dtype;
-        t.g_dtype = (uint8_t)from->g_dtype;
-        t.vec = aligned_for(t.P, ps) && aligned_for(t.G, gs) && aligned_for(t.master, 4) && aligned_for(t.M, ss) && aligned_for(t.V, ss);
-        units += ceil_div(t.n, (int64_t)kUnit);
-        table.end[n++] = units;
+// The tensors of one kind among those from *from on, as many as the table holds.
+struct Kind {
+    int p_dtype, g_dtype;
+    bool master;
+    bool operator==(const Kind& k) const { return p_dtype == k.p_dtype && g_dtype == k.g_dtype && master == k.master; }
+};
+Kind kind_of(const detox_adamw_tensor& t) { return Kind{t.p_dtype, t.g_dtype, t.master != nullptr}; }
+
+template <bool EIGHT, typename PT, typename GT, bool MASTER, int CAP>
+detox_status step_table(const Numbers& number, const Kind& kind, const detox_adamw_tensor* from, const detox_adamw_tensor* end, cudaStream_t s) {
+    Table<CAP> table;
+    while (from != end) {
+        int64_t units = 0;
+        int n = 0;
+        for (; from != end && n < CAP; ++from) {
+            if (from->n == 0 || !(kind_of(*from) == kind)) continue;
+            const int ss = EIGHT ? 1 : 4;
+            Tensor& t = table.of[n];
+            t.P = from->P; t.G = from->G; t.master = from->master;
+            t.M = from->M; t.ME = from->ME; t.V = from->V; t.VE = from->VE;
+            t.n = from->n;
+            t.weight_decay = from->weight_decay;
+            t.key = from->key;
+            t.vec = aligned_for(t.P, sizeof(PT)) && aligned_for(t.G, sizeof(GT)) && aligned_for(t.master, 4) && aligned_for(t.M, ss) && aligned_for(t.V, ss);
+            units += ceil_div(t.n, (int64_t)kUnit<EIGHT>);
+            table.end[n++] = units;
+        }
+        if (n == 0) break;
+        table.count = n;
+        const int64_t most = (int64_t)kSMs * kCtas<EIGHT>;
+        const detox_status st = launch_chained(adamw_kernel<EIGHT, PT, GT, MASTER, CAP>, (unsigned)(units < most ? units : most), kThreads, 0, 1, s, table, number);
+        if (st != DETOX_OK) return st;
     }
-    *next = from;
-    if (n == 0) return DETOX_OK;
-    table.count = n;
-    const int64_t need = ceil_div(units, (int64_t)(kThreads / 32)), most = (int64_t)kSMs * 4;
-    return launch_chained(adamw_kernel<EIGHT, CAP>, (unsigned)(need < most ? need : most), kThreads, 0, 1, s, table, number);
+    return DETOX_OK;
+}
+template <bool EIGHT, typename PT, typename GT, bool MASTER>
+detox_status step_kind(const Numbers& number, const Kind& kind, const detox_adamw_tensor* from, const detox_adamw_tensor* end, cudaStream_t s) {
+    return end - from <= kFew ? step_table<EIGHT, PT, GT, MASTER, kFew>(number, kind, from, end, s)
+                              : step_table<EIGHT, PT, GT, MASTER, kMany>(number, kind, from, end, s);
+}
+template <bool EIGHT, typename PT>
+detox_status step_types(const Numbers& number, const Kind& kind, const detox_adamw_tensor* from, const detox_adamw_tensor* end, cudaStream_t s) {
+    if constexpr (sizeof(PT) == 4) {
+        if (kind.master) return DETOX_ERR_UNSUPPORTED;
+        if (kind.g_dtype == DETOX_DTYPE_FLOAT) return step_kind<EIGHT, PT, float, false>(number, kind, from, end, s);
+        if (kind.g_dtype == DETOX_DTYPE_HALF) return step_kind<EIGHT, PT, __half, false>(number, kind, from, end, s);
+        return step_kind<EIGHT, PT, __nv_bfloat16, false>(number, kind, from, end, s);
+    } else {
+        if (kind.g_dtype == DETOX_DTYPE_FLOAT)
+            return kind.master ? step_kind<EIGHT, PT, float, true>(number, kind, from, end, s) : step_kind<EIGHT, PT, float, false>(number, kind, from, end, s);
+        if (kind.g_dtype != kind.p_dtype) return DETOX_ERR_UNSUPPORTED;
+        return kind.master ? step_kind<EIGHT, PT, PT, true>(number, kind, from, end, s) : step_kind<EIGHT, PT, PT, false>(number, kind, from, end, s);
+    }
+}
+template <bool EIGHT>
+detox_status step_types(const Numbers& number, const Kind& kind, const detox_adamw_tensor* from, const detox_adamw_tensor* end, cudaStream_t s) {
+    if (kind.p_dtype == DETOX_DTYPE_FLOAT) return step_types<EIGHT, float>(number, kind, from, end, s);
+    if (kind.p_dtype == DETOX_DTYPE_HALF) return step_types<EIGHT, __half>(number, kind, from, end, s);
+    return step_types<EIGHT, __nv_bfloat16>(number, kind, from, end, s);
 }
 
 }  // namespace
@@ -299,11 +382,16 @@ detox_status launch_adamw(const detox_adamw_desc& d, const detox_adamw_tensor* t
     number.lr_dev = d.lr_dev;
     number.step_dev = d.step_dev;
     const detox_adamw_tensor* end = tensors + count;
-    while (tensors != end) {
-        const bool few = end - tensors <= kFew;
-        detox_status st;
-        if (d.bits == 8) st = few ? step_of<true, kFew>(number, tensors, end, &tensors, s) : step_of<true, kMany>(number, tensors, end, &tensors, s);
-        else st = few ? step_of<false, kFew>(number, tensors, end, &tensors, s) : step_of<false, kMany>(number, tensors, end, &tensors, s);
+    Kind done[kKinds];
+    int kinds = 0;
+    for (const detox_adamw_tensor* t = tensors; t != end; ++t) {
+        if (t->n == 0) continue;
+        const Kind kind = kind_of(*t);
+        bool seen = false;
+        for (int i = 0; i < kinds; ++i) seen = seen || done[i] == kind;
+        if (seen) continue;
+        done[kinds++] = kind;
+        const detox_status st = d.bits == 8 ? step_types<true>(number, kind, t, end, s) : step_types<false>(number, kind, t, end, s);
         if (st != DETOX_OK) return st;
     }
     return DETOX_OK;

@@ -5,14 +5,14 @@
 // Gradient:  dW[v] = scale sum of dY[t] over the rows t with tokens[t] = v.  Bound by HBM too (rows of dY read once, rows of dW
 // written once), if the work is shared out evenly: tokens are as unevenly spread as words are, and a padded batch or a
 // short vocabulary puts thousands of rows on one token.  No atomics: the order of the sums is fixed by sizes and tokens.
-//   1. sort_tokens: a stable counting sort in one launch, without communication between CTAs.  Each CTA owns a range of the
-//      vocabulary and looks through all tokens, which lie in L2: it counts those below its range (where its output starts) and, warp by
-//      warp, those of each of its rows; then it goes through them again and writes the row numbers in order.
-//   2. sum_rows: the path that takes a step for every token (a row of dY read) and one for every row of the vocabulary (a row of dW
-//      written), in sorted order, is cut into spans of equal cost.  A warp has a span and a slice of the columns; it adds up
+//   1. sort_tokens: a stable counting sort in one launch, without communication between CTAs.  Each of 2^k CTAs owns every 2^k-th row of the
+//      vocabulary (neighbouring numbers are often equally frequent) and looks through all tokens, which lie in L2: it counts those of
+//      the CTAs before it (where its output starts) and, warp by warp, those of each of its rows; then it goes through them again and writes the
+//      row numbers in order.  The order of the tokens is that of their places: CTA by CTA, and in a CTA ascending.
+//   2. sum_rows: the sorted tokens are cut into spans of equal length, whatever lies in them.  A warp has a span and a slice of the columns; it adds up
 //      rows in registers and writes dW whenever the token changes.  The sum of a token that lies in several spans goes to the
-//      workspace in parts:
-//   3. join_spans: adds those, span by span.
+//      workspace in parts.  Other CTAs of the same launch write zeros to the rows of tokens that do not occur.
+//   3. join_spans: adds those parts, span by span.
 #include "worker.cuh"
 
 namespace detox {
@@ -56,28 +56,46 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const T* __restrict__ 
 // ---- the gradient's plan --------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortRows = kSortThreads;        // rows of the vocabulary that a CTA can own: a thread each
-constexpr int kSpanWarps = 32;                 // resident warps of an SM that the spans are cut for
-constexpr int kJoinThreads = 256;
+constexpr int kSumWarps = 48;                  // warps of an SM that there are spans for, where there are tokens enough
+constexpr int kAhead = 8;                      // rows of dY that a warp has in flight; a span's length is a multiple
+constexpr int kZeroPlaces = 32;                // places that a CTA looks after
+constexpr int kJoinThreads = 512;
 
+// Place p is row (i << bits) + c of the vocabulary with c = p / per, i = p % per; a few at the ends of CTAs' stretches are none.
+struct Places {
+    int32_t vocab, per, bits;
+    __host__ __device__ int32_t count() const { return per << bits; }
+    __device__ __forceinline__ int64_t row(int32_t place) const {
+        const int32_t c = place / per;
+        return ((int64_t)(place - c * per) << bits) + c;
+    }
+};
 struct Plan {
-    int64_t rows, vocab, cols;
+    int64_t rows, cols;
+    Places places;
     int slices;                                // slices of 32 pieces
-    int spans;
+    int spans, length;                         // length: tokens of a span
     int64_t ldp;                               // pitch of the partial sums
-    size_t order, sorted, counted, info, head, tail, bytes;   // offsets in the workspace
+    size_t order, sorted, starts, info, head, tail, bytes;   // offsets in the workspace
 };
 // `entries`: of a 16-byte piece
 Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries) {
-    Plan p{rows, vocab, cols, (int)ceil_div(cols, (int64_t)32 * entries), 1, ceil_div(cols, (int64_t)4) * 4, 0, 0, 0, 0, 0, 0, 0};
-    int64_t spans = (int64_t)kSMs * kSpanWarps / p.slices;
-    if (spans < 1) spans = 1;
-    if (spans > rows + vocab) spans = rows + vocab;
-    p.spans = (int)spans;
+    Plan p = {};
+    p.rows = rows;
+    p.cols = cols;
+    int bits = 7;                              // 128 CTAs, more where a CTA's threads are too few for its rows
+    while (((int64_t)kSortRows << bits) < vocab) ++bits;
+    p.places = Places{(int32_t)vocab, (int32_t)ceil_div(vocab, (int64_t)1 << bits), bits};
+    p.slices = (int)ceil_div(cols, (int64_t)32 * entries);
+    p.ldp = ceil_div(cols, (int64_t)4) * 4;
+    p.length = (int)(ceil_div(rows * p.slices, (int64_t)kSMs * kSumWarps * kAhead) * kAhead);
+    if (p.length < kAhead) p.length = kAhead;
+    p.spans = (int)ceil_div(rows, (int64_t)p.length);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at = align_up(at + bytes); return was; };
     p.order = take((size_t)rows * 4);
     p.sorted = take((size_t)rows * 4);
-    p.counted = take(4);
+    p.starts = take(((size_t)p.places.count() + 1) * 4);
     p.info = take((size_t)p.spans * 8);
     p.head = take((size_t)p.spans * (size_t)p.ldp * 4);
     p.tail = take((size_t)p.spans * (size_t)p.ldp * 4);
@@ -86,37 +104,40 @@ Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries) {
 }
 
 // ---- 1. sorting -----------------------------------------------------------------------------------
-// order: the rows by token, those of a token ascending; sorted: their tokens; counted: how many there are (tokens outside the
-// vocabulary are left out).  CTA b owns [b per, (b + 1) per).  Dynamic shared memory: per x (kSortWarps + 1) int32.
+// order: the rows by their tokens' places, those of a token ascending; sorted: those places; starts: where each place's rows start, and behind the
+// last place how many there are (tokens outside the vocabulary are left out).  Dynamic shared memory: per x (kSortWarps + 1) int32.
 template <typename I>
-__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __restrict__ tokens, int64_t rows, int64_t vocab, int per,
+__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __restrict__ tokens, int64_t rows, Places places,
                                                                    int32_t* __restrict__ order, int32_t* __restrict__ sorted,
-                                                                   int32_t* __restrict__ counted) {
+                                                                   int32_t* __restrict__ starts) {
     extern __shared__ int32_t hist[];          // [row][warp], a column more so that threads stepping through their rows do not collide
     __shared__ int32_t sums[kSortWarps];
     __shared__ int32_t start_of[kSortRows];
-    constexpr int kPitch = kSortWarps + 1, kAhead = 8;
+    constexpr int kPitch = kSortWarps + 1;
     pdl_trigger();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int64_t v0 = (int64_t)blockIdx.x * per, v1 = v0 + per < vocab ? v0 + per : vocab;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, per = places.per;
+    const int32_t own = (int32_t)blockIdx.x, mask = (1 << places.bits) - 1;
     for (int i = threadIdx.x; i < per * kPitch; i += kSortThreads) hist[i] = 0;
     pdl_wait();
     __syncthreads();
     // each warp has a stretch of the tokens
     const int64_t stretch = (rows + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
     const int64_t begin = warp * stretch, end = begin + stretch < rows ? begin + stretch : rows;
+    int32_t tok[kAhead];
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t t = t0 + i * 32 + lane, token = t < end ? (int64_t)tokens[t] : -1;
+            tok[i] = token >= 0 && token < places.vocab ? (int32_t)token : -1;
+        }
+    };
     int32_t below = 0;
     for (int64_t t0 = begin; t0 < end; t0 += 32 * kAhead) {
-        int64_t tok[kAhead];
+        fetch(t0);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int64_t t = t0 + i * 32 + lane;
-            tok[i] = t < end ? (int64_t)tokens[t] : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            below += tok[i] >= 0 && tok[i] < v0;
-            if (tok[i] >= v0 && tok[i] < v1) atomicAdd(&hist[(int)(tok[i] - v0) * kPitch + warp], 1);
+            below += tok[i] >= 0 && (tok[i] & mask) < own;
+            if (tok[i] >= 0 && (tok[i] & mask) == own) atomicAdd(&hist[(tok[i] >> places.bits) * kPitch + warp], 1);
         }
     }
 #pragma unroll
@@ -151,27 +172,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __re
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
     start_of[threadIdx.x] = below + before + upto - total;
-    if (threadIdx.x == kSortThreads - 1 && v1 == vocab && v0 < vocab) *counted = below + before + upto;
+    if ((int)threadIdx.x < per) starts[own * per + threadIdx.x] = below + before + upto - total;
+    if (threadIdx.x == kSortThreads - 1 && own == mask) starts[places.count()] = below + before + upto;
     __syncthreads();
+    const bool again = end - begin > 32 * kAhead;   // (else they are still there)
     for (int64_t t0 = begin; t0 < end; t0 += 32 * kAhead) {
-        int64_t tok[kAhead];
+        if (again) fetch(t0);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int64_t t = t0 + i * 32 + lane;
-            tok[i] = t < end ? (int64_t)tokens[t] : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const bool own = tok[i] >= v0 && tok[i] < v1;
-            if (!__any_sync(0xffffffffu, own)) continue;
-            const int r = own ? (int)(tok[i] - v0) : -1;
+            const bool mine = tok[i] >= 0 && (tok[i] & mask) == own;
+            if (!__any_sync(0xffffffffu, mine)) continue;
+            const int r = mine ? tok[i] >> places.bits : -1;
             const uint32_t peers = __match_any_sync(0xffffffffu, r);
-            int32_t* h = hist + (own ? r : 0) * kPitch + warp;
-            const int32_t at = own ? start_of[r] + *h + __popc(peers & ((1u << lane) - 1u)) : 0;
+            int32_t* h = hist + (mine ? r : 0) * kPitch + warp;
+            const int32_t at = mine ? start_of[r] + *h + __popc(peers & ((1u << lane) - 1u)) : 0;
             __syncwarp();
-            if (own) {
+            if (mine) {
                 order[at] = (int32_t)(t0 + i * 32 + lane);
-                sorted[at] = (int32_t)tok[i];
+                sorted[at] = own * per + r;
                 if (lane == __ffs(peers) - 1) *h += __popc(peers);
             }
             __syncwarp();
@@ -180,55 +198,33 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __re
 }
 
 // ---- 2. sums --------------------------------------------------------------------------------------
-// Where the path of steps is cut: `rows` tokens of the sorted list are behind the cut, and the rows of dW below `v` are written; row v is
-// open when some of its tokens are behind the cut already.
-struct Cut {
-    int32_t k, v;
-    bool open;
-};
-// The cut at cost `at`: a token costs `b`, a row of dW `a`.  (a = 0: only rows with tokens count, with their tokens.)
-// All lanes of a warp call this, each looking at a 32nd of the range.
-__device__ __forceinline__ Cut cut_at(const int32_t* __restrict__ sorted, int32_t n, int32_t vocab, int64_t at, int a, int b, int lane) {
-    // the first k with a sorted[k] + b k >= at
-    int32_t lo = 0, hi = n;
-    while (hi > lo) {
-        const int32_t step = (hi - lo + 31) / 32, k = lo + lane * step;
-        const bool less = k < hi && (int64_t)a * sorted[k] + (int64_t)b * k < at;
-        const int below = __popc(__ballot_sync(0xffffffffu, less));   // the first `below` probes are
-        if (below == 0) hi = lo;
-        else {
-            const int32_t next = lo + below * step;
-            lo += (below - 1) * step + 1;
-            hi = next < hi ? next : hi;
-        }
-    }
-    const int32_t last = lo > 0 ? sorted[lo - 1] : 0, next = lo < n ? sorted[lo] : vocab;
-    int64_t v = a > 0 ? (at - (int64_t)b * lo) / a : next;
-    v = v < last ? last : (v > next ? next : v);
-    return Cut{lo, (int32_t)v, lo > 0 && v < vocab && last == (int32_t)v};
-}
-
 struct SumRows {
     const void* dY;
     int64_t lddy;
     Span span;
-    const int32_t *order, *sorted, *counted;
-    int32_t vocab;
-    int cols, slices, spans;
-    int a, b;
+    const int32_t *order, *sorted, *starts;
+    Places places;
+    int cols, slices, spans, length;
+    unsigned sum_ctas;                         // the CTAs behind them write zeros
     float scale;
     void* dW;
     int64_t lddw;
     bool w_vec;                                // 16-byte accesses to dW
-    int32_t* info;                             // of each span: the row that was open at its start (or -1), the row at its end
+    bool w_wide;                               // 32-byte stores
+    int32_t* info;                             // of each span: the place of which earlier spans have tokens (or -1), and whether it is complete here
     float *head, *tail;
     int64_t ldp;
 };
 
-// N sums of a lane to `to` (entries c .. of a row): fp32, or rounded
+// N sums of a lane to entries c .. of a row: fp32, or rounded.  Eight fp32 sums leave in one 32-byte store: two of 16 bytes each fill half of every
+// sector that they touch .
 template <typename D, int N>
-__device__ __forceinline__ void store_sums(D* row, int c, int cols, bool vec, const uint64_t (&p)[N / 2]) {
+__device__ __forceinline__ void store_sums(D* row, int c, int cols, bool vec, bool wide, const uint64_t (&p)[N / 2]) {
     if constexpr (sizeof(D) == 4 && N == 8) {
+        if (wide && c + N <= cols) {
+            asm volatile("st.global.cs.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(row + c), "l"(p[0]), "l"(p[1]), "l"(p[2]), "l"(p[3]) : "memory");
+            return;
+        }
         if (vec && c + N <= cols) {
             float4* to = reinterpret_cast<float4*>(row + c);
             __stcs(to, make_float4(pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])));
@@ -264,122 +260,172 @@ __device__ __forceinline__ void load_sums(const D* row, int c, int cols, bool ve
     for (int j = 0; j < N / 2; ++j) p[j] = pair_of(f[2 * j], f[2 * j + 1]);
 }
 
+// zeros to the rows of kZeroPlaces places that have no tokens
+template <typename D>
+__device__ __forceinline__ void zero_rows(const SumRows& g, int64_t first) {
+    constexpr int N = Piece<D>::N, kWide = 32 / (int)sizeof(D);
+    const int64_t place = first + threadIdx.x % 32;
+    const int64_t row = place < g.places.count() ? g.places.row((int32_t)place) : g.places.vocab;
+    uint32_t empty = __ballot_sync(0xffffffffu, row < g.places.vocab && g.starts[place] == g.starts[place + 1]);
+    for (; empty; empty &= empty - 1) {
+        D* to = static_cast<D*>(g.dW) + __shfl_sync(0xffffffffu, row, __ffs(empty) - 1) * g.lddw;
+        if (g.w_wide) {
+            for (int c = threadIdx.x * kWide; c < g.cols; c += kThreads * kWide) {
+                if (c + kWide <= g.cols) {
+                    asm volatile("st.global.cs.v4.b64 [%0], {%1, %1, %1, %1};" ::"l"(to + c), "l"(0ull) : "memory");
+                } else {
+                    for (int j = c; j < g.cols; ++j) to[j] = from_f32<D>(0.f);
+                }
+            }
+        } else if (g.w_vec) {
+            for (int c = threadIdx.x * N; c < g.cols; c += kThreads * N) {
+                if (c + N <= g.cols) {
+                    st_stream_u4(to + c, make_uint4(0u, 0u, 0u, 0u));
+                } else {
+                    for (int j = c; j < g.cols; ++j) to[j] = from_f32<D>(0.f);
+                }
+            }
+        } else {
+            for (int c = threadIdx.x; c < g.cols; c += kThreads) to[c] = from_f32<D>(0.f);
+        }
+    }
+}
+
 template <typename T, typename D, bool ADD, bool ANY>
-__global__ void __launch_bounds__(kThreads) sum_rows_kernel(const __grid_constant__ SumRows g) {
-    constexpr int N = Piece<T>::N, kAhead = 8;
+__global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_constant__ SumRows g) {
+    constexpr int N = Piece<T>::N;
     pdl_trigger();
     pdl_wait();
+    if (!ADD && blockIdx.x >= g.sum_ctas) {
+        zero_rows<D>(g, (int64_t)(blockIdx.x - g.sum_ctas) * kZeroPlaces);
+        return;
+    }
     const int lane = threadIdx.x % 32;
     const int warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const int span = warp / g.slices, slice = warp - span * g.slices;
     if (span >= g.spans) return;
-    const int32_t n = *g.counted;
-    const int64_t cost = (int64_t)g.a * g.vocab + (int64_t)g.b * n;
-    const Cut from = cut_at(g.sorted, n, g.vocab, cost / g.spans * span + cost % g.spans * span / g.spans, g.a, g.b, lane);
-    Cut to{n, g.vocab, false};
-    if (span + 1 < g.spans)
-        to = cut_at(g.sorted, n, g.vocab, cost / g.spans * (span + 1) + cost % g.spans * (span + 1) / g.spans, g.a, g.b, lane);
+    const int32_t n = g.starts[g.places.count()], from = span * g.length;
+    const int32_t to = from + g.length < n ? from + g.length : n;
+    if (from >= to) {
+        if (slice == 0 && lane == 0) g.info[2 * span] = -1;
+        return;
+    }
+    int32_t place = g.sorted[from];
+    const bool open = from > 0 && g.sorted[from - 1] == place, goes_on = to < n && g.sorted[to] == g.sorted[to - 1];
     if (slice == 0 && lane == 0) {
-        g.info[2 * span] = from.open ? from.v : -1;
-        g.info[2 * span + 1] = to.v;
+        g.info[2 * span] = open ? place : -1;
+        g.info[2 * span + 1] = g.sorted[to - 1] != place || !goes_on;
     }
     const int c = (slice * 32 + lane) * N;
-    const T* dY = static_cast<const T*>(g.dY);
+    const T* dY = static_cast<const T*>(g.dY) + c;
+    D* dW = static_cast<D*>(g.dW);
     uint64_t acc[N / 2];
-    auto clear = [&] {
 #pragma unroll
-        for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
-    };
-    clear();
+    for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
     const uint64_t scale2 = pair_of(g.scale, g.scale);
-    int32_t v = from.v;
-    bool any = from.open;                      // row v has tokens
-    // row v is complete, and there are no tokens for those between it and `next`
-    auto close = [&](int32_t next) {
-        D* row = static_cast<D*>(g.dW) + (int64_t)v * g.lddw;
-        if (from.open && v == from.v) {
-            store_sums<float, N>(g.head + (int64_t)span * g.ldp, c, (int)g.ldp, true, acc);
-        } else if (!ADD || any) {
+    bool head = open;
+    int64_t row = 0;                           // of dW, for `place`
+    // the sum of a place is complete here
+    auto close = [&] {
+        if (head) {
+            store_sums<float, N>(g.head + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
+            head = false;
+        } else {
+            D* at = dW + row * g.lddw;
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) acc[j] = mul2(acc[j], scale2);
             if constexpr (ADD) {
                 uint64_t old[N / 2];
-                load_sums<D, N>(row, c, g.cols, g.w_vec, old);
+                load_sums<D, N>(at, c, g.cols, g.w_vec, old);
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], old[j]);
             }
-            store_sums<D, N>(row, c, g.cols, g.w_vec, acc);
+            store_sums<D, N>(at, c, g.cols, g.w_vec, g.w_wide, acc);
         }
-        clear();
-        any = false;
-        if constexpr (!ADD) {
-            for (++v, row += g.lddw; v < next; ++v, row += g.lddw) store_sums<D, N>(row, c, g.cols, g.w_vec, acc);
-        }
-        v = next;
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
     };
-    int32_t order = 0, token = 0;              // of 32 tokens, one a lane
-    for (int32_t k = from.k; k < to.k; k += kAhead) {
-        const int at = (k - from.k) & 31;
+    int32_t order = 0, its_place = 0;          // of 32 tokens, one a lane
+    int64_t its_row = 0;
+    for (int32_t k = from; k < to; k += kAhead) {
+        const int at = (k - from) & 31;
         if (at == 0) {
-            const bool there = k + lane < to.k;
+            const bool there = k + lane < to;
             order = there ? g.order[k + lane] : 0;
-            token = there ? g.sorted[k + lane] : 0;
+            its_place = there ? g.sorted[k + lane] : -1;
+            its_row = there ? g.places.row(its_place) : 0;
         }
         uint4 raw[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int32_t row = __shfl_sync(0xffffffffu, order, at + i);
-            raw[i] = load_piece<ANY>(dY + (int64_t)row * g.lddy, c, k + i < to.k ? g.cols : 0, g.span);
-        }
+        for (int i = 0; i < kAhead; ++i)
+            raw[i] = load_piece<ANY>(dY + (int64_t)__shfl_sync(0xffffffffu, order, at + i) * g.lddy, 0, k + i < to ? g.cols - c : 0, g.span);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int32_t t = __shfl_sync(0xffffffffu, token, at + i);
-            if (k + i >= to.k) break;
-            if (t != v) close(t);
-            any = true;
+            const int32_t p = __shfl_sync(0xffffffffu, its_place, at + i);
+            const int64_t r = __shfl_sync(0xffffffffu, its_row, at + i);
+            if (p >= 0 && p != place) {
+                close();
+                place = p;
+            }
+            if (p >= 0) row = r;
             uint64_t f[N / 2];
             Piece<T>::split(raw[i], f);
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], f[j]);
         }
     }
-    if (v < to.v) close(to.v);
-    if (to.open) store_sums<float, N>(g.tail + (int64_t)span * g.ldp, c, (int)g.ldp, true, acc);
+    if (goes_on) store_sums<float, N>(g.tail + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
+    else close();
 }
 
 // ---- 3. tokens that lie in several spans -----------------------------------------------------------
-// A CTA for each span that completes a row which was open at its start: the sum of the earlier spans' parts and its own.
+// A CTA for each span that completes a place which was open at its start: the sum of the earlier spans' parts and its own.
 template <typename D, bool ADD>
-__global__ void __launch_bounds__(kJoinThreads) join_spans_kernel(const int32_t* __restrict__ info, const float* __restrict__ head,
+__global__ void __launch_bounds__(kJoinThreads) join_spans_kernel(const int32_t* __restrict__ info, Places places, const float* __restrict__ head,
                                                                   const float* __restrict__ tail, int64_t ldp, int cols, float scale,
                                                                   D* __restrict__ dW, int64_t lddw) {
+    constexpr int kQuads = 128, kGroups = kJoinThreads / kQuads;   // of 4 columns; of parts, every kGroups-th one
+    __shared__ float4 sm[kGroups][kQuads];
     pdl_trigger();
     pdl_wait();
-    const int span = blockIdx.x, lane = threadIdx.x % 32;
-    const int32_t v = info[2 * span];
-    if (v < 0 || info[2 * span + 1] <= v) return;
-    // the first span with a part: the last one before this at whose start the row was not open
+    const int span = blockIdx.x, lane = threadIdx.x % 32, x = threadIdx.x % kQuads, group = threadIdx.x / kQuads;
+    const int32_t place = info[2 * span];
+    if (place < 0 || !info[2 * span + 1]) return;
+    // the first span with a part: the last one before this that has it, but not from earlier spans
     int first = span;
     for (bool more = true; more && first > 0;) {
         const int s = first - 1 - lane;
-        const uint32_t began = __ballot_sync(0xffffffffu, s < 0 || info[2 * s] != v);
+        const uint32_t began = __ballot_sync(0xffffffffu, s < 0 || info[2 * s] != place);
         more = began == 0;
         first -= more ? 32 : __ffs(began);
     }
     if (first < 0) first = 0;
-    for (int c = threadIdx.x * 4; c < cols; c += kJoinThreads * 4) {
+    D* row = dW + places.row(place) * lddw;
+    for (int c0 = 0; c0 < cols; c0 += 4 * kQuads) {
+        const int c = c0 + 4 * x;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < cols) {
 #pragma unroll 8
-        for (int s = first; s < span; ++s) {
-            const float4 x = *reinterpret_cast<const float4*>(tail + (int64_t)s * ldp + c);
-            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+            for (int s = first + group; s < span; s += kGroups) {
+                const float4 f = *reinterpret_cast<const float4*>(tail + (int64_t)s * ldp + c);
+                sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
+            }
         }
-        const float4 x = *reinterpret_cast<const float4*>(head + (int64_t)span * ldp + c);
-        const float f[4] = {sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w};
-        D* to = dW + (int64_t)v * lddw + c;
+        __syncthreads();
+        sm[group][x] = sum;
+        __syncthreads();
+        if (group == 0 && c < cols) {
+            sum = *reinterpret_cast<const float4*>(head + (int64_t)span * ldp + c);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < cols) to[j] = from_f32<D>(ADD ? fmaf(f[j], scale, to_f32(to[j])) : f[j] * scale);
+            for (int k = 0; k < kGroups; ++k) {
+                const float4 f = sm[k][x];
+                sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
+            }
+            const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < cols) row[c + j] = from_f32<D>(ADD ? fmaf(f[j], scale, to_f32(row[c + j])) : f[j] * scale);
+        }
     }
 }
 
@@ -413,18 +459,14 @@ detox_status lookup(const void* W, int64_t ldw, int64_t vocab, int64_t cols, int
 
 template <typename I>
 detox_status sort_tokens(const void* tokens, const Plan& p, char* ws, cudaStream_t s) {
-    // as many CTAs as SMs, more where a CTA's threads are too few for its rows
-    const int64_t least = ceil_div(p.vocab, (int64_t)kSortRows);
-    const int64_t ctas = p.vocab < kSMs ? p.vocab : (least > kSMs ? least : kSMs);
-    const int per = (int)ceil_div(p.vocab, ctas);
-    const size_t smem = (size_t)per * (kSortWarps + 1) * sizeof(int32_t);
+    const size_t smem = (size_t)p.places.per * (kSortWarps + 1) * sizeof(int32_t);
     if (smem > 40 * 1024 && cudaFuncSetAttribute(sort_tokens_kernel<I>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return DETOX_ERR_CUDA;
     }
-    return launch_chained(sort_tokens_kernel<I>, (unsigned)ceil_div(p.vocab, (int64_t)per), kSortThreads, smem, 1, s,
-                          static_cast<const I*>(tokens), p.rows, p.vocab, per, reinterpret_cast<int32_t*>(ws + p.order),
-                          reinterpret_cast<int32_t*>(ws + p.sorted), reinterpret_cast<int32_t*>(ws + p.counted));
+    return launch_chained(sort_tokens_kernel<I>, 1u << p.places.bits, kSortThreads, smem, 1, s, static_cast<const I*>(tokens), p.rows, p.places,
+                          reinterpret_cast<int32_t*>(ws + p.order), reinterpret_cast<int32_t*>(ws + p.sorted),
+                          reinterpret_cast<int32_t*>(ws + p.starts));
 }
 
 template <typename T, typename D, bool ADD>
@@ -434,23 +476,23 @@ detox_status sums(const void* dY, int64_t lddy, float scale, void* dW, int64_t l
     g.span = span_of<T>(dY, lddy, p.rows, p.cols);
     g.order = reinterpret_cast<int32_t*>(ws + p.order);
     g.sorted = reinterpret_cast<int32_t*>(ws + p.sorted);
-    g.counted = reinterpret_cast<int32_t*>(ws + p.counted);
-    g.vocab = (int32_t)p.vocab;
-    g.cols = (int)p.cols; g.slices = p.slices; g.spans = p.spans;
-    g.a = ADD ? 0 : (int)sizeof(D);
-    g.b = (int)sizeof(T);
+    g.starts = reinterpret_cast<int32_t*>(ws + p.starts);
+    g.places = p.places;
+    g.cols = (int)p.cols; g.slices = p.slices; g.spans = p.spans; g.length = p.length;
     g.scale = scale;
     g.dW = dW; g.lddw = lddw;
     g.w_vec = aligned16(dW) && lddw % Piece<D>::N == 0;
+    g.w_wide = aligned_to(dW, 32) && lddw * (int64_t)sizeof(D) % 32 == 0;
     g.info = reinterpret_cast<int32_t*>(ws + p.info);
     g.head = reinterpret_cast<float*>(ws + p.head);
     g.tail = reinterpret_cast<float*>(ws + p.tail);
     g.ldp = p.ldp;
     const bool any = !(p.cols % Piece<T>::N == 0 && g.span.vec);
-    const unsigned grid = (unsigned)ceil_div((int64_t)p.spans * p.slices, (int64_t)(kThreads / 32));
+    g.sum_ctas = (unsigned)ceil_div((int64_t)p.spans * p.slices, (int64_t)(kThreads / 32));
+    const unsigned grid = g.sum_ctas + (ADD ? 0u : (unsigned)ceil_div((int64_t)p.places.count(), (int64_t)kZeroPlaces));
     const detox_status st = launch_chained(any ? sum_rows_kernel<T, D, ADD, true> : sum_rows_kernel<T, D, ADD, false>, grid, kThreads, 0, 1, s, g);
-    if (st != DETOX_OK) return st;
-    return launch_chained(join_spans_kernel<D, ADD>, (unsigned)p.spans, kJoinThreads, 0, 1, s, g.info, g.head, g.tail, p.ldp, (int)p.cols, scale,
+    if (st != DETOX_OK || p.spans < 2) return st;
+    return launch_chained(join_spans_kernel<D, ADD>, (unsigned)p.spans, kJoinThreads, 0, 1, s, g.info, g.places, g.head, g.tail, p.ldp, (int)p.cols, scale,
                           static_cast<D*>(dW), lddw);
 }
 template <typename T>
@@ -471,7 +513,7 @@ detox_status launch_embedding(int dtype, const void* W, int64_t ldw, int64_t voc
 }
 
 size_t embedding_backward_ws_bytes(int64_t rows, int64_t vocab, int64_t cols) {
-    // (whatever the type: 16-bit rows have fewer slices and with them more spans)
+    // (whatever the type: 16-bit rows have fewer slices and with them shorter spans, and more)
     return plan_of(rows, vocab, cols, Piece<__half>::N).bytes;
 }
 

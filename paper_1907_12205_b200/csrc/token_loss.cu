@@ -4,11 +4,12 @@
 // All of it is bound by HBM: the logits are the largest matrix of a training step, and the least is to read them once and write their
 // gradient once.
 //
-//   rows_kernel      a cluster of 1 to 8 CTAs holds a row in registers: entries come in 16-byte pieces, each thread takes 2^(x - its own largest x), the
-//                    pairs (largest, sum) of all warps meet once a row (through distributed shared memory where there are several CTAs), and the policy
-//                    loss's gradient is the kept powers times one number a thread.  So the logits are read once, one power is taken of each entry (the
-//                    special-function unit would be the bound with two), and a row has one barrier.  The next row's pieces are asked for before the
-//                    present row's sums meet.
+//   policy_kernel    a cluster of 1 to 8 CTAs holds a row in registers: entries come in 16-byte pieces, each thread takes 2^(x - its own largest x), the
+//                    pairs (largest, sum) of all warps meet once a row (through distributed shared memory where there are several CTAs), and the
+//                    gradient is the kept powers times one number a thread.  So the logits are read once, one power is taken of each entry (the
+//                    special-function unit would be the bound with two), and a row has one barrier.  The next row's pieces are asked for as this
+//                    one's are used up.
+//   score_kernel     log-probabilities alone: a warp, a CTA or a cluster goes through a row with a running largest x and sum.
 //   backward_kernel  the gradient where lse is known: entry by entry.  The preference loss needs all of a pair's rows before any gradient, so it takes this
 //                    second pass; it goes through the rows backwards, since the last ones that were read still lie in L2.
 //   pairs_kernel     sums over sequences, margins and the rows' gradients, a CTA a pair.
@@ -52,9 +53,66 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b) {
     return make_float2(m, a.y * exp2_fast(a.x - m0) + b.y * exp2_fast(b.x - m0));
 }
 
-// ---- what a row has beside its logits --------------------------------------------------------------
-enum Mode { kLogp, kPolicy };
+__device__ __forceinline__ float warp_largest(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_total(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// the pairs of a warp's lanes as one, in all lanes
+__device__ __forceinline__ float2 joined_warp(float2 a) {
+    const float m = warp_largest(a.x), m0 = m == minus_inf() ? 0.f : m;
+    return make_float2(m, warp_total(a.y * exp2_fast(a.x - m0)));
+}
 
+// 16 bytes, or what was there before; issued where it is written
+__device__ __forceinline__ void load_if(uint4& v, const void* from, bool want) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)
+        : "l"(from), "r"((uint32_t)want)
+        : "memory");
+}
+// the entries of a piece, rounded
+template <typename T>
+__device__ __forceinline__ void store_entries(T* row, int c, int cols, bool vec, const float (&f)[Piece<T>::N]) {
+    constexpr int N = Piece<T>::N;
+    if (vec && c + N <= cols) {
+        st_stream_u4(row + c, Piece<T>::join(f));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
+    }
+}
+
+// What a row's pair says: zy is the chosen token's logit, `there` whether there is such a token.
+struct Scored {
+    float logp, lse;
+    bool empty;                    // nothing but -Inf
+};
+__device__ __forceinline__ Scored scored(float2 all, float zy, float k2, bool there) {
+    const float lg = log2f(all.y);
+    const bool empty = all.x == minus_inf() && all.y == 0.f;
+    return Scored{empty ? (there ? minus_inf() : zy) : (fmaf(zy, k2, -all.x) - lg) * kLn2, empty ? minus_inf() : (all.x + lg) * kLn2, empty};
+}
+
+// e^d - 1 - d: near 0 by its series (the next term is 10^-7 of it at 1/2), where the difference would lose its bits
+__device__ __forceinline__ float above_tangent(float d) {
+    float s = fmaf(d, 1.f / 40320.f, 1.f / 5040.f);
+    s = fmaf(d, s, 1.f / 720.f);
+    s = fmaf(d, s, 1.f / 120.f);
+    s = fmaf(d, s, 1.f / 24.f);
+    s = fmaf(d, s, 1.f / 6.f);
+    s = fmaf(d, s, 0.5f);
+    return fabsf(d) < 0.5f ? d * d * s : __expf(d) - 1.f - d;
+}
+
+// ---- the policy loss -------------------------------------------------------------------------------
 struct RowsArgs {
     const void* Z;
     int64_t ldz;
@@ -66,9 +124,6 @@ struct RowsArgs {
     bool wide;                     // y in 64 bits
     float k2;                      // scale log2(e)
     float* logp;
-    float* lse;
-    float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
-    // the policy loss
     const float *old_logp, *advantage, *ref_logp, *weight;
     float low, high, kl_coef, even_weight, grad_scale;   // grad_scale: times scale
     void* dZ;
@@ -128,16 +183,15 @@ __device__ __forceinline__ uint4 only_first(uint4 v, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Registers: a thread holds P pieces of the next row (not AHEAD: of this one, and is done with them when it has the powers) and, for the gradient,
-// this row's powers in fp32.  16 pieces of fp32 leave no room for both.
+// Registers: a thread holds P pieces of the next row (not AHEAD: of this one, and is done with them when it has the powers) and this row's
+// powers in fp32.  16 pieces of fp32 leave no room for both.
 template <typename T, int P> constexpr bool kAhead = P * Piece<T>::N + 4 * P <= 96;
-template <typename T, int P, Mode MODE>
-constexpr int kRegisters = (MODE == kPolicy ? P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) : 4 * P) + 32;
-template <typename T, int THREADS, int P, Mode MODE>
-constexpr int kCtas = 65536 / (THREADS * kRegisters<T, P, MODE>) < 2048 / THREADS ? 65536 / (THREADS * kRegisters<T, P, MODE>) : 2048 / THREADS;
+template <typename T, int P> constexpr int kRegisters = P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) + (sizeof(T) == 4 ? 48 : 32);
+template <typename T, int THREADS, int P>
+constexpr int kCtas = 65536 / (THREADS * kRegisters<T, P>) < 2048 / THREADS ? 65536 / (THREADS * kRegisters<T, P>) : 2048 / THREADS;
 
-template <typename T, int THREADS, int P, Mode MODE, bool ANY>
-__global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P, MODE>)) rows_kernel(const __grid_constant__ RowsArgs g) {
+template <typename T, int THREADS, int P, bool ANY>
+__global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel(const __grid_constant__ RowsArgs g) {
     constexpr int N = Piece<T>::N, WARPS = THREADS / 32;
     constexpr bool AHEAD = kAhead<T, P>;
     __shared__ float2 met[2][kMaxCluster * WARPS];
@@ -151,72 +205,78 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P, MODE>)) rows_ke
     pdl_wait();
     int64_t row = blockIdx.x / cluster;
     const T* Z = static_cast<const T*>(g.Z);
-    uint4 raw[P];
+    uint4 raw[P] = {};
     // a row's chosen token, -1 where the row does not count, and its weight
     auto look = [&](int64_t r, int64_t& token, float& weight) {
         token = -1;
         weight = 0.f;
         if (r >= g.rows) return;
         token = chosen(g.y, g.wide, r);
-        weight = MODE == kLogp ? 1.f : (g.weight ? g.weight[r] : g.even_weight);
+        weight = g.weight ? g.weight[r] : g.even_weight;
         if (weight == 0.f) token = -1;
     };
-    auto fetch = [&](int64_t r, bool want) {
-        const T* from = Z + r * g.ldz + begin;
-#pragma unroll
-        for (int i = 0; i < P; ++i) raw[i] = load_piece<ANY>(from, (int)(threadIdx.x + i * THREADS) * N, want ? cols : 0, g.span);
+    auto fetch = [&](int i, int64_t r, bool want) {
+        const int c = (int)(threadIdx.x + i * THREADS) * N;
+        if constexpr (ANY) raw[i] = load_piece<true>(Z + r * g.ldz + begin, c, want ? cols : 0, g.span);
+        else load_if(raw[i], Z + r * g.ldz + begin + c, want && c < cols);
     };
     int64_t y, next_y;
     float w, next_w;
     look(row, y, w);
     look(row + stride, next_y, next_w);
-    if (AHEAD) fetch(row, y >= 0);
+    if (AHEAD) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) fetch(i, row, y >= 0);
+    }
     double sum_loss = 0., sum_pg = 0., sum_kl = 0., sum_clip = 0.;
     int turn = 0;
     for (; row < g.rows; row += stride) {
         const int64_t next = row + stride;
         const bool live = y >= 0;                              // (the same in all CTAs of the cluster)
-        if (!AHEAD) fetch(row, live);
+        if (!AHEAD) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) fetch(i, row, live);
+        }
         float zy = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
         if (live) {
             zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
-            if (MODE == kPolicy) {
-                old = g.old_logp[row];
-                adv = g.advantage[row];
-                if (g.ref_logp) ref = g.ref_logp[row];
-            }
+            old = g.old_logp[row];
+            adv = g.advantage[row];
+            if (g.ref_logp) ref = g.ref_logp[row];
         }
-        float top = minus_inf(), sum = 0.f;
-        float e[MODE == kPolicy ? P * N : 1];
+        float top = minus_inf(), sum[4] = {0.f, 0.f, 0.f, 0.f}, base = 0.f;
+        float e[P * N];
         if (live) {
             Largest<T> most;
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const int c = (int)(threadIdx.x + i * THREADS) * N;
-                if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
+                if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);   // (where nothing was loaded: all of it)
                 most.take(raw[i]);
             }
             top = most.value() * g.k2;
-            const float base = top == minus_inf() ? 0.f : top;
+            if (top != minus_inf()) base = top;
+        }
+        // a piece's registers take the next row's as soon as its powers are formed
+        if (live) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 float f[N];
                 Piece<T>::split(raw[i], f);
+                if (AHEAD) fetch(i, next, next_y >= 0);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    f[j] = exp2_fast(fmaf(f[j], g.k2, -base));
-                    sum += f[j];
-                    if constexpr (MODE == kPolicy) e[i * N + j] = f[j];
+                    e[i * N + j] = exp2_fast(fmaf(f[j], g.k2, -base));
+                    sum[j & 3] += e[i * N + j];
                 }
             }
-        }
-        if (AHEAD) fetch(next, next_y >= 0);
-        float logp = 0.f, lse = 0.f, factor = 0.f, coef = 0.f;
-        if (live) {
-            float2 all = make_float2(top, sum);
+        } else if (AHEAD) {
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-                all = joined(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, o), __shfl_xor_sync(0xffffffffu, all.y, o)));
+            for (int i = 0; i < P; ++i) fetch(i, next, next_y >= 0);
+        }
+        float logp = 0.f, factor = 0.f, coef = 0.f;
+        if (live) {
+            float2 all = joined_warp(make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3])));
             // (slots are written again two live rows on, and every thread has passed the barrier between)
             float2* slots = met[turn & 1];
             ++turn;
@@ -228,79 +288,164 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P, MODE>)) rows_ke
                 cluster_meet();
             }
             all = make_float2(minus_inf(), 0.f);
-            for (int i = lane; i < cluster * WARPS; i += 32) all = joined(all, slots[i]);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-                all = joined(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, o), __shfl_xor_sync(0xffffffffu, all.y, o)));
-            const float lg = log2f(all.y);
-            const bool empty = all.x == minus_inf() && all.y == 0.f;   // nothing but -Inf
-            logp = empty ? (y < g.vocab ? minus_inf() : zy) : (fmaf(zy, g.k2, -all.x) - lg) * kLn2;
-            lse = empty ? minus_inf() : (all.x + lg) * kLn2;
-            if (MODE == kPolicy) {
-                const float r = expf(logp - old);
-                const float free = r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
-                const bool clipped = free > held;
-                const float pg = -(clipped ? held : free);
-                float kl = 0.f, slope = clipped ? 0.f : -free;
-                if (g.ref_logp) {
-                    const float d = ref - logp, x = expm1f(d);
-                    kl = x - d;
-                    slope = fmaf(-g.kl_coef, x, slope);
-                }
-                if (rank == 0 && threadIdx.x == 0) {
-                    sum_loss += (double)w * ((double)pg + (double)g.kl_coef * (double)kl);
-                    sum_pg += (double)w * (double)pg;
-                    sum_kl += (double)w * (double)kl;
-                    if (clipped) sum_clip += (double)w;
-                }
-                coef = empty ? 0.f : g.grad_scale * w * slope;
-                factor = empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
+            if (cluster == 1) {
+                if (lane < WARPS) all = slots[lane];
+            } else {
+                for (int i = lane; i < cluster * WARPS; i += 32) all = joined(all, slots[i]);
             }
+            all = joined_warp(all);
+            const Scored row_of = scored(all, zy, g.k2, y < g.vocab);
+            logp = row_of.logp;
+            const float r = __expf(logp - old);
+            const float free = r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
+            const bool clipped = free > held;
+            const float pg = -(clipped ? held : free);
+            float kl = 0.f, slope = clipped ? 0.f : -free;
+            if (g.ref_logp) {
+                const float d = ref - logp;
+                kl = above_tangent(d);
+                slope = fmaf(-g.kl_coef, d + kl, slope);
+            }
+            if (rank == 0 && threadIdx.x == 0) {
+                sum_loss += (double)(w * fmaf(g.kl_coef, kl, pg));
+                sum_pg += (double)(w * pg);
+                sum_kl += (double)(w * kl);
+                if (clipped) sum_clip += (double)w;
+            }
+            coef = row_of.empty ? 0.f : g.grad_scale * w * slope;
+            factor = row_of.empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
         }
-        if (rank == 0 && threadIdx.x == 0) {
-            if (g.logp) g.logp[row] = logp;
-            if (MODE == kLogp && g.lse) g.lse[row] = lse;
-            if (MODE == kLogp && g.zeros) g.zeros[row] = 0.f;
-        }
-        if constexpr (MODE == kPolicy) {
-            if (g.dZ) {
-                T* to = static_cast<T*>(g.dZ) + row * g.lddz + begin;
+        if (g.logp && rank == 0 && threadIdx.x == 0) g.logp[row] = logp;
+        if (g.dZ) {
+            T* to = static_cast<T*>(g.dZ) + row * g.lddz + begin;
+            if (live) {
                 const int at = (int)(y - begin);               // the chosen entry, if it is one of this CTA's
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
                     const int c = (int)(threadIdx.x + i * THREADS) * N;
                     if (c >= cols) continue;
-                    uint64_t out[N / 2];
+                    float out[N];
 #pragma unroll
-                    for (int j = 0; j < N / 2; ++j)
-                        out[j] = live ? mul2(pair_of(e[i * N + 2 * j], e[i * N + 2 * j + 1]), pair_of(factor, factor)) : 0ull;
-                    if (live && at >= c && at < c + N) {
+                    for (int j = 0; j < N; ++j) out[j] = e[i * N + j] * factor;
+                    if (at >= c && at < c + N) {
 #pragma unroll
-                        for (int j = 0; j < N / 2; ++j)
-                            out[j] = pair_of(pair_lo(out[j]) + (at == c + 2 * j ? coef : 0.f), pair_hi(out[j]) + (at == c + 2 * j + 1 ? coef : 0.f));
+                        for (int j = 0; j < N; ++j) out[j] += at == c + j ? coef : 0.f;
                     }
-                    store_piece(to, c, cols, !ANY || g.dz_vec, out);
+                    store_entries(to, c, cols, !ANY || g.dz_vec, out);
                 }
+            } else {
+                const float none[N] = {};
+                for (int c = (int)threadIdx.x * N; c < cols; c += THREADS * N) store_entries(to, c, cols, !ANY || g.dz_vec, none);
             }
         }
         y = next_y;
         w = next_w;
         look(next + stride, next_y, next_w);
     }
-    if (MODE == kPolicy && rank == 0 && threadIdx.x == 0) {
+    if (rank == 0 && threadIdx.x == 0) {
         double* to = g.parts + 4 * (blockIdx.x / cluster);
         to[0] = sum_loss; to[1] = sum_pg; to[2] = sum_kl; to[3] = sum_clip;
     }
     if (cluster > 1) cluster_meet();   // no CTA leaves while another may still write to its shared memory
 }
 
-// out[i] = factor * sum over k of parts[k][i], i < WIDTH; one warp, fixed order
-template <int WIDTH>
-__global__ void total_kernel(const double* __restrict__ parts, int64_t count, double factor, float* __restrict__ out) {
-    pdl_trigger();
+// ---- log-probabilities alone -------------------------------------------------------------------------
+// Nothing of a row has to stay: its threads go through it piece by piece with a running largest x and sum, and rows need no common
+// pace.  GROUP threads have a row, or a CTA of a cluster its part of one.
+constexpr int kScoreThreads = 256, kScorePieces = 4;
+
+struct ScoreArgs {
+    const void* Z;
+    int64_t ldz;
+    Span span;
+    int64_t rows;
+    int vocab, chunk;
+    int cluster;
+    const void* y;
+    bool wide;
+    float k2;
+    float *logp, *lse;
+    float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
+};
+
+template <typename T, int GROUP, bool ANY>
+__global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_constant__ ScoreArgs g) {
+    constexpr int N = Piece<T>::N, WARPS = kScoreThreads / 32;
+    __shared__ float2 met[kMaxCluster * WARPS];
+    if (g.cluster == 1) pdl_trigger();
     pdl_wait();
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, member = threadIdx.x % GROUP;
+    const uint32_t rank = GROUP > 32 && g.cluster > 1 ? cluster_rank() : 0u;
+    const int64_t row = GROUP == 32 ? (int64_t)blockIdx.x * WARPS + warp : (int64_t)(blockIdx.x / g.cluster);
+    if (row >= g.rows) return;                                 // (whole warps, and only with GROUP = 32)
+    const int begin = (int)rank * g.chunk, cols = g.vocab - begin < g.chunk ? g.vocab - begin : g.chunk;
+    const T* Z = static_cast<const T*>(g.Z) + row * g.ldz;
+    const int64_t y = chosen(g.y, g.wide, row);
+    const bool first = rank == 0 && member == 0;
+    if (first && g.zeros) g.zeros[row] = 0.f;
+    if (y < 0) {                                               // (the same in all threads of the row)
+        if (first && g.logp) g.logp[row] = 0.f;
+        if (first && g.lse) g.lse[row] = 0.f;
+        return;
+    }
+    float zy = 0.f;
+    if (first) zy = y < g.vocab ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
+    float top = minus_inf(), sum[2] = {0.f, 0.f};
+    for (int c0 = member * N; c0 < cols; c0 += GROUP * kScorePieces * N) {
+        uint4 raw[kScorePieces];
+#pragma unroll
+        for (int i = 0; i < kScorePieces; ++i) raw[i] = load_piece<ANY>(Z + begin, c0 + i * GROUP * N, cols, g.span);
+        Largest<T> most;
+#pragma unroll
+        for (int i = 0; i < kScorePieces; ++i) {
+            const int c = c0 + i * GROUP * N;
+            if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
+            most.take(raw[i]);
+        }
+        const float here = most.value() * g.k2;
+        if (here > top) {
+            const float less = exp2_fast(top - here);
+            sum[0] *= less;
+            sum[1] *= less;
+            top = here;
+        }
+        const float base = top == minus_inf() ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < kScorePieces; ++i) {
+            float f[N];
+            Piece<T>::split(raw[i], f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j & 1] += exp2_fast(fmaf(f[j], g.k2, -base));
+        }
+    }
+    float2 all = make_float2(top, sum[0] + sum[1]);
+    all = joined_warp(all);
+    if constexpr (GROUP > 32) {
+        if (g.cluster == 1) {
+            if (lane == 0) met[warp] = all;
+            __syncthreads();
+        } else {
+            if (lane == 0) store_at(&met[(int)rank * WARPS + warp], 0u, all);
+            cluster_meet();
+        }
+        if (rank != 0 || warp != 0) return;
+        all = make_float2(minus_inf(), 0.f);
+        for (int i = lane; i < g.cluster * WARPS; i += 32) all = joined(all, met[i]);
+        all = joined_warp(all);
+    }
+    if (first) {
+        const Scored s = scored(all, zy, g.k2, y < g.vocab);
+        if (g.logp) g.logp[row] = s.logp;
+        if (g.lse) g.lse[row] = s.lse;
+    }
+}
+
+// out[i] = factor * sum over k of parts[k][i], i < WIDTH, by one warp; fixed order
+template <int WIDTH>
+__device__ __forceinline__ void total_of(const double* __restrict__ parts, int64_t count, double factor, float* __restrict__ out) {
+    const int lane = threadIdx.x % 32;
     double sum[WIDTH] = {};
+#pragma unroll 4
     for (int64_t k = lane; k < count; k += 32)
 #pragma unroll
         for (int i = 0; i < WIDTH; ++i) sum[i] += parts[k * WIDTH + i];
@@ -310,6 +455,12 @@ __global__ void total_kernel(const double* __restrict__ parts, int64_t count, do
         for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
         if (lane == 0) out[i] = (float)(factor * sum[i]);
     }
+}
+template <int WIDTH>
+__global__ void total_kernel(const double* __restrict__ parts, int64_t count, double factor, float* __restrict__ out) {
+    pdl_trigger();
+    pdl_wait();
+    total_of<WIDTH>(parts, count, factor, out);
 }
 
 // ---- the gradient from lse -------------------------------------------------------------------------
@@ -328,6 +479,9 @@ struct BackArgs {
     void* dZ;
     int64_t lddz;
     bool dz_vec;
+    const double* parts;           // of the preference loss, which the first warp adds up on the way (a launch less); or NULL
+    int64_t pairs;
+    float* loss;
 };
 
 // a warp for each slice of 32 * kBackPieces pieces, from the last one back
@@ -337,6 +491,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x % 32;
+    if (g.loss && blockIdx.x == 0 && threadIdx.x < 32) total_of<1>(g.parts, g.pairs, 1.0 / (double)g.pairs, g.loss);
     const int64_t items = g.rows * g.slices, stride = (int64_t)gridDim.x * (kBackThreads / 32);
     for (int64_t k = (int64_t)blockIdx.x * (kBackThreads / 32) + threadIdx.x / 32; k < items; k += stride) {
         const int64_t item = items - 1 - k, row = item / g.slices;
@@ -351,6 +506,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
         for (int i = 0; i < kBackPieces; ++i) raw[i] = load_piece<ANY>(from, c0 + i * 32 * N, live ? g.vocab : 0, g.span);
         const float coef = y < g.vocab ? d * g.scale : __int_as_float(0x7fc00000);
         const float base = -lse * kLog2e;
+        const int at = y < g.vocab ? (int)y : -1;
         T* to = static_cast<T*>(g.dZ) + row * g.lddz;
 #pragma unroll
         for (int i = 0; i < kBackPieces; ++i) {
@@ -358,12 +514,15 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
             if (c >= g.vocab) continue;
             float f[N];
             Piece<T>::split(raw[i], f);
-            uint64_t out[N / 2];
+            if (live) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) f[j] = live ? coef * ((y == c + j ? 1.f : 0.f) - exp2_fast(fmaf(f[j], g.k2, base))) : 0.f;
+                for (int j = 0; j < N; ++j) f[j] = exp2_fast(fmaf(f[j], g.k2, base)) * -coef;
+                if (at >= c && at < c + N) {
 #pragma unroll
-            for (int j = 0; j < N / 2; ++j) out[j] = pair_of(f[2 * j], f[2 * j + 1]);
-            store_piece(to, c, g.vocab, !ANY || g.dz_vec, out);
+                    for (int j = 0; j < N; ++j) f[j] += at == c + j ? coef : 0.f;
+                }
+            }
+            store_entries(to, c, g.vocab, !ANY || g.dz_vec, f);
         }
     }
 }
@@ -454,39 +613,50 @@ detox_status by_chunk(int chunk, F f) {
     return DETOX_ERR_UNSUPPORTED;
 }
 
-template <typename T, Mode MODE, bool ANY>
-struct Rows {
+template <typename T, bool ANY>
+struct Policy {
     const RowsArgs& g;
     int64_t* clusters;
     cudaStream_t s;
     template <int THREADS, int P>
     detox_status operator()() const {
-        const int64_t most = (int64_t)kSMs * kCtas<T, THREADS, P, MODE> / g.cluster;
+        const int64_t most = (int64_t)kSMs * kCtas<T, THREADS, P> / g.cluster;
         *clusters = g.rows < most ? g.rows : most;
         // Clusters that fill the SMs' registers do not overlap with the stream's other kernels, as the gated products' pairs do not.
-        return launch(g.cluster == 1, rows_kernel<T, THREADS, P, MODE, ANY>, (unsigned)(*clusters * g.cluster), THREADS, 0, (unsigned)g.cluster, s, g);
+        return launch(g.cluster == 1, policy_kernel<T, THREADS, P, ANY>, (unsigned)(*clusters * g.cluster), THREADS, 0, (unsigned)g.cluster, s, g);
     }
 };
 template <typename T>
 bool pieces(const void* p, int64_t ld) {
     return aligned16(p) && ld % Piece<T>::N == 0;
 }
-// clusters: how many parts the policy loss has
-template <typename T, Mode MODE>
-detox_status rows_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
+// clusters: how many parts the loss has
+template <typename T>
+detox_status policy_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
     const Shape shape = shape_of<T>(g.rows, g.vocab);
     g.cluster = shape.cluster;
     g.chunk = shape.chunk;
     g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
     g.dz_vec = pieces<T>(g.dZ, g.lddz);
-    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec)) return by_chunk<T>(g.chunk, Rows<T, MODE, false>{g, clusters, s});
-    return by_chunk<T>(g.chunk, Rows<T, MODE, true>{g, clusters, s});
+    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec)) return by_chunk<T>(g.chunk, Policy<T, false>{g, clusters, s});
+    return by_chunk<T>(g.chunk, Policy<T, true>{g, clusters, s});
 }
-template <Mode MODE>
-detox_status rows_of(int dtype, const RowsArgs& g, int64_t* clusters, cudaStream_t s) {
-    if (dtype == DETOX_DTYPE_FLOAT) return rows_of<float, MODE>(g, clusters, s);
-    if (dtype == DETOX_DTYPE_HALF) return rows_of<__half, MODE>(g, clusters, s);
-    return rows_of<__nv_bfloat16, MODE>(g, clusters, s);
+
+// A warp for a row of up to 8 pieces a lane; else a CTA, or where rows are few a cluster, as long as its threads have pieces for a turn each.
+template <typename T>
+detox_status score_of(ScoreArgs g, cudaStream_t s) {
+    constexpr int N = Piece<T>::N;
+    g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
+    const bool any = !(g.vocab % N == 0 && g.span.vec);
+    g.cluster = 1;
+    g.chunk = g.vocab;
+    if (g.vocab <= 32 * 8 * N)
+        return launch_chained(any ? score_kernel<T, 32, true> : score_kernel<T, 32, false>, (unsigned)ceil_div(g.rows, (int64_t)(kScoreThreads / 32)),
+                              kScoreThreads, 0, 1, s, g);
+    while (g.cluster < kMaxCluster && g.rows * g.cluster <= kSMs * 2 && g.vocab >= g.cluster * 2 * kScoreThreads * kScorePieces * N) g.cluster *= 2;
+    g.chunk = (int)(ceil_div(ceil_div((int64_t)g.vocab, (int64_t)g.cluster), (int64_t)N) * N);
+    return launch(g.cluster == 1, any ? score_kernel<T, kScoreThreads, true> : score_kernel<T, kScoreThreads, false>, (unsigned)(g.rows * g.cluster),
+                  kScoreThreads, 0, (unsigned)g.cluster, s, g);
 }
 
 template <typename T>
@@ -504,18 +674,24 @@ detox_status backward_of(BackArgs g, cudaStream_t s) {
 detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
                                float* logp, float* lse, float* zeros, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
-    RowsArgs g = {};
+    ScoreArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
     g.k2 = scale * kLog2e;
     g.logp = logp; g.lse = lse; g.zeros = zeros;
-    int64_t clusters;
-    return rows_of<kLogp>(dtype, g, &clusters, s);
+    if (dtype == DETOX_DTYPE_FLOAT) return score_of<float>(g, s);
+    if (dtype == DETOX_DTYPE_HALF) return score_of<__half>(g, s);
+    return score_of<__nv_bfloat16>(g, s);
 }
 
-detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
-                                        float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s) {
-    if (rows == 0) return DETOX_OK;
+namespace {
+detox_status backward_of(int dtype, const BackArgs& g, cudaStream_t s) {
+    if (dtype == DETOX_DTYPE_FLOAT) return backward_of<float>(g, s);
+    if (dtype == DETOX_DTYPE_HALF) return backward_of<__half>(g, s);
+    return backward_of<__nv_bfloat16>(g, s);
+}
+BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, const float* lse,
+                   const float* dlogp, void* dZ, int64_t lddz) {
     BackArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
@@ -523,9 +699,14 @@ detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, i
     g.scale = scale;
     g.lse = lse; g.dlogp = dlogp;
     g.dZ = dZ; g.lddz = lddz;
-    if (dtype == DETOX_DTYPE_FLOAT) return backward_of<float>(g, s);
-    if (dtype == DETOX_DTYPE_HALF) return backward_of<__half>(g, s);
-    return backward_of<__nv_bfloat16>(g, s);
+    return g;
+}
+}  // namespace
+
+detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
+                                        float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s) {
+    if (rows == 0) return DETOX_OK;
+    return backward_of(dtype, back_args(Z, ldz, rows, vocab, index, y, scale, lse, dlogp, dZ, lddz), s);
 }
 
 size_t policy_loss_ws_bytes(int64_t rows) {
@@ -549,7 +730,10 @@ detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float*
         g.grad_scale = d.grad_scale * d.scale;
         g.dZ = dZ; g.lddz = lddz;
         g.parts = parts;
-        const detox_status st = rows_of<kPolicy>(d.dtype, g, &clusters, s);
+        detox_status st;
+        if (d.dtype == DETOX_DTYPE_FLOAT) st = policy_of<float>(g, &clusters, s);
+        else if (d.dtype == DETOX_DTYPE_HALF) st = policy_of<__half>(g, &clusters, s);
+        else st = policy_of<__nv_bfloat16>(g, &clusters, s);
         if (st != DETOX_OK) return st;
     }
     return launch_chained(total_kernel<4>, 1, 32, 0, 1, s, parts, clusters, 1.0, stats);
@@ -575,9 +759,15 @@ detox_status launch_preference_loss(const detox_preference_desc& d, float* loss,
                             d.pairs, d.beta, d.smoothing, grad, margin, sums, dZ && d.rows ? dlogp : nullptr, parts);
         if (st != DETOX_OK) return st;
     }
-    st = launch_chained(total_kernel<1>, 1, 32, 0, 1, s, parts, d.pairs, d.pairs > 0 ? 1.0 / (double)d.pairs : 0.0, loss);
-    if (st != DETOX_OK || !dZ) return st;
-    return launch_token_logp_backward(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, lse, dlogp, dZ, lddz, s);
+    if (dZ && d.rows > 0) {
+        BackArgs g = back_args(d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, lse, dlogp, dZ, lddz);
+        if (d.pairs > 0) {
+            g.parts = parts; g.pairs = d.pairs; g.loss = loss;
+        }
+        st = backward_of(d.dtype, g, s);
+        if (st != DETOX_OK || d.pairs > 0) return st;
+    }
+    return launch_chained(total_kernel<1>, 1, 32, 0, 1, s, parts, d.pairs, d.pairs > 0 ? 1.0 / (double)d.pairs : 0.0, loss);
 }
 
 }  // namespace detox

@@ -241,17 +241,18 @@ detox_status detox_preference_loss(const detox_preference_desc* d, float* loss, 
 
 detox_status detox_adamw(const detox_adamw_desc* d, const detox_adamw_tensor* tensors, int64_t count, void* stream) {
     if (!d || count < 0 || (count > 0 && !tensors) || (d->bits != 32 && d->bits != 8)) return DETOX_ERR_BAD_ARG;
-    if (!(d->lr_dev || std::isfinite(d->lr)) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !(d->eps >= 0.) ||
+    if (!(d->lr_dev || std::isfinite(d->lr)) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !(d->eps > 0.) ||
         !std::isfinite(d->eps) || !finite(d->grad_scale) || (!d->step_dev && d->step < 1) || !aligned_to(d->lr_dev, 4) || !aligned_to(d->step_dev, 8))
         return DETOX_ERR_BAD_ARG;
     for (int64_t i = 0; i < count; ++i) {
         const detox_adamw_tensor& t = tensors[i];
         const int ps = dtype_size(t.p_dtype), gs = dtype_size(t.g_dtype);
         if (t.n < 0 || ps == 0 || gs == 0 || !finite(t.weight_decay)) return DETOX_ERR_BAD_ARG;
-        if (t.n > ((int64_t)1 << 40)) return DETOX_ERR_UNSUPPORTED;
         if (t.n == 0) continue;
+        if (t.n > ((int64_t)1 << 40) || (t.p_dtype == DETOX_DTYPE_FLOAT ? t.master != nullptr : t.g_dtype != t.p_dtype && t.g_dtype != DETOX_DTYPE_FLOAT))
+            return DETOX_ERR_UNSUPPORTED;
         if (!t.P || !aligned_to(t.P, (size_t)ps) || !t.G || !aligned_to(t.G, (size_t)gs) || !aligned_to(t.master, 4) || !t.M || !t.V) return DETOX_ERR_BAD_ARG;
-        if (t.P == t.master || t.P == t.G || t.M == t.V) return DETOX_ERR_BAD_ARG;
+        if (t.P == t.G || t.master == t.G || t.M == t.V) return DETOX_ERR_BAD_ARG;
         if (d->bits == 32 ? !aligned_to(t.M, 4) || !aligned_to(t.V, 4) : !t.ME || !t.VE) return DETOX_ERR_BAD_ARG;
     }
     return launch_adamw(*d, tensors, count, static_cast<cudaStream_t>(stream));
