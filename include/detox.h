@@ -474,7 +474,8 @@ detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, i
  * Every dtype is computed in fp32 and rounded once.
  *   - y[t] < 0: the row has no chosen token.  It is not read; its logp and lse are 0, it takes no part in a loss, and its gradient is zero.
  *     y[t] >= vocab: logp is NaN (and with it the loss and the row's gradient).
- *   - Logits of -Inf (masked entries) have probability and gradient 0.  A row of nothing but -Inf: lse and logp are -Inf, its gradient zero.
+ *   - Logits of -Inf, or below -2^100 where others are above (masked entries), have probability and gradient 0.  A row of nothing but such entries: lse
+ *     and logp are -Inf, its gradient zero.
  *   - vocab <= DETOX_LOGITS_MAX_COLS (a cluster of CTAs holds a row).
  *   - dZ may be Z itself (same base and stride).
  *

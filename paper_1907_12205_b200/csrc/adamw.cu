@@ -269,17 +269,18 @@ template <bool EIGHT, typename PT, typename GT, bool MASTER, int CAP>
 __global__ void __launch_bounds__(kThreads, kCtas<EIGHT>) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Numbers number) {
     pdl_trigger();
     pdl_wait();
-    Now now{number.lr, number.c1, number.root_c2, 0u};
+    float lr = number.lr, c1 = number.c1, root_c2 = number.root_c2;
     uint32_t step = number.step;
-    if (number.lr_dev) now.lr = *number.lr_dev;
+    if (number.lr_dev) lr = *number.lr_dev;
     if (number.step_dev) {
         const int64_t t = *number.step_dev;
         step = (uint32_t)t;
         const float count = t < 1 ? 1.f : (float)t;
         // 1 - b^t = -(e^(t log b) - 1), without the difference's loss of bits (b = 0: log b = -Inf)
-        now.c1 = 1.f / -expm1f(count * number.log_beta1);
-        now.root_c2 = sqrtf(1.f / -expm1f(count * number.log_beta2));
+        c1 = 1.f / -expm1f(count * number.log_beta1);
+        root_c2 = sqrtf(1.f / -expm1f(count * number.log_beta2));
     }
+    Now now{lr, c1, root_c2, 0u};
     const uint32_t start = EIGHT ? mix(number.seed + 0x9e3779b9u * step) : 0u;
     const int64_t units = table.end[table.count - 1];
     int which = 0;

@@ -167,6 +167,11 @@ template <> struct Largest<__nv_bfloat16> {
     __device__ __forceinline__ float value() const { const float2 f = unpack2<__nv_bfloat16>(m); return fmaxf(f.x, f.y); }
     static constexpr uint32_t kNone = 0xff80ff80u;
 };
+// x of the largest entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
+__device__ __forceinline__ float largest_of(float z, float k2) {
+    const float x = z * k2;
+    return x < -1.2676506e30f ? minus_inf() : x;
+}
 // a piece of which only the first `n` entries are in the row: -Inf for the others
 template <typename T>
 __device__ __forceinline__ uint4 only_first(uint4 v, int n) {
@@ -254,7 +259,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);   // (where nothing was loaded: all of it)
                 most.take(raw[i]);
             }
-            top = most.value() * g.k2;
+            top = largest_of(most.value(), g.k2);
             if (top != minus_inf()) base = top;
         }
         // a piece's registers take the next row's as soon as its powers are formed
@@ -402,7 +407,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
             if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
             most.take(raw[i]);
         }
-        const float here = most.value() * g.k2;
+        const float here = largest_of(most.value(), g.k2);
         if (here > top) {
             const float less = exp2_fast(top - here);
             sum[0] *= less;
@@ -568,7 +573,8 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __rest
         const float plus = x >= 0.f ? up : (x < 0.f ? down : x), minus = x >= 0.f ? down : (x < 0.f ? up : x);   // sigmoid(x), sigmoid(-x)
         if (threadIdx.x == 0) {
             const float rise = x < 0.f ? -x : 0.f, fall = x > 0.f ? x : 0.f;
-            parts[p] = (double)((1.f - smoothing) * (rise + l) + smoothing * (fall + l));
+            // (a term without weight may be infinite)
+            parts[p] = (double)((smoothing < 1.f ? (1.f - smoothing) * (rise + l) : 0.f) + (smoothing > 0.f ? smoothing * (fall + l) : 0.f));
             margin[p] = x;
             sums[2 * p] = (float)s[0];
             sums[2 * p + 1] = (float)s[1];

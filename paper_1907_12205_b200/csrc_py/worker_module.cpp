@@ -674,9 +674,10 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
             t.P = entries_of(p, "params", t.n);
             t.G = entries_of(g, "grads", t.n);
             if (a[10] != Py_None && masters[i] != Py_None) t.master = static_cast<float*>(entries_of(masters[i], "masters", t.n, at::kFloat));
-            const bool eight = PyTuple_Check(ms[i]) || PyList_Check(ms[i]);
+            const auto is_pair = [](PyObject* o) { return PyTuple_Check(o) || PyList_Check(o); };
+            const bool eight = is_pair(ms[i]);
             if (i == 0) d.bits = eight ? 8 : 32;
-            if (eight != (d.bits == 8)) raise(PyExc_TypeError, "m, v: states of all tensors in 32 bits or all in 8");
+            if (eight != (d.bits == 8) || eight != is_pair(vs[i])) raise(PyExc_TypeError, "m, v: states of all tensors in 32 bits or all in 8");
             if (eight) {
                 const Items m(ms[i], "a state in 8 bits: values and scales", 2), v(vs[i], "a state in 8 bits: values and scales", 2);
                 t.M = entries_of(m[0], "m", t.n, kValues);
