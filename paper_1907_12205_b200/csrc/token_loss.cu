@@ -90,6 +90,9 @@ __device__ __forceinline__ void store_entries(T* row, int c, int cols, bool vec,
     }
 }
 
+// times ln 2, to its full bits: a factor that is always off to the same side would add up over a sequence
+__device__ __forceinline__ float in_nats(float v) { return fmaf(v, kLn2, v * -1.9046543e-9f); }
+
 // What a row's pair says: zy is the chosen token's logit, `there` whether there is such a token.
 struct Scored {
     float logp, lse;
@@ -98,7 +101,7 @@ struct Scored {
 __device__ __forceinline__ Scored scored(float2 all, float zy, float k2, bool there) {
     const float lg = log2f(all.y);
     const bool empty = all.x == minus_inf() && all.y == 0.f;
-    return Scored{empty ? (there ? minus_inf() : zy) : (fmaf(zy, k2, -all.x) - lg) * kLn2, empty ? minus_inf() : (all.x + lg) * kLn2, empty};
+    return Scored{empty ? (there ? minus_inf() : zy) : in_nats(fmaf(zy, k2, -all.x) - lg), empty ? minus_inf() : in_nats(all.x + lg), empty};
 }
 
 // e^d - 1 - d: near 0 by its series (the next term is 10^-7 of it at 1/2), where the difference would lose its bits
@@ -118,8 +121,7 @@ struct RowsArgs {
     int64_t ldz;
     Span span;
     int64_t rows;
-    int vocab, chunk;              // columns of a row, and of a CTA's part of it
-    int cluster;
+    int vocab, pieces, cluster;    // columns of a row; its pieces, which the CTAs of a cluster share
     const void* y;
     bool wide;                     // y in 64 bits
     float k2;                      // scale log2(e)
@@ -195,6 +197,8 @@ template <typename T, int P> constexpr int kRegisters = P * Piece<T>::N + (kAhea
 template <typename T, int THREADS, int P>
 constexpr int kCtas = 65536 / (THREADS * kRegisters<T, P>) < 2048 / THREADS ? 65536 / (THREADS * kRegisters<T, P>) : 2048 / THREADS;
 
+// P pieces a thread; but for ANY the CTAs of a cluster have more than (P - 1) * THREADS each, so that only a thread's last one may be missing (a comparison and a
+// branch for each piece took a third of the instructions).
 template <typename T, int THREADS, int P, bool ANY>
 __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel(const __grid_constant__ RowsArgs g) {
     constexpr int N = Piece<T>::N, WARPS = THREADS / 32;
@@ -202,15 +206,18 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
     __shared__ float2 met[2][kMaxCluster * WARPS];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int cluster = g.cluster;
-    const uint32_t rank = cluster > 1 ? cluster_rank() : 0u;
+    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
     const int64_t stride = gridDim.x / cluster;
-    const int begin = (int)rank * g.chunk;                    // this CTA's columns of a row
-    const int cols = g.vocab - begin < g.chunk ? g.vocab - begin : g.chunk;
+    const int first = rank * g.pieces / cluster, pieces = (rank + 1) * g.pieces / cluster - first;
+    const int begin = first * N;                              // this CTA's columns of a row
+    const int cols = g.vocab - begin < pieces * N ? g.vocab - begin : pieces * N;
     if (cluster == 1) pdl_trigger();
     pdl_wait();
     int64_t row = blockIdx.x / cluster;
     const T* Z = static_cast<const T*>(g.Z);
     uint4 raw[P] = {};
+    // whether thread's piece i is there
+    auto there = [&](int i) { return (!ANY && i < P - 1) || (int)threadIdx.x + i * THREADS < pieces; };
     // a row's chosen token, -1 where the row does not count, and its weight
     auto look = [&](int64_t r, int64_t& token, float& weight) {
         token = -1;
@@ -220,10 +227,9 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
         weight = g.weight ? g.weight[r] : g.even_weight;
         if (weight == 0.f) token = -1;
     };
-    auto fetch = [&](int i, int64_t r, bool want) {
-        const int c = (int)(threadIdx.x + i * THREADS) * N;
-        if constexpr (ANY) raw[i] = load_piece<true>(Z + r * g.ldz + begin, c, want ? cols : 0, g.span);
-        else load_if(raw[i], Z + r * g.ldz + begin + c, want && c < cols);
+    auto fetch = [&](int i, const T* from, bool want) {
+        if constexpr (ANY) raw[i] = load_piece<true>(from, (int)(threadIdx.x + i * THREADS) * N, want ? cols : 0, g.span);
+        else load_if(raw[i], from + (threadIdx.x + i * THREADS) * N, want && there(i));
     };
     int64_t y, next_y;
     float w, next_w;
@@ -231,116 +237,110 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
     look(row + stride, next_y, next_w);
     if (AHEAD) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) fetch(i, row, y >= 0);
+        for (int i = 0; i < P; ++i) fetch(i, Z + row * g.ldz + begin, y >= 0);
     }
     double sum_loss = 0., sum_pg = 0., sum_kl = 0., sum_clip = 0.;
     int turn = 0;
     for (; row < g.rows; row += stride) {
         const int64_t next = row + stride;
-        const bool live = y >= 0;                              // (the same in all CTAs of the cluster)
-        if (!AHEAD) {
+        const T *here = Z + row * g.ldz + begin, *there_next = Z + next * g.ldz + begin;
+        T* to = static_cast<T*>(g.dZ) + (g.dZ ? row * g.lddz + begin : 0);
+        if (y < 0) {                                           // (the same in all CTAs of the cluster)
+            if (AHEAD) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) fetch(i, row, live);
-        }
-        float zy = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
-        if (live) {
-            zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
-            old = g.old_logp[row];
-            adv = g.advantage[row];
-            if (g.ref_logp) ref = g.ref_logp[row];
-        }
-        float top = minus_inf(), sum[4] = {0.f, 0.f, 0.f, 0.f}, base = 0.f;
-        float e[P * N];
-        if (live) {
+                for (int i = 0; i < P; ++i) fetch(i, there_next, next_y >= 0);
+            }
+            if (g.logp && rank == 0 && threadIdx.x == 0) g.logp[row] = 0.f;
+            if (g.dZ) {
+                const float none[N] = {};
+                for (int c = (int)threadIdx.x * N; c < cols; c += THREADS * N) store_entries(to, c, cols, !ANY || g.dz_vec, none);
+            }
+        } else {
+            if (!AHEAD) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) fetch(i, here, true);
+            }
+            const float zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
+            const float old = g.old_logp[row], adv = g.advantage[row], ref = g.ref_logp ? g.ref_logp[row] : 0.f;
             Largest<T> most;
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const int c = (int)(threadIdx.x + i * THREADS) * N;
-                if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);   // (where nothing was loaded: all of it)
+                if constexpr (ANY) {
+                    const int c = (int)(threadIdx.x + i * THREADS) * N;
+                    if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
+                } else {
+                    if (!there(i)) raw[i] = make_uint4(Largest<T>::kNone, Largest<T>::kNone, Largest<T>::kNone, Largest<T>::kNone);
+                }
                 most.take(raw[i]);
             }
-            top = largest_of(most.value(), g.k2);
-            if (top != minus_inf()) base = top;
-        }
-        // a piece's registers take the next row's as soon as its powers are formed
-        if (live) {
+            const float top = largest_of(most.value(), g.k2), base = top == minus_inf() ? 0.f : top;
+            const uint64_t k22 = pair_of(g.k2, g.k2), base2 = pair_of(-base, -base);
+            uint64_t e[P * N / 2], sum2[2] = {0ull, 0ull};
+            // a piece's registers take the next row's as soon as its powers are formed
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                float f[N];
+                uint64_t f[N / 2];
                 Piece<T>::split(raw[i], f);
-                if (AHEAD) fetch(i, next, next_y >= 0);
+                if (AHEAD) fetch(i, there_next, next_y >= 0);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    e[i * N + j] = exp2_fast(fmaf(f[j], g.k2, -base));
-                    sum[j & 3] += e[i * N + j];
+                for (int j = 0; j < N / 2; ++j) {
+                    const uint64_t x = fma2(f[j], k22, base2);
+                    const uint64_t v = pair_of(exp2_fast(pair_lo(x)), exp2_fast(pair_hi(x)));
+                    sum2[j & 1] = add2(sum2[j & 1], v);
+                    e[i * (N / 2) + j] = v;
                 }
             }
-        } else if (AHEAD) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) fetch(i, next, next_y >= 0);
-        }
-        float logp = 0.f, factor = 0.f, coef = 0.f;
-        if (live) {
-            float2 all = joined_warp(make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3])));
-            // (slots are written again two live rows on, and every thread has passed the barrier between)
+            sum2[0] = add2(sum2[0], sum2[1]);
+            float2 all = joined_warp(make_float2(top, pair_lo(sum2[0]) + pair_hi(sum2[0])));
+            // (slots are written again two rows on, and every thread has passed the barrier between)
             float2* slots = met[turn & 1];
             ++turn;
             if (cluster == 1) {
                 if (lane == 0) slots[warp] = all;
                 __syncthreads();
+                all = lane < WARPS ? slots[lane] : make_float2(minus_inf(), 0.f);
             } else {
-                if (lane < cluster) store_at(&slots[(int)rank * WARPS + warp], (uint32_t)lane, all);
+                if (lane < cluster) store_at(&slots[rank * WARPS + warp], (uint32_t)lane, all);
                 cluster_meet();
-            }
-            all = make_float2(minus_inf(), 0.f);
-            if (cluster == 1) {
-                if (lane < WARPS) all = slots[lane];
-            } else {
+                all = make_float2(minus_inf(), 0.f);
                 for (int i = lane; i < cluster * WARPS; i += 32) all = joined(all, slots[i]);
             }
             all = joined_warp(all);
             const Scored row_of = scored(all, zy, g.k2, y < g.vocab);
-            logp = row_of.logp;
-            const float r = __expf(logp - old);
+            const float r = __expf(row_of.logp - old);
             const float free = r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
             const bool clipped = free > held;
-            const float pg = -(clipped ? held : free);
             float kl = 0.f, slope = clipped ? 0.f : -free;
             if (g.ref_logp) {
-                const float d = ref - logp;
+                const float d = ref - row_of.logp;
                 kl = above_tangent(d);
                 slope = fmaf(-g.kl_coef, d + kl, slope);
             }
+            const float coef = row_of.empty ? 0.f : g.grad_scale * w * slope;
+            const float factor = row_of.empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
+            if (g.dZ) {
+                const uint64_t factor2 = pair_of(factor, factor);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    uint64_t out[N / 2];
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j) out[j] = mul2(e[i * (N / 2) + j], factor2);
+                    const int c = (int)(threadIdx.x + i * THREADS) * N;
+                    if constexpr (ANY) store_piece(to, c, cols, g.dz_vec, out);
+                    else if (there(i)) st_stream_u4(to + c, Piece<T>::join(out));
+                }
+                // the chosen entry, by the thread that stored its piece
+                const int at = y < g.vocab ? (int)y - begin : -1;
+                if (at >= 0 && at < cols && at / N % THREADS == (int)threadIdx.x && !row_of.empty)
+                    to[at] = from_f32<T>(zy == minus_inf() ? coef : -coef * expm1f(row_of.logp));
+            }
             if (rank == 0 && threadIdx.x == 0) {
+                const float pg = -(clipped ? held : free);
+                if (g.logp) g.logp[row] = row_of.logp;
                 sum_loss += (double)(w * fmaf(g.kl_coef, kl, pg));
                 sum_pg += (double)(w * pg);
                 sum_kl += (double)(w * kl);
                 if (clipped) sum_clip += (double)w;
-            }
-            coef = row_of.empty ? 0.f : g.grad_scale * w * slope;
-            factor = row_of.empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
-        }
-        if (g.logp && rank == 0 && threadIdx.x == 0) g.logp[row] = logp;
-        if (g.dZ) {
-            T* to = static_cast<T*>(g.dZ) + row * g.lddz + begin;
-            if (live) {
-                const int at = (int)(y - begin);               // the chosen entry, if it is one of this CTA's
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const int c = (int)(threadIdx.x + i * THREADS) * N;
-                    if (c >= cols) continue;
-                    float out[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) out[j] = e[i * N + j] * factor;
-                    if (at >= c && at < c + N) {
-#pragma unroll
-                        for (int j = 0; j < N; ++j) out[j] += at == c + j ? coef : 0.f;
-                    }
-                    store_entries(to, c, cols, !ANY || g.dz_vec, out);
-                }
-            } else {
-                const float none[N] = {};
-                for (int c = (int)threadIdx.x * N; c < cols; c += THREADS * N) store_entries(to, c, cols, !ANY || g.dz_vec, none);
             }
         }
         y = next_y;
@@ -395,35 +395,43 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     }
     float zy = 0.f;
     if (first) zy = y < g.vocab ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
-    float top = minus_inf(), sum[2] = {0.f, 0.f};
+    float top = minus_inf();
+    uint64_t sum2[2] = {0ull, 0ull};
+    const uint64_t k22 = pair_of(g.k2, g.k2);
     for (int c0 = member * N; c0 < cols; c0 += GROUP * kScorePieces * N) {
         uint4 raw[kScorePieces];
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) raw[i] = load_piece<ANY>(Z + begin, c0 + i * GROUP * N, cols, g.span);
         Largest<T> most;
+        if (c0 + ((kScorePieces - 1) * GROUP + 1) * N > cols) {
 #pragma unroll
-        for (int i = 0; i < kScorePieces; ++i) {
-            const int c = c0 + i * GROUP * N;
-            if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
-            most.take(raw[i]);
+            for (int i = 0; i < kScorePieces; ++i) raw[i] = only_first<T>(raw[i], cols - c0 - i * GROUP * N);
         }
+#pragma unroll
+        for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
         const float here = largest_of(most.value(), g.k2);
         if (here > top) {
             const float less = exp2_fast(top - here);
-            sum[0] *= less;
-            sum[1] *= less;
+            const uint64_t less2 = pair_of(less, less);
+            sum2[0] = mul2(sum2[0], less2);
+            sum2[1] = mul2(sum2[1], less2);
             top = here;
         }
         const float base = top == minus_inf() ? 0.f : top;
+        const uint64_t base2 = pair_of(-base, -base);
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) {
-            float f[N];
+            uint64_t f[N / 2];
             Piece<T>::split(raw[i], f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum[j & 1] += exp2_fast(fmaf(f[j], g.k2, -base));
+            for (int j = 0; j < N / 2; ++j) {
+                const uint64_t x = fma2(f[j], k22, base2);
+                sum2[j & 1] = add2(sum2[j & 1], pair_of(exp2_fast(pair_lo(x)), exp2_fast(pair_hi(x))));
+            }
         }
     }
-    float2 all = make_float2(top, sum[0] + sum[1]);
+    sum2[0] = add2(sum2[0], sum2[1]);
+    float2 all = make_float2(top, pair_lo(sum2[0]) + pair_hi(sum2[0]));
     all = joined_warp(all);
     if constexpr (GROUP > 32) {
         if (g.cluster == 1) {
@@ -592,29 +600,39 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __rest
 // How many CTAs share a row: as many as its entries need registers of; then, while rows are so few that SMs are left over, more, down to
 // kLeastChunk entries each.
 constexpr int kLeastChunk = 2048;
-struct Shape {
-    int cluster, chunk;
-};
 template <typename T>
-Shape shape_of(int64_t rows, int64_t vocab) {
-    constexpr int N = Piece<T>::N;
-    int64_t cluster = ceil_div(vocab, (int64_t)512 * 8 * N);   // eight pieces a thread, the next row's beside them
-    if (cluster > kMaxCluster) cluster = kMaxCluster;          // (fp32: sixteen)
+int cluster_of(int64_t rows, int64_t vocab) {
+    int64_t cluster = ceil_div(vocab, (int64_t)512 * 8 * Piece<T>::N);   // eight pieces a thread, the next row's beside them
+    if (cluster > kMaxCluster) cluster = kMaxCluster;                    // (fp32: sixteen)
     while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= kSMs && vocab >= cluster * 2 * kLeastChunk) cluster *= 2;
-    const int64_t chunk = ceil_div(ceil_div(vocab, cluster), (int64_t)N) * N;
-    return Shape{(int)ceil_div(vocab, chunk), (int)chunk};
+    return (int)cluster;
 }
-// Calls f<THREADS, P>() with the smallest CTA that has room for `chunk` entries.
-template <typename T, typename F>
-detox_status by_chunk(int chunk, F f) {
-    constexpr int N = Piece<T>::N;
-    if (chunk <= 128 * 1 * N) return f.template operator()<128, 1>();
-    if (chunk <= 128 * 4 * N) return f.template operator()<128, 4>();
-    if (chunk <= 256 * 4 * N) return f.template operator()<256, 4>();
-    if (chunk <= 256 * 8 * N) return f.template operator()<256, 8>();
-    if (chunk <= 512 * 8 * N) return f.template operator()<512, 8>();
-    if constexpr (N == 4) {
-        if (chunk <= 512 * 16 * N) return f.template operator()<512, 16>();
+// Calls f<THREADS, P>() for CTAs of `pieces` pieces: P is what a thread has, and the CTA the smallest of which that is at most eight, four in CTAs of 128 (they wait
+// less for one another).
+template <typename T, bool ANY, typename F>
+detox_status by_pieces(int pieces, F f) {
+    switch (ceil_div(pieces, 128)) {
+        case 1: return f.template operator()<128, 1>();
+        case 2: return f.template operator()<128, 2>();
+        case 3: return f.template operator()<128, 3>();
+        case 4: return f.template operator()<128, 4>();
+    }
+    switch (ceil_div(pieces, 256)) {
+        case 3: return f.template operator()<256, 3>();
+        case 4: return f.template operator()<256, 4>();
+        case 5: return f.template operator()<256, 5>();
+        case 6: return f.template operator()<256, 6>();
+        case 7: return f.template operator()<256, 7>();
+        case 8: return f.template operator()<256, 8>();
+    }
+    switch (ceil_div(pieces, 512)) {
+        case 5: return f.template operator()<512, 5>();
+        case 6: return f.template operator()<512, 6>();
+        case 7: return f.template operator()<512, 7>();
+        case 8: return f.template operator()<512, 8>();
+    }
+    if constexpr (ANY && sizeof(T) == 4) {
+        if (pieces <= 512 * 16) return f.template operator()<512, 16>();
     }
     return DETOX_ERR_UNSUPPORTED;
 }
@@ -639,13 +657,13 @@ bool pieces(const void* p, int64_t ld) {
 // clusters: how many parts the loss has
 template <typename T>
 detox_status policy_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
-    const Shape shape = shape_of<T>(g.rows, g.vocab);
-    g.cluster = shape.cluster;
-    g.chunk = shape.chunk;
+    g.cluster = cluster_of<T>(g.rows, g.vocab);
+    g.pieces = (int)ceil_div((int64_t)g.vocab, (int64_t)Piece<T>::N);
     g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
     g.dz_vec = pieces<T>(g.dZ, g.lddz);
-    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec)) return by_chunk<T>(g.chunk, Policy<T, false>{g, clusters, s});
-    return by_chunk<T>(g.chunk, Policy<T, true>{g, clusters, s});
+    const int most = (int)ceil_div((int64_t)g.pieces, (int64_t)g.cluster);
+    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec) && most <= 512 * 8) return by_pieces<T, false>(most, Policy<T, false>{g, clusters, s});
+    return by_pieces<T, true>(most, Policy<T, true>{g, clusters, s});
 }
 
 // A warp for a row of up to 8 pieces a lane; else a CTA, or where rows are few a cluster, as long as its threads have pieces for a turn each.
