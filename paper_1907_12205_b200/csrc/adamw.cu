@@ -4,13 +4,15 @@
 //
 // Bound by HBM: every buffer is read once and written once (fp32 weights and states: 28 bytes an entry; bf16 weights, fp32 masters and
 // gradients, 8-bit states: 18).  The tensors' pointers travel as kernel parameters, so a step is one launch for each few hundred of them,
-// with nothing to copy and nothing to set up, and a captured one keeps them; tensors of different types take a launch for each kind.  A CTA takes a few thousand entries at a time, a warp 128 of them, 4 a lane, so that a block's scale is one warp-wide reduction and every access of a warp is contiguous: 16 bytes a lane in fp32, and where a buffer is not aligned for
-// that, single entries dealt round the lanes.
+// with nothing to copy and nothing to set up, and a captured one keeps them; tensors of different types take a launch for each kind.  A warp takes a block of 128 entries, 4 a lane, so that a block's scale is one
+// warp-wide reduction and every access of a warp is contiguous: 16 bytes a lane in fp32, and where a buffer is not aligned for that, single entries dealt round the
+// lanes.  Tensors whose buffers are all out of alignment by the same number of entries (slices of vectors of one layout) are taken from the boundary before their first one on.
 //
 // 8 bits: m and sqrt(v) as e4m3 numbers with a power-of-two scale for each block.  Of v the root is kept, since its range is half as
 // wide (v's would leave the form's 18 binary orders).  Rounding is random: added to the bits that the form drops, 16 random ones round up or down with
 // the right mean; a sum of thousands of steps that each change an entry by less than its spacing keeps its mean that way.
 #include <cmath>
+#include <cstring>
 
 #include "worker.cuh"
 
@@ -19,10 +21,14 @@ namespace detox {
 namespace {
 
 constexpr int kThreads = 256;
-// Blocks of 128 entries that a warp has in flight, and CTAs of an SM: what 64 Ki registers allow
-template <bool EIGHT> constexpr int kBlocks = EIGHT ? 2 : 2;
-template <bool EIGHT> constexpr int kCtas = EIGHT ? 4 : 4;
-template <bool EIGHT> constexpr int kUnit = kBlocks<EIGHT> * kKeepBlock * (kThreads / 32);   // entries that a CTA takes at a time
+constexpr int kCtas = 4;                         // on an SM
+// Blocks of 128 entries that a warp has in flight.  32 bits: two take 112 us for 21.7 M entries, one 100.  8 bits: 169 M entries take 600 us with one, 575 with two.
+template <bool EIGHT> constexpr int kBlocks = EIGHT ? 2 : 1;
+template <bool EIGHT> constexpr int kPart = kBlocks<EIGHT> * kKeepBlock * (kThreads / 32);   // entries that a CTA has in flight
+// Entries that a CTA takes at a time.  8 bits: two parts, so that the scales that it writes fill sectors of 32 bytes, by one store.  As single bytes, from several SMs into
+// one sector, they took a fifth of the time (618 us without any rounding, 498 without the scales' stores).
+template <bool EIGHT> constexpr int kUnit = EIGHT ? 2 * kPart<EIGHT> : kPart<EIGHT>;
+constexpr int kScales = kUnit<true> / kKeepBlock;
 constexpr int kKinds = 3 * 3 * 2;                // types of weights and gradients, with a master copy or without
 
 struct Tensor {
@@ -37,9 +43,11 @@ struct Tensor {
     float weight_decay;
     uint32_t key;
     bool vec;                                    // every buffer is aligned for a lane's 4 entries
+    int32_t skip;                                // the first entries are not the tensor's (the pointers are that far before it)
 };
 struct Numbers {
-    float lr, beta1, beta2, rest1, rest2, eps, grad_scale;   // rest: 1 - beta
+    uint64_t beta1, beta2, rest1, rest2, eps, grad_scale;   // twice each, as the packed arithmetic takes them; rest: 1 - beta
+    float lr;
     float c1, root_c2;                           // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     float log_beta1, log_beta2;
     uint32_t seed, step;
@@ -57,12 +65,14 @@ struct Table {
 constexpr int kFew = 32, kMany = 336;
 static_assert(sizeof(Table<kMany>) + sizeof(Numbers) <= 32764, "kernel parameters");
 
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
-    x ^= x >> 16;
+__device__ __forceinline__ uint32_t mix_rest(uint32_t x) {
     x *= 0x85ebca6bu;
     x ^= x >> 13;
     x *= 0xc2b2ae35u;
     return x ^ (x >> 16);
+}
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+    return mix_rest(x ^ (x >> 16));
 }
 
 // The root and the inverse to a unit or so, an instruction each (sqrtf and a division cost some eight an entry).  Numbers below 2^-126 count as 0: as v they
@@ -78,95 +88,116 @@ __device__ __forceinline__ float inverse_of(float x) {
     return y;
 }
 
-// 4 entries of a lane: contiguous ones (VEC), or lane, lane + 32, ... of the block, where there are so many
+// 4 entries of a lane: contiguous ones from entry `at` on (VEC), or at, at + 32, ... of the block, where there are so many.  Offsets in 32 bits from a pointer that is the same
+// for all threads take no registers for addresses.
 template <bool VEC, typename T>
-__device__ __forceinline__ void load4(const T* from, int lane, int left, float (&f)[4]) {
+__device__ __forceinline__ void load4(const T* from, unsigned at, int low, int left, float (&f)[4]) {
     if constexpr (!VEC) {
+        const int lane = threadIdx.x % 32;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j] = 32 * j + lane < left ? to_f32(from[32 * j + lane]) : 0.f;
+        for (int j = 0; j < 4; ++j) f[j] = 32 * j + lane >= low && 32 * j + lane < left ? to_f32(from[at + 32u * j]) : 0.f;
     } else if constexpr (sizeof(T) == 4) {
-        const float4 x = ld_stream_f4(reinterpret_cast<const float*>(from) + 4 * lane);
+        const float4 x = ld_stream_f4(reinterpret_cast<const float*>(from) + at);
         f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
     } else {
-        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(from + 4 * lane));
+        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(from + at));
         const float2 a = unpack2<T>(x.x), b = unpack2<T>(x.y);
         f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
     }
 }
 template <bool VEC, typename T>
-__device__ __forceinline__ void store4(T* to, int lane, int left, const float (&f)[4]) {
+__device__ __forceinline__ void store4(T* to, unsigned at, int low, int left, const float (&f)[4]) {
     if constexpr (!VEC) {
+        const int lane = threadIdx.x % 32;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (32 * j + lane < left) to[32 * j + lane] = from_f32<T>(f[j]);
+            if (32 * j + lane >= low && 32 * j + lane < left) to[at + 32u * j] = from_f32<T>(f[j]);
     } else if constexpr (sizeof(T) == 4) {
-        st_stream_f4(reinterpret_cast<float*>(to) + 4 * lane, make_float4(f[0], f[1], f[2], f[3]));
+        st_stream_f4(reinterpret_cast<float*>(to) + at, make_float4(f[0], f[1], f[2], f[3]));
     } else {
-        __stcs(reinterpret_cast<uint2*>(to + 4 * lane), make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])));
+        __stcs(reinterpret_cast<uint2*>(to + at), make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])));
     }
 }
 // 4 bytes of a lane, as one word
 template <bool VEC>
-__device__ __forceinline__ uint32_t load_bytes(const uint8_t* from, int lane, int left) {
+__device__ __forceinline__ uint32_t load_bytes(const uint8_t* from, unsigned at, int left) {
     uint32_t q = 0u;
     if constexpr (VEC) {
-        q = __ldcs(reinterpret_cast<const unsigned int*>(from) + lane);
+        q = __ldcs(reinterpret_cast<const unsigned int*>(from + at));
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (32 * j + lane < left) q |= (uint32_t)from[32 * j + lane] << (8 * j);
+            if (32 * j + (int)(threadIdx.x % 32) < left) q |= (uint32_t)from[at + 32u * j] << (8 * j);
     }
     return q;
 }
 template <bool VEC>
-__device__ __forceinline__ void store_bytes(uint8_t* to, int lane, int left, uint32_t q) {
+__device__ __forceinline__ void store_bytes(uint8_t* to, unsigned at, int left, uint32_t q) {
     if constexpr (VEC) {
-        __stcs(reinterpret_cast<unsigned int*>(to) + lane, q);
+        __stcs(reinterpret_cast<unsigned int*>(to + at), q);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (32 * j + lane < left) to[32 * j + lane] = (uint8_t)(q >> (8 * j));
+            if (32 * j + (int)(threadIdx.x % 32) < left) to[at + 32u * j] = (uint8_t)(q >> (8 * j));
     }
 }
 
-// The 8-bit form of a block, 4 entries a lane, rounded at random with `bits` (16 of them an entry).  POSITIVE: entries > 0 stay so.
+__device__ __forceinline__ float largest(float a, float b) {   // NaN where one is NaN
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Entries x, already divided by the scale, as e4m3 numbers, where some are small or not finite: a function of its own, since its registers are missed where it is not needed
+__device__ __noinline__ uint32_t small_at_random(float x0, float x1, float x2, float x3, uint32_t bits01, uint32_t bits23, bool positive) {
+    const float x[4] = {x0, x1, x2, x3};
+    const uint32_t bits[4] = {bits01 & 0xffffu, bits01 >> 16, bits23 & 0xffffu, bits23 >> 16};
+    float r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float v = fabsf(x[j]);
+        const float lift = v < 0.015625f ? 0.015625f : 0.f;
+        float k = __uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift;
+        if (positive && v > 0.f && k == 0.f) k = 0.001953125f;
+        r[j] = v <= 448.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);
+    }
+    return keep4(r[0], r[1], r[2], r[3]);
+}
+
+// The 8-bit form of a block, 4 entries a lane (two packed pairs), rounded at random with `bits` (16 of them an entry).  POSITIVE: entries > 0 stay so.
 // Inf and NaN become NaN and do not count for the scale.
 //
 // e4m3 keeps 3 of the 23 bits behind an fp32 number's first one, so the random bits are added to the number's own above the 4th lowest, and
 // the lowest 20 cut off.  Below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5: such an entry is lifted by 2^-6 for it.  Blocks
 // without such entries (most: they are 2^-15 of the block's largest) and with finite ones only need none of that.
 template <bool POSITIVE>
-__device__ __forceinline__ uint32_t keep_at_random(const float (&x)[4], const uint32_t (&bits)[4], uint32_t* q) {
-    uint32_t a[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) a[j] = POSITIVE ? __float_as_uint(x[j]) : __float_as_uint(x[j]) & 0x7fffffffu;   // (a root of NaN has no sign)
-    uint32_t top = __reduce_max_sync(0xffffffffu, max(max(a[0], a[1]), max(a[2], a[3])));
+__device__ __forceinline__ uint32_t keep_at_random(const uint64_t (&p)[2], const uint32_t (&bits)[4], uint32_t* q) {
+    const float x[4] = {pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])};
+    // (positive numbers and NaN are in order as integers, too)
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(largest(fabsf(x[0]), fabsf(x[1])), largest(fabsf(x[2]), fabsf(x[3])))) & 0x7fffffffu);
+    const uint32_t least = __reduce_min_sync(0xffffffffu, __float_as_uint(fminf(fminf(fabsf(x[0]), fabsf(x[1])), fminf(fabsf(x[2]), fabsf(x[3])))));
     const bool finite = top < 0x7f800000u;
     if (!finite) {
         top = 0u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (a[j] < 0x7f800000u) top = max(top, a[j]);
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a = __float_as_uint(x[j]) & 0x7fffffffu;
+            if (a < 0x7f800000u) top = max(top, a);
+        }
         top = __reduce_max_sync(0xffffffffu, top);
     }
     const uint32_t e = keep_exponent(__uint_as_float(top));
     const float inverse = keep_inverse(e);
-    const uint32_t least = __reduce_min_sync(0xffffffffu, min(min(a[0], a[1]), min(a[2], a[3])));
     float r[4];
     if (finite && __uint_as_float(least) * inverse >= 0.015625f) {
+        const uint64_t inverse2 = pair_of(inverse, inverse), a = mul2(p[0], inverse2), b = mul2(p[1], inverse2);
+        const float y[4] = {pair_lo(a), pair_hi(a), pair_lo(b), pair_hi(b)};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(x[j] * inverse) + (bits[j] << 4)) & 0xfff00000u);
+        for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(y[j]) + (bits[j] << 4)) & 0xfff00000u);
+        *q = keep4(r[0], r[1], r[2], r[3]);
     } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float v = fabsf(x[j]) * inverse;
-            const float lift = v < 0.015625f ? 0.015625f : 0.f;
-            float k = __uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift;
-            if (POSITIVE && v > 0.f && k == 0.f) k = 0.001953125f;
-            r[j] = v <= 448.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);
-        }
+        *q = small_at_random(x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse, bits[0] | bits[1] << 16, bits[2] | bits[3] << 16, POSITIVE);
     }
-    *q = keep4(r[0], r[1], r[2], r[3]);
     return e;
 }
 
@@ -174,87 +205,105 @@ struct Now {
     float lr, c1, root_c2;
     uint32_t seed;                               // of the tensor's random bits
 };
+__device__ __forceinline__ uint64_t both(float v) { return pair_of(v, v); }
+__device__ __forceinline__ uint64_t pairs_at(const float (&f)[4], int k) { return pair_of(f[2 * k], f[2 * k + 1]); }
 
-// A unit of tensor t from entry `at` on.  PT, GT: of the weights and the gradient
+// A part of tensor t from entry `at` on.  PT, GT: of the weights and the gradient.  The arithmetic goes two entries at a time.  VEC: the new scales go to `scales`,
+// a row for m and one for sqrt(v).
 template <bool EIGHT, bool VEC, typename PT, typename GT, bool MASTER>
-__device__ __forceinline__ void step_unit(const Tensor& t, int64_t at, const Numbers& number, const Now& now) {
+__device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Numbers& number, const Now& now, uint8_t* scales) {
     constexpr int B = kBlocks<EIGHT>, kStep = kKeepBlock * (kThreads / 32);
     const int lane = threadIdx.x % 32, first = threadIdx.x / 32 * kKeepBlock;   // this warp's blocks start at at + first + b kStep
+    const unsigned own = VEC ? 4 * threadIdx.x : first + lane;                  // and this lane's entries of them
     const GT* G = static_cast<const GT*>(t.G) + at;
     PT* P = static_cast<PT*>(t.P) + at;
     float* master = t.master + at;
-    const int rest = t.n - at < kUnit<EIGHT> ? (int)(t.n - at) : kUnit<EIGHT>;
+    uint8_t *M8 = static_cast<uint8_t*>(t.M) + at, *V8 = static_cast<uint8_t*>(t.V) + at;
+    float *M = static_cast<float*>(t.M) + at, *V = static_cast<float*>(t.V) + at;
+    const uint8_t *ME = t.ME + at / kKeepBlock, *VE = t.VE + at / kKeepBlock;
+    const int rest = t.n - at < kPart<EIGHT> ? (int)(t.n - at) : kPart<EIGHT>;
     float g[B][4], p[B][4];
     float m32[EIGHT ? 1 : B][4], v32[EIGHT ? 1 : B][4];
     uint32_t mq[B], vq[B];
     float ms[B], vs[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const int i = first + b * kStep;
-        const int left = rest - i;
+        const int i = first + b * kStep, left = rest - i, low = at == 0 ? t.skip - i : 0;
         if (!VEC && left <= 0) continue;
-        load4<VEC>(G + i, lane, left, g[b]);
-        if constexpr (MASTER) load4<VEC>(master + i, lane, left, p[b]);
-        else load4<VEC>(P + i, lane, left, p[b]);
+        load4<VEC>(G, own + b * kStep, low, left, g[b]);
+        if constexpr (MASTER) load4<VEC>(master, own + b * kStep, low, left, p[b]);
+        else load4<VEC>(P, own + b * kStep, low, left, p[b]);
         if constexpr (EIGHT) {
-            mq[b] = load_bytes<VEC>(static_cast<const uint8_t*>(t.M) + at + i, lane, left);
-            vq[b] = load_bytes<VEC>(static_cast<const uint8_t*>(t.V) + at + i, lane, left);
-            ms[b] = keep_scale_of_byte(t.ME[(at + i) / kKeepBlock]);
-            vs[b] = keep_scale_of_byte(t.VE[(at + i) / kKeepBlock]);
+            mq[b] = load_bytes<VEC>(M8, own + b * kStep, left);
+            vq[b] = load_bytes<VEC>(V8, own + b * kStep, left);
+            ms[b] = keep_scale_of_byte(ME[(unsigned)i / kKeepBlock]);
+            vs[b] = keep_scale_of_byte(VE[(unsigned)i / kKeepBlock]);
         } else {
-            load4<VEC>(static_cast<const float*>(t.M) + at + i, lane, left, m32[b]);
-            load4<VEC>(static_cast<const float*>(t.V) + at + i, lane, left, v32[b]);
+            load4<VEC>(M, own + b * kStep, low, left, m32[b]);
+            load4<VEC>(V, own + b * kStep, low, left, v32[b]);
         }
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const int i = first + b * kStep;
-        const int left = rest - i;
+        const int i = first + b * kStep, left = rest - i, low = at == 0 ? t.skip - i : 0;
         if (!VEC && left <= 0) continue;
-        float m[4], v[4], root[4];
+        uint64_t m[2], v[2], root[2];
         if constexpr (EIGHT) {
-            taken4(mq[b], m);
-            taken4(vq[b], v);
+            float f[4];
+            taken4(mq[b], f);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) m[k] = mul2(pairs_at(f, k), both(ms[b]));
+            taken4(vq[b], f);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v[k] = mul2(pairs_at(f, k), both(vs[b]));
+                v[k] = mul2(v[k], v[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                m[k] = pairs_at(m32[b], k);
+                v[k] = pairs_at(v32[b], k);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (EIGHT) {
-                m[j] *= ms[b];
-                v[j] *= vs[b];
-                v[j] *= v[j];
-            } else {
-                m[j] = m32[b][j];
-                v[j] = v32[b][j];
-            }
-            const float x = g[b][j] * number.grad_scale;
-            m[j] = fmaf(number.beta1, m[j], number.rest1 * x);
-            v[j] = fmaf(number.beta2, v[j], number.rest2 * (x * x));
-            root[j] = root_of(v[j]);
-            const float direction = m[j] * now.c1 * inverse_of(fmaf(root[j], now.root_c2, number.eps));
-            p[b][j] = fmaf(-now.lr, fmaf(t.weight_decay, p[b][j], direction), p[b][j]);
+        for (int k = 0; k < 2; ++k) {
+            const uint64_t x = mul2(pairs_at(g[b], k), number.grad_scale);
+            m[k] = fma2(number.beta1, m[k], mul2(number.rest1, x));
+            v[k] = fma2(number.beta2, v[k], mul2(number.rest2, mul2(x, x)));
+            root[k] = pair_of(root_of(pair_lo(v[k])), root_of(pair_hi(v[k])));
+            const uint64_t below = fma2(root[k], both(now.root_c2), number.eps);
+            const uint64_t way = mul2(mul2(m[k], both(now.c1)), pair_of(inverse_of(pair_lo(below)), inverse_of(pair_hi(below))));
+            const uint64_t was = pairs_at(p[b], k), is = fma2(both(-now.lr), fma2(both(t.weight_decay), was, way), was);
+            p[b][2 * k] = pair_lo(is);
+            p[b][2 * k + 1] = pair_hi(is);
         }
-        if constexpr (MASTER) store4<VEC>(master + i, lane, left, p[b]);
-        store4<VEC>(P + i, lane, left, p[b]);
+        if constexpr (MASTER) store4<VEC>(master, own + b * kStep, low, left, p[b]);
+        store4<VEC>(P, own + b * kStep, low, left, p[b]);
         if constexpr (EIGHT) {
             uint32_t rm[4], rv[4];
+            const uint32_t entry = (uint32_t)at + own + b * kStep;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t h = mix(now.seed ^ ((uint32_t)at + (uint32_t)(i + (VEC ? 4 * lane + j : 32 * j + lane))));
+                // (four entries from a multiple of four on differ in the lowest bits alone, which the first shift drops)
+                const uint32_t h = VEC ? mix_rest((now.seed ^ entry) ^ ((now.seed ^ entry) >> 16) ^ (uint32_t)j) : mix(now.seed ^ (entry + 32u * j));
                 rm[j] = h & 0xffffu;
                 rv[j] = h >> 16;
             }
             uint32_t q;
             const uint32_t me = keep_at_random<false>(m, rm, &q);
-            store_bytes<VEC>(static_cast<uint8_t*>(t.M) + at + i, lane, left, q);
+            store_bytes<VEC>(M8, own + b * kStep, left, q);
             const uint32_t ve = keep_at_random<true>(root, rv, &q);
-            store_bytes<VEC>(static_cast<uint8_t*>(t.V) + at + i, lane, left, q);
+            store_bytes<VEC>(V8, own + b * kStep, left, q);
             if (lane == 0) {
-                t.ME[(at + i) / kKeepBlock] = (uint8_t)me;
-                t.VE[(at + i) / kKeepBlock] = (uint8_t)ve;
+                (VEC ? scales + i / kKeepBlock : t.ME + (at + i) / kKeepBlock)[0] = (uint8_t)me;
+                (VEC ? scales + kScales + i / kKeepBlock : t.VE + (at + i) / kKeepBlock)[0] = (uint8_t)ve;
             }
         } else {
-            store4<VEC>(static_cast<float*>(t.M) + at + i, lane, left, m);
-            store4<VEC>(static_cast<float*>(t.V) + at + i, lane, left, v);
+            const float fm[4] = {pair_lo(m[0]), pair_hi(m[0]), pair_lo(m[1]), pair_hi(m[1])};
+            const float fv[4] = {pair_lo(v[0]), pair_hi(v[0]), pair_lo(v[1]), pair_hi(v[1])};
+            store4<VEC>(M, own + b * kStep, low, left, fm);
+            store4<VEC>(V, own + b * kStep, low, left, fv);
         }
     }
 }
@@ -262,11 +311,11 @@ __device__ __forceinline__ void step_unit(const Tensor& t, int64_t at, const Num
 // Tensors of any alignment, and the ends of all: a function of its own, since beside the other's its registers do not fit (5 to 80 words spilled)
 template <bool EIGHT, typename PT, typename GT, bool MASTER>
 __device__ __noinline__ void step_any(const Tensor& t, int64_t at, const Numbers& number, Now now) {
-    step_unit<EIGHT, false, PT, GT, MASTER>(t, at, number, now);
+    for (int64_t end = at + kUnit<EIGHT>; at < end && at < t.n; at += kPart<EIGHT>) step_part<EIGHT, false, PT, GT, MASTER>(t, at, number, now, nullptr);
 }
 
 template <bool EIGHT, typename PT, typename GT, bool MASTER, int CAP>
-__global__ void __launch_bounds__(kThreads, kCtas<EIGHT>) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Numbers number) {
+__global__ void __launch_bounds__(kThreads, kCtas) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Numbers number) {
     pdl_trigger();
     pdl_wait();
     float lr = number.lr, c1 = number.c1, root_c2 = number.root_c2;
@@ -283,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<EIGHT>) adamw_kernel(const __g
     Now now{lr, c1, root_c2, 0u};
     const uint32_t start = EIGHT ? mix(number.seed + 0x9e3779b9u * step) : 0u;
     const int64_t units = table.end[table.count - 1];
-    int which = 0;
+    int which = 0, turn = 0;
     for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
         if (unit >= table.end[which]) {
             // the first tensor that ends behind this unit
@@ -298,12 +347,33 @@ __global__ void __launch_bounds__(kThreads, kCtas<EIGHT>) adamw_kernel(const __g
         const Tensor& t = table.of[which];
         const int64_t at = (unit - (which ? table.end[which - 1] : 0)) * kUnit<EIGHT>;
         if (EIGHT) now.seed = mix(start + t.key);
-        if (t.vec && t.n - at >= kUnit<EIGHT>) step_unit<EIGHT, true, PT, GT, MASTER>(t, at, number, now);
-        else step_any<EIGHT, PT, GT, MASTER>(t, at, number, now);
+        if (!t.vec || t.n - at < kUnit<EIGHT> || at < t.skip) {
+            step_any<EIGHT, PT, GT, MASTER>(t, at, number, now);
+        } else if constexpr (!EIGHT) {
+            step_part<false, true, PT, GT, MASTER>(t, at, number, now, nullptr);
+        } else {
+            // (written again two units on, and every thread has passed the barrier between)
+            __shared__ uint8_t scales[2][2 * kScales];
+            uint8_t* here = scales[turn & 1];
+            ++turn;
+#pragma unroll 1
+            for (int part = 0; part < 2; ++part)
+                step_part<true, true, PT, GT, MASTER>(t, at + part * kPart<true>, number, now, here + part * (kScales / 2));
+            __syncthreads();
+            if (threadIdx.x < 2 * kScales) (threadIdx.x < kScales ? t.ME + threadIdx.x : t.VE + (threadIdx.x - kScales))[at / kKeepBlock] = here[threadIdx.x];
+        }
     }
 }
 
-bool aligned_for(const void* p, int size) { return aligned_to(p, (size_t)size * 4); }
+uint64_t twice(double v) {
+    const float f = (float)v;
+    uint32_t w;
+    memcpy(&w, &f, sizeof w);
+    return ((uint64_t)w << 32) | w;
+}
+
+// how many entries of `size` bytes p lies behind the last place that is aligned for four of them
+int behind(const void* p, int size) { return (int)(reinterpret_cast<uintptr_t>(p) / (uintptr_t)size % 4); }
 
 // The tensors of one kind among those from *from on, as many as the table holds.
 struct Kind {
@@ -321,20 +391,27 @@ detox_status step_table(const Numbers& number, const Kind& kind, const detox_ada
         int n = 0;
         for (; from != end && n < CAP; ++from) {
             if (from->n == 0 || !(kind_of(*from) == kind)) continue;
-            const int ss = EIGHT ? 1 : 4;
+            const int ss = EIGHT ? 1 : 4, off = behind(from->P, sizeof(PT));
+            const bool even = behind(from->G, sizeof(GT)) == off && (!MASTER || behind(from->master, 4) == off) && behind(from->M, ss) == off && behind(from->V, ss) == off;
             Tensor& t = table.of[n];
-            t.P = from->P; t.G = from->G; t.master = from->master;
-            t.M = from->M; t.ME = from->ME; t.V = from->V; t.VE = from->VE;
-            t.n = from->n;
+            // blocks of 8-bit states start with the tensor
+            t.vec = even && (off == 0 || !EIGHT);
+            t.skip = t.vec ? off : 0;
+            t.P = static_cast<PT*>(from->P) - t.skip;
+            t.G = static_cast<const GT*>(from->G) - t.skip;
+            t.master = MASTER ? from->master - t.skip : nullptr;
+            t.M = static_cast<char*>(from->M) - t.skip * ss;
+            t.V = static_cast<char*>(from->V) - t.skip * ss;
+            t.ME = from->ME; t.VE = from->VE;
+            t.n = from->n + t.skip;
             t.weight_decay = from->weight_decay;
             t.key = from->key;
-            t.vec = aligned_for(t.P, sizeof(PT)) && aligned_for(t.G, sizeof(GT)) && aligned_for(t.master, 4) && aligned_for(t.M, ss) && aligned_for(t.V, ss);
             units += ceil_div(t.n, (int64_t)kUnit<EIGHT>);
             table.end[n++] = units;
         }
         if (n == 0) break;
         table.count = n;
-        const int64_t most = (int64_t)kSMs * kCtas<EIGHT>;
+        const int64_t most = (int64_t)kSMs * kCtas;
         const detox_status st = launch_chained(adamw_kernel<EIGHT, PT, GT, MASTER, CAP>, (unsigned)(units < most ? units : most), kThreads, 0, 1, s, table, number);
         if (st != DETOX_OK) return st;
     }
@@ -371,10 +448,10 @@ detox_status step_types(const Numbers& number, const Kind& kind, const detox_ada
 detox_status launch_adamw(const detox_adamw_desc& d, const detox_adamw_tensor* tensors, int64_t count, cudaStream_t s) {
     Numbers number = {};
     number.lr = (float)d.lr;
-    number.beta1 = (float)d.beta1; number.beta2 = (float)d.beta2;
-    number.rest1 = (float)(1.0 - d.beta1); number.rest2 = (float)(1.0 - d.beta2);
-    number.eps = (float)d.eps;
-    number.grad_scale = d.grad_scale;
+    number.beta1 = twice(d.beta1); number.beta2 = twice(d.beta2);
+    number.rest1 = twice(1.0 - d.beta1); number.rest2 = twice(1.0 - d.beta2);
+    number.eps = twice(d.eps);
+    number.grad_scale = twice(d.grad_scale);
     number.log_beta1 = (float)log(d.beta1); number.log_beta2 = (float)log(d.beta2);
     number.c1 = (float)(1.0 / (1.0 - pow(d.beta1, (double)d.step)));
     number.root_c2 = (float)sqrt(1.0 / (1.0 - pow(d.beta2, (double)d.step)));
