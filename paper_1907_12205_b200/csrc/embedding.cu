@@ -11,8 +11,8 @@
 //      row numbers in order.  The order of the tokens is that of their places: CTA by CTA, and in a CTA ascending.
 //   2. sum_rows: the sorted tokens are cut into spans of equal length, whatever lies in them.  A warp has a span and a slice of the columns; it adds up
 //      rows in registers and writes dW whenever the token changes.  The sum of a token that lies in several spans goes to the
-//      workspace in parts.  Other CTAs of the same launch write zeros to the rows of tokens that do not occur.
-//   3. join_spans: adds those parts, span by span.
+//      workspace in parts, and the warp that leaves the last of them adds them, in the spans' order (a counter tells, so nobody waits).
+//      Other CTAs of the same launch write zeros to the rows of tokens that do not occur.
 #include "worker.cuh"
 
 namespace detox {
@@ -57,9 +57,11 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const T* __restrict__ 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortRows = kSortThreads;        // rows of the vocabulary that a CTA can own: a thread each
 constexpr int kSumWarps = 48;                  // warps of an SM that there are spans for, where there are tokens enough
-constexpr int kAhead = 8;                      // rows of dY that a warp has in flight; a span's length is a multiple
+// Rows of dY that a warp has in flight; a span's length is a multiple.  With a gradient to add to, a warp waits for its row at every token, so spans are shorter
+// where there are few tokens.
+template <bool ADD> constexpr int kAhead = ADD ? 4 : 8;
+constexpr int kSortAhead = 8;
 constexpr int kZeroPlaces = 32;                // places that a CTA looks after
-constexpr int kJoinThreads = 512;
 
 // Place p is row (i << bits) + c of the vocabulary with c = p / per, i = p % per; a few at the ends of CTAs' stretches are none.
 struct Places {
@@ -76,10 +78,11 @@ struct Plan {
     int slices;                                // slices of 32 pieces
     int spans, length;                         // length: tokens of a span
     int64_t ldp;                               // pitch of the partial sums
-    size_t order, sorted, starts, info, head, tail, bytes;   // offsets in the workspace
+    size_t order, sorted, starts, left, head, tail, bytes;   // offsets in the workspace
 };
 // `entries`: of a 16-byte piece
-Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries) {
+Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries, bool add) {
+    const int ahead = add ? kAhead<true> : kAhead<false>;
     Plan p = {};
     p.rows = rows;
     p.cols = cols;
@@ -88,15 +91,15 @@ Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries) {
     p.places = Places{(int32_t)vocab, (int32_t)ceil_div(vocab, (int64_t)1 << bits), bits};
     p.slices = (int)ceil_div(cols, (int64_t)32 * entries);
     p.ldp = ceil_div(cols, (int64_t)4) * 4;
-    p.length = (int)(ceil_div(rows * p.slices, (int64_t)kSMs * kSumWarps * kAhead) * kAhead);
-    if (p.length < kAhead) p.length = kAhead;
+    p.length = (int)(ceil_div(rows * p.slices, (int64_t)kSMs * kSumWarps * ahead) * ahead);
+    if (p.length < ahead) p.length = ahead;
     p.spans = (int)ceil_div(rows, (int64_t)p.length);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at = align_up(at + bytes); return was; };
     p.order = take((size_t)rows * 4);
     p.sorted = take((size_t)rows * 4);
     p.starts = take(((size_t)p.places.count() + 1) * 4);
-    p.info = take((size_t)p.spans * 8);
+    p.left = take((size_t)p.spans * (size_t)p.slices * 4);
     p.head = take((size_t)p.spans * (size_t)p.ldp * 4);
     p.tail = take((size_t)p.spans * (size_t)p.ldp * 4);
     p.bytes = at;
@@ -105,11 +108,11 @@ Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries) {
 
 // ---- 1. sorting -----------------------------------------------------------------------------------
 // order: the rows by their tokens' places, those of a token ascending; sorted: those places; starts: where each place's rows start, and behind the
-// last place how many there are (tokens outside the vocabulary are left out).  Dynamic shared memory: per x (kSortWarps + 1) int32.
+// last place how many there are (tokens outside the vocabulary are left out); left: counters for the next kernel, cleared.  Dynamic shared memory: per x (kSortWarps + 1) int32.
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __restrict__ tokens, int64_t rows, Places places,
                                                                    int32_t* __restrict__ order, int32_t* __restrict__ sorted,
-                                                                   int32_t* __restrict__ starts) {
+                                                                   int32_t* __restrict__ starts, int32_t* __restrict__ left, int64_t counters) {
     extern __shared__ int32_t hist[];          // [row][warp], a column more so that threads stepping through their rows do not collide
     __shared__ int32_t sums[kSortWarps];
     __shared__ int32_t start_of[kSortRows];
@@ -119,23 +122,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __re
     const int32_t own = (int32_t)blockIdx.x, mask = (1 << places.bits) - 1;
     for (int i = threadIdx.x; i < per * kPitch; i += kSortThreads) hist[i] = 0;
     pdl_wait();
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < counters; i += (int64_t)gridDim.x * kSortThreads) left[i] = 0;
     __syncthreads();
     // each warp has a stretch of the tokens
     const int64_t stretch = (rows + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
     const int64_t begin = warp * stretch, end = begin + stretch < rows ? begin + stretch : rows;
-    int32_t tok[kAhead];
+    int32_t tok[kSortAhead];
     auto fetch = [&](int64_t t0) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kSortAhead; ++i) {
             const int64_t t = t0 + i * 32 + lane, token = t < end ? (int64_t)tokens[t] : -1;
             tok[i] = token >= 0 && token < places.vocab ? (int32_t)token : -1;
         }
     };
     int32_t below = 0;
-    for (int64_t t0 = begin; t0 < end; t0 += 32 * kAhead) {
+    for (int64_t t0 = begin; t0 < end; t0 += 32 * kSortAhead) {
         fetch(t0);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kSortAhead; ++i) {
             below += tok[i] >= 0 && (tok[i] & mask) < own;
             if (tok[i] >= 0 && (tok[i] & mask) == own) atomicAdd(&hist[(tok[i] >> places.bits) * kPitch + warp], 1);
         }
@@ -175,11 +179,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const I* __re
     if ((int)threadIdx.x < per) starts[own * per + threadIdx.x] = below + before + upto - total;
     if (threadIdx.x == kSortThreads - 1 && own == mask) starts[places.count()] = below + before + upto;
     __syncthreads();
-    const bool again = end - begin > 32 * kAhead;   // (else they are still there)
-    for (int64_t t0 = begin; t0 < end; t0 += 32 * kAhead) {
+    const bool again = end - begin > 32 * kSortAhead;   // (else they are still there)
+    for (int64_t t0 = begin; t0 < end; t0 += 32 * kSortAhead) {
         if (again) fetch(t0);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kSortAhead; ++i) {
             const bool mine = tok[i] >= 0 && (tok[i] & mask) == own;
             if (!__any_sync(0xffffffffu, mine)) continue;
             const int r = mine ? tok[i] >> places.bits : -1;
@@ -211,8 +215,8 @@ struct SumRows {
     int64_t lddw;
     bool w_vec;                                // 16-byte accesses to dW
     bool w_wide;                               // 32-byte stores
-    int32_t* info;                             // of each span: the place of which earlier spans have tokens (or -1), and whether it is complete here
-    float *head, *tail;
+    int32_t* left;                             // for each span and slice: how many parts of the place that the span completes are there
+    float *head, *tail;                        // parts: of the place that a span completes, of the one that goes on behind it
     int64_t ldp;
 };
 
@@ -258,6 +262,18 @@ __device__ __forceinline__ void load_sums(const D* row, int c, int cols, bool ve
     for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) p[j] = pair_of(f[2 * j], f[2 * j + 1]);
+}
+
+// N sums of a part, past L1 (another SM may have left them)
+template <int N>
+__device__ __forceinline__ void load_part(const float* row, int c, int cols, uint64_t (&p)[N / 2]) {
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c + j < cols) x = __ldcg(reinterpret_cast<const float4*>(row + c + j));   // (cols: a multiple of 4)
+        p[j / 2] = pair_of(x.x, x.y);
+        p[j / 2 + 1] = pair_of(x.z, x.w);
+    }
 }
 
 // zeros to the rows of kZeroPlaces places that have no tokens
@@ -306,16 +322,9 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
     if (span >= g.spans) return;
     const int32_t n = g.starts[g.places.count()], from = span * g.length;
     const int32_t to = from + g.length < n ? from + g.length : n;
-    if (from >= to) {
-        if (slice == 0 && lane == 0) g.info[2 * span] = -1;
-        return;
-    }
+    if (from >= to) return;
     int32_t place = g.sorted[from];
     const bool open = from > 0 && g.sorted[from - 1] == place, goes_on = to < n && g.sorted[to] == g.sorted[to - 1];
-    if (slice == 0 && lane == 0) {
-        g.info[2 * span] = open ? place : -1;
-        g.info[2 * span + 1] = g.sorted[to - 1] != place || !goes_on;
-    }
     const int c = (slice * 32 + lane) * N;
     const T* dY = static_cast<const T*>(g.dY) + c;
     D* dW = static_cast<D*>(g.dW);
@@ -325,29 +334,50 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
     const uint64_t scale2 = pair_of(g.scale, g.scale);
     bool head = open;
     int64_t row = 0;                           // of dW, for `place`
+    auto write = [&] {
+        D* at = dW + row * g.lddw;
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) acc[j] = mul2(acc[j], scale2);
+        if constexpr (ADD) {
+            uint64_t old[N / 2];
+            load_sums<D, N>(at, c, g.cols, g.w_vec, old);
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], old[j]);
+        }
+        store_sums<D, N>(at, c, g.cols, g.w_vec, g.w_wide, acc);
+    };
+    // a part of a place's sum is complete; the warp that leaves the last one adds them all
+    auto part = [&](float* to) {
+        store_sums<float, N>(to + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
+        const int first = g.starts[place] / g.length, last = (g.starts[place + 1] - 1) / g.length;
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        if (lane == 0) before = atomicAdd(&g.left[(int64_t)last * g.slices + slice], 1);
+        if (__shfl_sync(0xffffffffu, before, 0) < last - first) return;
+        __threadfence();
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
+#pragma unroll 4
+        for (int s = first; s <= last; ++s) {
+            uint64_t x[N / 2];
+            load_part<N>((s < last ? g.tail : g.head) + (int64_t)s * g.ldp, c, (int)g.ldp, x);
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], x[j]);
+        }
+        write();
+    };
     // the sum of a place is complete here
     auto close = [&] {
-        if (head) {
-            store_sums<float, N>(g.head + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
-            head = false;
-        } else {
-            D* at = dW + row * g.lddw;
-#pragma unroll
-            for (int j = 0; j < N / 2; ++j) acc[j] = mul2(acc[j], scale2);
-            if constexpr (ADD) {
-                uint64_t old[N / 2];
-                load_sums<D, N>(at, c, g.cols, g.w_vec, old);
-#pragma unroll
-                for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], old[j]);
-            }
-            store_sums<D, N>(at, c, g.cols, g.w_vec, g.w_wide, acc);
-        }
+        if (head) part(g.head);
+        else write();
+        head = false;
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
     };
     int32_t order = 0, its_place = 0;          // of 32 tokens, one a lane
     int64_t its_row = 0;
-    for (int32_t k = from; k < to; k += kAhead) {
+    for (int32_t k = from; k < to; k += kAhead<ADD>) {
         const int at = (k - from) & 31;
         if (at == 0) {
             const bool there = k + lane < to;
@@ -355,12 +385,12 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
             its_place = there ? g.sorted[k + lane] : -1;
             its_row = there ? g.places.row(its_place) : 0;
         }
-        uint4 raw[kAhead];
+        uint4 raw[kAhead<ADD>];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+        for (int i = 0; i < kAhead<ADD>; ++i)
             raw[i] = load_piece<ANY>(dY + (int64_t)__shfl_sync(0xffffffffu, order, at + i) * g.lddy, 0, k + i < to ? g.cols - c : 0, g.span);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kAhead<ADD>; ++i) {
             const int32_t p = __shfl_sync(0xffffffffu, its_place, at + i);
             const int64_t r = __shfl_sync(0xffffffffu, its_row, at + i);
             if (p >= 0 && p != place) {
@@ -374,59 +404,8 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
             for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], f[j]);
         }
     }
-    if (goes_on) store_sums<float, N>(g.tail + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
+    if (goes_on) part(g.tail);
     else close();
-}
-
-// ---- 3. tokens that lie in several spans -----------------------------------------------------------
-// A CTA for each span that completes a place which was open at its start: the sum of the earlier spans' parts and its own.
-template <typename D, bool ADD>
-__global__ void __launch_bounds__(kJoinThreads) join_spans_kernel(const int32_t* __restrict__ info, Places places, const float* __restrict__ head,
-                                                                  const float* __restrict__ tail, int64_t ldp, int cols, float scale,
-                                                                  D* __restrict__ dW, int64_t lddw) {
-    constexpr int kQuads = 128, kGroups = kJoinThreads / kQuads;   // of 4 columns; of parts, every kGroups-th one
-    __shared__ float4 sm[kGroups][kQuads];
-    pdl_trigger();
-    pdl_wait();
-    const int span = blockIdx.x, lane = threadIdx.x % 32, x = threadIdx.x % kQuads, group = threadIdx.x / kQuads;
-    const int32_t place = info[2 * span];
-    if (place < 0 || !info[2 * span + 1]) return;
-    // the first span with a part: the last one before this that has it, but not from earlier spans
-    int first = span;
-    for (bool more = true; more && first > 0;) {
-        const int s = first - 1 - lane;
-        const uint32_t began = __ballot_sync(0xffffffffu, s < 0 || info[2 * s] != place);
-        more = began == 0;
-        first -= more ? 32 : __ffs(began);
-    }
-    if (first < 0) first = 0;
-    D* row = dW + places.row(place) * lddw;
-    for (int c0 = 0; c0 < cols; c0 += 4 * kQuads) {
-        const int c = c0 + 4 * x;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < cols) {
-#pragma unroll 8
-            for (int s = first + group; s < span; s += kGroups) {
-                const float4 f = *reinterpret_cast<const float4*>(tail + (int64_t)s * ldp + c);
-                sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
-            }
-        }
-        __syncthreads();
-        sm[group][x] = sum;
-        __syncthreads();
-        if (group == 0 && c < cols) {
-            sum = *reinterpret_cast<const float4*>(head + (int64_t)span * ldp + c);
-#pragma unroll
-            for (int k = 0; k < kGroups; ++k) {
-                const float4 f = sm[k][x];
-                sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
-            }
-            const float f[4] = {sum.x, sum.y, sum.z, sum.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < cols) row[c + j] = from_f32<D>(ADD ? fmaf(f[j], scale, to_f32(row[c + j])) : f[j] * scale);
-        }
-    }
 }
 
 template <typename T, typename I, int LANES>
@@ -466,7 +445,7 @@ detox_status sort_tokens(const void* tokens, const Plan& p, char* ws, cudaStream
     }
     return launch_chained(sort_tokens_kernel<I>, 1u << p.places.bits, kSortThreads, smem, 1, s, static_cast<const I*>(tokens), p.rows, p.places,
                           reinterpret_cast<int32_t*>(ws + p.order), reinterpret_cast<int32_t*>(ws + p.sorted),
-                          reinterpret_cast<int32_t*>(ws + p.starts));
+                          reinterpret_cast<int32_t*>(ws + p.starts), reinterpret_cast<int32_t*>(ws + p.left), (int64_t)p.spans * p.slices);
 }
 
 template <typename T, typename D, bool ADD>
@@ -483,17 +462,15 @@ detox_status sums(const void* dY, int64_t lddy, float scale, void* dW, int64_t l
     g.dW = dW; g.lddw = lddw;
     g.w_vec = aligned16(dW) && lddw % Piece<D>::N == 0;
     g.w_wide = aligned_to(dW, 32) && lddw * (int64_t)sizeof(D) % 32 == 0;
-    g.info = reinterpret_cast<int32_t*>(ws + p.info);
+    g.left = reinterpret_cast<int32_t*>(ws + p.left);
     g.head = reinterpret_cast<float*>(ws + p.head);
     g.tail = reinterpret_cast<float*>(ws + p.tail);
     g.ldp = p.ldp;
     const bool any = !(p.cols % Piece<T>::N == 0 && g.span.vec);
     g.sum_ctas = (unsigned)ceil_div((int64_t)p.spans * p.slices, (int64_t)(kThreads / 32));
     const unsigned grid = g.sum_ctas + (ADD ? 0u : (unsigned)ceil_div((int64_t)p.places.count(), (int64_t)kZeroPlaces));
-    const detox_status st = launch_chained(any ? sum_rows_kernel<T, D, ADD, true> : sum_rows_kernel<T, D, ADD, false>, grid, kThreads, 0, 1, s, g);
-    if (st != DETOX_OK || p.spans < 2) return st;
-    return launch_chained(join_spans_kernel<D, ADD>, (unsigned)p.spans, kJoinThreads, 0, 1, s, g.info, g.places, g.head, g.tail, p.ldp, (int)p.cols, scale,
-                          static_cast<D*>(dW), lddw);
+    if (grid == 0) return DETOX_OK;
+    return launch_chained(any ? sum_rows_kernel<T, D, ADD, true> : sum_rows_kernel<T, D, ADD, false>, grid, kThreads, 0, 1, s, g);
 }
 template <typename T>
 detox_status sums(const void* dY, int64_t lddy, float scale, void* dW, int64_t lddw, bool wide, bool add, const Plan& p, char* ws,
@@ -513,14 +490,15 @@ detox_status launch_embedding(int dtype, const void* W, int64_t ldw, int64_t voc
 }
 
 size_t embedding_backward_ws_bytes(int64_t rows, int64_t vocab, int64_t cols) {
-    // (whatever the type: 16-bit rows have fewer slices and with them shorter spans, and more)
-    return plan_of(rows, vocab, cols, Piece<__half>::N).bytes;
+    // (the larger of any type's; with `add` the spans are shorter, and more)
+    const size_t a = plan_of(rows, vocab, cols, Piece<__half>::N, true).bytes, b = plan_of(rows, vocab, cols, Piece<float>::N, true).bytes;
+    return a > b ? a : b;
 }
 
 detox_status launch_embedding_backward(int dtype, const void* dY, int64_t lddy, int index, const void* tokens, int64_t rows, int64_t vocab,
                                        int64_t cols, float scale, void* dW, int64_t lddw, int dw_dtype, bool add, void* ws, cudaStream_t s) {
     if (rows == 0 && add) return DETOX_OK;
-    const Plan p = plan_of(rows, vocab, cols, dtype == DETOX_DTYPE_FLOAT ? Piece<float>::N : Piece<__half>::N);
+    const Plan p = plan_of(rows, vocab, cols, dtype == DETOX_DTYPE_FLOAT ? Piece<float>::N : Piece<__half>::N, add);
     char* at = static_cast<char*>(ws);
     const detox_status st = index == DETOX_INDEX_INT32 ? sort_tokens<int32_t>(tokens, p, at, s) : sort_tokens<int64_t>(tokens, p, at, s);
     if (st != DETOX_OK) return st;
