@@ -148,7 +148,7 @@ __device__ __forceinline__ float largest(float a, float b) {   // NaN where one 
     return r;
 }
 
-// Entries x, already divided by the scale, as e4m3 numbers, where some are small or not finite: a function of its own, since its registers are missed where it is not needed
+// Entries x, already divided by the scale, as e4m3 numbers, whatever they are: a function of its own, since its registers are missed where it is not needed
 __device__ __noinline__ uint32_t small_at_random(float x0, float x1, float x2, float x3, uint32_t bits01, uint32_t bits23, bool positive) {
     const float x[4] = {x0, x1, x2, x3};
     const uint32_t bits[4] = {bits01 & 0xffffu, bits01 >> 16, bits23 & 0xffffu, bits23 >> 16};
@@ -159,45 +159,62 @@ __device__ __noinline__ uint32_t small_at_random(float x0, float x1, float x2, f
         const float lift = v < 0.015625f ? 0.015625f : 0.f;
         float k = __uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift;
         if (positive && v > 0.f && k == 0.f) k = 0.001953125f;
-        r[j] = v <= 448.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);
+        r[j] = v <= 449.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);   // (finite ones are 448 at most, or a unit more)
     }
     return keep4(r[0], r[1], r[2], r[3]);
 }
 
-// The 8-bit form of a block, 4 entries a lane (two packed pairs), rounded at random with `bits` (16 of them an entry).  POSITIVE: entries > 0 stay so.
-// Inf and NaN become NaN and do not count for the scale.
+// The largest entry of a block, 4 entries a lane (two packed pairs), as an integer (positive numbers, Inf and NaN are in that order).
+__device__ __forceinline__ uint32_t largest_of(const uint64_t (&p)[2]) {
+    const float lane = largest(largest(fabsf(pair_lo(p[0])), fabsf(pair_hi(p[0]))), largest(fabsf(pair_lo(p[1])), fabsf(pair_hi(p[1]))));
+    return __reduce_max_sync(0xffffffffu, __float_as_uint(lane) & 0x7fffffffu);
+}
+// ... and of its finite entries alone
+__device__ __noinline__ uint32_t largest_finite(uint64_t p0, uint64_t p1) {
+    const uint32_t a[4] = {(uint32_t)p0, (uint32_t)(p0 >> 32), (uint32_t)p1, (uint32_t)(p1 >> 32)};
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if ((a[j] & 0x7fffffffu) < 0x7f800000u) top = max(top, a[j] & 0x7fffffffu);
+    return __reduce_max_sync(0xffffffffu, top);
+}
+
+// The 8-bit form of a block, rounded at random with `bits` (16 of them an entry).  ROOTS: entries > 0 stay so.  Inf and NaN become NaN and do not count for the scale.
 //
 // e4m3 keeps 3 of the 23 bits behind an fp32 number's first one, so the random bits are added to the number's own above the 4th lowest, and
-// the lowest 20 cut off.  Below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5: such an entry is lifted by 2^-6 for it.  Blocks
-// without such entries (most: they are 2^-15 of the block's largest) and with finite ones only need none of that.
-template <bool POSITIVE>
-__device__ __forceinline__ uint32_t keep_at_random(const uint64_t (&p)[2], const uint32_t (&bits)[4], uint32_t* q) {
+// the lowest 20 cut off.  Below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5: such an entry is lifted by 2^-6 for it.  Nearly every
+// block of m has one (they are 2^-15 of the block's largest), hardly one of roots has.
+//
+// of: the entries (ROOTS: their squares), and top their largest, from which the scale is taken.  It decides over a whole block's scale, so its root is rounded properly
+// here; an approximate root beside it may come out a unit above 448, which the conversion cuts off.
+template <bool ROOTS>
+__device__ __forceinline__ uint32_t keep_at_random(const uint64_t (&p)[2], const uint64_t (&of)[2], uint32_t top, const uint32_t (&bits)[4], uint32_t* q) {
     const float x[4] = {pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])};
-    // (positive numbers and NaN are in order as integers, too)
-    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(largest(fabsf(x[0]), fabsf(x[1])), largest(fabsf(x[2]), fabsf(x[3])))) & 0x7fffffffu);
-    const uint32_t least = __reduce_min_sync(0xffffffffu, __float_as_uint(fminf(fminf(fabsf(x[0]), fabsf(x[1])), fminf(fabsf(x[2]), fabsf(x[3])))));
     const bool finite = top < 0x7f800000u;
-    if (!finite) {
-        top = 0u;
+    if (!finite) top = largest_finite(of[0], of[1]);
+    const uint32_t e = keep_exponent(ROOTS ? sqrtf(__uint_as_float(top)) : __uint_as_float(top));
+    const float inverse = keep_inverse(e);
+    const uint64_t inverse2 = pair_of(inverse, inverse), a = mul2(p[0], inverse2), b = mul2(p[1], inverse2);
+    float r[4] = {pair_lo(a), pair_hi(a), pair_lo(b), pair_hi(b)};
+    if (ROOTS) {
+        const float least = fminf(fminf(r[0], r[1]), fminf(r[2], r[3]));
+        if (finite && __all_sync(0xffffffffu, least >= 0.015625f)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(r[j]) + (bits[j] << 4)) & 0xfff00000u);
+            *q = keep4(r[0], r[1], r[2], r[3]);
+            return e;
+        }
+    } else if (finite) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t a = __float_as_uint(x[j]) & 0x7fffffffu;
-            if (a < 0x7f800000u) top = max(top, a);
+            const float v = fabsf(r[j]);
+            const float lift = v < 0.015625f ? 0.015625f : 0.f;
+            r[j] = copysignf(__uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift, r[j]);
         }
-        top = __reduce_max_sync(0xffffffffu, top);
-    }
-    const uint32_t e = keep_exponent(__uint_as_float(top));
-    const float inverse = keep_inverse(e);
-    float r[4];
-    if (finite && __uint_as_float(least) * inverse >= 0.015625f) {
-        const uint64_t inverse2 = pair_of(inverse, inverse), a = mul2(p[0], inverse2), b = mul2(p[1], inverse2);
-        const float y[4] = {pair_lo(a), pair_hi(a), pair_lo(b), pair_hi(b)};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(y[j]) + (bits[j] << 4)) & 0xfff00000u);
         *q = keep4(r[0], r[1], r[2], r[3]);
-    } else {
-        *q = small_at_random(x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse, bits[0] | bits[1] << 16, bits[2] | bits[3] << 16, POSITIVE);
+        return e;
     }
+    *q = small_at_random(r[0], r[1], r[2], r[3], bits[0] | bits[1] << 16, bits[2] | bits[3] << 16, ROOTS);
     return e;
 }
 
@@ -281,6 +298,7 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
         if constexpr (MASTER) store4<VEC>(master, own + b * kStep, low, left, p[b]);
         store4<VEC>(P, own + b * kStep, low, left, p[b]);
         if constexpr (EIGHT) {
+            const uint32_t top_m = largest_of(m), top_v = largest_of(v);
             uint32_t rm[4], rv[4];
             const uint32_t entry = (uint32_t)at + own + b * kStep;
 #pragma unroll
@@ -291,9 +309,9 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
                 rv[j] = h >> 16;
             }
             uint32_t q;
-            const uint32_t me = keep_at_random<false>(m, rm, &q);
+            const uint32_t me = keep_at_random<false>(m, m, top_m, rm, &q);
             store_bytes<VEC>(M8, own + b * kStep, left, q);
-            const uint32_t ve = keep_at_random<true>(root, rv, &q);
+            const uint32_t ve = keep_at_random<true>(root, v, top_v, rv, &q);
             store_bytes<VEC>(V8, own + b * kStep, left, q);
             if (lane == 0) {
                 (VEC ? scales + i / kKeepBlock : t.ME + (at + i) / kKeepBlock)[0] = (uint8_t)me;
