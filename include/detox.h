@@ -483,7 +483,8 @@ detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, i
  *   y        dev, rows                 int32 or int64 (`index`)
  *   logp, lse, dlogp                   dev, rows, fp32
  * detox_token_logp_backward: dZ[t][j] = scale dlogp[t] (1[j = y[t]] - exp(scale Z[t][j] - lse[t])), lse as detox_token_logp left it.  A row whose
- * dlogp is 0 is not read, and its gradient is zero.
+ * dlogp is 0 is not read, and its gradient is zero.  lse being fp32, its probabilities are off by up to |lse| 2^-24 of themselves, here and in the
+ * preference loss (logits of a few tens: 10^-6); the policy loss's are not.
  * ------------------------------------------------------------------------------------------- */
 #define DETOX_LOGITS_MAX_COLS 262144
 detox_status detox_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
@@ -568,7 +569,9 @@ detox_status detox_preference_loss(const detox_preference_desc* desc, float* los
  *
  * tensors: host, `count` of them; read before the call returns.  No two buffers of a call may overlap, but P may be the master itself (FLOAT; give
  * it as P alone).  Entries are contiguous; any alignment to the entry's size works, 16 bytes (8 for 16-bit entries, 4 for 8-bit ones) is faster.
- * A tensor without entries is passed over.  No workspace.
+ * A tensor without entries is passed over.  eps > 0; beta1 and beta2 in [0, 1).  FLOAT weights take a gradient of any type and have no master;
+ * HALF and BFLOAT ones take a gradient of their own type or FLOAT (else DETOX_ERR_UNSUPPORTED).  A tensor whose buffers are all off a 16-byte boundary by
+ * the same number of entries, as slices of vectors of one layout are, is as fast as an aligned one (32 bits).  No workspace.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
     void* P;                     /* dev, n: the weights */

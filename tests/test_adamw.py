@@ -265,8 +265,20 @@ def test_refusals():
                        (TypeError, dict(lr=torch.ones(1))), (ValueError, dict(m=[(m8[0][0], m8[0][1][:0])], v=v8))):
         with pytest.raises(error):
             ok(**bad)
+    both = dict(grads=[p + 1, p + 1], weight_decay=[0.1, 0.0])
+    other = [torch.zeros(64, device=DEV) for _ in range(3)]
+    for bad in (dict(params=[p, p], m=[m[0], other[0]], v=[v[0], other[1]]), dict(params=[p, other[0]], m=[m[0], m[0]], v=[v[0], other[1]]),
+                dict(params=[p, other[0]], m=[m[0], v[0]], v=[v[0], other[1]])):
+        with pytest.raises(ValueError, match="twice"):
+            ok(**both, **bad)
+    ok(**both, params=[p, other[0]], m=[m[0], other[1]], v=[v[0], other[2]])
     w = torch.zeros(64, device=DEV, requires_grad=True)
     with pytest.raises(RuntimeError, match="requires grad"):
         ok(params=[w])
     with torch.no_grad():
         ok(params=[w])
+    loss = (w * w).sum()
+    with torch.no_grad():
+        ok(params=[w])
+    with pytest.raises(RuntimeError, match="modified"):
+        loss.backward()                            # it needs the weights as they were
