@@ -28,7 +28,7 @@ template <bool EIGHT> constexpr int kPart = kBlocks<EIGHT> * kKeepBlock * (kThre
 // Entries that a CTA takes at a time.  8 bits: two parts, so that the scales that it writes fill sectors of 32 bytes, by one store.  As single bytes, from several SMs into
 // one sector, they took a fifth of the time (618 us without any rounding, 498 without the scales' stores).
 template <bool EIGHT> constexpr int kUnit = EIGHT ? 2 * kPart<EIGHT> : kPart<EIGHT>;
-constexpr int kScales = kUnit<true> / kKeepBlock;
+static_assert(kUnit<true> / kKeepBlock == 32 && 4 * (kThreads / 32) == 32, "a scale for each lane, four for each warp");
 constexpr int kKinds = 3 * 3 * 2;                // types of weights and gradients, with a master copy or without
 
 struct Tensor {
@@ -148,20 +148,43 @@ __device__ __forceinline__ float largest(float a, float b) {   // NaN where one 
     return r;
 }
 
-// Entries x, already divided by the scale, as e4m3 numbers, whatever they are: a function of its own, since its registers are missed where it is not needed
-__device__ __noinline__ uint32_t small_at_random(float x0, float x1, float x2, float x3, uint32_t bits01, uint32_t bits23, bool positive) {
-    const float x[4] = {x0, x1, x2, x3};
-    const uint32_t bits[4] = {bits01 & 0xffffu, bits01 >> 16, bits23 & 0xffffu, bits23 >> 16};
-    float r[4];
+// The 8-bit form of entries, rounded at random
+//
+// e4m3 keeps 3 of the 23 bits behind an fp32 number's first one, so a random number of 20 bits (16 random ones and zeros) is added to the number's own bits and the lowest 20 are
+// cut off.  Divided by the scale and by 2^120 an entry is an fp32 number whose bits 26 .. 20 are the e4m3 number's, below 2^-6, where e4m3's steps stay 2^-9
+// wide, too: fp32's own numbers without a first bit begin at 2^-126.  So entries of any size take the same path, without a conversion: added, shifted, a byte taken out.
+//
+// Four of a lane, finite, the block's largest at most 448 after the scale (a root that is a unit too large there does no harm: the random numbers are at least 16 short of a
+// carry).  ROOTS: of the hash h's upper half, and entries > 0 stay so; else of its lower half, and with signs.
+template <bool ROOTS>
+__device__ __forceinline__ uint32_t rounded4(const uint64_t (&p)[2], float inverse, const uint32_t (&h)[4]) {
+    const uint64_t inverse2 = pair_of(inverse, inverse), down2 = pair_of(7.52316385e-37f, 7.52316385e-37f);   // 2^-120
+    const uint64_t a = mul2(mul2(p[0], inverse2), down2), b = mul2(mul2(p[1], inverse2), down2);
+    const uint32_t w[4] = {(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    uint32_t r[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float v = fabsf(x[j]);
-        const float lift = v < 0.015625f ? 0.015625f : 0.f;
-        float k = __uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift;
-        if (positive && v > 0.f && k == 0.f) k = 0.001953125f;
-        r[j] = v <= 449.f ? copysignf(k, x[j]) : __int_as_float(0x7fc00000);   // (finite ones are 448 at most, or a unit more)
+    for (int j = 0; j < 4; ++j) r[j] = (w[j] << 4) + __byte_perm(h[j], 0u, ROOTS ? 0x4324 : 0x4104);   // the byte on top is the number
+    auto tops = [](uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) { return __byte_perm(__byte_perm(x0, x1, 0x0073), __byte_perm(x2, x3, 0x0073), 0x5410); };
+    uint32_t q = tops(r[0], r[1], r[2], r[3]);
+    if (!ROOTS) return q | (tops(w[0], w[1], w[2], w[3]) & 0x80808080u);
+    if ((q - 0x01010101u) & ~q & 0x80808080u) {   // a byte is 0
+        const float x[4] = {pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (((q >> (8 * j)) & 0xffu) == 0u && x[j] > 0.f) q |= 1u << (8 * j);
     }
-    return keep4(r[0], r[1], r[2], r[3]);
+    return q;
+}
+// The same, and NaN for what is not finite: a function of its own, since it is hardly ever needed and its registers would be missed
+template <bool ROOTS>
+__device__ __noinline__ uint32_t rounded4_any(uint64_t p0, uint64_t p1, float inverse, uint32_t h0, uint32_t h1, uint32_t h2, uint32_t h3) {
+    const uint64_t p[2] = {p0, p1};
+    const uint32_t h[4] = {h0, h1, h2, h3}, x[4] = {(uint32_t)p0, (uint32_t)(p0 >> 32), (uint32_t)p1, (uint32_t)(p1 >> 32)};
+    uint32_t q = rounded4<ROOTS>(p, inverse, h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if ((x[j] & 0x7fffffffu) >= 0x7f800000u) q |= 0x7fu << (8 * j);
+    return q;
 }
 
 // The largest entry of a block, 4 entries a lane (two packed pairs), as an integer (positive numbers, Inf and NaN are in that order).
@@ -179,42 +202,18 @@ __device__ __noinline__ uint32_t largest_finite(uint64_t p0, uint64_t p1) {
     return __reduce_max_sync(0xffffffffu, top);
 }
 
-// The 8-bit form of a block, rounded at random with `bits` (16 of them an entry).  ROOTS: entries > 0 stay so.  Inf and NaN become NaN and do not count for the scale.
-//
-// e4m3 keeps 3 of the 23 bits behind an fp32 number's first one, so the random bits are added to the number's own above the 4th lowest, and
-// the lowest 20 cut off.  Below 2^-6 the form's steps are 2^-9 wide, as they are from there to 2^-5: such an entry is lifted by 2^-6 for it.  Nearly every
-// block of m has one (they are 2^-15 of the block's largest), hardly one of roots has.
+// The 8-bit form of a block, rounded at random.  Returns the scale's biased exponent.  Inf and NaN become NaN and do not count for it.
 //
 // of: the entries (ROOTS: their squares), and top their largest, from which the scale is taken.  It decides over a whole block's scale, so its root is rounded properly
-// here; an approximate root beside it may come out a unit above 448, which the conversion cuts off.
+// here; the entries' own are approximate.
 template <bool ROOTS>
-__device__ __forceinline__ uint32_t keep_at_random(const uint64_t (&p)[2], const uint64_t (&of)[2], uint32_t top, const uint32_t (&bits)[4], uint32_t* q) {
-    const float x[4] = {pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])};
+__device__ __forceinline__ uint32_t keep_at_random(const uint64_t (&p)[2], const uint64_t (&of)[2], uint32_t top, const uint32_t (&h)[4], uint32_t* q) {
     const bool finite = top < 0x7f800000u;
     if (!finite) top = largest_finite(of[0], of[1]);
     const uint32_t e = keep_exponent(ROOTS ? sqrtf(__uint_as_float(top)) : __uint_as_float(top));
     const float inverse = keep_inverse(e);
-    const uint64_t inverse2 = pair_of(inverse, inverse), a = mul2(p[0], inverse2), b = mul2(p[1], inverse2);
-    float r[4] = {pair_lo(a), pair_hi(a), pair_lo(b), pair_hi(b)};
-    if (ROOTS) {
-        const float least = fminf(fminf(r[0], r[1]), fminf(r[2], r[3]));
-        if (finite && __all_sync(0xffffffffu, least >= 0.015625f)) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) r[j] = __uint_as_float((__float_as_uint(r[j]) + (bits[j] << 4)) & 0xfff00000u);
-            *q = keep4(r[0], r[1], r[2], r[3]);
-            return e;
-        }
-    } else if (finite) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float v = fabsf(r[j]);
-            const float lift = v < 0.015625f ? 0.015625f : 0.f;
-            r[j] = copysignf(__uint_as_float((__float_as_uint(v + lift) + (bits[j] << 4)) & 0xfff00000u) - lift, r[j]);
-        }
-        *q = keep4(r[0], r[1], r[2], r[3]);
-        return e;
-    }
-    *q = small_at_random(r[0], r[1], r[2], r[3], bits[0] | bits[1] << 16, bits[2] | bits[3] << 16, ROOTS);
+    if (finite) *q = rounded4<ROOTS>(p, inverse, h);
+    else *q = rounded4_any<ROOTS>(p[0], p[1], inverse, h[0], h[1], h[2], h[3]);
     return e;
 }
 
@@ -225,10 +224,11 @@ struct Now {
 __device__ __forceinline__ uint64_t both(float v) { return pair_of(v, v); }
 __device__ __forceinline__ uint64_t pairs_at(const float (&f)[4], int k) { return pair_of(f[2 * k], f[2 * k + 1]); }
 
-// A part of tensor t from entry `at` on.  PT, GT: of the weights and the gradient.  The arithmetic goes two entries at a time.  VEC: the new scales go to `scales`,
-// a row for m and one for sqrt(v).
+// A part of tensor t from entry `at` on.  PT, GT: of the weights and the gradient.  The arithmetic goes two entries at a time.  EIGHT and VEC:
+// `part` of a unit; scales_m and scales_v hold the unit's scales, one a lane, and the new ones are left in keep_m and keep_v, a byte for each of this warp's blocks.
 template <bool EIGHT, bool VEC, typename PT, typename GT, bool MASTER>
-__device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Numbers& number, const Now& now, uint8_t* scales) {
+__device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Numbers& number, const Now& now, int part, float scales_m, float scales_v, uint32_t& keep_m,
+                                          uint32_t& keep_v) {
     constexpr int B = kBlocks<EIGHT>, kStep = kKeepBlock * (kThreads / 32);
     const int lane = threadIdx.x % 32, first = threadIdx.x / 32 * kKeepBlock;   // this warp's blocks start at at + first + b kStep
     const unsigned own = VEC ? 4 * threadIdx.x : first + lane;                  // and this lane's entries of them
@@ -253,8 +253,14 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
         if constexpr (EIGHT) {
             mq[b] = load_bytes<VEC>(M8, own + b * kStep, left);
             vq[b] = load_bytes<VEC>(V8, own + b * kStep, left);
-            ms[b] = keep_scale_of_byte(ME[(unsigned)i / kKeepBlock]);
-            vs[b] = keep_scale_of_byte(VE[(unsigned)i / kKeepBlock]);
+            if constexpr (VEC) {
+                const int block = (part * kPart<true> + i) / kKeepBlock;
+                ms[b] = __shfl_sync(0xffffffffu, scales_m, block);
+                vs[b] = __shfl_sync(0xffffffffu, scales_v, block);
+            } else {
+                ms[b] = keep_scale_of_byte(ME[(unsigned)i / kKeepBlock]);
+                vs[b] = keep_scale_of_byte(VE[(unsigned)i / kKeepBlock]);
+            }
         } else {
             load4<VEC>(M, own + b * kStep, low, left, m32[b]);
             load4<VEC>(V, own + b * kStep, low, left, v32[b]);
@@ -299,23 +305,22 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
         store4<VEC>(P, own + b * kStep, low, left, p[b]);
         if constexpr (EIGHT) {
             const uint32_t top_m = largest_of(m), top_v = largest_of(v);
-            uint32_t rm[4], rv[4];
+            uint32_t h[4];
             const uint32_t entry = (uint32_t)at + own + b * kStep;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // (four entries from a multiple of four on differ in the lowest bits alone, which the first shift drops)
-                const uint32_t h = VEC ? mix_rest((now.seed ^ entry) ^ ((now.seed ^ entry) >> 16) ^ (uint32_t)j) : mix(now.seed ^ (entry + 32u * j));
-                rm[j] = h & 0xffffu;
-                rv[j] = h >> 16;
-            }
+            for (int j = 0; j < 4; ++j)   // (four entries from a multiple of four on differ in the lowest bits alone, which the first shift drops)
+                h[j] = VEC ? mix_rest((now.seed ^ entry) ^ ((now.seed ^ entry) >> 16) ^ (uint32_t)j) : mix(now.seed ^ (entry + 32u * j));
             uint32_t q;
-            const uint32_t me = keep_at_random<false>(m, m, top_m, rm, &q);
+            const uint32_t me = keep_at_random<false>(m, m, top_m, h, &q);
             store_bytes<VEC>(M8, own + b * kStep, left, q);
-            const uint32_t ve = keep_at_random<true>(root, v, top_v, rv, &q);
+            const uint32_t ve = keep_at_random<true>(root, v, top_v, h, &q);
             store_bytes<VEC>(V8, own + b * kStep, left, q);
-            if (lane == 0) {
-                (VEC ? scales + i / kKeepBlock : t.ME + (at + i) / kKeepBlock)[0] = (uint8_t)me;
-                (VEC ? scales + kScales + i / kKeepBlock : t.VE + (at + i) / kKeepBlock)[0] = (uint8_t)ve;
+            if constexpr (VEC) {
+                keep_m |= me << (8 * (part * B + b));
+                keep_v |= ve << (8 * (part * B + b));
+            } else if (lane == 0) {
+                t.ME[(at + i) / kKeepBlock] = (uint8_t)me;
+                t.VE[(at + i) / kKeepBlock] = (uint8_t)ve;
             }
         } else {
             const float fm[4] = {pair_lo(m[0]), pair_hi(m[0]), pair_lo(m[1]), pair_hi(m[1])};
@@ -329,7 +334,10 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
 // Tensors of any alignment, and the ends of all: a function of its own, since beside the other's its registers do not fit (5 to 80 words spilled)
 template <bool EIGHT, typename PT, typename GT, bool MASTER>
 __device__ __noinline__ void step_any(const Tensor& t, int64_t at, const Numbers& number, Now now) {
-    for (int64_t end = at + kUnit<EIGHT>; at < end && at < t.n; at += kPart<EIGHT>) step_part<EIGHT, false, PT, GT, MASTER>(t, at, number, now, nullptr);
+    for (int64_t end = at + kUnit<EIGHT>; at < end && at < t.n; at += kPart<EIGHT>) {
+        uint32_t none = 0u;
+        step_part<EIGHT, false, PT, GT, MASTER>(t, at, number, now, 0, 0.f, 0.f, none, none);
+    }
 }
 
 template <bool EIGHT, typename PT, typename GT, bool MASTER, int CAP>
@@ -368,17 +376,27 @@ __global__ void __launch_bounds__(kThreads, kCtas) adamw_kernel(const __grid_con
         if (!t.vec || t.n - at < kUnit<EIGHT> || at < t.skip) {
             step_any<EIGHT, PT, GT, MASTER>(t, at, number, now);
         } else if constexpr (!EIGHT) {
-            step_part<false, true, PT, GT, MASTER>(t, at, number, now, nullptr);
+            uint32_t none = 0u;
+            step_part<false, true, PT, GT, MASTER>(t, at, number, now, 0, 0.f, 0.f, none, none);
         } else {
             // (written again two units on, and every thread has passed the barrier between)
-            __shared__ uint8_t scales[2][2 * kScales];
-            uint8_t* here = scales[turn & 1];
+            __shared__ uint32_t scales[2][2][kThreads / 32];
+            uint32_t(*here)[kThreads / 32] = scales[turn & 1];
             ++turn;
+            const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+            const int64_t block = at / kKeepBlock;
+            const float scales_m = keep_scale_of_byte(t.ME[block + lane]), scales_v = keep_scale_of_byte(t.VE[block + lane]);
+            uint32_t keep_m = 0u, keep_v = 0u;
 #pragma unroll 1
             for (int part = 0; part < 2; ++part)
-                step_part<true, true, PT, GT, MASTER>(t, at + part * kPart<true>, number, now, here + part * (kScales / 2));
+                step_part<true, true, PT, GT, MASTER>(t, at + part * kPart<true>, number, now, part, scales_m, scales_v, keep_m, keep_v);
+            if (lane == 0) {
+                here[0][warp] = keep_m;
+                here[1][warp] = keep_v;
+            }
             __syncthreads();
-            if (threadIdx.x < 2 * kScales) (threadIdx.x < kScales ? t.ME + threadIdx.x : t.VE + (threadIdx.x - kScales))[at / kKeepBlock] = here[threadIdx.x];
+            // (byte i of a warp's word is that of block warp + i * warps)
+            if (warp < 2) (warp == 0 ? t.ME : t.VE)[block + lane] = (uint8_t)(here[warp][lane % (kThreads / 32)] >> (8 * (lane / (kThreads / 32))));
         }
     }
 }
