@@ -62,6 +62,7 @@ constexpr int kSumWarps = 48;                  // warps of an SM that there are 
 template <bool ADD> constexpr int kAhead = ADD ? 4 : 8;
 constexpr int kSortAhead = 8;
 constexpr int kZeroPlaces = 32;                // places that a CTA looks after
+constexpr int kZeroCtas = 6;                   // CTAs of an SM that there should be for that
 
 // Place p is row (i << bits) + c of the vocabulary with c = p / per, i = p % per; a few at the ends of CTAs' stretches are none.
 struct Places {
@@ -209,7 +210,7 @@ struct SumRows {
     const int32_t *order, *sorted, *starts;
     Places places;
     int cols, slices, spans, length;
-    unsigned sum_ctas;                         // the CTAs behind them write zeros
+    unsigned sum_ctas, zero_splits;            // the CTAs behind them write zeros, so many to a stretch of places
     float scale;
     void* dW;
     int64_t lddw;
@@ -276,34 +277,24 @@ __device__ __forceinline__ void load_part(const float* row, int c, int cols, uin
     }
 }
 
-// zeros to the rows of kZeroPlaces places that have no tokens
+// zeros to one of `splits` stretches of the rows of kZeroPlaces places that have no tokens: 32 bytes a store, but for the ends of a stretch
 template <typename D>
-__device__ __forceinline__ void zero_rows(const SumRows& g, int64_t first) {
-    constexpr int N = Piece<D>::N, kWide = 32 / (int)sizeof(D);
+__device__ __forceinline__ void zero_rows(const SumRows& g, int64_t first, int split, int splits) {
     const int64_t place = first + threadIdx.x % 32;
     const int64_t row = place < g.places.count() ? g.places.row((int32_t)place) : g.places.vocab;
     uint32_t empty = __ballot_sync(0xffffffffu, row < g.places.vocab && g.starts[place] == g.starts[place + 1]);
+    const int length = (g.cols + splits - 1) / splits, begin = split * length, end = begin + length < g.cols ? begin + length : g.cols;
+    if (begin >= end) return;
     for (; empty; empty &= empty - 1) {
         D* to = static_cast<D*>(g.dW) + __shfl_sync(0xffffffffu, row, __ffs(empty) - 1) * g.lddw;
-        if (g.w_wide) {
-            for (int c = threadIdx.x * kWide; c < g.cols; c += kThreads * kWide) {
-                if (c + kWide <= g.cols) {
-                    asm volatile("st.global.cs.v4.b64 [%0], {%1, %1, %1, %1};" ::"l"(to + c), "l"(0ull) : "memory");
-                } else {
-                    for (int j = c; j < g.cols; ++j) to[j] = from_f32<D>(0.f);
-                }
-            }
-        } else if (g.w_vec) {
-            for (int c = threadIdx.x * N; c < g.cols; c += kThreads * N) {
-                if (c + N <= g.cols) {
-                    st_stream_u4(to + c, make_uint4(0u, 0u, 0u, 0u));
-                } else {
-                    for (int j = c; j < g.cols; ++j) to[j] = from_f32<D>(0.f);
-                }
-            }
-        } else {
-            for (int c = threadIdx.x; c < g.cols; c += kThreads) to[c] = from_f32<D>(0.f);
-        }
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(to + begin), hi = reinterpret_cast<uintptr_t>(to + end);
+        uintptr_t from = (lo + 31) & ~(uintptr_t)31, until = hi & ~(uintptr_t)31;
+        if (from > until) from = until = hi;   // (within 32 bytes)
+        for (uintptr_t at = from + 32 * threadIdx.x; at < until; at += 32 * kThreads)
+            asm volatile("st.global.cs.v4.b64 [%0], {%1, %1, %1, %1};" ::"l"(at), "l"(0ull) : "memory");
+        const uintptr_t head = lo + sizeof(D) * threadIdx.x, tail = until + sizeof(D) * threadIdx.x;
+        if (head < from) *reinterpret_cast<D*>(head) = from_f32<D>(0.f);
+        if (tail < hi) *reinterpret_cast<D*>(tail) = from_f32<D>(0.f);
     }
 }
 
@@ -313,7 +304,8 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
     pdl_trigger();
     pdl_wait();
     if (!ADD && blockIdx.x >= g.sum_ctas) {
-        zero_rows<D>(g, (int64_t)(blockIdx.x - g.sum_ctas) * kZeroPlaces);
+        const unsigned k = blockIdx.x - g.sum_ctas;
+        zero_rows<D>(g, (int64_t)(k / g.zero_splits) * kZeroPlaces, (int)(k % g.zero_splits), (int)g.zero_splits);
         return;
     }
     const int lane = threadIdx.x % 32;
@@ -468,7 +460,11 @@ detox_status sums(const void* dY, int64_t lddy, float scale, void* dW, int64_t l
     g.ldp = p.ldp;
     const bool any = !(p.cols % Piece<T>::N == 0 && g.span.vec);
     g.sum_ctas = (unsigned)ceil_div((int64_t)p.spans * p.slices, (int64_t)(kThreads / 32));
-    const unsigned grid = g.sum_ctas + (ADD ? 0u : (unsigned)ceil_div((int64_t)p.places.count(), (int64_t)kZeroPlaces));
+    // few places: several CTAs to a row, as long as each has a store for all its threads
+    const int64_t stretches = ceil_div((int64_t)p.places.count(), (int64_t)kZeroPlaces), wide = ceil_div(p.cols * (int64_t)sizeof(D), (int64_t)32 * kThreads);
+    const int64_t splits = ceil_div((int64_t)kSMs * kZeroCtas, stretches);
+    g.zero_splits = (unsigned)(splits < wide ? splits : wide);
+    const unsigned grid = g.sum_ctas + (ADD ? 0u : (unsigned)stretches * g.zero_splits);
     if (grid == 0) return DETOX_OK;
     return launch_chained(any ? sum_rows_kernel<T, D, ADD, true> : sum_rows_kernel<T, D, ADD, false>, grid, kThreads, 0, 1, s, g);
 }

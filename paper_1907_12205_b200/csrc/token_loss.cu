@@ -194,8 +194,8 @@ __device__ __forceinline__ uint4 only_first(uint4 v, int n) {
 // powers in fp32.  16 pieces of fp32 leave no room for both.
 template <typename T, int P> constexpr bool kAhead = P * Piece<T>::N + 4 * P <= 96;
 template <typename T, int P> constexpr int kRegisters = P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) + (sizeof(T) == 4 ? 48 : 32);
-template <typename T, int THREADS, int P>
-constexpr int kCtas = 65536 / (THREADS * kRegisters<T, P>) < 2048 / THREADS ? 65536 / (THREADS * kRegisters<T, P>) : 2048 / THREADS;
+constexpr int between(int least, int most, int v) { return v < least ? least : (v > most ? most : v); }
+template <typename T, int THREADS, int P> constexpr int kCtas = between(1, 2048 / THREADS, 65536 / (THREADS * kRegisters<T, P>));
 
 // P pieces a thread; but for ANY the CTAs of a cluster have more than (P - 1) * THREADS each, so that only a thread's last one may be missing (a comparison and a
 // branch for each piece took a third of the instructions).
@@ -600,15 +600,17 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __rest
 // How many CTAs share a row: as many as its entries need registers of; then, while rows are so few that SMs are left over, more, down to
 // kLeastChunk entries each.
 constexpr int kLeastChunk = 2048;
+// pieces of a thread with the next row's beside them: eight of 16 bits, twelve of fp32
+template <typename T> constexpr int kMostPieces = 96 / (Piece<T>::N + 4);
 template <typename T>
 int cluster_of(int64_t rows, int64_t vocab) {
-    int64_t cluster = ceil_div(vocab, (int64_t)512 * 8 * Piece<T>::N);   // eight pieces a thread, the next row's beside them
-    if (cluster > kMaxCluster) cluster = kMaxCluster;                    // (fp32: sixteen)
+    int64_t cluster = 1;                                       // 1, 2, 4 or 8
+    while (cluster < kMaxCluster && vocab > cluster * 512 * kMostPieces<T> * Piece<T>::N) cluster *= 2;   // (fp32 beyond eight: sixteen pieces a thread)
     while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= kSMs && vocab >= cluster * 2 * kLeastChunk) cluster *= 2;
     return (int)cluster;
 }
-// Calls f<THREADS, P>() for CTAs of `pieces` pieces: P is what a thread has, and the CTA the smallest of which that is at most eight, four in CTAs of 128 (they wait
-// less for one another).
+// Calls f<THREADS, P>() for CTAs of `pieces` pieces: P is what a thread has, and the CTA the smallest of which that is at most eight (of 512 threads: kMostPieces), four in
+// CTAs of 128 (they wait less for one another).
 template <typename T, bool ANY, typename F>
 detox_status by_pieces(int pieces, F f) {
     switch (ceil_div(pieces, 128)) {
@@ -630,6 +632,14 @@ detox_status by_pieces(int pieces, F f) {
         case 6: return f.template operator()<512, 6>();
         case 7: return f.template operator()<512, 7>();
         case 8: return f.template operator()<512, 8>();
+    }
+    if constexpr (sizeof(T) == 4) {
+        switch (ceil_div(pieces, 512)) {
+            case 9: return f.template operator()<512, 9>();
+            case 10: return f.template operator()<512, 10>();
+            case 11: return f.template operator()<512, 11>();
+            case 12: return f.template operator()<512, 12>();
+        }
     }
     if constexpr (ANY && sizeof(T) == 4) {
         if (pieces <= 512 * 16) return f.template operator()<512, 16>();
@@ -662,7 +672,7 @@ detox_status policy_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
     g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
     g.dz_vec = pieces<T>(g.dZ, g.lddz);
     const int most = (int)ceil_div((int64_t)g.pieces, (int64_t)g.cluster);
-    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec) && most <= 512 * 8) return by_pieces<T, false>(most, Policy<T, false>{g, clusters, s});
+    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec) && most <= 512 * kMostPieces<T>) return by_pieces<T, false>(most, Policy<T, false>{g, clusters, s});
     return by_pieces<T, true>(most, Policy<T, true>{g, clusters, s});
 }
 

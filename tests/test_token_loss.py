@@ -51,7 +51,8 @@ def dz_bound(want, coef, coef_off, p, y, scale, dtype, off):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 7), (9, 100), (40, 256), (33, 1000), (2, 1025), (70, 2051), (4, 4099), (300, 3001), (3, 8200), (5, 16390), (2, 32000),
-          (7, 32770), (160, 5000), (80, 50257), (2, 131072), (1, 140001), (2, 262144)]
+          (7, 32770), (160, 5000), (80, 50257), (2, 131072), (1, 140001), (2, 262144), (2, 24584), (1, 75000), (2, 100008), (1, 120007),
+          (2, 170000), (1, 200008), (1, 230000)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
