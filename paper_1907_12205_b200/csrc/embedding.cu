@@ -222,47 +222,56 @@ struct SumRows {
 };
 
 // N sums of a lane to entries c .. of a row: fp32, or rounded.  Eight fp32 sums leave in one 32-byte store: two of 16 bytes each fill half of every
-// sector that they touch .
+// sector that they touch.  Rows that are not aligned go through the warp's `buffer`, so that its lanes store neighbouring entries (as each lane's own ones, one at a time, every
+// store touches 32 sectors).  Whole warps call this.
 template <typename D, int N>
-__device__ __forceinline__ void store_sums(D* row, int c, int cols, bool vec, bool wide, const uint64_t (&p)[N / 2]) {
+__device__ __forceinline__ void store_sums(D* row, int c, int cols, bool vec, bool wide, const uint64_t (&p)[N / 2], float* buffer) {
+    constexpr int M = Piece<D>::N;
+    if (!vec) {
+        const int lane = threadIdx.x % 32, c0 = c - lane * N;
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) *reinterpret_cast<uint64_t*>(buffer + lane * N + 2 * j) = p[j];
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c0 + 32 * j + lane < cols) row[c0 + 32 * j + lane] = from_f32<D>(buffer[32 * j + lane]);
+        __syncwarp();
+        return;
+    }
     if constexpr (sizeof(D) == 4 && N == 8) {
         if (wide && c + N <= cols) {
             asm volatile("st.global.cs.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(row + c), "l"(p[0]), "l"(p[1]), "l"(p[2]), "l"(p[3]) : "memory");
             return;
         }
-        if (vec && c + N <= cols) {
-            float4* to = reinterpret_cast<float4*>(row + c);
-            __stcs(to, make_float4(pair_lo(p[0]), pair_hi(p[0]), pair_lo(p[1]), pair_hi(p[1])));
-            __stcs(to + 1, make_float4(pair_lo(p[2]), pair_hi(p[2]), pair_lo(p[3]), pair_hi(p[3])));
-            return;
-        }
+    }
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (c + j < cols) row[c + j] = j & 1 ? pair_hi(p[j / 2]) : pair_lo(p[j / 2]);
-    } else {
-        store_piece(row, c, cols, vec, p);
+    for (int k = 0; k < N; k += M) {
+        uint64_t part[M / 2];
+#pragma unroll
+        for (int j = 0; j < M / 2; ++j) part[j] = p[k / 2 + j];
+        store_piece(row, c + k, cols, true, part);
     }
 }
 template <typename D, int N>
-__device__ __forceinline__ void load_sums(const D* row, int c, int cols, bool vec, uint64_t (&p)[N / 2]) {
-    if constexpr (Piece<D>::N == N) {
-        if (vec && c + N <= cols) {
-            Piece<D>::split(ld_stream_u4(row + c), p);
-            return;
-        }
-    }
-    if constexpr (sizeof(D) == 4 && N == 8) {
-        if (vec && c + N <= cols) {
-            const float4 x = ld_stream_f4(row + c), y = ld_stream_f4(row + c + 4);
-            p[0] = pair_of(x.x, x.y); p[1] = pair_of(x.z, x.w); p[2] = pair_of(y.x, y.y); p[3] = pair_of(y.z, y.w);
-            return;
-        }
-    }
-    float f[N];
+__device__ __forceinline__ void load_sums(const D* row, int c, int cols, bool vec, uint64_t (&p)[N / 2], float* buffer) {
+    constexpr int M = Piece<D>::N;
+    const int lane = threadIdx.x % 32, c0 = c - lane * N;
+    if (vec && c0 + 32 * N <= cols) {          // (the same for all lanes)
 #pragma unroll
-    for (int j = 0; j < N; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.f;
+        for (int k = 0; k < N; k += M) {
+            uint64_t part[M / 2];
+            Piece<D>::split(ld_stream_u4(row + c + k), part);
 #pragma unroll
-    for (int j = 0; j < N / 2; ++j) p[j] = pair_of(f[2 * j], f[2 * j + 1]);
+            for (int j = 0; j < M / 2; ++j) p[k / 2 + j] = part[j];
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) buffer[32 * j + lane] = c0 + 32 * j + lane < cols ? to_f32(row[c0 + 32 * j + lane]) : 0.f;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) p[j] = *reinterpret_cast<const uint64_t*>(buffer + lane * N + 2 * j);
+    __syncwarp();
 }
 
 // N sums of a part, past L1 (another SM may have left them)
@@ -308,6 +317,8 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
         zero_rows<D>(g, (int64_t)(k / g.zero_splits) * kZeroPlaces, (int)(k % g.zero_splits), (int)g.zero_splits);
         return;
     }
+    __shared__ __align__(16) float buffers[kThreads / 32][32 * N];
+    float* buffer = buffers[threadIdx.x / 32];
     const int lane = threadIdx.x % 32;
     const int warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const int span = warp / g.slices, slice = warp - span * g.slices;
@@ -332,15 +343,15 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
         for (int j = 0; j < N / 2; ++j) acc[j] = mul2(acc[j], scale2);
         if constexpr (ADD) {
             uint64_t old[N / 2];
-            load_sums<D, N>(at, c, g.cols, g.w_vec, old);
+            load_sums<D, N>(at, c, g.cols, g.w_vec, old, buffer);
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) acc[j] = add2(acc[j], old[j]);
         }
-        store_sums<D, N>(at, c, g.cols, g.w_vec, g.w_wide, acc);
+        store_sums<D, N>(at, c, g.cols, g.w_vec, g.w_wide, acc, buffer);
     };
     // a part of a place's sum is complete; the warp that leaves the last one adds them all
     auto part = [&](float* to) {
-        store_sums<float, N>(to + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc);
+        store_sums<float, N>(to + (int64_t)span * g.ldp, c, (int)g.ldp, true, false, acc, buffer);
         const int first = g.starts[place] / g.length, last = (g.starts[place + 1] - 1) / g.length;
         __threadfence();
         __syncwarp();
