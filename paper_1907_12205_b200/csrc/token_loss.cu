@@ -28,6 +28,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// ex2.approx comes out 5.1e-8 of itself too small on average (2^20 arguments in (-1, 0]; at most 1.4e-7).  Over the sums of a sequence's log-probabilities that adds up, so
+// where these are formed it is put right: for the sums of powers at the end, and here for the factors between sums (1 stays 1).
+constexpr float kPowerShort = 5.1e-8f;
+__device__ __forceinline__ float factor_of(float x) {
+    const float y = exp2_fast(x);
+    return fmaf(y, kPowerShort, y);
+}
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
 
 // ---- clusters -------------------------------------------------------------------------------------
@@ -50,7 +57,7 @@ __device__ __forceinline__ void store_at(const float2* here, uint32_t rank, floa
 __device__ __forceinline__ float2 joined(float2 a, float2 b) {
     const float m = a.x > b.x ? a.x : b.x;   // (NaN sums stay NaN whatever m is)
     const float m0 = m == minus_inf() ? 0.f : m;
-    return make_float2(m, a.y * exp2_fast(a.x - m0) + b.y * exp2_fast(b.x - m0));
+    return make_float2(m, a.y * factor_of(a.x - m0) + b.y * factor_of(b.x - m0));
 }
 
 __device__ __forceinline__ float warp_largest(float v) {
@@ -66,7 +73,7 @@ __device__ __forceinline__ float warp_total(float v) {
 // the pairs of a warp's lanes as one, in all lanes
 __device__ __forceinline__ float2 joined_warp(float2 a) {
     const float m = warp_largest(a.x), m0 = m == minus_inf() ? 0.f : m;
-    return make_float2(m, warp_total(a.y * exp2_fast(a.x - m0)));
+    return make_float2(m, warp_total(a.y * factor_of(a.x - m0)));
 }
 
 // 16 bytes, or what was there before; issued where it is written
@@ -369,7 +376,8 @@ struct ScoreArgs {
     const void* y;
     bool wide;
     float k2;
-    float *logp, *lse;
+    float *logp, *lse;             // either may be NULL
+    double* logp64;                // the same before its rounding, for sums over sequences; or NULL
     float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
 };
 
@@ -390,6 +398,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     if (first && g.zeros) g.zeros[row] = 0.f;
     if (y < 0) {                                               // (the same in all threads of the row)
         if (first && g.logp) g.logp[row] = 0.f;
+        if (first && g.logp64) g.logp64[row] = 0.;
         if (first && g.lse) g.lse[row] = 0.f;
         return;
     }
@@ -411,7 +420,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
         const float here = largest_of(most.value(), g.k2);
         if (here > top) {
-            const float less = exp2_fast(top - here);
+            const float less = factor_of(top - here);
             const uint64_t less2 = pair_of(less, less);
             sum2[0] = mul2(sum2[0], less2);
             sum2[1] = mul2(sum2[1], less2);
@@ -447,9 +456,13 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         all = joined_warp(all);
     }
     if (first) {
-        const Scored s = scored(all, zy, g.k2, y < g.vocab);
-        if (g.logp) g.logp[row] = s.logp;
-        if (g.lse) g.lse[row] = s.lse;
+        // One thread's work: in 64 bits.  (The largest entry's power is 1, the others are short.)
+        const bool empty = all.x == minus_inf() && all.y == 0.f;
+        const double lg = log2((double)all.y + (double)kPowerShort * ((double)all.y - 1.)), ln2 = 0.69314718055994531;
+        const double logp = empty ? (double)(y < g.vocab ? minus_inf() : zy) : (((double)zy * (double)g.k2 - (double)all.x) - lg) * ln2;
+        if (g.logp) g.logp[row] = (float)logp;
+        if (g.logp64) g.logp64[row] = logp;
+        if (g.lse) g.lse[row] = empty ? minus_inf() : (float)(((double)all.x + lg) * ln2);
     }
 }
 
@@ -543,7 +556,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
 // ---- pairs of sequences ----------------------------------------------------------------------------
 constexpr int kPairThreads = 256;
 
-__global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __restrict__ logp, int64_t rows, const int32_t* __restrict__ offsets,
+__global__ void __launch_bounds__(kPairThreads) pairs_kernel(const double* __restrict__ logp, int64_t rows, const int32_t* __restrict__ offsets,
                                                              const float* __restrict__ ref, int64_t pairs, float beta, float smoothing,
                                                              float grad, float* __restrict__ margin, float* __restrict__ sums,
                                                              float* __restrict__ dlogp, double* __restrict__ parts) {
@@ -562,7 +575,7 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const float* __rest
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             double x = 0.;
-            for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kPairThreads) x += (double)logp[t];
+            for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kPairThreads) x += logp[t];
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
             if (lane == 0) sm[i][warp] = x;
@@ -705,20 +718,19 @@ detox_status backward_of(BackArgs g, cudaStream_t s) {
 
 }  // namespace
 
-detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
-                               float* logp, float* lse, float* zeros, cudaStream_t s) {
+namespace {
+detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, float* logp,
+                           double* logp64, float* lse, float* zeros, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
     ScoreArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
     g.k2 = scale * kLog2e;
-    g.logp = logp; g.lse = lse; g.zeros = zeros;
+    g.logp = logp; g.logp64 = logp64; g.lse = lse; g.zeros = zeros;
     if (dtype == DETOX_DTYPE_FLOAT) return score_of<float>(g, s);
     if (dtype == DETOX_DTYPE_HALF) return score_of<__half>(g, s);
     return score_of<__nv_bfloat16>(g, s);
 }
-
-namespace {
 detox_status backward_of(int dtype, const BackArgs& g, cudaStream_t s) {
     if (dtype == DETOX_DTYPE_FLOAT) return backward_of<float>(g, s);
     if (dtype == DETOX_DTYPE_HALF) return backward_of<__half>(g, s);
@@ -736,6 +748,11 @@ BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int 
     return g;
 }
 }  // namespace
+
+detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
+                               float* logp, float* lse, cudaStream_t s) {
+    return launch_scores(dtype, Z, ldz, rows, vocab, index, y, scale, logp, nullptr, lse, nullptr, s);
+}
 
 detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
                                         float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s) {
@@ -773,18 +790,18 @@ detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float*
     return launch_chained(total_kernel<4>, 1, 32, 0, 1, s, parts, clusters, 1.0, stats);
 }
 
-// lse, logp and its gradient for each row, then a part of the loss for each pair
+// logp in 64 bits, lse and logp's gradient for each row, then a part of the loss for each pair
 size_t preference_loss_ws_bytes(int64_t rows, int64_t pairs) {
-    return 3 * align_up((size_t)rows * sizeof(float)) + align_up((size_t)pairs * sizeof(double));
+    return align_up((size_t)rows * sizeof(double)) + 2 * align_up((size_t)rows * sizeof(float)) + align_up((size_t)pairs * sizeof(double));
 }
 
 detox_status launch_preference_loss(const detox_preference_desc& d, float* loss, float* margin, float* sums, void* dZ, int64_t lddz, void* ws,
                                     cudaStream_t s) {
-    const size_t vector = align_up((size_t)d.rows * sizeof(float));
+    const size_t wide = align_up((size_t)d.rows * sizeof(double)), vector = align_up((size_t)d.rows * sizeof(float));
     char* at = static_cast<char*>(ws);
-    float *logp = reinterpret_cast<float*>(at), *lse = reinterpret_cast<float*>(at + vector), *dlogp = reinterpret_cast<float*>(at + 2 * vector);
-    double* parts = reinterpret_cast<double*>(at + 3 * vector);
-    detox_status st = launch_token_logp(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, logp, lse, dZ ? dlogp : nullptr, s);
+    double *logp = reinterpret_cast<double*>(at), *parts = reinterpret_cast<double*>(at + wide + 2 * vector);
+    float *lse = reinterpret_cast<float*>(at + wide), *dlogp = reinterpret_cast<float*>(at + wide + vector);
+    detox_status st = launch_scores(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, nullptr, logp, lse, dZ ? dlogp : nullptr, s);
     if (st != DETOX_OK) return st;
     if (d.pairs > 0) {
         const int64_t most = (int64_t)kSMs * 8;

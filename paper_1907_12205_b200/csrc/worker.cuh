@@ -316,9 +316,8 @@ detox_status launch_embedding_backward(int dtype, const void* dY, int64_t lddy, 
                                        int64_t cols, float scale, void* dW, int64_t lddw, int dw_dtype, bool add, void* ws, cudaStream_t s);
 
 // token_loss.cu
-// zeros: a vector of `rows` entries that is cleared on the way; or NULL
 detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
-                               float* logp, float* lse, float* zeros, cudaStream_t s);
+                               float* logp, float* lse, cudaStream_t s);
 detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
                                         float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s);
 size_t policy_loss_ws_bytes(int64_t rows);

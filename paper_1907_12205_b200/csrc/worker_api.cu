@@ -193,7 +193,7 @@ detox_status detox_token_logp(int dtype, const void* Z, int64_t ldz, int64_t row
     if (st != DETOX_OK) return st;
     if (rows == 0) return DETOX_OK;
     if ((!logp && !lse) || !aligned_to(logp, 4) || !aligned_to(lse, 4)) return DETOX_ERR_BAD_ARG;
-    return launch_token_logp(dtype, Z, ldz, rows, vocab, index, y, scale, logp, lse, nullptr, static_cast<cudaStream_t>(stream));
+    return launch_token_logp(dtype, Z, ldz, rows, vocab, index, y, scale, logp, lse, static_cast<cudaStream_t>(stream));
 }
 
 detox_status detox_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
