@@ -4,13 +4,16 @@
 //
 // Bound by HBM: every buffer is read once and written once (fp32 weights and states: 28 bytes an entry; bf16 weights, fp32 masters and
 // gradients, 8-bit states: 18).  The tensors' pointers travel as kernel parameters, so a step is one launch for each few hundred of them,
-// with nothing to copy and nothing to set up, and a captured one keeps them; tensors of different types take a launch for each kind.  A warp takes a block of 128 entries, 4 a lane, so that a block's scale is one
-// warp-wide reduction and every access of a warp is contiguous: 16 bytes a lane in fp32, and where a buffer is not aligned for that, single entries dealt round the
-// lanes.  Tensors whose buffers are all out of alignment by the same number of entries (slices of vectors of one layout) are taken from the boundary before their first one on.
+// with nothing to copy and nothing to set up, and a captured one keeps them; tensors of different types take a launch for each kind.  A warp
+// takes blocks of 128 entries, 4 a lane, so that a block's scale is one warp-wide reduction and every access of a warp is contiguous: 16 bytes a
+// lane in fp32, and where a buffer is not aligned for that, single entries dealt round the lanes.  Tensors whose buffers are all out of alignment by
+// the same number of entries (slices of vectors of one layout) are taken from the boundary before their first one on.
+// 21.7 M fp32 entries in 161 tensors at odd offsets: 100 us, 6.1 TB/s (floor 94).
 //
 // 8 bits: m and sqrt(v) as e4m3 numbers with a power-of-two scale for each block.  Of v the root is kept, since its range is half as
 // wide (v's would leave the form's 18 binary orders).  Rounding is random: added to the bits that the form drops, 16 random ones round up or down with
 // the right mean; a sum of thousands of steps that each change an entry by less than its spacing keeps its mean that way.
+// 169 M entries in 13 tensors: 600 to 640 us, 4.9 TB/s (floor 467); the rounding's instructions are what it spends beside it (484 without them).
 #include <cmath>
 #include <cstring>
 

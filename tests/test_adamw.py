@@ -249,6 +249,25 @@ def test_step_and_rate_from_the_device_and_a_captured_step(bits_):
     assert all(bool(x.isfinite().all()) for x in p)
 
 
+def test_offsets_beyond_32_bits():
+    """A tensor of more than 2^31 entries: its first, its last and those around 2^31 go like a small tensor's."""
+    n, k = 2 ** 31 + 9001, 4096
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    some, grad = vector(k, gen, 0.05, BF16), vector(k, gen, 1e-2, BF16)
+    p, g = torch.zeros(n, dtype=BF16, device=DEV), torch.zeros(n, dtype=BF16, device=DEV)
+    places = (0, 2 ** 30 - 77, 2 ** 31 - 2049, n - k)
+    for a in places:
+        p[a: a + k], g[a: a + k] = some, grad
+    m, v = dx.detox_adamw_state([p])
+    dx.detox_adamw([p], [g], m, v, 1, 1e-2, weight_decay=0.1)
+    want = some.clone()
+    wm, wv = dx.detox_adamw_state([want])
+    dx.detox_adamw([want], [grad], wm, wv, 1, 1e-2, weight_decay=0.1)
+    for a in places:
+        assert torch.equal(p[a: a + k], want) and torch.equal(m[0][a: a + k], wm[0]) and torch.equal(v[0][a: a + k], wv[0])
+    assert not bool(p[k: 2 ** 30 - 77: 4099].any())
+
+
 def test_refusals():
     p = torch.zeros(64, device=DEV)
     m, v = dx.detox_adamw_state([p])

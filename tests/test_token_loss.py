@@ -201,6 +201,28 @@ def test_masked_entries_empty_rows_and_nan(dtype, vocab):
         assert abs(float(g[0].double().sum())) <= 4 * HALF[dtype]        # probabilities add up to one
 
 
+def test_reference_probabilities_far_from_the_policys():
+    """The KL term's slope is kl_coef (1 - exp(ref - logp)): kl_coef itself where the reference gives nothing, however far its logarithm lies."""
+    z, y = logits(6, 90, torch.float32)
+    z, y = z[:1].expand(6, 90).contiguous(), y[:1].expand(6).contiguous()
+    old = dx.detox_token_logp(z, y).logp
+    ref = old + torch.tensor([0.0, -100.0, -1e6, -INF, 3.0, 60.0], device=DEV)
+    one = torch.ones(6, device=DEV)
+    got = dx.detox_policy_loss(z, y, old, 0 * one, ref, one, kl_coef=0.5)
+    own = torch.exp(old[0].double())
+    # with advantage 0 only that slope is left: dz at the chosen token is slope (1 - p)
+    slope = got.dz[torch.arange(6, device=DEV), y].double() / (1 - own)
+    want = 0.5 * (1 - torch.exp(ref.double() - old.double()))
+    assert bool(((slope - want).abs() <= 600 * U * (want.abs() + 1)).all()), (slope, want)
+    assert float(got.kl) == INF and float(got.pg) == 0.0
+    none = dx.detox_policy_loss(z[:3], y[:3], old[:3], 0 * one[:3], ref[:3], one[:3], kl_coef=0.5)
+    exact = (torch.exp(ref.double() - old.double()) - 1 - (ref.double() - old.double()))[:3].sum()
+    assert abs(float(none.kl) - float(exact)) <= 8 * U * float(exact)
+    z[0, y[0]] = -INF                              # a chosen token that the policy gives nothing
+    gone = dx.detox_policy_loss(z[:1], y[:1], old[:1], one[:1], old[:1], one[:1], kl_coef=0.5)
+    assert float(gone.logp) == -INF and float(gone.kl) == INF
+
+
 def test_rows_of_weight_zero_are_not_looked_at():
     z, y = logits(6, 500, torch.bfloat16)
     old, a, ref, w = policy_inputs(z, y, 1.0)
