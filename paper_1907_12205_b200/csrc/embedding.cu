@@ -63,6 +63,7 @@ constexpr int kSumWarps = 48;                  // warps of an SM that there are 
 // where there are few tokens.
 template <bool ADD> constexpr int kAhead = ADD ? 4 : 8;
 constexpr int kSortAhead = 8;
+constexpr int kManyTokens = 4096, kManyLength = 16;   // a frequent token of many has as many parts as spans, which one warp adds: fewer, longer ones
 constexpr int kZeroPlaces = 32;                // places that a CTA looks after
 constexpr int kZeroCtas = 6;                   // CTAs of an SM that there should be for that
 
@@ -96,6 +97,7 @@ Plan plan_of(int64_t rows, int64_t vocab, int64_t cols, int entries, bool add) {
     p.ldp = ceil_div(cols, (int64_t)4) * 4;
     p.length = (int)(ceil_div(rows * p.slices, (int64_t)kSMs * kSumWarps * ahead) * ahead);
     if (p.length < ahead) p.length = ahead;
+    if (rows > kManyTokens && p.length < kManyLength) p.length = kManyLength;
     p.spans = (int)ceil_div(rows, (int64_t)p.length);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at = align_up(at + bytes); return was; };
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 3) sum_rows_kernel(const __grid_cons
         __threadfence();
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) acc[j] = 0ull;
-#pragma unroll 4
+#pragma unroll 8
         for (int s = first; s <= last; ++s) {
             uint64_t x[N / 2];
             load_part<N>((s < last ? g.tail : g.head) + (int64_t)s * g.ldp, c, (int)g.ldp, x);
