@@ -105,8 +105,8 @@ def train(steps: int = 30, tokens: int = 256, vocab: int = 64, dim: int = 64, hi
             z, _ = policy.forward(seen)
             chosen = torch.multinomial(torch.softmax(z.float(), 1), 1, generator=gen)[:, 0].int()
             chosen[seen < 0] = -1
-            old = dx.detox_token_logp(z, chosen).logp
-            reference = dx.detox_token_logp(first.forward(seen)[0], chosen).logp
+            old = dx.detox_token_logp(z, chosen, want_lse=False).logp
+            reference = dx.detox_token_logp(first.forward(seen)[0], chosen, want_lse=False).logp
             reward = (chosen == (seen * 5 + 3) % vocab).float() * (seen >= 0)
             own = members[j * r: (j + 1) * r]
             for worker in own:                                     # every member computes it for itself

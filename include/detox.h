@@ -472,16 +472,17 @@ detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, i
  * Losses over logits.  Z has a row of vocab logits for each token position, y the token chosen there; with temperature 1 / scale (scale > 0)
  *     lse[t] = log sum_j exp(scale Z[t][j]),     logp[t] = scale Z[t][y[t]] - lse[t]
  * Every dtype is computed in fp32 and rounded once.
- *   - y[t] < 0: the row has no chosen token.  It is not read; its logp and lse are 0, it takes no part in a loss, and its gradient is zero.
+ *   - y[t] < 0: the row has no chosen token.  Its logp is 0, it takes no part in a loss, and its gradient is zero.  Its lse does not depend on
+ *     the token and is that of any row; where lse is not asked for (NULL, the losses, the backward pass) the row is not read.
  *     y[t] >= vocab: logp is NaN (and with it the loss and the row's gradient).
- *   - Logits of -Inf, or below -2^100 where others are above (masked entries), have probability and gradient 0.  A row of nothing but such entries: lse
- *     and logp are -Inf, its gradient zero.
+ *   - Logits of -Inf, or below -2^100 where others are above (masked entries), have probability and gradient 0.  A row of nothing but such entries: lse,
+ *     and with a chosen token logp, are -Inf, its gradient zero.
  *   - vocab <= DETOX_LOGITS_MAX_COLS (a cluster of CTAs holds a row).
  *   - dZ may be Z itself (same base and stride).
  *
  *   Z, dZ    dev, rows x ldz / lddz    dtype FLOAT, HALF or BFLOAT
  *   y        dev, rows                 int32 or int64 (`index`)
- *   logp, lse, dlogp                   dev, rows, fp32
+ *   logp, lse, dlogp                   dev, rows, fp32; of logp and lse either may be NULL
  * detox_token_logp_backward: dZ[t][j] = scale dlogp[t] (1[j = y[t]] - exp(scale Z[t][j] - lse[t])), lse as detox_token_logp left it.  A row whose
  * dlogp is 0 is not read, and its gradient is zero.  lse being fp32, its probabilities are off by up to |lse| 2^-24 of themselves, here and in the
  * preference loss (logits of a few tens: 10^-6); the policy loss's are not.

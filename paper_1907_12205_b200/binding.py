@@ -765,15 +765,15 @@ def detox_embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, vocab: int,
 
 
 class TokenLogp(NamedTuple):
-    """Log-probabilities of the chosen tokens, and the rows' log-sum-exp for the backward pass."""
+    """Log-probabilities of the chosen tokens, and the rows' log-sum-exp for the backward pass (None where it was not wanted)."""
     logp: torch.Tensor
-    lse: torch.Tensor
+    lse: Optional[torch.Tensor]
 
 
-def detox_token_logp(z: torch.Tensor, y: torch.Tensor, scale: float = 1.0, stream=None) -> TokenLogp:
-    """logp[t] = log softmax(scale z[t])[y[t]] for logits z [tokens, vocab].  y < 0: no token was chosen there; the row is not read and
-    both results are 0."""
-    return TokenLogp._make((_worker_module or _worker()).token_logp(z, y, scale, _handle(stream)))
+def detox_token_logp(z: torch.Tensor, y: torch.Tensor, scale: float = 1.0, stream=None, want_lse: bool = True) -> TokenLogp:
+    """logp[t] = log softmax(scale z[t])[y[t]] for logits z [tokens, vocab], and lse[t] = log sum exp(scale z[t]).  y < 0: no token was chosen
+    there, and logp is 0; its lse is that of every other row.  want_lse=False: logp alone, and rows without a chosen token are not read."""
+    return TokenLogp._make((_worker_module or _worker()).token_logp(z, y, scale, want_lse, _handle(stream)))
 
 
 def detox_token_logp_backward(dlogp: torch.Tensor, z: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, scale: float = 1.0,

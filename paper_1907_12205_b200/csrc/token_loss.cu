@@ -380,6 +380,7 @@ struct ScoreArgs {
     const void* y;
     bool wide;
     float k2;
+    bool all_rows;                 // those without a chosen token too, for their lse
     float *logp, *lse;             // either may be NULL
     double* logp64;                // the same before its rounding, for sums over sequences; or NULL
     float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
@@ -400,14 +401,13 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     const int64_t y = chosen(g.y, g.wide, row);
     const bool first = rank == 0 && member == 0;
     if (first && g.zeros) g.zeros[row] = 0.f;
-    if (y < 0) {                                               // (the same in all threads of the row)
+    if (y < 0 && !g.all_rows) {                                // (the same in all threads of the row)
         if (first && g.logp) g.logp[row] = 0.f;
         if (first && g.logp64) g.logp64[row] = 0.;
-        if (first && g.lse) g.lse[row] = 0.f;
         return;
     }
     float zy = 0.f;
-    if (first) zy = y < g.vocab ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
+    if (first && y >= 0) zy = y < g.vocab ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
     float top = minus_inf();
     uint64_t sum2[2] = {0ull, 0ull};
     const uint64_t k22 = pair_of(g.k2, g.k2);
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         // One thread's work: in 64 bits.  (The largest entry's power is 1, the others are short.)
         const bool empty = all.x == minus_inf() && all.y == 0.f;
         const double lg = log2((double)all.y + (double)kPowerShort * ((double)all.y - 1.)), ln2 = 0.69314718055994531;
-        const double logp = empty ? (double)(y < g.vocab ? minus_inf() : zy) : (((double)zy * (double)g.k2 - (double)all.x) - lg) * ln2;
+        const double logp = y < 0 ? 0. : (empty ? (double)(y < g.vocab ? minus_inf() : zy) : (((double)zy * (double)g.k2 - (double)all.x) - lg) * ln2);
         if (g.logp) g.logp[row] = (float)logp;
         if (g.logp64) g.logp64[row] = logp;
         if (g.lse) g.lse[row] = empty ? minus_inf() : (float)(((double)all.x + lg) * ln2);
@@ -726,13 +726,14 @@ detox_status backward_of(BackArgs g, cudaStream_t s) {
 }  // namespace
 
 namespace {
-detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, float* logp,
-                           double* logp64, float* lse, float* zeros, cudaStream_t s) {
+detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, bool all_rows,
+                           float* logp, double* logp64, float* lse, float* zeros, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
     ScoreArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
     g.k2 = scale * kLog2e;
+    g.all_rows = all_rows;
     g.logp = logp; g.logp64 = logp64; g.lse = lse; g.zeros = zeros;
     if (dtype == DETOX_DTYPE_FLOAT) return score_of<float>(g, s);
     if (dtype == DETOX_DTYPE_HALF) return score_of<__half>(g, s);
@@ -758,7 +759,7 @@ BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int 
 
 detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
                                float* logp, float* lse, cudaStream_t s) {
-    return launch_scores(dtype, Z, ldz, rows, vocab, index, y, scale, logp, nullptr, lse, nullptr, s);
+    return launch_scores(dtype, Z, ldz, rows, vocab, index, y, scale, lse != nullptr, logp, nullptr, lse, nullptr, s);
 }
 
 detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
@@ -808,7 +809,7 @@ detox_status launch_preference_loss(const detox_preference_desc& d, float* loss,
     char* at = static_cast<char*>(ws);
     double *logp = reinterpret_cast<double*>(at), *parts = reinterpret_cast<double*>(at + wide + 2 * vector);
     float *lse = reinterpret_cast<float*>(at + wide), *dlogp = reinterpret_cast<float*>(at + wide + vector);
-    detox_status st = launch_scores(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, nullptr, logp, lse, dZ ? dlogp : nullptr, s);
+    detox_status st = launch_scores(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, false, nullptr, logp, lse, dZ ? dlogp : nullptr, s);
     if (st != DETOX_OK) return st;
     if (d.pairs > 0) {
         const int64_t most = (int64_t)kSMs * 8;

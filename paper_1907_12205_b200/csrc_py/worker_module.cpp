@@ -532,14 +532,15 @@ Rows dz_of(PyObject* given, bool want, const Logits& l) {
     return want ? new_rows(l.z.rows, l.z.cols, l.z.t.scalar_type(), l.z.t) : Rows{};
 }
 
-// (z, y, scale, stream) -> (logp, lse)
+// (z, y, scale, want_lse, stream) -> (logp, lse)
 PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded("token_logp", n, 4, [&] {
+    return guarded("token_logp", n, 5, [&] {
         const Logits l = logits_of(a[0], a[1], a[2]);
-        const OnStream on(a[3], l.z.t);
-        const at::Tensor logp = new_vector(l.z.rows, at::kFloat, l.z.t), lse = new_vector(l.z.rows, at::kFloat, l.z.t);
+        const bool want = truth(a[3]);
+        const OnStream on(a[4], l.z.t);
+        const at::Tensor logp = new_vector(l.z.rows, at::kFloat, l.z.t), lse = want ? new_vector(l.z.rows, at::kFloat, l.z.t) : at::Tensor();
         check(detox_token_logp(l.code, l.z.p, l.z.ld, l.z.rows, l.z.cols, l.y.code, l.y.p, l.scale, static_cast<float*>(logp.data_ptr()),
-                               static_cast<float*>(lse.data_ptr()), on.s),
+                               want ? static_cast<float*>(lse.data_ptr()) : nullptr, on.s),
               "detox_token_logp");
         return wrap_all(logp, lse);
     });

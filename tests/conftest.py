@@ -12,7 +12,15 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a CUDA device (sm_100a)")
 
 
+def holds_an_old_value(item):
+    """Cases that expect a value since found wrong, and fail: a log-sum-exp of 0 for the row without a chosen token that their batches of more than two rows have
+    (tests/test_token_lse.py has the right one).  They run last, so that they hide nothing in a run that stops at the first failure."""
+    params = item.callspec.params if hasattr(item, "callspec") else {}
+    return getattr(item, "originalname", "") == "test_logp_and_its_gradient" and params.get("rows", 0) > 2
+
+
 def pytest_collection_modifyitems(config, items):
+    items.sort(key=holds_an_old_value)
     try:
         import torch
         have = torch.cuda.is_available()
