@@ -47,6 +47,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Another CTA's shared memory may be written only once that CTA has started, which being launched together does not say: every CTA tells it first and waits for the others
+// before its first store.  (Two steps, so that the loads between them hide it; a CTA that has told waits on every path.)
+__device__ __forceinline__ void cluster_tell_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_started() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // two floats to the same place in another CTA's shared memory
 __device__ __forceinline__ void store_at(const float2* here, uint32_t rank, float2 v) {
     uint32_t at = (uint32_t)__cvta_generic_to_shared(here), there;
@@ -222,6 +226,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
     const int begin = first * N;                              // this CTA's columns of a row
     const int cols = g.vocab - begin < pieces * N ? g.vocab - begin : pieces * N;
     if (cluster == 1) pdl_trigger();
+    else cluster_tell_started();
     pdl_wait();
     int64_t row = blockIdx.x / cluster;
     const T* Z = static_cast<const T*>(g.Z);
@@ -251,6 +256,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
     }
     double sum_loss = 0., sum_pg = 0., sum_kl = 0., sum_clip = 0.;
     int turn = 0;
+    if (cluster > 1) cluster_wait_started();
     for (; row < g.rows; row += stride) {
         const int64_t next = row + stride;
         const T *here = Z + row * g.ldz + begin, *there_next = Z + next * g.ldz + begin;
@@ -391,11 +397,12 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     constexpr int N = Piece<T>::N, WARPS = kScoreThreads / 32;
     __shared__ float2 met[kMaxCluster * WARPS];
     if (g.cluster == 1) pdl_trigger();
+    else cluster_tell_started();
     pdl_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, member = threadIdx.x % GROUP;
     const uint32_t rank = GROUP > 32 && g.cluster > 1 ? cluster_rank() : 0u;
     const int64_t row = GROUP == 32 ? (int64_t)blockIdx.x * WARPS + warp : (int64_t)(blockIdx.x / g.cluster);
-    if (row >= g.rows) return;                                 // (whole warps, and only with GROUP = 32)
+    if (row >= g.rows) return;                                 // (whole warps, and only with GROUP = 32, where there are no clusters)
     const int begin = (int)rank * g.chunk, cols = g.vocab - begin < g.chunk ? g.vocab - begin : g.chunk;
     const T* Z = static_cast<const T*>(g.Z) + row * g.ldz;
     const int64_t y = chosen(g.y, g.wide, row);
@@ -404,6 +411,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     if (y < 0 && !g.all_rows) {                                // (the same in all threads of the row)
         if (first && g.logp) g.logp[row] = 0.f;
         if (first && g.logp64) g.logp64[row] = 0.;
+        if (g.cluster > 1) cluster_wait_started();
         return;
     }
     float zy = 0.f;
@@ -451,6 +459,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
             if (lane == 0) met[warp] = all;
             __syncthreads();
         } else {
+            cluster_wait_started();
             if (lane == 0) store_at(&met[(int)rank * WARPS + warp], 0u, all);
             cluster_meet();
         }

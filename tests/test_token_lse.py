@@ -69,3 +69,39 @@ def test_rows_that_are_masked_infinite_or_nan(dtype):
     assert torch.equal(dx.detox_token_logp(z, y, want_lse=False).logp, got.logp)
     dz = dx.detox_token_logp_backward(torch.ones(6, device=DEV), z, y, got.lse)
     assert bool((dz[[0, 1, 2, 3, 5]] == 0).all()) and bool(dz[4].isfinite().all())
+
+
+def gradient_bound(exact, d, p, y, scale, dtype, off):
+    """A rounding to the type; two roundings of the coefficient; the probabilities' relative error."""
+    own = torch.zeros_like(p).scatter_(1, y.clamp(min=0)[:, None].long(), 1.0)
+    near = (own - p).abs() * 2 * U * d.abs()[:, None] + d.abs()[:, None] * (p * off[:, None] + 4 * U * (own + p))
+    tiny = {torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25, torch.float32: 2.0 ** -126}[dtype]
+    return exact.abs() * torch.finfo(dtype).eps / 2 * 1.001 + 1.01 * scale * near + tiny
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(3, 2), (5, 7), (9, 100), (40, 256), (33, 1000), (70, 2051), (4, 4099), (300, 3001), (3, 8200), (5, 16390), (7, 32770),
+                                        (160, 5000), (80, 50257), (3, 131072), (4, 262144)])
+def test_the_gradient_of_a_batch_with_rows_without_a_token(dtype, rows, vocab):
+    for pad, offset, scale, index in ((0, 0, 1.0, torch.int64), (5, 3, 0.7, torch.int32)):
+        z, y = logits(rows, vocab, dtype, pad, offset)
+        y[1], y[0] = -1, vocab - 1
+        y = y.to(index)
+        x = z.double() * scale
+        lse = torch.logsumexp(x, 1)
+        got = dx.detox_token_logp(z, y, scale=scale)
+        off = slack(z, scale)
+        assert bool(((got.lse.double() - lse).abs() <= off).all())
+        d = torch.randn(rows, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3))
+        if rows > 4:
+            d[2] = 0.0
+        dz = dx.detox_token_logp_backward(d, z, y, got.lse, scale=scale)
+        p = torch.exp(x - lse[:, None])
+        exact = -p * d.double()[:, None]
+        exact.scatter_add_(1, y.clamp(min=0)[:, None].long(), d.double()[:, None])
+        exact = torch.where((y >= 0)[:, None], exact, 0.0) * scale
+        # the rounding of lse to fp32 enters every probability
+        assert bool(((dz.double() - exact).abs() <= gradient_bound(exact, d.double(), p, y, scale, dtype, 2 * off + 2 * U * lse.abs())).all())
+        assert bool((dz[1] == 0).all()) and (rows <= 4 or bool((dz[2] == 0).all()))
+        z2 = torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV).copy_(z)   # in place
+        assert torch.equal(dx.detox_token_logp_backward(d, z2, y, got.lse, scale=scale, dz=z2), dz) and torch.equal(z2, dz)
