@@ -496,7 +496,7 @@ detox_status detox_token_logp_backward(int dtype, const void* Z, int64_t ldz, in
 /* ---------------------------------------------------------------------------------------------
  * Clipped policy loss with a KL term, and the gradient of the logits in the same pass over them.  With the ratio r = exp(logp - old[t]),
  *     pg[t] = -min(r A[t], min(max(r, 1 - clip_low), 1 + clip_high) A[t])
- *     kl[t] = exp(ref[t] - logp) - (ref[t] - logp) - 1                  (0 without ref)
+ *     kl[t] = exp(ref[t] - logp) - (ref[t] - logp) - 1                  (0 without ref; with kl_coef = 0 in stats alone, whatever it is)
  *     loss  = sum over t of w[t] (pg[t] + kl_coef kl[t])                (without w: w[t] = 1 / rows)
  *   old, A   dev, rows (fp32)    log-probability under the policy that chose the tokens, and advantage
  *   ref      dev, rows (fp32)    log-probability under the reference policy; may be NULL

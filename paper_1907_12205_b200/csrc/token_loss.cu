@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 const float d = ref - row_of.logp;
                 const float2 x = above_one(d);
                 kl = x.y;
-                slope = fmaf(-g.kl_coef, x.x, slope);
+                if (g.kl_coef != 0.f) slope = fmaf(-g.kl_coef, x.x, slope);   // (a term without weight may be infinite)
             }
             const float coef = row_of.empty ? 0.f : g.grad_scale * w * slope;
             const float factor = row_of.empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
             if (rank == 0 && threadIdx.x == 0) {
                 const float pg = -(clipped ? held : free);
                 if (g.logp) g.logp[row] = row_of.logp;
-                sum_loss += (double)(w * fmaf(g.kl_coef, kl, pg));
+                sum_loss += (double)(w * (g.kl_coef != 0.f ? fmaf(g.kl_coef, kl, pg) : pg));
                 sum_pg += (double)(w * pg);
                 sum_kl += (double)(w * kl);
                 if (clipped) sum_clip += (double)w;
