@@ -506,7 +506,7 @@ detox_status detox_token_logp_backward(int dtype, const void* Z, int64_t ldz, in
  *   logp     dev, rows (fp32)    out; may be NULL
  *   dZ       dev, rows x lddz    out: grad_scale * d loss / d Z; NULL: not wanted
  *   ws       detox_policy_loss_workspace_bytes(rows) bytes
- * clip_low in [0, 1], clip_high >= 0.
+ * clip_low in [0, 1], clip_high >= 0.  A ratio or an exp(ref - logp) beyond fp32's range is Inf; with an advantage of 0 the former's term is 0.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
     int32_t dtype, index;        /* detox_dtype of the logits, detox_index of y */

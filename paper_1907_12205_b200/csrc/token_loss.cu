@@ -323,8 +323,9 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
             }
             all = joined_warp(all);
             const Scored row_of = scored(all, zy, g.k2, y < g.vocab);
-            const float r = __expf(row_of.logp - old);
-            const float free = r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
+            const float gap = row_of.logp - old, r = __expf(gap);
+            // (a ratio beyond fp32's range is no infinity that an advantage of 0 could not take away)
+            const float free = adv == 0.f && gap < -minus_inf() ? 0.f : r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
             const bool clipped = free > held;
             float kl = 0.f, slope = clipped ? 0.f : -free;
             if (g.ref_logp) {

@@ -35,3 +35,23 @@ def test_a_kl_term_without_weight_counts_nowhere_but_in_its_statistic(dtype, voc
     near = dx.detox_policy_loss(z[:1], y[:1], old[:1], a[:1], old[:1], w[:1], kl_coef=0.0)
     d = old[:1].double() - logp[:1]
     assert abs(float(near.kl) - 0.125 * float(torch.expm1(d) - d)) <= 1e-6 * 0.125
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_ratio_beyond_the_range_with_an_advantage_of_zero(dtype):
+    n = 5
+    z, y = rows_of(n, 50, dtype)
+    logp = torch.log_softmax(z.double(), 1).gather(1, y[:, None])[:, 0]
+    old = (logp - torch.tensor([100.0, 700.0, 100.0, 0.1, 100.0], device=DEV)).float()
+    a = torch.tensor([0.0, -0.0, 2.0, 1.0, 0.0], device=DEV)
+    w = torch.full((n,), 0.25, device=DEV)
+    got = dx.detox_policy_loss(z, y, old, a, None, w, clip_low=0.2, clip_high=0.3)
+    # rows 0, 1 and 4 count nothing, row 2 is clipped at 1.3, row 3 is inside
+    want = -0.25 * (1.3 * 2.0 + float(torch.exp(logp[3] - old[3].double())))
+    assert abs(float(got.loss) - want) <= 1e-5 and abs(float(got.clipped) - 0.25) == 0.0
+    assert bool((got.dz[[0, 1, 2, 4]] == 0).all()) and bool(got.dz.isfinite().all()) and bool((got.dz[3] != 0).any())
+    # where it is infinite, or a number is missing, that shows
+    bad = dx.detox_policy_loss(z[:1], y[:1], torch.tensor([-INF], device=DEV), a[:1], None, w[:1])
+    assert bool(bad.loss.isnan())
+    bad = dx.detox_policy_loss(z[:1], y[:1], torch.tensor([float("nan")], device=DEV), a[:1], None, w[:1])
+    assert bool(bad.loss.isnan())
