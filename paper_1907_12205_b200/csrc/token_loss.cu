@@ -1,6 +1,8 @@
 // Losses over logits: log-probabilities of chosen tokens, the clipped policy loss with a KL term, the preference loss of paired log ratios.
 //
 // Per row, with x = scale z log2(e):  lse = ln sum 2^x,  logp = (x_y - log2 sum) ln 2,  d loss / d z_j = c (1[j = y] - 2^x_j / sum).
+// A sum leaves out the chosen entry: with q = sum over the others of 2^(x - x_y),  logp = -ln(1 + q)  keeps its bits however sure of the token the row is (of
+// 1 + q, q = 10^-9 would be lost).
 // All of it is bound by HBM: the logits are the largest matrix of a training step, and the least is to read them once and write their
 // gradient once.
 //
@@ -30,7 +32,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 // ex2.approx comes out 5.1e-8 of itself too small on average (2^20 arguments in (-1, 0]; at most 1.4e-7).  Over the sums of a sequence's log-probabilities that adds up, so
-// where these are formed it is put right: for the sums of powers at the end, and here for the factors between sums (1 stays 1).
+// where these are formed it is put right: for the sums of powers at the end, and here for the factors between sums.
 constexpr float kPowerShort = 5.1e-8f;
 __device__ __forceinline__ float factor_of(float x) {
     const float y = exp2_fast(x);
@@ -100,6 +102,44 @@ __device__ __forceinline__ void store_entries(T* row, int c, int cols, bool vec,
         for (int j = 0; j < N; ++j)
             if (c + j < cols) row[c + j] = from_f32<T>(f[j]);
     }
+}
+
+// hi + lo, for what a row needs more than fp32's bits of: sums over a sequence add its log-probabilities up, and a ratio is formed of their difference to others.
+struct Two {
+    float hi, lo;
+};
+__device__ __forceinline__ Two sum_of(float a, float b) {   // exactly
+    const float s = a + b, t = s - a;
+    return Two{s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ double wide(Two v) { return (double)v.hi + (double)v.lo; }
+constexpr float kLn2Rest = -1.9046543e-9f;             // ln 2 - kLn2
+// a sum of powers: its exponent and the logarithm of the rest, within 0.6 of 0
+__device__ __forceinline__ void split_log2(float sum, float& exponent, float& rest) {
+    const int bits = __float_as_int(sum), e = (bits - 0x3f400000) >> 23;
+    exponent = (float)e;
+    rest = log2f(__int_as_float(bits - (e << 23))) + (sum - sum);   // (NaN stays NaN)
+}
+// x of the largest entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
+__device__ __forceinline__ bool is_nothing(float x) { return x < -1.2676506e30f; }
+
+// The chosen token's log-probability, from its logit zy (NaN where there is no such token) and the sum of the others' powers of 2^(x - base).  What is below 2^-126 of the
+// largest is nothing.
+constexpr float kLeast = 1.17549435e-38f;
+__device__ __forceinline__ Two logp_of(float base, float sum, float zy, float k2) {
+    const float x = zy * k2;
+    if (is_nothing(x)) return Two{minus_inf() + (sum - sum), 0.f};   // (NaN stays NaN)
+    if (sum < kLeast) return Two{x - x, 0.f};
+    // log2 q = hi + lo
+    const float low = fmaf(zy, k2, -x);
+    float exponent, mantissa;
+    split_log2(sum, exponent, mantissa);
+    const Two d = sum_of(base, -x), t = sum_of(d.hi, exponent);
+    const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low);
+    const bool less = hi + lo <= 0.f;
+    const float l = log1pf(factor_of(less ? hi : -hi) * factor_of(less ? lo : -lo));   // of q, or of 1 / q: at most 1
+    const float a = hi * kLn2, b = fmaf(hi, kLn2, -a) + fmaf(hi, kLn2Rest, lo * kLn2);
+    return less ? Two{-l, 0.f} : sum_of(-a, -(b + l));
 }
 
 // times ln 2, to its full bits: a factor that is always off to the same side would add up over a sequence
@@ -183,10 +223,9 @@ template <> struct Largest<__nv_bfloat16> {
     __device__ __forceinline__ float value() const { const float2 f = unpack2<__nv_bfloat16>(m); return fmaxf(f.x, f.y); }
     static constexpr uint32_t kNone = 0xff80ff80u;
 };
-// x of the largest entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
 __device__ __forceinline__ float largest_of(float z, float k2) {
     const float x = z * k2;
-    return x < -1.2676506e30f ? minus_inf() : x;
+    return is_nothing(x) ? minus_inf() : x;
 }
 // a piece of which only the first `n` entries are in the row: -Inf for the others
 template <typename T>
@@ -199,6 +238,21 @@ __device__ __forceinline__ uint4 only_first(uint4 v, int n) {
         } else {
             if (2 * i >= n) w[i] = Largest<T>::kNone;
             else if (2 * i + 1 >= n) w[i] = (w[i] & 0xffffu) | (Largest<T>::kNone & 0xffff0000u);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// a piece with -Inf for entry j
+template <typename T>
+__device__ __forceinline__ uint4 without(uint4 v, int j) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            if (i == j) w[i] = Largest<T>::kNone;
+        } else {
+            if (2 * i == j) w[i] = (w[i] & 0xffff0000u) | (Largest<T>::kNone & 0xffffu);
+            if (2 * i + 1 == j) w[i] = (w[i] & 0xffffu) | (Largest<T>::kNone & 0xffff0000u);
         }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -386,7 +440,7 @@ struct ScoreArgs {
     int cluster;
     const void* y;
     bool wide;
-    float k2;
+    float k2, scale;
     bool all_rows;                 // those without a chosen token too, for their lse
     float *logp, *lse;             // either may be NULL
     double* logp64;                // the same before its rounding, for sums over sequences; or NULL
@@ -415,8 +469,11 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if (g.cluster > 1) cluster_wait_started();
         return;
     }
-    float zy = 0.f;
-    if (first && y >= 0) zy = y < g.vocab ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
+    const bool there = y >= 0 && y < g.vocab;
+    const float zy = first && there ? to_f32(Z[y]) : __int_as_float(0x7fc00000);
+    // the chosen entry, where one of this thread's pieces has it: left out of the sum
+    const int at = there ? (int)y - begin : -1;
+    const int chosen_piece = at >= 0 && at < cols && at / N % GROUP == member ? at / N * N : -1;
     float top = minus_inf();
     uint64_t sum2[2] = {0ull, 0ull};
     const uint64_t k22 = pair_of(g.k2, g.k2);
@@ -428,6 +485,11 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if (c0 + ((kScorePieces - 1) * GROUP + 1) * N > cols) {
 #pragma unroll
             for (int i = 0; i < kScorePieces; ++i) raw[i] = only_first<T>(raw[i], cols - c0 - i * GROUP * N);
+        }
+        if ((unsigned)(chosen_piece - c0) < (unsigned)(GROUP * kScorePieces * N)) {
+#pragma unroll
+            for (int i = 0; i < kScorePieces; ++i)
+                if (chosen_piece == c0 + i * GROUP * N) raw[i] = without<T>(raw[i], at % N);
         }
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
@@ -470,13 +532,19 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         all = joined_warp(all);
     }
     if (first) {
-        // One thread's work: in 64 bits.  (The largest entry's power is 1, the others are short.)
-        const bool empty = all.x == minus_inf() && all.y == 0.f;
-        const double lg = log2((double)all.y + (double)kPowerShort * ((double)all.y - 1.)), ln2 = 0.69314718055994531;
-        const double logp = y < 0 ? 0. : (empty ? (double)(y < g.vocab ? minus_inf() : zy) : (((double)zy * (double)g.k2 - (double)all.x) - lg) * ln2);
+        all.y = fmaf(all.y, kPowerShort, all.y);
+        const double logp = y < 0 ? 0. : wide(logp_of(all.x, all.y, zy, g.k2));
         if (g.logp) g.logp[row] = (float)logp;
         if (g.logp64) g.logp64[row] = logp;
-        if (g.lse) g.lse[row] = empty ? minus_inf() : (float)(((double)all.x + lg) * ln2);
+        if (g.lse) {
+            double lse = (double)zy * (double)g.scale - logp;
+            if (!there || is_nothing(zy * g.k2)) {              // the others' alone
+                float exponent, rest;
+                split_log2(all.y, exponent, rest);
+                lse = all.x == minus_inf() && all.y == 0.f ? (double)minus_inf() : (wide(sum_of(all.x, exponent)) + (double)rest) * 0.69314718055994531;
+            }
+            g.lse[row] = (float)lse;
+        }
     }
 }
 
@@ -743,6 +811,7 @@ detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, 
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
     g.k2 = scale * kLog2e;
+    g.scale = scale;
     g.all_rows = all_rows;
     g.logp = logp; g.logp64 = logp64; g.lse = lse; g.zeros = zeros;
     if (dtype == DETOX_DTYPE_FLOAT) return score_of<float>(g, s);
