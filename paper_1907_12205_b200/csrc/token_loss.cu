@@ -1,8 +1,8 @@
 // Losses over logits: log-probabilities of chosen tokens, the clipped policy loss with a KL term, the preference loss of paired log ratios.
 //
 // Per row, with x = scale z log2(e):  lse = ln sum 2^x,  logp = (x_y - log2 sum) ln 2,  d loss / d z_j = c (1[j = y] - 2^x_j / sum).
-// A sum leaves out the chosen entry: with q = sum over the others of 2^(x - x_y),  logp = -ln(1 + q)  keeps its bits however sure of the token the row is (of
-// 1 + q, q = 10^-9 would be lost).
+// A sum leaves out the chosen entry: with q = sum over the others of 2^(x - x_y),  logp = -ln(1 + q)  and  1 - p_y = q / (1 + q)  keep their bits however sure
+// of the token the row is (of 1 + q, q = 10^-9 would be lost).
 // All of it is bound by HBM: the logits are the largest matrix of a training step, and the least is to read them once and write their
 // gradient once.
 //
@@ -142,31 +142,66 @@ __device__ __forceinline__ Two logp_of(float base, float sum, float zy, float k2
     return less ? Two{-l, 0.f} : sum_of(-a, -(b + l));
 }
 
-// times ln 2, to its full bits: a factor that is always off to the same side would add up over a sequence
-__device__ __forceinline__ float in_nats(float v) { return v == minus_inf() ? v : fmaf(v, kLn2, v * -1.9046543e-9f); }
-
-// What a row's pair says: zy is the chosen token's logit, `there` whether there is such a token.
-struct Scored {
-    float logp;
-    bool empty;                    // nothing but -Inf
-};
-__device__ __forceinline__ Scored scored(float2 all, float zy, float k2, bool there) {
-    const float lg = log2f(all.y);
-    const bool empty = all.x == minus_inf() && all.y == 0.f;
-    return Scored{empty ? (there ? minus_inf() : zy) : in_nats(fmaf(zy, k2, -all.x) - lg), empty};
+// 1 / x of a normal number, to a unit
+__device__ __forceinline__ float inverse_of(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return fmaf(fmaf(-x, y, 1.f), y, y);
+}
+// 2^(hi + lo); infinities of hi or of the result stay
+__device__ __forceinline__ float power_of(float hi, float lo) {
+    const float y = exp2_fast(hi);
+    return fabsf(hi) < -minus_inf() ? fmaf(y < -minus_inf() ? y : 0.f, lo * kLn2, y) : y;
+}
+// v log2(e)
+__device__ __forceinline__ Two in_powers(float v) {
+    const float hi = v * kLog2e;
+    return Two{hi, fmaf(v, kLog2e, -hi) + v * 1.92596299e-8f};   // log2 e - kLog2e
 }
 
-// e^d - 1 and e^d - 1 - d: near 0 by the series (the next term is 10^-7 of it at 1/2), where the differences would lose their bits
-__device__ __forceinline__ float2 above_one(float d) {
+// What all threads need of a row for its gradient, from (largest x, sum of the others' powers of 2^(x - largest)).  With q = sum 2^(largest - x_y) the token has p = 1 / (1 + q).
+// The ratio p e^-old and e^ref / p are a power of two each, whose exponent is formed as hi + lo, without the logarithm of p: they are off by what the sum is off, a few
+// units of 2^-23, and by nothing of the size of the logarithms.  (The same in 64 bits would cost 16 warps' worth of them a row.)
+struct Chosen {
+    float p;                       // p is this times 2^(at.hi + at.lo), which may lie outside of fp32's range
+    float p_inverse;
+    Two at;
+    float rest;                    // 1 - p
+    float share;                   // times 2^(x_j - largest): p_j
+    bool empty;                    // nothing but -Inf
+};
+__device__ __forceinline__ Chosen chosen_of(float2 all, float zy, float k2) {
+    const float product = zy * k2;
+    const bool nothing = is_nothing(product), none = all.y < kLeast;
+    const float x = nothing ? -1e30f : product, low = nothing ? 0.f : fmaf(zy, k2, -product), sum = none ? 1.f : all.y;
+    const int bits = __float_as_int(sum), e = (bits - 0x3f400000) >> 23;
+    const float m = __int_as_float(bits - (e << 23)) + (sum - sum), m_inverse = inverse_of(m);   // within 0.75 .. 1.5; NaN stays NaN
+    // q = m 2^(hi + lo)
+    const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -1e30f : d.hi, (float)e);
+    const float hi = t.hi, lo = d.lo + t.lo - low + kPowerShort * kLog2e;
+    const bool less = hi <= 0.f;
+    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, (less ? lo : -lo) * kLn2, power) * (less ? m : m_inverse);   // q, or 1 / q
+    const float inverse = inverse_of(1.f + u);
+    Chosen c;
+    c.p = less ? inverse : inverse * m_inverse;
+    c.p_inverse = less ? 1.f + u : (1.f + u) * m;
+    c.at = less ? Two{0.f, 0.f} : Two{-hi, -lo};
+    c.rest = less ? u * inverse : inverse;
+    c.share = c.rest * m_inverse * __int_as_float((127 - e) << 23);
+    c.empty = nothing && none;
+    return c;
+}
+
+// e^d - 1 - d, from e^d: near 0 by the series (the next term is 10^-7 of it at 1/2), where the difference would lose its bits
+__device__ __forceinline__ float above_line(float d, float power) {
     float s = fmaf(d, 1.f / 40320.f, 1.f / 5040.f);
     s = fmaf(d, s, 1.f / 720.f);
     s = fmaf(d, s, 1.f / 120.f);
     s = fmaf(d, s, 1.f / 24.f);
     s = fmaf(d, s, 1.f / 6.f);
     s = d * d * fmaf(d, s, 0.5f);
-    const float x = __expf(d) - 1.f;
-    if (fabsf(d) < 0.5f) return make_float2(d + s, s);
-    return make_float2(x, d == -minus_inf() ? x : x - d);
+    if (fabsf(d) < 0.5f) return s;
+    return d == -minus_inf() ? d : (power - 1.f) - d;
 }
 
 // ---- the policy loss -------------------------------------------------------------------------------
@@ -242,22 +277,18 @@ __device__ __forceinline__ uint4 only_first(uint4 v, int n) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// a piece with -Inf for entry j
+// the bits of entry j of a piece, and a piece with -Inf in the place of such bits
 template <typename T>
-__device__ __forceinline__ uint4 without(uint4 v, int j) {
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            if (i == j) w[i] = Largest<T>::kNone;
-        } else {
-            if (2 * i == j) w[i] = (w[i] & 0xffff0000u) | (Largest<T>::kNone & 0xffffu);
-            if (2 * i + 1 == j) w[i] = (w[i] & 0xffffu) | (Largest<T>::kNone & 0xffff0000u);
-        }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint4 entry_mask(int j) {
+    constexpr int A = 4 / (int)sizeof(T);                      // entries of a word
+    const uint32_t bits = sizeof(T) == 4 ? 0xffffffffu : 0xffffu << (16 * (j & 1));
+    return make_uint4(j / A == 0 ? bits : 0u, j / A == 1 ? bits : 0u, j / A == 2 ? bits : 0u, j / A == 3 ? bits : 0u);
 }
-
+template <typename T>
+__device__ __forceinline__ uint4 hidden(uint4 v, uint4 m) {
+    constexpr uint32_t none = sizeof(T) == 4 ? Largest<T>::kNone : (Largest<T>::kNone & 0xffffu) * 0x10001u;
+    return make_uint4((v.x & ~m.x) | (none & m.x), (v.y & ~m.y) | (none & m.y), (v.z & ~m.z) | (none & m.z), (v.w & ~m.w) | (none & m.w));
+}
 // Registers: a thread holds P pieces of the next row (not AHEAD: of this one, and is done with them when it has the powers) and this row's
 // powers in fp32.  16 pieces of fp32 leave no room for both.
 template <typename T, int P> constexpr bool kAhead = P * Piece<T>::N + 4 * P <= 96;
@@ -271,6 +302,7 @@ template <typename T, int THREADS, int P, bool ANY>
 __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel(const __grid_constant__ RowsArgs g) {
     constexpr int N = Piece<T>::N, WARPS = THREADS / 32;
     constexpr bool AHEAD = kAhead<T, P>;
+    constexpr int kTeller = THREADS - 32;      // who keeps the sums: in the warp that has the fewest pieces
     __shared__ float2 met[2][kMaxCluster * WARPS];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int cluster = g.cluster;
@@ -332,9 +364,16 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
             }
             const float zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
             const float old = g.old_logp[row], adv = g.advantage[row], ref = g.ref_logp ? g.ref_logp[row] : 0.f;
+            // The chosen entry, where one of this thread's pieces has it, becomes -Inf.  (8192 x 32000 bf16: 182 us, 179 with the entry left in.  Its power taken out of the sum
+            // again afterwards, in a branch that one warp enters, held the others up at the barrier: 185 to 190.)
+            const int at = y < g.vocab ? (int)y - begin : -1;
+            const bool mine = at >= 0 && at < cols && at / N % THREADS == (int)threadIdx.x;
+            const int own = mine ? at / (N * THREADS) : -1;
+            const uint4 hide = entry_mask<T>(at % N);
             Largest<T> most;
 #pragma unroll
             for (int i = 0; i < P; ++i) {
+                if (own == i) raw[i] = hidden<T>(raw[i], hide);
                 if constexpr (ANY) {
                     const int c = (int)(threadIdx.x + i * THREADS) * N;
                     if (c + N > cols) raw[i] = only_first<T>(raw[i], cols - c);
@@ -376,20 +415,21 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 for (int i = lane; i < cluster * WARPS; i += 32) all = joined(all, slots[i]);
             }
             all = joined_warp(all);
-            const Scored row_of = scored(all, zy, g.k2, y < g.vocab);
-            const float gap = row_of.logp - old, r = __expf(gap);
+            const Chosen token = chosen_of(all, zy, g.k2);
+            const Two o = in_powers(old), gap = sum_of(token.at.hi, -o.hi);
+            const float r = token.empty ? 0.f : token.p * power_of(gap.hi, gap.lo + token.at.lo - o.lo);
             // (a ratio beyond fp32's range is no infinity that an advantage of 0 could not take away)
-            const float free = adv == 0.f && gap < -minus_inf() ? 0.f : r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
+            const bool away = adv == 0.f && r == -minus_inf() && gap.hi < -minus_inf();
+            const float free = away ? 0.f : r * adv, held = fminf(fmaxf(r, g.low), g.high) * adv;
             const bool clipped = free > held;
-            float kl = 0.f, slope = clipped ? 0.f : -free;
+            float up = 0.f, slope = clipped ? 0.f : -free;     // up: e^(ref - logp)
             if (g.ref_logp) {
-                const float d = ref - row_of.logp;
-                const float2 x = above_one(d);
-                kl = x.y;
-                if (g.kl_coef != 0.f) slope = fmaf(-g.kl_coef, x.x, slope);   // (a term without weight may be infinite)
+                const Two f = in_powers(ref), d = sum_of(f.hi, -token.at.hi);
+                up = token.empty ? -minus_inf() : token.p_inverse * power_of(d.hi, d.lo + f.lo - token.at.lo);
+                if (g.kl_coef != 0.f) slope = fmaf(-g.kl_coef, up - 1.f, slope);   // (a term without weight may be infinite)
             }
-            const float coef = row_of.empty ? 0.f : g.grad_scale * w * slope;
-            const float factor = row_of.empty || top == minus_inf() ? 0.f : -coef * exp2_fast(top - all.x) / all.y;
+            const float coef = token.empty ? 0.f : g.grad_scale * w * slope;
+            const float share = factor_of(top - (all.x == minus_inf() ? 0.f : all.x)) * token.share, factor = share == 0.f ? 0.f : -coef * share;
             if (g.dZ) {
                 const uint64_t factor2 = pair_of(factor, factor);
 #pragma unroll
@@ -402,16 +442,20 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                     else if (there(i)) st_stream_u4(to + c, Piece<T>::join(out));
                 }
                 // the chosen entry, by the thread that stored its piece
-                const int at = y < g.vocab ? (int)y - begin : -1;
-                if (at >= 0 && at < cols && at / N % THREADS == (int)threadIdx.x && !row_of.empty)
-                    to[at] = from_f32<T>(zy == minus_inf() ? coef : -coef * expm1f(row_of.logp));
+                if (mine && !token.empty) to[at] = from_f32<T>(coef * token.rest);
             }
-            if (rank == 0 && threadIdx.x == 0) {
-                const float pg = -(clipped ? held : free);
-                if (g.logp) g.logp[row] = row_of.logp;
-                sum_loss += (double)(w * (g.kl_coef != 0.f ? fmaf(g.kl_coef, kl, pg) : pg));
-                sum_pg += (double)(w * pg);
-                sum_kl += (double)(w * kl);
+            if (rank == 0 && threadIdx.x == kTeller) {
+                const Two logp = logp_of(all.x, fmaf(all.y, kPowerShort, all.y), zy, g.k2);
+                float kl = 0.f;
+                if (g.ref_logp) {
+                    const Two d = sum_of(ref, -logp.hi);
+                    kl = above_line(fabsf(d.hi) < -minus_inf() ? d.hi + (d.lo - logp.lo) : d.hi, up);
+                }
+                const double pg = -(double)(clipped ? held : free);
+                if (g.logp) g.logp[row] = logp.hi + logp.lo;
+                sum_loss += (double)w * (g.kl_coef != 0.f ? (double)g.kl_coef * (double)kl + pg : pg);
+                sum_pg += (double)w * pg;
+                sum_kl += (double)w * (double)kl;
                 if (clipped) sum_clip += (double)w;
             }
         }
@@ -419,7 +463,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
         w = next_w;
         look(next + stride, next_y, next_w);
     }
-    if (rank == 0 && threadIdx.x == 0) {
+    if (rank == 0 && threadIdx.x == kTeller) {
         double* to = g.parts + 4 * (blockIdx.x / cluster);
         to[0] = sum_loss; to[1] = sum_pg; to[2] = sum_kl; to[3] = sum_clip;
     }
@@ -489,7 +533,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if ((unsigned)(chosen_piece - c0) < (unsigned)(GROUP * kScorePieces * N)) {
 #pragma unroll
             for (int i = 0; i < kScorePieces; ++i)
-                if (chosen_piece == c0 + i * GROUP * N) raw[i] = without<T>(raw[i], at % N);
+                if (chosen_piece == c0 + i * GROUP * N) raw[i] = hidden<T>(raw[i], entry_mask<T>(at % N));
         }
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
