@@ -17,6 +17,8 @@
 //                    second pass; it goes through the rows backwards, since the last ones that were read still lie in L2.  5510 x 32000 bf16: 102 us.
 //   pairs_kernel     Sums over sequences, margins and the rows' gradients, a CTA a pair.
 //   total_kernel     Sums of the CTAs' parts, in order.
+#include <cmath>
+
 #include "worker.cuh"
 
 namespace detox {
@@ -108,12 +110,23 @@ __device__ __forceinline__ void store_entries(T* row, int c, int cols, bool vec,
 struct Two {
     float hi, lo;
 };
+// (rounded products and sums by name where their roundings count: the compiler joins a * b + c into one otherwise)
 __device__ __forceinline__ Two sum_of(float a, float b) {   // exactly
-    const float s = a + b, t = s - a;
-    return Two{s, (a - (s - t)) + (b - t)};
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return Two{s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two product_of(float a, float b) {   // exactly
+    const float p = __fmul_rn(a, b);
+    return Two{p, fmaf(a, b, -p)};
 }
 __device__ __forceinline__ double wide(Two v) { return (double)v.hi + (double)v.lo; }
 constexpr float kLn2Rest = -1.9046543e-9f;             // ln 2 - kLn2
+// scale log2(e) as hi + lo.  One fp32 number would be off by up to 2^-24 of itself, which is another temperature: the same way for every token of a sequence, and times the
+// logits' size in a ratio.
+struct Powers {
+    float hi, lo;                  // powers of 2^(z hi + z lo - base), or, with lo = 0, of 2^(z hi - base);
+    float rest;                    // then what lo would be, over hi, is what the distance from the largest entry to the chosen one lacks
+};
 // a sum of powers: its exponent and the logarithm of the rest, within 0.6 of 0
 __device__ __forceinline__ void split_log2(float sum, float& exponent, float& rest) {
     const int bits = __float_as_int(sum), e = (bits - 0x3f400000) >> 23;
@@ -126,20 +139,20 @@ __device__ __forceinline__ bool is_nothing(float x) { return x < -1.2676506e30f;
 // The chosen token's log-probability, from its logit zy (NaN where there is no such token) and the sum of the others' powers of 2^(x - base).  What is below 2^-126 of the
 // largest is nothing.
 constexpr float kLeast = 1.17549435e-38f;
-__device__ __forceinline__ Two logp_of(float base, float sum, float zy, float k2) {
-    const float x = zy * k2;
-    if (is_nothing(x)) return Two{minus_inf() + (sum - sum), 0.f};   // (NaN stays NaN)
-    if (sum < kLeast) return Two{x - x, 0.f};
+__device__ __forceinline__ Two logp_of(float base, float sum, float zy, Powers k2) {
+    const Two x = product_of(zy, k2.hi);
+    if (is_nothing(x.hi)) return Two{minus_inf() + (sum - sum), 0.f};   // (NaN stays NaN)
+    if (sum < kLeast) return Two{x.hi - x.hi, 0.f};
     // log2 q = hi + lo
-    const float low = fmaf(zy, k2, -x);
+    const float low = x.lo + zy * k2.lo;
     float exponent, mantissa;
     split_log2(sum, exponent, mantissa);
-    const Two d = sum_of(base, -x), t = sum_of(d.hi, exponent);
-    const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low);
+    const Two d = sum_of(base, -x.hi), t = sum_of(d.hi, exponent);
+    const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low) + d.hi * k2.rest;
     const bool less = hi + lo <= 0.f;
     const float l = log1pf(factor_of(less ? hi : -hi) * factor_of(less ? lo : -lo));   // of q, or of 1 / q: at most 1
-    const float a = hi * kLn2, b = fmaf(hi, kLn2, -a) + fmaf(hi, kLn2Rest, lo * kLn2);
-    return less ? Two{-l, 0.f} : sum_of(-a, -(b + l));
+    const Two a = product_of(hi, kLn2);
+    return less ? Two{-l, 0.f} : sum_of(-a.hi, -(a.lo + fmaf(hi, kLn2Rest, lo * kLn2) + l));
 }
 
 // 1 / x of a normal number, to a unit
@@ -155,8 +168,8 @@ __device__ __forceinline__ float power_of(float hi, float lo) {
 }
 // v log2(e)
 __device__ __forceinline__ Two in_powers(float v) {
-    const float hi = v * kLog2e;
-    return Two{hi, fmaf(v, kLog2e, -hi) + v * 1.92596299e-8f};   // log2 e - kLog2e
+    const Two p = product_of(v, kLog2e);
+    return Two{p.hi, p.lo + v * 1.92596299e-8f};               // log2 e - kLog2e
 }
 
 // What all threads need of a row for its gradient, from (largest x, sum of the others' powers of 2^(x - largest)).  With q = sum 2^(largest - x_y) the token has p = 1 / (1 + q).
@@ -170,15 +183,15 @@ struct Chosen {
     float share;                   // times 2^(x_j - largest): p_j
     bool empty;                    // nothing but -Inf
 };
-__device__ __forceinline__ Chosen chosen_of(float2 all, float zy, float k2) {
-    const float product = zy * k2;
-    const bool nothing = is_nothing(product), none = all.y < kLeast;
-    const float x = nothing ? -1e30f : product, low = nothing ? 0.f : fmaf(zy, k2, -product), sum = none ? 1.f : all.y;
+__device__ __forceinline__ Chosen chosen_of(float2 all, float zy, Powers k2) {
+    const Two product = product_of(zy, k2.hi);
+    const bool nothing = is_nothing(product.hi), none = all.y < kLeast;
+    const float x = nothing ? -1e30f : product.hi, low = nothing ? 0.f : product.lo, sum = none ? 1.f : all.y;
     const int bits = __float_as_int(sum), e = (bits - 0x3f400000) >> 23;
     const float m = __int_as_float(bits - (e << 23)) + (sum - sum), m_inverse = inverse_of(m);   // within 0.75 .. 1.5; NaN stays NaN
     // q = m 2^(hi + lo)
     const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -1e30f : d.hi, (float)e);
-    const float hi = t.hi, lo = d.lo + t.lo - low + kPowerShort * kLog2e;
+    const float hi = t.hi, lo = fmaf(d.hi, k2.rest, d.lo + t.lo - low + kPowerShort * kLog2e);
     const bool less = hi <= 0.f;
     const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, (less ? lo : -lo) * kLn2, power) * (less ? m : m_inverse);   // q, or 1 / q
     const float inverse = inverse_of(1.f + u);
@@ -213,7 +226,7 @@ struct RowsArgs {
     int vocab, pieces, cluster;    // columns of a row; its pieces, which the CTAs of a cluster share
     const void* y;
     bool wide;                     // y in 64 bits
-    float k2;                      // scale log2(e)
+    Powers k2;                     // scale log2(e)
     float* logp;
     const float *old_logp, *advantage, *ref_logp, *weight;
     float low, high, kl_coef, even_weight, grad_scale;   // grad_scale: times scale
@@ -382,8 +395,8 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 }
                 most.take(raw[i]);
             }
-            const float top = largest_of(most.value(), g.k2), base = top == minus_inf() ? 0.f : top;
-            const uint64_t k22 = pair_of(g.k2, g.k2), base2 = pair_of(-base, -base);
+            const float top = largest_of(most.value(), g.k2.hi), base = top == minus_inf() ? 0.f : top;
+            const uint64_t k22 = pair_of(g.k2.hi, g.k2.hi), base2 = pair_of(-base, -base);
             uint64_t e[P * N / 2], sum2[2] = {0ull, 0ull};
             // a piece's registers take the next row's as soon as its powers are formed
 #pragma unroll
@@ -484,7 +497,8 @@ struct ScoreArgs {
     int cluster;
     const void* y;
     bool wide;
-    float k2, scale;
+    Powers k2;
+    float scale;
     bool all_rows;                 // those without a chosen token too, for their lse
     float *logp, *lse;             // either may be NULL
     double* logp64;                // the same before its rounding, for sums over sequences; or NULL
@@ -520,7 +534,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     const int chosen_piece = at >= 0 && at < cols && at / N % GROUP == member ? at / N * N : -1;
     float top = minus_inf();
     uint64_t sum2[2] = {0ull, 0ull};
-    const uint64_t k22 = pair_of(g.k2, g.k2);
+    const uint64_t k22 = pair_of(g.k2.hi, g.k2.hi), low2 = pair_of(g.k2.lo, g.k2.lo);
     for (int c0 = member * N; c0 < cols; c0 += GROUP * kScorePieces * N) {
         uint4 raw[kScorePieces];
 #pragma unroll
@@ -537,7 +551,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         }
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
-        const float here = largest_of(most.value(), g.k2);
+        const float here = largest_of(most.value(), g.k2.hi);
         if (here > top) {
             const float less = factor_of(top - here);
             const uint64_t less2 = pair_of(less, less);
@@ -553,7 +567,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
             Piece<T>::split(raw[i], f);
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) {
-                const uint64_t x = fma2(f[j], k22, base2);
+                const uint64_t x = fma2(f[j], low2, fma2(f[j], k22, base2));
                 sum2[j & 1] = add2(sum2[j & 1], pair_of(exp2_fast(pair_lo(x)), exp2_fast(pair_hi(x))));
             }
         }
@@ -582,7 +596,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if (g.logp64) g.logp64[row] = logp;
         if (g.lse) {
             double lse = (double)zy * (double)g.scale - logp;
-            if (!there || is_nothing(zy * g.k2)) {              // the others' alone
+            if (!there || is_nothing(zy * g.k2.hi)) {              // the others' alone
                 float exponent, rest;
                 split_log2(all.y, exponent, rest);
                 lse = all.x == minus_inf() && all.y == 0.f ? (double)minus_inf() : (wide(sum_of(all.x, exponent)) + (double)rest) * 0.69314718055994531;
@@ -848,13 +862,23 @@ detox_status backward_of(BackArgs g, cudaStream_t s) {
 }  // namespace
 
 namespace {
+// For powers that have both parts, lo is above 0, so that -Inf stays -Inf through both products.  (8192 x 32000 bf16, policy loss: a second product for each entry takes 202 us
+// instead of 182.  There the entries have hi alone, and only their common base both: what is left is lo times their distance from the largest, at most 10^-7 of the sum.)
+Powers powers_of(float scale, bool both) {
+    const double k = (double)scale * 1.4426950408889634;
+    float hi = (float)k;
+    if (both && (double)hi >= k) hi = nextafterf(hi, 0.f);
+    const float lo = (float)(k - (double)hi), least = 1.4e-45f;
+    if (!both) return Powers{hi, 0.f, lo / hi};
+    return Powers{hi > least ? hi : least, lo > least ? lo : least, 0.f};
+}
 detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, bool all_rows,
                            float* logp, double* logp64, float* lse, float* zeros, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
     ScoreArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
-    g.k2 = scale * kLog2e;
+    g.k2 = powers_of(scale, true);
     g.scale = scale;
     g.all_rows = all_rows;
     g.logp = logp; g.logp64 = logp64; g.lse = lse; g.zeros = zeros;
@@ -903,7 +927,7 @@ detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float*
         RowsArgs g = {};
         g.Z = d.Z; g.ldz = d.ldz; g.rows = d.rows; g.vocab = (int)d.vocab;
         g.y = d.y; g.wide = d.index == DETOX_INDEX_INT64;
-        g.k2 = d.scale * kLog2e;
+        g.k2 = powers_of(d.scale, false);
         g.logp = logp;
         g.old_logp = d.old_logp; g.advantage = d.advantage; g.ref_logp = d.ref_logp; g.weight = d.weight;
         g.low = 1.f - d.clip_low; g.high = 1.f + d.clip_high;
