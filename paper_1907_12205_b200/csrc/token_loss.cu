@@ -33,13 +33,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// ex2.approx comes out 5.1e-8 of itself too small on average (2^20 arguments in (-1, 0]; at most 1.4e-7).  Over the sums of a sequence's log-probabilities that adds up, so
-// where these are formed it is put right: for the sums of powers at the end, and here for the factors between sums.
-constexpr float kPowerShort = 5.1e-8f;
-__device__ __forceinline__ float factor_of(float x) {
-    const float y = exp2_fast(x);
-    return fmaf(y, kPowerShort, y);
-}
+// ex2.approx is off by up to 1.4e-7 of itself, and comes out 5.0e-8 too small on average (2^20 arguments in each of (-24, -23] .. (-2, -1]: 4.9e-8 to 5.1e-8; in (-1, 0] 4.0e-8).
+// Over the sums of a sequence's log-probabilities that adds up, so it is put right in the logarithm of a sum.  (As a factor of the sum it would be a unit of its last
+// place or nothing.)  Powers are taken relative to whole numbers: the factors between sums are then powers of two, which have no error.
+constexpr float kPowerShort = 5.0e-8f;
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
 
 // ---- clusters -------------------------------------------------------------------------------------
@@ -62,11 +59,11 @@ __device__ __forceinline__ void store_at(const float2* here, uint32_t rank, floa
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
 }
 
-// (largest x, sum of 2^(x - largest)) of two sets; the empty set is (-Inf, 0)
+// (base, sum of 2^(x - base)) of two sets, the base no less than the largest x; the empty set is (-Inf, 0)
 __device__ __forceinline__ float2 joined(float2 a, float2 b) {
     const float m = a.x > b.x ? a.x : b.x;   // (NaN sums stay NaN whatever m is)
     const float m0 = m == minus_inf() ? 0.f : m;
-    return make_float2(m, a.y * factor_of(a.x - m0) + b.y * factor_of(b.x - m0));
+    return make_float2(m, a.y * exp2_fast(a.x - m0) + b.y * exp2_fast(b.x - m0));
 }
 
 __device__ __forceinline__ float warp_largest(float v) {
@@ -82,7 +79,7 @@ __device__ __forceinline__ float warp_total(float v) {
 // the pairs of a warp's lanes as one, in all lanes
 __device__ __forceinline__ float2 joined_warp(float2 a) {
     const float m = warp_largest(a.x), m0 = m == minus_inf() ? 0.f : m;
-    return make_float2(m, warp_total(a.y * factor_of(a.x - m0)));
+    return make_float2(m, warp_total(a.y * exp2_fast(a.x - m0)));
 }
 
 // 16 bytes, or what was there before; issued where it is written
@@ -133,7 +130,7 @@ __device__ __forceinline__ void split_log2(float sum, float& exponent, float& re
     exponent = (float)e;
     rest = log2f(__int_as_float(bits - (e << 23))) + (sum - sum);   // (NaN stays NaN)
 }
-// x of the largest entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
+// x of an entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
 __device__ __forceinline__ bool is_nothing(float x) { return x < -1.2676506e30f; }
 
 // The chosen token's log-probability, from its logit zy (NaN where there is no such token) and the sum of the others' powers of 2^(x - base).  What is below 2^-126 of the
@@ -148,9 +145,9 @@ __device__ __forceinline__ Two logp_of(float base, float sum, float zy, Powers k
     float exponent, mantissa;
     split_log2(sum, exponent, mantissa);
     const Two d = sum_of(base, -x.hi), t = sum_of(d.hi, exponent);
-    const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low) + d.hi * k2.rest;
+    const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low) + fmaf(d.hi, k2.rest, kPowerShort * kLog2e);
     const bool less = hi + lo <= 0.f;
-    const float l = log1pf(factor_of(less ? hi : -hi) * factor_of(less ? lo : -lo));   // of q, or of 1 / q: at most 1
+    const float u = exp2_fast(less ? hi : -hi) * exp2_fast(less ? lo : -lo), l = log1pf(fmaf(u, 2.f * kPowerShort, u));   // of q, or of 1 / q: at most 1
     const Two a = product_of(hi, kLn2);
     return less ? Two{-l, 0.f} : sum_of(-a.hi, -(a.lo + fmaf(hi, kLn2Rest, lo * kLn2) + l));
 }
@@ -193,7 +190,7 @@ __device__ __forceinline__ Chosen chosen_of(float2 all, float zy, Powers k2) {
     const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -1e30f : d.hi, (float)e);
     const float hi = t.hi, lo = fmaf(d.hi, k2.rest, d.lo + t.lo - low + kPowerShort * kLog2e);
     const bool less = hi <= 0.f;
-    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, (less ? lo : -lo) * kLn2, power) * (less ? m : m_inverse);   // q, or 1 / q
+    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, fmaf(less ? lo : -lo, kLn2, kPowerShort), power) * (less ? m : m_inverse);   // q, or 1 / q
     const float inverse = inverse_of(1.f + u);
     Chosen c;
     c.p = less ? inverse : inverse * m_inverse;
@@ -227,6 +224,7 @@ struct RowsArgs {
     const void* y;
     bool wide;                     // y in 64 bits
     Powers k2;                     // scale log2(e)
+    int32_t zero;                  // 0, which the compiler does not know
     float* logp;
     const float *old_logp, *advantage, *ref_logp, *weight;
     float low, high, kl_coef, even_weight, grad_scale;   // grad_scale: times scale
@@ -271,9 +269,10 @@ template <> struct Largest<__nv_bfloat16> {
     __device__ __forceinline__ float value() const { const float2 f = unpack2<__nv_bfloat16>(m); return fmaxf(f.x, f.y); }
     static constexpr uint32_t kNone = 0xff80ff80u;
 };
-__device__ __forceinline__ float largest_of(float z, float k2) {
+// what powers of entries up to z are taken relative to: the whole number from z's x on
+__device__ __forceinline__ float base_of(float z, float k2) {
     const float x = z * k2;
-    return is_nothing(x) ? minus_inf() : x;
+    return is_nothing(x) ? minus_inf() : ceilf(x);
 }
 // a piece of which only the first `n` entries are in the row: -Inf for the others
 template <typename T>
@@ -303,9 +302,10 @@ __device__ __forceinline__ uint4 hidden(uint4 v, uint4 m) {
     return make_uint4((v.x & ~m.x) | (none & m.x), (v.y & ~m.y) | (none & m.y), (v.z & ~m.z) | (none & m.z), (v.w & ~m.w) | (none & m.w));
 }
 // Registers: a thread holds P pieces of the next row (not AHEAD: of this one, and is done with them when it has the powers) and this row's
-// powers in fp32.  16 pieces of fp32 leave no room for both.
+// powers in fp32.  16 pieces of fp32 leave no room for both.  Beside them a row's numbers: with one or two pieces these decide (9000 x 300 bf16, one piece: 41.6 us with 32 for them, 37.5 with
+// 40; 20000 x 2050 at odd offsets, three: 140 and 157).
 template <typename T, int P> constexpr bool kAhead = P * Piece<T>::N + 4 * P <= 96;
-template <typename T, int P> constexpr int kRegisters = P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) + (sizeof(T) == 4 ? 48 : 32);
+template <typename T, int P> constexpr int kRegisters = P * Piece<T>::N + (kAhead<T, P> ? 4 * P : 0) + (sizeof(T) == 4 ? 48 : 32) + (P <= 2 ? 8 : 0);
 constexpr int between(int least, int most, int v) { return v < least ? least : (v > most ? most : v); }
 template <typename T, int THREADS, int P> constexpr int kCtas = between(1, 2048 / THREADS, 65536 / (THREADS * kRegisters<T, P>));
 
@@ -341,9 +341,9 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
         weight = g.weight ? g.weight[r] : g.even_weight;
         if (weight == 0.f) token = -1;
     };
-    auto fetch = [&](int i, const T* from, bool want) {
-        if constexpr (ANY) raw[i] = load_piece<true>(from, (int)(threadIdx.x + i * THREADS) * N, want ? cols : 0, g.span);
-        else load_if(raw[i], from + (threadIdx.x + i * THREADS) * N, want && there(i));
+    auto fetch = [&](int i, const T* from, bool want, int behind = 0) {
+        if constexpr (ANY) raw[i] = load_piece<true>(from, (int)(threadIdx.x + i * THREADS) * N + behind, want ? cols : 0, g.span);
+        else load_if(raw[i], from + ((int)(threadIdx.x + i * THREADS) * N + behind), want && there(i));
     };
     int64_t y, next_y;
     float w, next_w;
@@ -395,15 +395,15 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 }
                 most.take(raw[i]);
             }
-            const float top = largest_of(most.value(), g.k2.hi), base = top == minus_inf() ? 0.f : top;
+            const float top = base_of(most.value(), g.k2.hi), base = top == minus_inf() ? 0.f : top;
             const uint64_t k22 = pair_of(g.k2.hi, g.k2.hi), base2 = pair_of(-base, -base);
             uint64_t e[P * N / 2], sum2[2] = {0ull, 0ull};
-            // a piece's registers take the next row's as soon as its powers are formed
+            // A piece's registers take the next row's as soon as its powers are formed.  The address depends on one of these, so that the loads go out one by one: left free, the
+            // compiler unpacked all pieces first and asked for all of the next row at once in some builds, which holds up the load unit (8192 x 32000 bf16: 198 us, so 184).
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 uint64_t f[N / 2];
                 Piece<T>::split(raw[i], f);
-                if (AHEAD) fetch(i, there_next, next_y >= 0);
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) {
                     const uint64_t x = fma2(f[j], k22, base2);
@@ -411,6 +411,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                     sum2[j & 1] = add2(sum2[j & 1], v);
                     e[i * (N / 2) + j] = v;
                 }
+                if (AHEAD) fetch(i, there_next, next_y >= 0, (int)e[i * (N / 2)] & g.zero);
             }
             sum2[0] = add2(sum2[0], sum2[1]);
             float2 all = joined_warp(make_float2(top, pair_lo(sum2[0]) + pair_hi(sum2[0])));
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 if (g.kl_coef != 0.f) slope = fmaf(-g.kl_coef, up - 1.f, slope);   // (a term without weight may be infinite)
             }
             const float coef = token.empty ? 0.f : g.grad_scale * w * slope;
-            const float share = factor_of(top - (all.x == minus_inf() ? 0.f : all.x)) * token.share, factor = share == 0.f ? 0.f : -coef * share;
+            const float share = exp2_fast(top - (all.x == minus_inf() ? 0.f : all.x)) * token.share, factor = share == 0.f ? 0.f : -coef * share;
             if (g.dZ) {
                 const uint64_t factor2 = pair_of(factor, factor);
 #pragma unroll
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
                 if (mine && !token.empty) to[at] = from_f32<T>(coef * token.rest);
             }
             if (rank == 0 && threadIdx.x == kTeller) {
-                const Two logp = logp_of(all.x, fmaf(all.y, kPowerShort, all.y), zy, g.k2);
+                const Two logp = logp_of(all.x, all.y, zy, g.k2);
                 float kl = 0.f;
                 if (g.ref_logp) {
                     const Two d = sum_of(ref, -logp.hi);
@@ -551,9 +552,9 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         }
 #pragma unroll
         for (int i = 0; i < kScorePieces; ++i) most.take(raw[i]);
-        const float here = largest_of(most.value(), g.k2.hi);
+        const float here = base_of(most.value(), g.k2.hi);
         if (here > top) {
-            const float less = factor_of(top - here);
+            const float less = exp2_fast(top - here);
             const uint64_t less2 = pair_of(less, less);
             sum2[0] = mul2(sum2[0], less2);
             sum2[1] = mul2(sum2[1], less2);
@@ -590,18 +591,19 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         all = joined_warp(all);
     }
     if (first) {
-        all.y = fmaf(all.y, kPowerShort, all.y);
-        const double logp = y < 0 ? 0. : wide(logp_of(all.x, all.y, zy, g.k2));
-        if (g.logp) g.logp[row] = (float)logp;
-        if (g.logp64) g.logp64[row] = logp;
+        const Two lp = y < 0 ? Two{0.f, 0.f} : logp_of(all.x, all.y, zy, g.k2);
+        if (g.logp) g.logp[row] = lp.hi + lp.lo;
+        if (g.logp64) g.logp64[row] = wide(lp);
         if (g.lse) {
-            double lse = (double)zy * (double)g.scale - logp;
+            const Two own = product_of(zy, g.scale);
+            float lse = own.hi - lp.hi + (own.lo - lp.lo);
             if (!there || is_nothing(zy * g.k2.hi)) {              // the others' alone
                 float exponent, rest;
                 split_log2(all.y, exponent, rest);
-                lse = all.x == minus_inf() && all.y == 0.f ? (double)minus_inf() : (wide(sum_of(all.x, exponent)) + (double)rest) * 0.69314718055994531;
+                const Two t = sum_of(all.x, exponent), a = product_of(t.hi, kLn2);
+                lse = all.x == minus_inf() && all.y == 0.f ? minus_inf() : a.hi + (a.lo + fmaf(t.hi, kLn2Rest, (t.lo + rest + kPowerShort * kLog2e) * kLn2));
             }
-            g.lse[row] = (float)lse;
+            g.lse[row] = lse;
         }
     }
 }

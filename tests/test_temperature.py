@@ -31,6 +31,23 @@ def test_the_sums_of_long_sequences(dtype, scale):
     assert bool(((got.sums.double() - sums).abs() <= U * sums.abs() + n * 6e-8).all())
 
 
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_the_errors_of_powers_do_not_line_up(seed):
+    """bf16 logits are multiples of one step where they count, so the same arguments come up in every row.  A power's error has a mean within 1e-8 of what is put right; over some
+    twenty arguments that carry most of a sum it deviates by 1.4e-7 / sqrt(3) / sqrt(20) = 1.8e-8: two of those a token, and the margin's rounding."""
+    n, vocab, beta, scale = 2000, 32000, 0.5, 1.25
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    z = (2.5 * torch.randn((n + 1, vocab), generator=gen, device=DEV)).to(torch.bfloat16)
+    y = torch.randint(0, vocab, (n + 1,), generator=gen, device=DEV)
+    logp = torch.log_softmax(z.double() * scale, 1).gather(1, y[:, None])[:, 0]
+    sums = torch.stack([logp[:n].sum(), logp[n]])
+    ref = sums.float()
+    got = dx.detox_preference_loss(z, y, torch.tensor([0, n, n + 1], dtype=torch.int32, device=DEV), ref, beta=beta, scale=scale, want_grad=False)
+    gap = sums - ref.double()
+    want = beta * float(gap[0] - gap[1])
+    assert abs(float(got.margin[0]) - want) <= beta * (n + 1) * (1e-8 + 3.6e-8) + 2 * U * abs(want)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("scale", SCALES)
 @pytest.mark.parametrize("vocab", [200, 3001, 40000])
