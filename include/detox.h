@@ -484,8 +484,10 @@ detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, i
  *   y        dev, rows                 int32 or int64 (`index`)
  *   logp, lse, dlogp                   dev, rows, fp32; of logp and lse either may be NULL
  * detox_token_logp_backward: dZ[t][j] = scale dlogp[t] (1[j = y[t]] - exp(scale Z[t][j] - lse[t])), lse as detox_token_logp left it.  A row whose
- * dlogp is 0 is not read, and its gradient is zero.  lse being fp32, its probabilities are off by up to |lse| 2^-24 of themselves, here and in the
- * preference loss (logits of a few tens: 10^-6); the policy loss's are not.
+ * dlogp is 0 is not read, and its gradient is zero.  lse being fp32, its own rounding puts up to |lse| 2^-24 on every probability here (logits of a few tens: 10^-6), and
+ * 1 - p of a token that a row is sure of is a difference; the losses, which keep more of it, have neither.
+ * Precision: a row's sum is known to a few 2^-23 of itself; logp is -log(1 + q), q being the sum of the other tokens' probabilities over the chosen one's, so it is known
+ * to as much of itself near 0, and elsewhere to as much in absolute numbers, before it is rounded to fp32.  Probabilities below 2^-126 of a row's largest count as 0.
  * ------------------------------------------------------------------------------------------- */
 #define DETOX_LOGITS_MAX_COLS 262144
 detox_status detox_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,

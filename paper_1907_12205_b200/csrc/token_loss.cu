@@ -158,10 +158,15 @@ __device__ __forceinline__ float inverse_of(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return fmaf(fmaf(-x, y, 1.f), y, y);
 }
+// 2^lo - 1 for what a rounding has left (2^-9 at most where logits have some 10^4)
+__device__ __forceinline__ float little_power(float lo) {
+    const float t = lo * kLn2;
+    return fmaf(t, 0.5f * t, t);
+}
 // 2^(hi + lo); infinities of hi or of the result stay
 __device__ __forceinline__ float power_of(float hi, float lo) {
     const float y = exp2_fast(hi);
-    return fabsf(hi) < -minus_inf() ? fmaf(y < -minus_inf() ? y : 0.f, lo * kLn2, y) : y;
+    return fabsf(hi) < -minus_inf() ? fmaf(y < -minus_inf() ? y : 0.f, little_power(lo), y) : y;
 }
 // v log2(e)
 __device__ __forceinline__ Two in_powers(float v) {
@@ -188,9 +193,9 @@ __device__ __forceinline__ Chosen chosen_of(float2 all, float zy, Powers k2) {
     const float m = __int_as_float(bits - (e << 23)) + (sum - sum), m_inverse = inverse_of(m);   // within 0.75 .. 1.5; NaN stays NaN
     // q = m 2^(hi + lo)
     const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -1e30f : d.hi, (float)e);
-    const float hi = t.hi, lo = fmaf(d.hi, k2.rest, d.lo + t.lo - low + kPowerShort * kLog2e);
+    const float hi = t.hi, lo = fmaf(nothing ? 0.f : d.hi, k2.rest, d.lo + t.lo - low + kPowerShort * kLog2e);
     const bool less = hi <= 0.f;
-    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, fmaf(less ? lo : -lo, kLn2, kPowerShort), power) * (less ? m : m_inverse);   // q, or 1 / q
+    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, little_power(less ? lo : -lo) + kPowerShort, power) * (less ? m : m_inverse);   // q, or 1 / q
     const float inverse = inverse_of(1.f + u);
     Chosen c;
     c.p = less ? inverse : inverse * m_inverse;
@@ -503,8 +508,17 @@ struct ScoreArgs {
     bool all_rows;                 // those without a chosen token too, for their lse
     float *logp, *lse;             // either may be NULL
     double* logp64;                // the same before its rounding, for sums over sequences; or NULL
+    Two* base;                     // what the backward pass takes its powers relative to, see base_from; or NULL
+    Two per_lse;
     float* zeros;                  // a vector of `rows` zeros to write (the preference loss's gradients of logp), or NULL
 };
+
+// Powers of 2^(z hi - base) are probabilities times 2^(base's rest), with hi the temperature's first part and base = lse hi / scale (`per`: hi / scale): then what lo would add is in the
+// base as far as entries near lse have it, and an entry lacks lo times its distance from there.  Infinities and NaN have no rest.
+__device__ __forceinline__ Two base_from(Two lse, Two per) {
+    const Two p = product_of(lse.hi, per.hi);
+    return Two{p.hi, fabsf(p.hi) < -minus_inf() ? p.lo + fmaf(lse.hi, per.lo, lse.lo * per.hi) : 0.f};
+}
 
 template <typename T, int GROUP, bool ANY>
 __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_constant__ ScoreArgs g) {
@@ -594,16 +608,19 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         const Two lp = y < 0 ? Two{0.f, 0.f} : logp_of(all.x, all.y, zy, g.k2);
         if (g.logp) g.logp[row] = lp.hi + lp.lo;
         if (g.logp64) g.logp64[row] = wide(lp);
-        if (g.lse) {
+        if (g.lse || g.base) {
             const Two own = product_of(zy, g.scale);
-            float lse = own.hi - lp.hi + (own.lo - lp.lo);
+            Two lse = sum_of(own.hi, -lp.hi);
+            lse.lo += own.lo - lp.lo;
             if (!there || is_nothing(zy * g.k2.hi)) {              // the others' alone
                 float exponent, rest;
                 split_log2(all.y, exponent, rest);
                 const Two t = sum_of(all.x, exponent), a = product_of(t.hi, kLn2);
-                lse = all.x == minus_inf() && all.y == 0.f ? minus_inf() : a.hi + (a.lo + fmaf(t.hi, kLn2Rest, (t.lo + rest + kPowerShort * kLog2e) * kLn2));
+                const bool empty = all.x == minus_inf() && all.y == 0.f;
+                lse = empty ? Two{minus_inf(), 0.f} : Two{a.hi, a.lo + fmaf(t.hi, kLn2Rest, (t.lo + rest + kPowerShort * kLog2e) * kLn2)};
             }
-            g.lse[row] = lse;
+            if (g.lse) g.lse[row] = lse.hi + lse.lo;
+            if (g.base) g.base[row] = base_from(lse, g.per_lse);
         }
     }
 }
@@ -644,6 +661,9 @@ struct BackArgs {
     bool wide;
     float k2, scale;               // scale: of the logits and of the gradient
     const float *lse, *dlogp;
+    Two per_lse;
+    const Two* base;               // instead of lse: what a forward pass left, and
+    const double* logp;            // the chosen token's log-probability beside it
     void* dZ;
     int64_t lddz;
     bool dz_vec;
@@ -666,14 +686,14 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
         const int c0 = (int)(item - row * g.slices) * kSlice + lane * N;
         const int64_t y = chosen(g.y, g.wide, row);
         const float d = g.dlogp[row];
-        const float lse = g.lse[row];
-        const bool live = y >= 0 && d != 0.f && lse != minus_inf();
+        const Two base = g.base ? g.base[row] : base_from(Two{g.lse[row], 0.f}, g.per_lse);
+        const bool live = y >= 0 && d != 0.f && base.hi != minus_inf();
         const T* from = static_cast<const T*>(g.Z) + row * g.ldz;
         uint4 raw[kBackPieces];
 #pragma unroll
         for (int i = 0; i < kBackPieces; ++i) raw[i] = load_piece<ANY>(from, c0 + i * 32 * N, live ? g.vocab : 0, g.span);
         const float coef = y < g.vocab ? d * g.scale : __int_as_float(0x7fc00000);
-        const float base = -lse * kLog2e;
+        const float factor = -coef * exp2_fast(-base.lo);
         const int at = y < g.vocab ? (int)y : -1;
         T* to = static_cast<T*>(g.dZ) + row * g.lddz;
 #pragma unroll
@@ -684,10 +704,13 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
             Piece<T>::split(raw[i], f);
             if (live) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = exp2_fast(fmaf(f[j], g.k2, base)) * -coef;
+                for (int j = 0; j < N; ++j) f[j] = exp2_fast(fmaf(f[j], g.k2, -base.hi)) * factor;
                 if (at >= c && at < c + N) {
+                    // 1 - p from log p, where that is known: the difference has few bits left for a token that the row is sure of
+                    const float rest = g.logp ? -expm1f((float)g.logp[row]) : 0.f;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) f[j] += at == c + j ? coef : 0.f;
+                    for (int j = 0; j < N; ++j)
+                        if (at == c + j) f[j] = g.logp ? coef * rest : f[j] + coef;
                 }
             }
             store_entries(to, c, g.vocab, !ANY || g.dz_vec, f);
@@ -874,8 +897,12 @@ Powers powers_of(float scale, bool both) {
     if (!both) return Powers{hi, 0.f, lo / hi};
     return Powers{hi > least ? hi : least, lo > least ? lo : least, 0.f};
 }
+Two per_lse_of(float scale) {
+    const double per = (double)powers_of(scale, false).hi / (double)scale;
+    return Two{(float)per, (float)(per - (double)(float)per)};
+}
 detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, bool all_rows,
-                           float* logp, double* logp64, float* lse, float* zeros, cudaStream_t s) {
+                           float* logp, float* lse, double* logp64, Two* base, float* zeros, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
     ScoreArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
@@ -883,7 +910,8 @@ detox_status launch_scores(int dtype, const void* Z, int64_t ldz, int64_t rows, 
     g.k2 = powers_of(scale, true);
     g.scale = scale;
     g.all_rows = all_rows;
-    g.logp = logp; g.logp64 = logp64; g.lse = lse; g.zeros = zeros;
+    g.logp = logp; g.lse = lse; g.logp64 = logp64; g.base = base; g.zeros = zeros;
+    g.per_lse = per_lse_of(scale);
     if (dtype == DETOX_DTYPE_FLOAT) return score_of<float>(g, s);
     if (dtype == DETOX_DTYPE_HALF) return score_of<__half>(g, s);
     return score_of<__nv_bfloat16>(g, s);
@@ -893,14 +921,15 @@ detox_status backward_of(int dtype, const BackArgs& g, cudaStream_t s) {
     if (dtype == DETOX_DTYPE_HALF) return backward_of<__half>(g, s);
     return backward_of<__nv_bfloat16>(g, s);
 }
-BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, const float* lse,
-                   const float* dlogp, void* dZ, int64_t lddz) {
+BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale, const float* dlogp, void* dZ,
+                   int64_t lddz) {
     BackArgs g = {};
     g.Z = Z; g.ldz = ldz; g.rows = rows; g.vocab = (int)vocab;
     g.y = y; g.wide = index == DETOX_INDEX_INT64;
-    g.k2 = scale * kLog2e;
+    g.k2 = powers_of(scale, false).hi;
     g.scale = scale;
-    g.lse = lse; g.dlogp = dlogp;
+    g.per_lse = per_lse_of(scale);
+    g.dlogp = dlogp;
     g.dZ = dZ; g.lddz = lddz;
     return g;
 }
@@ -908,13 +937,15 @@ BackArgs back_args(const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int 
 
 detox_status launch_token_logp(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y, float scale,
                                float* logp, float* lse, cudaStream_t s) {
-    return launch_scores(dtype, Z, ldz, rows, vocab, index, y, scale, lse != nullptr, logp, nullptr, lse, nullptr, s);
+    return launch_scores(dtype, Z, ldz, rows, vocab, index, y, scale, lse != nullptr, logp, lse, nullptr, nullptr, nullptr, s);
 }
 
 detox_status launch_token_logp_backward(int dtype, const void* Z, int64_t ldz, int64_t rows, int64_t vocab, int index, const void* y,
                                         float scale, const float* lse, const float* dlogp, void* dZ, int64_t lddz, cudaStream_t s) {
     if (rows == 0) return DETOX_OK;
-    return backward_of(dtype, back_args(Z, ldz, rows, vocab, index, y, scale, lse, dlogp, dZ, lddz), s);
+    BackArgs g = back_args(Z, ldz, rows, vocab, index, y, scale, dlogp, dZ, lddz);
+    g.lse = lse;
+    return backward_of(dtype, g, s);
 }
 
 size_t policy_loss_ws_bytes(int64_t rows) {
@@ -947,18 +978,19 @@ detox_status launch_policy_loss(const detox_policy_desc& d, float* stats, float*
     return launch_chained(total_kernel<4>, 1, 32, 0, 1, s, parts, clusters, 1.0, stats);
 }
 
-// logp in 64 bits, lse and logp's gradient for each row, then a part of the loss for each pair
+// logp in 64 bits, the backward pass's base in two parts and logp's gradient for each row, then a part of the loss for each pair
 size_t preference_loss_ws_bytes(int64_t rows, int64_t pairs) {
-    return align_up((size_t)rows * sizeof(double)) + 2 * align_up((size_t)rows * sizeof(float)) + align_up((size_t)pairs * sizeof(double));
+    return 2 * align_up((size_t)rows * 8) + align_up((size_t)rows * sizeof(float)) + align_up((size_t)pairs * sizeof(double));
 }
 
 detox_status launch_preference_loss(const detox_preference_desc& d, float* loss, float* margin, float* sums, void* dZ, int64_t lddz, void* ws,
                                     cudaStream_t s) {
-    const size_t wide = align_up((size_t)d.rows * sizeof(double)), vector = align_up((size_t)d.rows * sizeof(float));
+    const size_t wide = align_up((size_t)d.rows * 8), vector = align_up((size_t)d.rows * sizeof(float));
     char* at = static_cast<char*>(ws);
-    double *logp = reinterpret_cast<double*>(at), *parts = reinterpret_cast<double*>(at + wide + 2 * vector);
-    float *lse = reinterpret_cast<float*>(at + wide), *dlogp = reinterpret_cast<float*>(at + wide + vector);
-    detox_status st = launch_scores(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, false, nullptr, logp, lse, dZ ? dlogp : nullptr, s);
+    double *logp = reinterpret_cast<double*>(at), *parts = reinterpret_cast<double*>(at + 2 * wide + vector);
+    Two* base = reinterpret_cast<Two*>(at + wide);
+    float* dlogp = reinterpret_cast<float*>(at + 2 * wide);
+    detox_status st = launch_scores(d.dtype, d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, false, nullptr, nullptr, logp, dZ ? base : nullptr, dZ ? dlogp : nullptr, s);
     if (st != DETOX_OK) return st;
     if (d.pairs > 0) {
         const int64_t most = (int64_t)kSMs * 8;
@@ -968,7 +1000,8 @@ detox_status launch_preference_loss(const detox_preference_desc& d, float* loss,
         if (st != DETOX_OK) return st;
     }
     if (dZ && d.rows > 0) {
-        BackArgs g = back_args(d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, lse, dlogp, dZ, lddz);
+        BackArgs g = back_args(d.Z, d.ldz, d.rows, d.vocab, d.index, d.y, d.scale, dlogp, dZ, lddz);
+        g.base = base; g.logp = logp;
         if (d.pairs > 0) {
             g.parts = parts; g.pairs = d.pairs; g.loss = loss;
         }
