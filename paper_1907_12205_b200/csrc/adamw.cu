@@ -351,9 +351,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) adamw_kernel(const __grid_con
     uint32_t step = number.step;
     if (number.lr_dev) lr = *number.lr_dev;
     if (number.step_dev) {
-        const int64_t t = *number.step_dev;
+        const int64_t there = *number.step_dev, t = there < 1 ? 1 : there;
         step = (uint32_t)t;
-        const float count = t < 1 ? 1.f : (float)t;
+        const float count = (float)t;
         // 1 - b^t = -(e^(t log b) - 1), without the difference's loss of bits (b = 0: log b = -Inf)
         c1 = 1.f / -expm1f(count * number.log_beta1);
         root_c2 = sqrtf(1.f / -expm1f(count * number.log_beta2));
