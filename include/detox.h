@@ -572,10 +572,14 @@ detox_status detox_preference_loss(const detox_preference_desc* desc, float* los
  *
  * tensors: host, `count` of them; read before the call returns.  No two buffers of a call may overlap, but P may be the master itself (FLOAT; give
  * it as P alone).  Entries are contiguous; any alignment to the entry's size works, 16 bytes (8 for 16-bit entries, 4 for 8-bit ones) is faster.
- * A tensor without entries is passed over.  eps > 0; beta1 and beta2 in [0, 1).  FLOAT weights take a gradient of any type and have no master;
+ * A tensor without entries is passed over.  eps >= DETOX_ADAMW_LEAST_EPS, in 8
+ * bits DETOX_ADAMW_LEAST_EPS_8 (fp32's squares end at 10^-45, and in 8 bits what is below 10^-38 counts as 0: beside a smaller eps a root would not be known, and eps itself
+ * could be 0 in fp32); beta1 and beta2 in [0, 1).  FLOAT weights take a gradient of any type and have no master;
  * HALF and BFLOAT ones take a gradient of their own type or FLOAT (else DETOX_ERR_UNSUPPORTED).  A tensor whose buffers are all off a 16-byte boundary by
  * the same number of entries, as slices of vectors of one layout are, is as fast as an aligned one (32 bits).  No workspace.
  * ------------------------------------------------------------------------------------------- */
+#define DETOX_ADAMW_LEAST_EPS 1e-18
+#define DETOX_ADAMW_LEAST_EPS_8 1e-15
 typedef struct {
     void* P;                     /* dev, n: the weights */
     const void* G;               /* dev, n: the gradient */

@@ -863,7 +863,7 @@ def detox_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m
     """One AdamW step over all tensors, in place.  step counts from 1; step and lr may be CUDA tensors of one int64 and one float32, which the
     step reads when it runs (so a captured one can be replayed).  m, v: as detox_adamw_state makes them; in 8 bits v holds the root, and both
     are rounded at random with bits that follow from seed, step, a tensor's place in the list and the entry.  weight_decay: a number, or one
-    for each tensor.  masters: float32 copies of the params (or None for some), which then are what is stepped."""
+    for each tensor.  masters: float32 copies of the params (or None for some), which then are what is stepped.  eps: at least 1e-18, with 8-bit states 1e-15."""
     (_worker_module or _worker()).adamw(params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, masters, grad_scale, seed,
                                         _handle(stream))
 

@@ -78,11 +78,14 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return mix_rest(x ^ (x >> 16));
 }
 
-// The root and the inverse to a unit or so, an instruction each (sqrtf and a division cost some eight an entry).  Numbers below 2^-126 count as 0: as v they
-// are squares that fp32 has lost most bits of already.
+// The root and the inverse to a unit or so, an instruction each (sqrtf and a division cost some eight an entry).  In 32 bits the root of v below 2^-126 is taken, too, since beside the
+// least eps it counts.  In 8 bits such v count as 0: the three instructions that it takes would cost a tenth (169 M entries 597 -> 653 us), and the least eps is larger for it.  What
+// the inverse is taken of is no less than eps.
+template <bool SMALL>
 __device__ __forceinline__ float root_of(float x) {
     float y;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    if constexpr (SMALL) asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float inverse_of(float x) {
@@ -297,7 +300,7 @@ __device__ __forceinline__ void step_part(const Tensor& t, int64_t at, const Num
             const uint64_t x = mul2(pairs_at(g[b], k), number.grad_scale);
             m[k] = fma2(number.beta1, m[k], mul2(number.rest1, x));
             v[k] = fma2(number.beta2, v[k], mul2(number.rest2, mul2(x, x)));
-            root[k] = pair_of(root_of(pair_lo(v[k])), root_of(pair_hi(v[k])));
+            root[k] = pair_of(root_of<!EIGHT>(pair_lo(v[k])), root_of<!EIGHT>(pair_hi(v[k])));
             const uint64_t below = fma2(root[k], both(now.root_c2), number.eps);
             const uint64_t way = mul2(mul2(m[k], both(now.c1)), pair_of(inverse_of(pair_lo(below)), inverse_of(pair_hi(below))));
             const uint64_t was = pairs_at(p[b], k), is = fma2(both(-now.lr), fma2(both(t.weight_decay), was, way), was);

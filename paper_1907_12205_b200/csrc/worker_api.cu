@@ -241,7 +241,7 @@ detox_status detox_preference_loss(const detox_preference_desc* d, float* loss, 
 
 detox_status detox_adamw(const detox_adamw_desc* d, const detox_adamw_tensor* tensors, int64_t count, void* stream) {
     if (!d || count < 0 || (count > 0 && !tensors) || (d->bits != 32 && d->bits != 8)) return DETOX_ERR_BAD_ARG;
-    if (!(d->lr_dev || std::isfinite(d->lr)) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !(d->eps > 0.) ||
+    if (!(d->lr_dev || std::isfinite(d->lr)) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !(d->eps >= (d->bits == 8 ? DETOX_ADAMW_LEAST_EPS_8 : DETOX_ADAMW_LEAST_EPS)) ||
         !std::isfinite(d->eps) || !finite(d->grad_scale) || (!d->step_dev && d->step < 1) || !aligned_to(d->lr_dev, 4) || !aligned_to(d->step_dev, 8))
         return DETOX_ERR_BAD_ARG;
     for (int64_t i = 0; i < count; ++i) {
