@@ -717,11 +717,13 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
         std::vector<const void*> stepped;
         for (const detox_adamw_tensor& t : of) {
             if (t.n == 0) continue;
-            for (const void* p : {(const void*)t.P, (const void*)t.master, (const void*)t.M, (const void*)t.V})
+            for (const void* p : {(const void*)t.P, (const void*)t.master, (const void*)t.M, (const void*)t.V, (const void*)t.ME, (const void*)t.VE})
                 if (p) stepped.push_back(p);
         }
         std::sort(stepped.begin(), stepped.end());
         if (std::adjacent_find(stepped.begin(), stepped.end()) != stepped.end()) raise(PyExc_ValueError, "params, masters, m, v: a tensor is there twice");
+        for (const detox_adamw_tensor& t : of)
+            if (t.n != 0 && std::binary_search(stepped.begin(), stepped.end(), t.G)) raise(PyExc_ValueError, "grads: a tensor is there that is stepped, too");
         const OnStream on(a[13], like);
         check(detox_adamw(&d, of.data(), (int64_t)of.size(), on.s), "detox_adamw");
         // graphs that saved the weights learn that they have changed

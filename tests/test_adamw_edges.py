@@ -76,3 +76,19 @@ def test_an_eps_that_is_too_small_is_refused():
     dx.detox_adamw([p], [p + 1], m8, v8, 1, 0.0, eps=1e-15)
     dx.detox_adamw([p], [p + 1], m, v, 1, 0.1, eps=1e-18)
     assert bool(((p + 0.1).abs() <= 1e-6).all())
+
+
+def test_what_is_stepped_twice_or_read_as_a_gradient_is_refused():
+    new = lambda: torch.zeros(300, device=DEV)  # noqa: E731
+    p, q, g = new(), new(), new() + 1
+    m, v = dx.detox_adamw_state([p, q], 8)
+    dx.detox_adamw([p, q], [g, g], m, v, 1, 0.1)                         # one gradient for both is fine
+    for bad_m, bad_v in (([m[0], (m[1][0], m[0][1])], v), (m, [v[0], (v[1][0], v[0][1])]), (m, [(v[0][0], m[0][1]), v[1]])):
+        with pytest.raises(ValueError, match="twice"):
+            dx.detox_adamw([p, q], [g, g], bad_m, bad_v, 1, 0.1)
+    m, v = dx.detox_adamw_state([p, q])
+    for grads in ([g, p], [q, g], [g, m[0]], [v[1], g]):
+        with pytest.raises(ValueError, match="stepped"):
+            dx.detox_adamw([p, q], grads, m, v, 1, 0.1)
+    empty = torch.empty(0, device=DEV)
+    dx.detox_adamw([p, empty], [g, empty], [m[0], empty], [v[0], empty], 1, 0.1)
