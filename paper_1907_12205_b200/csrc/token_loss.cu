@@ -781,13 +781,16 @@ constexpr int kLeastChunk = 2048;
 // pieces of a thread with the next row's beside them: eight of 16 bits, twelve of fp32
 template <typename T> constexpr int kMostPieces = 96 / (Piece<T>::N + 4);
 template <typename T>
-int cluster_of(int64_t rows, int64_t vocab) {
+int cluster_of(int64_t rows, int64_t vocab, bool aligned) {
     int64_t cluster = 1;                                       // 1, 2, 4 or 8
     while (cluster < kMaxCluster && vocab > cluster * 512 * kMostPieces<T> * Piece<T>::N) cluster *= 2;   // (fp32 beyond eight: sixteen pieces a thread)
     while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= kSMs && vocab >= cluster * 2 * kLeastChunk) cluster *= 2;
-    // Where a few rows would need a second turn of large CTAs, smaller ones, several to an SM, wait less (77 rows of 50257 fp16: 18.5 -> 16.5 us, of 50264 bf16:
-    // 14.4 -> 12.4; rows of one CTA each stay: 150 of 32000 take 10.6 us, with clusters of four 13.3).
-    if (cluster > 1 && cluster < kMaxCluster && rows * cluster > kSMs && rows * cluster < 2 * kSMs) cluster *= 2;
+    // Where a few rows would need a second turn of large CTAs, smaller ones, several to an SM, wait less.  Eight instead of four CTAs, 38 to 73 rows of bf16: 65544 columns
+    // 14.3 -> 12.4 us (73: 18.5 -> 17.8), 100000 16.2 -> 14.5 (22.7 -> 21.2), 131072 16.5 -> 16.0 (24.5 -> 21.7).  Four instead of two pay only for rows that no vector load
+    // fits, and for few: 75 and 90 of 50257 36.3 -> 33.3 and 39.0 -> 37.3, 110 40.8 -> 40.6, 147 44.1 -> 59.7; aligned 75 of 40000 and 50264 12.4 -> 12.9 and 14.4 -> 14.4, 147 13.5 ->
+    // 18.5 and 14.4 -> 20.5.  (Rows of one CTA each stay: 150 of 32000 take 10.6 us, with clusters of four 13.3.)
+    const int64_t ctas = rows * cluster;
+    if (ctas > kSMs && ((cluster == 4 && ctas < 2 * kSMs) || (cluster == 2 && !aligned && 4 * ctas <= 5 * kSMs))) cluster *= 2;
     return (int)cluster;
 }
 // Calls f<THREADS, P>() for CTAs of `pieces` pieces: P is what a thread has, and the CTA the smallest of which that is at most eight (of 512 threads: kMostPieces), four in
@@ -848,12 +851,13 @@ bool pieces(const void* p, int64_t ld) {
 // clusters: how many parts the loss has
 template <typename T>
 detox_status policy_of(RowsArgs g, int64_t* clusters, cudaStream_t s) {
-    g.cluster = cluster_of<T>(g.rows, g.vocab);
     g.pieces = (int)ceil_div((int64_t)g.vocab, (int64_t)Piece<T>::N);
     g.span = span_of<T>(g.Z, g.ldz, g.rows, g.vocab);
     g.dz_vec = pieces<T>(g.dZ, g.lddz);
+    const bool aligned = g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec);
+    g.cluster = cluster_of<T>(g.rows, g.vocab, aligned);
     const int most = (int)ceil_div((int64_t)g.pieces, (int64_t)g.cluster);
-    if (g.vocab % Piece<T>::N == 0 && g.span.vec && (!g.dZ || g.dz_vec) && most <= 512 * kMostPieces<T>) return by_pieces<T, false>(most, Policy<T, false>{g, clusters, s});
+    if (aligned && most <= 512 * kMostPieces<T>) return by_pieces<T, false>(most, Policy<T, false>{g, clusters, s});
     return by_pieces<T, true>(most, Policy<T, true>{g, clusters, s});
 }
 
