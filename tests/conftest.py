@@ -1,3 +1,4 @@
+import inspect
 import os
 import sys
 
@@ -32,3 +33,21 @@ def pytest_collection_modifyitems(config, items):
     for it in items:
         if "gpu" in it.keywords:
             it.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def memory_for_side_streams(request):
+    """For tests that look whether a side stream is still busy when a call returns: memory that this process has already, for every stream that they can be given.  A call that
+    had to get it from the driver took 20 to 45 ms now and then on machines shared with others, of the 50 that such a stream is kept busy."""
+    function = getattr(request, "function", None)
+    if function is None or "side.query()" not in inspect.getsource(function):
+        yield
+        return
+    import torch
+    if torch.cuda.is_available():
+        for _ in range(32):                        # torch hands out 32 streams in turn
+            with torch.cuda.stream(torch.cuda.Stream()):
+                held = [torch.empty(n, dtype=torch.uint8, device="cuda:0") for n in (1 << 27, 1 << 19, 1 << 19, 1 << 12)]
+                del held
+        torch.cuda.synchronize()
+    yield
