@@ -13,7 +13,8 @@
 // 8 bits: m and sqrt(v) as e4m3 numbers with a power-of-two scale for each block.  Of v the root is kept, since its range is half as
 // wide (v's would leave the form's 18 binary orders).  Rounding is random: added to the bits that the form drops, 16 random ones round up or down with
 // the right mean; a sum of thousands of steps that each change an entry by less than its spacing keeps its mean that way.
-// 169 M entries in 13 tensors: 600 to 640 us, 4.9 TB/s (floor 467); the rounding's instructions are what it spends beside it (484 without them).
+// 169 M entries in 13 tensors: 597 to 645 us by machine, 4.7 to 5.1 TB/s (floor 467); the rounding's instructions are what it spends beside it (484 without them).  Slices that start off a
+// boundary go byte by byte: 48 M entries in 12 tensors 180 us aligned, 305 otherwise.
 #include <cmath>
 #include <cstring>
 

@@ -1,6 +1,6 @@
 // Token embedding: rows of a table, scaled, and the table's gradient.
 //
-// Lookup:    Y[t] = scale W[tokens[t]].  Bound by HBM; a warp takes 4 pieces of 16 bytes a lane of one row.  8192 x 4096 bf16 of 32000 rows: 14 us.
+// Lookup:    Y[t] = scale W[tokens[t]].  Bound by HBM; a warp takes 4 pieces of 16 bytes a lane of one row.  8192 x 4096 bf16 of 32000 rows: 16.7 us.
 //
 // Gradient:  dW[v] = scale sum of dY[t] over the rows t with tokens[t] = v.  Bound by HBM too (rows of dY read once, rows of dW
 // written once), if the work is shared out evenly: tokens are as unevenly spread as words are, and a padded batch or a
@@ -8,12 +8,12 @@
 //   1. sort_tokens: a stable counting sort in one launch, without communication between CTAs.  Each of 2^k CTAs owns every 2^k-th row of the
 //      vocabulary (neighbouring numbers are often equally frequent) and looks through all tokens, which lie in L2: it counts those of
 //      the CTAs before it (where its output starts) and, warp by warp, those of each of its rows; then it goes through them again and writes the
-//      row numbers in order.  The order of the tokens is that of their places: CTA by CTA, and in a CTA ascending.
+//      row numbers in order.  (So all CTAs read all tokens, twice: 6 us for 8192, but 330 of 711 us for a million of them into 32000 x 64.)  The order of the tokens is that of their places: CTA by CTA, and in a CTA ascending.
 //   2. sum_rows: the sorted tokens are cut into spans of equal length, whatever lies in them.  A warp has a span and a slice of the columns; it adds up
 //      rows in registers and writes dW whenever the token changes.  The sum of a token that lies in several spans goes to the
 //      workspace in parts, and the warp that leaves the last of them adds them, in the spans' order (a counter tells, so nobody waits).
 //      Other CTAs of the same launch write zeros to the rows of tokens that do not occur.
-// 8192 tokens, bf16, to 32000 x 2048 fp32: 61 us (floor 45): 6 of sorting, 50 of the second kernel at 5.8 TB/s.  Cut into spans of equal cost over tokens and rows of the table
+// 8192 tokens, bf16, to 32000 x 2048 fp32: 61 to 63 us (floor 45): 6 of sorting, 50 of the second kernel at 5.8 TB/s.  Cut into spans of equal cost over tokens and rows of the table
 // alike it took 123: adding is bound by latency, writing zeros by bandwidth, and a warp that does both in turn keeps neither busy.
 #include "worker.cuh"
 
@@ -63,7 +63,8 @@ constexpr int kSumWarps = 48;                  // warps of an SM that there are 
 // where there are few tokens.
 template <bool ADD> constexpr int kAhead = ADD ? 4 : 8;
 constexpr int kSortAhead = 8;
-constexpr int kManyTokens = 4096, kManyLength = 16;   // a frequent token of many has as many parts as spans, which one warp adds: fewer, longer ones
+constexpr int kManyTokens = 4096, kManyLength = 16;   // a frequent token of many has as many parts as spans, which one warp adds: fewer, longer ones (added to: 4097 x 64
+// 23.3 -> 19.8 us, 6000 x 512 28.6 -> 22.4, 16384 x 64 52.4 -> 34.3, 30000 x 192 74.8 -> 58.3; overwritten: 40.8 -> 39.9 to 77.1 -> 56.1)
 constexpr int kZeroPlaces = 32;                // places that a CTA looks after
 constexpr int kZeroCtas = 6;                   // CTAs of an SM that there should be for that
 

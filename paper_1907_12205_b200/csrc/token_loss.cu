@@ -6,13 +6,14 @@
 // All of it is bound by HBM: the logits are the largest matrix of a training step, and the least is to read them once and write their
 // gradient once.
 //
-//   policy_kernel    A cluster of 1 to 8 CTAs holds a row in registers.  Entries come in 16-byte pieces, each thread takes 2^(x - its own largest x), the
-//                    pairs (largest, sum) of all warps meet once a row (through distributed shared memory where there are several CTAs), and the
+//   policy_kernel    A cluster of 1 to 8 CTAs holds a row in registers.  Entries come in 16-byte pieces, each thread takes 2^(x - base), its base the next whole number
+//                    from its largest x on, the pairs (base, sum) of all warps meet once a row (through distributed shared memory where there are several CTAs), and the
 //                    gradient is the kept powers times one number a thread.  So the logits are read once, one power is taken of each entry (the
 //                    special-function unit would be the bound with two), and a row has one barrier.  The next row's pieces are asked for as this
-//                    one's are used up.  8192 x 32000 bf16, a tenth of the rows without a token: 173 us, 5.8 TB/s (floor 152).
-//   score_kernel     Log-probabilities alone: a warp, a CTA or a cluster goes through a row with a running largest x and sum.  2048 x 128000 bf16:
-//                    84 us, 5.6 TB/s (floor 72); the special-function unit is at 64 %.  Through the kernel above it took 189.
+//                    one's are used up.  8192 x 32000 bf16, a tenth of the rows without a token: 180 to 189 us by machine, 5.3 to 5.5 TB/s (floor of what is read and written 152).  On clusters a full batch is far
+//                    from that: 2048 x 128000 464 us (floor 160), 4096 x 64000 264; one CTA an SM, and the CTAs of a row wait for one another.
+//   score_kernel     Log-probabilities alone: a warp, a CTA or a cluster goes through a row with a running base and sum.  2048 x 128000 bf16, all
+//                    rows read: 93 to 103 us by machine, 5.1 to 5.6 TB/s (floor 80); the special-function unit is at 66 %, issue slots at 59 %.
 //   backward_kernel  The gradient where lse is known: entry by entry.  The preference loss needs all of a pair's rows before any gradient, so it takes this
 //                    second pass; it goes through the rows backwards, since the last ones that were read still lie in L2.  5510 x 32000 bf16: 102 us.
 //   pairs_kernel     Sums over sequences, margins and the rows' gradients, a CTA a pair.
@@ -174,7 +175,7 @@ __device__ __forceinline__ Two in_powers(float v) {
     return Two{p.hi, p.lo + v * 1.92596299e-8f};               // log2 e - kLog2e
 }
 
-// What all threads need of a row for its gradient, from (largest x, sum of the others' powers of 2^(x - largest)).  With q = sum 2^(largest - x_y) the token has p = 1 / (1 + q).
+// What all threads need of a row for its gradient, from (base, sum of the others' powers of 2^(x - base)).  With q = sum 2^(base - x_y) the token has p = 1 / (1 + q).
 // The ratio p e^-old and e^ref / p are a power of two each, whose exponent is formed as hi + lo, without the logarithm of p: they are off by what the sum is off, a few
 // units of 2^-23, and by nothing of the size of the logarithms.  (The same in 64 bits would cost 16 warps' worth of them a row.)
 struct Chosen {
@@ -182,7 +183,7 @@ struct Chosen {
     float p_inverse;
     Two at;
     float rest;                    // 1 - p
-    float share;                   // times 2^(x_j - largest): p_j
+    float share;                   // times 2^(x_j - base): p_j
     bool empty;                    // nothing but -Inf
 };
 __device__ __forceinline__ Chosen chosen_of(float2 all, float zy, Powers k2) {
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
             }
             const float zy = y < g.vocab ? to_f32(Z[row * g.ldz + y]) : __int_as_float(0x7fc00000);
             const float old = g.old_logp[row], adv = g.advantage[row], ref = g.ref_logp ? g.ref_logp[row] : 0.f;
-            // The chosen entry, where one of this thread's pieces has it, becomes -Inf.  (8192 x 32000 bf16: 182 us, 179 with the entry left in.  Its power taken out of the sum
+            // The chosen entry, where one of this thread's pieces has it, becomes -Inf.  (8192 x 32000 bf16: 182 us, 179 with the entry left in, as it was then.  Its power taken out of the sum
             // again afterwards, in a branch that one warp enters, held the others up at the barrier: 185 to 190.)
             const int at = y < g.vocab ? (int)y - begin : -1;
             const bool mine = at >= 0 && at < cols && at / N % THREADS == (int)threadIdx.x;
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(THREADS, (kCtas<T, THREADS, P>)) policy_kernel
 }
 
 // ---- log-probabilities alone -------------------------------------------------------------------------
-// Nothing of a row has to stay: its threads go through it piece by piece with a running largest x and sum, and rows need no common
+// Nothing of a row has to stay: its threads go through it piece by piece with a running base and sum, and rows need no common
 // pace.  GROUP threads have a row, or a CTA of a cluster its part of one.
 constexpr int kScoreThreads = 256, kScorePieces = 4;
 
