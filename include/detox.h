@@ -475,8 +475,9 @@ detox_status detox_embedding_backward(int dtype, const void* dY, int64_t lddy, i
  *   - y[t] < 0: the row has no chosen token.  Its logp is 0, it takes no part in a loss, and its gradient is zero.  Its lse does not depend on
  *     the token and is that of any row; where lse is not asked for (NULL, the losses, the backward pass) the row is not read.
  *     y[t] >= vocab: logp is NaN (and with it the loss and the row's gradient).
- *   - Logits of -Inf, or below -2^100 where others are above (masked entries), have probability and gradient 0.  A row of nothing but such entries: lse,
- *     and with a chosen token logp, are -Inf, its gradient zero.
+ *   - Logits of -Inf, or with scale Z below -2^31 ln 2 = -1.49e9, have probability and gradient 0 (masked entries; fp32 tells larger numbers of this size apart by 64 at
+ *     best).  A row of nothing but such entries: lse, and with a chosen token logp, are -Inf, its gradient zero.  scale Z above
+ *     2^31 ln 2 is out of range.
  *   - vocab <= DETOX_LOGITS_MAX_COLS (a cluster of CTAs holds a row).
  *   - dZ may be Z itself (same base and stride).
  *

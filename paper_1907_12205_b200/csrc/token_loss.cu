@@ -131,8 +131,10 @@ __device__ __forceinline__ void split_log2(float sum, float& exponent, float& re
     exponent = (float)e;
     rest = log2f(__int_as_float(bits - (e << 23))) + (sum - sum);   // (NaN stays NaN)
 }
-// x of an entry.  Nothing above -2^100 is nothing: entries masked with the lowest number of their type, whose products leave fp32's range.
-__device__ __forceinline__ bool is_nothing(float x) { return x < -1.2676506e30f; }
+// x of an entry.  Below -2^31 it is nothing: entries masked with some number.  From there on a product's rounding, and with it the exponent of a power that should be near 1, may
+// be beyond 128 (masks of -10^10 or -10^20 made NaN of rows where a thread has no other entries), and the lowest numbers of bf16 and fp32 leave fp32's range.
+constexpr float kFar = 2147483648.f;
+__device__ __forceinline__ bool is_nothing(float x) { return x < -kFar; }
 
 // The chosen token's log-probability, from its logit zy (NaN where there is no such token) and the sum of the others' powers of 2^(x - base).  What is below 2^-126 of the
 // largest is nothing.
@@ -148,7 +150,8 @@ __device__ __forceinline__ Two logp_of(float base, float sum, float zy, Powers k
     const Two d = sum_of(base, -x.hi), t = sum_of(d.hi, exponent);
     const float hi = t.hi, lo = d.lo + t.lo + (mantissa - low) + fmaf(d.hi, k2.rest, kPowerShort * kLog2e);
     const bool less = hi + lo <= 0.f;
-    const float u = exp2_fast(less ? hi : -hi) * exp2_fast(less ? lo : -lo), l = log1pf(fmaf(u, 2.f * kPowerShort, u));   // of q, or of 1 / q: at most 1
+    // of q, or of 1 / q: at most 1.  (Of distances that leave nothing of it, as to entries masked with -10^9, lo is not small either.)
+    const float whole = exp2_fast(less ? hi : -hi), u = whole > 0.f ? whole * exp2_fast(less ? lo : -lo) : whole, l = log1pf(fmaf(u, 2.f * kPowerShort, u));
     const Two a = product_of(hi, kLn2);
     return less ? Two{-l, 0.f} : sum_of(-a.hi, -(a.lo + fmaf(hi, kLn2Rest, lo * kLn2) + l));
 }
@@ -159,15 +162,10 @@ __device__ __forceinline__ float inverse_of(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return fmaf(fmaf(-x, y, 1.f), y, y);
 }
-// 2^lo - 1 for what a rounding has left (2^-9 at most where logits have some 10^4)
-__device__ __forceinline__ float little_power(float lo) {
-    const float t = lo * kLn2;
-    return fmaf(t, 0.5f * t, t);
-}
-// 2^(hi + lo); infinities of hi or of the result stay
+// 2^(hi + lo), lo what a rounding of hi's size has left: its square is left out (10^-6 of the power where logits have some 10^4).  Infinities of hi or of the result stay
 __device__ __forceinline__ float power_of(float hi, float lo) {
     const float y = exp2_fast(hi);
-    return fabsf(hi) < -minus_inf() ? fmaf(y < -minus_inf() ? y : 0.f, little_power(lo), y) : y;
+    return fabsf(hi) < -minus_inf() ? fmaf(y < -minus_inf() ? y : 0.f, lo * kLn2, y) : y;
 }
 // v log2(e)
 __device__ __forceinline__ Two in_powers(float v) {
@@ -189,14 +187,15 @@ struct Chosen {
 __device__ __forceinline__ Chosen chosen_of(float2 all, float zy, Powers k2) {
     const Two product = product_of(zy, k2.hi);
     const bool nothing = is_nothing(product.hi), none = all.y < kLeast;
-    const float x = nothing ? -1e30f : product.hi, low = nothing ? 0.f : product.lo, sum = none ? 1.f : all.y;
+    const float x = nothing ? -2.f * kFar : product.hi, low = nothing ? 0.f : product.lo, sum = none ? 1.f : all.y;
     const int bits = __float_as_int(sum), e = (bits - 0x3f400000) >> 23;
     const float m = __int_as_float(bits - (e << 23)) + (sum - sum), m_inverse = inverse_of(m);   // within 0.75 .. 1.5; NaN stays NaN
     // q = m 2^(hi + lo)
-    const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -1e30f : d.hi, (float)e);
+    const Two d = sum_of(all.x == minus_inf() ? 0.f : all.x, -x), t = sum_of(none ? -2.f * kFar : d.hi, (float)e);
     const float hi = t.hi, lo = fmaf(nothing ? 0.f : d.hi, k2.rest, d.lo + t.lo - low + kPowerShort * kLog2e);
     const bool less = hi <= 0.f;
-    const float power = exp2_fast(less ? hi : -hi), u = fmaf(power, little_power(less ? lo : -lo) + kPowerShort, power) * (less ? m : m_inverse);   // q, or 1 / q
+    const float power = exp2_fast(less ? hi : -hi);
+    const float u = fmaf(power, fmaf(less ? lo : -lo, kLn2, kPowerShort), power) * (less ? m : m_inverse);   // q, or 1 / q
     const float inverse = inverse_of(1.f + u);
     Chosen c;
     c.p = less ? inverse : inverse * m_inverse;
